@@ -14,10 +14,12 @@ PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 INCLUDE = ROOT / "include"
 CSRC = PKG / "csrc"
-SOURCES = [CSRC / "cpdp.cu", CSRC / "cpdp_ragged.cu", CSRC / "cpdp_split.cu"]
+SOURCES = [CSRC / "cpdp.cu", CSRC / "cpdp_ragged.cu", CSRC / "cpdp_split.cu", CSRC / "cpdp_norm.cu",
+           CSRC / "cpdp_checkpoint.cu", CSRC / "cpdp_weight_gradient.cu", CSRC / "cpdp_recurrence.cu"]
 DEPENDS = SOURCES + [CSRC / "cpdp_kernels.cuh", CSRC / "cpdp_shapes.cuh", CSRC / "cpdp_tma.cuh",
                      CSRC / "cpdp_floor.cuh", CSRC / "cpdp_shuffle.cuh", CSRC / "cpdp_split.cuh",
-                     CSRC / "cpdp_launch.cuh", INCLUDE / "cpdp.h"]
+                     CSRC / "cpdp_launch.cuh", CSRC / "cpdp_layers.cuh", INCLUDE / "cpdp.h",
+                     INCLUDE / "cpdp_layers.h"]
 LIBRARY = PKG / "libcpdp.so"
 CHECKED_LIBRARY = PKG / "libcpdp_checked.so"  # debug build: kernels count out-of-range indices
 BUILD_DIR = ROOT / "_build"

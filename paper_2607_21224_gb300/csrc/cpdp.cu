@@ -8,6 +8,7 @@
 #include "cpdp_floor.cuh"
 #include "cpdp_kernels.cuh"
 #include "cpdp_launch.cuh"
+#include "cpdp_layers.cuh"
 #include "cpdp_shapes.cuh"
 #include "cpdp_shuffle.cuh"
 #include "cpdp_split.cuh"
@@ -424,6 +425,18 @@ bool finite_all(std::initializer_list<float> xs) {
 }
 
 }  // namespace
+
+// The layers' calls have no context.
+cpdp_status cpdp::layer_error(cpdp_status st, const char* fmt, ...) {
+    char msg[512];
+    va_list ap;
+    va_start(ap, fmt);
+    std::vsnprintf(msg, sizeof msg, fmt, ap);
+    va_end(ap);
+    return set_error(nullptr, st, "%s", msg);
+}
+
+cpdp_status cpdp::layer_launched(cudaError_t launched, const char* what) { return check_launch(nullptr, launched, what); }
 
 extern "C" {
 

@@ -1,0 +1,117 @@
+// What the files of the worker-batched layers (include/cpdp_layers.h) share:
+// argument checks, launches, and loads and stores of the two element types.
+#pragma once
+
+#include <cstdint>
+#include <cuda_runtime.h>
+#include <cuda_bf16.h>
+
+#include "cpdp_layers.h"
+
+namespace cpdp {
+
+// The message of a failed call that has no context (cpdp_last_error(NULL)); returns `st`.
+cpdp_status layer_error(cpdp_status st, const char* fmt, ...);
+// CPDP_OK, or CPDP_ECUDA with the launch's error (else one that the runtime recorded).
+cpdp_status layer_launched(cudaError_t launched, const char* what);
+
+constexpr int64_t kLayerMaxElements = int64_t(1) << 40;
+constexpr int64_t kLayerMaxRows = (int64_t(1) << 31) - 1;
+constexpr int kSMs = 152;
+constexpr int kBlock8 = 32;  // features that share an exponent
+
+__host__ __device__ constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline bool known_dtype(cpdp_dtype t) { return t == CPDP_F32 || t == CPDP_BF16; }
+inline int64_t dtype_size(cpdp_dtype t) { return t == CPDP_F32 ? 4 : 2; }
+inline bool aligned_to(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// W, M and D of an array [W][M][D].
+inline cpdp_status check_sizes(int W, int64_t M, int64_t D) {
+    if (W < 1 || W > 4096) return layer_error(CPDP_EINVAL, "W=%d must be in [1, 4096]", W);
+    if (M < 0 || D < 1) return layer_error(CPDP_EINVAL, "rows (%lld) must be >= 0 and features (%lld) >= 1", (long long)M, (long long)D);
+    if (M > kLayerMaxRows / W || (M > 0 && D > kLayerMaxElements / (W * M)))
+        return layer_error(CPDP_EINVAL, "W=%d, rows=%lld, features=%lld: W * rows is at most 2^31 - 1 and all elements at most 2^40",
+                           W, (long long)M, (long long)D);
+    return CPDP_OK;
+}
+
+// An array that the call needs (`wanted`: it has elements): not NULL, aligned to its element, strides >= 0.
+inline cpdp_status check_array(const char* name, const void* p, bool wanted, int64_t size, int64_t stride_a = 0,
+                               int64_t stride_b = 0) {
+    if (p == nullptr && wanted) return layer_error(CPDP_EINVAL, "%s is NULL", name);
+    if (!aligned_to(p, size)) return layer_error(CPDP_EALIGN, "%s %p is not aligned to its %d-byte elements", name, p, (int)size);
+    if (stride_a < 0 || stride_b < 0 || stride_a > kLayerMaxElements || stride_b > kLayerMaxElements)
+        return layer_error(CPDP_EINVAL, "%s: strides %lld and %lld must be in [0, 2^40]", name, (long long)stride_a, (long long)stride_b);
+    return CPDP_OK;
+}
+
+inline cpdp_status check_workspace(const void* p, size_t bytes, size_t needed) {
+    if (needed == 0) return CPDP_OK;
+    if (p == nullptr || bytes < needed)
+        return layer_error(CPDP_EINVAL, "workspace of %zu bytes: %zu are needed", p == nullptr ? size_t(0) : bytes, needed);
+    if (!aligned_to(p, 16)) return layer_error(CPDP_EALIGN, "workspace %p is not 16-byte aligned", p);
+    return CPDP_OK;
+}
+
+#define CPDP_TRY(call)                               \
+    do {                                             \
+        const cpdp_status try_st = (call);           \
+        if (try_st != CPDP_OK) return try_st;        \
+    } while (0)
+
+// Launch with programmatic dependent launch: the grid may begin while the one
+// before it on the stream drains, and every kernel waits for that one's
+// completion (layer_begin) before it touches memory.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_layer(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, void* stream, Args... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void layer_begin() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T from_float(float x);
+template <>
+__device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// The exponent byte of a block of 8-bit values whose largest magnitude is
+// `top`, given as its bits: e = the least with top <= 127 * 2^e. top = m * 2^k
+// with m in [1, 2), 127 = 1.984375 * 2^6, so e is k - 6 or, above 1.984375,
+// k - 5: an integer addition to the bits carries into the exponent exactly
+// there. 255 where top is infinite or NaN.
+__device__ __forceinline__ uint32_t exponent_byte(uint32_t top_bits) {
+    if (top_bits >= 0x7f800000u) return 255u;
+    const int k = static_cast<int>((top_bits + 0x0001ffffu) >> 23);  // k + 127, one more above 1.984375
+    return static_cast<uint32_t>(min(max(k - 6, 1), 248));
+}
+// 2^e and 2^-e of an exponent byte; NaN and 0 for 255.
+__device__ __forceinline__ float unit_of(uint32_t byte) { return __uint_as_float(byte == 255u ? 0x7fc00000u : byte << 23); }
+__device__ __forceinline__ float inverse_unit_of(uint32_t byte) {
+    return __uint_as_float(byte == 255u ? 0u : (254u - byte) << 23);
+}
+// The code of x in units of 1 / inverse (0 where x is not finite and the block reads back as NaN).
+__device__ __forceinline__ int code_of(float x, float inverse) {
+    return max(-127, min(127, __float2int_rn(x * inverse)));
+}
+#endif
+
+}  // namespace cpdp

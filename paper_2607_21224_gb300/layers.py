@@ -1,0 +1,413 @@
+"""Worker-batched layers on torch tensors: the operators declared in
+include/cpdp_layers.h, which make the gradients that ``CPDPState`` steps with.
+
+- ``add_rmsnorm`` / ``add_rmsnorm_backward``: residual addition and
+  root-mean-square norm, its output optionally held in 8 bits
+- ``checkpoint`` / ``restore`` / ``weight_gradient``: activations held in 8 bits
+  for the backward pass, and the weight gradient that reads them
+- ``gated_recurrence`` / ``gated_recurrence_backward`` /
+  ``gated_recurrence_step``: h_t = a_t h_(t-1) + (1 - a_t) v_t, a = sigmoid(gate)
+
+Activations are (W, M, D): W workers, M tokens each, D features, contiguous
+along D, float32 or bfloat16. One model's (M, D) is taken too, with a weight
+(D,). Weights are float32 and may be slices of ``CPDPState.params``, and weight
+gradients are written into slices of the [W][N] gradient buffer::
+
+    weight = st.params[:, a:a + D]                          # (W, D)
+    y, s, saved = layers.add_rmsnorm(x, weight, residual, checkpoint=True)
+    ...
+    layers.weight_gradient(dy, saved, out=grads[:, b:b + O * D].view(W, O, D))
+    dx, _ = layers.add_rmsnorm_backward(dy, s, weight, ds, dweight=grads[:, a:a + D])
+
+Calls run on the current stream of their tensors' device (or on ``stream``) and
+return without waiting. Outputs are allocated by torch; nothing is kept between
+calls. There is no autograd and no CPU implementation. A tensor that a call
+cannot take is refused with ValueError or TypeError, anything that the library
+refuses with ``CPDPError``.
+"""
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass
+
+import torch
+
+from . import cpdp as _c
+from .state import _raw_stream
+
+BLOCK = 32  # features that share an exponent
+CARRY_STEPS = 64  # CPDP_CARRY_STEPS
+NORM_MAX_FEATURES = 16384  # CPDP_NORM_MAX_FEATURES
+
+_P, _I, _L, _F, _Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+# Every entry point declared in include/cpdp_layers.h: (result, arguments).
+SIGNATURES = {
+    "cpdp_add_rmsnorm": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _I, _I, _L, _I, _F, _P, _P, _P, _P, _P]),
+    "cpdp_add_rmsnorm_backward_workspace": (_Z, [_I, _L, _I]),
+    "cpdp_add_rmsnorm_backward": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _L, _P, _L, _I, _I, _L, _I, _F, _P, _P, _L, _I, _P,
+                                       _Z, _P]),
+    "cpdp_checkpoint": (_I, [_P, _L, _L, _I, _I, _L, _I, _P, _P, _P, _P]),
+    "cpdp_restore": (_I, [_P, _P, _I, _L, _I, _P, _P]),
+    "cpdp_weight_gradient_workspace": (_Z, [_I, _L, _I, _I]),
+    "cpdp_weight_gradient": (_I, [_P, _L, _L, _I, _P, _P, _I, _L, _I, _I, _P, _L, _I, _P, _Z, _P]),
+    "cpdp_gated_recurrence_workspace": (_Z, [_I, _L, _I]),
+    "cpdp_gated_recurrence": (_I, [_P, _L, _L, _P, _L, _L, _I, _I, _L, _I, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "cpdp_gated_recurrence_backward": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _L, _I, _I, _L, _I, _P, _P, _P, _P, _P, _L, _L,
+                                            _P, _P, _Z, _P]),
+    "cpdp_gated_recurrence_step": (_I, [_P, _L, _P, _L, _I, _I, _I, _P, _P, _P]),
+}
+
+_lib = None
+
+
+def lib() -> ctypes.CDLL:
+    """libcpdp with the layers' entry points declared."""
+    global _lib
+    if _lib is None:
+        L = _c.lib()
+        for name, (result, arguments) in SIGNATURES.items():
+            f = getattr(L, name)
+            f.restype, f.argtypes = result, arguments
+        _lib = L
+    return _lib
+
+
+_CODES = {torch.float32: _c.CPDP_F32, torch.bfloat16: _c.CPDP_BF16}
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _check(status: int) -> None:
+    if status:
+        _c._check(status)
+
+
+def _stream(device: torch.device) -> int:
+    if _raw_stream is not None:
+        return _raw_stream(device.index)
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _on(device: torch.device, stream):
+    """The context in which a call's outputs are allocated and its kernels
+    launched, or None where that is the current one."""
+    if stream is None and device.index == torch.cuda.current_device():
+        return None
+    if stream is None:
+        return torch.cuda.device(device)
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device) if isinstance(stream, int) else stream)
+
+
+def _input(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype, device: torch.device) -> None:
+    """An input of this shape and type, contiguous along its last axis."""
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.stride(-1) != 1 and shape[-1] > 1:
+        raise ValueError(f"{name} must be contiguous along its last axis")
+
+
+def _cuda(t: torch.Tensor, name: str) -> torch.device:
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} is on {t.device}; the layers run on a CUDA device")
+    return t.device
+
+
+def _whole(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, device: torch.device) -> None:
+    if t is not None:
+        _input(t, name, shape, dtype, device)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+
+
+def _workspace(nbytes: int, device: torch.device) -> torch.Tensor | None:
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _ptr(t: torch.Tensor | None) -> int | None:
+    return None if t is None else t.data_ptr()
+
+
+@dataclass(frozen=True)
+class Checkpoint:
+    """Activations held in 8 bits: ``codes`` int8 (W, M, 32 * ceil(D / 32)),
+    ``exponents`` uint8 (W, M, ceil(D / 32)), and the number D of features.
+    A value is code * 2^(exponent - 127), exact in bfloat16."""
+    codes: torch.Tensor
+    exponents: torch.Tensor
+    features: int
+
+    @property
+    def nbytes(self) -> int:
+        return self.codes.numel() + self.exponents.numel()
+
+
+def _new_checkpoint(W: int, M: int, D: int, device: torch.device) -> Checkpoint:
+    blocks = -(-D // BLOCK)
+    return Checkpoint(torch.empty((W, M, blocks * BLOCK), dtype=torch.int8, device=device),
+                      torch.empty((W, M, blocks), dtype=torch.uint8, device=device), D)
+
+
+def _rows(x: torch.Tensor, weight: torch.Tensor, name: str) -> torch.device:
+    device = _cuda(x, name)
+    if x.dim() != 3:
+        raise ValueError(f"{name} must be (W, M, D), or (M, D) with a weight (D,); got {tuple(x.shape)}")
+    _input(weight, "weight", (x.shape[0], x.shape[2]), torch.float32, device)
+    return device
+
+
+def add_rmsnorm(x, weight, residual=None, *, eps: float = 1e-6, checkpoint: bool = False, stream=None):
+    """s = x + residual (rounded to x's type), y = weight * s / sqrt(mean(s^2) + eps).
+
+    Returns (y, s, saved). Without a residual s is x itself. With ``checkpoint``
+    y is held in 8 bits, ``saved`` is that Checkpoint and y is bfloat16, the
+    values that it stands for: the product that follows and its weight gradient
+    then see the same numbers. Else y has x's type and ``saved`` is None."""
+    if weight.dim() == 1 and x.dim() == 2:
+        y, s, saved = add_rmsnorm(x[None], weight[None], None if residual is None else residual[None], eps=eps,
+                                  checkpoint=checkpoint, stream=stream)
+        return y[0], x if residual is None else s[0], saved
+    device = _rows(x, weight, "x")
+    on = _on(device, stream)
+    if on is not None:
+        with on:
+            return add_rmsnorm(x, weight, residual, eps=eps, checkpoint=checkpoint)
+    W, M, D = x.shape
+    code = _dtype(x, "x")
+    _input(x, "x", (W, M, D), x.dtype, device)
+    s = x
+    if residual is not None:
+        _input(residual, "residual", (W, M, D), x.dtype, device)
+        s = torch.empty((W, M, D), dtype=x.dtype, device=device)
+    saved = _new_checkpoint(W, M, D, device) if checkpoint else None
+    y = torch.empty((W, M, D), dtype=torch.bfloat16 if checkpoint else x.dtype, device=device)
+    r = residual
+    _check(lib().cpdp_add_rmsnorm(
+        x.data_ptr(), x.stride(0), x.stride(1), _ptr(r), r.stride(0) if r is not None else 0,
+        r.stride(1) if r is not None else 0, weight.data_ptr(), weight.stride(0), code, W, M, D, eps, y.data_ptr(),
+        s.data_ptr() if r is not None else None, saved.codes.data_ptr() if saved else None,
+        saved.exponents.data_ptr() if saved else None, _stream(device)))
+    return y, s, saved
+
+
+def _gradient_out(out, name: str, shape: tuple, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    """The caller's slice of the gradient rows (each worker's part contiguous), or a new tensor."""
+    if out is None:
+        if dtype not in _CODES:
+            raise TypeError(f"{name} must be float32 or bfloat16, got {dtype}")
+        return torch.empty(shape, dtype=dtype, device=device)
+    _dtype(out, name)
+    if tuple(out.shape) != shape or out.device != device:
+        raise ValueError(f"{name} must have shape {shape} on {device}, got {tuple(out.shape)} on {out.device}")
+    if out.shape[0] > 0 and not out[0].is_contiguous():
+        raise ValueError(f"each worker's part of {name} must be contiguous")
+    return out
+
+
+def add_rmsnorm_backward(dy, s, weight, ds=None, *, eps: float = 1e-6, dweight=None, dtype=torch.float32, stream=None):
+    """Gradients of ``add_rmsnorm``: (dx, dweight). dy is the gradient of y and
+    s what the forward pass returned as s; ds, where given, is the gradient that
+    reaches s by other ways (the residual stream's) and is added to dx. dx is
+    the gradient of x and of the residual. dweight is written into the tensor
+    given, (W, D) float32 or bfloat16, or into a new one of ``dtype``."""
+    if weight.dim() == 1 and s.dim() == 2:
+        dx, dw = add_rmsnorm_backward(dy[None], s[None], weight[None], None if ds is None else ds[None], eps=eps,
+                                      dweight=None if dweight is None else dweight[None], dtype=dtype, stream=stream)
+        return dx[0], dw[0]
+    device = _rows(s, weight, "s")
+    on = _on(device, stream)
+    if on is not None:
+        with on:
+            return add_rmsnorm_backward(dy, s, weight, ds, eps=eps, dweight=dweight, dtype=dtype)
+    W, M, D = s.shape
+    code = _dtype(s, "s")
+    _input(s, "s", (W, M, D), s.dtype, device)
+    _input(dy, "dy", (W, M, D), s.dtype, device)
+    if ds is not None:
+        _input(ds, "ds", (W, M, D), s.dtype, device)
+    dweight = _gradient_out(dweight, "dweight", (W, D), dtype, device)
+    dx = torch.empty((W, M, D), dtype=s.dtype, device=device)
+    L = lib()
+    ws = _workspace(L.cpdp_add_rmsnorm_backward_workspace(W, M, D), device)
+    _check(L.cpdp_add_rmsnorm_backward(
+        dy.data_ptr(), dy.stride(0), dy.stride(1), s.data_ptr(), s.stride(0), s.stride(1), _ptr(ds),
+        ds.stride(0) if ds is not None else 0, ds.stride(1) if ds is not None else 0, weight.data_ptr(), weight.stride(0),
+        code, W, M, D, eps, dx.data_ptr(), dweight.data_ptr(), dweight.stride(0), _CODES[dweight.dtype], _ptr(ws),
+        ws.numel() if ws is not None else 0, _stream(device)))
+    return dx, dweight
+
+
+def checkpoint(x, *, values: bool = True, stream=None):
+    """x (W, M, D) held in 8 bits: (Checkpoint, the bfloat16 values that it
+    stands for). values=False: None in their place."""
+    if x.dim() == 2:
+        saved, held = checkpoint(x[None], values=values, stream=stream)
+        return saved, held[0] if values else None
+    device = _cuda(x, "x")
+    if x.dim() != 3:
+        raise ValueError(f"x must be (W, M, D) or (M, D), got {tuple(x.shape)}")
+    on = _on(device, stream)
+    if on is not None:
+        with on:
+            return checkpoint(x, values=values)
+    W, M, D = x.shape
+    code = _dtype(x, "x")
+    _input(x, "x", (W, M, D), x.dtype, device)
+    saved = _new_checkpoint(W, M, D, device)
+    held = torch.empty((W, M, D), dtype=torch.bfloat16, device=device) if values else None
+    _check(lib().cpdp_checkpoint(x.data_ptr(), x.stride(0), x.stride(1), code, W, M, D, saved.codes.data_ptr(),
+                                 saved.exponents.data_ptr(), _ptr(held), _stream(device)))
+    return saved, held
+
+
+def _saved(saved: Checkpoint) -> tuple[int, int, int]:
+    """(W, M, D) of a Checkpoint that the library can read."""
+    codes, exponents, D = saved.codes, saved.exponents, saved.features
+    blocks = -(-D // BLOCK)
+    device = _cuda(codes, "codes")
+    if codes.dim() != 3:
+        raise ValueError(f"codes must be (W, M, {blocks * BLOCK}), got {tuple(codes.shape)}")
+    W, M = codes.shape[:2]
+    _whole(codes, "codes", (W, M, blocks * BLOCK), torch.int8, device)
+    _whole(exponents, "exponents", (W, M, blocks), torch.uint8, device)
+    return W, M, D
+
+
+def restore(saved: Checkpoint, *, stream=None):
+    """The bfloat16 values (W, M, D) that a Checkpoint stands for."""
+    W, M, D = _saved(saved)
+    device = saved.codes.device
+    on = _on(device, stream)
+    if on is not None:
+        with on:
+            return restore(saved)
+    held = torch.empty((W, M, D), dtype=torch.bfloat16, device=device)
+    _check(lib().cpdp_restore(saved.codes.data_ptr(), saved.exponents.data_ptr(), W, M, D, held.data_ptr(), _stream(device)))
+    return held
+
+
+def weight_gradient(dy, saved: Checkpoint, *, out=None, dtype=torch.float32, stream=None):
+    """dW[w] = dy[w]^T x^[w] of a linear layer whose input the Checkpoint holds:
+    dy (W, M, O), x^ (W, M, I), dW (W, O, I), written into ``out`` (float32 or
+    bfloat16, e.g. a view of the gradient rows) or a new tensor of ``dtype``.
+    float32 dy is rounded to bfloat16, the type of the product's operands; the
+    sums are float32."""
+    if dy.dim() == 2:
+        return weight_gradient(dy[None], saved, out=None if out is None else out[None], dtype=dtype, stream=stream)[0]
+    W, M, D = _saved(saved)
+    device = saved.codes.device
+    on = _on(device, stream)
+    if on is not None:
+        with on:
+            return weight_gradient(dy, saved, out=out, dtype=dtype)
+    code = _dtype(dy, "dy")
+    if dy.dim() != 3:
+        raise ValueError(f"dy must be (W, M, O) or (M, O), got {tuple(dy.shape)}")
+    O = dy.shape[2]
+    _input(dy, "dy", (W, M, O), dy.dtype, device)
+    out = _gradient_out(out, "out", (W, O, D), dtype, device)
+    L = lib()
+    ws = _workspace(L.cpdp_weight_gradient_workspace(W, M, O, D), device)
+    _check(L.cpdp_weight_gradient(
+        dy.data_ptr(), dy.stride(0), dy.stride(1), code, saved.codes.data_ptr(), saved.exponents.data_ptr(), W, M, O, D,
+        out.data_ptr(), out.stride(0), _CODES[out.dtype], _ptr(ws), ws.numel() if ws is not None else 0, _stream(device)))
+    return out
+
+
+def _sequences(gate, value) -> torch.device:
+    device = _cuda(gate, "gate")
+    if gate.dim() != 3:
+        raise ValueError(f"gate must be (B, T, D), got {tuple(gate.shape)}")
+    _dtype(gate, "gate")
+    _input(gate, "gate", tuple(gate.shape), gate.dtype, device)
+    _input(value, "value", tuple(gate.shape), gate.dtype, device)
+    return device
+
+
+def gated_recurrence(gate, value, h0=None, lengths=None, *, carry: bool = True, stream=None):
+    """h_t = a_t h_(t-1) + (1 - a_t) v_t with a = sigmoid(gate), for B sequences.
+
+    gate, value (B, T, D) float32 or bfloat16 (two halves of one product's
+    output, say); h0 float32 (B, D) or None for zeros; lengths int32 (B,) or
+    None: beyond its length a sequence keeps its state and h is 0. Returns
+    (h, h_last, carry): h (B, T, D) of gate's type, h_last float32 (B, D), and
+    the states at every CARRY_STEPS steps, float32, which the backward pass
+    starts from (carry=False: None)."""
+    device = _sequences(gate, value)
+    on = _on(device, stream)
+    if on is not None:
+        with on:
+            return gated_recurrence(gate, value, h0, lengths, carry=carry)
+    B, T, D = gate.shape
+    _whole(h0, "h0", (B, D), torch.float32, device)
+    _whole(lengths, "lengths", (B,), torch.int32, device)
+    h = torch.empty((B, T, D), dtype=gate.dtype, device=device)
+    last = torch.empty((B, D), dtype=torch.float32, device=device)
+    carries = torch.empty((B, -(-T // CARRY_STEPS), D), dtype=torch.float32, device=device) if carry else None
+    L = lib()
+    ws = _workspace(L.cpdp_gated_recurrence_workspace(B, T, D), device)
+    _check(L.cpdp_gated_recurrence(
+        gate.data_ptr(), gate.stride(0), gate.stride(1), value.data_ptr(), value.stride(0), value.stride(1),
+        _CODES[gate.dtype], B, T, D, _ptr(h0), _ptr(lengths), h.data_ptr(), last.data_ptr(), _ptr(carries), _ptr(ws),
+        ws.numel() if ws is not None else 0, _stream(device)))
+    return h, last, carries
+
+
+def gated_recurrence_backward(dh, gate, value, carry, dh_last=None, lengths=None, *, out=None, stream=None):
+    """Gradients of ``gated_recurrence``: (dgate, dvalue, dh0) from dh (B, T, D)
+    and dh_last float32 (B, D) or None. dgate and dvalue are the halves of one
+    (B, T, 2 D) tensor, ``out`` where given (contiguous along its last axis):
+    the gradient of one product that made gate and value."""
+    device = _sequences(gate, value)
+    on = _on(device, stream)
+    if on is not None:
+        with on:
+            return gated_recurrence_backward(dh, gate, value, carry, dh_last, lengths, out=out)
+    B, T, D = gate.shape
+    _input(dh, "dh", (B, T, D), gate.dtype, device)
+    _whole(carry, "carry", (B, -(-T // CARRY_STEPS), D), torch.float32, device)
+    _whole(dh_last, "dh_last", (B, D), torch.float32, device)
+    _whole(lengths, "lengths", (B,), torch.int32, device)
+    if out is None:
+        out = torch.empty((B, T, 2 * D), dtype=gate.dtype, device=device)
+    else:
+        _input(out, "out", (B, T, 2 * D), gate.dtype, device)
+    dgate, dvalue = out[..., :D], out[..., D:]
+    dh0 = torch.empty((B, D), dtype=torch.float32, device=device)
+    L = lib()
+    ws = _workspace(L.cpdp_gated_recurrence_workspace(B, T, D), device)
+    _check(L.cpdp_gated_recurrence_backward(
+        dh.data_ptr(), dh.stride(0), dh.stride(1), gate.data_ptr(), gate.stride(0), gate.stride(1), value.data_ptr(),
+        value.stride(0), value.stride(1), _CODES[gate.dtype], B, T, D, carry.data_ptr(), _ptr(dh_last), _ptr(lengths),
+        dgate.data_ptr(), dvalue.data_ptr(), out.stride(0), out.stride(1), dh0.data_ptr(), _ptr(ws),
+        ws.numel() if ws is not None else 0, _stream(device)))
+    return dgate, dvalue, dh0
+
+
+def gated_recurrence_step(gate, value, state, *, stream=None):
+    """One token for each of B sequences: ``state`` (float32, (B, D)) is replaced
+    by the next state, which is returned rounded to gate's type. gate, value (B, D)."""
+    device = _cuda(gate, "gate")
+    if gate.dim() != 2:
+        raise ValueError(f"gate must be (B, D), got {tuple(gate.shape)}")
+    code = _dtype(gate, "gate")
+    shape = tuple(gate.shape)
+    _input(gate, "gate", shape, gate.dtype, device)
+    _input(value, "value", shape, gate.dtype, device)
+    _whole(state, "state", shape, torch.float32, device)
+    on = _on(device, stream)
+    if on is not None:
+        with on:
+            return gated_recurrence_step(gate, value, state)
+    h = torch.empty(shape, dtype=gate.dtype, device=device)
+    _check(lib().cpdp_gated_recurrence_step(gate.data_ptr(), gate.stride(0), value.data_ptr(), value.stride(0), code,
+                                            shape[0], shape[1], state.data_ptr(), h.data_ptr(), _stream(device)))
+    return h
