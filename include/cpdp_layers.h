@@ -176,6 +176,14 @@ cpdp_status cpdp_gated_recurrence_backward(const void *dh, int64_t dh_seq, int64
 cpdp_status cpdp_gated_recurrence_step(const void *gate, int64_t gate_seq, const void *value, int64_t value_seq,
                                        cpdp_dtype dtype, int B, int D, float *state, void *h, void *stream);
 
+/*
+ * cpdp_layer_timeouts — the number of bounded waits in the recurrence's kernels
+ * that ran out since the last call (0 expected; what they waited for counts as
+ * NaN). The blocks of a long sequence wait for one another's results, each wait
+ * for some seconds at most. Waits for the device.
+ */
+cpdp_status cpdp_layer_timeouts(int64_t *count);
+
 #ifdef __cplusplus
 }
 #endif

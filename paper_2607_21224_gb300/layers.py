@@ -55,6 +55,7 @@ SIGNATURES = {
     "cpdp_gated_recurrence_backward": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _L, _I, _I, _L, _I, _P, _P, _P, _P, _P, _L, _L,
                                             _P, _P, _Z, _P]),
     "cpdp_gated_recurrence_step": (_I, [_P, _L, _P, _L, _I, _I, _I, _P, _P, _P]),
+    "cpdp_layer_timeouts": (_I, [ctypes.POINTER(_L)]),
 }
 
 _lib = None
@@ -411,3 +412,11 @@ def gated_recurrence_step(gate, value, state, *, stream=None):
     _check(lib().cpdp_gated_recurrence_step(gate.data_ptr(), gate.stride(0), value.data_ptr(), value.stride(0), code,
                                             shape[0], shape[1], state.data_ptr(), h.data_ptr(), _stream(device)))
     return h
+
+
+def wait_timeouts() -> int:
+    """Bounded waits of the recurrence's kernels that ran out since the last
+    call (0 expected). Waits for the current device."""
+    count = _L()
+    _check(lib().cpdp_layer_timeouts(ctypes.byref(count)))
+    return count.value

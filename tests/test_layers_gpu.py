@@ -261,6 +261,24 @@ def test_recurrence(shape, dtype, ragged, layout):
     assert all(torch.equal(p, q) for p, q in zip(again, (dgate, dvalue, dh0)))
 
 
+def test_recurrence_of_many_tiles_has_no_wait_run_out():
+    """A long sequence next to short ones: several groups of tiles, more blocks than the GPU runs at once."""
+    shape = (3, 20000, 200)
+    gate, value, dh, h0, dh_last, _ = recurrence_inputs(shape, F32, False)
+    lengths = torch.tensor([20000, 4097, 15000], dtype=torch.int32)
+    f = ref.recurrence(gate, value, h0, lengths)
+    b = ref.recurrence_backward(dh, gate, value, h0, dh_last, lengths)
+    layers.wait_timeouts()
+    for _ in range(3):
+        h, last, carry = layers.gated_recurrence(gate.cuda(), value.cuda(), h0.cuda(), lengths.cuda())
+        grads = layers.gated_recurrence_backward(dh.cuda(), gate.cuda(), value.cuda(), carry, dh_last.cuda(), lengths.cuda())
+        assert layers.wait_timeouts() == 0
+    near(h, f["h"], f["eh"])
+    near(last, f["last"], f["elast"])
+    for got, name in zip(grads, ("dgate", "dvalue", "dh0")):
+        near(got, b[name], b["e" + name])
+
+
 def test_recurrence_reads_nothing_beyond_a_length():
     gate, value, dh, h0, dh_last, _ = recurrence_inputs((3, 90, 40), F32, False)
     lengths = torch.tensor([0, 17, 200], dtype=torch.int32)  # clamped to T
