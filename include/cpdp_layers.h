@@ -28,8 +28,8 @@
  * with max|x| <= 127 * 2^e, kept between -126 and 121; a value is held as the
  * whole number nearest to x / 2^e (ties to even), within +-127. So a value
  * that is read back is exact in bfloat16. codes: int8 [W][M][P], with
- * P = 32 * ceil(D / 32) (the padding is written as 0); exponents: uint8
- * [W][M][P / 32], e + 127. A block in which a value is infinite or NaN has the
+ * P = 32 * ceil(D / 32) (the padding is written as 0), 16-byte aligned;
+ * exponents: uint8 [W][M][P / 32], e + 127. A block in which a value is infinite or NaN has the
  * exponent byte 255 and reads back as NaN.
  *
  * Calls launch on `stream` (a cudaStream_t; NULL is the default stream) of the
@@ -177,10 +177,11 @@ cpdp_status cpdp_gated_recurrence_step(const void *gate, int64_t gate_seq, const
                                        cpdp_dtype dtype, int B, int D, float *state, void *h, void *stream);
 
 /*
- * cpdp_layer_timeouts — the number of bounded waits in the recurrence's kernels
- * that ran out since the last call (0 expected; what they waited for counts as
- * NaN). The blocks of a long sequence wait for one another's results, each wait
- * for some seconds at most. Waits for the device.
+ * cpdp_layer_timeouts — the number of bounded waits in these kernels that ran
+ * out since the last call (0 expected; results after one are not valid). The
+ * blocks of a long sequence wait for one another's results, and the weight
+ * gradient's warps for their slots, each wait for some seconds at most. Waits
+ * for the device.
  */
 cpdp_status cpdp_layer_timeouts(int64_t *count);
 

@@ -44,7 +44,7 @@ cpdp_status cpdp_checkpoint(const void* x, int64_t x_worker, int64_t x_row, cpdp
     CPDP_TRY(check_sizes(W, M, D));
     if (!known_dtype(dtype)) return layer_error(CPDP_EINVAL, "unknown dtype %d", (int)dtype);
     CPDP_TRY(check_array("x", x, M > 0, dtype_size(dtype), x_worker, x_row));
-    CPDP_TRY(check_array("codes", codes, M > 0, 1));
+    CPDP_TRY(check_array("codes", codes, M > 0, 16));
     CPDP_TRY(check_array("exponents", exponents, M > 0, 1));
     CPDP_TRY(check_array("values", values, false, 2));
     if (M == 0) return CPDP_OK;
@@ -63,7 +63,7 @@ cpdp_status cpdp_checkpoint(const void* x, int64_t x_worker, int64_t x_row, cpdp
 
 cpdp_status cpdp_restore(const int8_t* codes, const uint8_t* exponents, int W, int64_t M, int D, void* values, void* stream) {
     CPDP_TRY(check_sizes(W, M, D));
-    CPDP_TRY(check_array("codes", codes, M > 0, 1));
+    CPDP_TRY(check_array("codes", codes, M > 0, 16));
     CPDP_TRY(check_array("exponents", exponents, M > 0, 1));
     CPDP_TRY(check_array("values", values, M > 0, 2));
     if (M == 0) return CPDP_OK;

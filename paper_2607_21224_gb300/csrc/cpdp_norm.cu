@@ -136,6 +136,7 @@ cpdp_status cpdp_add_rmsnorm(const void* x, int64_t x_worker, int64_t x_row, con
     if (some && residual == nullptr && s != nullptr) return layer_error(CPDP_EINVAL, "s is x where there is no residual: pass NULL");
     if ((codes == nullptr) != (exponents == nullptr))
         return layer_error(CPDP_EINVAL, "codes and exponents go together: one of them is NULL");
+    CPDP_TRY(check_array("codes", codes, false, 16));
     if (!some) return CPDP_OK;
     const NormIn xi{x, x_worker, x_row}, ri{residual, residual_worker, residual_row};
     const dim3 grid(static_cast<unsigned>(M), W);

@@ -430,7 +430,9 @@ cpdp_status cpdp_layer_timeouts(int64_t* count) {
     cudaError_t e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&seen, wait_timeouts, sizeof seen);
     if (e == cudaSuccess) e = cudaMemcpyToSymbol(wait_timeouts, &zero, sizeof zero);
-    *count = static_cast<int64_t>(seen);
+    unsigned long long others = 0;
+    if (e == cudaSuccess) e = take_weight_gradient_timeouts(&others);
+    *count = static_cast<int64_t>(seen + others);
     return layer_launched(e, "cpdp_layer_timeouts");
 }
 

@@ -1,43 +1,351 @@
 // The weight gradient dW = dy^T x^ from activations held in 8 bits
 // (include/cpdp_layers.h).
+#include <cuda.h>
+
 #include "cpdp_layers.cuh"
 
 namespace cpdp {
 namespace {
 
-constexpr int kTile = 64, kDepth = 16, kThreads = 256;
+// One block computes 128 (i) x 256 (o) of dW, transposed on the tensor cores:
+// the accumulator's 128 lanes are neighbouring i, so that a warp's stores of
+// one column are 32 neighbours of dW's row. Tokens pass in steps of 64 through
+// a ring of shared-memory slots. Both operands have the tokens, the axis summed
+// over, as their slow axis; a slot holds them as rows of 64 elements (128
+// bytes) per token in the 128-byte swizzle, one block of rows per 64 columns:
+//   dy   bfloat16, by one tensor copy per block of rows
+//   x^   made by the eight converting warps from codes and exponents, each
+//        thread one block of 32 features of one token: exact in bfloat16
+// One thread issues the matrix instructions. The accumulator is in tensor
+// memory; the converting warps read it back when all steps are done.
+constexpr int kTileI = 128, kTileO = 256, kStep = 64, kSlots = 4;
+constexpr int kConvertWarps = 8, kThreads = (kConvertWarps + 2) * 32;  // and a copying and a multiplying warp
+constexpr int kBlockBytes = kStep * 128;                               // a step's rows of 64 elements
+constexpr int kXBytes = kTileI / 64 * kBlockBytes, kDyBytes = kTileO / 64 * kBlockBytes, kSlotBytes = kXBytes + kDyBytes;
+constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;  // and room to align the slots
+constexpr int kAhead = 4;                               // steps whose codes are loaded ahead
+constexpr unsigned long long kWaitLimitNs = 2000000000ull;
+static_assert(kStep * kTileI == kConvertWarps * 32 * kBlock8, "one block of features per converting thread and step");
 
-// 64 x 64 of dW per block, 4 x 4 per thread.
-template <typename T, typename G>
-__global__ void __launch_bounds__(kThreads)
-weight_gradient_kernel(const T* dy, int64_t dy_worker, int64_t dy_row, const int8_t* codes, const uint8_t* exponents,
-                       int64_t M, int O, int I, G* dW, int64_t dW_worker) {
-    layer_begin();
-    __shared__ float a[kDepth][kTile], b[kDepth][kTile];
-    const int64_t w = blockIdx.z;
-    const int o0 = blockIdx.y * kTile, i0 = blockIdx.x * kTile, blocks = (I + kBlock8 - 1) / kBlock8;
-    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    float acc[4][4] = {};
-    for (int64_t m0 = 0; m0 < M; m0 += kDepth) {
-        for (int k = threadIdx.x; k < kDepth * kTile; k += kThreads) {
-            const int64_t m = m0 + k / kTile;
-            const int o = o0 + k % kTile, i = i0 + k % kTile;
-            a[k / kTile][k % kTile] =
-                m < M && o < O ? to_float(__float2bfloat16_rn(to_float(dy[w * dy_worker + m * dy_row + o]))) : 0.f;
-            b[k / kTile][k % kTile] = m < M && i < I ? codes[(w * M + m) * blocks * kBlock8 + i] *
-                                                           unit_of(exponents[(w * M + m) * blocks + i / kBlock8])
-                                                     : 0.f;
+__device__ unsigned long long wait_timeouts;
+
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ unsigned long long now_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+__device__ __forceinline__ void barrier_init(uint64_t* b, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint64_t* b) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_at(b)) : "memory");
+}
+__device__ __forceinline__ bool barrier_done(uint64_t* b, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_at(b)), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+// False, and counted, where the phase does not end within the limit.
+__device__ __noinline__ bool barrier_wait_long(uint64_t* b, uint32_t parity) {
+    const unsigned long long start = now_ns();
+    while (!barrier_done(b, parity))
+        if (now_ns() - start > kWaitLimitNs) {
+            atomicAdd(&wait_timeouts, 1ull);
+            return false;
         }
-        __syncthreads();
-        for (int k = 0; k < kDepth; ++k)
-            for (int r = 0; r < 4; ++r)
-                for (int c = 0; c < 4; ++c) acc[r][c] += a[k][ty * 4 + r] * b[k][tx * 4 + c];
-        __syncthreads();
+    return true;
+}
+__device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity) {
+    return barrier_done(b, parity) || barrier_wait_long(b, parity);
+}
+
+// A matrix in shared memory whose rows of 64 elements run along the summed
+// axis: blocks of columns kBlockBytes apart, groups of 8 rows 1,024 bytes
+// apart, 128-byte swizzle.
+__device__ __forceinline__ uint64_t matrix_at(uint32_t address) {
+    return static_cast<uint64_t>((address & 0x3ffffu) >> 4) | static_cast<uint64_t>(kBlockBytes >> 4) << 16 |
+           static_cast<uint64_t>(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// float32 sums, both operands bfloat16 with the summed axis slow, 128 x 256.
+constexpr uint32_t kInstruction = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (kTileO / 8) << 17 | (kTileI / 16) << 24;
+
+__device__ __forceinline__ void multiply(uint32_t sums, uint64_t a, uint64_t b, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(sums),
+        "l"(a), "l"(b), "r"(kInstruction), "r"(add ? 1u : 0u)
+        : "memory");
+}
+__device__ __forceinline__ void arrive_when_multiplied(uint64_t* b) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(b)) : "memory");
+}
+// 32 columns of the warp's 32 lanes.
+__device__ __forceinline__ void read_sums(uint32_t at, float (&v)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at)
+        : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_pair(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Four codes as bfloat16 times `unit` (a pair of the same power of two). With
+// a code's lower seven bits n and its sign s, 0x4300 | n is 128 + n and
+// 0x4300 | 0x80 s is 128 or 256, so their difference is the code; every step
+// is exact.
+__device__ __forceinline__ uint2 values_of(uint32_t codes, uint32_t unit) {
+    const uint32_t low = codes & 0x7f7f7f7fu, sign = codes & 0x80808080u, k = 0x43434343u;
+    return make_uint2(mul_pair(sub_pair(__byte_perm(low, k, 0x4140), __byte_perm(sign, k, 0x4140)), unit),
+                      mul_pair(sub_pair(__byte_perm(low, k, 0x4342), __byte_perm(sign, k, 0x4342)), unit));
+}
+
+struct Codes {
+    uint4 half[2];
+    uint32_t byte;
+};
+
+struct WeightGradient {
+    const void* dy;
+    int64_t dy_worker, dy_row;
+    const int8_t* codes;
+    const uint8_t* exponents;
+    int64_t M;
+    int O, I, W, blocks;  // blocks of 32 features in a row of x^
+    int splits;           // of the tokens; more than one: parts [splits][W][O][I] of float32
+    int64_t split_steps;
+    void* out;
+    int64_t out_worker, out_split;
+};
+
+// T: dy's type. TENSOR: dy arrives by tensor copies (bfloat16, 16-byte aligned
+// strides); else the converting warps load it element by element. G: the
+// output's type.
+template <typename T, bool TENSOR, typename G>
+__global__ void __launch_bounds__(kThreads, 1)
+weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p) {
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[kSlots], empty[kSlots], done;
+    __shared__ uint32_t tensor_memory;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t slots = (smem_at(raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kSlots; ++s) {
+            barrier_init(&full[s], kConvertWarps + (TENSOR ? 1 : 0));
+            barrier_init(&empty[s], 1);
+        }
+        barrier_init(&done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    for (int r = 0; r < 4; ++r)
-        for (int c = 0; c < 4; ++c)
-            if (o0 + ty * 4 + r < O && i0 + tx * 4 + c < I)
-                dW[w * dW_worker + (int64_t)(o0 + ty * 4 + r) * I + i0 + tx * 4 + c] = from_float<G>(acc[r][c]);
+    if (warp == kConvertWarps + 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tensor_memory)), "r"(kTileO)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t sums = tensor_memory;
+    layer_begin();
+
+    const int i0 = blockIdx.x * kTileI, o0 = blockIdx.y * kTileO;
+    const int w = blockIdx.z % p.W, split = blockIdx.z / p.W;
+    const int64_t first = split * p.split_steps * kStep;
+    const int64_t tokens = min(p.M - first, p.split_steps * kStep);
+    const int steps = static_cast<int>((tokens + kStep - 1) / kStep);
+
+    if (warp == kConvertWarps) {
+        if (TENSOR && lane == 0) {
+            int k = 0;
+            for (; k < steps; ++k) {
+                const int s = k % kSlots;
+                if (k >= kSlots && !barrier_wait(&empty[s], (k / kSlots - 1) & 1)) break;
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(&full[s])), "r"(kDyBytes) : "memory");
+                for (int c = 0; c < kTileO / 64; ++c)
+                    asm volatile(
+                        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                            slots + s * kSlotBytes + kXBytes + c * kBlockBytes),
+                        "l"(&map), "r"(o0 + c * 64), "r"(static_cast<int>(first) + k * kStep), "r"(w), "r"(smem_at(&full[s]))
+                        : "memory");
+            }
+            // no copy may be in flight when the block ends: where a wait ran out, see the issued ones through
+            if (k < steps)
+                for (int q = max(k - kSlots, 0); q < k; ++q) barrier_wait(&full[q % kSlots], q / kSlots & 1);
+        }
+    } else if (warp == kConvertWarps + 1) {
+        if (lane == 0) {
+            bool ok = true;
+            for (int k = 0; k < steps && ok; ++k) {
+                const int s = k % kSlots;
+                ok = barrier_wait(&full[s], k / kSlots & 1);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint64_t a = matrix_at(slots + s * kSlotBytes), b = matrix_at(slots + s * kSlotBytes + kXBytes);
+#pragma unroll
+                for (int c = 0; c < kStep / 16; ++c) multiply(sums, a + c * (2048 >> 4), b + c * (2048 >> 4), k > 0 || c > 0);
+                arrive_when_multiplied(&empty[s]);
+            }
+            if (steps > 0) arrive_when_multiplied(&done);
+        }
+    } else {
+        // thread: token 8 * warp + lane / 4 of the step, features 32 * (lane % 4) + 0..31 of the tile
+        const int token = warp * 8 + lane / 4, quarter = lane % 4, block = i0 / kBlock8 + quarter;
+        // rows of 64 elements are two blocks of 32; the two rows' threads store their 16-byte pieces in another
+        // order, so that eight neighbouring threads meet in no bank
+        const int swap = quarter / 2;
+        const uint32_t row = slots + (quarter / 2) * kBlockBytes + token * 128;
+        const int64_t base = w * p.M + first;
+        const auto load = [&](int k) {
+            Codes c{};
+            const int64_t m = (int64_t)k * kStep + token;
+            if (m < tokens && block < p.blocks) {
+                const uint4* q = reinterpret_cast<const uint4*>(p.codes + ((base + m) * p.blocks + block) * kBlock8);
+                c.half[0] = __ldg(q + swap);
+                c.half[1] = __ldg(q + (swap ^ 1));
+                c.byte = __ldg(p.exponents + (base + m) * p.blocks + block);
+            }
+            return c;
+        };
+        Codes ahead[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) ahead[u] = load(u);
+        bool ok = true;
+        for (int k0 = 0; k0 < steps && ok; k0 += kAhead) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int k = k0 + u, s = k % kSlots;
+                if (k >= steps || !ok) break;
+                const Codes c = ahead[u];
+                ahead[u] = load(k + kAhead);
+                if (k >= kSlots) ok = __all_sync(~0u, barrier_wait(&empty[s], (k / kSlots - 1) & 1));
+                if (!ok) break;
+                // a block with an infinite or NaN value reads as NaN
+                const uint32_t unit = c.byte == 255u ? 0x7fc07fc0u : c.byte << 7 | c.byte << 23;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint2 lo = values_of(e == 0 ? c.half[h].x : c.half[h].z, unit);
+                        const uint2 hi = values_of(e == 0 ? c.half[h].y : c.half[h].w, unit);
+                        const int piece = (quarter % 2) * 4 + ((h ^ swap) * 2 + e);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + s * kSlotBytes + ((piece ^ (token % 8)) << 4)),
+                                     "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y)
+                                     : "memory");
+                    }
+                if (!TENSOR) {
+                    // rows of dy: the warp's 8 tokens, neighbouring elements in neighbouring lanes
+                    const T* dy = static_cast<const T*>(p.dy) + w * p.dy_worker + o0 + lane;
+#pragma unroll 2
+                    for (int r = 0; r < 8; ++r) {
+                        const int t = warp * 8 + r;
+                        const int64_t m = (int64_t)k * kStep + t;
+                        __nv_bfloat16 v[kTileO / 32];
+#pragma unroll
+                        for (int c = 0; c < kTileO / 32; ++c)
+                            v[c] = m < tokens && o0 + c * 32 + lane < p.O
+                                       ? from_float<__nv_bfloat16>(to_float(dy[(first + m) * p.dy_row + c * 32]))
+                                       : __ushort_as_bfloat16(0);
+#pragma unroll
+                        for (int c = 0; c < kTileO / 32; ++c) {
+                            const int o = c * 32 + lane;
+                            const uint32_t at = slots + s * kSlotBytes + kXBytes + (o / 64) * kBlockBytes + t * 128 +
+                                                (((o % 64 / 8) ^ (t % 8)) << 4) + o % 8 * 2;
+                            asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(__bfloat16_as_ushort(v[c])) : "memory");
+                        }
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) barrier_arrive(&full[s]);
+            }
+        }
+        // warp: lanes 32 * (warp % 4) of the accumulator, half of its columns
+        if (steps > 0) __all_sync(~0u, barrier_wait(&done, 0));
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int i = i0 + warp % 4 * 32 + lane;
+        G* out = static_cast<G*>(p.out) + split * p.out_split + w * p.out_worker + i;
+#pragma unroll 1
+        for (int c = warp / 4 * (kTileO / 2); c < (warp / 4 + 1) * (kTileO / 2) && o0 + c < p.O; c += 32) {
+            float v[32];
+            if (steps > 0) read_sums(sums + (warp % 4 * 32 << 16) + c, v);
+            if (i < p.I)
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (o0 + c + j < p.O) out[(int64_t)(o0 + c + j) * p.I] = from_float<G>(steps > 0 ? v[j] : 0.f);
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    __syncthreads();
+    if (warp == kConvertWarps + 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(kTileO));
+    }
+}
+
+// The sum of the splits' parts, in their order.
+template <typename G>
+__global__ void __launch_bounds__(256)
+sum_parts_kernel(const float* parts, int splits, int64_t per_worker, int64_t all, G* dW, int64_t dW_worker) {
+    layer_begin();
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
+        float s = 0.f;
+        for (int k = 0; k < splits; ++k) s += __ldcs(parts + k * all + at);
+        const int64_t w = at / per_worker;
+        dW[w * dW_worker + (at - w * per_worker)] = from_float<G>(s);
+    }
+}
+
+// Splits of the token axis: where there are fewer tiles than SMs, as many as
+// fill them, of at least 4 steps each.
+struct Splits {
+    int64_t steps, each;
+    int count;
+};
+Splits splits_of(int W, int64_t M, int O, int I) {
+    const int64_t steps = ceil_div(M, kStep), tiles = ceil_div(I, kTileI) * ceil_div(O, kTileO) * W;
+    int64_t count = tiles >= kSMs ? 1 : kSMs / tiles;
+    if (count > steps / 4) count = steps / 4;
+    if (count < 1) count = 1;
+    const int64_t each = ceil_div(steps, count);
+    return {steps, each, each > 0 ? static_cast<int>(ceil_div(steps, each)) : 1};
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return f;
 }
 
 }  // namespace
@@ -45,34 +353,84 @@ weight_gradient_kernel(const T* dy, int64_t dy_worker, int64_t dy_row, const int
 
 using namespace cpdp;
 
+static cpdp_status check_weight_gradient(int W, int64_t M, int O, int I) {
+    CPDP_TRY(check_sizes(W, M, O));
+    CPDP_TRY(check_sizes(W, M, I));
+    CPDP_TRY(check_sizes(W, O, I));
+    if (M > kLayerMaxRows - kStep) return layer_error(CPDP_EINVAL, "M=%lld is at most 2^31 - 65", (long long)M);
+    const int64_t tiles_o = ceil_div(O, kTileO), splits = splits_of(W, M, O, I).count;
+    if (tiles_o > 65535 || splits * W > 65535)
+        return layer_error(CPDP_EINVAL, "W=%d, M=%lld, O=%d: more blocks than a launch takes", W, (long long)M, O);
+    return CPDP_OK;
+}
+
 size_t cpdp_weight_gradient_workspace(int W, int64_t M, int O, int I) {
-    (void)W, (void)M, (void)O, (void)I;
-    return 0;
+    if (check_weight_gradient(W, M, O, I) != CPDP_OK) return 0;
+    const int count = splits_of(W, M, O, I).count;
+    return count > 1 ? static_cast<size_t>(count) * W * O * I * 4 : 0;
 }
 
 cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_row, cpdp_dtype dy_dtype,
                                  const int8_t* codes, const uint8_t* exponents, int W, int64_t M, int O, int I, void* dW,
                                  int64_t dW_worker, cpdp_dtype dW_dtype, void* workspace, size_t workspace_bytes,
                                  void* stream) {
-    CPDP_TRY(check_sizes(W, M, O));
-    CPDP_TRY(check_sizes(W, M, I));
-    CPDP_TRY(check_sizes(W, O, I));
+    CPDP_TRY(check_weight_gradient(W, M, O, I));
     if (!known_dtype(dy_dtype) || !known_dtype(dW_dtype))
         return layer_error(CPDP_EINVAL, "unknown dtype: dy's is %d, dW's %d", (int)dy_dtype, (int)dW_dtype);
     CPDP_TRY(check_array("dy", dy, M > 0, dtype_size(dy_dtype), dy_worker, dy_row));
-    CPDP_TRY(check_array("codes", codes, M > 0, 1));
+    CPDP_TRY(check_array("codes", codes, M > 0, 16));
     CPDP_TRY(check_array("exponents", exponents, M > 0, 1));
     CPDP_TRY(check_array("dW", dW, true, dtype_size(dW_dtype), dW_worker));
     CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_weight_gradient_workspace(W, M, O, I)));
-    const dim3 grid(ceil_div(I, kTile), ceil_div(O, kTile), W);
-    const auto go = [&](auto* g, auto* out) {
-        using T = std::remove_const_t<std::remove_pointer_t<decltype(g)>>;
-        using G = std::remove_pointer_t<decltype(out)>;
-        return launch_layer(weight_gradient_kernel<T, G>, grid, kThreads, 0, stream, g, dy_worker, dy_row, codes, exponents, M, O, I, out, dW_worker);
+    const Splits sp = splits_of(W, M, O, I);
+    const bool parts = sp.count > 1;
+    WeightGradient p{};
+    p.dy = dy, p.dy_worker = dy_worker, p.dy_row = dy_row;
+    p.codes = codes, p.exponents = exponents;
+    p.M = M, p.O = O, p.I = I, p.W = W, p.blocks = static_cast<int>(ceil_div(I, kBlock8));
+    p.splits = sp.count, p.split_steps = sp.each;
+    p.out = parts ? workspace : dW;
+    p.out_worker = parts ? (int64_t)O * I : dW_worker;
+    p.out_split = (int64_t)W * O * I;
+
+    // Tensor copies of dy: bfloat16, rows and workers at multiples of 16 bytes.
+    CUtensorMap map{};
+    const int64_t rows = M > 1 ? dy_row : ceil_div(O, 8) * 8, workers = W > 1 ? dy_worker : rows * M;
+    const bool tensor = dy_dtype == CPDP_BF16 && M > 0 && aligned_to(dy, 16) && rows % 8 == 0 && rows >= O && workers % 8 == 0 && workers > 0;
+    if (tensor) {
+        const EncodeTiled encode = encode_tiled();
+        if (encode == nullptr) return layer_error(CPDP_ECUDA, "the CUDA driver has no cuTensorMapEncodeTiled");
+        const cuuint64_t dims[3] = {(cuuint64_t)O, (cuuint64_t)M, (cuuint64_t)W}, strides[2] = {(cuuint64_t)rows * 2, (cuuint64_t)workers * 2};
+        const cuuint32_t box[3] = {64, kStep, 1}, one[3] = {1, 1, 1};
+        const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(dy), dims, strides, box, one,
+                                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r != CUDA_SUCCESS) return layer_error(CPDP_ECUDA, "cuTensorMapEncodeTiled: error %d", (int)r);
+    }
+    const dim3 grid(ceil_div(I, kTileI), ceil_div(O, kTileO), sp.count * W);
+    const auto go = [&](auto kernel) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+        return e != cudaSuccess ? e : launch_layer(kernel, grid, kThreads, kSmemBytes, stream, map, p);
     };
-    const auto typed = [&](auto* out) {
-        return dy_dtype == CPDP_F32 ? go(static_cast<const float*>(dy), out) : go(static_cast<const __nv_bfloat16*>(dy), out);
+    const auto typed = [&](auto g) {
+        using G = decltype(g);
+        return dy_dtype == CPDP_F32 ? go(weight_gradient_kernel<float, false, G>)
+               : tensor             ? go(weight_gradient_kernel<__nv_bfloat16, true, G>)
+                                    : go(weight_gradient_kernel<__nv_bfloat16, false, G>);
     };
-    return layer_launched(dW_dtype == CPDP_F32 ? typed(static_cast<float*>(dW)) : typed(static_cast<__nv_bfloat16*>(dW)),
-                          "cpdp_weight_gradient");
+    CPDP_TRY(layer_launched(parts || dW_dtype == CPDP_F32 ? typed(0.f) : typed(__nv_bfloat16{}), "cpdp_weight_gradient"));
+    if (!parts) return CPDP_OK;
+    const int64_t per_worker = (int64_t)O * I, all = per_worker * W;
+    const unsigned blocks = static_cast<unsigned>(ceil_div(all, 256) < kSMs * 8 ? ceil_div(all, 256) : kSMs * 8);
+    const auto sum = [&](auto* out) {
+        return launch_layer(sum_parts_kernel<std::remove_pointer_t<decltype(out)>>, blocks, 256, 0, stream, static_cast<const float*>(workspace),
+                            sp.count, per_worker, all, out, dW_worker);
+    };
+    return layer_launched(dW_dtype == CPDP_F32 ? sum(static_cast<float*>(dW)) : sum(static_cast<__nv_bfloat16*>(dW)), "cpdp_weight_gradient");
+}
+
+cudaError_t cpdp::take_weight_gradient_timeouts(unsigned long long* count) {
+    const unsigned long long zero = 0;
+    const cudaError_t e = cudaMemcpyFromSymbol(count, wait_timeouts, sizeof *count);
+    return e != cudaSuccess ? e : cudaMemcpyToSymbol(wait_timeouts, &zero, sizeof zero);
 }
