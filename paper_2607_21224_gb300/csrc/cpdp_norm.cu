@@ -1,110 +1,322 @@
 // Residual addition and root-mean-square norm for W workers, with an optional
 // 8-bit output, and its backward pass (include/cpdp_layers.h).
+#include <type_traits>
+
 #include "cpdp_layers.cuh"
 
 namespace cpdp {
 namespace {
-
-constexpr int kThreads = 256;
-
-__device__ __forceinline__ float block_sum(float v) {
-    __shared__ float part[kThreads / 32];
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-    __syncthreads();
-    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = v;
-    __syncthreads();
-    float s = 0.f;
-    for (int i = 0; i < kThreads / 32; ++i) s += part[i];
-    return s;
-}
 
 struct NormIn {
     const void* p;
     int64_t worker, row;
 };
 
-// One block per row.
-template <typename T, bool CHECKPOINT>
-__global__ void __launch_bounds__(kThreads)
-norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weight_worker, int64_t M, int D, float eps,
-                    void* y, void* s, int8_t* codes, uint8_t* exponents) {
-    layer_begin();
-    const int64_t m = blockIdx.x, w = blockIdx.y, row = w * M + m;
-    const T* xr = static_cast<const T*>(x.p) + w * x.worker + m * x.row;
-    const T* rr = static_cast<const T*>(residual.p) + w * residual.worker + m * residual.row;
-    const float* wt = weight + w * weight_worker;
-    float sum = 0.f;
-    for (int d = threadIdx.x; d < D; d += kThreads) {
-        float v = to_float(xr[d]);
-        if (residual.p != nullptr) {
-            const T r = from_float<T>(v + to_float(rr[d]));
-            static_cast<T*>(s)[row * D + d] = r;
-            v = to_float(r);
-        }
-        sum += v * v;
+// A row is spread over TPR threads, E elements each, in pieces of V
+// neighbours: piece j of thread t starts at element (j * TPR + t) * V. V is 16
+// bytes' worth where every row of every array starts at a multiple of that,
+// else 1. Rows of up to 1,024 elements take a warp, longer ones a block.
+template <typename T, int V>
+struct Piece;
+template <>
+struct Piece<float, 4> {
+    float4 v;
+    __device__ __forceinline__ float get(int e) const { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; }
+    __device__ __forceinline__ void load(const float* p) { v = __ldcs(reinterpret_cast<const float4*>(p)); }
+};
+template <>
+struct Piece<__nv_bfloat16, 8> {
+    uint4 v;
+    __device__ __forceinline__ float get(int e) const {
+        const uint32_t u = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
+        return __uint_as_float(e % 2 ? u & 0xffff0000u : u << 16);
     }
-    const float k = rsqrtf(block_sum(sum) / D + eps);
-    const int blocks = (D + kBlock8 - 1) / kBlock8;
-    for (int d = threadIdx.x; d < blocks * kBlock8; d += kThreads) {
-        float v = 0.f;
-        if (d < D) {
-            v = to_float(xr[d]);
-            if (residual.p != nullptr) v = to_float(from_float<T>(v + to_float(rr[d])));
-            v = v * k * wt[d];
-        }
-        if (CHECKPOINT) {
-            const uint32_t top = __reduce_max_sync(~0u, __float_as_uint(v) & 0x7fffffffu);
-            const uint32_t e = exponent_byte(top);
-            const int q = code_of(v, inverse_unit_of(e));
-            codes[row * blocks * kBlock8 + d] = static_cast<int8_t>(q);
-            if (threadIdx.x % 32 == 0) exponents[row * blocks + d / kBlock8] = static_cast<uint8_t>(e);
-            if (d < D) static_cast<__nv_bfloat16*>(y)[row * D + d] = from_float<__nv_bfloat16>(q * unit_of(e));
-        } else if (d < D) {
-            static_cast<T*>(y)[row * D + d] = from_float<T>(v);
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
+};
+template <>
+struct Piece<float, 1> {
+    float v;
+    __device__ __forceinline__ float get(int) const { return v; }
+    __device__ __forceinline__ void load(const float* p) { v = __ldcs(p); }
+};
+template <>
+struct Piece<__nv_bfloat16, 1> {
+    uint16_t v;
+    __device__ __forceinline__ float get(int) const { return __uint_as_float(uint32_t(v) << 16); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint16_t*>(p)); }
+};
+
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <int V>
+__device__ __forceinline__ void store_piece(float* p, const float* v) {
+    if constexpr (V == 4)
+        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else
+        *p = v[0];
+}
+template <int V>
+__device__ __forceinline__ void store_piece(__nv_bfloat16* p, const float* v) {
+    if constexpr (V == 8)
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]), pack(v[6], v[7]));
+    else if constexpr (V == 4)
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack(v[0], v[1]), pack(v[2], v[3]));
+    else
+        *p = __float2bfloat16_rn(v[0]);
+}
+template <int V>
+__device__ __forceinline__ void store_codes(int8_t* p, const int* q) {
+    const auto word = [](const int* c) { return (c[0] & 255) | (c[1] & 255) << 8 | (c[2] & 255) << 16 | c[3] << 24; };
+    if constexpr (V == 8)
+        *reinterpret_cast<int2*>(p) = make_int2(word(q), word(q + 4));
+    else if constexpr (V == 4)
+        *reinterpret_cast<int*>(p) = word(q);
+    else
+        *p = static_cast<int8_t>(q[0]);
+}
+
+// The sum over the row's threads, of N values at once. Blocks use two sets of
+// partial sums in turn, so one barrier per row is enough.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], int turn) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(~0u, v[k], o);
+    if constexpr (TPR > 32) {
+        __shared__ float part[2][N][TPR / 32];
+        if (threadIdx.x % 32 == 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) part[turn][k][threadIdx.x / 32] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = 0.f;
+#pragma unroll
+            for (int i = 0; i < TPR / 32; ++i) v[k] += part[turn][k][i];
         }
     }
 }
 
-// One block per row; the row's scale goes to `scale` for the weight's gradient.
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_t weight_worker, int64_t M, int D,
-                     float eps, void* dx, float* scale) {
-    layer_begin();
-    const int64_t m = blockIdx.x, w = blockIdx.y, row = w * M + m;
-    const T* g = static_cast<const T*>(dy.p) + w * dy.worker + m * dy.row;
-    const T* sr = static_cast<const T*>(s.p) + w * s.worker + m * s.row;
-    const T* dr = static_cast<const T*>(ds.p) + w * ds.worker + m * ds.row;
-    const float* wt = weight + w * weight_worker;
-    float squares = 0.f, dot = 0.f;
-    for (int d = threadIdx.x; d < D; d += kThreads) {
-        const float v = to_float(sr[d]);
-        squares += v * v;
-        dot += to_float(g[d]) * wt[d] * v;
-    }
-    squares = block_sum(squares);
-    dot = block_sum(dot);
-    const float k = rsqrtf(squares / D + eps);
-    const float c = k * k * k * (dot / D);
-    if (threadIdx.x == 0) scale[row] = k;
-    for (int d = threadIdx.x; d < D; d += kThreads) {
-        const float through = ds.p != nullptr ? to_float(dr[d]) : 0.f;
-        static_cast<T*>(dx)[row * D + d] = from_float<T>(through + k * to_float(g[d]) * wt[d] - c * to_float(sr[d]));
-    }
-}
+template <int TPR>
+struct RowThreads {
+    static constexpr int block = TPR > 128 ? TPR : 128, rows = block / TPR;
+};
 
-template <typename T, typename G>
-__global__ void __launch_bounds__(kThreads)
-norm_weight_kernel(NormIn dy, NormIn s, const float* scale, int64_t M, int D, G* dweight, int64_t dweight_worker) {
+template <typename T, int V, int TPR, int E, bool CHECKPOINT>
+__global__ void __launch_bounds__(RowThreads<TPR>::block)
+norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weight_worker, int64_t M, int D, float eps, void* y,
+                    void* s, int8_t* codes, uint8_t* exponents) {
     layer_begin();
-    const int d = blockIdx.x * kThreads + threadIdx.x;
+    constexpr int rows = RowThreads<TPR>::rows, J = E / V;
+    using Out = std::conditional_t<CHECKPOINT, __nv_bfloat16, T>;
+    const int t = threadIdx.x % TPR;
     const int64_t w = blockIdx.y;
-    if (d >= D) return;
+    const int blocks = (D + kBlock8 - 1) / kBlock8;
+    float wt[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+        const int d = (k / V * TPR + t) * V + k % V;
+        wt[k] = d < D ? __ldg(weight + w * weight_worker + d) : 0.f;
+    }
+    int turn = 0;
+    for (int64_t m = (int64_t)blockIdx.x * rows + threadIdx.x / TPR; m < M; m += (int64_t)gridDim.x * rows, turn ^= 1) {
+        const T* xr = static_cast<const T*>(x.p) + w * x.worker + m * x.row;
+        const T* rr = static_cast<const T*>(residual.p) + w * residual.worker + m * residual.row;
+        const int64_t row = w * M + m;
+        float v[E];
+        {
+            Piece<T, V> a[J], b[J];
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int d = (j * TPR + t) * V;
+                a[j] = b[j] = Piece<T, V>{};
+                if (d < D) {
+                    a[j].load(xr + d);
+                    if (residual.p != nullptr) b[j].load(rr + d);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+                v[k] = a[k / V].get(k % V);
+                // the norm is of the sum as it is stored: what the backward pass reads
+                if (residual.p != nullptr) v[k] = to_float(from_float<T>(v[k] + b[k / V].get(k % V)));
+            }
+        }
+        float sum[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < E; ++k) sum[0] = fmaf(v[k], v[k], sum[0]);
+        if (residual.p != nullptr)
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int d = (j * TPR + t) * V;
+                if (d < D) store_piece<V>(static_cast<T*>(s) + row * D + d, v + j * V);
+            }
+        row_sum<TPR>(sum, turn);
+        const float k = rsqrtf(sum[0] / D + eps);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int d = (j * TPR + t) * V;
+            float o[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] = v[j * V + e] * k * wt[j * V + e];
+            if constexpr (CHECKPOINT) {
+                if ((j * TPR + t / 32 * 32) * V >= blocks * kBlock8) break;  // the warp is past the row
+                uint32_t top = 0;
+#pragma unroll
+                for (int e = 0; e < V; ++e) top = max(top, __float_as_uint(d < D ? o[e] : 0.f) & 0x7fffffffu);
+                // a block is 32 / V neighbouring threads
+                if constexpr (V == 1)
+                    top = __reduce_max_sync(~0u, top);
+                else
+#pragma unroll
+                    for (int h = 1; h < kBlock8 / V; h <<= 1) top = max(top, __shfl_xor_sync(~0u, top, h));
+                const uint32_t byte = exponent_byte(top);
+                const float inverse = inverse_unit_of(byte), unit = unit_of(byte);
+                int q[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    q[e] = d < D ? code_of(o[e], inverse) : 0;
+                    o[e] = q[e] * unit;
+                }
+                if (d < blocks * kBlock8) {
+                    store_codes<V>(codes + row * blocks * kBlock8 + d, q);
+                    if (d % kBlock8 == 0) exponents[row * blocks + d / kBlock8] = static_cast<uint8_t>(byte);
+                }
+            }
+            if (d < D) store_piece<V>(static_cast<Out*>(y) + row * D + d, o);
+        }
+    }
+}
+
+// The row's dx, and dweight's sums over the block's rows kept in registers
+// from row to row; `parts` receives them, one row per block. KEEP: the weights
+// stay in registers too.
+template <typename T, int V, int TPR, int E, bool KEEP>
+__global__ void __launch_bounds__(RowThreads<TPR>::block)
+norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_t weight_worker, int64_t M, int D, float eps,
+                     void* dx, float* parts) {
+    layer_begin();
+    constexpr int rows = RowThreads<TPR>::rows, J = E / V;
+    const int t = threadIdx.x % TPR;
+    const int64_t w = blockIdx.y;
+    const auto weight_at = [&](int k) {
+        const int d = (k / V * TPR + t) * V + k % V;
+        return d < D ? __ldg(weight + w * weight_worker + d) : 0.f;
+    };
+    float wt[KEEP ? E : 1], sums[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+        if constexpr (KEEP) wt[k] = weight_at(k);
+        sums[k] = 0.f;
+    }
+    int turn = 0;
+    for (int64_t m = (int64_t)blockIdx.x * rows + threadIdx.x / TPR; m < M; m += (int64_t)gridDim.x * rows, turn ^= 1) {
+        const T* gr = static_cast<const T*>(dy.p) + w * dy.worker + m * dy.row;
+        const T* sr = static_cast<const T*>(s.p) + w * s.worker + m * s.row;
+        const T* dr = static_cast<const T*>(ds.p) + w * ds.worker + m * ds.row;
+        Piece<T, V> g[J], r[J], through[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int d = (j * TPR + t) * V;
+            g[j] = r[j] = through[j] = Piece<T, V>{};
+            if (d < D) {
+                g[j].load(gr + d);
+                r[j].load(sr + d);
+                if (KEEP && ds.p != nullptr) through[j].load(dr + d);
+            }
+        }
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            const float v = r[k / V].get(k % V);
+            sum[0] = fmaf(v, v, sum[0]);
+            sum[1] = fmaf(g[k / V].get(k % V) * (KEEP ? wt[KEEP ? k : 0] : weight_at(k)), v, sum[1]);
+        }
+        row_sum<TPR>(sum, turn);
+        const float k1 = rsqrtf(sum[0] / D + eps), k3 = k1 * k1 * k1 * (sum[1] / D);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int d = (j * TPR + t) * V;
+            if (!KEEP && ds.p != nullptr && d < D) through[j].load(dr + d);
+            float o[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const int k = j * V + e;
+                const float v = r[j].get(e), gk = g[j].get(e) * k1;
+                o[e] = fmaf(gk, KEEP ? wt[KEEP ? k : 0] : weight_at(k), through[j].get(e)) - v * k3;
+                sums[k] = fmaf(gk, v, sums[k]);
+            }
+            if (d < D) store_piece<V>(static_cast<T*>(dx) + (w * M + m) * D + d, o);
+        }
+    }
+    float* part = parts + (w * gridDim.x + blockIdx.x) * D;
+    if constexpr (rows > 1) {
+        __shared__ float all[rows - 1][E * TPR];
+        const int own = threadIdx.x / TPR;
+        if (own > 0)
+#pragma unroll
+            for (int k = 0; k < E; ++k) all[own - 1][k * TPR + t] = sums[k];
+        __syncthreads();
+        if (own > 0) return;
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+            for (int i = 0; i < rows - 1; ++i) sums[k] += all[i][k * TPR + t];
+    }
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+        const int d = (k / V * TPR + t) * V + k % V;
+        if (d < D) part[d] = sums[k];
+    }
+}
+
+// dweight: the sum of the blocks' parts, in an order fixed by their number.
+constexpr int kColumns = 32, kLines = 16;
+template <typename G>
+__global__ void __launch_bounds__(kColumns * kLines)
+norm_weight_kernel(const float* parts, int count, int D, G* dweight, int64_t dweight_worker) {
+    layer_begin();
+    __shared__ float line[kLines][kColumns];
+    const int c = threadIdx.x % kColumns, l = threadIdx.x / kColumns, d = blockIdx.x * kColumns + c;
+    const int64_t w = blockIdx.y;
     float sum = 0.f;
-    for (int64_t m = 0; m < M; ++m)
-        sum += to_float(static_cast<const T*>(dy.p)[w * dy.worker + m * dy.row + d]) *
-               to_float(static_cast<const T*>(s.p)[w * s.worker + m * s.row + d]) * scale[w * M + m];
-    dweight[w * dweight_worker + d] = from_float<G>(sum);
+    if (d < D)
+#pragma unroll 4
+        for (int i = l; i < count; i += kLines) sum += __ldcs(parts + (w * count + i) * D + d);
+    line[l][c] = sum;
+    __syncthreads();
+    if (l == 0 && d < D) {
+        for (int i = 1; i < kLines; ++i) sum += line[i][c];
+        dweight[w * dweight_worker + d] = from_float<G>(sum);
+    }
+}
+
+// Threads per row and elements per thread for D features: f(TPR, E).
+template <int N>
+using Int = std::integral_constant<int, N>;
+template <typename F>
+cudaError_t with_shape(int D, const F& f) {
+    if (D <= 512) return f(Int<32>{}, Int<16>{});
+    if (D <= 1024) return f(Int<32>{}, Int<32>{});
+    if (D <= 2048) return f(Int<128>{}, Int<16>{});
+    if (D <= 4096) return f(Int<128>{}, Int<32>{});
+    if (D <= 8192) return f(Int<512>{}, Int<16>{});
+    return f(Int<512>{}, Int<32>{});
+}
+static_assert(CPDP_NORM_MAX_FEATURES == 512 * 32, "the largest shape");
+
+// Blocks per worker: the rows' blocks, at most so many as run at once.
+unsigned blocks_for(int W, int64_t M, int rows, int resident) {
+    const int64_t all = ceil_div(M, rows), most = ceil_div(int64_t(kSMs) * resident, W);
+    return static_cast<unsigned>(all < most ? all : most);
+}
+int rows_per_block(int D) { return D <= 1024 ? 4 : 1; }
+// The backward pass's blocks per worker: what its registers let run at once. The workspace's size goes by it.
+unsigned backward_blocks(int W, int64_t M, int D) {
+    const int resident = D <= 512 ? 4 : D <= 1024 ? 2 : D <= 2048 ? 4 : D <= 4096 ? 2 : 1;
+    return blocks_for(W, M, rows_per_block(D), resident);
 }
 
 }  // namespace
@@ -119,6 +331,12 @@ static cpdp_status check_norm(int W, int64_t M, int D, cpdp_dtype dtype, float e
     if (!known_dtype(dtype)) return layer_error(CPDP_EINVAL, "unknown dtype %d", (int)dtype);
     if (!(eps > 0.f) || eps > 3.0e38f) return layer_error(CPDP_EINVAL, "eps=%g must be positive and finite", (double)eps);
     return CPDP_OK;
+}
+
+// Whether every row starts at a multiple of 16 bytes and has whole pieces.
+static bool in_pieces(const NormIn& a, int64_t size, int D) {
+    const int64_t n = 16 / size;
+    return aligned_to(a.p, 16) && a.worker % n == 0 && a.row % n == 0 && D % n == 0;
 }
 
 cpdp_status cpdp_add_rmsnorm(const void* x, int64_t x_worker, int64_t x_row, const void* residual,
@@ -139,19 +357,26 @@ cpdp_status cpdp_add_rmsnorm(const void* x, int64_t x_worker, int64_t x_row, con
     CPDP_TRY(check_array("codes", codes, false, 16));
     if (!some) return CPDP_OK;
     const NormIn xi{x, x_worker, x_row}, ri{residual, residual_worker, residual_row};
-    const dim3 grid(static_cast<unsigned>(M), W);
-    const auto go = [&](auto kernel) {
-        return launch_layer(kernel, grid, kThreads, 0, stream, xi, ri, weight, weight_worker, M, D, eps, y, s, codes, exponents);
-    };
-    const cudaError_t launched =
-        dtype == CPDP_F32 ? (codes ? go(norm_forward_kernel<float, true>) : go(norm_forward_kernel<float, false>))
-                          : (codes ? go(norm_forward_kernel<__nv_bfloat16, true>) : go(norm_forward_kernel<__nv_bfloat16, false>));
+    const bool wide = in_pieces(xi, e, D) && in_pieces(ri, e, D) && aligned_to(y, 16) && aligned_to(s, 16);
+    const cudaError_t launched = with_shape(D, [&](auto tpr, auto elements) {
+        constexpr int TPR = decltype(tpr)::value, E = decltype(elements)::value;
+        const auto go = [&](auto kernel) {
+            const dim3 grid(blocks_for(W, M, RowThreads<TPR>::rows, 2048 / RowThreads<TPR>::block), W);
+            return launch_layer(kernel, grid, RowThreads<TPR>::block, 0, stream, xi, ri, weight, weight_worker, M, D, eps, y, s, codes, exponents);
+        };
+        const auto held = [&](auto checkpoint) {
+            constexpr bool C = decltype(checkpoint)::value;
+            if (dtype == CPDP_F32) return wide ? go(norm_forward_kernel<float, 4, TPR, E, C>) : go(norm_forward_kernel<float, 1, TPR, E, C>);
+            return wide ? go(norm_forward_kernel<__nv_bfloat16, 8, TPR, E, C>) : go(norm_forward_kernel<__nv_bfloat16, 1, TPR, E, C>);
+        };
+        return codes != nullptr ? held(std::true_type{}) : held(std::false_type{});
+    });
     return layer_launched(launched, "cpdp_add_rmsnorm");
 }
 
 size_t cpdp_add_rmsnorm_backward_workspace(int W, int64_t M, int D) {
     if (check_norm(W, M, D, CPDP_F32, 1.f) != CPDP_OK) return 0;
-    return static_cast<size_t>(W) * M * 4;
+    return static_cast<size_t>(W) * backward_blocks(W, M, D) * D * 4;
 }
 
 cpdp_status cpdp_add_rmsnorm_backward(const void* dy, int64_t dy_worker, int64_t dy_row, const void* s, int64_t s_worker,
@@ -171,21 +396,24 @@ cpdp_status cpdp_add_rmsnorm_backward(const void* dy, int64_t dy_worker, int64_t
     CPDP_TRY(check_array("dweight", dweight, true, dtype_size(dweight_dtype), dweight_worker));
     CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_add_rmsnorm_backward_workspace(W, M, D)));
     const NormIn gi{dy, dy_worker, dy_row}, si{s, s_worker, s_row}, di{ds, ds_worker, ds_row};
-    float* scale = static_cast<float*>(workspace);
-    if (some) {
-        const auto go = [&](auto kernel) {
-            return launch_layer(kernel, dim3(static_cast<unsigned>(M), W), kThreads, 0, stream, gi, si, di, weight, weight_worker, M, D, eps, dx, scale);
-        };
-        CPDP_TRY(layer_launched(dtype == CPDP_F32 ? go(norm_backward_kernel<float>) : go(norm_backward_kernel<__nv_bfloat16>),
-                                "cpdp_add_rmsnorm_backward"));
-    }
-    const auto go = [&](auto kernel, auto* out) {
-        return launch_layer(kernel, dim3(ceil_div(D, kThreads), W), kThreads, 0, stream, gi, si, scale, M, D, out, dweight_worker);
+    float* parts = static_cast<float*>(workspace);
+    const unsigned blocks = backward_blocks(W, M, D);
+    const bool wide = in_pieces(gi, e, D) && in_pieces(si, e, D) && in_pieces(di, e, D) && aligned_to(dx, 16);
+    if (some)
+        CPDP_TRY(layer_launched(with_shape(D, [&](auto tpr, auto elements) {
+            constexpr int TPR = decltype(tpr)::value, E = decltype(elements)::value;
+            constexpr bool K = TPR * E <= 8192;  // longer rows have too few registers for it
+            const auto go = [&](auto kernel) {
+                return launch_layer(kernel, dim3(blocks, W), RowThreads<TPR>::block, 0, stream, gi, si, di, weight, weight_worker, M, D,
+                                    eps, dx, parts);
+            };
+            if (dtype == CPDP_F32) return wide ? go(norm_backward_kernel<float, 4, TPR, E, K>) : go(norm_backward_kernel<float, 1, TPR, E, K>);
+            return wide ? go(norm_backward_kernel<__nv_bfloat16, 8, TPR, E, K>) : go(norm_backward_kernel<__nv_bfloat16, 1, TPR, E, K>);
+        }), "cpdp_add_rmsnorm_backward"));
+    const auto sum = [&](auto* out) {
+        return launch_layer(norm_weight_kernel<std::remove_pointer_t<decltype(out)>>, dim3(ceil_div(D, kColumns), W), kColumns * kLines, 0,
+                            stream, static_cast<const float*>(parts), static_cast<int>(blocks), D, out, dweight_worker);
     };
-    const auto typed = [&](auto* out) {
-        using G = std::remove_pointer_t<decltype(out)>;
-        return dtype == CPDP_F32 ? go(norm_weight_kernel<float, G>, out) : go(norm_weight_kernel<__nv_bfloat16, G>, out);
-    };
-    return layer_launched(dweight_dtype == CPDP_F32 ? typed(static_cast<float*>(dweight)) : typed(static_cast<__nv_bfloat16*>(dweight)),
+    return layer_launched(dweight_dtype == CPDP_F32 ? sum(static_cast<float*>(dweight)) : sum(static_cast<__nv_bfloat16*>(dweight)),
                           "cpdp_add_rmsnorm_backward");
 }
