@@ -1,5 +1,7 @@
 // The gated linear recurrence h_t = a_t h_(t-1) + (1 - a_t) v_t, its backward
 // pass and its single step (include/cpdp_layers.h).
+#include <type_traits>
+
 #include "cpdp_layers.cuh"
 
 namespace cpdp {
@@ -22,12 +24,19 @@ struct SeqIn {
     int64_t seq, step;
 };
 
-// a = sigmoid(x) and 1 - a, both to a few ulps: neither is formed as a
-// difference from 1.
+// a = sigmoid(x) and 1 - a, neither formed as a difference from 1. With
+// t = e^-|x| in [0, 1] they are 1 / (1 + t) and t / (1 + t). The power is 2^p of
+// the rounded product p = |x| log2(e), so t's relative error is some ulps and
+// grows with |x| (1e-6 at 16, where t itself is 1e-7). The scans are bound by
+// the instructions that they issue: exact range reduction and division, with
+// their cases for tiny numbers, took 2.5 times as many.
 __device__ __forceinline__ void gate_of(float x, float& a, float& rest) {
-    const float t = expf(-fabsf(x)), r = __fdividef(1.f, 1.f + t);
-    a = x >= 0.f ? r : t * r;
-    rest = x >= 0.f ? t * r : r;
+    float t, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(-1.44269504f * fabsf(x)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + t));
+    const float q = t * r;
+    a = x >= 0.f ? r : q;
+    rest = x >= 0.f ? q : r;
 }
 
 __device__ __forceinline__ int64_t length_of(const int32_t* lengths, int64_t b, int64_t steps) {
@@ -205,22 +214,25 @@ recurrence_kernel(SeqIn gate, SeqIn value, int64_t steps, int D, const float* h0
             for (int r = 0; r < written; ++r) store_two<PAIR>(out + (int64_t)r * D, make_float2(0.f, 0.f), second);
         return;
     }
+    // whether all steps and channels of the warp are there: no tests in the loops then
+    const bool whole_warp = inside == R && c - 2 * lane + kChannels <= D;
     float2 a[R], u[R];
-    {
+    const auto load = [&](auto known) {
+        constexpr bool ALL = decltype(known)::value;
         Two<T> graw[R], vraw[R];
         const T* g = static_cast<const T*>(gate.p) + at.b * gate.seq + t0 * gate.step + c;
         const T* v = static_cast<const T*>(value.p) + at.b * value.seq + t0 * value.step + c;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (live && r < inside) {
-                graw[r] = load_two<PAIR>(g + r * gate.step, second);
-                vraw[r] = load_two<PAIR>(v + r * value.step, second);
+        for (int r = 0; r < R; ++r, g += gate.step, v += value.step)
+            if (ALL || (live && r < inside)) {
+                graw[r] = load_two<PAIR>(g, ALL || second);
+                vraw[r] = load_two<PAIR>(v, ALL || second);
             }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             a[r] = make_float2(1.f, 1.f);
             u[r] = make_float2(0.f, 0.f);
-            if (live && r < inside) {
+            if (ALL || (live && r < inside)) {
                 const float2 gr = graw[r].get(), vr = vraw[r].get();
                 float2 rest;
                 gate_of(gr.x, a[r].x, rest.x);
@@ -228,7 +240,11 @@ recurrence_kernel(SeqIn gate, SeqIn value, int64_t steps, int D, const float* h0
                 u[r] = make_float2(rest.x * vr.x, rest.y * vr.y);
             }
         }
-    }
+    };
+    if (whole_warp)
+        load(std::true_type{});
+    else
+        load(std::false_type{});
     Map m{a[0], u[0]};
 #pragma unroll
     for (int r = 1; r < R; ++r) m = then(m, Map{a[r], u[r]});
@@ -253,10 +269,18 @@ recurrence_kernel(SeqIn gate, SeqIn value, int64_t steps, int D, const float* h0
     }
     const bool last = inside > 0 && t0 + inside == n;
     if (n == 0 && warp == 0) store_two<false>(h_last + at.b * D + c, start, second);
+    if (whole_warp) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        s = apply(Map{a[r], u[r]}, s);  // beyond the length the identity
-        if (r < written) store_two<PAIR>(out + (int64_t)r * D, r < inside ? s : make_float2(0.f, 0.f), second);
+        for (int r = 0; r < R; ++r, out += D) {
+            s = apply(Map{a[r], u[r]}, s);
+            store_two<PAIR>(out, s, true);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r, out += D) {
+            s = apply(Map{a[r], u[r]}, s);  // beyond the length the identity
+            if (r < written) store_two<PAIR>(out, r < inside ? s : make_float2(0.f, 0.f), second);
+        }
     }
     if (last) store_two<false>(h_last + at.b * D + c, s, second);
 }
@@ -291,33 +315,39 @@ recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int64_t steps, int
             }
         return;
     }
+    const bool whole_warp = inside == R && c - 2 * lane + kChannels <= D;
     Two<T> vraw[R], oraw[R];
     float2 a[R], rest[R];
-    {
+    const auto load = [&](auto known) {
+        constexpr bool ALL = decltype(known)::value;
         Two<T> graw[R];
         const T* g = static_cast<const T*>(gate.p) + at.b * gate.seq + t0 * gate.step + c;
         const T* v = static_cast<const T*>(value.p) + at.b * value.seq + t0 * value.step + c;
         const T* o = static_cast<const T*>(dh.p) + at.b * dh.seq + t0 * dh.step + c;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            vraw[r] = oraw[r] = Two<T>{};
-            if (live && r < inside) {
-                graw[r] = load_two<PAIR>(g + r * gate.step, second);
-                vraw[r] = load_two<PAIR>(v + r * value.step, second);
-                oraw[r] = load_two<PAIR>(o + r * dh.step, second);
+        for (int r = 0; r < R; ++r, g += gate.step, v += value.step, o += dh.step) {
+            if (!ALL) vraw[r] = oraw[r] = Two<T>{};
+            if (ALL || (live && r < inside)) {
+                graw[r] = load_two<PAIR>(g, ALL || second);
+                vraw[r] = load_two<PAIR>(v, ALL || second);
+                oraw[r] = load_two<PAIR>(o, ALL || second);
             }
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             a[r] = make_float2(1.f, 1.f);
             rest[r] = make_float2(0.f, 0.f);
-            if (live && r < inside) {
+            if (ALL || (live && r < inside)) {
                 const float2 gr = graw[r].get();
                 gate_of(gr.x, a[r].x, rest[r].x);
                 gate_of(gr.y, a[r].y, rest[r].y);
             }
         }
-    }
+    };
+    if (whole_warp)
+        load(std::true_type{});
+    else
+        load(std::false_type{});
     // the thread's steps as a map of the state (forwards) and of the flow (backwards)
     Map m{make_float2(1.f, 1.f), make_float2(0.f, 0.f)};
     float2 flow = make_float2(0.f, 0.f);
@@ -362,18 +392,25 @@ recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int64_t steps, int
         away[r] = make_float2(s.x - v.x, s.y - v.y);
         s = apply(Map{a[r], make_float2(rest[r].x * v.x, rest[r].y * v.y)}, s);
     }
+    const auto finish = [&](auto known) {
+        constexpr bool ALL = decltype(known)::value;
+        T *dg = dgate + first_out + (R - 1) * grad_step, *dv = dvalue + first_out + (R - 1) * grad_step;
 #pragma unroll
-    for (int r = R - 1; r >= 0; --r) {
-        const float2 o = oraw[r].get(), g = make_float2(o.x + flow.x, o.y + flow.y);
-        flow = make_float2(a[r].x * g.x, a[r].y * g.y);
-        if (r < written) {
-            const float2 dv = make_float2(rest[r].x * g.x, rest[r].y * g.y);
-            float2 dg = make_float2(dv.x * away[r].x * a[r].x, dv.y * away[r].y * a[r].y);
-            if (r >= inside) dg = make_float2(0.f, 0.f);
-            store_two<PAIR>(dvalue + first_out + r * grad_step, r < inside ? dv : make_float2(0.f, 0.f), second);
-            store_two<PAIR>(dgate + first_out + r * grad_step, dg, second);
+        for (int r = R - 1; r >= 0; --r, dg -= grad_step, dv -= grad_step) {
+            const float2 o = oraw[r].get(), g = make_float2(o.x + flow.x, o.y + flow.y);
+            flow = make_float2(a[r].x * g.x, a[r].y * g.y);
+            const bool in = ALL || r < inside;
+            if (ALL || r < written) {
+                const float2 x = make_float2(rest[r].x * g.x, rest[r].y * g.y), zero = make_float2(0.f, 0.f);
+                store_two<PAIR>(dv, in ? x : zero, ALL || second);
+                store_two<PAIR>(dg, in ? make_float2(x.x * away[r].x * a[r].x, x.y * away[r].y * a[r].y) : zero, ALL || second);
+            }
         }
-    }
+    };
+    if (whole_warp)
+        finish(std::true_type{});
+    else
+        finish(std::false_type{});
     if (dh0 != nullptr && tile == 0 && warp == 0) store_two<false>(dh0 + at.b * D + c, flow, second);
 }
 
