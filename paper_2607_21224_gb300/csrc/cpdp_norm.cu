@@ -16,66 +16,6 @@ struct NormIn {
 // neighbours: piece j of thread t starts at element (j * TPR + t) * V. V is 16
 // bytes' worth where every row of every array starts at a multiple of that,
 // else 1. Rows of up to 1,024 elements take a warp, longer ones a block.
-template <typename T, int V>
-struct Piece;
-template <>
-struct Piece<float, 4> {
-    float4 v;
-    __device__ __forceinline__ float get(int e) const { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; }
-    __device__ __forceinline__ void load(const float* p) { v = __ldcs(reinterpret_cast<const float4*>(p)); }
-};
-template <>
-struct Piece<__nv_bfloat16, 8> {
-    uint4 v;
-    __device__ __forceinline__ float get(int e) const {
-        const uint32_t u = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
-        return __uint_as_float(e % 2 ? u & 0xffff0000u : u << 16);
-    }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
-};
-template <>
-struct Piece<float, 1> {
-    float v;
-    __device__ __forceinline__ float get(int) const { return v; }
-    __device__ __forceinline__ void load(const float* p) { v = __ldcs(p); }
-};
-template <>
-struct Piece<__nv_bfloat16, 1> {
-    uint16_t v;
-    __device__ __forceinline__ float get(int) const { return __uint_as_float(uint32_t(v) << 16); }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint16_t*>(p)); }
-};
-
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-template <int V>
-__device__ __forceinline__ void store_piece(float* p, const float* v) {
-    if constexpr (V == 4)
-        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else
-        *p = v[0];
-}
-template <int V>
-__device__ __forceinline__ void store_piece(__nv_bfloat16* p, const float* v) {
-    if constexpr (V == 8)
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]), pack(v[6], v[7]));
-    else if constexpr (V == 4)
-        *reinterpret_cast<uint2*>(p) = make_uint2(pack(v[0], v[1]), pack(v[2], v[3]));
-    else
-        *p = __float2bfloat16_rn(v[0]);
-}
-template <int V>
-__device__ __forceinline__ void store_codes(int8_t* p, const int* q) {
-    const auto word = [](const int* c) { return (c[0] & 255) | (c[1] & 255) << 8 | (c[2] & 255) << 16 | c[3] << 24; };
-    if constexpr (V == 8)
-        *reinterpret_cast<int2*>(p) = make_int2(word(q), word(q + 4));
-    else if constexpr (V == 4)
-        *reinterpret_cast<int*>(p) = word(q);
-    else
-        *p = static_cast<int8_t>(q[0]);
-}
 
 // The sum over the row's threads, of N values at once. Blocks use two sets of
 // partial sums in turn, so one barrier per row is enough.
