@@ -116,8 +116,12 @@ cpdp_status cpdp_restore(const int8_t *codes, const uint8_t *exponents, int W, i
  *         product's operands
  *   dW    dW_dtype, worker w's [O][I] at dW + w * dW_worker. The order of the
  *         sums is fixed by the sizes.
+ * A dy that is not bfloat16 at a multiple of 16 bytes, with strides of whole
+ * multiples of 8 elements and rows apart, is first copied to such a form in the
+ * workspace.
  */
-size_t cpdp_weight_gradient_workspace(int W, int64_t M, int O, int I);
+size_t cpdp_weight_gradient_workspace(const void *dy, int64_t dy_worker, int64_t dy_row, cpdp_dtype dy_dtype,
+                                      int W, int64_t M, int O, int I);
 cpdp_status cpdp_weight_gradient(const void *dy, int64_t dy_worker, int64_t dy_row, cpdp_dtype dy_dtype,
                                  const int8_t *codes, const uint8_t *exponents,
                                  int W, int64_t M, int O, int I,

@@ -128,8 +128,6 @@ struct Codes {
 };
 
 struct WeightGradient {
-    const void* dy;
-    int64_t dy_worker, dy_row;
     const int8_t* codes;
     const uint8_t* exponents;
     int64_t M;
@@ -140,10 +138,8 @@ struct WeightGradient {
     int64_t out_worker, out_split;
 };
 
-// T: dy's type. TENSOR: dy arrives by tensor copies (bfloat16, 16-byte aligned
-// strides); else the converting warps load it element by element. G: the
-// output's type.
-template <typename T, bool TENSOR, typename G>
+// G: the output's type.
+template <typename G>
 __global__ void __launch_bounds__(kThreads, 1)
 weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p) {
     extern __shared__ uint8_t raw[];
@@ -153,7 +149,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
     const uint32_t slots = (smem_at(raw) + 1023u) & ~1023u;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kSlots; ++s) {
-            barrier_init(&full[s], kConvertWarps + (TENSOR ? 1 : 0));
+            barrier_init(&full[s], kConvertWarps + 1);
             barrier_init(&empty[s], 1);
         }
         barrier_init(&done, 1);
@@ -177,7 +173,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
     const int steps = static_cast<int>((tokens + kStep - 1) / kStep);
 
     if (warp == kConvertWarps) {
-        if (TENSOR && lane == 0) {
+        if (lane == 0) {
             int k = 0;
             for (; k < steps; ++k) {
                 const int s = k % kSlots;
@@ -254,28 +250,6 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
                                      "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y)
                                      : "memory");
                     }
-                if (!TENSOR) {
-                    // rows of dy: the warp's 8 tokens, neighbouring elements in neighbouring lanes
-                    const T* dy = static_cast<const T*>(p.dy) + w * p.dy_worker + o0 + lane;
-#pragma unroll 2
-                    for (int r = 0; r < 8; ++r) {
-                        const int t = warp * 8 + r;
-                        const int64_t m = (int64_t)k * kStep + t;
-                        __nv_bfloat16 v[kTileO / 32];
-#pragma unroll
-                        for (int c = 0; c < kTileO / 32; ++c)
-                            v[c] = m < tokens && o0 + c * 32 + lane < p.O
-                                       ? from_float<__nv_bfloat16>(to_float(dy[(first + m) * p.dy_row + c * 32]))
-                                       : __ushort_as_bfloat16(0);
-#pragma unroll
-                        for (int c = 0; c < kTileO / 32; ++c) {
-                            const int o = c * 32 + lane;
-                            const uint32_t at = slots + s * kSlotBytes + kXBytes + (o / 64) * kBlockBytes + t * 128 +
-                                                (((o % 64 / 8) ^ (t % 8)) << 4) + o % 8 * 2;
-                            asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(__bfloat16_as_ushort(v[c])) : "memory");
-                        }
-                    }
-                }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) barrier_arrive(&full[s]);
@@ -301,6 +275,38 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
     if (warp == kConvertWarps + 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(kTileO));
+    }
+}
+
+// dy as the tensor copies need it: bfloat16 rows at multiples of 16 bytes. A
+// warp per row, two elements per lane: out of two neighbouring 32-bit words
+// where the row starts between words. Only words that hold elements of the row
+// are read.
+template <typename T>
+__global__ void __launch_bounds__(256)
+align_kernel(const T* dy, int64_t dy_worker, int64_t dy_row, int64_t M, int64_t rows, int O, int pitch, uint32_t* out) {
+    layer_begin();
+    const int lane = threadIdx.x % 32, words = (O + 1) / 2;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; row < rows; row += (int64_t)gridDim.x * 8) {
+        const int64_t w = row / M;
+        const T* p = dy + w * dy_worker + (row - w * M) * dy_row;
+        uint32_t* to = out + row * (pitch / 2);
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll 4
+            for (int k = lane; k < words; k += 32) {
+                const __nv_bfloat162 v = __floats2bfloat162_rn(p[2 * k], 2 * k + 1 < O ? p[2 * k + 1] : 0.f);
+                to[k] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+        } else {
+            const bool between = reinterpret_cast<uintptr_t>(p) % 4 != 0;
+            const uint32_t* q = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(3));
+            const int held = (O + between + 1) / 2;  // words that hold the row's elements
+#pragma unroll 4
+            for (int k = lane; k < words; k += 32) {
+                const uint32_t a = __ldg(q + k), b = between && k + 1 < held ? __ldg(q + k + 1) : 0u;
+                to[k] = between ? __byte_perm(a, b, 0x5432) : a;
+            }
+        }
     }
 }
 
@@ -364,10 +370,23 @@ static cpdp_status check_weight_gradient(int W, int64_t M, int O, int I) {
     return CPDP_OK;
 }
 
-size_t cpdp_weight_gradient_workspace(int W, int64_t M, int O, int I) {
-    if (check_weight_gradient(W, M, O, I) != CPDP_OK) return 0;
+// Whether the tensor copies can read dy where it is. A stride that no index
+// uses does not matter.
+static bool in_place(const void* dy, int64_t dy_worker, int64_t dy_row, cpdp_dtype dtype, int W, int64_t M, int O) {
+    return dtype == CPDP_BF16 && aligned_to(dy, 16) && (M <= 1 || (dy_row % 8 == 0 && dy_row >= O)) &&
+           (W <= 1 || (dy_worker % 8 == 0 && dy_worker > 0));
+}
+static size_t parts_bytes(int W, int64_t M, int O, int I) {
     const int count = splits_of(W, M, O, I).count;
-    return count > 1 ? static_cast<size_t>(count) * W * O * I * 4 : 0;
+    return count > 1 ? ceil_div(static_cast<int64_t>(count) * W * O * I * 4, 16) * 16 : 0;
+}
+static int64_t pitch_of(int O) { return ceil_div(O, 8) * 8; }
+
+size_t cpdp_weight_gradient_workspace(const void* dy, int64_t dy_worker, int64_t dy_row, cpdp_dtype dy_dtype, int W, int64_t M, int O,
+                                      int I) {
+    if (check_weight_gradient(W, M, O, I) != CPDP_OK) return 0;
+    const size_t copy = in_place(dy, dy_worker, dy_row, dy_dtype, W, M, O) ? 0 : static_cast<size_t>(W) * M * pitch_of(O) * 2;
+    return parts_bytes(W, M, O, I) + copy;
 }
 
 cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_row, cpdp_dtype dy_dtype,
@@ -381,11 +400,10 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     CPDP_TRY(check_array("codes", codes, M > 0, 16));
     CPDP_TRY(check_array("exponents", exponents, M > 0, 1));
     CPDP_TRY(check_array("dW", dW, true, dtype_size(dW_dtype), dW_worker));
-    CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_weight_gradient_workspace(W, M, O, I)));
+    CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_weight_gradient_workspace(dy, dy_worker, dy_row, dy_dtype, W, M, O, I)));
     const Splits sp = splits_of(W, M, O, I);
     const bool parts = sp.count > 1;
     WeightGradient p{};
-    p.dy = dy, p.dy_worker = dy_worker, p.dy_row = dy_row;
     p.codes = codes, p.exponents = exponents;
     p.M = M, p.O = O, p.I = I, p.W = W, p.blocks = static_cast<int>(ceil_div(I, kBlock8));
     p.splits = sp.count, p.split_steps = sp.each;
@@ -393,11 +411,23 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     p.out_worker = parts ? (int64_t)O * I : dW_worker;
     p.out_split = (int64_t)W * O * I;
 
-    // Tensor copies of dy: bfloat16, rows and workers at multiples of 16 bytes.
     CUtensorMap map{};
-    const int64_t rows = M > 1 ? dy_row : ceil_div(O, 8) * 8, workers = W > 1 ? dy_worker : rows * M;
-    const bool tensor = dy_dtype == CPDP_BF16 && M > 0 && aligned_to(dy, 16) && rows % 8 == 0 && rows >= O && workers % 8 == 0 && workers > 0;
-    if (tensor) {
+    if (M > 0) {
+        int64_t rows = dy_row, workers = dy_worker;
+        if (!in_place(dy, dy_worker, dy_row, dy_dtype, W, M, O)) {
+            char* copy = static_cast<char*>(workspace) + parts_bytes(W, M, O, I);
+            const int64_t all = W * M, blocks = ceil_div(all, 8) < kSMs * 8 ? ceil_div(all, 8) : kSMs * 8;
+            const auto align = [&](auto* in) {
+                return launch_layer(align_kernel<std::remove_const_t<std::remove_pointer_t<decltype(in)>>>, static_cast<unsigned>(blocks), 256,
+                                    0, stream, in, dy_worker, dy_row, M, all, O, static_cast<int>(pitch_of(O)),
+                                    reinterpret_cast<uint32_t*>(copy));
+            };
+            CPDP_TRY(layer_launched(dy_dtype == CPDP_F32 ? align(static_cast<const float*>(dy)) : align(static_cast<const __nv_bfloat16*>(dy)),
+                                    "cpdp_weight_gradient"));
+            dy = copy, rows = pitch_of(O), workers = rows * M;
+        }
+        if (M == 1) rows = pitch_of(O);  // strides that no index uses
+        if (W == 1) workers = rows * M;
         const EncodeTiled encode = encode_tiled();
         if (encode == nullptr) return layer_error(CPDP_ECUDA, "the CUDA driver has no cuTensorMapEncodeTiled");
         const cuuint64_t dims[3] = {(cuuint64_t)O, (cuuint64_t)M, (cuuint64_t)W}, strides[2] = {(cuuint64_t)rows * 2, (cuuint64_t)workers * 2};
@@ -414,9 +444,7 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     };
     const auto typed = [&](auto g) {
         using G = decltype(g);
-        return dy_dtype == CPDP_F32 ? go(weight_gradient_kernel<float, false, G>)
-               : tensor             ? go(weight_gradient_kernel<__nv_bfloat16, true, G>)
-                                    : go(weight_gradient_kernel<__nv_bfloat16, false, G>);
+        return go(weight_gradient_kernel<G>);
     };
     CPDP_TRY(layer_launched(parts || dW_dtype == CPDP_F32 ? typed(0.f) : typed(__nv_bfloat16{}), "cpdp_weight_gradient"));
     if (!parts) return CPDP_OK;

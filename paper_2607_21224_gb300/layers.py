@@ -48,7 +48,7 @@ SIGNATURES = {
                                        _Z, _P]),
     "cpdp_checkpoint": (_I, [_P, _L, _L, _I, _I, _L, _I, _P, _P, _P, _P]),
     "cpdp_restore": (_I, [_P, _P, _I, _L, _I, _P, _P]),
-    "cpdp_weight_gradient_workspace": (_Z, [_I, _L, _I, _I]),
+    "cpdp_weight_gradient_workspace": (_Z, [_P, _L, _L, _I, _I, _L, _I, _I]),
     "cpdp_weight_gradient": (_I, [_P, _L, _L, _I, _P, _P, _I, _L, _I, _I, _P, _L, _I, _P, _Z, _P]),
     "cpdp_gated_recurrence_workspace": (_Z, [_I, _L, _I]),
     "cpdp_gated_recurrence": (_I, [_P, _L, _L, _P, _L, _L, _I, _I, _L, _I, _P, _P, _P, _P, _P, _P, _Z, _P]),
@@ -316,7 +316,7 @@ def weight_gradient(dy, saved: Checkpoint, *, out=None, dtype=torch.float32, str
     _input(dy, "dy", (W, M, O), dy.dtype, device)
     out = _gradient_out(out, "out", (W, O, D), dtype, device)
     L = lib()
-    ws = _workspace(L.cpdp_weight_gradient_workspace(W, M, O, D), device)
+    ws = _workspace(L.cpdp_weight_gradient_workspace(dy.data_ptr(), dy.stride(0), dy.stride(1), code, W, M, O, D), device)
     _check(L.cpdp_weight_gradient(
         dy.data_ptr(), dy.stride(0), dy.stride(1), code, saved.codes.data_ptr(), saved.exponents.data_ptr(), W, M, O, D,
         out.data_ptr(), out.stride(0), _CODES[out.dtype], _ptr(ws), ws.numel() if ws is not None else 0, _stream(device)))

@@ -79,7 +79,7 @@ def test_refused_alignment(name, i):
 def test_workspace_sizes_of_refused_sizes_are_zero():
     L = layers.lib()
     assert L.cpdp_add_rmsnorm_backward_workspace(0, 5, 32) == 0
-    assert L.cpdp_weight_gradient_workspace(1, -1, 32, 32) == 0
+    assert L.cpdp_weight_gradient_workspace(P, 320, 32, 1, 1, -1, 32, 32) == 0
     assert L.cpdp_gated_recurrence_workspace(1, 1 << 50, 32) == 0
 
 
