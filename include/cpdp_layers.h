@@ -58,7 +58,7 @@ extern "C" {
 #define CPDP_NORM_MAX_FEATURES 16384
 
 /* The recurrence keeps the state at every so many steps for its backward pass. */
-#define CPDP_CARRY_STEPS 64
+#define CPDP_CARRY_STEPS 16
 
 /*
  * cpdp_add_rmsnorm — the residual's addition and the norm.
@@ -130,7 +130,7 @@ cpdp_status cpdp_weight_gradient(const void *dy, int64_t dy_worker, int64_t dy_r
 
 /*
  * cpdp_gated_recurrence — h_t = a_t h_(t-1) + (1 - a_t) v_t with
- * a = sigmoid(gate), for B sequences of T steps and D channels.
+ * a = sigmoid(gate), for B <= 65535 sequences of T <= 2^30 steps and D channels.
  *   gate, value  [B][T][D] of dtype, with a sequence and a step stride
  *   h0           float32 [B][D], the states before the first step (NULL: 0)
  *   lengths      int32 [B], each sequence's number of steps, clamped to 0..T
@@ -181,11 +181,10 @@ cpdp_status cpdp_gated_recurrence_step(const void *gate, int64_t gate_seq, const
                                        cpdp_dtype dtype, int B, int D, float *state, void *h, void *stream);
 
 /*
- * cpdp_layer_timeouts — the number of bounded waits in these kernels that ran
- * out since the last call (0 expected; results after one are not valid). The
- * blocks of a long sequence wait for one another's results, and the weight
- * gradient's warps for their slots, each wait for some seconds at most. Waits
- * for the device.
+ * cpdp_layer_timeouts — the number of bounded waits that ran out since the last
+ * call (0 expected; results after one are not valid): the weight gradient's
+ * warps wait for the slots of a ring, for some seconds at most. Waits for the
+ * device.
  */
 cpdp_status cpdp_layer_timeouts(int64_t *count);
 

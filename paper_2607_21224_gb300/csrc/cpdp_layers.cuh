@@ -15,9 +15,6 @@ cpdp_status layer_error(cpdp_status st, const char* fmt, ...);
 // CPDP_OK, or CPDP_ECUDA with the launch's error (else one that the runtime recorded).
 cpdp_status layer_launched(cudaError_t launched, const char* what);
 
-// The weight gradient's bounded waits that ran out, read and set to 0.
-cudaError_t take_weight_gradient_timeouts(unsigned long long* count);
-
 constexpr int64_t kLayerMaxElements = int64_t(1) << 40;
 constexpr int64_t kLayerMaxRows = (int64_t(1) << 31) - 1;
 constexpr int kSMs = 152;

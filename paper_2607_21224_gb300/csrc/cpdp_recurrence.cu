@@ -7,17 +7,19 @@
 namespace cpdp {
 namespace {
 
-constexpr int kThreads = 128;   // of the single step's kernel
-constexpr int kWarps = 8;       // of a tile: each takes R consecutive steps
-constexpr int kChannels = 64;   // of a tile: two per lane
-constexpr int kForwardSteps = 16, kBackwardSteps = 8;  // R
-constexpr int kForwardTile = kWarps * kForwardSteps, kBackwardTile = kWarps * kBackwardSteps;
-constexpr int kGroup = 16;      // tiles between two published states
-constexpr int kSpinLimit = 1 << 22;
-static_assert(kBackwardTile == CPDP_CARRY_STEPS, "a backward tile starts from a carry");
-static_assert(kForwardTile % CPDP_CARRY_STEPS == 0 && CPDP_CARRY_STEPS % kForwardSteps == 0, "carries fall on warps' first steps");
-
-__device__ unsigned long long wait_timeouts;  // bounded waits that ran out
+constexpr int kThreads = 128;       // of the single step's kernel
+constexpr int kWarps = 4;           // per block of the scans
+constexpr int kChannels = 64;       // per warp: two per lane
+constexpr int R = CPDP_CARRY_STEPS; // steps of a chunk
+// Slots of a warp's ring of chunks, and the warps per SM that registers and
+// shared memory then allow: 8 warps with two chunks each in flight reach the
+// memory's rate.
+constexpr int kForwardRing = 3;
+template <typename T>
+constexpr int kBackwardRing = sizeof(T) == 2 ? 3 : 2;
+template <typename T>
+constexpr int kForwardWarps = sizeof(T) == 2 ? 16 : 8;
+constexpr int kBackwardWarps = 8;
 
 struct SeqIn {
     const void* p;
@@ -30,388 +32,400 @@ struct SeqIn {
 // grows with |x| (1e-6 at 16, where t itself is 1e-7). The scans are bound by
 // the instructions that they issue: exact range reduction and division, with
 // their cases for tiny numbers, took 2.5 times as many.
-__device__ __forceinline__ void gate_of(float x, float& a, float& rest) {
-    float t, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(-1.44269504f * fabsf(x)));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + t));
-    const float q = t * r;
-    a = x >= 0.f ? r : q;
-    rest = x >= 0.f ? q : r;
+// Two floats in a pair of registers, for the instructions that work on both.
+using Pair = unsigned long long;
+constexpr Pair kOnes = 0x3f8000003f800000ull, kZeros = 0, kMinusOnes = 0xbf800000bf800000ull;
+__device__ __forceinline__ Pair pair(float x, float y) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
+    return p;
 }
-
-__device__ __forceinline__ int64_t length_of(const int32_t* lengths, int64_t b, int64_t steps) {
-    return lengths == nullptr ? steps : min(max((int64_t)lengths[b], (int64_t)0), steps);
-}
-
-// Two neighbouring channels as they lie in memory. PAIR: one load or store,
-// possible where D and the strides are even and the pointers aligned to two
-// elements; else element by element, `second` telling whether there are two.
-template <typename T>
-struct Two;
-template <>
-struct Two<float> {
+__device__ __forceinline__ float2 floats(Pair p) {
     float2 v;
-    __device__ __forceinline__ float2 get() const { return v; }
-};
-template <>
-struct Two<__nv_bfloat16> {
-    uint32_t v;
-    __device__ __forceinline__ float2 get() const { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
-};
-template <bool PAIR>
-__device__ __forceinline__ Two<float> load_two(const float* p, bool second) {
-    if (PAIR) return {__ldcs(reinterpret_cast<const float2*>(p))};
-    return {make_float2(__ldcs(p), second ? __ldcs(p + 1) : 0.f)};
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
 }
-template <bool PAIR>
-__device__ __forceinline__ Two<__nv_bfloat16> load_two(const __nv_bfloat16* p, bool second) {
-    if (PAIR) return {__ldcs(reinterpret_cast<const uint32_t*>(p))};
-    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-    return {static_cast<uint32_t>(__ldcs(q)) | (second ? static_cast<uint32_t>(__ldcs(q + 1)) << 16 : 0u)};
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
 }
-template <bool PAIR>
-__device__ __forceinline__ void store_two(float* p, float2 v, bool second) {
-    if (PAIR) {
-        *reinterpret_cast<float2*>(p) = v;
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float power_of_minus(float x) {
+    float t;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(-1.44269504f * fabsf(x)));
+    return t;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ void gate_of(Pair gates, Pair& a, Pair& rest) {
+    const float2 x = floats(gates);
+    const Pair t = pair(power_of_minus(x.x), power_of_minus(x.y));
+    const float2 s = floats(add2(t, kOnes)), r = make_float2(reciprocal(s.x), reciprocal(s.y)), q = floats(mul2(t, pair(r.x, r.y)));
+    a = pair(x.x >= 0.f ? r.x : q.x, x.y >= 0.f ? r.y : q.y);
+    rest = pair(x.x >= 0.f ? q.x : r.x, x.y >= 0.f ? q.y : r.y);
+}
+
+// A lane's two channels. WIDE, where every row starts at a multiple of 16
+// bytes: neighbours, moved together. Else 32 apart, moved one by one, each with
+// the other lanes' next to it.
+template <bool WIDE>
+__device__ __forceinline__ int first_channel(int lane) { return WIDE ? 2 * lane : lane; }
+template <bool WIDE>
+constexpr int kSecond = WIDE ? 1 : 32;
+
+__device__ __forceinline__ Pair pair_at(const float* p) { return *reinterpret_cast<const Pair*>(p); }
+__device__ __forceinline__ Pair pair_at(const __nv_bfloat16* p) {
+    const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+    return pair(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+template <bool WIDE>
+__device__ __forceinline__ void store_two(float* p, Pair both, bool second) {
+    const float2 v = floats(both);
+    if (WIDE) {
+        *reinterpret_cast<Pair*>(p) = both;
     } else {
         p[0] = v.x;
-        if (second) p[1] = v.y;
+        if (second) p[32] = v.y;
     }
 }
-template <bool PAIR>
-__device__ __forceinline__ void store_two(__nv_bfloat16* p, float2 v, bool second) {
-    if (PAIR) {
+template <bool WIDE>
+__device__ __forceinline__ void store_two(__nv_bfloat16* p, Pair both, bool second) {
+    const float2 v = floats(both);
+    if (WIDE) {
         *reinterpret_cast<__nv_bfloat162*>(p) = __float22bfloat162_rn(v);
     } else {
         p[0] = __float2bfloat16_rn(v.x);
-        if (second) p[1] = __float2bfloat16_rn(v.y);
+        if (second) p[32] = __float2bfloat16_rn(v.y);
     }
+}
+// Two float32 channels that need not be aligned.
+template <bool WIDE>
+__device__ __forceinline__ Pair load_state(const float* p, bool second) { return pair(p[0], second ? p[kSecond<WIDE>] : 0.f); }
+template <bool WIDE>
+__device__ __forceinline__ void store_state(float* p, Pair s, bool second) {
+    const float2 v = floats(s);
+    p[0] = v.x;
+    if (second) p[kSecond<WIDE>] = v.y;
 }
 
 // x -> a x + b for two channels, and one such map after another.
-struct Map {
-    float2 a, b;
+struct alignas(16) Map {
+    Pair a, b;
 };
-__device__ __forceinline__ float2 apply(const Map& m, float2 x) { return make_float2(fmaf(m.a.x, x.x, m.b.x), fmaf(m.a.y, x.y, m.b.y)); }
+constexpr Map kSame{kOnes, kZeros};
+__device__ __forceinline__ Pair apply(const Map& m, Pair x) { return fma2(m.a, x, m.b); }
 __device__ __forceinline__ Map then(const Map& first, const Map& second) {
-    return {make_float2(second.a.x * first.a.x, second.a.y * first.a.y), apply(second, first.b)};
+    return {mul2(second.a, first.a), apply(second, first.b)};
 }
 
-// What tiles tell each other, in the workspace: for every tile and channel its
-// map (a, b) in one 64-bit word, and for every group of tiles and channel the
-// state after it in 32 bits. All ones means "not there yet" (the workspace is
-// set to that before the launch); no arithmetic makes that NaN, and a value
-// that has it is stored as the usual NaN. A word is written whole, so the
-// readers need no flag and no fence.
-struct Exchange {
-    unsigned* ticket;
-    uint64_t* maps;    // [B][tiles][channels]
-    uint32_t* states;  // [B][groups][channels]
-    int tiles, groups, channels;  // channels: a multiple of kChannels
+// How the scans are shared out. A warp takes 64 channels of a sequence (a
+// column) and walks a segment of its steps, the state in registers. Where
+// there are columns enough, a segment is the whole sequence. Else the steps are
+// split into `count` segments (1, 2 or a multiple of 4) of `steps` (a
+// multiple of R): a first pass makes each segment's map of the state, a second
+// one composes the maps before its segment and walks. `order` counts segments
+// from where the scan starts.
+struct Segments {
+    int count, steps, groups;  // groups of channels per sequence
+    int64_t columns;
+    Map* maps;                 // [columns][count][32 lanes]
 };
-
-__device__ __forceinline__ uint32_t told(float x) {
-    const uint32_t u = __float_as_uint(x);
-    return u == 0xffffffffu ? 0x7fffffffu : u;
-}
-__device__ __forceinline__ void tell_map(uint64_t* p, const Map& m) {
-    const uint64_t x = (uint64_t)told(m.a.x) << 32 | __float_as_uint(m.b.x), y = (uint64_t)told(m.a.y) << 32 | __float_as_uint(m.b.y);
-    asm volatile("st.relaxed.gpu.global.v2.b64 [%0], {%1, %2};" ::"l"(p), "l"(x), "l"(y) : "memory");
-}
-__device__ __forceinline__ void tell_state(uint32_t* p, float2 s) {
-    asm volatile("st.relaxed.gpu.global.v2.b32 [%0], {%1, %2};" ::"l"(p), "r"(told(s.x)), "r"(told(s.y)) : "memory");
-}
-// The waits are bounded: one that runs out is counted and answers NaN. Tiles
-// take tickets in the order of their dependences, so what a tile waits for
-// comes from blocks that are running or done.
-__device__ __forceinline__ Map hear_map(const uint64_t* p) {
-    uint64_t x, y;
-    for (int i = 0; i < kSpinLimit; ++i) {
-        asm volatile("ld.relaxed.gpu.global.v2.b64 {%0, %1}, [%2];" : "=l"(x), "=l"(y) : "l"(p) : "memory");
-        if ((x >> 32) != 0xffffffffu && (y >> 32) != 0xffffffffu)
-            return {make_float2(__uint_as_float(x >> 32), __uint_as_float(y >> 32)), make_float2(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)y))};
-    }
-    atomicAdd(&wait_timeouts, 1ull);
-    const float nan = __uint_as_float(0x7fffffffu);
-    return {make_float2(nan, nan), make_float2(nan, nan)};
-}
-__device__ __forceinline__ float2 hear_state(const uint32_t* p) {
-    uint32_t x, y;
-    for (int i = 0; i < kSpinLimit; ++i) {
-        asm volatile("ld.relaxed.gpu.global.v2.b32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "l"(p) : "memory");
-        if (x != 0xffffffffu && y != 0xffffffffu) return make_float2(__uint_as_float(x), __uint_as_float(y));
-    }
-    atomicAdd(&wait_timeouts, 1ull);
-    return make_float2(__uint_as_float(0x7fffffffu), __uint_as_float(0x7fffffffu));
+struct Task {
+    int64_t column;
+    int b, channel, order;
+};
+__device__ __forceinline__ Task task_of(const Segments& x) {
+    const int64_t i = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32, column = i / x.count;
+    const int b = static_cast<int>(column / x.groups);
+    return {column, b, static_cast<int>(column - (int64_t)b * x.groups) * kChannels, static_cast<int>(i - column * x.count)};
 }
 
-// The state before the `order`-th tile of a sequence, counted from where the
-// scan starts; tile_at(i) is the i-th tile's index, `start` the scan's first
-// state. The group's earlier tiles are heard by all warps, two each, and the
-// group before by the last one; the maps are applied in the scan's order, so
-// the result does not depend on which tile was ready when.
-template <typename TileAt>
-__device__ __forceinline__ float2 state_before(const Exchange& x, int64_t b, int channel, int order, TileAt tile_at, float2 start,
-                                               Map (*maps)[32], float2* state) {
-    constexpr int kEach = kGroup / kWarps;
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, first = order - order % kGroup, group = order / kGroup;
-    Map m{make_float2(1.f, 1.f), make_float2(0.f, 0.f)};
+// The state before the task's segment: the maps of the segments before it
+// applied to `start`, in an order fixed by their number. Those before the
+// block's first are composed by its warps together.
+__device__ __forceinline__ Pair state_before(const Segments& x, const Task& task, Pair start) {
+    __shared__ Map parts[kWarps][32];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, first = x.count >= kWarps ? task.order - warp : 0;
+    const Map* maps = x.maps + task.column * x.count * 32 + lane;
+    Pair s = start;
+    if (first > 0) {  // the same for all warps of the block
+        const int each = (first + kWarps - 1) / kWarps, end = min(first, (warp + 1) * each);
+        Map m = kSame;
+#pragma unroll 8
+        for (int i = warp * each; i < end; ++i) m = then(m, maps[i * 32]);
+        parts[warp][lane] = m;
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int at = first + warp * kEach + i;
-        if (at < order) m = then(m, hear_map(x.maps + ((int64_t)b * x.tiles + tile_at(at)) * x.channels + channel));
+        for (int i = 0; i < kWarps; ++i) s = apply(parts[i][lane], s);
     }
-    maps[warp][lane] = m;
-    if (warp == kWarps - 1)
-        state[lane] = group > 0 ? hear_state(x.states + ((int64_t)b * x.groups + group - 1) * x.channels + channel) : start;
-    __syncthreads();
-    float2 s = state[lane];
-    const int heard = (order - first + kEach - 1) / kEach;
-    for (int i = 0; i < heard; ++i) s = apply(maps[i][lane], s);
+#pragma unroll 8
+    for (int i = first; i < task.order; ++i) s = apply(maps[i * 32], s);
     return s;
 }
 
-// The block's place: tiles in the order of the scan, all sequences and
-// channels of one before the next.
-struct Place {
-    int order, channel;
-    int64_t b;
-};
-__device__ __forceinline__ Place take_place(const Exchange& x, int columns) {
-    __shared__ unsigned ticket;
-    unsigned id = blockIdx.x;
-    if (x.tiles > 1) {
-        if (threadIdx.x == 0) ticket = atomicAdd(x.ticket, 1u) + 1u;  // from all ones
-        __syncthreads();
-        id = ticket;
-    }
-    const int per = x.channels / kChannels, c = id % columns;
-    return {static_cast<int>(id / columns), c % per * kChannels + static_cast<int>(threadIdx.x % 32) * 2, c / per};
-}
+// A chunk of R steps of the warp's channels, brought by asynchronous 16-byte
+// copies into the warp's ring in shared memory, some chunks before its use.
+// Where rows do not start at multiples of 16 bytes, the copies start at the
+// multiple before (the same 16 bytes hold the row's first element), and a row
+// has its first element that much further in its slot.
+template <typename T, bool WIDE>
+constexpr int kRowBytes = kChannels * sizeof(T) + (WIDE ? 0 : 16);
+template <typename T, bool WIDE>
+constexpr int kChunkBytes = R * kRowBytes<T, WIDE>;
 
-// Forward pass: one block per tile of kForwardTile steps and 64 channels, R
-// steps of a pair of channels per thread, read once and kept in registers. A
-// tile's steps compose to one map of the state; the warps exchange theirs in
-// shared memory, the tiles through `x`, and with the state before its steps
-// each thread runs through them again.
-template <typename T, bool PAIR>
-__global__ void __launch_bounds__(kWarps * 32, 2)
-recurrence_kernel(SeqIn gate, SeqIn value, int64_t steps, int D, const float* h0, const int32_t* lengths, T* h, float* h_last,
-                  float* carry, Exchange x, int columns) {
-    layer_begin();
-    constexpr int R = kForwardSteps;
-    __shared__ Map own[kWarps][32], heard[kWarps][32];
-    __shared__ float2 state[32];
-    const Place at = take_place(x, columns);
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = at.channel;
-    const bool live = c < D, second = c + 1 < D;
-    const int64_t n = length_of(lengths, at.b, steps), tile0 = (int64_t)at.order * kForwardTile, t0 = tile0 + warp * R;
-    const int inside = static_cast<int>(min(max(n - t0, (int64_t)0), (int64_t)R));  // of the thread's steps
-    const int written = static_cast<int>(min(max(steps - t0, (int64_t)0), (int64_t)R));
-    T* out = h + (at.b * steps + t0) * D + c;
-    if (tile0 >= n && at.order > 0) {  // wholly beyond the length: nothing to hear or to tell
-        if (live)
-            for (int r = 0; r < written; ++r) store_two<PAIR>(out + (int64_t)r * D, make_float2(0.f, 0.f), second);
-        return;
-    }
-    // whether all steps and channels of the warp are there: no tests in the loops then
-    const bool whole_warp = inside == R && c - 2 * lane + kChannels <= D;
-    float2 a[R], u[R];
-    const auto load = [&](auto known) {
-        constexpr bool ALL = decltype(known)::value;
-        Two<T> graw[R], vraw[R];
-        const T* g = static_cast<const T*>(gate.p) + at.b * gate.seq + t0 * gate.step + c;
-        const T* v = static_cast<const T*>(value.p) + at.b * value.seq + t0 * value.step + c;
+__device__ __forceinline__ void copy_16(uint32_t to, const void* from, int bytes) {  // the rest of the 16 is set to 0
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+template <typename T, bool WIDE>
+__device__ __forceinline__ void fill(uint8_t* to, const T* from, int64_t step, int rows, int channels) {
+    const int lane = threadIdx.x % 32;
+    const uint32_t slot = static_cast<uint32_t>(__cvta_generic_to_shared(to));
+    if constexpr (WIDE) {
+        constexpr int each = 16 / sizeof(T), per_row = kChannels / each, down = 32 / per_row;  // rows per round
+        const int c = lane % per_row * each, r0 = lane / per_row;
+        const bool there = c < channels;
+        const T* p = from + r0 * step + c;
+        const uint32_t at = slot + (r0 * kChannels + c) * sizeof(T);
 #pragma unroll
-        for (int r = 0; r < R; ++r, g += gate.step, v += value.step)
-            if (ALL || (live && r < inside)) {
-                graw[r] = load_two<PAIR>(g, ALL || second);
-                vraw[r] = load_two<PAIR>(v, ALL || second);
-            }
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            a[r] = make_float2(1.f, 1.f);
-            u[r] = make_float2(0.f, 0.f);
-            if (ALL || (live && r < inside)) {
-                const float2 gr = graw[r].get(), vr = vraw[r].get();
-                float2 rest;
-                gate_of(gr.x, a[r].x, rest.x);
-                gate_of(gr.y, a[r].y, rest.y);
-                u[r] = make_float2(rest.x * vr.x, rest.y * vr.y);
-            }
-        }
-    };
-    if (whole_warp)
-        load(std::true_type{});
-    else
-        load(std::false_type{});
-    Map m{a[0], u[0]};
-#pragma unroll
-    for (int r = 1; r < R; ++r) m = then(m, Map{a[r], u[r]});
-    own[warp][lane] = m;
-    __syncthreads();
-    const bool more = n > tile0 + kForwardTile;  // a later tile has steps
-    Map whole = own[0][lane];
-    if (more && warp == 0) {
-        for (int i = 1; i < kWarps; ++i) whole = then(whole, own[i][lane]);
-        tell_map(x.maps + (at.b * x.tiles + at.order) * x.channels + c, whole);
-    }
-    const float2 start = h0 != nullptr && live ? make_float2(h0[at.b * D + c], second ? h0[at.b * D + c + 1] : 0.f) : make_float2(0.f, 0.f);
-    float2 s = start;
-    if (at.order > 0) s = state_before(x, at.b, c, at.order, [](int i) { return i; }, start, heard, state);
-    if (more && warp == 0 && at.order % kGroup == kGroup - 1)
-        tell_state(x.states + (at.b * x.groups + at.order / kGroup) * x.channels + c, apply(whole, s));
-    for (int i = 0; i < warp; ++i) s = apply(own[i][lane], s);
-    if (!live) return;
-    if (carry != nullptr && inside > 0 && t0 % CPDP_CARRY_STEPS == 0) {
-        const int64_t carries = (steps + CPDP_CARRY_STEPS - 1) / CPDP_CARRY_STEPS;
-        store_two<false>(carry + (at.b * carries + t0 / CPDP_CARRY_STEPS) * D + c, s, second);
-    }
-    const bool last = inside > 0 && t0 + inside == n;
-    if (n == 0 && warp == 0) store_two<false>(h_last + at.b * D + c, start, second);
-    if (whole_warp) {
-#pragma unroll
-        for (int r = 0; r < R; ++r, out += D) {
-            s = apply(Map{a[r], u[r]}, s);
-            store_two<PAIR>(out, s, true);
+        for (int k = 0; k < R / down; ++k, p += down * step) {
+            const bool here = there && r0 + k * down < rows;
+            copy_16(at + k * down * kRowBytes<T, true>, here ? p : from, here ? 16 : 0);
         }
     } else {
+        constexpr int per_row = kRowBytes<T, false> / 16, all = R * per_row;
+        const int width = min(channels, kChannels) * static_cast<int>(sizeof(T));
 #pragma unroll
-        for (int r = 0; r < R; ++r, out += D) {
-            s = apply(Map{a[r], u[r]}, s);  // beyond the length the identity
-            if (r < written) store_two<PAIR>(out, r < inside ? s : make_float2(0.f, 0.f), second);
+        for (int k = 0; k < (all + 31) / 32; ++k) {
+            const int i = k * 32 + lane, r = i / per_row, piece = i % per_row;
+            if (k * 32 + 32 > all && i >= all) break;
+            const uintptr_t row = reinterpret_cast<uintptr_t>(from + min(r, rows - 1) * step), first = (row & ~uintptr_t(15)) + piece * 16;
+            const int bytes = r < rows ? static_cast<int>(min(max((int64_t)(row + width - first), (int64_t)0), (int64_t)16)) : 0;
+            copy_16(slot + i * 16, reinterpret_cast<const void*>(bytes > 0 ? first : row & ~uintptr_t(15)), bytes);
         }
     }
-    if (last) store_two<false>(h_last + at.b * D + c, s, second);
+}
+__device__ __forceinline__ void end_fill() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LATER>
+__device__ __forceinline__ void wait_filled() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(LATER) : "memory");
+    __syncwarp();
 }
 
-// Backward pass, tiles of kBackwardTile steps from the last to the first. What
-// flows from step t to t - 1 is f_t = a_t (dh_t + f_(t+1)), a map like the
-// state's, scanned the other way. The states inside the tile are made again
-// from the carry at its first step: reading the stored h would bring its
-// rounding into dgate, and more bytes.
-template <typename T, bool PAIR>
-__global__ void __launch_bounds__(kWarps * 32, 2)
-recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int64_t steps, int D, const float* carry, const float* dh_last,
-                           const int32_t* lengths, T* dgate, T* dvalue, int64_t grad_seq, int64_t grad_step, float* dh0, Exchange x,
-                           int columns) {
+// The lane's channels of a chunk in its slot.
+template <typename T, bool WIDE>
+struct Chunk {
+    const uint8_t* slot;
+    uint32_t shift, each;  // of the first row, and from row to row
+    __device__ __forceinline__ Chunk(const uint8_t* at, const T* from, int64_t step)
+        : slot(at + first_channel<WIDE>(threadIdx.x % 32) * sizeof(T)), shift(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(from))),
+          each(static_cast<uint32_t>(step) * sizeof(T)) {}
+    __device__ __forceinline__ Pair get(int r) const {
+        if constexpr (WIDE) {
+            return pair_at(reinterpret_cast<const T*>(slot + r * kRowBytes<T, true>));
+        } else {
+            const T* p = reinterpret_cast<const T*>(slot + r * kRowBytes<T, false> + ((shift + r * each) & 15u));
+            return pair(to_float(p[0]), to_float(p[32]));
+        }
+    }
+};
+
+// Forward pass: chunks of R steps pass through the warp's ring of shared
+// memory; the only chain from step to step is one fused multiply-add.
+// MAPS: the first pass, which makes the segment's map.
+template <typename T, bool WIDE, bool MAPS>
+__global__ void __launch_bounds__(kWarps * 32, kForwardWarps<T> / kWarps)
+recurrence_kernel(SeqIn gate, SeqIn value, int steps, int D, const float* h0, const int32_t* lengths, T* h, float* h_last,
+                  float* carry, Segments x) {
     layer_begin();
-    constexpr int R = kBackwardSteps;
-    __shared__ Map own[kWarps][32], heard[kWarps][32];
-    __shared__ float2 flows[kWarps][32], state[32];
-    const Place at = take_place(x, columns);
-    const int tile = x.tiles - 1 - at.order;
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = at.channel;
-    const bool live = c < D, second = c + 1 < D;
-    const int64_t n = length_of(lengths, at.b, steps), tile0 = (int64_t)tile * kBackwardTile, t0 = tile0 + warp * R;
-    const int inside = static_cast<int>(min(max(n - t0, (int64_t)0), (int64_t)R));
-    const int written = static_cast<int>(min(max(steps - t0, (int64_t)0), (int64_t)R));
-    const int64_t first_out = at.b * grad_seq + t0 * grad_step + c;
-    if (tile0 >= n && tile > 0) {
-        if (live)
-            for (int r = 0; r < written; ++r) {
-                store_two<PAIR>(dgate + first_out + r * grad_step, make_float2(0.f, 0.f), second);
-                store_two<PAIR>(dvalue + first_out + r * grad_step, make_float2(0.f, 0.f), second);
-            }
-        return;
-    }
-    const bool whole_warp = inside == R && c - 2 * lane + kChannels <= D;
-    Two<T> vraw[R], oraw[R];
-    float2 a[R], rest[R];
-    const auto load = [&](auto known) {
-        constexpr bool ALL = decltype(known)::value;
-        Two<T> graw[R];
-        const T* g = static_cast<const T*>(gate.p) + at.b * gate.seq + t0 * gate.step + c;
-        const T* v = static_cast<const T*>(value.p) + at.b * value.seq + t0 * value.step + c;
-        const T* o = static_cast<const T*>(dh.p) + at.b * dh.seq + t0 * dh.step + c;
-#pragma unroll
-        for (int r = 0; r < R; ++r, g += gate.step, v += value.step, o += dh.step) {
-            if (!ALL) vraw[r] = oraw[r] = Two<T>{};
-            if (ALL || (live && r < inside)) {
-                graw[r] = load_two<PAIR>(g, ALL || second);
-                vraw[r] = load_two<PAIR>(v, ALL || second);
-                oraw[r] = load_two<PAIR>(o, ALL || second);
-            }
+    constexpr int kRing = kForwardRing, kChunk = kChunkBytes<T, WIDE>;
+    extern __shared__ __align__(16) uint8_t inputs[];
+    const int lane = threadIdx.x % 32;
+    uint8_t* const ring = inputs + threadIdx.x / 32 * (kRing * 2 * kChunk);
+    const Task task = task_of(x);
+    if (task.column >= x.columns) return;
+    if (MAPS && task.order == x.count - 1) return;  // nobody asks for the last one
+    const int c = task.channel + first_channel<WIDE>(lane), n = lengths == nullptr ? steps : min(max(lengths[task.b], 0), steps);
+    const int first = task.order * x.steps, end = min(first + x.steps, steps), inside = min(max(n - first, 0), end - first);
+    const bool live = c < D, second = c + kSecond<WIDE> < D, all_channels = task.channel + kChannels <= D;
+    const T* g = static_cast<const T*>(gate.p) + task.b * gate.seq + first * gate.step + task.channel;
+    const T* v = static_cast<const T*>(value.p) + task.b * value.seq + first * value.step + task.channel;
+    const auto fetch = [&](int k) {
+        const int t = k * R;
+        if (t < inside) {
+            uint8_t* to = ring + k % kRing * (2 * kChunk);
+            fill<T, WIDE>(to, g + t * gate.step, gate.step, inside - t, D - task.channel);
+            fill<T, WIDE>(to + kChunk, v + t * value.step, value.step, inside - t, D - task.channel);
         }
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            a[r] = make_float2(1.f, 1.f);
-            rest[r] = make_float2(0.f, 0.f);
-            if (ALL || (live && r < inside)) {
-                const float2 gr = graw[r].get();
-                gate_of(gr.x, a[r].x, rest[r].x);
-                gate_of(gr.y, a[r].y, rest[r].y);
-            }
-        }
+        end_fill();
     };
-    if (whole_warp)
-        load(std::true_type{});
-    else
-        load(std::false_type{});
-    // the thread's steps as a map of the state (forwards) and of the flow (backwards)
-    Map m{make_float2(1.f, 1.f), make_float2(0.f, 0.f)};
-    float2 flow = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const float2 v = vraw[r].get();
-        m = then(m, Map{a[r], make_float2(rest[r].x * v.x, rest[r].y * v.y)});
+    for (int k = 0; k < kRing - 1; ++k) fetch(k);
+    Pair s = kZeros;
+    Map m = kSame;
+    if constexpr (!MAPS) {
+        if (h0 != nullptr && live) s = load_state<WIDE>(h0 + (int64_t)task.b * D + c, second);
+        if (x.count > 1) s = state_before(x, task, s);
     }
-#pragma unroll
-    for (int r = R - 1; r >= 0; --r) {
-        const float2 o = oraw[r].get();
-        flow = make_float2(a[r].x * (o.x + flow.x), a[r].y * (o.y + flow.y));
-    }
-    own[warp][lane] = m;
-    flows[warp][lane] = flow;
-    __syncthreads();
-    const int last_tile = n > 0 ? static_cast<int>((n - 1) / kBackwardTile) : 0, order = last_tile - tile;
-    Map whole{own[kWarps - 1][lane].a, flows[kWarps - 1][lane]};
-    if (tile > 0 && warp == 0) {
-        for (int i = kWarps - 2; i >= 0; --i) whole = then(whole, Map{own[i][lane].a, flows[i][lane]});
-        tell_map(x.maps + (at.b * x.tiles + tile) * x.channels + c, whole);
-    }
-    const float2 start = dh_last != nullptr && live ? make_float2(dh_last[at.b * D + c], second ? dh_last[at.b * D + c + 1] : 0.f)
-                                                    : make_float2(0.f, 0.f);
-    flow = start;
-    if (order > 0) flow = state_before(x, at.b, c, order, [=](int i) { return last_tile - i; }, start, heard, state);
-    if (tile > 0 && warp == 0 && order % kGroup == kGroup - 1)
-        tell_state(x.states + (at.b * x.groups + order / kGroup) * x.channels + c, apply(whole, flow));
-    if (!live) return;
-    float2 s = make_float2(0.f, 0.f);
-    if (n > 0) {
-        const int64_t carries = (steps + CPDP_CARRY_STEPS - 1) / CPDP_CARRY_STEPS;
-        const float* p = carry + (at.b * carries + tile) * D + c;
-        s = make_float2(p[0], second ? p[1] : 0.f);
-    }
-    for (int i = 0; i < warp; ++i) s = apply(own[i][lane], s);
-    for (int i = kWarps - 1; i > warp; --i) flow = apply(Map{own[i][lane].a, flows[i][lane]}, flow);
-    float2 away[R];  // h_(t-1) - v_t
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const float2 v = vraw[r].get();
-        away[r] = make_float2(s.x - v.x, s.y - v.y);
-        s = apply(Map{a[r], make_float2(rest[r].x * v.x, rest[r].y * v.y)}, s);
-    }
-    const auto finish = [&](auto known) {
-        constexpr bool ALL = decltype(known)::value;
-        T *dg = dgate + first_out + (R - 1) * grad_step, *dv = dvalue + first_out + (R - 1) * grad_step;
-#pragma unroll
-        for (int r = R - 1; r >= 0; --r, dg -= grad_step, dv -= grad_step) {
-            const float2 o = oraw[r].get(), g = make_float2(o.x + flow.x, o.y + flow.y);
-            flow = make_float2(a[r].x * g.x, a[r].y * g.y);
-            const bool in = ALL || r < inside;
-            if (ALL || r < written) {
-                const float2 x = make_float2(rest[r].x * g.x, rest[r].y * g.y), zero = make_float2(0.f, 0.f);
-                store_two<PAIR>(dv, in ? x : zero, ALL || second);
-                store_two<PAIR>(dg, in ? make_float2(x.x * away[r].x * a[r].x, x.y * away[r].y * a[r].y) : zero, ALL || second);
-            }
+    T* out = h + ((int64_t)task.b * steps + first) * D + c;
+    float* carries = carry + ((int64_t)task.b * ((steps + R - 1) / R) + first / R) * D + c;
+    for (int k = 0; k * R < inside; ++k) {
+        const int t = k * R, rows = inside - t;
+        wait_filled<kRing - 2>();
+        fetch(k + kRing - 1);  // into the slot of the chunk before
+        const uint8_t* slot = ring + k % kRing * (2 * kChunk);
+        const Chunk<T, WIDE> gs(slot, g + t * gate.step, gate.step), vs(slot + kChunk, v + t * value.step, value.step);
+        if (!MAPS && carry != nullptr && live) {
+            store_two<WIDE>(carries, s, second);
+            carries += D;
         }
+        const auto walk = [&](auto known) {
+            constexpr bool ALL = decltype(known)::value;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (!ALL && r >= rows) break;
+                Map one;
+                Pair rest;
+                gate_of(gs.get(r), one.a, rest);
+                one.b = mul2(rest, vs.get(r));
+                if constexpr (MAPS) {
+                    m = then(m, one);
+                } else {
+                    s = apply(one, s);
+                    if (ALL || live) store_two<WIDE>(out, s, ALL || second);
+                    out += D;
+                }
+            }
+        };
+        if (rows >= R && all_channels)
+            walk(std::true_type{});
+        else
+            walk(std::false_type{});
+        __syncwarp();
+    }
+    if constexpr (MAPS) {
+        x.maps[(task.column * x.count + task.order) * 32 + lane] = m;
+    } else if (live) {
+        for (int t = inside; t < end - first; ++t, out += D) store_two<WIDE>(out, kZeros, second);
+        if (n > first ? n <= end : n == 0 && first == 0) store_state<WIDE>(h_last + (int64_t)task.b * D + c, s, second);
+    }
+}
+
+// Backward pass, from the last step to the first. What flows from step t to
+// t - 1 is f_t = a_t (dh_t + f_(t+1)), a map like the state's. The states
+// inside a chunk are made again from the carry at its first step: reading the
+// stored h would bring its rounding into dgate, and more bytes.
+template <typename T, bool WIDE, bool MAPS>
+__global__ void __launch_bounds__(kWarps * 32, kBackwardWarps / kWarps)
+recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int steps, int D, const float* carry, const float* dh_last,
+                           const int32_t* lengths, T* dgate, T* dvalue, int64_t grad_seq, int64_t grad_step, float* dh0, Segments x) {
+    layer_begin();
+    constexpr int kRing = kBackwardRing<T>, kChunk = kChunkBytes<T, WIDE>, kArrays = MAPS ? 2 : 3;
+    extern __shared__ __align__(16) uint8_t inputs[];
+    const int lane = threadIdx.x % 32;
+    uint8_t* const ring = inputs + threadIdx.x / 32 * (kRing * kArrays * kChunk);
+    const Task task = task_of(x);
+    if (task.column >= x.columns) return;
+    if (MAPS && task.order == x.count - 1) return;
+    const int c = task.channel + first_channel<WIDE>(lane), n = lengths == nullptr ? steps : min(max(lengths[task.b], 0), steps);
+    const int first = (x.count - 1 - task.order) * x.steps, end = min(first + x.steps, steps), inside = min(max(n - first, 0), max(end - first, 0));
+    const bool live = c < D, second = c + kSecond<WIDE> < D, all_channels = task.channel + kChannels <= D;
+    const T* g = static_cast<const T*>(gate.p) + task.b * gate.seq + first * gate.step + task.channel;
+    const T* v = static_cast<const T*>(value.p) + task.b * value.seq + first * value.step + task.channel;
+    const T* o = static_cast<const T*>(dh.p) + task.b * dh.seq + first * dh.step + task.channel;
+    const int chunks = (inside + R - 1) / R;
+    const auto fetch = [&](int i) {  // the i-th chunk from the end
+        const int t = (chunks - 1 - i) * R;
+        if (i < chunks) {
+            uint8_t* to = ring + i % kRing * (kArrays * kChunk);
+            fill<T, WIDE>(to, g + t * gate.step, gate.step, inside - t, D - task.channel);
+            fill<T, WIDE>(to + kChunk, o + t * dh.step, dh.step, inside - t, D - task.channel);
+            if constexpr (!MAPS) fill<T, WIDE>(to + 2 * kChunk, v + t * value.step, value.step, inside - t, D - task.channel);
+        }
+        end_fill();
     };
-    if (whole_warp)
-        finish(std::true_type{});
-    else
-        finish(std::false_type{});
-    if (dh0 != nullptr && tile == 0 && warp == 0) store_two<false>(dh0 + at.b * D + c, flow, second);
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) fetch(i);
+    Pair flow = kZeros;
+    Map m = kSame;
+    if constexpr (!MAPS) {
+        if (dh_last != nullptr && live) flow = load_state<WIDE>(dh_last + (int64_t)task.b * D + c, second);
+        if (x.count > 1) flow = state_before(x, task, flow);
+    }
+    const int64_t out0 = task.b * grad_seq + first * grad_step + c;
+    if (!MAPS && live)
+        for (int64_t t = inside; t < end - first; ++t) {
+            store_two<WIDE>(dgate + out0 + t * grad_step, kZeros, second);
+            store_two<WIDE>(dvalue + out0 + t * grad_step, kZeros, second);
+        }
+    const float* carries = carry + ((int64_t)task.b * ((steps + R - 1) / R) + first / R) * D + c;
+    for (int i = 0; i < chunks; ++i) {
+        const int t = (chunks - 1 - i) * R, rows = inside - t;
+        Pair s = kZeros;
+        if (!MAPS && live) {
+            const float* p = carries + (int64_t)(t / R) * D;
+            s = load_state<WIDE>(p, second);
+        }
+        wait_filled<kRing - 2>();
+        fetch(i + kRing - 1);
+        const uint8_t* slot = ring + i % kRing * (kArrays * kChunk);
+        const Chunk<T, WIDE> gs(slot, g + t * gate.step, gate.step), os(slot + kChunk, o + t * dh.step, dh.step),
+            vs(slot + 2 * kChunk, v + t * value.step, value.step);
+        const auto walk = [&](auto known) {
+            constexpr bool ALL = decltype(known)::value;
+            if constexpr (MAPS) {
+#pragma unroll
+                for (int r = R - 1; r >= 0; --r) {
+                    if (!ALL && r >= rows) continue;
+                    Pair a, rest;
+                    gate_of(gs.get(r), a, rest);
+                    m = Map{mul2(a, m.a), mul2(a, add2(os.get(r), m.b))};
+                }
+            } else {
+                Pair a[R], rest[R], away[R];  // away: (h_(t-1) - v_t) a_t
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if (!ALL && r >= rows) break;
+                    gate_of(gs.get(r), a[r], rest[r]);
+                    const Pair vr = vs.get(r);
+                    away[r] = mul2(fma2(vr, kMinusOnes, s), a[r]);
+                    s = fma2(a[r], s, mul2(rest[r], vr));
+                }
+                T *dg = dgate + out0 + (t + R - 1) * grad_step, *dv = dvalue + out0 + (t + R - 1) * grad_step;
+#pragma unroll
+                for (int r = R - 1; r >= 0; --r, dg -= grad_step, dv -= grad_step) {
+                    if (!ALL && r >= rows) continue;
+                    const Pair both = add2(os.get(r), flow), y = mul2(rest[r], both);
+                    flow = mul2(a[r], both);
+                    if (ALL || live) {
+                        store_two<WIDE>(dv, y, ALL || second);
+                        store_two<WIDE>(dg, mul2(y, away[r]), ALL || second);
+                    }
+                }
+            }
+        };
+        if (rows >= R && all_channels)
+            walk(std::true_type{});
+        else
+            walk(std::false_type{});
+        __syncwarp();
+    }
+    if constexpr (MAPS)
+        x.maps[(task.column * x.count + task.order) * 32 + lane] = m;
+    else if (dh0 != nullptr && first == 0 && live)
+        store_state<WIDE>(dh0 + (int64_t)task.b * D + c, flow, second);
 }
 
 template <typename T>
@@ -421,9 +435,9 @@ recurrence_step_kernel(const T* gate, int64_t gate_seq, const T* value, int64_t 
     const int64_t b = blockIdx.y;
     const int d = blockIdx.x * kThreads + threadIdx.x;
     if (d >= D) return;
-    float a, rest;
-    gate_of(to_float(gate[b * gate_seq + d]), a, rest);
-    const float next = a * state[b * D + d] + rest * to_float(value[b * value_seq + d]);
+    Pair a, rest;
+    gate_of(pair(to_float(gate[b * gate_seq + d]), 0.f), a, rest);
+    const float next = fmaf(floats(a).x, state[b * D + d], floats(rest).x * to_float(value[b * value_seq + d]));
     state[b * D + d] = next;
     h[b * D + d] = from_float<T>(next);
 }
@@ -436,6 +450,7 @@ using namespace cpdp;
 static cpdp_status check_recurrence(int B, int64_t T, int D, cpdp_dtype dtype) {
     if (B < 0 || B > 65535) return layer_error(CPDP_EINVAL, "B=%d must be in [0, 65535]", B);
     CPDP_TRY(check_sizes(1, T, D));
+    if (T > int64_t(1) << 30) return layer_error(CPDP_EINVAL, "T=%lld is at most 2^30", (long long)T);
     if (B > 0) {
         if (T > kLayerMaxRows / B || (T > 0 && D > kLayerMaxElements / (B * T)))
             return layer_error(CPDP_EINVAL, "B=%d, T=%lld, D=%d: B * T is at most 2^31 - 1 and all elements at most 2^40", B, (long long)T, D);
@@ -444,53 +459,36 @@ static cpdp_status check_recurrence(int B, int64_t T, int D, cpdp_dtype dtype) {
     return CPDP_OK;
 }
 
-// The workspace: a ticket, then the tiles' maps, then the groups' states.
-static size_t lay_out(int B, int64_t T, int D, int tile, void* workspace, Exchange* x) {
-    const int64_t tiles = ceil_div(T, tile), groups = ceil_div(tiles, kGroup), channels = ceil_div(D, kChannels) * kChannels;
-    const int64_t maps = B * tiles * channels, states = B * groups * channels;
-    if (x != nullptr) {
-        char* p = static_cast<char*>(workspace);
-        *x = Exchange{reinterpret_cast<unsigned*>(p), reinterpret_cast<uint64_t*>(p + 16),
-                      reinterpret_cast<uint32_t*>(p + 16 + 8 * maps), (int)tiles, (int)groups, (int)channels};
-    }
-    return tiles > 1 && B > 0 ? static_cast<size_t>(16 + 8 * maps + 4 * states) : 0;
+// Segments for B sequences of T steps and D channels, of a kernel that runs
+// `warps` warps per SM. A split costs a second reading of two inputs, so it has
+// to gain more than that: 3 columns per SM go half as fast unsplit as 8. Below,
+// as many warps as run at once (more would wait for a second turn), of at least
+// 4 chunks each.
+static Segments segments_of(int B, int64_t T, int D, int warps) {
+    const int64_t groups = ceil_div(D, kChannels), columns = B * groups;
+    int64_t count = columns > 0 && columns < 3 * kSMs ? int64_t(warps) * kSMs / columns : 1;
+    if (count > T / (4 * R)) count = T / (4 * R);
+    count = count < 2 ? 1 : count < 4 ? 2 : count / 4 * 4;
+    const int64_t steps = ceil_div(ceil_div(T > 0 ? T : 1, count), R) * R;
+    return {static_cast<int>(count), static_cast<int>(steps), static_cast<int>(groups), columns, nullptr};
 }
 
 size_t cpdp_gated_recurrence_workspace(int B, int64_t T, int D) {
     if (check_recurrence(B, T, D, CPDP_F32) != CPDP_OK) return 0;
-    return lay_out(B, T, D, kBackwardTile, nullptr, nullptr);
+    const Segments x = segments_of(B, T, D, kForwardWarps<__nv_bfloat16>);  // the most warps: the most segments
+    return x.count > 1 ? static_cast<size_t>(x.columns) * x.count * 32 * sizeof(Map) : 0;
 }
 
-cpdp_status cpdp_layer_timeouts(int64_t* count) {
-    if (count == nullptr) return layer_error(CPDP_EINVAL, "count is NULL");
-    unsigned long long seen = 0, zero = 0;
-    cudaError_t e = cudaDeviceSynchronize();
-    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&seen, wait_timeouts, sizeof seen);
-    if (e == cudaSuccess) e = cudaMemcpyToSymbol(wait_timeouts, &zero, sizeof zero);
-    unsigned long long others = 0;
-    if (e == cudaSuccess) e = take_weight_gradient_timeouts(&others);
-    *count = static_cast<int64_t>(seen + others);
-    return layer_launched(e, "cpdp_layer_timeouts");
+// Whether an array's rows start at multiples of 16 bytes.
+static bool in_pieces(const void* p, int64_t size, int64_t a, int64_t b) {
+    return aligned_to(p, 16) && a * size % 16 == 0 && b * size % 16 == 0;
 }
 
-// The exchange of one pass, its words set to "not there yet".
-static cpdp_status begin_exchange(int B, int64_t T, int D, int tile, void* workspace, size_t workspace_bytes, void* stream, Exchange* x) {
-    CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_gated_recurrence_workspace(B, T, D)));
-    const size_t used = lay_out(B, T, D, tile, workspace, x);
-    const int64_t blocks = int64_t(x->tiles > 0 ? x->tiles : 1) * B * (x->channels / kChannels);
-    if (blocks > kLayerMaxRows)
-        return layer_error(CPDP_EINVAL, "B=%d, T=%lld, D=%d: more than 2^31 - 1 blocks", B, (long long)T, D);
-    if (used > 0) return layer_launched(cudaMemsetAsync(workspace, 0xff, used, static_cast<cudaStream_t>(stream)), "setting the workspace");
-    return CPDP_OK;
+template <typename... KArgs, typename... Args>
+static cudaError_t launch_walk(void (*kernel)(KArgs...), const Segments& x, size_t smem, void* stream, Args... args) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    return e != cudaSuccess ? e : launch_layer(kernel, static_cast<unsigned>(ceil_div(x.columns * x.count, kWarps)), kWarps * 32, smem, stream, args..., x);
 }
-
-static unsigned blocks_of(const Exchange& x, int B) {
-    return static_cast<unsigned>(x.tiles > 0 ? x.tiles : 1) * B * (x.channels / kChannels);
-}
-
-// Whether pairs of channels can be moved as one: D even, and every array's
-// pointer and strides in whole pairs.
-static bool even(const void* p, int64_t size, int64_t a, int64_t b) { return aligned_to(p, 2 * size) && a % 2 == 0 && b % 2 == 0; }
 
 cpdp_status cpdp_gated_recurrence(const void* gate, int64_t gate_seq, int64_t gate_step, const void* value,
                                   int64_t value_seq, int64_t value_step, cpdp_dtype dtype, int B, int64_t T, int D,
@@ -506,21 +504,26 @@ cpdp_status cpdp_gated_recurrence(const void* gate, int64_t gate_seq, int64_t ga
     CPDP_TRY(check_array("h", h, some, e));
     CPDP_TRY(check_array("h_last", h_last, B > 0, 4));
     CPDP_TRY(check_array("carry", carry, false, 4));
-    Exchange x;
+    CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_gated_recurrence_workspace(B, T, D)));
     if (B == 0) return CPDP_OK;
-    CPDP_TRY(begin_exchange(B, T, D, kForwardTile, workspace, workspace_bytes, stream, &x));
+    Segments x = segments_of(B, T, D, dtype == CPDP_F32 ? kForwardWarps<float> : kForwardWarps<__nv_bfloat16>);
+    x.maps = static_cast<Map*>(workspace);
     const SeqIn g{gate, gate_seq, gate_step}, v{value, value_seq, value_step};
-    const bool pair = D % 2 == 0 && even(gate, e, gate_seq, gate_step) && even(value, e, value_seq, value_step) && even(h, e, 0, 0);
-    const unsigned blocks = blocks_of(x, B);
-    const auto go = [&](auto kernel, auto* out) {
-        return launch_layer(kernel, blocks, kWarps * 32, 0, stream, g, v, T, D, h0, lengths, out, h_last, carry, x,
-                            B * (x.channels / kChannels));
-    };
-    const auto typed = [&](auto* out) {
+    const bool wide = D * e % 16 == 0 && in_pieces(gate, e, gate_seq, gate_step) && in_pieces(value, e, value_seq, value_step) &&
+                      aligned_to(h, 16) && aligned_to(carry, 8);
+    const auto go = [&](auto* out, auto rows) {
         using E = std::remove_pointer_t<decltype(out)>;
-        return pair ? go(recurrence_kernel<E, true>, out) : go(recurrence_kernel<E, false>, out);
+        constexpr bool WIDE = decltype(rows)::value;
+        const auto pass = [&](auto kernel) {
+            return launch_walk(kernel, x, kWarps * kForwardRing * 2 * kChunkBytes<E, WIDE>, stream, g, v, static_cast<int>(T), D, h0,
+                               lengths, out, h_last, carry);
+        };
+        const cudaError_t first = x.count > 1 ? pass(recurrence_kernel<E, WIDE, true>) : cudaSuccess;
+        return first != cudaSuccess ? first : pass(recurrence_kernel<E, WIDE, false>);
     };
-    return layer_launched(dtype == CPDP_F32 ? typed(static_cast<float*>(h)) : typed(static_cast<__nv_bfloat16*>(h)), "cpdp_gated_recurrence");
+    const auto typed = [&](auto* out) { return wide ? go(out, std::true_type{}) : go(out, std::false_type{}); };
+    const cudaError_t launched = dtype == CPDP_F32 ? typed(static_cast<float*>(h)) : typed(static_cast<__nv_bfloat16*>(h));
+    return layer_launched(launched, "cpdp_gated_recurrence");
 }
 
 cpdp_status cpdp_gated_recurrence_backward(const void* dh, int64_t dh_seq, int64_t dh_step, const void* gate,
@@ -541,25 +544,26 @@ cpdp_status cpdp_gated_recurrence_backward(const void* dh, int64_t dh_seq, int64
     CPDP_TRY(check_array("dgate", dgate, some, e, grad_seq, grad_step));
     CPDP_TRY(check_array("dvalue", dvalue, some, e));
     CPDP_TRY(check_array("dh0", dh0, false, 4));
-    Exchange x;
+    CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_gated_recurrence_workspace(B, T, D)));
     if (B == 0) return CPDP_OK;
-    CPDP_TRY(begin_exchange(B, T, D, kBackwardTile, workspace, workspace_bytes, stream, &x));
-    if (x.tiles == 0) x.tiles = 1;  // no steps: one tile passes dh_last on to dh0
+    Segments x = segments_of(B, T, D, kBackwardWarps);
+    x.maps = static_cast<Map*>(workspace);
     const SeqIn o{dh, dh_seq, dh_step}, g{gate, gate_seq, gate_step}, v{value, value_seq, value_step};
-    const bool pair = D % 2 == 0 && even(dh, e, dh_seq, dh_step) && even(gate, e, gate_seq, gate_step) &&
-                      even(value, e, value_seq, value_step) && even(dgate, e, grad_seq, grad_step) && even(dvalue, e, 0, 0);
-    const unsigned blocks = blocks_of(x, B);
-    const auto go = [&](auto kernel, auto* dg, auto* dv) {
-        return launch_layer(kernel, blocks, kWarps * 32, 0, stream, o, g, v, T, D, carry, dh_last, lengths, dg, dv, grad_seq, grad_step,
-                            dh0, x, B * (x.channels / kChannels));
-    };
-    const auto typed = [&](auto* dg, auto* dv) {
+    const bool wide = D * e % 16 == 0 && in_pieces(dh, e, dh_seq, dh_step) && in_pieces(gate, e, gate_seq, gate_step) &&
+                      in_pieces(value, e, value_seq, value_step) && in_pieces(dgate, e, grad_seq, grad_step) && aligned_to(dvalue, 16);
+    const auto go = [&](auto* dg, auto rows) {
         using E = std::remove_pointer_t<decltype(dg)>;
-        return pair ? go(recurrence_backward_kernel<E, true>, dg, dv) : go(recurrence_backward_kernel<E, false>, dg, dv);
+        constexpr bool WIDE = decltype(rows)::value;
+        const auto pass = [&](auto kernel, int arrays) {
+            return launch_walk(kernel, x, kWarps * kBackwardRing<E> * arrays * kChunkBytes<E, WIDE>, stream, o, g, v,
+                               static_cast<int>(T), D, carry, dh_last, lengths, dg, static_cast<E*>(dvalue), grad_seq, grad_step, dh0);
+        };
+        const cudaError_t first = x.count > 1 ? pass(recurrence_backward_kernel<E, WIDE, true>, 2) : cudaSuccess;
+        return first != cudaSuccess ? first : pass(recurrence_backward_kernel<E, WIDE, false>, 3);
     };
-    return layer_launched(dtype == CPDP_F32 ? typed(static_cast<float*>(dgate), static_cast<float*>(dvalue))
-                                            : typed(static_cast<__nv_bfloat16*>(dgate), static_cast<__nv_bfloat16*>(dvalue)),
-                          "cpdp_gated_recurrence_backward");
+    const auto typed = [&](auto* dg) { return wide ? go(dg, std::true_type{}) : go(dg, std::false_type{}); };
+    const cudaError_t launched = dtype == CPDP_F32 ? typed(static_cast<float*>(dgate)) : typed(static_cast<__nv_bfloat16*>(dgate));
+    return layer_launched(launched, "cpdp_gated_recurrence_backward");
 }
 
 cpdp_status cpdp_gated_recurrence_step(const void* gate, int64_t gate_seq, const void* value, int64_t value_seq,

@@ -457,8 +457,12 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     return layer_launched(dW_dtype == CPDP_F32 ? sum(static_cast<float*>(dW)) : sum(static_cast<__nv_bfloat16*>(dW)), "cpdp_weight_gradient");
 }
 
-cudaError_t cpdp::take_weight_gradient_timeouts(unsigned long long* count) {
-    const unsigned long long zero = 0;
-    const cudaError_t e = cudaMemcpyFromSymbol(count, wait_timeouts, sizeof *count);
-    return e != cudaSuccess ? e : cudaMemcpyToSymbol(wait_timeouts, &zero, sizeof zero);
+cpdp_status cpdp_layer_timeouts(int64_t* count) {
+    if (count == nullptr) return layer_error(CPDP_EINVAL, "count is NULL");
+    unsigned long long seen = 0, zero = 0;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&seen, wait_timeouts, sizeof seen);
+    if (e == cudaSuccess) e = cudaMemcpyToSymbol(wait_timeouts, &zero, sizeof zero);
+    *count = static_cast<int64_t>(seen);
+    return layer_launched(e, "cpdp_layer_timeouts");
 }

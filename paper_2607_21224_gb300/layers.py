@@ -36,7 +36,7 @@ from . import cpdp as _c
 from .state import _raw_stream
 
 BLOCK = 32  # features that share an exponent
-CARRY_STEPS = 64  # CPDP_CARRY_STEPS
+CARRY_STEPS = 16  # CPDP_CARRY_STEPS
 NORM_MAX_FEATURES = 16384  # CPDP_NORM_MAX_FEATURES
 
 _P, _I, _L, _F, _Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -415,7 +415,7 @@ def gated_recurrence_step(gate, value, state, *, stream=None):
 
 
 def wait_timeouts() -> int:
-    """Bounded waits of the recurrence's kernels that ran out since the last
+    """Bounded waits of the weight gradient's kernel that ran out since the last
     call (0 expected). Waits for the current device."""
     count = _L()
     _check(lib().cpdp_layer_timeouts(ctypes.byref(count)))

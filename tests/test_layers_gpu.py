@@ -261,8 +261,8 @@ def test_recurrence(shape, dtype, ragged, layout):
     assert all(torch.equal(p, q) for p, q in zip(again, (dgate, dvalue, dh0)))
 
 
-def test_recurrence_of_many_tiles_has_no_wait_run_out():
-    """A long sequence next to short ones: several groups of tiles, more blocks than the GPU runs at once."""
+def test_recurrence_of_long_ragged_sequences():
+    """A long sequence next to shorter ones: many segments, ends inside and between them, the same bits each time."""
     shape = (3, 20000, 200)
     gate, value, dh, h0, dh_last, _ = recurrence_inputs(shape, F32, False)
     lengths = torch.tensor([20000, 4097, 15000], dtype=torch.int32)
