@@ -139,9 +139,10 @@ struct Piece<float, 1> {
 };
 template <>
 struct Piece<__nv_bfloat16, 1> {
-    uint16_t v;
-    __device__ __forceinline__ float get(int) const { return __uint_as_float(uint32_t(v) << 16); }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint16_t*>(p)); }
+    uint32_t v;
+    __device__ __forceinline__ float get(int) const { return __uint_as_float(v << 16); }
+    // into a register of its own: a 16-bit variable shares one with another, and waits for that one's load
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { asm("ld.global.cs.u16 %0, [%1];" : "=r"(v) : "l"(p)); }
 };
 
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
