@@ -153,40 +153,50 @@ norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_
         sums[k] = 0.f;
     }
     int turn = 0;
-    for (int64_t m = (int64_t)blockIdx.x * rows + threadIdx.x / TPR; m < M; m += (int64_t)gridDim.x * rows, turn ^= 1) {
-        const T* gr = static_cast<const T*>(dy.p) + w * dy.worker + m * dy.row;
-        const T* sr = static_cast<const T*>(s.p) + w * s.worker + m * s.row;
-        const T* dr = static_cast<const T*>(ds.p) + w * ds.worker + m * ds.row;
-        Piece<T, V> g[J], r[J], through[J];
+    Piece<T, V> g[J], r[J], through[J];
+    const auto row_of = [&](const NormIn& in, int64_t m) { return static_cast<const T*>(in.p) + w * in.worker + m * in.row; };
+    const auto load = [&](int64_t m) {
+        const T *gr = row_of(dy, m), *sr = row_of(s, m), *dr = row_of(ds, m);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int d = (j * TPR + t) * V;
             g[j] = r[j] = through[j] = Piece<T, V>{};
-            if (d < D) {
+            if (m < M && d < D) {
                 g[j].load(gr + d);
                 r[j].load(sr + d);
                 if (KEEP && ds.p != nullptr) through[j].load(dr + d);
             }
         }
+    };
+    // the next row is on its way while one is worked on, where it takes few registers (at 4,096 features 213 -> 180 us)
+    constexpr bool ahead = V > 1 && sizeof(T) == 2 && KEEP;
+    const int64_t first = (int64_t)blockIdx.x * rows + threadIdx.x / TPR, step = (int64_t)gridDim.x * rows;
+    if (ahead) load(first);
+    for (int64_t m = first; m < M; m += step, turn ^= 1) {
+        if (!ahead) load(m);
+        Piece<T, V> g0[J], r0[J], through0[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) g0[j] = g[j], r0[j] = r[j], through0[j] = through[j];
+        if (ahead) load(m + step);
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-            const float v = r[k / V].get(k % V);
+            const float v = r0[k / V].get(k % V);
             sum[0] = fmaf(v, v, sum[0]);
-            sum[1] = fmaf(g[k / V].get(k % V) * (KEEP ? wt[KEEP ? k : 0] : weight_at(k)), v, sum[1]);
+            sum[1] = fmaf(g0[k / V].get(k % V) * (KEEP ? wt[KEEP ? k : 0] : weight_at(k)), v, sum[1]);
         }
         row_sum<TPR>(sum, turn);
         const float k1 = rsqrtf(sum[0] / D + eps), k3 = k1 * k1 * k1 * (sum[1] / D);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int d = (j * TPR + t) * V;
-            if (!KEEP && ds.p != nullptr && d < D) through[j].load(dr + d);
+            if (!KEEP && ds.p != nullptr && d < D) through0[j].load(row_of(ds, m) + d);
             float o[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const int k = j * V + e;
-                const float v = r[j].get(e), gk = g[j].get(e) * k1;
-                o[e] = fmaf(gk, KEEP ? wt[KEEP ? k : 0] : weight_at(k), through[j].get(e)) - v * k3;
+                const float v = r0[j].get(e), gk = g0[j].get(e) * k1;
+                o[e] = fmaf(gk, KEEP ? wt[KEEP ? k : 0] : weight_at(k), through0[j].get(e)) - v * k3;
                 sums[k] = fmaf(gk, v, sums[k]);
             }
             if (d < D) store_piece<V>(static_cast<T*>(dx) + (w * M + m) * D + d, o);

@@ -58,22 +58,32 @@ SIGNATURES = {
     "cpdp_layer_timeouts": (_I, [ctypes.POINTER(_L)]),
 }
 
-_lib = None
+_loaded: dict = {}
 
 
 def lib() -> ctypes.CDLL:
     """libcpdp with the layers' entry points declared."""
-    global _lib
-    if _lib is None:
-        L = _c.lib()
+    L = _c.lib()
+    if not _loaded:
         for name, (result, arguments) in SIGNATURES.items():
             f = getattr(L, name)
             f.restype, f.argtypes = result, arguments
-        _lib = L
-    return _lib
+            _loaded[name] = f
+    return L
+
+
+def _entry(name: str):
+    """An entry point by name. A small call's cost is what Python does around
+    it, so this and the checks below keep to one look at each property."""
+    if not _loaded:
+        lib()
+    return _loaded[name]
 
 
 _CODES = {torch.float32: _c.CPDP_F32, torch.bfloat16: _c.CPDP_BF16}
+_F32, _BF16 = torch.float32, torch.bfloat16
+# The current device's index without the checks of the public function, where torch has it.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _dtype(t: torch.Tensor, name: str) -> int:
@@ -88,45 +98,53 @@ def _check(status: int) -> None:
         _c._check(status)
 
 
-def _stream(device: torch.device) -> int:
+def _stream(index: int) -> int:
     if _raw_stream is not None:
-        return _raw_stream(device.index)
-    return torch.cuda.current_stream(device).cuda_stream
+        return _raw_stream(index)
+    return torch.cuda.current_stream(index).cuda_stream
 
 
-def _on(device: torch.device, stream):
-    """The context in which a call's outputs are allocated and its kernels
-    launched, or None where that is the current one."""
-    if stream is None and device.index == torch.cuda.current_device():
-        return None
+def _elsewhere(device: torch.device, stream) -> bool:
+    """Whether a call runs on another device or stream than the current one."""
+    return stream is not None or device.index != _current_device()
+
+
+def _there(device: torch.device, stream):
+    """The context in which such a call's outputs are allocated and its kernels
+    launched."""
     if stream is None:
         return torch.cuda.device(device)
     return torch.cuda.stream(torch.cuda.ExternalStream(stream, device) if isinstance(stream, int) else stream)
 
 
-def _input(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype, device: torch.device) -> None:
-    """An input of this shape and type, contiguous along its last axis."""
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+def _input(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype, device: torch.device) -> tuple:
+    """The strides of an input of this shape and type, contiguous along its last axis."""
+    strides = t.stride()
+    if t.shape == shape and t.dtype is dtype and t.device == device and (strides[-1] == 1 or shape[-1] <= 1):
+        return strides
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if t.stride(-1) != 1 and shape[-1] > 1:
-        raise ValueError(f"{name} must be contiguous along its last axis")
+    raise ValueError(f"{name} must be contiguous along its last axis")
 
 
 def _cuda(t: torch.Tensor, name: str) -> torch.device:
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} is on {t.device}; the layers run on a CUDA device")
     return t.device
 
 
-def _whole(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, device: torch.device) -> None:
-    if t is not None:
-        _input(t, name, shape, dtype, device)
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
+def _whole(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, device: torch.device) -> int | None:
+    """The address of a contiguous array, or None where there is none."""
+    if t is None:
+        return None
+    _input(t, name, shape, dtype, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def _workspace(nbytes: int, device: torch.device) -> torch.Tensor | None:
@@ -157,12 +175,10 @@ def _new_checkpoint(W: int, M: int, D: int, device: torch.device) -> Checkpoint:
                       torch.empty((W, M, blocks), dtype=torch.uint8, device=device), D)
 
 
-def _rows(x: torch.Tensor, weight: torch.Tensor, name: str) -> torch.device:
-    device = _cuda(x, name)
-    if x.dim() != 3:
-        raise ValueError(f"{name} must be (W, M, D), or (M, D) with a weight (D,); got {tuple(x.shape)}")
-    _input(weight, "weight", (x.shape[0], x.shape[2]), torch.float32, device)
-    return device
+def _three(t: torch.Tensor, name: str) -> tuple:
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be (W, M, D), or (M, D) of one model; got {tuple(t.shape)}")
+    return t.shape
 
 
 def add_rmsnorm(x, weight, residual=None, *, eps: float = 1e-6, checkpoint: bool = False, stream=None):
@@ -172,30 +188,31 @@ def add_rmsnorm(x, weight, residual=None, *, eps: float = 1e-6, checkpoint: bool
     y is held in 8 bits, ``saved`` is that Checkpoint and y is bfloat16, the
     values that it stands for: the product that follows and its weight gradient
     then see the same numbers. Else y has x's type and ``saved`` is None."""
-    if weight.dim() == 1 and x.dim() == 2:
+    if x.dim() == 2 and weight.dim() == 1:
         y, s, saved = add_rmsnorm(x[None], weight[None], None if residual is None else residual[None], eps=eps,
                                   checkpoint=checkpoint, stream=stream)
         return y[0], x if residual is None else s[0], saved
-    device = _rows(x, weight, "x")
-    on = _on(device, stream)
-    if on is not None:
-        with on:
+    device = _cuda(x, "x")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
             return add_rmsnorm(x, weight, residual, eps=eps, checkpoint=checkpoint)
-    W, M, D = x.shape
-    code = _dtype(x, "x")
-    _input(x, "x", (W, M, D), x.dtype, device)
-    s = x
+    W, M, D = shape = _three(x, "x")
+    dtype, code = x.dtype, _dtype(x, "x")
+    xs, ws, rs = _input(x, "x", shape, dtype, device), _input(weight, "weight", (W, D), _F32, device), (0, 0)
+    s, s_at, r_at = x, None, None
     if residual is not None:
-        _input(residual, "residual", (W, M, D), x.dtype, device)
-        s = torch.empty((W, M, D), dtype=x.dtype, device=device)
-    saved = _new_checkpoint(W, M, D, device) if checkpoint else None
-    y = torch.empty((W, M, D), dtype=torch.bfloat16 if checkpoint else x.dtype, device=device)
-    r = residual
-    _check(lib().cpdp_add_rmsnorm(
-        x.data_ptr(), x.stride(0), x.stride(1), _ptr(r), r.stride(0) if r is not None else 0,
-        r.stride(1) if r is not None else 0, weight.data_ptr(), weight.stride(0), code, W, M, D, eps, y.data_ptr(),
-        s.data_ptr() if r is not None else None, saved.codes.data_ptr() if saved else None,
-        saved.exponents.data_ptr() if saved else None, _stream(device)))
+        rs, r_at = _input(residual, "residual", shape, dtype, device), residual.data_ptr()
+        s = torch.empty(shape, dtype=dtype, device=device)
+        s_at = s.data_ptr()
+    if checkpoint:
+        saved = _new_checkpoint(W, M, D, device)
+        y = torch.empty(shape, dtype=_BF16, device=device)
+        codes, exponents = saved.codes.data_ptr(), saved.exponents.data_ptr()
+    else:
+        y = torch.empty(shape, dtype=dtype, device=device)
+        saved = codes = exponents = None
+    _check(_entry("cpdp_add_rmsnorm")(x.data_ptr(), xs[0], xs[1], r_at, rs[0], rs[1], weight.data_ptr(), ws[0], code, W, M, D, eps,
+                                      y.data_ptr(), s_at, codes, exponents, _stream(device.index)))
     return y, s, saved
 
 
@@ -208,7 +225,7 @@ def _gradient_out(out, name: str, shape: tuple, dtype: torch.dtype, device: torc
     _dtype(out, name)
     if tuple(out.shape) != shape or out.device != device:
         raise ValueError(f"{name} must have shape {shape} on {device}, got {tuple(out.shape)} on {out.device}")
-    if out.shape[0] > 0 and not out[0].is_contiguous():
+    if not out.is_contiguous() and not out[0].is_contiguous():
         raise ValueError(f"each worker's part of {name} must be contiguous")
     return out
 
@@ -219,30 +236,27 @@ def add_rmsnorm_backward(dy, s, weight, ds=None, *, eps: float = 1e-6, dweight=N
     reaches s by other ways (the residual stream's) and is added to dx. dx is
     the gradient of x and of the residual. dweight is written into the tensor
     given, (W, D) float32 or bfloat16, or into a new one of ``dtype``."""
-    if weight.dim() == 1 and s.dim() == 2:
+    if s.dim() == 2 and weight.dim() == 1:
         dx, dw = add_rmsnorm_backward(dy[None], s[None], weight[None], None if ds is None else ds[None], eps=eps,
                                       dweight=None if dweight is None else dweight[None], dtype=dtype, stream=stream)
         return dx[0], dw[0]
-    device = _rows(s, weight, "s")
-    on = _on(device, stream)
-    if on is not None:
-        with on:
+    device = _cuda(s, "s")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
             return add_rmsnorm_backward(dy, s, weight, ds, eps=eps, dweight=dweight, dtype=dtype)
-    W, M, D = s.shape
-    code = _dtype(s, "s")
-    _input(s, "s", (W, M, D), s.dtype, device)
-    _input(dy, "dy", (W, M, D), s.dtype, device)
+    W, M, D = shape = _three(s, "s")
+    kind, code = s.dtype, _dtype(s, "s")
+    ss, gs = _input(s, "s", shape, kind, device), _input(dy, "dy", shape, kind, device)
+    ws, ts, t_at = _input(weight, "weight", (W, D), _F32, device), (0, 0), None
     if ds is not None:
-        _input(ds, "ds", (W, M, D), s.dtype, device)
+        ts, t_at = _input(ds, "ds", shape, kind, device), ds.data_ptr()
     dweight = _gradient_out(dweight, "dweight", (W, D), dtype, device)
-    dx = torch.empty((W, M, D), dtype=s.dtype, device=device)
-    L = lib()
-    ws = _workspace(L.cpdp_add_rmsnorm_backward_workspace(W, M, D), device)
-    _check(L.cpdp_add_rmsnorm_backward(
-        dy.data_ptr(), dy.stride(0), dy.stride(1), s.data_ptr(), s.stride(0), s.stride(1), _ptr(ds),
-        ds.stride(0) if ds is not None else 0, ds.stride(1) if ds is not None else 0, weight.data_ptr(), weight.stride(0),
-        code, W, M, D, eps, dx.data_ptr(), dweight.data_ptr(), dweight.stride(0), _CODES[dweight.dtype], _ptr(ws),
-        ws.numel() if ws is not None else 0, _stream(device)))
+    dx = torch.empty(shape, dtype=kind, device=device)
+    needed = _entry("cpdp_add_rmsnorm_backward_workspace")(W, M, D)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_add_rmsnorm_backward")(
+        dy.data_ptr(), gs[0], gs[1], s.data_ptr(), ss[0], ss[1], t_at, ts[0], ts[1], weight.data_ptr(), ws[0], code, W, M, D, eps,
+        dx.data_ptr(), dweight.data_ptr(), dweight.stride(0), _CODES[dweight.dtype], _ptr(work), needed, _stream(device.index)))
     return dx, dweight
 
 
@@ -253,19 +267,16 @@ def checkpoint(x, *, values: bool = True, stream=None):
         saved, held = checkpoint(x[None], values=values, stream=stream)
         return saved, held[0] if values else None
     device = _cuda(x, "x")
-    if x.dim() != 3:
-        raise ValueError(f"x must be (W, M, D) or (M, D), got {tuple(x.shape)}")
-    on = _on(device, stream)
-    if on is not None:
-        with on:
+    if _elsewhere(device, stream):
+        with _there(device, stream):
             return checkpoint(x, values=values)
-    W, M, D = x.shape
+    W, M, D = shape = _three(x, "x")
     code = _dtype(x, "x")
-    _input(x, "x", (W, M, D), x.dtype, device)
+    xs = _input(x, "x", shape, x.dtype, device)
     saved = _new_checkpoint(W, M, D, device)
-    held = torch.empty((W, M, D), dtype=torch.bfloat16, device=device) if values else None
-    _check(lib().cpdp_checkpoint(x.data_ptr(), x.stride(0), x.stride(1), code, W, M, D, saved.codes.data_ptr(),
-                                 saved.exponents.data_ptr(), _ptr(held), _stream(device)))
+    held = torch.empty(shape, dtype=_BF16, device=device) if values else None
+    _check(_entry("cpdp_checkpoint")(x.data_ptr(), xs[0], xs[1], code, W, M, D, saved.codes.data_ptr(), saved.exponents.data_ptr(),
+                                     _ptr(held), _stream(device.index)))
     return saved, held
 
 
@@ -286,12 +297,11 @@ def restore(saved: Checkpoint, *, stream=None):
     """The bfloat16 values (W, M, D) that a Checkpoint stands for."""
     W, M, D = _saved(saved)
     device = saved.codes.device
-    on = _on(device, stream)
-    if on is not None:
-        with on:
+    if _elsewhere(device, stream):
+        with _there(device, stream):
             return restore(saved)
-    held = torch.empty((W, M, D), dtype=torch.bfloat16, device=device)
-    _check(lib().cpdp_restore(saved.codes.data_ptr(), saved.exponents.data_ptr(), W, M, D, held.data_ptr(), _stream(device)))
+    held = torch.empty((W, M, D), dtype=_BF16, device=device)
+    _check(_entry("cpdp_restore")(saved.codes.data_ptr(), saved.exponents.data_ptr(), W, M, D, held.data_ptr(), _stream(device.index)))
     return held
 
 
@@ -305,32 +315,27 @@ def weight_gradient(dy, saved: Checkpoint, *, out=None, dtype=torch.float32, str
         return weight_gradient(dy[None], saved, out=None if out is None else out[None], dtype=dtype, stream=stream)[0]
     W, M, D = _saved(saved)
     device = saved.codes.device
-    on = _on(device, stream)
-    if on is not None:
-        with on:
+    if _elsewhere(device, stream):
+        with _there(device, stream):
             return weight_gradient(dy, saved, out=out, dtype=dtype)
     code = _dtype(dy, "dy")
-    if dy.dim() != 3:
-        raise ValueError(f"dy must be (W, M, O) or (M, O), got {tuple(dy.shape)}")
-    O = dy.shape[2]
-    _input(dy, "dy", (W, M, O), dy.dtype, device)
+    O = _three(dy, "dy")[2]
+    gs = _input(dy, "dy", (W, M, O), dy.dtype, device)
     out = _gradient_out(out, "out", (W, O, D), dtype, device)
-    L = lib()
-    ws = _workspace(L.cpdp_weight_gradient_workspace(dy.data_ptr(), dy.stride(0), dy.stride(1), code, W, M, O, D), device)
-    _check(L.cpdp_weight_gradient(
-        dy.data_ptr(), dy.stride(0), dy.stride(1), code, saved.codes.data_ptr(), saved.exponents.data_ptr(), W, M, O, D,
-        out.data_ptr(), out.stride(0), _CODES[out.dtype], _ptr(ws), ws.numel() if ws is not None else 0, _stream(device)))
+    dy_at = dy.data_ptr()
+    needed = _entry("cpdp_weight_gradient_workspace")(dy_at, gs[0], gs[1], code, W, M, O, D)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_weight_gradient")(
+        dy_at, gs[0], gs[1], code, saved.codes.data_ptr(), saved.exponents.data_ptr(), W, M, O, D, out.data_ptr(), out.stride(0),
+        _CODES[out.dtype], _ptr(work), needed, _stream(device.index)))
     return out
 
 
-def _sequences(gate, value) -> torch.device:
-    device = _cuda(gate, "gate")
+def _sequences(gate) -> tuple:
     if gate.dim() != 3:
         raise ValueError(f"gate must be (B, T, D), got {tuple(gate.shape)}")
     _dtype(gate, "gate")
-    _input(gate, "gate", tuple(gate.shape), gate.dtype, device)
-    _input(value, "value", tuple(gate.shape), gate.dtype, device)
-    return device
+    return gate.shape
 
 
 def gated_recurrence(gate, value, h0=None, lengths=None, *, carry: bool = True, stream=None):
@@ -342,23 +347,22 @@ def gated_recurrence(gate, value, h0=None, lengths=None, *, carry: bool = True, 
     (h, h_last, carry): h (B, T, D) of gate's type, h_last float32 (B, D), and
     the states at every CARRY_STEPS steps, float32, which the backward pass
     starts from (carry=False: None)."""
-    device = _sequences(gate, value)
-    on = _on(device, stream)
-    if on is not None:
-        with on:
+    device = _cuda(gate, "gate")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
             return gated_recurrence(gate, value, h0, lengths, carry=carry)
-    B, T, D = gate.shape
-    _whole(h0, "h0", (B, D), torch.float32, device)
-    _whole(lengths, "lengths", (B,), torch.int32, device)
-    h = torch.empty((B, T, D), dtype=gate.dtype, device=device)
-    last = torch.empty((B, D), dtype=torch.float32, device=device)
-    carries = torch.empty((B, -(-T // CARRY_STEPS), D), dtype=torch.float32, device=device) if carry else None
-    L = lib()
-    ws = _workspace(L.cpdp_gated_recurrence_workspace(B, T, D), device)
-    _check(L.cpdp_gated_recurrence(
-        gate.data_ptr(), gate.stride(0), gate.stride(1), value.data_ptr(), value.stride(0), value.stride(1),
-        _CODES[gate.dtype], B, T, D, _ptr(h0), _ptr(lengths), h.data_ptr(), last.data_ptr(), _ptr(carries), _ptr(ws),
-        ws.numel() if ws is not None else 0, _stream(device)))
+    B, T, D = shape = _sequences(gate)
+    dtype = gate.dtype
+    gs, vs = _input(gate, "gate", shape, dtype, device), _input(value, "value", shape, dtype, device)
+    h0_at, n_at = _whole(h0, "h0", (B, D), _F32, device), _whole(lengths, "lengths", (B,), torch.int32, device)
+    h = torch.empty(shape, dtype=dtype, device=device)
+    last = torch.empty((B, D), dtype=_F32, device=device)
+    carries = torch.empty((B, -(-T // CARRY_STEPS), D), dtype=_F32, device=device) if carry else None
+    needed = _entry("cpdp_gated_recurrence_workspace")(B, T, D)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_gated_recurrence")(
+        gate.data_ptr(), gs[0], gs[1], value.data_ptr(), vs[0], vs[1], _CODES[dtype], B, T, D, h0_at, n_at, h.data_ptr(),
+        last.data_ptr(), _ptr(carries), _ptr(work), needed, _stream(device.index)))
     return h, last, carries
 
 
@@ -367,29 +371,26 @@ def gated_recurrence_backward(dh, gate, value, carry, dh_last=None, lengths=None
     and dh_last float32 (B, D) or None. dgate and dvalue are the halves of one
     (B, T, 2 D) tensor, ``out`` where given (contiguous along its last axis):
     the gradient of one product that made gate and value."""
-    device = _sequences(gate, value)
-    on = _on(device, stream)
-    if on is not None:
-        with on:
+    device = _cuda(gate, "gate")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
             return gated_recurrence_backward(dh, gate, value, carry, dh_last, lengths, out=out)
-    B, T, D = gate.shape
-    _input(dh, "dh", (B, T, D), gate.dtype, device)
-    _whole(carry, "carry", (B, -(-T // CARRY_STEPS), D), torch.float32, device)
-    _whole(dh_last, "dh_last", (B, D), torch.float32, device)
-    _whole(lengths, "lengths", (B,), torch.int32, device)
+    B, T, D = shape = _sequences(gate)
+    dtype = gate.dtype
+    gs, vs = _input(gate, "gate", shape, dtype, device), _input(value, "value", shape, dtype, device)
+    os = _input(dh, "dh", shape, dtype, device)
+    carry_at = _whole(carry, "carry", (B, -(-T // CARRY_STEPS), D), _F32, device)
+    last_at, n_at = _whole(dh_last, "dh_last", (B, D), _F32, device), _whole(lengths, "lengths", (B,), torch.int32, device)
     if out is None:
-        out = torch.empty((B, T, 2 * D), dtype=gate.dtype, device=device)
-    else:
-        _input(out, "out", (B, T, 2 * D), gate.dtype, device)
+        out = torch.empty((B, T, 2 * D), dtype=dtype, device=device)
+    ps = _input(out, "out", (B, T, 2 * D), dtype, device)
     dgate, dvalue = out[..., :D], out[..., D:]
-    dh0 = torch.empty((B, D), dtype=torch.float32, device=device)
-    L = lib()
-    ws = _workspace(L.cpdp_gated_recurrence_workspace(B, T, D), device)
-    _check(L.cpdp_gated_recurrence_backward(
-        dh.data_ptr(), dh.stride(0), dh.stride(1), gate.data_ptr(), gate.stride(0), gate.stride(1), value.data_ptr(),
-        value.stride(0), value.stride(1), _CODES[gate.dtype], B, T, D, carry.data_ptr(), _ptr(dh_last), _ptr(lengths),
-        dgate.data_ptr(), dvalue.data_ptr(), out.stride(0), out.stride(1), dh0.data_ptr(), _ptr(ws),
-        ws.numel() if ws is not None else 0, _stream(device)))
+    dh0 = torch.empty((B, D), dtype=_F32, device=device)
+    needed = _entry("cpdp_gated_recurrence_workspace")(B, T, D)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_gated_recurrence_backward")(
+        dh.data_ptr(), os[0], os[1], gate.data_ptr(), gs[0], gs[1], value.data_ptr(), vs[0], vs[1], _CODES[dtype], B, T, D, carry_at,
+        last_at, n_at, dgate.data_ptr(), dvalue.data_ptr(), ps[0], ps[1], dh0.data_ptr(), _ptr(work), needed, _stream(device.index)))
     return dgate, dvalue, dh0
 
 
@@ -397,20 +398,17 @@ def gated_recurrence_step(gate, value, state, *, stream=None):
     """One token for each of B sequences: ``state`` (float32, (B, D)) is replaced
     by the next state, which is returned rounded to gate's type. gate, value (B, D)."""
     device = _cuda(gate, "gate")
-    if gate.dim() != 2:
-        raise ValueError(f"gate must be (B, D), got {tuple(gate.shape)}")
-    code = _dtype(gate, "gate")
-    shape = tuple(gate.shape)
-    _input(gate, "gate", shape, gate.dtype, device)
-    _input(value, "value", shape, gate.dtype, device)
-    _whole(state, "state", shape, torch.float32, device)
-    on = _on(device, stream)
-    if on is not None:
-        with on:
+    if _elsewhere(device, stream):
+        with _there(device, stream):
             return gated_recurrence_step(gate, value, state)
-    h = torch.empty(shape, dtype=gate.dtype, device=device)
-    _check(lib().cpdp_gated_recurrence_step(gate.data_ptr(), gate.stride(0), value.data_ptr(), value.stride(0), code,
-                                            shape[0], shape[1], state.data_ptr(), h.data_ptr(), _stream(device)))
+    shape, dtype, code = gate.shape, gate.dtype, _dtype(gate, "gate")
+    if len(shape) != 2:
+        raise ValueError(f"gate must be (B, D), got {tuple(shape)}")
+    gs, vs = _input(gate, "gate", shape, dtype, device), _input(value, "value", shape, dtype, device)
+    state_at = _whole(state, "state", shape, _F32, device)
+    h = torch.empty(shape, dtype=dtype, device=device)
+    _check(_entry("cpdp_gated_recurrence_step")(gate.data_ptr(), gs[0], value.data_ptr(), vs[0], code, shape[0], shape[1], state_at,
+                                                h.data_ptr(), _stream(device.index)))
     return h
 
 
@@ -418,5 +416,5 @@ def wait_timeouts() -> int:
     """Bounded waits of the weight gradient's kernel that ran out since the last
     call (0 expected). Waits for the current device."""
     count = _L()
-    _check(lib().cpdp_layer_timeouts(ctypes.byref(count)))
+    _check(_entry("cpdp_layer_timeouts")(ctypes.byref(count)))
     return count.value
