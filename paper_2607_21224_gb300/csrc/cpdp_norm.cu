@@ -135,7 +135,7 @@ norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weig
 // from row to row; `parts` receives them, one row per block. KEEP: the weights
 // stay in registers too.
 template <typename T, int V, int TPR, int E, bool KEEP>
-__global__ void __launch_bounds__(RowThreads<TPR>::block)
+__global__ void __launch_bounds__(RowThreads<TPR>::block, TPR > 128 ? 1 : E == 32 ? 2 : 4)
 norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_t weight_worker, int64_t M, int D, float eps,
                      void* dx, float* parts) {
     layer_begin();
