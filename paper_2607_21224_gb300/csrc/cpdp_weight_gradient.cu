@@ -14,18 +14,21 @@ namespace {
 // over, as their slow axis; a slot holds them as rows of 64 elements (128
 // bytes) per token in the 128-byte swizzle, one block of rows per 64 columns:
 //   dy   bfloat16, by one tensor copy per block of rows
-//   x^   made by the eight converting warps from codes and exponents, each
-//        thread one block of 32 features of one token: exact in bfloat16
+//   x^   made by converting warps from codes and exponents, each thread one
+//        block of 32 features of one token: exact in bfloat16. Groups of eight
+//        warps take the steps in turn: one group needs 900 clocks for a step
+//        (wait, convert, store, hand over), the tensor core 512.
 // One thread issues the matrix instructions. The accumulator is in tensor
 // memory; the converting warps read it back when all steps are done.
 constexpr int kTileI = 128, kTileO = 256, kStep = 64, kSlots = 4;
-constexpr int kConvertWarps = 8, kThreads = (kConvertWarps + 2) * 32;  // and a copying and a multiplying warp
+constexpr int kGroupWarps = 8, kGroups = 2, kConvertWarps = kGroupWarps * kGroups;
+constexpr int kThreads = (kConvertWarps + 2) * 32;  // and a copying and a multiplying warp
 constexpr int kBlockBytes = kStep * 128;                               // a step's rows of 64 elements
 constexpr int kXBytes = kTileI / 64 * kBlockBytes, kDyBytes = kTileO / 64 * kBlockBytes, kSlotBytes = kXBytes + kDyBytes;
 constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;  // and room to align the slots
-constexpr int kAhead = 4;                               // steps whose codes are loaded ahead
+constexpr int kAhead = 2;                               // of its steps whose codes a group loads ahead
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
-static_assert(kStep * kTileI == kConvertWarps * 32 * kBlock8, "one block of features per converting thread and step");
+static_assert(kStep * kTileI == kGroupWarps * 32 * kBlock8, "one block of features per converting thread and step");
 
 __device__ unsigned long long wait_timeouts;
 
@@ -41,19 +44,20 @@ __device__ __forceinline__ void barrier_init(uint64_t* b, uint32_t count) {
 __device__ __forceinline__ void barrier_arrive(uint64_t* b) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_at(b)) : "memory");
 }
-__device__ __forceinline__ bool barrier_done(uint64_t* b, uint32_t parity) {
+// Whether the phase is done, after waiting in hardware for up to `ns`.
+__device__ __forceinline__ bool barrier_done(uint64_t* b, uint32_t parity, uint32_t ns) {
     uint32_t done;
     asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
-        : "r"(smem_at(b)), "r"(parity)
+        : "r"(smem_at(b)), "r"(parity), "r"(ns)
         : "memory");
     return done != 0;
 }
 // False, and counted, where the phase does not end within the limit.
 __device__ __noinline__ bool barrier_wait_long(uint64_t* b, uint32_t parity) {
     const unsigned long long start = now_ns();
-    while (!barrier_done(b, parity))
+    while (!barrier_done(b, parity, 100000u))
         if (now_ns() - start > kWaitLimitNs) {
             atomicAdd(&wait_timeouts, 1ull);
             return false;
@@ -61,7 +65,7 @@ __device__ __noinline__ bool barrier_wait_long(uint64_t* b, uint32_t parity) {
     return true;
 }
 __device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity) {
-    return barrier_done(b, parity) || barrier_wait_long(b, parity);
+    return barrier_done(b, parity, 100000u) || barrier_wait_long(b, parity);
 }
 
 // A matrix in shared memory whose rows of 64 elements run along the summed
@@ -149,7 +153,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
     const uint32_t slots = (smem_at(raw) + 1023u) & ~1023u;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kSlots; ++s) {
-            barrier_init(&full[s], kConvertWarps + 1);
+            barrier_init(&full[s], kGroupWarps + 1);
             barrier_init(&empty[s], 1);
         }
         barrier_init(&done, 1);
@@ -206,35 +210,45 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
             if (steps > 0) arrive_when_multiplied(&done);
         }
     } else {
-        // thread: token 8 * warp + lane / 4 of the step, features 32 * (lane % 4) + 0..31 of the tile
-        const int token = warp * 8 + lane / 4, quarter = lane % 4, block = i0 / kBlock8 + quarter;
+        // thread: token 8 * (its warp in the group) + lane / 4 of the step, features 32 * (lane % 4) + 0..31 of the tile
+        const int token = warp % kGroupWarps * 8 + lane / 4, quarter = lane % 4, block = i0 / kBlock8 + quarter;
         // rows of 64 elements are two blocks of 32; the two rows' threads store their 16-byte pieces in another
         // order, so that eight neighbouring threads meet in no bank
         const int swap = quarter / 2;
         const uint32_t row = slots + (quarter / 2) * kBlockBytes + token * 128;
-        const int64_t base = w * p.M + first;
-        const auto load = [&](int k) {
+        uint32_t piece[4];  // where the four 16-byte pieces go
+#pragma unroll
+        for (int k = 0; k < 4; ++k) piece[k] = row + (((quarter % 2 * 4 + (k ^ swap * 2)) ^ token % 8) << 4);
+        // the thread's next step, its codes and its exponent
+        const int64_t at = (w * p.M + first + warp / kGroupWarps * kStep + token) * p.blocks + block;
+        const uint4* next_codes = reinterpret_cast<const uint4*>(p.codes + at * kBlock8) + swap;
+        const uint8_t* next_byte = p.exponents + at;
+        const int64_t down = (int64_t)kGroups * kStep * p.blocks;
+        const int other = swap ? -1 : 1;
+        int left = block < p.blocks ? static_cast<int>(tokens) - token - warp / kGroupWarps * kStep : 0;  // > 0: there is a token
+        const auto load = [&]() {
             Codes c{};
-            const int64_t m = (int64_t)k * kStep + token;
-            if (m < tokens && block < p.blocks) {
-                const uint4* q = reinterpret_cast<const uint4*>(p.codes + ((base + m) * p.blocks + block) * kBlock8);
-                c.half[0] = __ldg(q + swap);
-                c.half[1] = __ldg(q + (swap ^ 1));
-                c.byte = __ldg(p.exponents + (base + m) * p.blocks + block);
+            if (left > 0) {
+                c.half[0] = __ldg(next_codes);
+                c.half[1] = __ldg(next_codes + other);
+                c.byte = __ldg(next_byte);
             }
+            left -= kGroups * kStep;
+            next_codes += down * (kBlock8 / 16);
+            next_byte += down;
             return c;
         };
         Codes ahead[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) ahead[u] = load(u);
+        for (int u = 0; u < kAhead; ++u) ahead[u] = load();
         bool ok = true;
-        for (int k0 = 0; k0 < steps && ok; k0 += kAhead) {
+        for (int k0 = warp / kGroupWarps; k0 < steps && ok; k0 += kAhead * kGroups) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int k = k0 + u, s = k % kSlots;
+                const int k = k0 + u * kGroups, s = k % kSlots;
                 if (k >= steps || !ok) break;
                 const Codes c = ahead[u];
-                ahead[u] = load(k + kAhead);
+                ahead[u] = load();
                 if (k >= kSlots) ok = __all_sync(~0u, barrier_wait(&empty[s], (k / kSlots - 1) & 1));
                 if (!ok) break;
                 // a block with an infinite or NaN value reads as NaN
@@ -245,8 +259,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
                     for (int e = 0; e < 2; ++e) {
                         const uint2 lo = values_of(e == 0 ? c.half[h].x : c.half[h].z, unit);
                         const uint2 hi = values_of(e == 0 ? c.half[h].y : c.half[h].w, unit);
-                        const int piece = (quarter % 2) * 4 + ((h ^ swap) * 2 + e);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + s * kSlotBytes + ((piece ^ (token % 8)) << 4)),
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece[h * 2 + e] + s * kSlotBytes),
                                      "r"(lo.x), "r"(lo.y), "r"(hi.x), "r"(hi.y)
                                      : "memory");
                     }
@@ -255,13 +268,14 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
                 if (lane == 0) barrier_arrive(&full[s]);
             }
         }
-        // warp: lanes 32 * (warp % 4) of the accumulator, half of its columns
+        // warp: lanes 32 * (warp % 4) of the accumulator, one in kConvertWarps / 4 parts of its columns
         if (steps > 0) __all_sync(~0u, barrier_wait(&done, 0));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        constexpr int kPart = kTileO * 4 / kConvertWarps;
         const int i = i0 + warp % 4 * 32 + lane;
         G* out = static_cast<G*>(p.out) + split * p.out_split + w * p.out_worker + i;
 #pragma unroll 1
-        for (int c = warp / 4 * (kTileO / 2); c < (warp / 4 + 1) * (kTileO / 2) && o0 + c < p.O; c += 32) {
+        for (int c = warp / 4 * kPart; c < (warp / 4 + 1) * kPart && o0 + c < p.O; c += 32) {
             float v[32];
             if (steps > 0) read_sums(sums + (warp % 4 * 32 << 16) + c, v);
             if (i < p.I)
@@ -323,19 +337,27 @@ sum_parts_kernel(const float* parts, int splits, int64_t per_worker, int64_t all
     }
 }
 
-// Splits of the token axis: where there are fewer tiles than SMs, as many as
-// fill them, of at least 4 steps each.
+// How the tokens are split: the number of parts that takes least time, by the
+// turns that the blocks take on the SMs. A step of a block takes 0.36 us, its
+// start and end 4; parts cost their writing and reading at 4 TB/s and a launch.
 struct Splits {
-    int64_t steps, each;
     int count;
+    int64_t each;  // steps of a part
 };
 Splits splits_of(int W, int64_t M, int O, int I) {
     const int64_t steps = ceil_div(M, kStep), tiles = ceil_div(I, kTileI) * ceil_div(O, kTileO) * W;
-    int64_t count = tiles >= kSMs ? 1 : kSMs / tiles;
-    if (count > steps / 4) count = steps / 4;
-    if (count < 1) count = 1;
-    const int64_t each = ceil_div(steps, count);
-    return {steps, each, each > 0 ? static_cast<int>(ceil_div(steps, each)) : 1};
+    Splits best{1, steps};
+    double least = 0;
+    for (int64_t count = 1; count <= 64 && (count == 1 || count * 4 <= steps); ++count) {
+        const int64_t each = ceil_div(steps, count), parts = each > 0 ? ceil_div(steps, each) : 1;
+        double us = static_cast<double>(ceil_div(tiles * parts, kSMs)) * (each * 0.36 + 4.0);
+        if (parts > 1) us += 3.0 + 2e-6 * parts * W * O * I;
+        if (count == 1 || us < least) {
+            least = us;
+            best = {static_cast<int>(parts), each};
+        }
+    }
+    return best;
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
