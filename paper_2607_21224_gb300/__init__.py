@@ -3,6 +3,7 @@
 
 - ``cpdp``: binding of the C ABI in include/cpdp.h (libcpdp.so, CUDA, sm_103a)
 - ``state.CPDPState``: W replicas on one GPU driven through that library
+- ``layers``: worker-batched layers (include/cpdp_layers.h) that make the gradients
 - ``workloads``: seeded synthetic inputs shaped like the paper's models
 - ``build``: compiles libcpdp.so in-tree
 """
