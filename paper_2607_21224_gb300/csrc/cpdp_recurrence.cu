@@ -259,7 +259,7 @@ recurrence_kernel(SeqIn gate, SeqIn value, int steps, int D, const float* h0, co
     if (MAPS && task.order == x.count - 1) return;  // nobody asks for the last one
     const int c = task.channel + first_channel<WIDE>(lane), n = lengths == nullptr ? steps : min(max(lengths[task.b], 0), steps);
     const int first = task.order * x.steps, end = min(first + x.steps, steps), inside = min(max(n - first, 0), end - first);
-    const bool live = c < D, second = c + kSecond<WIDE> < D, all_channels = task.channel + kChannels <= D;
+    const bool live = c < D, second = c + kSecond<WIDE> < D;
     const T* g = static_cast<const T*>(gate.p) + task.b * gate.seq + first * gate.step + task.channel;
     const T* v = static_cast<const T*>(value.p) + task.b * value.seq + first * value.step + task.channel;
     const auto fetch = [&](int k) {
@@ -291,25 +291,27 @@ recurrence_kernel(SeqIn gate, SeqIn value, int steps, int D, const float* h0, co
             store_two<WIDE>(carries, s, second);
             carries += D;
         }
+        // FULL: all R steps are inside. Else those beyond are the identity; a
+        // break there would leave nothing to overlap, 250 clocks a step.
         const auto walk = [&](auto known) {
-            constexpr bool ALL = decltype(known)::value;
+            constexpr bool FULL = decltype(known)::value;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                if (!ALL && r >= rows) break;
                 Map one;
                 Pair rest;
                 gate_of(gs.get(r), one.a, rest);
                 one.b = mul2(rest, vs.get(r));
+                if (!FULL && r >= rows) one = kSame;
                 if constexpr (MAPS) {
                     m = then(m, one);
                 } else {
                     s = apply(one, s);
-                    if (ALL || live) store_two<WIDE>(out, s, ALL || second);
-                    out += D;
+                    if (live && (FULL || r < rows)) store_two<WIDE>(out + (int64_t)r * D, s, second);
                 }
             }
+            out += (int64_t)min(rows, R) * D;
         };
-        if (rows >= R && all_channels)
+        if (rows >= R)
             walk(std::true_type{});
         else
             walk(std::false_type{});
@@ -383,22 +385,23 @@ recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int steps, int D, 
         const uint8_t* slot = ring + i % kRing * (kArrays * kChunk);
         const Chunk<T, WIDE> gs(slot, g + t * gate.step, gate.step), os(slot + kChunk, o + t * dh.step, dh.step),
             vs(slot + 2 * kChunk, v + t * value.step, value.step);
-        const auto walk = [&](auto known) {
-            constexpr bool ALL = decltype(known)::value;
+        const auto walk = [&](auto known, auto every) {
+            constexpr bool FULL = decltype(known)::value;
             if constexpr (MAPS) {
 #pragma unroll
                 for (int r = R - 1; r >= 0; --r) {
-                    if (!ALL && r >= rows) continue;
                     Pair a, rest;
                     gate_of(gs.get(r), a, rest);
+                    if (!FULL && r >= rows) a = kOnes;  // dh is 0 there
                     m = Map{mul2(a, m.a), mul2(a, add2(os.get(r), m.b))};
                 }
             } else {
+                constexpr bool ALL = FULL && decltype(every)::value;
                 Pair a[R], rest[R], away[R];  // away: (h_(t-1) - v_t) a_t
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    if (!ALL && r >= rows) break;
                     gate_of(gs.get(r), a[r], rest[r]);
+                    if (!FULL && r >= rows) a[r] = kOnes, rest[r] = kZeros;
                     const Pair vr = vs.get(r);
                     away[r] = mul2(fma2(vr, kMinusOnes, s), a[r]);
                     s = fma2(a[r], s, mul2(rest[r], vr));
@@ -406,20 +409,21 @@ recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int steps, int D, 
                 T *dg = dgate + out0 + (t + R - 1) * grad_step, *dv = dvalue + out0 + (t + R - 1) * grad_step;
 #pragma unroll
                 for (int r = R - 1; r >= 0; --r, dg -= grad_step, dv -= grad_step) {
-                    if (!ALL && r >= rows) continue;
                     const Pair both = add2(os.get(r), flow), y = mul2(rest[r], both);
                     flow = mul2(a[r], both);
-                    if (ALL || live) {
-                        store_two<WIDE>(dv, y, ALL || second);
-                        store_two<WIDE>(dg, mul2(y, away[r]), ALL || second);
+                    if (ALL || (live && (FULL || r < rows))) {
+                        store_two<WIDE>(dv, y, second);
+                        store_two<WIDE>(dg, mul2(y, away[r]), second);
                     }
                 }
             }
         };
         if (rows >= R && all_channels)
-            walk(std::true_type{});
+            walk(std::true_type{}, std::true_type{});
+        else if (rows >= R)
+            walk(std::true_type{}, std::false_type{});
         else
-            walk(std::false_type{});
+            walk(std::false_type{}, std::false_type{});
         __syncwarp();
     }
     if constexpr (MAPS)
