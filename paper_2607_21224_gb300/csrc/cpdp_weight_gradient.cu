@@ -1,5 +1,6 @@
 // The weight gradient dW = dy^T x^ from activations held in 8 bits
 // (include/cpdp_layers.h).
+#include <climits>
 #include <cuda.h>
 
 #include "cpdp_layers.cuh"
@@ -18,11 +19,20 @@ namespace {
 //        block of 32 features of one token: exact in bfloat16. Groups of eight
 //        warps take the steps in turn: one group needs 900 clocks for a step
 //        (wait, convert, store, hand over), the tensor core 512.
-// One thread issues the matrix instructions. The accumulator is in tensor
-// memory; the converting warps read it back when all steps are done.
+// One thread issues the matrix instructions. The sums are in tensor memory, in
+// two halves that take chunks of the steps in turn: four writing warps add a
+// finished chunk to the output while the next one is multiplied, the converting
+// warps the last one. The tensor core cuts its float32
+// sums off where others round them, always towards 0: over 16,384 tokens that
+// made dW 6e-6 too small. So where the output is float32 a chunk has kChunk
+// steps, and the chunks are added up, rounded to nearest, in the output; 2,048
+// tokens lose 7e-7. A bfloat16 output, which rounds to 4e-3, is one chunk.
 constexpr int kTileI = 128, kTileO = 256, kStep = 64, kSlots = 4;
 constexpr int kGroupWarps = 8, kGroups = 2, kConvertWarps = kGroupWarps * kGroups;
-constexpr int kThreads = (kConvertWarps + 2) * 32;  // and a copying and a multiplying warp
+constexpr int kCopyWarp = kConvertWarps, kMultiplyWarp = kConvertWarps + 1, kWriteWarp = kConvertWarps + 2;  // the first of four
+template <typename G>
+constexpr int kThreads = (kConvertWarps + 2 + (sizeof(G) == 4 ? 4 : 0)) * 32;  // one chunk needs no writing warps
+constexpr int kChunk = 32;  // steps
 constexpr int kBlockBytes = kStep * 128;                               // a step's rows of 64 elements
 constexpr int kXBytes = kTileI / 64 * kBlockBytes, kDyBytes = kTileO / 64 * kBlockBytes, kSlotBytes = kXBytes + kDyBytes;
 constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;  // and room to align the slots
@@ -88,22 +98,19 @@ __device__ __forceinline__ void multiply(uint32_t sums, uint64_t a, uint64_t b, 
 __device__ __forceinline__ void arrive_when_multiplied(uint64_t* b) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(b)) : "memory");
 }
-// 32 columns of the warp's 32 lanes.
-__device__ __forceinline__ void read_sums(uint32_t at, float (&v)[32]) {
-    uint32_t r[32];
+// 16 columns of the warp's 32 lanes.
+__device__ __forceinline__ void read_sums(uint32_t at, float (&v)[16]) {
+    uint32_t r[16];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(at)
         : "memory");
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 __device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
@@ -138,16 +145,51 @@ struct WeightGradient {
     int O, I, W, blocks;  // blocks of 32 features in a row of x^
     int splits;           // of the tokens; more than one: parts [splits][W][O][I] of float32
     int64_t split_steps;
+    int chunk;            // steps that are summed in tensor memory before they are written out
     void* out;
     int64_t out_worker, out_split;
 };
 
+// Columns [first, first + count) of the sums at `sums` to the output, the
+// warp's 32 lanes of i: added to what is there (`add`), or in its place; zeros
+// where there are no sums (`any` false). The additions are done by L2, which
+// spares the wait for what is there. Each element has one adder at a time, in
+// the chunks' order, so the result does not vary; sums below 1.2e-38 become 0.
+template <typename G>
+__device__ __forceinline__ void write_out(const WeightGradient& p, uint32_t sums, int i0, int o0, int first, int count, bool add, bool any,
+                                          G* out) {
+    const int quarter = threadIdx.x / 32 % 4 * 32, i = i0 + quarter + static_cast<int>(threadIdx.x % 32);
+    const int end = min(p.O - o0, first + count);
+    G* to = out + (int64_t)(o0 + first) * p.I + i;
+#pragma unroll 1
+    for (int o = first; o < end; o += 16, to += (int64_t)16 * p.I) {
+        float v[16] = {};
+        if (any) read_sums(sums + (quarter << 16) + o, v);
+        if (i < p.I) {
+            bool stored = false;
+            if constexpr (sizeof(G) == 4)
+                if (add) {
+                    stored = true;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (o + j < end) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(to + (int64_t)j * p.I), "f"(v[j]) : "memory");
+                }
+            if (!stored) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (o + j < end) to[(int64_t)j * p.I] = from_float<G>(v[j]);
+            }
+        }
+        __syncwarp();
+    }
+}
+
 // G: the output's type.
 template <typename G>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads<G>, 1)
 weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p) {
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[kSlots], empty[kSlots], done;
+    __shared__ uint64_t full[kSlots], empty[kSlots], summed[2], written[2], all_written;
     __shared__ uint32_t tensor_memory;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t slots = (smem_at(raw) + 1023u) & ~1023u;
@@ -156,11 +198,15 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
             barrier_init(&full[s], kGroupWarps + 1);
             barrier_init(&empty[s], 1);
         }
-        barrier_init(&done, 1);
+        for (int h = 0; h < 2; ++h) {
+            barrier_init(&summed[h], 1);
+            barrier_init(&written[h], 4);
+        }
+        barrier_init(&all_written, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kConvertWarps + 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tensor_memory)), "r"(kTileO)
+    if (warp == kMultiplyWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tensor_memory)), "r"(2 * kTileO)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -174,9 +220,10 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
     const int w = blockIdx.z % p.W, split = blockIdx.z / p.W;
     const int64_t first = split * p.split_steps * kStep;
     const int64_t tokens = min(p.M - first, p.split_steps * kStep);
-    const int steps = static_cast<int>((tokens + kStep - 1) / kStep);
+    const int steps = static_cast<int>((tokens + kStep - 1) / kStep), chunks = (steps + p.chunk - 1) / p.chunk;
 
-    if (warp == kConvertWarps) {
+    G* const out0 = static_cast<G*>(p.out) + split * p.out_split + w * p.out_worker;
+    if (warp == kCopyWarp) {
         if (lane == 0) {
             int k = 0;
             for (; k < steps; ++k) {
@@ -194,20 +241,42 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
             if (k < steps)
                 for (int q = max(k - kSlots, 0); q < k; ++q) barrier_wait(&full[q % kSlots], q / kSlots & 1);
         }
-    } else if (warp == kConvertWarps + 1) {
+    } else if (warp == kMultiplyWarp) {
         if (lane == 0) {
             bool ok = true;
-            for (int k = 0; k < steps && ok; ++k) {
-                const int s = k % kSlots;
-                ok = barrier_wait(&full[s], k / kSlots & 1);
-                if (!ok) break;
+            for (int c = 0; c < chunks && ok; ++c) {
+                const int h = c % 2, end = min((c + 1) * p.chunk, steps);
+                if (c >= 2) ok = barrier_wait(&written[h], (c / 2 - 1) & 1);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint64_t a = matrix_at(slots + s * kSlotBytes), b = matrix_at(slots + s * kSlotBytes + kXBytes);
+                for (int k = c * p.chunk; k < end && ok; ++k) {
+                    const int s = k % kSlots;
+                    ok = barrier_wait(&full[s], k / kSlots & 1);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t a = matrix_at(slots + s * kSlotBytes), b = matrix_at(slots + s * kSlotBytes + kXBytes);
 #pragma unroll
-                for (int c = 0; c < kStep / 16; ++c) multiply(sums, a + c * (2048 >> 4), b + c * (2048 >> 4), k > 0 || c > 0);
-                arrive_when_multiplied(&empty[s]);
+                    for (int q = 0; q < kStep / 16; ++q)
+                        multiply(sums + h * kTileO, a + q * (2048 >> 4), b + q * (2048 >> 4), k > c * p.chunk || q > 0);
+                    arrive_when_multiplied(&empty[s]);
+                }
+                arrive_when_multiplied(&summed[h]);
             }
-            if (steps > 0) arrive_when_multiplied(&done);
+        }
+    } else if (warp >= kWriteWarp) {
+        if constexpr (sizeof(G) == 4) {
+            bool ok = true;
+            for (int c = 0; c < chunks - 1 && ok; ++c) {
+                const int h = c % 2;
+                ok = __all_sync(~0u, barrier_wait(&summed[h], c / 2 & 1));
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                write_out(p, sums + h * kTileO, i0, o0, 0, kTileO, c > 0, true, out0);
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) barrier_arrive(&written[h]);
+            }
+            __threadfence();  // these additions before those of the converting warps
+            __syncwarp();
+            if (lane == 0) barrier_arrive(&all_written);
         }
     } else {
         // thread: token 8 * (its warp in the group) + lane / 4 of the step, features 32 * (lane % 4) + 0..31 of the tile
@@ -268,27 +337,21 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
                 if (lane == 0) barrier_arrive(&full[s]);
             }
         }
-        // warp: lanes 32 * (warp % 4) of the accumulator, one in kConvertWarps / 4 parts of its columns
-        if (steps > 0) __all_sync(~0u, barrier_wait(&done, 0));
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        // The last chunk, after those before it are in the output. Its barrier has
+        // by now seen the chunk two before: the slots just filled were free, so
+        // the products are at most 2 kSlots steps behind.
+        static_assert(kChunk >= 2 * kSlots, "the parity of `summed` tells the last chunk from the one two before");
         constexpr int kPart = kTileO * 4 / kConvertWarps;
-        const int i = i0 + warp % 4 * 32 + lane;
-        G* out = static_cast<G*>(p.out) + split * p.out_split + w * p.out_worker + i;
-#pragma unroll 1
-        for (int c = warp / 4 * kPart; c < (warp / 4 + 1) * kPart && o0 + c < p.O; c += 32) {
-            float v[32];
-            if (steps > 0) read_sums(sums + (warp % 4 * 32 << 16) + c, v);
-            if (i < p.I)
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (o0 + c + j < p.O) out[(int64_t)(o0 + c + j) * p.I] = from_float<G>(steps > 0 ? v[j] : 0.f);
-        }
+        if (chunks > 0) __all_sync(~0u, barrier_wait(&summed[(chunks - 1) % 2], (chunks - 1) / 2 & 1));
+        if (chunks > 1) __all_sync(~0u, barrier_wait(&all_written, 0));
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        write_out(p, sums + (chunks > 0 ? (chunks - 1) % 2 : 0) * kTileO, i0, o0, warp / 4 * kPart, kPart, chunks > 1, chunks > 0, out0);
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
     __syncthreads();
-    if (warp == kConvertWarps + 1) {
+    if (warp == kMultiplyWarp) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(kTileO));
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(2 * kTileO));
     }
 }
 
@@ -440,6 +503,7 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     p.codes = codes, p.exponents = exponents;
     p.M = M, p.O = O, p.I = I, p.W = W, p.blocks = static_cast<int>(ceil_div(I, kBlock8));
     p.splits = sp.count, p.split_steps = sp.each;
+    p.chunk = parts || dW_dtype == CPDP_F32 ? kChunk : INT_MAX / 2;
     p.out = parts ? workspace : dW;
     p.out_worker = parts ? (int64_t)O * I : dW_worker;
     p.out_split = (int64_t)W * O * I;
@@ -471,13 +535,13 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
         if (r != CUDA_SUCCESS) return layer_error(CPDP_ECUDA, "cuTensorMapEncodeTiled: error %d", (int)r);
     }
     const dim3 grid(ceil_div(I, kTileI), ceil_div(O, kTileO), sp.count * W);
-    const auto go = [&](auto kernel) {
+    const auto go = [&](auto kernel, int threads) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-        return e != cudaSuccess ? e : launch_layer(kernel, grid, kThreads, kSmemBytes, stream, map, p);
+        return e != cudaSuccess ? e : launch_layer(kernel, grid, threads, kSmemBytes, stream, map, p);
     };
     const auto typed = [&](auto g) {
         using G = decltype(g);
-        return go(weight_gradient_kernel<G>);
+        return go(weight_gradient_kernel<G>, kThreads<G>);
     };
     CPDP_TRY(layer_launched(parts || dW_dtype == CPDP_F32 ? typed(0.f) : typed(__nv_bfloat16{}), "cpdp_weight_gradient"));
     if (!parts) return CPDP_OK;

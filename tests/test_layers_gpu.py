@@ -203,6 +203,55 @@ def test_weight_gradient(shape, grad, layout):
     assert torch.equal(layers.weight_gradient(dy.cuda(), saved, dtype=grad), got)
 
 
+def test_weight_gradient_of_many_tokens_keeps_its_precision():
+    """128 tiles of 16,384 tokens, so no split of the tokens: one chain of 1,024 products would cut dW by 6e-6.
+    Chunks of 128 products, each cutting at most 2^-25 of a sum that is two thirds of the last on average: 2.5e-6."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(16, 16384, 512, generator=gen, device="cuda")
+    dy = torch.randn(16, 16384, 512, generator=gen, device="cuda").to(BF16)
+    saved, values = layers.checkpoint(x)
+    dW = layers.weight_gradient(dy, saved)
+    again = layers.weight_gradient(dy, saved)
+    want = torch.einsum("wmo,wmi->woi", dy.double(), values.double())
+    assert float((dW.double() - want).norm() / want.norm()) <= 2.5e-6
+    assert torch.equal(dW, again)
+    half = layers.weight_gradient(dy, saved, dtype=BF16)
+    near(half, want.cpu(), 2e-4 * want.abs().cpu() + 2e-3)
+
+
+def test_arrays_of_more_than_two_to_the_31_elements():
+    """The last rows of arrays past 32-bit offsets, against the same rows alone."""
+    M, D, tail = 540_000, 4096, 64
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.empty(1, M, D, dtype=BF16, device="cuda").normal_(generator=gen)
+    assert x.numel() > 2 ** 31
+    w = torch.rand(1, D, generator=gen, device="cuda")
+    last = x[:, -tail:].contiguous()
+    y, _, saved = layers.add_rmsnorm(x, w, x, checkpoint=True)
+    y2, s2, saved2 = layers.add_rmsnorm(last, w, last, checkpoint=True)
+    assert torch.equal(y[:, -tail:], y2) and torch.equal(saved.codes[:, -tail:], saved2.codes)
+    assert torch.equal(layers.restore(saved)[:, -tail:], y2)
+    del y
+    dx, dw = layers.add_rmsnorm_backward(x, x, w)
+    assert torch.equal(dx[:, -tail:], layers.add_rmsnorm_backward(last, last, w)[0]) and torch.isfinite(dw).all()
+    del dx
+    held, values = layers.checkpoint(x)
+    assert torch.equal(values[:, -tail:], layers.checkpoint(last)[1])
+    del values
+    dy = torch.zeros(1, M, 16, dtype=BF16, device="cuda")
+    dy[:, -tail:] = 1
+    part = layers.weight_gradient(dy[:, -tail:].contiguous(), layers.checkpoint(last)[0])
+    assert torch.allclose(layers.weight_gradient(dy, held), part, rtol=1e-5, atol=1e-3)
+    del held
+    h, end, carry = layers.gated_recurrence(x, x)
+    h2, end2, carry2 = layers.gated_recurrence(last, last, carry[:, (M - tail) // layers.CARRY_STEPS])
+    assert torch.allclose(h[:, -tail:].float(), h2.float(), rtol=1e-2, atol=1e-5) and torch.allclose(end, end2, rtol=1e-5, atol=1e-6)
+    dgate, dvalue, _ = layers.gated_recurrence_backward(x, x, x, carry)
+    dgate2, dvalue2, _ = layers.gated_recurrence_backward(last, last, last, carry2)
+    assert torch.allclose(dgate[:, -tail:].float(), dgate2.float(), rtol=1e-2, atol=1e-5)
+    assert torch.allclose(dvalue[:, -tail:].float(), dvalue2.float(), rtol=1e-2, atol=1e-5)
+
+
 def test_weight_gradient_of_no_tokens_and_of_nan():
     saved, _ = layers.checkpoint(torch.empty(2, 0, 40, device="cuda"))
     out = torch.full((2, 24, 40), 3.0, device="cuda")
