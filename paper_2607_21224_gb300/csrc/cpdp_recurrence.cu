@@ -19,7 +19,8 @@ template <typename T>
 constexpr int kBackwardRing = sizeof(T) == 2 ? 3 : 2;
 template <typename T>
 constexpr int kForwardWarps = sizeof(T) == 2 ? 16 : 8;
-constexpr int kBackwardWarps = 8;
+template <typename T>
+constexpr int kBackwardWarps = sizeof(T) == 2 ? 12 : 8;
 
 struct SeqIn {
     const void* p;
@@ -330,7 +331,7 @@ recurrence_kernel(SeqIn gate, SeqIn value, int steps, int D, const float* h0, co
 // inside a chunk are made again from the carry at its first step: reading the
 // stored h would bring its rounding into dgate, and more bytes.
 template <typename T, bool WIDE, bool MAPS>
-__global__ void __launch_bounds__(kWarps * 32, kBackwardWarps / kWarps)
+__global__ void __launch_bounds__(kWarps * 32, kBackwardWarps<T> / kWarps)
 recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int steps, int D, const float* carry, const float* dh_last,
                            const int32_t* lengths, T* dgate, T* dvalue, int64_t grad_seq, int64_t grad_step, float* dh0, Segments x) {
     layer_begin();
@@ -550,7 +551,7 @@ cpdp_status cpdp_gated_recurrence_backward(const void* dh, int64_t dh_seq, int64
     CPDP_TRY(check_array("dh0", dh0, false, 4));
     CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_gated_recurrence_workspace(B, T, D)));
     if (B == 0) return CPDP_OK;
-    Segments x = segments_of(B, T, D, kBackwardWarps);
+    Segments x = segments_of(B, T, D, dtype == CPDP_F32 ? kBackwardWarps<float> : kBackwardWarps<__nv_bfloat16>);
     x.maps = static_cast<Map*>(workspace);
     const SeqIn o{dh, dh_seq, dh_step}, g{gate, gate_seq, gate_step}, v{value, value_seq, value_step};
     const bool wide = D * e % 16 == 0 && in_pieces(dh, e, dh_seq, dh_step) && in_pieces(gate, e, gate_seq, gate_step) &&
