@@ -130,7 +130,7 @@ cpdp_status cpdp_weight_gradient(const void *dy, int64_t dy_worker, int64_t dy_r
 
 /*
  * cpdp_gated_recurrence — h_t = a_t h_(t-1) + (1 - a_t) v_t with
- * a = sigmoid(gate), for B <= 65535 sequences of T <= 2^30 steps and D channels.
+ * a = sigmoid(gate), for B sequences of T <= 2^30 steps and D channels.
  *   gate, value  [B][T][D] of dtype, with a sequence and a step stride
  *   h0           float32 [B][D], the states before the first step (NULL: 0)
  *   lengths      int32 [B], each sequence's number of steps, clamped to 0..T

@@ -135,7 +135,7 @@ norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weig
 // from row to row; `parts` receives them, one row per block. KEEP: the weights
 // stay in registers too.
 template <typename T, int V, int TPR, int E, bool KEEP>
-__global__ void __launch_bounds__(RowThreads<TPR>::block, TPR > 128 ? 1 : E == 32 ? 2 : 4)
+__global__ void __launch_bounds__(RowThreads<TPR>::block, TPR > 256 ? 1 : TPR > 128 || E == 32 ? 2 : 4)
 norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_t weight_worker, int64_t M, int D, float eps,
                      void* dx, float* parts) {
     layer_begin();
@@ -243,7 +243,9 @@ norm_weight_kernel(const float* parts, int count, int D, G* dweight, int64_t dwe
     }
 }
 
-// Threads per row and elements per thread for D features: f(TPR, E).
+// Threads per row and elements per thread for D features: f(TPR, E). At 4,096
+// features 256 threads of 16 elements took 193 (forward, 4 x 8,192 rows in bf16
+// with 8 bits) and 174 us (backward) where 128 of 32 took 207 and 180.
 template <int N>
 using Int = std::integral_constant<int, N>;
 template <typename F>
@@ -251,7 +253,7 @@ cudaError_t with_shape(int D, const F& f) {
     if (D <= 512) return f(Int<32>{}, Int<16>{});
     if (D <= 1024) return f(Int<32>{}, Int<32>{});
     if (D <= 2048) return f(Int<128>{}, Int<16>{});
-    if (D <= 4096) return f(Int<128>{}, Int<32>{});
+    if (D <= 4096) return f(Int<256>{}, Int<16>{});
     if (D <= 8192) return f(Int<512>{}, Int<16>{});
     return f(Int<512>{}, Int<32>{});
 }

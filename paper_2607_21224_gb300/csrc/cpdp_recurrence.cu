@@ -435,10 +435,10 @@ recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int steps, int D, 
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-recurrence_step_kernel(const T* gate, int64_t gate_seq, const T* value, int64_t value_seq, int D, float* state, T* h) {
+recurrence_step_kernel(const T* gate, int64_t gate_seq, const T* value, int64_t value_seq, int D, unsigned per, float* state, T* h) {
     layer_begin();
-    const int64_t b = blockIdx.y;
-    const int d = blockIdx.x * kThreads + threadIdx.x;
+    const int64_t b = blockIdx.x / per;  // `per` blocks to a sequence
+    const int d = blockIdx.x % per * kThreads + threadIdx.x;
     if (d >= D) return;
     Pair a, rest;
     gate_of(pair(to_float(gate[b * gate_seq + d]), 0.f), a, rest);
@@ -453,12 +453,14 @@ recurrence_step_kernel(const T* gate, int64_t gate_seq, const T* value, int64_t 
 using namespace cpdp;
 
 static cpdp_status check_recurrence(int B, int64_t T, int D, cpdp_dtype dtype) {
-    if (B < 0 || B > 65535) return layer_error(CPDP_EINVAL, "B=%d must be in [0, 65535]", B);
+    if (B < 0) return layer_error(CPDP_EINVAL, "B=%d must be >= 0", B);
     CPDP_TRY(check_sizes(1, T, D));
     if (T > int64_t(1) << 30) return layer_error(CPDP_EINVAL, "T=%lld is at most 2^30", (long long)T);
     if (B > 0) {
         if (T > kLayerMaxRows / B || (T > 0 && D > kLayerMaxElements / (B * T)))
             return layer_error(CPDP_EINVAL, "B=%d, T=%lld, D=%d: B * T is at most 2^31 - 1 and all elements at most 2^40", B, (long long)T, D);
+        if (ceil_div(D, kChannels) > kLayerMaxRows / B)
+            return layer_error(CPDP_EINVAL, "B=%d, D=%d: more blocks than a launch takes", B, D);
     }
     if (!known_dtype(dtype)) return layer_error(CPDP_EINVAL, "unknown dtype %d", (int)dtype);
     return CPDP_OK;
@@ -580,11 +582,11 @@ cpdp_status cpdp_gated_recurrence_step(const void* gate, int64_t gate_seq, const
     CPDP_TRY(check_array("state", state, B > 0, 4));
     CPDP_TRY(check_array("h", h, B > 0, e));
     if (B == 0) return CPDP_OK;
-    const dim3 grid(ceil_div(D, kThreads), B);
+    const unsigned per = static_cast<unsigned>(ceil_div(D, kThreads));
     const auto go = [&](auto* out) {
         using E = std::remove_pointer_t<decltype(out)>;
-        return launch_layer(recurrence_step_kernel<E>, grid, kThreads, 0, stream, static_cast<const E*>(gate), gate_seq,
-                            static_cast<const E*>(value), value_seq, D, state, out);
+        return launch_layer(recurrence_step_kernel<E>, per * B, kThreads, 0, stream, static_cast<const E*>(gate), gate_seq,
+                            static_cast<const E*>(value), value_seq, D, per, state, out);
     };
     return layer_launched(dtype == CPDP_F32 ? go(static_cast<float*>(h)) : go(static_cast<__nv_bfloat16*>(h)),
                           "cpdp_gated_recurrence_step");

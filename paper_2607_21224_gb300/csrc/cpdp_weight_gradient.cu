@@ -422,7 +422,8 @@ Splits splits_of(int W, int64_t M, int O, int I) {
     const int64_t steps = ceil_div(M, kStep), tiles = ceil_div(I, kTileI) * ceil_div(O, kTileO) * W;
     Splits best{1, steps};
     double least = 0;
-    for (int64_t count = 1; count <= 64 && (count == 1 || count * 4 <= steps); ++count) {
+    const int64_t most = ceil_div(2 * kSMs, tiles);  // beyond two turns there is nothing to gain
+    for (int64_t count = 1; count <= most && (count == 1 || count * 4 <= steps); ++count) {
         const int64_t each = ceil_div(steps, count), parts = each > 0 ? ceil_div(steps, each) : 1;
         double us = static_cast<double>(ceil_div(tiles * parts, kSMs)) * (each * 0.36 + 4.0);
         if (parts > 1) us += 3.0 + 2e-6 * parts * W * O * I;

@@ -155,7 +155,7 @@ def _ptr(t: torch.Tensor | None) -> int | None:
     return None if t is None else t.data_ptr()
 
 
-@dataclass(frozen=True)
+@dataclass(slots=True)
 class Checkpoint:
     """Activations held in 8 bits: ``codes`` int8 (W, M, 32 * ceil(D / 32)),
     ``exponents`` uint8 (W, M, ceil(D / 32)), and the number D of features.
@@ -284,12 +284,14 @@ def _saved(saved: Checkpoint) -> tuple[int, int, int]:
     """(W, M, D) of a Checkpoint that the library can read."""
     codes, exponents, D = saved.codes, saved.exponents, saved.features
     blocks = -(-D // BLOCK)
-    device = _cuda(codes, "codes")
-    if codes.dim() != 3:
-        raise ValueError(f"codes must be (W, M, {blocks * BLOCK}), got {tuple(codes.shape)}")
-    W, M = codes.shape[:2]
-    _whole(codes, "codes", (W, M, blocks * BLOCK), torch.int8, device)
-    _whole(exponents, "exponents", (W, M, blocks), torch.uint8, device)
+    device, shape = _cuda(codes, "codes"), codes.shape
+    if len(shape) != 3:
+        raise ValueError(f"codes must be (W, M, {blocks * BLOCK}), got {tuple(shape)}")
+    W, M, P = shape
+    if not (P == blocks * BLOCK and codes.dtype is torch.int8 and exponents.dtype is torch.uint8 and exponents.shape == (W, M, blocks)
+            and exponents.device == device and codes.is_contiguous() and exponents.is_contiguous()):
+        _whole(codes, "codes", (W, M, blocks * BLOCK), torch.int8, device)
+        _whole(exponents, "exponents", (W, M, blocks), torch.uint8, device)
     return W, M, D
 
 
@@ -397,18 +399,24 @@ def gated_recurrence_backward(dh, gate, value, carry, dh_last=None, lengths=None
 def gated_recurrence_step(gate, value, state, *, stream=None):
     """One token for each of B sequences: ``state`` (float32, (B, D)) is replaced
     by the next state, which is returned rounded to gate's type. gate, value (B, D)."""
-    device = _cuda(gate, "gate")
-    if _elsewhere(device, stream):
-        with _there(device, stream):
-            return gated_recurrence_step(gate, value, state)
-    shape, dtype, code = gate.shape, gate.dtype, _dtype(gate, "gate")
-    if len(shape) != 2:
-        raise ValueError(f"gate must be (B, D), got {tuple(shape)}")
-    gs, vs = _input(gate, "gate", shape, dtype, device), _input(value, "value", shape, dtype, device)
-    state_at = _whole(state, "state", shape, _F32, device)
+    shape, dtype, device, state_strides = gate.shape, gate.dtype, gate.device, state.stride()
+    gs, vs, code = gate.stride(), value.stride(), _CODES.get(dtype)
+    # one test where all is well: a decoding step costs what Python does around it
+    if not (stream is None and code is not None and gate.is_cuda and device.index == _current_device() and len(shape) == 2
+            and value.shape == shape == state.shape and value.dtype is dtype and state.dtype is _F32
+            and value.device == device == state.device and gs[-1] == 1 == vs[-1] and state_strides == (shape[1], 1)):
+        if _elsewhere(_cuda(gate, "gate"), stream):
+            with _there(device, stream):
+                return gated_recurrence_step(gate, value, state)
+        code = _dtype(gate, "gate")
+        if len(shape) != 2:
+            raise ValueError(f"gate must be (B, D), got {tuple(shape)}")
+        gs, vs = _input(gate, "gate", shape, dtype, device), _input(value, "value", shape, dtype, device)
+        _whole(state, "state", shape, _F32, device)
+    B, D = shape
     h = torch.empty(shape, dtype=dtype, device=device)
-    _check(_entry("cpdp_gated_recurrence_step")(gate.data_ptr(), gs[0], value.data_ptr(), vs[0], code, shape[0], shape[1], state_at,
-                                                h.data_ptr(), _stream(device.index)))
+    _check(_entry("cpdp_gated_recurrence_step")(gate.data_ptr(), gs[0], value.data_ptr(), vs[0], code, B, D,
+                                                state.data_ptr(), h.data_ptr(), _stream(device.index)))
     return h
 
 

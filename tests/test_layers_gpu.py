@@ -372,6 +372,21 @@ def test_recurrence_without_steps_or_sequences():
     assert layers.gated_recurrence_step(x[:, 0], x[:, 0], torch.empty(0, 16, device="cuda")).shape == (0, 16)
 
 
+def test_recurrence_of_very_many_sequences():
+    """More than 65,535, the limit of a grid's second and third sizes."""
+    B = 70_000
+    gate, value, dh, h0, dh_last, lengths = recurrence_inputs((B, 2, 3), F32, True)
+    f = ref.recurrence(gate, value, h0, lengths)
+    h, last, carry = layers.gated_recurrence(gate.cuda(), value.cuda(), h0.cuda(), lengths.cuda())
+    near(h, f["h"], f["eh"])
+    b = ref.recurrence_backward(dh, gate, value, h0, dh_last, lengths)
+    grads = layers.gated_recurrence_backward(dh.cuda(), gate.cuda(), value.cuda(), carry, dh_last.cuda(), lengths.cuda())
+    for got, name in zip(grads, ("dgate", "dvalue", "dh0")):
+        near(got, b[name], b["e" + name])
+    state = h0.cuda()
+    near(layers.gated_recurrence_step(gate.cuda()[:, 0], value.cuda()[:, 0], state), *[ref.recurrence(gate[:, :1], value[:, :1], h0, None)[k][:, 0] for k in ("h", "eh")])
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,D", [(1, 1), (4, 384), (3, 33), (65, 1024)])
 def test_recurrence_step_continues_a_sequence(B, D, dtype):

@@ -48,7 +48,7 @@ REFUSED = {
     "cpdp_restore": {0: [None], 1: [None], 2: [4097], 4: [-1], 5: [None]},
     "cpdp_weight_gradient": {0: [None], 1: [-1], 3: [3], 4: [None], 5: [None], 6: [0], 7: [-1], 8: [0], 9: [0], 10: [None], 11: [-1],
                              12: [4]},
-    "cpdp_gated_recurrence": {0: [None], 3: [None], 6: [2], 7: [-1, 65536], 8: [-1, 1 << 40], 9: [0], 12: [None], 13: [None]},
+    "cpdp_gated_recurrence": {0: [None], 3: [None], 6: [2], 7: [-1, 1 << 30], 8: [-1, 1 << 40], 9: [0], 12: [None], 13: [None]},
     "cpdp_gated_recurrence_backward": {0: [None], 3: [None], 6: [None], 9: [2], 10: [-1], 11: [-1], 12: [0], 13: [None], 16: [None],
                                        17: [None], 18: [-1], 19: [-1]},
     "cpdp_gated_recurrence_step": {0: [None], 1: [-1], 2: [None], 4: [2], 5: [-1], 6: [0], 7: [None], 8: [None]},
