@@ -192,13 +192,20 @@ def add_rmsnorm(x, weight, residual=None, *, eps: float = 1e-6, checkpoint: bool
         y, s, saved = add_rmsnorm(x[None], weight[None], None if residual is None else residual[None], eps=eps,
                                   checkpoint=checkpoint, stream=stream)
         return y[0], x if residual is None else s[0], saved
-    device = _cuda(x, "x")
-    if _elsewhere(device, stream):
-        with _there(device, stream):
-            return add_rmsnorm(x, weight, residual, eps=eps, checkpoint=checkpoint)
-    W, M, D = shape = _three(x, "x")
-    dtype, code = x.dtype, _dtype(x, "x")
-    xs, ws, rs = _input(x, "x", shape, dtype, device), _input(weight, "weight", (W, D), _F32, device), (0, 0)
+    shape, dtype, device = x.shape, x.dtype, x.device
+    xs, ws, code = x.stride(), weight.stride(), _CODES.get(dtype)
+    # one test where all is well: a decoding step costs what Python does around it
+    if not (stream is None and code is not None and x.is_cuda and device.index == _current_device() and len(shape) == 3
+            and weight.shape == (shape[0], shape[2]) and weight.dtype is _F32 and weight.device == device
+            and xs[-1] == 1 == ws[-1]):
+        if _elsewhere(_cuda(x, "x"), stream):
+            with _there(device, stream):
+                return add_rmsnorm(x, weight, residual, eps=eps, checkpoint=checkpoint)
+        code = _dtype(x, "x")
+        _input(x, "x", _three(x, "x"), dtype, device)
+        _input(weight, "weight", (shape[0], shape[2]), _F32, device)
+    W, M, D = shape
+    rs = (0, 0)
     s, s_at, r_at = x, None, None
     if residual is not None:
         rs, r_at = _input(residual, "residual", shape, dtype, device), residual.data_ptr()
