@@ -15,14 +15,15 @@ struct NormIn {
 // A row is spread over TPR threads, E elements each, in pieces of V
 // neighbours: piece j of thread t starts at element (j * TPR + t) * V. V is 16
 // bytes' worth where every row of every array starts at a multiple of that,
-// else 1. Rows of up to 1,024 elements take a warp, longer ones a block.
+// else 1. Rows of up to 128 elements in such pieces take 8 lanes, of up to 1,024
+// a warp, longer ones a block.
 
 // The sum over the row's threads, of N values at once. Blocks use two sets of
 // partial sums in turn, so one barrier per row is enough.
 template <int TPR, int N>
 __device__ __forceinline__ void row_sum(float (&v)[N], int turn) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(~0u, v[k], o);
     if constexpr (TPR > 32) {
@@ -62,7 +63,10 @@ norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weig
         wt[k] = d < D ? __ldg(weight + w * weight_worker + d) : 0.f;
     }
     int turn = 0;
-    for (int64_t m = (int64_t)blockIdx.x * rows + threadIdx.x / TPR; m < M; m += (int64_t)gridDim.x * rows, turn ^= 1) {
+    // a warp's rows leave the loop together
+    const int beside = TPR < 32 ? threadIdx.x % 32 / TPR : 0;
+    for (int64_t m = (int64_t)blockIdx.x * rows + threadIdx.x / TPR; m - beside < M; m += (int64_t)gridDim.x * rows, turn ^= 1) {
+        const bool there = TPR >= 32 || m < M;
         const T* xr = static_cast<const T*>(x.p) + w * x.worker + m * x.row;
         const T* rr = static_cast<const T*>(residual.p) + w * residual.worker + m * residual.row;
         const int64_t row = w * M + m;
@@ -73,7 +77,7 @@ norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weig
             for (int j = 0; j < J; ++j) {
                 const int d = (j * TPR + t) * V;
                 a[j] = b[j] = Piece<T, V>{};
-                if (d < D) {
+                if (there && d < D) {
                     a[j].load(xr + d);
                     if (residual.p != nullptr) b[j].load(rr + d);
                 }
@@ -92,7 +96,7 @@ norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weig
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const int d = (j * TPR + t) * V;
-                if (d < D) store_piece<V>(static_cast<T*>(s) + row * D + d, v + j * V);
+                if (there && d < D) store_piece<V>(static_cast<T*>(s) + row * D + d, v + j * V);
             }
         row_sum<TPR>(sum, turn);
         const float k = rsqrtf(sum[0] / D + eps);
@@ -121,12 +125,12 @@ norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weig
                     q[e] = d < D ? code_of(o[e], inverse) : 0;
                     o[e] = q[e] * unit;
                 }
-                if (d < blocks * kBlock8) {
+                if (there && d < blocks * kBlock8) {
                     store_codes<V>(codes + row * blocks * kBlock8 + d, q);
                     if (d % kBlock8 == 0) exponents[row * blocks + d / kBlock8] = static_cast<uint8_t>(byte);
                 }
             }
-            if (d < D) store_piece<V>(static_cast<Out*>(y) + row * D + d, o);
+            if (there && d < D) store_piece<V>(static_cast<Out*>(y) + row * D + d, o);
         }
     }
 }
@@ -172,7 +176,8 @@ norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_
     constexpr bool ahead = V > 1 && sizeof(T) == 2 && KEEP;
     const int64_t first = (int64_t)blockIdx.x * rows + threadIdx.x / TPR, step = (int64_t)gridDim.x * rows;
     if (ahead) load(first);
-    for (int64_t m = first; m < M; m += step, turn ^= 1) {
+    const int beside = TPR < 32 ? threadIdx.x % 32 / TPR : 0;  // a warp's rows leave the loop together
+    for (int64_t m = first; m - beside < M; m += step, turn ^= 1) {
         if (!ahead) load(m);
         Piece<T, V> g0[J], r0[J], through0[J];
 #pragma unroll
@@ -199,7 +204,7 @@ norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_
                 o[e] = fmaf(gk, KEEP ? wt[KEEP ? k : 0] : weight_at(k), through0[j].get(e)) - v * k3;
                 sums[k] = fmaf(gk, v, sums[k]);
             }
-            if (d < D) store_piece<V>(static_cast<T*>(dx) + (w * M + m) * D + d, o);
+            if (d < D && (TPR >= 32 || m < M)) store_piece<V>(static_cast<T*>(dx) + (w * M + m) * D + d, o);
         }
     }
     float* part = parts + (w * gridDim.x + blockIdx.x) * D;
@@ -249,7 +254,8 @@ norm_weight_kernel(const float* parts, int count, int D, G* dweight, int64_t dwe
 template <int N>
 using Int = std::integral_constant<int, N>;
 template <typename F>
-cudaError_t with_shape(int D, const F& f) {
+cudaError_t with_shape(int D, bool wide, const F& f) {
+    if (D <= 128 && wide) return f(Int<8>{}, Int<16>{});
     if (D <= 512) return f(Int<32>{}, Int<16>{});
     if (D <= 1024) return f(Int<32>{}, Int<32>{});
     if (D <= 2048) return f(Int<128>{}, Int<16>{});
@@ -264,11 +270,12 @@ unsigned blocks_for(int W, int64_t M, int rows, int resident) {
     const int64_t all = ceil_div(M, rows), most = ceil_div(int64_t(kSMs) * resident, W);
     return static_cast<unsigned>(all < most ? all : most);
 }
-int rows_per_block(int D) { return D <= 1024 ? 4 : 1; }
-// The backward pass's blocks per worker: what its registers let run at once. The workspace's size goes by it.
-unsigned backward_blocks(int W, int64_t M, int D) {
+int rows_per_block(int D, bool wide) { return D <= 128 && wide ? 16 : D <= 1024 ? 4 : 1; }
+// The backward pass's blocks per worker: what its registers let run at once.
+// The workspace has a row for each, of rows that are not wide: there are no fewer.
+unsigned backward_blocks(int W, int64_t M, int D, bool wide) {
     const int resident = D <= 512 ? 4 : D <= 1024 ? 2 : D <= 2048 ? 4 : D <= 4096 ? 2 : 1;
-    return blocks_for(W, M, rows_per_block(D), resident);
+    return blocks_for(W, M, rows_per_block(D, wide), resident);
 }
 
 }  // namespace
@@ -310,7 +317,7 @@ cpdp_status cpdp_add_rmsnorm(const void* x, int64_t x_worker, int64_t x_row, con
     if (!some) return CPDP_OK;
     const NormIn xi{x, x_worker, x_row}, ri{residual, residual_worker, residual_row};
     const bool wide = in_pieces(xi, e, D) && in_pieces(ri, e, D) && aligned_to(y, 16) && aligned_to(s, 16);
-    const cudaError_t launched = with_shape(D, [&](auto tpr, auto elements) {
+    const cudaError_t launched = with_shape(D, wide, [&](auto tpr, auto elements) {
         constexpr int TPR = decltype(tpr)::value, E = decltype(elements)::value;
         const auto go = [&](auto kernel) {
             const dim3 grid(blocks_for(W, M, RowThreads<TPR>::rows, 2048 / RowThreads<TPR>::block), W);
@@ -318,8 +325,10 @@ cpdp_status cpdp_add_rmsnorm(const void* x, int64_t x_worker, int64_t x_row, con
         };
         const auto held = [&](auto checkpoint) {
             constexpr bool C = decltype(checkpoint)::value;
-            if (dtype == CPDP_F32) return wide ? go(norm_forward_kernel<float, 4, TPR, E, C>) : go(norm_forward_kernel<float, 1, TPR, E, C>);
-            return wide ? go(norm_forward_kernel<__nv_bfloat16, 8, TPR, E, C>) : go(norm_forward_kernel<__nv_bfloat16, 1, TPR, E, C>);
+            if constexpr (TPR >= 32)
+                if (!wide)
+                    return dtype == CPDP_F32 ? go(norm_forward_kernel<float, 1, TPR, E, C>) : go(norm_forward_kernel<__nv_bfloat16, 1, TPR, E, C>);
+            return dtype == CPDP_F32 ? go(norm_forward_kernel<float, 4, TPR, E, C>) : go(norm_forward_kernel<__nv_bfloat16, 8, TPR, E, C>);
         };
         return codes != nullptr ? held(std::true_type{}) : held(std::false_type{});
     });
@@ -328,7 +337,7 @@ cpdp_status cpdp_add_rmsnorm(const void* x, int64_t x_worker, int64_t x_row, con
 
 size_t cpdp_add_rmsnorm_backward_workspace(int W, int64_t M, int D) {
     if (check_norm(W, M, D, CPDP_F32, 1.f) != CPDP_OK) return 0;
-    return static_cast<size_t>(W) * backward_blocks(W, M, D) * D * 4;
+    return static_cast<size_t>(W) * backward_blocks(W, M, D, false) * D * 4;
 }
 
 cpdp_status cpdp_add_rmsnorm_backward(const void* dy, int64_t dy_worker, int64_t dy_row, const void* s, int64_t s_worker,
@@ -349,18 +358,20 @@ cpdp_status cpdp_add_rmsnorm_backward(const void* dy, int64_t dy_worker, int64_t
     CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_add_rmsnorm_backward_workspace(W, M, D)));
     const NormIn gi{dy, dy_worker, dy_row}, si{s, s_worker, s_row}, di{ds, ds_worker, ds_row};
     float* parts = static_cast<float*>(workspace);
-    const unsigned blocks = backward_blocks(W, M, D);
     const bool wide = in_pieces(gi, e, D) && in_pieces(si, e, D) && in_pieces(di, e, D) && aligned_to(dx, 16);
+    const unsigned blocks = backward_blocks(W, M, D, wide);
     if (some)
-        CPDP_TRY(layer_launched(with_shape(D, [&](auto tpr, auto elements) {
+        CPDP_TRY(layer_launched(with_shape(D, wide, [&](auto tpr, auto elements) {
             constexpr int TPR = decltype(tpr)::value, E = decltype(elements)::value;
             constexpr bool K = TPR * E <= 8192;  // longer rows have too few registers for it
             const auto go = [&](auto kernel) {
                 return launch_layer(kernel, dim3(blocks, W), RowThreads<TPR>::block, 0, stream, gi, si, di, weight, weight_worker, M, D,
                                     eps, dx, parts);
             };
-            if (dtype == CPDP_F32) return wide ? go(norm_backward_kernel<float, 4, TPR, E, K>) : go(norm_backward_kernel<float, 1, TPR, E, K>);
-            return wide ? go(norm_backward_kernel<__nv_bfloat16, 8, TPR, E, K>) : go(norm_backward_kernel<__nv_bfloat16, 1, TPR, E, K>);
+            if constexpr (TPR >= 32)
+                if (!wide)
+                    return dtype == CPDP_F32 ? go(norm_backward_kernel<float, 1, TPR, E, K>) : go(norm_backward_kernel<__nv_bfloat16, 1, TPR, E, K>);
+            return dtype == CPDP_F32 ? go(norm_backward_kernel<float, 4, TPR, E, K>) : go(norm_backward_kernel<__nv_bfloat16, 8, TPR, E, K>);
         }), "cpdp_add_rmsnorm_backward"));
     const auto sum = [&](auto* out) {
         return launch_layer(norm_weight_kernel<std::remove_pointer_t<decltype(out)>>, dim3(ceil_div(D, kColumns), W), kColumns * kLines, 0,
