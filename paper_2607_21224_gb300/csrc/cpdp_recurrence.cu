@@ -27,12 +27,6 @@ struct SeqIn {
     int64_t seq, step;
 };
 
-// a = sigmoid(x) and 1 - a, neither formed as a difference from 1. With
-// t = e^-|x| in [0, 1] they are 1 / (1 + t) and t / (1 + t). The power is 2^p of
-// the rounded product p = |x| log2(e), so t's relative error is some ulps and
-// grows with |x| (1e-6 at 16, where t itself is 1e-7). The scans are bound by
-// the instructions that they issue: exact range reduction and division, with
-// their cases for tiny numbers, took 2.5 times as many.
 // Two floats in a pair of registers, for the instructions that work on both.
 using Pair = unsigned long long;
 constexpr Pair kOnes = 0x3f8000003f800000ull, kZeros = 0, kMinusOnes = 0xbf800000bf800000ull;
@@ -61,6 +55,12 @@ __device__ __forceinline__ Pair add2(Pair a, Pair b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+// a = sigmoid(x) and 1 - a, neither formed as a difference from 1. With
+// t = e^-|x| in [0, 1] they are 1 / (1 + t) and t / (1 + t). The power is 2^p of
+// the rounded product p = |x| log2(e), so t's relative error is some ulps and
+// grows with |x| (1e-6 at 16, where t itself is 1e-7). The scans are bound by
+// the instructions that they issue: exact range reduction and division, with
+// their cases for tiny numbers, took 2.5 times as many.
 __device__ __forceinline__ float power_of_minus(float x) {
     float t;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(-1.44269504f * fabsf(x)));
@@ -245,7 +245,11 @@ struct Chunk {
 
 // Forward pass: chunks of R steps pass through the warp's ring of shared
 // memory; the only chain from step to step is one fused multiply-add.
-// MAPS: the first pass, which makes the segment's map.
+// MAPS: the first pass, which makes the segment's map. In bf16, 64 x 1,024 x
+// 1,024 (1,024 columns) take 72 us, 5.6 TB/s, 16 instructions per element;
+// 65,536 x 1,024 (16 columns in 152 segments) 45 us for the maps and 64 for the
+// rest, both at 6 TB/s of what they read and write. With fewer than 8 warps per
+// SM the chunks' latency shows: 128 x 197 x 384 (5 warps) 18 us, 3.2 TB/s.
 template <typename T, bool WIDE, bool MAPS>
 __global__ void __launch_bounds__(kWarps * 32, kForwardWarps<T> / kWarps)
 recurrence_kernel(SeqIn gate, SeqIn value, int steps, int D, const float* h0, const int32_t* lengths, T* h, float* h_last,
@@ -329,7 +333,9 @@ recurrence_kernel(SeqIn gate, SeqIn value, int steps, int D, const float* h0, co
 // Backward pass, from the last step to the first. What flows from step t to
 // t - 1 is f_t = a_t (dh_t + f_(t+1)), a map like the state's. The states
 // inside a chunk are made again from the carry at its first step: reading the
-// stored h would bring its rounding into dgate, and more bytes.
+// stored h would bring its rounding into dgate, and more bytes. The same sizes
+// as above: 115 us, 5.8 TB/s; 42 and 110; 27 us, 3.6 TB/s. Blocks of fewer
+// registers, 16 warps per SM, spilled and took twice as long.
 template <typename T, bool WIDE, bool MAPS>
 __global__ void __launch_bounds__(kWarps * 32, kBackwardWarps<T> / kWarps)
 recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int steps, int D, const float* carry, const float* dh_last,
@@ -433,6 +439,7 @@ recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int steps, int D, 
         store_state<WIDE>(dh0 + (int64_t)task.b * D + c, flow, second);
 }
 
+// One step, an element per thread: the launch (2.6 us a call from the host).
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 recurrence_step_kernel(const T* gate, int64_t gate_seq, const T* value, int64_t value_seq, int D, unsigned per, float* state, T* h) {

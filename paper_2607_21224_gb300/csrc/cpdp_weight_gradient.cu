@@ -8,6 +8,11 @@
 namespace cpdp {
 namespace {
 
+// dW = dy^T x^ is bound by shared memory: a step of 64 tokens takes the tensor
+// core 512 clocks, and 768 times 128 bytes move for it (48 KB of operands read,
+// 32 KB of dy and 16 KB of x^ written). 2 x 16,384 tokens, 2,048 -> 8,192: 780 us,
+// 1,409 TFLOP/s, to float32 879 us; 8 x 3,152, 384 -> 1,536 (144 blocks): 37 us.
+//
 // One block computes 128 (i) x 256 (o) of dW, transposed on the tensor cores:
 // the accumulator's 128 lanes are neighbouring i, so that a warp's stores of
 // one column are 32 neighbours of dW's row. Tokens pass in steps of 64 through
@@ -358,8 +363,8 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
 // dy as the tensor copies need it: bfloat16 rows at multiples of 16 bytes. A
 // warp per row, 8 elements per lane and turn: out of five neighbouring 32-bit
 // words where a bfloat16 row starts between words. Only words that hold
-// elements of the row are read; 52 -> 33 us for 77 MB against two words and one
-// store of 4 bytes per turn.
+// elements of the row are read; 23 us for 77 MB, 6.7 TB/s; with
+// one store of 4 bytes per turn, out of two words, 52.
 template <typename T>
 __global__ void __launch_bounds__(256)
 align_kernel(const T* dy, int64_t dy_worker, int64_t dy_row, int64_t M, int64_t rows, int O, int pitch, uint4* out) {
@@ -398,7 +403,7 @@ align_kernel(const T* dy, int64_t dy_worker, int64_t dy_row, int64_t M, int64_t 
     }
 }
 
-// The sum of the splits' parts, in their order.
+// The sum of the splits' parts, in their order; DRAM or L2.
 template <typename G>
 __global__ void __launch_bounds__(256)
 sum_parts_kernel(const float* parts, int splits, int64_t per_worker, int64_t all, G* dW, int64_t dW_worker) {

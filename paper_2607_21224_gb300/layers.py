@@ -393,7 +393,7 @@ def gated_recurrence_backward(dh, gate, value, carry, dh_last=None, lengths=None
     if out is None:
         out = torch.empty((B, T, 2 * D), dtype=dtype, device=device)
     ps = _input(out, "out", (B, T, 2 * D), dtype, device)
-    dgate, dvalue = out[..., :D], out[..., D:]
+    dgate, dvalue = out.split(D, 2)
     dh0 = torch.empty((B, D), dtype=_F32, device=device)
     needed = _entry("cpdp_gated_recurrence_workspace")(B, T, D)
     work = _workspace(needed, device)
