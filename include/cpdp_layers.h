@@ -40,7 +40,7 @@
  * the stream is done. Errors are status codes; the message is at
  * cpdp_last_error(NULL). A refused call launches nothing.
  *
- * Limits: 1 <= W <= 4096, 0 <= M, 1 <= D, W * M * D <= 2^40 and
+ * Limits: 1 <= W <= 4096, 0 <= M, 1 <= D <= 2^30, W * M * D <= 2^40 and
  * W * M <= 2^31 - 1; further ones at each call. A call with no rows (M, B or T
  * of 0) writes the gradients or states that it owes (zeros, or the initial
  * state) and nothing else; pointers to arrays of no elements may be NULL.

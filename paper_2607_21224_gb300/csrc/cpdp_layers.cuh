@@ -17,6 +17,7 @@ cpdp_status layer_launched(cudaError_t launched, const char* what);
 
 constexpr int64_t kLayerMaxElements = int64_t(1) << 40;
 constexpr int64_t kLayerMaxRows = (int64_t(1) << 31) - 1;
+constexpr int64_t kLayerMaxFeatures = int64_t(1) << 30;
 constexpr int kSMs = 152;
 constexpr int kBlock8 = 32;  // features that share an exponent
 
@@ -29,7 +30,8 @@ inline bool aligned_to(const void* p, int64_t n) { return reinterpret_cast<uintp
 // W, M and D of an array [W][M][D].
 inline cpdp_status check_sizes(int W, int64_t M, int64_t D) {
     if (W < 1 || W > 4096) return layer_error(CPDP_EINVAL, "W=%d must be in [1, 4096]", W);
-    if (M < 0 || D < 1) return layer_error(CPDP_EINVAL, "rows (%lld) must be >= 0 and features (%lld) >= 1", (long long)M, (long long)D);
+    if (M < 0 || D < 1 || D > kLayerMaxFeatures)
+        return layer_error(CPDP_EINVAL, "rows (%lld) must be >= 0 and features (%lld) in [1, 2^30]", (long long)M, (long long)D);
     if (M > kLayerMaxRows / W || (M > 0 && D > kLayerMaxElements / (W * M)))
         return layer_error(CPDP_EINVAL, "W=%d, rows=%lld, features=%lld: W * rows is at most 2^31 - 1 and all elements at most 2^40",
                            W, (long long)M, (long long)D);

@@ -36,6 +36,7 @@ from . import cpdp as _c
 from .state import _raw_stream
 
 BLOCK = 32  # features that share an exponent
+MAX_SIZE = 1 << 30  # of every axis
 CARRY_STEPS = 16  # CPDP_CARRY_STEPS
 NORM_MAX_FEATURES = 16384  # CPDP_NORM_MAX_FEATURES
 
@@ -175,10 +176,17 @@ def _new_checkpoint(W: int, M: int, D: int, device: torch.device) -> Checkpoint:
                       torch.empty((W, M, blocks), dtype=torch.uint8, device=device), D)
 
 
+def _sized(t: torch.Tensor, name: str) -> tuple:
+    """The shape of an array whose sizes the library's arguments can hold."""
+    if max(t.shape) > MAX_SIZE:
+        raise ValueError(f"{name} has an axis of more than {MAX_SIZE}: {tuple(t.shape)}")
+    return t.shape
+
+
 def _three(t: torch.Tensor, name: str) -> tuple:
     if t.dim() != 3:
         raise ValueError(f"{name} must be (W, M, D), or (M, D) of one model; got {tuple(t.shape)}")
-    return t.shape
+    return _sized(t, name)
 
 
 def add_rmsnorm(x, weight, residual=None, *, eps: float = 1e-6, checkpoint: bool = False, stream=None):
@@ -195,7 +203,7 @@ def add_rmsnorm(x, weight, residual=None, *, eps: float = 1e-6, checkpoint: bool
     shape, dtype, device = x.shape, x.dtype, x.device
     xs, ws, code = x.stride(), weight.stride(), _CODES.get(dtype)
     # one test where all is well: a decoding step costs what Python does around it
-    if not (stream is None and code is not None and x.is_cuda and device.index == _current_device() and len(shape) == 3
+    if not (stream is None and code is not None and x.is_cuda and device.index == _current_device() and len(shape) == 3 and max(shape) <= MAX_SIZE
             and weight.shape == (shape[0], shape[2]) and weight.dtype is _F32 and weight.device == device
             and xs[-1] == 1 == ws[-1]):
         if _elsewhere(_cuda(x, "x"), stream):
@@ -295,6 +303,7 @@ def _saved(saved: Checkpoint) -> tuple[int, int, int]:
     if len(shape) != 3:
         raise ValueError(f"codes must be (W, M, {blocks * BLOCK}), got {tuple(shape)}")
     W, M, P = shape
+    _sized(codes, "codes")
     if not (P == blocks * BLOCK and codes.dtype is torch.int8 and exponents.dtype is torch.uint8 and exponents.shape == (W, M, blocks)
             and exponents.device == device and codes.is_contiguous() and exponents.is_contiguous()):
         _whole(codes, "codes", (W, M, blocks * BLOCK), torch.int8, device)
@@ -344,7 +353,7 @@ def _sequences(gate) -> tuple:
     if gate.dim() != 3:
         raise ValueError(f"gate must be (B, T, D), got {tuple(gate.shape)}")
     _dtype(gate, "gate")
-    return gate.shape
+    return _sized(gate, "gate")
 
 
 def gated_recurrence(gate, value, h0=None, lengths=None, *, carry: bool = True, stream=None):
@@ -393,7 +402,7 @@ def gated_recurrence_backward(dh, gate, value, carry, dh_last=None, lengths=None
     if out is None:
         out = torch.empty((B, T, 2 * D), dtype=dtype, device=device)
     ps = _input(out, "out", (B, T, 2 * D), dtype, device)
-    dgate, dvalue = out.split(D, 2)
+    dgate, dvalue = out.chunk(2, 2)
     dh0 = torch.empty((B, D), dtype=_F32, device=device)
     needed = _entry("cpdp_gated_recurrence_workspace")(B, T, D)
     work = _workspace(needed, device)
@@ -410,7 +419,7 @@ def gated_recurrence_step(gate, value, state, *, stream=None):
     gs, vs, code = gate.stride(), value.stride(), _CODES.get(dtype)
     # one test where all is well: a decoding step costs what Python does around it
     if not (stream is None and code is not None and gate.is_cuda and device.index == _current_device() and len(shape) == 2
-            and value.shape == shape == state.shape and value.dtype is dtype and state.dtype is _F32
+            and value.shape == shape == state.shape and max(shape) <= MAX_SIZE and value.dtype is dtype and state.dtype is _F32
             and value.device == device == state.device and gs[-1] == 1 == vs[-1] and state_strides == (shape[1], 1)):
         if _elsewhere(_cuda(gate, "gate"), stream):
             with _there(device, stream):
@@ -418,6 +427,7 @@ def gated_recurrence_step(gate, value, state, *, stream=None):
         code = _dtype(gate, "gate")
         if len(shape) != 2:
             raise ValueError(f"gate must be (B, D), got {tuple(shape)}")
+        _sized(gate, "gate")
         gs, vs = _input(gate, "gate", shape, dtype, device), _input(value, "value", shape, dtype, device)
         _whole(state, "state", shape, _F32, device)
     B, D = shape

@@ -203,6 +203,21 @@ def test_weight_gradient(shape, grad, layout):
     assert torch.equal(layers.weight_gradient(dy.cuda(), saved, dtype=grad), got)
 
 
+def test_weight_gradient_of_repeated_and_shifted_dy():
+    """dy whose rows repeat, overlap or start between words, against the same values laid out anew."""
+    gen = rng(21)
+    saved, _ = layers.checkpoint(normal(gen, 2, 70, 96).cuda())
+    row = normal(gen, 1, 1, 40, dtype=BF16).cuda()
+    long = normal(gen, 2 * 5000, dtype=BF16).cuda()
+    def laid(t, worker, step, first=0):
+        return t.as_strided((2, 70, 40), (worker, step, 1), first)
+
+    for dy in (row.expand(2, 70, 40), laid(long, 3000, 8), laid(long, 0, 48), laid(long, 3000, 41, 1), laid(long, 4096, 48, 3),
+               laid(long.float(), 3000, 41, 1)):
+        want = layers.weight_gradient(dy.contiguous().clone(), saved)
+        assert torch.equal(layers.weight_gradient(dy, saved), want)
+
+
 def test_weight_gradient_of_many_tokens_keeps_its_precision():
     """128 tiles of 16,384 tokens, so no split of the tokens: one chain of 1,024 products would cut dW by 6e-6.
     Chunks of 128 products, each cutting at most 2^-25 of a sum that is two thirds of the last on average: 2.5e-6."""

@@ -44,7 +44,7 @@ REFUSED = {
                          11: [0, -5, 16385], 12: [0.0, -1.0, float("nan"), float("inf")], 13: [None], 14: [P], 15: [P], 16: [P]},
     "cpdp_add_rmsnorm_backward": {0: [None], 3: [None], 9: [None], 11: [7], 12: [0], 13: [-1], 14: [0, 16385], 15: [0.0], 16: [None],
                                   17: [None], 18: [-1], 19: [9], 20: [None], 21: [0, 8]},
-    "cpdp_checkpoint": {0: [None], 3: [5], 4: [0], 5: [-1], 6: [0], 7: [None], 8: [None]},
+    "cpdp_checkpoint": {0: [None], 3: [5], 4: [0], 5: [-1], 6: [0, (1 << 30) + 1], 7: [None], 8: [None]},
     "cpdp_restore": {0: [None], 1: [None], 2: [4097], 4: [-1], 5: [None]},
     "cpdp_weight_gradient": {0: [None], 1: [-1], 3: [3], 4: [None], 5: [None], 6: [0], 7: [-1], 8: [0], 9: [0], 10: [None], 11: [-1],
                              12: [4]},
@@ -113,6 +113,14 @@ def test_reference_gradients_against_differences():
     want = (g(*(a + h * u for a, u in zip((gate, value, h0), us))) - g(*(a - h * u for a, u in zip((gate, value, h0), us)))) / (2 * h)
     got = sum((r[k] * u).sum() for k, u in zip(("dgate", "dvalue", "dh0"), us))
     assert abs(got - want) <= 1e-7 * sum(float((r[k] * u).abs().sum()) for k, u in zip(("dgate", "dvalue", "dh0"), us))
+
+
+def test_axes_beyond_the_arguments_are_refused():
+    """Sizes that would be cut to 32 bits on their way into the library."""
+    with pytest.raises(ValueError, match="axis"):
+        layers._three(torch.zeros(1).expand(1, 1, 2 ** 32 + 64), "x")
+    with pytest.raises(ValueError, match="axis"):
+        layers._sequences(torch.zeros(1).expand(2 ** 32 + 1, 1, 1))
 
 
 def test_held_values_are_within_half_a_unit():
