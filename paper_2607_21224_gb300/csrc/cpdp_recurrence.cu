@@ -504,7 +504,9 @@ static cudaError_t launch_walk(void (*kernel)(KArgs...), const Segments& x, size
     // 4 left 112 SMs with 4 warps and 40 with 8
     const int warps = x.count > 1 ? kWarps : 1;
     const size_t smem = warps * warp_smem;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    // what a launch may have without asking is enough for single warps
+    const cudaError_t e =
+        smem <= 32 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     return e != cudaSuccess ? e : launch_layer(kernel, static_cast<unsigned>(ceil_div(x.columns * x.count, warps)), warps * 32, smem, stream, args..., x);
 }
 

@@ -1,5 +1,6 @@
 // The weight gradient dW = dy^T x^ from activations held in 8 bits
 // (include/cpdp_layers.h).
+#include <atomic>
 #include <climits>
 #include <cuda.h>
 
@@ -148,8 +149,7 @@ struct WeightGradient {
     const uint8_t* exponents;
     int64_t M;
     int O, I, W, blocks;  // blocks of 32 features in a row of x^
-    int splits;           // of the tokens; more than one: parts [splits][W][O][I] of float32
-    int64_t split_steps;
+    int64_t split_steps;  // of a part of the tokens; more than one: parts [part][W][O][I] of float32
     int chunk;            // steps that are summed in tensor memory before they are written out
     void* out;
     int64_t out_worker, out_split;
@@ -508,7 +508,7 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     WeightGradient p{};
     p.codes = codes, p.exponents = exponents;
     p.M = M, p.O = O, p.I = I, p.W = W, p.blocks = static_cast<int>(ceil_div(I, kBlock8));
-    p.splits = sp.count, p.split_steps = sp.each;
+    p.split_steps = sp.each;
     p.chunk = parts || dW_dtype == CPDP_F32 ? kChunk : INT_MAX / 2;
     p.out = parts ? workspace : dW;
     p.out_worker = parts ? (int64_t)O * I : dW_worker;
@@ -541,13 +541,17 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
         if (r != CUDA_SUCCESS) return layer_error(CPDP_ECUDA, "cuTensorMapEncodeTiled: error %d", (int)r);
     }
     const dim3 grid(ceil_div(I, kTileI), ceil_div(O, kTileO), sp.count * W);
-    const auto go = [&](auto kernel, int threads) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-        return e != cudaSuccess ? e : launch_layer(kernel, grid, threads, kSmemBytes, stream, map, p);
-    };
     const auto typed = [&](auto g) {
         using G = decltype(g);
-        return go(weight_gradient_kernel<G>, kThreads<G>);
+        static std::atomic<uint64_t> allowed{0};  // the devices on which this kernel has been allowed its shared memory
+        int device = 0;
+        cudaError_t e = cudaGetDevice(&device);
+        const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+        if (e == cudaSuccess && (allowed.load() & bit) == 0) {
+            e = cudaFuncSetAttribute(weight_gradient_kernel<G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+            if (e == cudaSuccess) allowed |= bit;
+        }
+        return e != cudaSuccess ? e : launch_layer(weight_gradient_kernel<G>, grid, kThreads<G>, kSmemBytes, stream, map, p);
     };
     CPDP_TRY(layer_launched(parts || dW_dtype == CPDP_F32 ? typed(0.f) : typed(__nv_bfloat16{}), "cpdp_weight_gradient"));
     if (!parts) return CPDP_OK;
