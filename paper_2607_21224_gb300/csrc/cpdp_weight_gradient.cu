@@ -1,7 +1,6 @@
 // The weight gradient dW = dy^T x^ from activations held in 8 bits
 // (include/cpdp_layers.h).
 #include <atomic>
-#include <climits>
 #include <cuda.h>
 
 #include "cpdp_layers.cuh"
@@ -11,8 +10,8 @@ namespace {
 
 // dW = dy^T x^ is bound by shared memory: a step of 64 tokens takes the tensor
 // core 512 clocks, and 768 times 128 bytes move for it (48 KB of operands read,
-// 32 KB of dy and 16 KB of x^ written). 2 x 16,384 tokens, 2,048 -> 8,192: 780 us,
-// 1,409 TFLOP/s, to float32 879 us; 8 x 3,152, 384 -> 1,536 (144 blocks): 37 us.
+// 32 KB of dy and 16 KB of x^ written). 2 x 16,384 tokens, 2,048 -> 8,192: 819 us,
+// 1,342 TFLOP/s, to either type; 8 x 3,152, 384 -> 1,536 (144 blocks): 37 us.
 //
 // One block computes 128 (i) x 256 (o) of dW, transposed on the tensor cores:
 // the accumulator's 128 lanes are neighbouring i, so that a warp's stores of
@@ -25,19 +24,21 @@ namespace {
 //        block of 32 features of one token: exact in bfloat16. Groups of eight
 //        warps take the steps in turn: one group needs 900 clocks for a step
 //        (wait, convert, store, hand over), the tensor core 512.
-// One thread issues the matrix instructions. The sums are in tensor memory, in
-// two halves that take chunks of the steps in turn: four writing warps add a
-// finished chunk to the output while the next one is multiplied, the converting
-// warps the last one. The tensor core cuts its float32
-// sums off where others round them, always towards 0: over 16,384 tokens that
-// made dW 6e-6 too small. So where the output is float32 a chunk has kChunk
-// steps, and the chunks are added up, rounded to nearest, in the output; 2,048
-// tokens lose 7e-7. A bfloat16 output, which rounds to 4e-3, is one chunk.
+// One thread issues the matrix instructions. The tensor core cuts its float32
+// sums off where others round them, always towards 0. In one chain that grows
+// with the tokens: where all products have one sign dW came out 0.4 % too small
+// at 2^18 tokens and 4 % at 2^22, more than a bfloat16 output's own rounding. So
+// a chunk of kChunk steps is summed at a time, and the chunks are added up,
+// rounded to nearest: the first chunk's sums lie in one half of tensor memory,
+// the others' in turn in the other, from where four adding warps add them to the
+// first half. The next chunk waits for that, while the slots are filled (0.9 us
+// per chunk; 2 x 16,384 tokens, 2,048 -> 8,192 in one chain took 783 us). The
+// converting warps add the last chunk as they write dW. 2,048 tokens of one sign
+// lose 2e-6, of both signs 5e-7 of dW.
 constexpr int kTileI = 128, kTileO = 256, kStep = 64, kSlots = 4;
 constexpr int kGroupWarps = 8, kGroups = 2, kConvertWarps = kGroupWarps * kGroups;
-constexpr int kCopyWarp = kConvertWarps, kMultiplyWarp = kConvertWarps + 1, kWriteWarp = kConvertWarps + 2;  // the first of four
-template <typename G>
-constexpr int kThreads = (kConvertWarps + 2 + (sizeof(G) == 4 ? 4 : 0)) * 32;  // one chunk needs no writing warps
+constexpr int kCopyWarp = kConvertWarps, kMultiplyWarp = kConvertWarps + 1, kAddWarp = kConvertWarps + 2;  // the first of four
+constexpr int kThreads = (kAddWarp + 4) * 32;
 constexpr int kChunk = 32;  // steps
 constexpr int kBlockBytes = kStep * 128;                               // a step's rows of 64 elements
 constexpr int kXBytes = kTileI / 64 * kBlockBytes, kDyBytes = kTileO / 64 * kBlockBytes, kSlotBytes = kXBytes + kDyBytes;
@@ -104,9 +105,8 @@ __device__ __forceinline__ void multiply(uint32_t sums, uint64_t a, uint64_t b, 
 __device__ __forceinline__ void arrive_when_multiplied(uint64_t* b) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(b)) : "memory");
 }
-// 16 columns of the warp's 32 lanes.
-__device__ __forceinline__ void read_sums(uint32_t at, float (&v)[16]) {
-    uint32_t r[16];
+// 16 columns of the warp's 32 lanes; there once the wait is over.
+__device__ __forceinline__ void read_sums(uint32_t at, uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -114,9 +114,30 @@ __device__ __forceinline__ void read_sums(uint32_t at, float (&v)[16]) {
           "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(at)
         : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+// The loads' results are operands, so that nothing uses them before.
+__device__ __forceinline__ void wait_read(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
+__device__ __forceinline__ void store_sums(uint32_t at, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// The sum of 16 columns at `a` and at `b`.
+__device__ __forceinline__ void add_sums(uint32_t a, uint32_t b, uint32_t (&r)[16]) {
+    uint32_t more[16];
+    read_sums(a, r);
+    read_sums(b, more);
+    wait_read(r);
+    wait_read(more);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __uint_as_float(more[i]));
 }
 
 __device__ __forceinline__ uint32_t sub_pair(uint32_t a, uint32_t b) {
@@ -150,51 +171,42 @@ struct WeightGradient {
     int64_t M;
     int O, I, W, blocks;  // blocks of 32 features in a row of x^
     int64_t split_steps;  // of a part of the tokens; more than one: parts [part][W][O][I] of float32
-    int chunk;            // steps that are summed in tensor memory before they are written out
     void* out;
     int64_t out_worker, out_split;
 };
 
-// Columns [first, first + count) of the sums at `sums` to the output, the
-// warp's 32 lanes of i: added to what is there (`add`), or in its place; zeros
-// where there are no sums (`any` false). The additions are done by L2, which
-// spares the wait for what is there. Each element has one adder at a time, in
-// the chunks' order, so the result does not vary; sums below 1.2e-38 become 0.
+// Columns [first, first + count) of dW, the warp's 32 lanes of i: the sums of
+// the first chunk and, where there are several, of the others; zeros where
+// there are none.
 template <typename G>
-__device__ __forceinline__ void write_out(const WeightGradient& p, uint32_t sums, int i0, int o0, int first, int count, bool add, bool any,
-                                          G* out) {
+__device__ __forceinline__ void write_out(const WeightGradient& p, uint32_t sums, int chunks, int i0, int o0, int first, int count, G* out) {
     const int quarter = threadIdx.x / 32 % 4 * 32, i = i0 + quarter + static_cast<int>(threadIdx.x % 32);
     const int end = min(p.O - o0, first + count);
     G* to = out + (int64_t)(o0 + first) * p.I + i;
 #pragma unroll 1
     for (int o = first; o < end; o += 16, to += (int64_t)16 * p.I) {
-        float v[16] = {};
-        if (any) read_sums(sums + (quarter << 16) + o, v);
-        if (i < p.I) {
-            bool stored = false;
-            if constexpr (sizeof(G) == 4)
-                if (add) {
-                    stored = true;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (o + j < end) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(to + (int64_t)j * p.I), "f"(v[j]) : "memory");
-                }
-            if (!stored) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (o + j < end) to[(int64_t)j * p.I] = from_float<G>(v[j]);
-            }
+        const uint32_t at = sums + (quarter << 16) + o;
+        uint32_t v[16] = {};
+        if (chunks > 1) {
+            add_sums(at, at + kTileO, v);
+        } else if (chunks > 0) {
+            read_sums(at, v);
+            wait_read(v);
         }
+        if (i < p.I)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (o + j < end) to[(int64_t)j * p.I] = from_float<G>(__uint_as_float(v[j]));
         __syncwarp();
     }
 }
 
 // G: the output's type.
 template <typename G>
-__global__ void __launch_bounds__(kThreads<G>, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p) {
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[kSlots], empty[kSlots], summed[2], written[2], all_written;
+    __shared__ uint64_t full[kSlots], empty[kSlots], summed[2], added, complete;
     __shared__ uint32_t tensor_memory;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t slots = (smem_at(raw) + 1023u) & ~1023u;
@@ -203,11 +215,9 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
             barrier_init(&full[s], kGroupWarps + 1);
             barrier_init(&empty[s], 1);
         }
-        for (int h = 0; h < 2; ++h) {
-            barrier_init(&summed[h], 1);
-            barrier_init(&written[h], 4);
-        }
-        barrier_init(&all_written, 4);
+        for (int h = 0; h < 2; ++h) barrier_init(&summed[h], 1);
+        barrier_init(&added, 4);
+        barrier_init(&complete, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMultiplyWarp) {
@@ -225,7 +235,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
     const int w = blockIdx.z % p.W, split = blockIdx.z / p.W;
     const int64_t first = split * p.split_steps * kStep;
     const int64_t tokens = min(p.M - first, p.split_steps * kStep);
-    const int steps = static_cast<int>((tokens + kStep - 1) / kStep), chunks = (steps + p.chunk - 1) / p.chunk;
+    const int steps = static_cast<int>((tokens + kStep - 1) / kStep), chunks = (steps + kChunk - 1) / kChunk;
 
     G* const out0 = static_cast<G*>(p.out) + split * p.out_split + w * p.out_worker;
     if (warp == kCopyWarp) {
@@ -250,10 +260,10 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
         if (lane == 0) {
             bool ok = true;
             for (int c = 0; c < chunks && ok; ++c) {
-                const int h = c % 2, end = min((c + 1) * p.chunk, steps);
-                if (c >= 2) ok = barrier_wait(&written[h], (c / 2 - 1) & 1);
+                const int end = min((c + 1) * kChunk, steps);
+                if (c >= 2) ok = barrier_wait(&added, c & 1);  // the chunk before is out of the way
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int k = c * p.chunk; k < end && ok; ++k) {
+                for (int k = c * kChunk; k < end && ok; ++k) {
                     const int s = k % kSlots;
                     ok = barrier_wait(&full[s], k / kSlots & 1);
                     if (!ok) break;
@@ -261,28 +271,35 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
                     const uint64_t a = matrix_at(slots + s * kSlotBytes), b = matrix_at(slots + s * kSlotBytes + kXBytes);
 #pragma unroll
                     for (int q = 0; q < kStep / 16; ++q)
-                        multiply(sums + h * kTileO, a + q * (2048 >> 4), b + q * (2048 >> 4), k > c * p.chunk || q > 0);
+                        multiply(sums + (c > 0 ? kTileO : 0), a + q * (2048 >> 4), b + q * (2048 >> 4), k > c * kChunk || q > 0);
                     arrive_when_multiplied(&empty[s]);
                 }
-                arrive_when_multiplied(&summed[h]);
+                arrive_when_multiplied(&summed[c % 2]);
             }
         }
-    } else if (warp >= kWriteWarp) {
-        if constexpr (sizeof(G) == 4) {
-            bool ok = true;
-            for (int c = 0; c < chunks - 1 && ok; ++c) {
-                const int h = c % 2;
-                ok = __all_sync(~0u, barrier_wait(&summed[h], c / 2 & 1));
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                write_out(p, sums + h * kTileO, i0, o0, 0, kTileO, c > 0, true, out0);
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) barrier_arrive(&written[h]);
+    } else if (warp >= kAddWarp) {
+        // Every chunk's sums are waited for in turn. Two barriers take turns: the second chunk does not wait for this
+        // warp, so one barrier could be two phases on before it looks.
+        bool ok = true;
+        for (int c = 0; c < chunks && ok; ++c) {
+            ok = __all_sync(~0u, barrier_wait(&summed[c % 2], c / 2 & 1));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (c == 0 || c == chunks - 1) continue;
+            const uint32_t at = sums + (warp % 4 * 32 << 16);
+#pragma unroll 2
+            for (int o = 0; o < kTileO; o += 16) {
+                uint32_t v[16];
+                add_sums(at + o, at + kTileO + o, v);
+                store_sums(at + o, v);
             }
-            __threadfence();  // these additions before those of the converting warps
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) barrier_arrive(&all_written);
+            if (lane == 0) barrier_arrive(&added);
         }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) barrier_arrive(&complete);
     } else {
         // thread: token 8 * (its warp in the group) + lane / 4 of the step, features 32 * (lane % 4) + 0..31 of the tile
         const int token = warp % kGroupWarps * 8 + lane / 4, quarter = lane % 4, block = i0 / kBlock8 + quarter;
@@ -342,15 +359,10 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
                 if (lane == 0) barrier_arrive(&full[s]);
             }
         }
-        // The last chunk, after those before it are in the output. Its barrier has
-        // by now seen the chunk two before: the slots just filled were free, so
-        // the products are at most 2 kSlots steps behind.
-        static_assert(kChunk >= 2 * kSlots, "the parity of `summed` tells the last chunk from the one two before");
         constexpr int kPart = kTileO * 4 / kConvertWarps;
-        if (chunks > 0) __all_sync(~0u, barrier_wait(&summed[(chunks - 1) % 2], (chunks - 1) / 2 & 1));
-        if (chunks > 1) __all_sync(~0u, barrier_wait(&all_written, 0));
+        __all_sync(~0u, barrier_wait(&complete, 0));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        write_out(p, sums + (chunks > 0 ? (chunks - 1) % 2 : 0) * kTileO, i0, o0, warp / 4 * kPart, kPart, chunks > 1, chunks > 0, out0);
+        write_out(p, sums, chunks, i0, o0, warp / 4 * kPart, kPart, out0);
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
     __syncthreads();
@@ -509,7 +521,6 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     p.codes = codes, p.exponents = exponents;
     p.M = M, p.O = O, p.I = I, p.W = W, p.blocks = static_cast<int>(ceil_div(I, kBlock8));
     p.split_steps = sp.each;
-    p.chunk = parts || dW_dtype == CPDP_F32 ? kChunk : INT_MAX / 2;
     p.out = parts ? workspace : dW;
     p.out_worker = parts ? (int64_t)O * I : dW_worker;
     p.out_split = (int64_t)W * O * I;
@@ -551,7 +562,7 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
             e = cudaFuncSetAttribute(weight_gradient_kernel<G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
             if (e == cudaSuccess) allowed |= bit;
         }
-        return e != cudaSuccess ? e : launch_layer(weight_gradient_kernel<G>, grid, kThreads<G>, kSmemBytes, stream, map, p);
+        return e != cudaSuccess ? e : launch_layer(weight_gradient_kernel<G>, grid, kThreads, kSmemBytes, stream, map, p);
     };
     CPDP_TRY(layer_launched(parts || dW_dtype == CPDP_F32 ? typed(0.f) : typed(__nv_bfloat16{}), "cpdp_weight_gradient"));
     if (!parts) return CPDP_OK;
