@@ -21,8 +21,9 @@
  *
  * Types. Activations are float32 or bfloat16 (cpdp_dtype); all arithmetic,
  * sums and states are float32, and an output is rounded once (to nearest even)
- * when it is stored. Infinities and NaN follow from the formulas. A square
- * above the float32 range (|s| > 1.8e19) makes the norm's scale 0.
+ * when it is stored. Infinities and NaN follow from the formulas. A row whose
+ * sum of squares is above the float32 range (a root mean square above
+ * 1.8e19 / sqrt(D)) has the scale k = 0 in the norm.
  *
  * 8 bits. Blocks of 32 neighbouring features share an exponent e, the least
  * with max|x| <= 127 * 2^e, kept between -126 and 121; a value is held as the

@@ -199,7 +199,9 @@ norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_
             sum[1] = fmaf(g0[k / V].get(k % V) * (KEEP ? wt[KEEP ? k : 0] : weight_at(k)), v, sum[1]);
         }
         row_sum<TPR>(sum, turn);
-        const float k1 = rsqrtf(sum[0] / D + eps), k3 = k1 * k1 * k1 * (sum[1] / D);
+        // s k^3 mean(dy weight s) as (s k)(k mean(dy weight s) k): k^3 alone leaves float32's range at rows of 1e13, or where
+        // eps is 1e-26
+        const float k1 = rsqrtf(sum[0] / D + eps), slope = sum[1] / D * k1 * k1;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int d = (j * TPR + t) * V;
@@ -209,7 +211,7 @@ norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_
             for (int e = 0; e < V; ++e) {
                 const int k = j * V + e;
                 const float v = r0[j].get(e), gk = g0[j].get(e) * k1;
-                o[e] = fmaf(gk, KEEP ? wt[KEEP ? k : 0] : weight_at(k), through0[j].get(e)) - v * k3;
+                o[e] = fmaf(gk, KEEP ? wt[KEEP ? k : 0] : weight_at(k), through0[j].get(e)) - v * k1 * slope;
                 sums[k] = fmaf(gk, v, sums[k]);
             }
             if (d < D && (TPR >= 32 || m < M)) store_piece<V>(static_cast<T*>(dx) + (w * M + m) * D + d, o);

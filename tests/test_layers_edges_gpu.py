@@ -62,3 +62,37 @@ def test_weight_gradient_in_bfloat16_of_a_million_tokens():
     want = torch.full((UNSPLIT, 8, 8), M * 127 * 129 / 2.0 ** 14, dtype=torch.float64, device="cuda")
     for grad in (F32, BF16):
         near(layers.weight_gradient(dy, saved, dtype=grad), want, sum_error(M) * want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("eps", [1e-6, 1e-30])
+@pytest.mark.parametrize("size", [1e-15, 1e-8, 1.0, 1e12, 1e14, 1e15, 1e16, 1e17])
+@pytest.mark.parametrize("shape", [(2, 5, 64), (1, 3, 771), (1, 2, 4096), (1, 2, 16384)])
+def test_norm_backward_of_small_and_large_rows(shape, size, eps, dtype):
+    """dy has a part along s, which the projection takes away: the term that rows of 1e13 and more used to lose."""
+    gen = gpu_rng(shape[2])
+    s = (torch.randn(shape, generator=gen, device="cuda") * size).to(dtype)
+    dy = (torch.randn(shape, generator=gen, device="cuda") + s.float() / size).to(dtype)
+    ds = (torch.randn(shape, generator=gen, device="cuda") * 0.1 / size).to(dtype)
+    w = 1 + 0.3 * torch.randn(shape[0], shape[2], generator=gen, device="cuda")
+    for through in (None, ds):
+        want, dweight, bound, bound_w = (t.cuda() for t in ref.norm_backward(dy.cpu(), s.cpu(), w.cpu(), None if through is None else ds.cpu(), eps))
+        dx, dw = layers.add_rmsnorm_backward(dy, s, w, through, eps=eps)
+        near(dx, want, bound)
+        near(dw, dweight, bound_w)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("eps", [1e-6, 1e-26, 1e-30, 1e-37])
+@pytest.mark.parametrize("D", [64, 771, 4096, 16384])
+def test_norm_backward_of_rows_of_zeros(D, eps, dtype):
+    """k = 1 / sqrt(eps) there: dx is ds + k dy weight, with nothing to take away."""
+    gen = gpu_rng(D)
+    s = torch.zeros(1, 3, D, dtype=dtype, device="cuda")
+    dy, ds = (torch.randn(1, 3, D, generator=gen, device="cuda").to(dtype) for _ in range(2))
+    w = torch.rand(1, D, generator=gen, device="cuda")
+    dx, dw = layers.add_rmsnorm_backward(dy, s, w, ds, eps=eps)
+    k = torch.tensor(eps, dtype=F32).double().item() ** -0.5
+    want = ds.double() + k * dy.double() * w.double()
+    near(dx, want, 16 * ref.U32 * (ds.double().abs() + k * (dy.double() * w.double()).abs()))
+    assert (dw == 0).all()
