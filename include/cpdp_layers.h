@@ -17,7 +17,8 @@
  * weights and their gradients lie inside the workers' [W][N] parameter and
  * gradient rows (cpdp.h): worker w's is at pointer + w * stride, contiguous,
  * at any element alignment. Other pointers are aligned to their element.
- * Outputs must not overlap inputs or each other.
+ * Outputs must not overlap inputs or each other. An output whose own strides
+ * make its parts overlap is refused.
  *
  * Types. Activations are float32 or bfloat16 (cpdp_dtype); all arithmetic,
  * sums and states are float32, and an output is rounded once (to nearest even)
@@ -163,7 +164,9 @@ cpdp_status cpdp_gated_recurrence(const void *gate, int64_t gate_seq, int64_t ga
  *   carry           what the forward pass wrote; the states between are made
  *                   again from gate and value
  *   dgate, dvalue   of dtype, with one sequence and one step stride for both
- *                   (two halves of one [B][T][2 D], say); 0 beyond a length
+ *                   (two halves of one [B][T][2 D], say; all of a sequence's
+ *                   steps between two sequences, or all sequences between two
+ *                   steps); 0 beyond a length
  *   dh0             float32 [B][D] (NULL: not wanted)
  * The workspace is that of the forward pass.
  */

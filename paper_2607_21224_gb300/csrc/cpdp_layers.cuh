@@ -48,6 +48,17 @@ inline cpdp_status check_array(const char* name, const void* p, bool wanted, int
     return CPDP_OK;
 }
 
+// Parts of an output, `size` elements each and `stride` apart, that different blocks write.
+inline cpdp_status check_apart(const char* name, int64_t count, int64_t stride, int64_t size) {
+    if (count > 1 && stride < size)
+        return layer_error(CPDP_EINVAL, "%s: parts of %lld elements at a stride of %lld overlap", name, (long long)size, (long long)stride);
+    return CPDP_OK;
+}
+// Whether n rows of `inner` elements of stride lie between neighbours of stride `outer`.
+inline bool nested(int64_t count, int64_t outer, int64_t n, int64_t inner, int64_t size) {
+    return (n <= 1 || inner >= size) && (count <= 1 || (outer >= size && (n <= 1 || n - 1 <= (outer - size) / inner)));
+}
+
 inline cpdp_status check_workspace(const void* p, size_t bytes, size_t needed) {
     if (needed == 0) return CPDP_OK;
     if (p == nullptr || bytes < needed)

@@ -366,6 +366,7 @@ cpdp_status cpdp_add_rmsnorm_backward(const void* dy, int64_t dy_worker, int64_t
     CPDP_TRY(check_array("dx", dx, some, e));
     if (!known_dtype(dweight_dtype)) return layer_error(CPDP_EINVAL, "unknown dtype %d of dweight", (int)dweight_dtype);
     CPDP_TRY(check_array("dweight", dweight, true, dtype_size(dweight_dtype), dweight_worker));
+    CPDP_TRY(check_apart("dweight", W, dweight_worker, D));
     CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_add_rmsnorm_backward_workspace(W, M, D)));
     const NormIn gi{dy, dy_worker, dy_row}, si{s, s_worker, s_row}, di{ds, ds_worker, ds_row};
     float* parts = static_cast<float*>(workspace);

@@ -563,6 +563,9 @@ cpdp_status cpdp_gated_recurrence_backward(const void* dh, int64_t dh_seq, int64
     CPDP_TRY(check_array("lengths", lengths, false, 4));
     CPDP_TRY(check_array("dgate", dgate, some, e, grad_seq, grad_step));
     CPDP_TRY(check_array("dvalue", dvalue, some, e));
+    if (some && !nested(B, grad_seq, T, grad_step, D) && !nested(T, grad_step, B, grad_seq, D))
+        return layer_error(CPDP_EINVAL, "dgate and dvalue: rows of %d elements at strides of %lld and %lld overlap", D, (long long)grad_seq,
+                           (long long)grad_step);
     CPDP_TRY(check_array("dh0", dh0, false, 4));
     CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_gated_recurrence_workspace(B, T, D)));
     if (B == 0) return CPDP_OK;

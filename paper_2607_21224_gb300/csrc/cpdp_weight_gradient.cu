@@ -514,6 +514,7 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     CPDP_TRY(check_array("codes", codes, M > 0, 16));
     CPDP_TRY(check_array("exponents", exponents, M > 0, 1));
     CPDP_TRY(check_array("dW", dW, true, dtype_size(dW_dtype), dW_worker));
+    CPDP_TRY(check_apart("dW", W, dW_worker, (int64_t)O * I));
     CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_weight_gradient_workspace(dy, dy_worker, dy_row, dy_dtype, W, M, O, I)));
     const Splits sp = splits_of(W, M, O, I);
     const bool parts = sp.count > 1;

@@ -28,6 +28,7 @@ refuses with ``CPDPError``.
 from __future__ import annotations
 
 import ctypes
+import math
 from dataclasses import dataclass
 
 import torch
@@ -242,7 +243,21 @@ def _gradient_out(out, name: str, shape: tuple, dtype: torch.dtype, device: torc
         raise ValueError(f"{name} must have shape {shape} on {device}, got {tuple(out.shape)} on {out.device}")
     if not out.is_contiguous() and not out[0].is_contiguous():
         raise ValueError(f"each worker's part of {name} must be contiguous")
+    if shape[0] > 1 and out.stride(0) < math.prod(shape[1:]):
+        raise ValueError(f"the workers' parts of {name} overlap: worker stride {out.stride(0)}")
     return out
+
+
+def _rows_apart(t: torch.Tensor, name: str) -> None:
+    """Refuses an output (A, B, D) some of whose rows share memory: all of one axis's rows lie between two of the other's."""
+    (A, B, D), (a, b, _) = t.shape, t.stride()
+    if A > 1 and B > 1:
+        (n, inner), outer = ((B, b), a) if a >= b else ((A, a), b)
+        apart = inner >= D and outer >= (n - 1) * inner + D
+    else:
+        apart = (A <= 1 or a >= D) and (B <= 1 or b >= D)
+    if not apart and t.numel():
+        raise ValueError(f"rows of {name} overlap: shape {tuple(t.shape)}, strides {t.stride()}")
 
 
 def add_rmsnorm_backward(dy, s, weight, ds=None, *, eps: float = 1e-6, dweight=None, dtype=torch.float32, stream=None):
@@ -402,6 +417,7 @@ def gated_recurrence_backward(dh, gate, value, carry, dh_last=None, lengths=None
     if out is None:
         out = torch.empty((B, T, 2 * D), dtype=dtype, device=device)
     ps = _input(out, "out", (B, T, 2 * D), dtype, device)
+    _rows_apart(out, "out")
     dgate, dvalue = out.chunk(2, 2)
     dh0 = torch.empty((B, D), dtype=_F32, device=device)
     needed = _entry("cpdp_gated_recurrence_workspace")(B, T, D)

@@ -96,3 +96,29 @@ def test_norm_backward_of_rows_of_zeros(D, eps, dtype):
     want = ds.double() + k * dy.double() * w.double()
     near(dx, want, 16 * ref.U32 * (ds.double().abs() + k * (dy.double() * w.double()).abs()))
     assert (dw == 0).all()
+
+
+def test_outputs_that_overlap_themselves_are_refused():
+    x, w = torch.ones(2, 3, 32, device="cuda"), torch.ones(2, 32, device="cuda")
+    saved, _ = layers.checkpoint(x)
+    carry = layers.gated_recurrence(x, x)[2]
+    long = torch.full((500,), 7.0, device="cuda")
+    for call in (lambda: layers.add_rmsnorm_backward(x, x, w, dweight=long[:32].expand(2, 32)),
+                 lambda: layers.add_rmsnorm_backward(x, x, w, dweight=long.as_strided((2, 32), (31, 1))),
+                 lambda: layers.weight_gradient(x, saved, out=torch.zeros(1, 32, 32, device="cuda").expand(2, 32, 32)),
+                 lambda: layers.gated_recurrence_backward(x, x, x, carry, out=long[:64].expand(2, 3, 64)),
+                 lambda: layers.gated_recurrence_backward(x, x, x, carry, out=long.as_strided((2, 3, 64), (64 * 3, 63, 1)))):
+        with pytest.raises(ValueError, match="overlap"):
+            call()
+    assert (long == 7).all()
+
+
+@pytest.mark.parametrize("D", [32, 33])
+def test_recurrence_gradients_into_arrays_with_the_steps_outside(D):
+    gen = gpu_rng(D)
+    gate, value, dh = (torch.randn(3, 70, D, generator=gen, device="cuda") for _ in range(3))
+    carry = layers.gated_recurrence(gate, value)[2]
+    want = layers.gated_recurrence_backward(dh, gate, value, carry)
+    out = torch.full((70, 3, 2 * D), float("nan"), device="cuda").transpose(0, 1)
+    got = layers.gated_recurrence_backward(dh, gate, value, carry, out=out)
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and torch.equal(out, torch.cat(want[:2], 2))

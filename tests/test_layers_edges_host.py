@@ -1,0 +1,54 @@
+"""Host-side refusals of the layers that need no GPU: outputs that overlap
+themselves."""
+import pytest
+import torch
+
+from paper_2607_21224_gb300 import cpdp, layers
+
+P = 1 << 20  # an address that no refused call reads
+L40 = 1 << 40
+
+
+def norm_backward(W, stride, D=32):
+    return "cpdp_add_rmsnorm_backward", [P, 10 * D, D, P, 10 * D, D, None, 0, 0, P, D, 0, W, 10, D, 1e-6, P, P, stride, 0, P, L40, None]
+
+
+def weight_gradient(W, stride, O=32, I=32):
+    return "cpdp_weight_gradient", [P, 10 * O, O, 1, P, P, W, 10, O, I, P, stride, 0, P, L40, None]
+
+
+def recurrence_backward(B, T, seq, step, D=32):
+    return "cpdp_gated_recurrence_backward", [P, T * D, D, P, T * D, D, P, T * D, D, 0, B, T, D, P, None, None, P, P, seq, step, None,
+                                              P, L40, None]
+
+
+OVERLAPPING = [norm_backward(2, 0), norm_backward(2, 31), norm_backward(4096, 1), weight_gradient(2, 0), weight_gradient(2, 1023),
+               recurrence_backward(1, 10, 0, 0), recurrence_backward(1, 10, 0, 31), recurrence_backward(2, 10, 0, 32),
+               recurrence_backward(2, 10, 319, 32), recurrence_backward(2, 1, 31, 0), recurrence_backward(2, 10, 32, 63),
+               recurrence_backward(3, 10, 32, 95), recurrence_backward(2, 10, L40, 0), recurrence_backward(2, 1 << 20, 1 << 30, 1 << 11)]
+
+
+@pytest.mark.parametrize("name,arguments", OVERLAPPING, ids=lambda v: v if isinstance(v, str) else None)
+def test_overlapping_outputs_are_refused(name, arguments):
+    assert getattr(layers.lib(), name)(*arguments) == cpdp.CPDP_EINVAL
+    assert "overlap" in cpdp.cpdp_last_error(None)
+
+
+def test_python_refuses_overlapping_outputs():
+    cpu = torch.device("cpu")
+    for shape, view in [((2, 8), torch.zeros(1, 8).expand(2, 8)), ((2, 8), torch.zeros(20).as_strided((2, 8), (7, 1))),
+                        ((3, 4, 8), torch.zeros(1, 4, 8).expand(3, 4, 8)), ((2, 4, 8), torch.zeros(99).as_strided((2, 4, 8), (31, 8, 1)))]:
+        with pytest.raises(ValueError, match="overlap"):
+            layers._gradient_out(view, "out", shape, torch.float32, cpu)
+    for shape, view in [((2, 8), torch.zeros(20).as_strided((2, 8), (8, 1))), ((1, 8), torch.zeros(8).as_strided((1, 8), (0, 1))),
+                        ((2, 4, 8), torch.zeros(2, 40)[:, 3:35].view(2, 4, 8)), ((2, 1), torch.zeros(2, 9)[:, :1])]:
+        assert layers._gradient_out(view, "out", shape, torch.float32, cpu) is view
+    long = torch.zeros(4000)
+    for shape, strides in [((2, 5, 8), (40, 0, 1)), ((2, 5, 8), (0, 8, 1)), ((2, 5, 8), (39, 8, 1)), ((1, 5, 8), (0, 7, 1)),
+                           ((2, 5, 8), (8, 15, 1)), ((5, 1, 8), (7, 0, 1))]:
+        with pytest.raises(ValueError, match="overlap"):
+            layers._rows_apart(long.as_strided(shape, strides), "out")
+    # sequences outside, steps outside, gaps, axes of one or none
+    for shape, strides in [((2, 5, 8), (40, 8, 1)), ((2, 5, 8), (8, 16, 1)), ((2, 5, 8), (100, 11, 1)), ((1, 5, 8), (0, 8, 1)),
+                           ((5, 1, 8), (8, 0, 1)), ((1, 1, 8), (0, 0, 1)), ((0, 5, 8), (0, 0, 1)), ((5, 0, 8), (0, 8, 1)), ((2, 5, 8), (32 + 8, 8, 1))]:
+        layers._rows_apart(long.as_strided(shape, strides), "out")
