@@ -188,9 +188,9 @@ cpdp_status cpdp_gated_recurrence_step(const void *gate, int64_t gate_seq, const
 
 /*
  * cpdp_layer_timeouts — the number of bounded waits that ran out since the last
- * call (0 expected; results after one are not valid): the weight gradient's
- * warps wait for the slots of a ring, for some seconds at most. Waits for the
- * device.
+ * call (0 expected): the weight gradient's warps wait for the slots of a ring,
+ * for some seconds at most. A block in which one ran out writes NaN for all of
+ * its tile of dW. Waits for the device.
  */
 cpdp_status cpdp_layer_timeouts(int64_t *count);
 

@@ -10,8 +10,8 @@ namespace {
 
 // dW = dy^T x^ is bound by shared memory: a step of 64 tokens takes the tensor
 // core 512 clocks, and 768 times 128 bytes move for it (48 KB of operands read,
-// 32 KB of dy and 16 KB of x^ written). 2 x 16,384 tokens, 2,048 -> 8,192: 819 us,
-// 1,342 TFLOP/s, to either type; 8 x 3,152, 384 -> 1,536 (144 blocks): 37 us.
+// 32 KB of dy and 16 KB of x^ written). 2 x 16,384 tokens, 2,048 -> 8,192: 809 us,
+// 1,359 TFLOP/s, to either type; 8 x 3,152, 384 -> 1,536 (144 blocks): 37 us.
 //
 // One block computes 128 (i) x 256 (o) of dW, transposed on the tensor cores:
 // the accumulator's 128 lanes are neighbouring i, so that a warp's stores of
@@ -44,7 +44,13 @@ constexpr int kBlockBytes = kStep * 128;                               // a step
 constexpr int kXBytes = kTileI / 64 * kBlockBytes, kDyBytes = kTileO / 64 * kBlockBytes, kSlotBytes = kXBytes + kDyBytes;
 constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;  // and room to align the slots
 constexpr int kAhead = 2;                               // of its steps whose codes a group loads ahead
+#ifdef CPDP_CHECKED
+constexpr unsigned long long kWaitLimitNs = 200000000ull;
+// A step whose dy is never copied, so that waits run out; -1: none. Debug build only.
+__device__ int dropped_step = -1;
+#else
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
+#endif
 static_assert(kStep * kTileI == kGroupWarps * 32 * kBlock8, "one block of features per converting thread and step");
 
 __device__ unsigned long long wait_timeouts;
@@ -71,18 +77,19 @@ __device__ __forceinline__ bool barrier_done(uint64_t* b, uint32_t parity, uint3
         : "memory");
     return done != 0;
 }
-// False, and counted, where the phase does not end within the limit.
-__device__ __noinline__ bool barrier_wait_long(uint64_t* b, uint32_t parity) {
+// False, counted and noted in the block's `failed`, where the phase does not end within the limit.
+__device__ __noinline__ bool barrier_wait_long(uint64_t* b, uint32_t parity, int* failed) {
     const unsigned long long start = now_ns();
     while (!barrier_done(b, parity, 100000u))
         if (now_ns() - start > kWaitLimitNs) {
             atomicAdd(&wait_timeouts, 1ull);
+            *static_cast<volatile int*>(failed) = 1;
             return false;
         }
     return true;
 }
-__device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity) {
-    return barrier_done(b, parity, 100000u) || barrier_wait_long(b, parity);
+__device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, int* failed) {
+    return barrier_done(b, parity, 100000u) || barrier_wait_long(b, parity, failed);
 }
 
 // A matrix in shared memory whose rows of 64 elements run along the summed
@@ -206,11 +213,13 @@ template <typename G>
 __global__ void __launch_bounds__(kThreads, 1)
 weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p) {
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[kSlots], empty[kSlots], summed[2], added, complete;
+    __shared__ uint64_t full[kSlots], empty[kSlots], summed[2], added, complete, drained;
     __shared__ uint32_t tensor_memory;
+    __shared__ int failed;  // a wait of the block ran out
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t slots = (smem_at(raw) + 1023u) & ~1023u;
     if (threadIdx.x == 0) {
+        failed = 0;
         for (int s = 0; s < kSlots; ++s) {
             barrier_init(&full[s], kGroupWarps + 1);
             barrier_init(&empty[s], 1);
@@ -218,6 +227,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
         for (int h = 0; h < 2; ++h) barrier_init(&summed[h], 1);
         barrier_init(&added, 4);
         barrier_init(&complete, 4);
+        barrier_init(&drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMultiplyWarp) {
@@ -243,7 +253,10 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
             int k = 0;
             for (; k < steps; ++k) {
                 const int s = k % kSlots;
-                if (k >= kSlots && !barrier_wait(&empty[s], (k / kSlots - 1) & 1)) break;
+                if (k >= kSlots && !barrier_wait(&empty[s], (k / kSlots - 1) & 1, &failed)) break;
+#ifdef CPDP_CHECKED
+                if (k == *static_cast<volatile int*>(&dropped_step)) continue;
+#endif
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(&full[s])), "r"(kDyBytes) : "memory");
                 for (int c = 0; c < kTileO / 64; ++c)
                     asm volatile(
@@ -252,20 +265,19 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
                         "l"(&map), "r"(o0 + c * 64), "r"(static_cast<int>(first) + k * kStep), "r"(w), "r"(smem_at(&full[s]))
                         : "memory");
             }
-            // no copy may be in flight when the block ends: where a wait ran out, see the issued ones through
-            if (k < steps)
-                for (int q = max(k - kSlots, 0); q < k; ++q) barrier_wait(&full[q % kSlots], q / kSlots & 1);
+            // no copy may be in flight when the block ends, also where a wait ran out
+            for (int q = max(k - kSlots, 0); q < k; ++q) barrier_wait(&full[q % kSlots], q / kSlots & 1, &failed);
         }
     } else if (warp == kMultiplyWarp) {
         if (lane == 0) {
             bool ok = true;
             for (int c = 0; c < chunks && ok; ++c) {
                 const int end = min((c + 1) * kChunk, steps);
-                if (c >= 2) ok = barrier_wait(&added, c & 1);  // the chunk before is out of the way
+                if (c >= 2) ok = barrier_wait(&added, c & 1, &failed);  // the chunk before is out of the way
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 for (int k = c * kChunk; k < end && ok; ++k) {
                     const int s = k % kSlots;
-                    ok = barrier_wait(&full[s], k / kSlots & 1);
+                    ok = barrier_wait(&full[s], k / kSlots & 1, &failed);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t a = matrix_at(slots + s * kSlotBytes), b = matrix_at(slots + s * kSlotBytes + kXBytes);
@@ -276,13 +288,17 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
                 }
                 arrive_when_multiplied(&summed[c % 2]);
             }
+            // nor a product
+            arrive_when_multiplied(&drained);
+            barrier_wait(&drained, 0, &failed);
         }
     } else if (warp >= kAddWarp) {
         // Every chunk's sums are waited for in turn. Two barriers take turns: the second chunk does not wait for this
         // warp, so one barrier could be two phases on before it looks.
         bool ok = true;
         for (int c = 0; c < chunks && ok; ++c) {
-            ok = __all_sync(~0u, barrier_wait(&summed[c % 2], c / 2 & 1));
+            ok = __all_sync(~0u, barrier_wait(&summed[c % 2], c / 2 & 1, &failed));
+            if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (c == 0 || c == chunks - 1) continue;
             const uint32_t at = sums + (warp % 4 * 32 << 16);
@@ -340,7 +356,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
                 if (k >= steps || !ok) break;
                 const Codes c = ahead[u];
                 ahead[u] = load();
-                if (k >= kSlots) ok = __all_sync(~0u, barrier_wait(&empty[s], (k / kSlots - 1) & 1));
+                if (k >= kSlots) ok = __all_sync(~0u, barrier_wait(&empty[s], (k / kSlots - 1) & 1, &failed));
                 if (!ok) break;
                 // a block with an infinite or NaN value reads as NaN
                 const uint32_t unit = c.byte == 255u ? 0x7fc07fc0u : c.byte << 7 | c.byte << 23;
@@ -360,7 +376,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
             }
         }
         constexpr int kPart = kTileO * 4 / kConvertWarps;
-        __all_sync(~0u, barrier_wait(&complete, 0));
+        __all_sync(~0u, barrier_wait(&complete, 0, &failed));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         write_out(p, sums, chunks, i0, o0, warp / 4 * kPart, kPart, out0);
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -370,6 +386,12 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(2 * kTileO));
     }
+    // what a block makes whose wait ran out is not dW: it says so
+    if (failed)
+        for (int k = threadIdx.x; k < kTileI * kTileO; k += kThreads) {
+            const int i = i0 + k % kTileI, o = o0 + k / kTileI;
+            if (i < p.I && o < p.O) out0[(int64_t)o * p.I + i] = from_float<G>(__uint_as_float(0x7fc00000u));
+        }
 }
 
 // dy as the tensor copies need it: bfloat16 rows at multiples of 16 bytes. A
@@ -575,6 +597,12 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     };
     return layer_launched(dW_dtype == CPDP_F32 ? sum(static_cast<float*>(dW)) : sum(static_cast<__nv_bfloat16*>(dW)), "cpdp_weight_gradient");
 }
+
+#ifdef CPDP_CHECKED
+extern "C" cpdp_status cpdp_layer_drop_step(int step) {
+    return layer_launched(cudaMemcpyToSymbol(dropped_step, &step, sizeof step), "cpdp_layer_drop_step");
+}
+#endif
 
 cpdp_status cpdp_layer_timeouts(int64_t* count) {
     if (count == nullptr) return layer_error(CPDP_EINVAL, "count is NULL");

@@ -455,7 +455,8 @@ def gated_recurrence_step(gate, value, state, *, stream=None):
 
 def wait_timeouts() -> int:
     """Bounded waits of the weight gradient's kernel that ran out since the last
-    call (0 expected). Waits for the current device."""
+    call (0 expected; the tiles of dW concerned are NaN). Waits for the current
+    device."""
     count = _L()
     _check(_entry("cpdp_layer_timeouts")(ctypes.byref(count)))
     return count.value

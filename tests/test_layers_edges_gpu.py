@@ -2,14 +2,26 @@
 tokens in one sum, activations and eps far from 1, gates far from 0, buffers
 that change between calls. References are the formulas in 64 bits; a tolerance
 is what the stated order of the operations may add."""
+import json
+import os
+import subprocess
+import sys
+from pathlib import Path
+
 import pytest
 import torch
 
 import layers_reference as ref
-from paper_2607_21224_gb300 import layers
+from paper_2607_21224_gb300 import build, layers
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(autouse=True)
+def no_wait_runs_out():
+    yield
+    assert layers.wait_timeouts() == 0
 
 
 def gpu_rng(seed):
@@ -122,3 +134,16 @@ def test_recurrence_gradients_into_arrays_with_the_steps_outside(D):
     out = torch.full((70, 3, 2 * D), float("nan"), device="cuda").transpose(0, 1)
     got = layers.gated_recurrence_backward(dh, gate, value, carry, out=out)
     assert all(torch.equal(p, q) for p, q in zip(got, want)) and torch.equal(out, torch.cat(want[:2], 2))
+
+
+def test_weight_gradient_is_nan_where_a_wait_ran_out():
+    """In the debug build, where a copy can be left out: its slot never fills, every role's wait ends by its limit, and what
+    the blocks write is NaN, through the sum of split tokens too. The next call is whole again."""
+    program = Path(__file__).resolve().parent / "checked_layers.py"
+    env = dict(os.environ, CPDP_LIBRARY=str(build.build_library(checked=True)))
+    proc = subprocess.run([sys.executable, str(program)], env=env, capture_output=True, text=True, timeout=300)
+    assert proc.returncode == 0, proc.stderr[-3000:]
+    for name, r in json.loads(proc.stdout.strip().splitlines()[-1]).items():
+        assert r["before"] == 0 and r["finite"], name
+        assert r["ran_out"] > 0 and r["all_nan"] and r["beside"], name
+        assert r["same_after"] and r["after"] == 0, name
