@@ -107,7 +107,7 @@ checkpoint_rows_kernel(const T* x, int64_t x_worker, int64_t x_row, int64_t M, i
 #pragma unroll
     for (int k = 0; k < kSpan; ++k) {
         in[k] = Piece<T, 1>{};
-        if (k < at.count && d0 + k * kBlock8 < D) in[k].load(p + k * kBlock8);
+        in[k].load(p + k * kBlock8, k < at.count && d0 + k * kBlock8 < D);
     }
     int8_t* q = codes + (at.row * blocks + at.first) * kBlock8 + lane;
     __nv_bfloat16* v = values + at.row * D + d0;
@@ -140,8 +140,8 @@ restore_kernel(const int8_t* codes, const uint8_t* exponents, int D, int blocks,
         in[u] = make_int2(0, 0);
         byte[u] = 0;
         if (at.find(u, row, piece)) {
-            in[u] = __ldcs(reinterpret_cast<const int2*>(codes + row * blocks * kBlock8 + piece * V));
-            byte[u] = __ldg(exponents + row * blocks + piece * V / kBlock8);
+            in[u] = load_once(reinterpret_cast<const int2*>(codes + row * blocks * kBlock8 + piece * V));
+            byte[u] = exponents[row * blocks + piece * V / kBlock8];
         }
     }
 #pragma unroll
@@ -164,10 +164,10 @@ restore_rows_kernel(const int8_t* codes, const uint8_t* exponents, int64_t rows,
     if (at.count <= 0) return;
     const int lane = threadIdx.x % 32, d0 = at.first * kBlock8 + lane;
     const int8_t* q = codes + (at.row * blocks + at.first) * kBlock8 + lane;
-    const uint32_t kept = lane < at.count ? __ldg(exponents + at.row * blocks + at.first + lane) : 0u;
+    const uint32_t kept = lane < at.count ? exponents[at.row * blocks + at.first + lane] : 0u;
     int code[kSpan];
 #pragma unroll
-    for (int k = 0; k < kSpan; ++k) code[k] = k < at.count ? __ldcs(q + k * kBlock8) : 0;
+    for (int k = 0; k < kSpan; ++k) code[k] = k < at.count ? load_once(q + k * kBlock8) : 0;
 #pragma unroll
     for (int k = 0; k < kSpan; ++k) {
         const uint32_t byte = __shfl_sync(~0u, kept, k);

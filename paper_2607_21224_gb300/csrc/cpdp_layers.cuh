@@ -97,6 +97,52 @@ __device__ __forceinline__ void layer_begin() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// Loads of what is read once, first out of L2. The launch before on the stream
+// may have written it while this grid's blocks were already there, so loads here
+// are coherent ones and stay below layer_begin's wait: volatile, with a memory
+// clobber (or plain C++ loads), never ld.global.nc, whose contents must not
+// change while a kernel runs.
+__device__ __forceinline__ float load_once(const float* p) {
+    float v;
+    asm volatile("ld.global.cs.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 load_once(const float4* p) {
+    float4 v;
+    asm volatile("ld.global.cs.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+    uint4 v;
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ int2 load_once(const int2* p) {
+    int2 v;
+    asm volatile("ld.global.cs.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ int load_once(const int8_t* p) {
+    int v;
+    asm volatile("ld.global.cs.s8 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+// Single elements where `there`; else v stays as it is. Predicates, not branches: loads in stretches of code of their own
+// do not overlap (rows of bfloat16 off 16 bytes took 2 to 4 times as long). A bfloat16's bits go to a register of their
+// own: a 16-bit variable shares one with another, and waits for that one's load.
+__device__ __forceinline__ void load_once(float& v, const float* p, bool there) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.cs.f32 %0, [%1];\n\t}"
+                 : "+f"(v)
+                 : "l"(p), "r"(there ? 1u : 0u)
+                 : "memory");
+}
+__device__ __forceinline__ void load_once(uint32_t& v, const __nv_bfloat16* p, bool there) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.cs.u16 %0, [%1];\n\t}"
+                 : "+r"(v)
+                 : "l"(p), "r"(there ? 1u : 0u)
+                 : "memory");
+}
+
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <typename T>
@@ -126,14 +172,14 @@ __device__ __forceinline__ int code_of(float x, float inverse) {
     return max(-127, min(127, __float2int_rn(x * inverse)));
 }
 // V neighbouring elements of a row as they lie in memory: 16 bytes' worth,
-// or one.
+// or one, which is loaded where it is there.
 template <typename T, int V>
 struct Piece;
 template <>
 struct Piece<float, 4> {
     float4 v;
     __device__ __forceinline__ float get(int e) const { return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w; }
-    __device__ __forceinline__ void load(const float* p) { v = __ldcs(reinterpret_cast<const float4*>(p)); }
+    __device__ __forceinline__ void load(const float* p) { v = load_once(reinterpret_cast<const float4*>(p)); }
 };
 template <>
 struct Piece<__nv_bfloat16, 8> {
@@ -142,20 +188,19 @@ struct Piece<__nv_bfloat16, 8> {
         const uint32_t u = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
         return __uint_as_float(e % 2 ? u & 0xffff0000u : u << 16);
     }
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = load_once(reinterpret_cast<const uint4*>(p)); }
 };
 template <>
 struct Piece<float, 1> {
     float v;
     __device__ __forceinline__ float get(int) const { return v; }
-    __device__ __forceinline__ void load(const float* p) { v = __ldcs(p); }
+    __device__ __forceinline__ void load(const float* p, bool there) { load_once(v, p, there); }
 };
 template <>
 struct Piece<__nv_bfloat16, 1> {
     uint32_t v;
     __device__ __forceinline__ float get(int) const { return __uint_as_float(v << 16); }
-    // into a register of its own: a 16-bit variable shares one with another, and waits for that one's load
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { asm("ld.global.cs.u16 %0, [%1];" : "=r"(v) : "l"(p)); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool there) { load_once(v, p, there); }
 };
 
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {

@@ -65,7 +65,7 @@ norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weig
 #pragma unroll
     for (int k = 0; k < E; ++k) {
         const int d = (k / V * TPR + t) * V + k % V;
-        wt[k] = d < D ? __ldg(weight + w * weight_worker + d) : 0.f;
+        wt[k] = d < D ? weight[w * weight_worker + d] : 0.f;
     }
     int turn = 0;
     // a warp's rows leave the loop together
@@ -82,9 +82,14 @@ norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weig
             for (int j = 0; j < J; ++j) {
                 const int d = (j * TPR + t) * V;
                 a[j] = b[j] = Piece<T, V>{};
-                if (there && d < D) {
-                    a[j].load(xr + d);
-                    if (residual.p != nullptr) b[j].load(rr + d);
+                if constexpr (V > 1) {
+                    if (there && d < D) {
+                        a[j].load(xr + d);
+                        if (residual.p != nullptr) b[j].load(rr + d);
+                    }
+                } else {
+                    a[j].load(xr + d, there && d < D);
+                    b[j].load(rr + d, there && d < D && residual.p != nullptr);
                 }
             }
 #pragma unroll
@@ -156,7 +161,7 @@ norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_
     const int64_t w = blockIdx.y;
     const auto weight_at = [&](int k) {
         const int d = (k / V * TPR + t) * V + k % V;
-        return d < D ? __ldg(weight + w * weight_worker + d) : 0.f;
+        return d < D ? weight[w * weight_worker + d] : 0.f;
     };
     float wt[KEEP ? E : 1], sums[E];
 #pragma unroll
@@ -173,10 +178,17 @@ norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_
         for (int j = 0; j < J; ++j) {
             const int d = (j * TPR + t) * V;
             g[j] = r[j] = through[j] = Piece<T, V>{};
-            if (m < M && d < D) {
-                g[j].load(gr + d);
-                r[j].load(sr + d);
-                if (KEEP && ds.p != nullptr) through[j].load(dr + d);
+            const bool there = m < M && d < D;
+            if constexpr (V > 1) {
+                if (there) {
+                    g[j].load(gr + d);
+                    r[j].load(sr + d);
+                    if (KEEP && ds.p != nullptr) through[j].load(dr + d);
+                }
+            } else {
+                g[j].load(gr + d, there);
+                r[j].load(sr + d, there);
+                if (KEEP) through[j].load(dr + d, there && ds.p != nullptr);
             }
         }
     };
@@ -205,7 +217,11 @@ norm_backward_kernel(NormIn dy, NormIn s, NormIn ds, const float* weight, int64_
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int d = (j * TPR + t) * V;
-            if (!KEEP && ds.p != nullptr && d < D) through0[j].load(row_of(ds, m) + d);
+            if constexpr (!KEEP && V > 1) {
+                if (d < D && ds.p != nullptr) through0[j].load(row_of(ds, m) + d);
+            } else if constexpr (!KEEP) {
+                through0[j].load(row_of(ds, m) + d, d < D && ds.p != nullptr);
+            }
             float o[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -250,7 +266,7 @@ norm_weight_kernel(const float* parts, int count, int D, G* dweight, int64_t dwe
     float sum = 0.f;
     if (d < D)
 #pragma unroll 4
-        for (int i = l; i < count; i += kLines) sum += __ldcs(parts + (w * count + i) * D + d);
+        for (int i = l; i < count; i += kLines) sum += load_once(parts + (w * count + i) * D + d);
     line[l][c] = sum;
     __syncthreads();
     if (l == 0 && d < D) {

@@ -336,9 +336,9 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map, WeightGradient p
         const auto load = [&]() {
             Codes c{};
             if (left > 0) {
-                c.half[0] = __ldg(next_codes);
-                c.half[1] = __ldg(next_codes + other);
-                c.byte = __ldg(next_byte);
+                c.half[0] = *next_codes;
+                c.half[1] = next_codes[other];
+                c.byte = *next_byte;
             }
             left -= kGroups * kStep;
             next_codes += down * (kBlock8 / 16);
@@ -415,7 +415,7 @@ align_kernel(const T* dy, int64_t dy_worker, int64_t dy_row, int64_t M, int64_t 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int o = k * 8 + e * 2;
-                    const __nv_bfloat162 both = __floats2bfloat162_rn(o < O ? __ldcs(p + o) : 0.f, o + 1 < O ? __ldcs(p + o + 1) : 0.f);
+                    const __nv_bfloat162 both = __floats2bfloat162_rn(o < O ? load_once(p + o) : 0.f, o + 1 < O ? load_once(p + o + 1) : 0.f);
                     v[e] = *reinterpret_cast<const uint32_t*>(&both);
                 }
                 to[k] = make_uint4(v[0], v[1], v[2], v[3]);
@@ -429,7 +429,7 @@ align_kernel(const T* dy, int64_t dy_worker, int64_t dy_row, int64_t M, int64_t 
             for (int k = lane; k < pieces; k += 32) {
                 uint32_t a[5];
 #pragma unroll
-                for (int e = 0; e < 5; ++e) a[e] = k * 4 + e < held ? __ldg(q + k * 4 + e) : 0u;
+                for (int e = 0; e < 5; ++e) a[e] = k * 4 + e < held ? q[k * 4 + e] : 0u;
                 to[k] = make_uint4(__byte_perm(a[0], a[1], take), __byte_perm(a[1], a[2], take), __byte_perm(a[2], a[3], take),
                                    __byte_perm(a[3], a[4], take));
             }
@@ -444,7 +444,7 @@ sum_parts_kernel(const float* parts, int splits, int64_t per_worker, int64_t all
     layer_begin();
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
         float s = 0.f;
-        for (int k = 0; k < splits; ++k) s += __ldcs(parts + k * all + at);
+        for (int k = 0; k < splits; ++k) s += load_once(parts + k * all + at);
         const int64_t w = at / per_worker;
         dW[w * dW_worker + (at - w * per_worker)] = from_float<G>(s);
     }

@@ -147,3 +147,48 @@ def test_weight_gradient_is_nan_where_a_wait_ran_out():
         assert r["before"] == 0 and r["finite"], name
         assert r["ran_out"] > 0 and r["all_nan"] and r["beside"], name
         assert r["same_after"] and r["after"] == 0, name
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [384, 771])
+def test_what_one_launch_writes_the_next_one_reads(D, dtype):
+    """Chains of calls over the same few buffers, whose contents change from turn to turn, with nothing waited for: each call
+    reads what the launch just before it wrote. The same chains with a wait after every call give the same bits."""
+    W, M = 4, 700
+    gen = gpu_rng(D)
+    turns = [[torch.randn(W, M, D, generator=gen, device="cuda").to(dtype) for _ in range(2)] for _ in range(3)]
+    first = 1 + 0.1 * torch.randn(W, D, generator=gen, device="cuda")
+
+    def chain(wait):
+        def done(x):
+            if wait:
+                torch.cuda.synchronize()
+            return x
+
+        results = []
+        w = torch.empty_like(first)
+        w.copy_(first)
+        for i in range(24):
+            x, dy = turns[i % 3]
+            # the weight is what the backward pass of the turn before wrote, the last thing on the stream
+            y, s, saved = done(layers.add_rmsnorm(x, w, dy, checkpoint=True))
+            values = done(layers.restore(saved))
+            dW = done(layers.weight_gradient(dy, saved))
+            held, _ = done(layers.checkpoint(s))
+            dW2 = done(layers.weight_gradient(dy, held, dtype=BF16))
+            h, last, carry = done(layers.gated_recurrence(s, x, w))
+            dg, dv, dh0 = done(layers.gated_recurrence_backward(h, s, x, carry, last))
+            state = last.clone()
+            one = done(layers.gated_recurrence_step(dg[:, 0], dv[:, 0], state))
+            dx, _ = done(layers.add_rmsnorm_backward(dv, dg, w, dx_before(results), dweight=w))
+            results.append([y, values, dW, dW2, h, dg, one, dx, w.clone()])
+            w.mul_(1e-2).add_(1.0) if i % 2 else done(layers.add_rmsnorm_backward(dx, dx, first, dweight=w))
+        torch.cuda.synchronize()
+        return results
+
+    def dx_before(results):
+        return results[-1][7] if results else None
+
+    got, want = chain(False), chain(True)
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert all(torch.equal(p.nan_to_num(7.0), q.nan_to_num(7.0)) for p, q in zip(a, b)), i

@@ -1,5 +1,8 @@
 """Host-side refusals of the layers that need no GPU: outputs that overlap
 themselves."""
+import re
+from pathlib import Path
+
 import pytest
 import torch
 
@@ -52,3 +55,21 @@ def test_python_refuses_overlapping_outputs():
     for shape, strides in [((2, 5, 8), (40, 8, 1)), ((2, 5, 8), (8, 16, 1)), ((2, 5, 8), (100, 11, 1)), ((1, 5, 8), (0, 8, 1)),
                            ((5, 1, 8), (8, 0, 1)), ((1, 1, 8), (0, 0, 1)), ((0, 5, 8), (0, 0, 1)), ((5, 0, 8), (0, 8, 1)), ((2, 5, 8), (32 + 8, 8, 1))]:
         layers._rows_apart(long.as_strided(shape, strides), "out")
+
+
+CSRC = Path(layers.__file__).resolve().parent / "csrc"
+
+
+@pytest.mark.parametrize("name", ["cpdp_layers.cuh", "cpdp_norm.cu", "cpdp_checkpoint.cu", "cpdp_weight_gradient.cu", "cpdp_recurrence.cu"])
+def test_loads_stay_below_the_wait_for_the_launch_before(name):
+    """Under programmatic dependent launch a block may be there while the launch before still writes what it will read. Loads
+    that a compiler may move or merge (the read-only and hinted builtins, assembly that is not volatile or does not clobber
+    memory) or that need not be coherent are not used."""
+    text = re.sub(r"//[^\n]*", "", (CSRC / name).read_text())
+    assert not re.findall(r"__ld(?:g|cs|cg|ca|lu|cv)\b", text)
+    assert "__restrict__" not in text
+    statements = re.findall(r"\basm\b(\s*volatile)?\s*\((.*?)\)\s*;", text, flags=re.S)
+    loads = [(volatile, body) for volatile, body in statements if re.search(r"\b(?:ld|st|red|atom|cp)\.[\w.:]*(?:global|shared)", body)]
+    assert all(volatile and '"memory"' in body and ".nc" not in body for volatile, body in loads), loads
+    if name == "cpdp_layers.cuh":
+        assert len(loads) >= 6
