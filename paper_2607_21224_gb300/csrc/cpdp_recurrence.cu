@@ -56,24 +56,47 @@ __device__ __forceinline__ Pair add2(Pair a, Pair b) {
     return d;
 }
 // a = sigmoid(x) and 1 - a, neither formed as a difference from 1. With
-// t = e^-|x| in [0, 1] they are 1 / (1 + t) and t / (1 + t). The power is 2^p of
-// the rounded product p = |x| log2(e), so t's relative error is some ulps and
-// grows with |x| (1e-6 at 16, where t itself is 1e-7). The scans are bound by
-// the instructions that they issue: exact range reduction and division, with
-// their cases for tiny numbers, took 2.5 times as many.
-__device__ __forceinline__ float power_of_minus(float x) {
+// t = e^-|x| in [0, 1] they are 1 / (1 + t) and t / (1 + t); below 1e-38 t is 0.
+// The power is 2^-p of the rounded product p = |x| log2(e). What the rounding
+// left out makes t's relative error grow with |x| (1e-6 at 16, 4e-6 at 80). For
+// float32 gates t is multiplied by e^r, r = p ln 2 - |x|, of which 1 + r is
+// enough (1 to 5 % of a scan's time). bfloat16 gates, whose own spacing is 30,000
+// times that, go without (it took 3 to 15 %). The scans are bound by the
+// instructions that they issue: exact range reduction and division, with their
+// cases for tiny numbers, took 2.5 times as many.
+constexpr float kLog2eHigh = 1.44269502162933349609375f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147180559945309f;  // High: the float32
+__device__ __forceinline__ float power_of_minus(float p) {
     float t;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(-1.44269504f * fabsf(x)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(-p));
     return t;
+}
+__device__ __forceinline__ float size_of(float x) {  // beyond 128 t is 0 all the same, and r stays finite; NaN stays NaN
+    float m;
+    asm("min.NaN.f32 %0, %1, 0f43000000;" : "=f"(m) : "f"(fabsf(x)));
+    return m;
+}
+__device__ __forceinline__ Pair twice(float x) { return pair(x, x); }
+template <typename T>
+__device__ __forceinline__ Pair exp_of_minus(float2 x) {
+    if constexpr (sizeof(T) == 2) {
+        return pair(power_of_minus(kLog2eHigh * fabsf(x.x)), power_of_minus(kLog2eHigh * fabsf(x.y)));
+    } else {
+        const Pair m = pair(size_of(x.x), size_of(x.y)), p = mul2(m, twice(kLog2eHigh));
+        const Pair t = pair(power_of_minus(floats(p).x), power_of_minus(floats(p).y));
+        const Pair rounded = fma2(m, twice(-kLog2eHigh), p);  // exact
+        return fma2(t, fma2(rounded, twice(kLn2), mul2(m, twice(-kLog2eLow * kLn2))), t);
+    }
 }
 __device__ __forceinline__ float reciprocal(float x) {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// T: the gates' type.
+template <typename T>
 __device__ __forceinline__ void gate_of(Pair gates, Pair& a, Pair& rest) {
     const float2 x = floats(gates);
-    const Pair t = pair(power_of_minus(x.x), power_of_minus(x.y));
+    const Pair t = exp_of_minus<T>(x);
     const float2 s = floats(add2(t, kOnes)), r = make_float2(reciprocal(s.x), reciprocal(s.y)), q = floats(mul2(t, pair(r.x, r.y)));
     a = pair(x.x >= 0.f ? r.x : q.x, x.y >= 0.f ? r.y : q.y);
     rest = pair(x.x >= 0.f ? q.x : r.x, x.y >= 0.f ? q.y : r.y);
@@ -304,7 +327,7 @@ recurrence_kernel(SeqIn gate, SeqIn value, int steps, int D, const float* h0, co
             for (int r = 0; r < R; ++r) {
                 Map one;
                 Pair rest;
-                gate_of(gs.get(r), one.a, rest);
+                gate_of<T>(gs.get(r), one.a, rest);
                 one.b = mul2(rest, vs.get(r));
                 if (!FULL && r >= rows) one = kSame;
                 if constexpr (MAPS) {
@@ -398,7 +421,7 @@ recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int steps, int D, 
 #pragma unroll
                 for (int r = R - 1; r >= 0; --r) {
                     Pair a, rest;
-                    gate_of(gs.get(r), a, rest);
+                    gate_of<T>(gs.get(r), a, rest);
                     if (!FULL && r >= rows) a = kOnes;  // dh is 0 there
                     m = Map{mul2(a, m.a), mul2(a, add2(os.get(r), m.b))};
                 }
@@ -407,7 +430,7 @@ recurrence_backward_kernel(SeqIn dh, SeqIn gate, SeqIn value, int steps, int D, 
                 Pair a[R], rest[R], away[R];  // away: (h_(t-1) - v_t) a_t
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    gate_of(gs.get(r), a[r], rest[r]);
+                    gate_of<T>(gs.get(r), a[r], rest[r]);
                     if (!FULL && r >= rows) a[r] = kOnes, rest[r] = kZeros;
                     const Pair vr = vs.get(r);
                     away[r] = mul2(fma2(vr, kMinusOnes, s), a[r]);
@@ -448,7 +471,7 @@ recurrence_step_kernel(const T* gate, int64_t gate_seq, const T* value, int64_t 
     const int d = blockIdx.x % per * kThreads + threadIdx.x;
     if (d >= D) return;
     Pair a, rest;
-    gate_of(pair(to_float(gate[b * gate_seq + d]), 0.f), a, rest);
+    gate_of<T>(pair(to_float(gate[b * gate_seq + d]), 0.f), a, rest);
     const float next = fmaf(floats(a).x, state[b * D + d], floats(rest).x * to_float(value[b * value_seq + d]));
     state[b * D + d] = next;
     h[b * D + d] = from_float<T>(next);

@@ -192,3 +192,43 @@ def test_what_one_launch_writes_the_next_one_reads(D, dtype):
     got, want = chain(False), chain(True)
     for i, (a, b) in enumerate(zip(got, want)):
         assert all(torch.equal(p.nan_to_num(7.0), q.nan_to_num(7.0)) for p, q in zip(a, b)), i
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gates_far_from_zero_keep_their_precision(dtype):
+    """a and 1 - a at every gate: one step from a state of 0 and of 1, and its gradients. float32 gates have 16 roundings to
+    spare, as in ref.STEP; with bfloat16 gates the power's exponent is a product that is rounded once, with a constant that is:
+    2 U32 |x| more."""
+    gate = torch.cat([torch.linspace(-86, 86, 4097), torch.tensor([0.0, 16.0, -16.0, 1e-30, -1e-30])]).to(dtype).cuda()[None, None]
+    D = gate.shape[2]
+    one, zero = torch.ones(1, 1, D, dtype=dtype, device="cuda"), torch.zeros(1, 1, D, dtype=dtype, device="cuda")
+    state = torch.ones(1, D, device="cuda")
+    x = gate[0].double()
+    a, rest = 1 / (1 + torch.exp(-x)), 1 / (1 + torch.exp(x))
+    room = ref.STEP + (0 if dtype == F32 else 2 * ref.U32 * x.abs())
+    for value, start, want in ((one, None, rest), (zero, state, a)):
+        h, last, carry = layers.gated_recurrence(gate, value, start)
+        near(last, want, room * want)
+        near(h[0], want, room * want)
+        step = torch.zeros(1, D, device="cuda") if start is None else start.clone()
+        near(layers.gated_recurrence_step(gate[0], value[0], step), want, room * want)
+        near(step, want, room * want)
+    dgate, dvalue, dh0 = layers.gated_recurrence_backward(one, gate, zero, carry)
+    near(dvalue[0], rest, room * rest)
+    near(dh0, a, room * a)
+    near(dgate[0], a * rest, 2 * room * a * rest)
+
+
+def test_gates_that_hold_a_state_for_long():
+    """Gates of 14 to 18 over 20,000 steps: what leaks in is 1 - a, 1e-7 a step, and its error stays that of the roundings."""
+    gen = gpu_rng(3)
+    T, D = 20000, 64
+    gate = 14 + 4 * torch.rand(1, T, D, generator=gen, device="cuda")
+    value = torch.ones(1, T, D, device="cuda")
+    h, last, _ = layers.gated_recurrence(gate, value)
+    rest = 1 / (1 + torch.exp(gate.double()))
+    want = torch.zeros(D, dtype=torch.float64, device="cuda")
+    for t in range(T):
+        want = want + rest[0, t] * (1 - want)
+    # each step adds 1e-7 with 16 roundings of its own and rounds the state, whose own error is at most U32 of it a step
+    near(last[0], want, (ref.STEP + T * ref.U32 / 2) * want)
