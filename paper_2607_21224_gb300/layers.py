@@ -21,9 +21,10 @@ gradients are written into slices of the [W][N] gradient buffer::
 
 Calls run on the current stream of their tensors' device (or on ``stream``) and
 return without waiting. Outputs are allocated by torch; nothing is kept between
-calls. There is no autograd and no CPU implementation. A tensor that a call
-cannot take is refused with ValueError or TypeError, anything that the library
-refuses with ``CPDPError``.
+calls. There is no autograd (tensors that require a gradient are refused where
+gradients are recorded; inside an autograd.Function they are not) and no CPU
+implementation. A tensor that a call cannot take is refused with ValueError or
+TypeError, anything that the library refuses with ``CPDPError``.
 """
 from __future__ import annotations
 
@@ -104,6 +105,13 @@ def _stream(index: int) -> int:
     if _raw_stream is not None:
         return _raw_stream(index)
     return torch.cuda.current_stream(index).cuda_stream
+
+
+def _no_autograd(**tensors) -> None:
+    """Refuses tensors whose gradient would be lost without a word."""
+    for name, t in tensors.items():
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, which these calls do not record: detach it, or call under torch.no_grad()")
 
 
 def _elsewhere(device: torch.device, stream) -> bool:
@@ -206,7 +214,8 @@ def add_rmsnorm(x, weight, residual=None, *, eps: float = 1e-6, checkpoint: bool
     # one test where all is well: a decoding step costs what Python does around it
     if not (stream is None and code is not None and x.is_cuda and device.index == _current_device() and len(shape) == 3 and max(shape) <= MAX_SIZE
             and weight.shape == (shape[0], shape[2]) and weight.dtype is _F32 and weight.device == device
-            and xs[-1] == 1 == ws[-1]):
+            and xs[-1] == 1 == ws[-1] and not (x.requires_grad or weight.requires_grad or residual is not None and residual.requires_grad)):
+        _no_autograd(x=x, weight=weight, residual=residual)
         if _elsewhere(_cuda(x, "x"), stream):
             with _there(device, stream):
                 return add_rmsnorm(x, weight, residual, eps=eps, checkpoint=checkpoint)
@@ -270,6 +279,7 @@ def add_rmsnorm_backward(dy, s, weight, ds=None, *, eps: float = 1e-6, dweight=N
         dx, dw = add_rmsnorm_backward(dy[None], s[None], weight[None], None if ds is None else ds[None], eps=eps,
                                       dweight=None if dweight is None else dweight[None], dtype=dtype, stream=stream)
         return dx[0], dw[0]
+    _no_autograd(dy=dy, s=s, weight=weight, ds=ds, dweight=dweight)
     device = _cuda(s, "s")
     if _elsewhere(device, stream):
         with _there(device, stream):
@@ -296,6 +306,7 @@ def checkpoint(x, *, values: bool = True, stream=None):
     if x.dim() == 2:
         saved, held = checkpoint(x[None], values=values, stream=stream)
         return saved, held[0] if values else None
+    _no_autograd(x=x)
     device = _cuda(x, "x")
     if _elsewhere(device, stream):
         with _there(device, stream):
@@ -346,6 +357,7 @@ def weight_gradient(dy, saved: Checkpoint, *, out=None, dtype=torch.float32, str
     sums are float32."""
     if dy.dim() == 2:
         return weight_gradient(dy[None], saved, out=None if out is None else out[None], dtype=dtype, stream=stream)[0]
+    _no_autograd(dy=dy, out=out)
     W, M, D = _saved(saved)
     device = saved.codes.device
     if _elsewhere(device, stream):
@@ -380,6 +392,7 @@ def gated_recurrence(gate, value, h0=None, lengths=None, *, carry: bool = True, 
     (h, h_last, carry): h (B, T, D) of gate's type, h_last float32 (B, D), and
     the states at every CARRY_STEPS steps, float32, which the backward pass
     starts from (carry=False: None)."""
+    _no_autograd(gate=gate, value=value, h0=h0)
     device = _cuda(gate, "gate")
     if _elsewhere(device, stream):
         with _there(device, stream):
@@ -404,6 +417,7 @@ def gated_recurrence_backward(dh, gate, value, carry, dh_last=None, lengths=None
     and dh_last float32 (B, D) or None. dgate and dvalue are the halves of one
     (B, T, 2 D) tensor, ``out`` where given (contiguous along its last axis):
     the gradient of one product that made gate and value."""
+    _no_autograd(dh=dh, gate=gate, value=value, carry=carry, dh_last=dh_last, out=out)
     device = _cuda(gate, "gate")
     if _elsewhere(device, stream):
         with _there(device, stream):
@@ -436,7 +450,9 @@ def gated_recurrence_step(gate, value, state, *, stream=None):
     # one test where all is well: a decoding step costs what Python does around it
     if not (stream is None and code is not None and gate.is_cuda and device.index == _current_device() and len(shape) == 2
             and value.shape == shape == state.shape and max(shape) <= MAX_SIZE and value.dtype is dtype and state.dtype is _F32
-            and value.device == device == state.device and gs[-1] == 1 == vs[-1] and state_strides == (shape[1], 1)):
+            and value.device == device == state.device and gs[-1] == 1 == vs[-1] and state_strides == (shape[1], 1)
+            and not (gate.requires_grad or value.requires_grad or state.requires_grad)):
+        _no_autograd(gate=gate, value=value, state=state)
         if _elsewhere(_cuda(gate, "gate"), stream):
             with _there(device, stream):
                 return gated_recurrence_step(gate, value, state)

@@ -232,3 +232,27 @@ def test_gates_that_hold_a_state_for_long():
         want = want + rest[0, t] * (1 - want)
     # each step adds 1e-7 with 16 roundings of its own and rounds the state, whose own error is at most U32 of it a step
     near(last[0], want, (ref.STEP + T * ref.U32 / 2) * want)
+
+
+def test_calls_inside_an_autograd_function():
+    """Gradients are not recorded inside one, so tensors that require them are taken, and the gradients arrive."""
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w):
+            ctx.save_for_backward(x, w)
+            return layers.add_rmsnorm(x, w)[0]
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, w = ctx.saved_tensors
+            return layers.add_rmsnorm_backward(dy.contiguous(), x, w)
+
+    gen = gpu_rng(1)
+    x, dy = (torch.randn(2, 9, 96, generator=gen, device="cuda") for _ in range(2))
+    w = torch.rand(2, 96, generator=gen, device="cuda")
+    want = layers.add_rmsnorm_backward(dy, x, w)
+    x.requires_grad_(), w.requires_grad_()
+    Norm.apply(x, w).backward(dy)
+    assert torch.equal(x.grad, want[0]) and torch.equal(w.grad, want[1])
+    with pytest.raises(ValueError, match="requires a gradient"):
+        layers.add_rmsnorm(x, w)

@@ -1,5 +1,6 @@
-"""Host-side refusals of the layers that need no GPU: outputs that overlap
-themselves."""
+"""Host-side tests of the layers that need no GPU: refusals of outputs that
+overlap themselves and of tensors that require gradients, and how the kernels
+load."""
 import re
 from pathlib import Path
 
@@ -73,3 +74,29 @@ def test_loads_stay_below_the_wait_for_the_launch_before(name):
     assert all(volatile and '"memory"' in body and ".nc" not in body for volatile, body in loads), loads
     if name == "cpdp_layers.cuh":
         assert len(loads) >= 6
+
+
+def test_tensors_that_require_a_gradient_are_refused():
+    """Their gradient would be lost without a word. Under no_grad, as inside an autograd.Function, they are taken (and refused
+    here for being on the CPU)."""
+    x, w = torch.zeros(2, 3, 32), torch.ones(2, 32)
+    saved = layers.Checkpoint(torch.zeros(2, 3, 32, dtype=torch.int8), torch.zeros(2, 3, 1, dtype=torch.uint8), 32)
+    calls = {"add_rmsnorm": [x, w, x.clone()], "add_rmsnorm_backward": [x, x.clone(), w, x.clone()], "checkpoint": [x],
+             "weight_gradient": [x, saved], "gated_recurrence": [x, x.clone(), w], "gated_recurrence_backward": [x, x.clone(), x.clone(), w, w.clone()],
+             "gated_recurrence_step": [w, w.clone(), w.clone()]}
+    for name, arguments in calls.items():
+        for i, t in enumerate(arguments):
+            if not isinstance(t, torch.Tensor):
+                continue
+            given = list(arguments)
+            given[i] = t.clone().requires_grad_()
+            with pytest.raises(ValueError, match="requires a gradient"):
+                getattr(layers, name)(*given)
+            with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):
+                getattr(layers, name)(*given)
+    for name, arguments, key, out in [("add_rmsnorm_backward", [x, x, w], "dweight", w), ("weight_gradient", [x, saved], "out", torch.zeros(2, 32, 32)),
+                                      ("gated_recurrence_backward", [x, x, x, w], "out", torch.zeros(2, 3, 64))]:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            getattr(layers, name)(*arguments, **{key: out.clone().requires_grad_()})
+    with pytest.raises(ValueError, match="requires a gradient"):  # one model's
+        layers.add_rmsnorm(x[0], w[0].clone().requires_grad_())
