@@ -124,7 +124,11 @@ def _there(device: torch.device, stream):
     launched."""
     if stream is None:
         return torch.cuda.device(device)
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device) if isinstance(stream, int) else stream)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device)
+    elif stream.device != device:
+        raise ValueError(f"the stream is one of {stream.device}, the tensors are on {device}")
+    return torch.cuda.stream(stream)
 
 
 def _input(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype, device: torch.device) -> tuple:

@@ -100,3 +100,12 @@ def test_tensors_that_require_a_gradient_are_refused():
             getattr(layers, name)(*arguments, **{key: out.clone().requires_grad_()})
     with pytest.raises(ValueError, match="requires a gradient"):  # one model's
         layers.add_rmsnorm(x[0], w[0].clone().requires_grad_())
+
+
+def test_a_stream_of_another_device_is_refused():
+    """The call would have run on the current stream of its tensors' device instead."""
+    class Stream:
+        device = torch.device("cuda", 1)
+
+    with pytest.raises(ValueError, match="stream"):
+        layers._there(torch.device("cuda", 0), Stream())
