@@ -256,3 +256,107 @@ def test_calls_inside_an_autograd_function():
     assert torch.equal(x.grad, want[0]) and torch.equal(w.grad, want[1])
     with pytest.raises(ValueError, match="requires a gradient"):
         layers.add_rmsnorm(x, w)
+
+
+class Guarded:
+    """Device memory for an output, `shift` bytes past an allocation's start, with 4 KB around it that must not change."""
+
+    def __init__(self, nbytes, shift=0):
+        self.first, self.nbytes = 4096 + shift, nbytes
+        self.all = torch.full((2 * 4096 + shift + nbytes,), 0xA5, dtype=torch.uint8, device="cuda")
+        self.ptr = self.all.data_ptr() + self.first
+
+    def whole(self):
+        return bool((self.all[:self.first] == 0xA5).all() and (self.all[self.first + self.nbytes:] == 0xA5).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shift", [0, 4])
+@pytest.mark.parametrize("W,M,D", [(1, 1, 1), (3, 5, 33), (2, 7, 64), (1, 3, 129), (2, 33, 384), (1, 17, 771), (3, 2, 1024), (1, 5, 2056), (2, 3, 4099),
+                                   (1, 2, 8200), (1, 1, 16384)])
+def test_nothing_beside_an_output_is_written(W, M, D, shift, dtype):
+    """Every output of every call, from C, at sizes that fill their last tile and at others, aligned and not."""
+    lib, gen = layers.lib(), gpu_rng(D)
+    e, code, n = (4, 0, W * M * D) if dtype == F32 else (2, 1, W * M * D)
+    blocks = -(-D // 32)
+    x, r, dy = (torch.randn(n, generator=gen, device="cuda").to(dtype) for _ in range(3))
+    w = torch.rand(W, D, generator=gen, device="cuda")
+    s3 = [M * D, D]
+    stream = torch.cuda.current_stream().cuda_stream
+    made = []
+
+    def out(nbytes, at=shift):
+        made.append(Guarded(nbytes, at))
+        return made[-1].ptr
+
+    def work(nbytes):
+        return out(nbytes, 0) if nbytes else None
+
+    y, s = out(n * e), out(n * e)
+    assert lib.cpdp_add_rmsnorm(x.data_ptr(), *s3, r.data_ptr(), *s3, w.data_ptr(), D, code, W, M, D, 1e-6, y, s, None, None, stream) == 0
+    codes, exponents = out(W * M * blocks * 32, 0), out(W * M * blocks)
+    assert lib.cpdp_add_rmsnorm(x.data_ptr(), *s3, None, 0, 0, w.data_ptr(), D, code, W, M, D, 1e-6, out(n * 2), None, codes, exponents, stream) == 0
+    assert lib.cpdp_restore(codes, exponents, W, M, D, out(n * 2), stream) == 0
+    size = lib.cpdp_add_rmsnorm_backward_workspace(W, M, D)
+    assert lib.cpdp_add_rmsnorm_backward(dy.data_ptr(), *s3, x.data_ptr(), *s3, r.data_ptr(), *s3, w.data_ptr(), D, code, W, M, D, 1e-6, out(n * e),
+                                         out(W * D * e), D, code, work(size), size, stream) == 0
+    codes, exponents = out(W * M * blocks * 32, 0), out(W * M * blocks)
+    assert lib.cpdp_checkpoint(x.data_ptr(), *s3, code, W, M, D, codes, exponents, out(n * 2), stream) == 0
+    O = 300 if D < 100 else 7
+    g = torch.randn(W * M * O, generator=gen, device="cuda").to(dtype)
+    size = lib.cpdp_weight_gradient_workspace(g.data_ptr(), M * O, O, code, W, M, O, D)
+    assert lib.cpdp_weight_gradient(g.data_ptr(), M * O, O, code, codes, exponents, W, M, O, D, out(W * O * D * e), O * D, code, work(size), size, stream) == 0
+    # W sequences of M steps
+    carry, size = out(W * -(-M // 16) * D * 4), lib.cpdp_gated_recurrence_workspace(W, M, D)
+    assert lib.cpdp_gated_recurrence(x.data_ptr(), *s3, r.data_ptr(), *s3, code, W, M, D, None, None, out(n * e), out(W * D * 4), carry, work(size), size,
+                                     stream) == 0
+    assert lib.cpdp_gated_recurrence_backward(dy.data_ptr(), *s3, x.data_ptr(), *s3, r.data_ptr(), *s3, code, W, M, D, carry, None, None, out(n * e),
+                                              out(n * e), *s3, out(W * D * 4), work(size), size, stream) == 0
+    state = Guarded(W * D * 4, shift)
+    state.all[state.first:state.first + state.nbytes] = 0
+    made.append(state)
+    assert lib.cpdp_gated_recurrence_step(x.data_ptr(), M * D, r.data_ptr(), M * D, code, W, D, state.ptr, out(W * D * e), stream) == 0
+    torch.cuda.synchronize()
+    assert [i for i, m in enumerate(made) if not m.whole()] == []
+
+
+@pytest.mark.parametrize("D", [8, 64, 200, 1000, 3000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_split_recurrences_repeat_themselves(D, dtype):
+    """Ragged sequences whose steps are split into none, a few and many segments: the same bits each time."""
+    gen = gpu_rng(D)
+    B, T = 3, 5000
+    gate, value, dh = (torch.randn(B, T, D, generator=gen, device="cuda").to(dtype) for _ in range(3))
+    h0 = torch.randn(B, D, generator=gen, device="cuda")
+    lengths = torch.tensor([T, 1234, 0], dtype=torch.int32, device="cuda")
+    first = None
+    for _ in range(4):
+        h, last, carry = layers.gated_recurrence(gate, value, h0, lengths)
+        got = (h, last, *layers.gated_recurrence_backward(dh, gate, value, carry, h0, lengths))
+        first = first or got
+        assert all(torch.equal(p, q) for p, q in zip(got, first))
+
+
+@pytest.mark.parametrize("T", [50, 5000])
+def test_recurrence_with_infinities(T):
+    """What is not finite by the formulas is not finite, nothing else is touched: an infinite state, value and gradient in
+    channels of their own."""
+    gen = gpu_rng(T)
+    B, D = 2, 40
+    gate, value, dh = (torch.randn(B, T, D, generator=gen, device="cuda") for _ in range(3))
+    h0 = torch.randn(B, D, generator=gen, device="cuda")
+    h0[0, 3] = float("inf")
+    value[0, T // 3, 7], value[1, T // 2, 8] = float("-inf"), float("nan")
+    dh[0, T // 2, 11], gate[1, T // 4, 12] = float("inf"), float("nan")
+    h, last, carry = layers.gated_recurrence(gate, value, h0)
+    bad = torch.zeros(B, T, D, dtype=torch.bool, device="cuda")
+    bad[0, :, 3] = True
+    bad[0, T // 3:, 7], bad[1, T // 2:, 8], bad[1, T // 4:, 12] = True, True, True
+    assert torch.equal(~torch.isfinite(h), bad) and torch.equal(~torch.isfinite(last), bad[:, -1])
+    dgate, dvalue, dh0 = layers.gated_recurrence_backward(dh, gate, value, carry)
+    back = torch.zeros_like(bad)
+    back[0, :T // 2 + 1, 11], back[1, :T // 4 + 1, 12] = True, True
+    assert torch.equal(~torch.isfinite(dvalue), back)
+    before = torch.cat([~torch.isfinite(h0)[:, None], bad[:, :-1]], 1)
+    assert torch.equal(~torch.isfinite(dgate), back | before | ~torch.isfinite(value))
+    assert torch.equal(~torch.isfinite(dh0), back[:, 0])
