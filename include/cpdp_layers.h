@@ -22,7 +22,9 @@
  *
  * Types. Activations are float32 or bfloat16 (cpdp_dtype); all arithmetic,
  * sums and states are float32, and an output is rounded once (to nearest even)
- * when it is stored. Infinities and NaN follow from the formulas. A row whose
+ * when it is stored. Infinities and NaN follow from the formulas, except that an
+ * infinite state or gradient of the recurrence may go on as NaN, where the steps
+ * of a long sequence are shared out. A row whose
  * sum of squares is above the float32 range (a root mean square above
  * 1.8e19 / sqrt(D)) has the scale k = 0 in the norm.
  *
@@ -89,7 +91,8 @@ cpdp_status cpdp_add_rmsnorm(const void *x, int64_t x_worker, int64_t x_row,
  *                counts as the identity.
  *   dx           [W][M][D] of dtype: the gradient of x, and of residual
  *   dweight      dweight_dtype, worker w's at dweight + w * dweight_worker;
- *                the order of its sums is fixed by the sizes
+ *                the order of its sums is fixed by the sizes and by whether
+ *                every row is one of whole 16-byte pieces
  */
 size_t cpdp_add_rmsnorm_backward_workspace(int W, int64_t M, int D);
 cpdp_status cpdp_add_rmsnorm_backward(const void *dy, int64_t dy_worker, int64_t dy_row,

@@ -21,7 +21,7 @@ DEPENDS = SOURCES + [CSRC / "cpdp_kernels.cuh", CSRC / "cpdp_shapes.cuh", CSRC /
                      CSRC / "cpdp_launch.cuh", CSRC / "cpdp_layers.cuh", INCLUDE / "cpdp.h",
                      INCLUDE / "cpdp_layers.h"]
 LIBRARY = PKG / "libcpdp.so"
-CHECKED_LIBRARY = PKG / "libcpdp_checked.so"  # debug build: kernels count out-of-range indices
+CHECKED_LIBRARY = PKG / "libcpdp_checked.so"  # debug build: the step and reconcile kernels count out-of-range indices
 BUILD_DIR = ROOT / "_build"
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
@@ -53,7 +53,8 @@ def build_library(force: bool = False, verbose: bool = False, checked: bool = Fa
     """Compile libcpdp.so if it is missing or older than its sources. The ptxas
     report (registers, spills, shared memory per kernel) goes to _build/ptxas.txt.
     With `checked`, the debug build libcpdp_checked.so instead (-DCPDP_CHECKED:
-    every kernel index is checked against its buffer's extent; report in
+    every index of the optimizer and reconcile kernels is checked against its
+    buffer's extent, and a weight gradient's copy can be left out; report in
     _build/ptxas_checked.txt)."""
     out = CHECKED_LIBRARY if checked else LIBRARY
     if not force and not is_stale(out):

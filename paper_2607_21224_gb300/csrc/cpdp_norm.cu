@@ -47,10 +47,10 @@ struct RowThreads {
 };
 
 // Forward: a row is read once into registers, its squares are summed, and it is
-// scaled and stored from there; the weights stay in registers from row to row.
-// Bound by DRAM where there are rows enough: 4 x 8,192 x 4,096 in bf16 with the
-// residual and the 8-bit output take 193 us, 6.3 TB/s; 8 x 3,152 x 384, with 5 rows
-// per warp, 22 us, 3.9; rows off 16 bytes, element by element, 2.2 to 4.
+// scaled and stored from there; the weights stay in registers through a block's
+// rows. Bound by DRAM where there are rows enough: 4 x 8,192 x 4,096 in bf16 with
+// the residual and the 8-bit output take 193 us, 6.3 TB/s; 8 x 3,152 x 384, with 2 or
+// 3 rows per warp, 22 us, 3.9; rows off 16 bytes, element by element, 1.9 to 4.3.
 template <typename T, int V, int TPR, int E, bool CHECKPOINT>
 __global__ void __launch_bounds__(RowThreads<TPR>::block)
 norm_forward_kernel(NormIn x, NormIn residual, const float* weight, int64_t weight_worker, int64_t M, int D, float eps, void* y,
@@ -292,7 +292,10 @@ cudaError_t with_shape(int D, bool wide, const F& f) {
 }
 static_assert(CPDP_NORM_MAX_FEATURES == 512 * 32, "the largest shape");
 
-// Blocks per worker: the rows' blocks, at most so many as run at once.
+// Blocks per worker: the rows' blocks, at most `resident` per SM between all
+// workers. The backward pass asks for what runs at once. The forward pass asks
+// for an SM's 2,048 threads, of which 56 to 163 registers a thread let a fifth to a
+// half run at once: a long grid takes 2 to 5 turns, each with the weights anew.
 unsigned blocks_for(int W, int64_t M, int rows, int resident) {
     const int64_t all = ceil_div(M, rows), most = ceil_div(int64_t(kSMs) * resident, W);
     return static_cast<unsigned>(all < most ? all : most);

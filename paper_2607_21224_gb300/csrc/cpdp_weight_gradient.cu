@@ -11,7 +11,7 @@ namespace {
 // dW = dy^T x^ is bound by shared memory: a step of 64 tokens takes the tensor
 // core 512 clocks, and 768 times 128 bytes move for it (48 KB of operands read,
 // 32 KB of dy and 16 KB of x^ written). 2 x 16,384 tokens, 2,048 -> 8,192: 809 us,
-// 1,359 TFLOP/s, to either type; 8 x 3,152, 384 -> 1,536 (144 blocks): 37 us.
+// 1,359 TFLOP/s, to either type; 8 x 3,152, 384 -> 1,536 (144 blocks): 35 us.
 //
 // One block computes 128 (i) x 256 (o) of dW, transposed on the tensor cores:
 // the accumulator's 128 lanes are neighbouring i, so that a warp's stores of
