@@ -9,6 +9,8 @@
  *               weight gradient that reads them: dW = dy^T x^
  *   recurrence  h_t = a_t h_(t-1) + (1 - a_t) v_t, a = sigmoid(gate); its
  *               backward pass, and its step for one token
+ *   loss        softmax cross entropy over a vocabulary from the activations
+ *               and the head's weight, without the logits; its backward pass
  *
  * Layout. Arrays [W][M][D] hold worker w's M tokens (rows) of D features.
  * Features are contiguous; inputs have a worker stride and a row stride, in
@@ -190,10 +192,56 @@ cpdp_status cpdp_gated_recurrence_step(const void *gate, int64_t gate_seq, const
                                        cpdp_dtype dtype, int B, int D, float *state, void *h, void *stream);
 
 /*
+ * cpdp_linear_cross_entropy — for each token, with the logits l = weight x
+ * over the vocabulary's V words,
+ *   lse = log(sum(exp(l))),  loss = lse - l[target]
+ *   x        [W][M][D] of dtype
+ *   weight   [W][V][D] of dtype, with a worker and a row stride
+ *   targets  int64 [W][M], contiguous. Where a target is negative the token is
+ *            ignored: its loss is 0 (lse is not). Where it is V or more its loss
+ *            is NaN.
+ *   loss, lse  float32 [W][M]
+ * The logits are float32 sums and stay on the chip. float32 operands are split
+ * into three bfloat16 parts each, and products below 2^-24 of the largest part's
+ * are left out; an infinite operand gives NaN there where the formula has an
+ * infinity. W * V and the elements of [W][M][V] are bounded as those of an array.
+ */
+size_t cpdp_linear_cross_entropy_workspace(const void *x, int64_t x_worker, int64_t x_row,
+                                           const void *weight, int64_t weight_worker, int64_t weight_row,
+                                           cpdp_dtype dtype, int W, int64_t M, int V, int D);
+cpdp_status cpdp_linear_cross_entropy(const void *x, int64_t x_worker, int64_t x_row,
+                                      const void *weight, int64_t weight_worker, int64_t weight_row,
+                                      const int64_t *targets, cpdp_dtype dtype, int W, int64_t M, int V, int D,
+                                      float *loss, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * cpdp_linear_cross_entropy_backward — with d = dloss (exp(l - lse) - onehot(target)),
+ *   dx = d weight,  dweight = d^T x
+ * The logits are made again, for a piece of the vocabulary at a time.
+ *   dloss    float32 [W][M]: the gradient of each token's loss
+ *   lse      what the forward pass gave
+ *   dx       [W][M][D] of dtype; 0 in the rows of ignored tokens, whose x, dloss
+ *            and lse reach nothing, infinite and NaN ones included
+ *   dweight  dweight_dtype, worker w's [V][D] at dweight + w * dweight_worker
+ * For bfloat16 operands d is rounded to bfloat16, relative to the worker's
+ * largest |dloss|; sums are float32, in an order fixed by the sizes, by whether
+ * weight is read in place (16-byte pieces), and by the type.
+ */
+size_t cpdp_linear_cross_entropy_backward_workspace(const void *x, int64_t x_worker, int64_t x_row,
+                                                    const void *weight, int64_t weight_worker, int64_t weight_row,
+                                                    cpdp_dtype dtype, int W, int64_t M, int V, int D);
+cpdp_status cpdp_linear_cross_entropy_backward(const float *dloss, const void *x, int64_t x_worker, int64_t x_row,
+                                               const void *weight, int64_t weight_worker, int64_t weight_row,
+                                               const int64_t *targets, const float *lse,
+                                               cpdp_dtype dtype, int W, int64_t M, int V, int D, void *dx,
+                                               void *dweight, int64_t dweight_worker, cpdp_dtype dweight_dtype,
+                                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * cpdp_layer_timeouts — the number of bounded waits that ran out since the last
- * call (0 expected): the weight gradient's warps wait for the slots of a ring,
- * for some seconds at most. A block in which one ran out writes NaN for all of
- * its tile of dW. Waits for the device.
+ * call (0 expected): the warps of the weight gradient and of the loss wait for
+ * the slots of a ring, for some seconds at most. A block in which one ran out
+ * writes NaN for all of its tiles. Waits for the device.
  */
 cpdp_status cpdp_layer_timeouts(int64_t *count);
 

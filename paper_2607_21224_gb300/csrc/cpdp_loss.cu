@@ -1,0 +1,770 @@
+// Softmax cross entropy over a vocabulary, from the activations and the head's
+// weight, without the logits in memory (include/cpdp_layers.h).
+#include <algorithm>
+
+#include "cpdp_tensor.cuh"
+
+namespace cpdp {
+namespace {
+
+// All of it is products on the tensor cores, C[a][b] = sum over k of A[a][k] B[b][k]:
+//   logits   a: tokens, b: words, k: features; an epilogue leaves each row's
+//            maximum and sum of exponentials over 128 words
+//   again    the same in the backward pass; the epilogue leaves
+//            d = r (exp(l - lse) - onehot), for a piece of the vocabulary
+//   dx       a: features, b: tokens, k: words of the piece
+//   dweight  a: features, b: words of the piece, k: tokens
+// One block per SM walks tiles of 128 (a) x 256 (b). k passes in steps of 64
+// through a ring of shared-memory slots, filled by tensor copies; one thread
+// issues the matrix instructions. Sums alternate between the halves of tensor
+// memory, so that a tile's epilogue runs while the next one is multiplied. The
+// accumulator's 128 lanes are a: a thread of the logits' epilogue holds 128 words
+// of one token, and the products that are written out have their contiguous
+// axis there, so that a warp's store is of 32 neighbours at any alignment.
+//
+// The tensor core cuts its float32 sums off where others round them, always
+// towards 0: chains of kChunk steps are summed at a time and added up, rounded
+// to nearest, in the epilogue's registers.
+constexpr int kTileA = 128, kTileB = 256, kStep = 64, kSlots = 4;
+constexpr int kEpilogueWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kThreads = 10 * 32;
+constexpr int kHalf = kTileB / 2;  // columns of a thread
+constexpr int kChunk = 32;         // steps
+constexpr int kABytes = kTileA * kStep * 2, kBBytes = kTileB * kStep * 2, kSlotBytes = kABytes + kBBytes;
+constexpr int kBlockBytes = kStep * 128;  // 64 columns of an operand that has k as its slow axis
+constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;
+constexpr int kGroup = 8;  // neighbouring tiles along b that pass before the next along a
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ float power(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Float32 operands are held as three bfloat16 planes, each the rounded rest of
+// those before it: 24 bits. Six products of planes, k passing once for each,
+// leave out what is below 2^-24 of a product.
+constexpr int kPlanes = 3, kPlaneProducts = 6;
+constexpr uint32_t kPlanesA = 0x021010u, kPlanesB = 0x201100u;  // four bits each, the first lowest: 00 10 01 11 20 02
+
+struct Product {
+    int W, tiles_a, tiles_b, splits;
+    int a_extent, b_extent;
+    int steps, segments;         // of k, and how often it passes
+    int each;                    // steps of a split, segments passing one after another
+    int a_k, b_k, a_at, b_at;    // where k and the tiles begin in each operand
+};
+
+struct Tile {
+    int w, split, a, b;
+};
+__device__ __forceinline__ int64_t tiles_of(const Product& p) { return (int64_t)p.W * p.splits * p.tiles_a * p.tiles_b; }
+// Groups of tiles along b, so that the tiles in work at a time share operands in L2.
+__device__ __forceinline__ Tile tile_of(const Product& p, int64_t i) {
+    const int64_t per = (int64_t)p.tiles_a * p.tiles_b;
+    const int batch = static_cast<int>(i / per);
+    const int64_t j = i - batch * per;
+    const int group = static_cast<int>(j / ((int64_t)p.tiles_a * kGroup)), first = group * kGroup, wide = min(kGroup, p.tiles_b - first);
+    const int64_t in = j - (int64_t)group * p.tiles_a * kGroup;
+    const int a = static_cast<int>(in / wide);
+    return {batch % p.W, batch / p.W, a, first + static_cast<int>(in - (int64_t)a * wide)};
+}
+
+template <bool SLOW>  // whether k is the operand's slow axis
+__device__ __forceinline__ uint64_t matrix_at(uint32_t address) {
+    return static_cast<uint64_t>((address & 0x3ffffu) >> 4) | static_cast<uint64_t>(SLOW ? kBlockBytes >> 4 : 1) << 16 |
+           static_cast<uint64_t>(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+template <bool A_SLOW, bool B_SLOW>
+constexpr uint32_t kInstruction = 1u << 4 | 1u << 7 | 1u << 10 | (A_SLOW ? 1u << 15 : 0u) | (B_SLOW ? 1u << 16 : 0u) | (kTileB / 8) << 17 |
+                                  (kTileA / 16) << 24;
+
+__device__ __forceinline__ void multiply(uint32_t sums, uint64_t a, uint64_t b, uint32_t instruction, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(sums),
+        "l"(a), "l"(b), "r"(instruction), "r"(add ? 1u : 0u)
+        : "memory");
+}
+__device__ __forceinline__ void arrive_when_multiplied(uint64_t* b) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(b)) : "memory");
+}
+__device__ __forceinline__ void copy_tile(uint32_t to, const CUtensorMap* map, int inner, int outer, int w, int plane, uint64_t* full) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
+        "l"(map), "r"(inner), "r"(outer), "r"(w), "r"(plane), "r"(smem_at(full))
+        : "memory");
+}
+template <bool SLOW, int EXTENT>
+__device__ __forceinline__ void copy_operand(uint32_t to, const CUtensorMap* map, int at, int k, int w, int plane, uint64_t* full) {
+    if constexpr (SLOW) {
+#pragma unroll
+        for (int c = 0; c < EXTENT / 64; ++c) copy_tile(to + c * kBlockBytes, map, at + c * 64, k, w, plane, full);
+    } else {
+        copy_tile(to, map, k, at, w, plane, full);
+    }
+}
+
+// E: the epilogue. run(v, w, split, a, b) takes 128 sums of lane a, columns b to b + 127.
+template <bool A_SLOW, bool B_SLOW, typename E>
+__global__ void __launch_bounds__(kThreads, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, Product p, E epilogue) {
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[kSlots], empty[kSlots], summed[2], taken[2], drained;
+    __shared__ uint32_t tensor_memory;
+    __shared__ int failed;  // a wait of the block ran out
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t slots = (smem_at(raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 0) {
+        failed = 0;
+        for (int s = 0; s < kSlots; ++s) {
+            barrier_init(&full[s], 1);
+            barrier_init(&empty[s], 1);
+        }
+        for (int h = 0; h < 2; ++h) {
+            barrier_init(&summed[h], 1);
+            barrier_init(&taken[h], kEpilogueWarps);
+        }
+        barrier_init(&drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMultiplyWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tensor_memory)), "r"(2 * kTileB)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t sums = tensor_memory;
+    layer_begin();
+
+    const int64_t tiles = tiles_of(p);
+    const auto range = [&](const Tile& t, int& first, int& count) {
+        first = t.split * p.each;
+        count = min(p.steps * p.segments - first, p.each);
+    };
+    if (warp == kCopyWarp) {
+        if (lane == 0) {
+            int64_t n = 0;  // steps copied
+            bool ok = true;
+            for (int64_t i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+                const Tile t = tile_of(p, i);
+                int first, count;
+                range(t, first, count);
+                for (int k = 0; k < count; ++k, ++n) {
+                    const int s = static_cast<int>(n % kSlots);
+                    ok = n < kSlots || barrier_wait(&empty[s], (n / kSlots - 1) & 1, &failed);
+                    if (!ok) break;
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(&full[s])), "r"(kSlotBytes) : "memory");
+                    const int segment = (first + k) / p.steps, at = (first + k - segment * p.steps) * kStep;
+                    const uint32_t slot = slots + s * kSlotBytes;
+                    copy_operand<A_SLOW, kTileA>(slot, &map_a, p.a_at + t.a * kTileA, p.a_k + at, t.w, kPlanesA >> 4 * segment & 15, &full[s]);
+                    copy_operand<B_SLOW, kTileB>(slot + kABytes, &map_b, p.b_at + t.b * kTileB, p.b_k + at, t.w, kPlanesB >> 4 * segment & 15,
+                                                 &full[s]);
+                }
+            }
+            // no copy may be in flight when the block ends, also where a wait ran out
+            for (int64_t q = n > kSlots ? n - kSlots : 0; q < n; ++q) barrier_wait(&full[q % kSlots], q / kSlots & 1, &failed);
+        }
+    } else if (warp == kMultiplyWarp) {
+        if (lane == 0) {
+            int64_t n = 0, c = 0;  // steps and chunks multiplied
+            bool ok = true;
+            for (int64_t i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+                int first, count;
+                range(tile_of(p, i), first, count);
+                for (int k0 = 0; k0 < count && ok; k0 += kChunk, ++c) {
+                    const int half = c & 1, end = min(k0 + kChunk, count);
+                    if (c >= 2) ok = barrier_wait(&taken[half], (c / 2 - 1) & 1, &failed);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    for (int k = k0; k < end && ok; ++k, ++n) {
+                        const int s = static_cast<int>(n % kSlots);
+                        ok = barrier_wait(&full[s], n / kSlots & 1, &failed);
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint64_t a = matrix_at<A_SLOW>(slots + s * kSlotBytes), b = matrix_at<B_SLOW>(slots + s * kSlotBytes + kABytes);
+#pragma unroll
+                        for (int q = 0; q < kStep / 16; ++q)
+                            multiply(sums + half * kTileB, a + q * (A_SLOW ? 2048 >> 4 : 32 >> 4), b + q * (B_SLOW ? 2048 >> 4 : 32 >> 4),
+                                     kInstruction<A_SLOW, B_SLOW>, k > k0 || q > 0);
+                        arrive_when_multiplied(&empty[s]);
+                    }
+                    if (ok) arrive_when_multiplied(&summed[half]);  // else nobody is told that the sums are there
+                }
+            }
+            // nor a product
+            arrive_when_multiplied(&drained);
+            barrier_wait(&drained, 0, &failed);
+        }
+    } else {
+        const int quarter = warp % 4 * 32, side = warp / 4 * kHalf;
+        int64_t c = 0;
+        bool ok = true;
+        for (int64_t i = blockIdx.x; i < tiles; i += gridDim.x) {
+            const Tile t = tile_of(p, i);
+            int first, count;
+            range(t, first, count);
+            float v[kHalf];
+            if (count <= 0)
+#pragma unroll
+                for (int j = 0; j < kHalf; ++j) v[j] = 0.f;
+            for (int k0 = 0; k0 < count && ok; k0 += kChunk, ++c) {
+                const int half = c & 1;
+                ok = __all_sync(~0u, barrier_wait(&summed[half], c / 2 & 1, &failed));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t at = sums + half * kTileB + (quarter << 16) + side;
+#pragma unroll
+                for (int j = 0; j < kHalf; j += 32) {
+                    uint32_t lo[16], hi[16];
+                    read_sums(at + j, lo);
+                    read_sums(at + j + 16, hi);
+                    wait_read(lo);
+                    wait_read(hi);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        v[j + e] = k0 == 0 ? __uint_as_float(lo[e]) : v[j + e] + __uint_as_float(lo[e]);
+                        v[j + 16 + e] = k0 == 0 ? __uint_as_float(hi[e]) : v[j + 16 + e] + __uint_as_float(hi[e]);
+                    }
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) barrier_arrive(&taken[half]);
+            }
+            // what a block makes whose wait ran out is not the product: from there on it says so
+            if (!ok)
+#pragma unroll
+                for (int j = 0; j < kHalf; ++j) v[j] = __uint_as_float(0x7fc00000u);
+            epilogue.run(v, t.w, t.split, t.a * kTileA + quarter + lane, t.b * kTileB + side);
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    __syncthreads();
+    if (warp == kMultiplyWarp) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sums), "r"(2 * kTileB));
+    }
+}
+
+// Of 128 neighbouring logits of a token: their maximum and the sum of
+// exp(l - maximum), for the words that there are; and the target's logit.
+struct RowSums {
+    const int64_t* targets;
+    float2* parts;  // [blocks of 128 words][W * M]
+    float* chosen;  // [W * M]
+    int64_t M, rows;
+    int V;
+    __device__ __forceinline__ void run(const float (&v)[kHalf], int w, int, int a, int b) const {
+        const int there = V - b;
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j) top[j % 4] = fmaxf(top[j % 4], j < there ? v[j] : -INFINITY);
+        const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const float shift = isinf(most) ? 0.f : -most * kLog2e;  // an infinite one leaves infinity or 0, as the formula has it
+        float sum[4] = {};
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j) {
+            const float e = power(fmaf(v[j], kLog2e, shift));
+            sum[j % 4] += j < there ? e : 0.f;
+        }
+        const bool real = a < M;
+        const int64_t row = w * M + a;
+        const int64_t target = real ? targets[row] - b : -1;
+        const bool mine = target >= 0 && target < kHalf && target < there;
+        if (__any_sync(~0u, mine)) {
+            float l = 0.f;
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j) l = j == target ? v[j] : l;
+            if (mine) chosen[row] = l;
+        }
+        if (real) parts[(int64_t)(b / kHalf) * rows + row] = make_float2(isinf(most) ? 0.f : most, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+    }
+};
+
+// lse and loss of each token from its parts: 32 tokens per block, every eighth part to a warp.
+__global__ void __launch_bounds__(256)
+finish_rows_kernel(const float2* parts, const float* chosen, const int64_t* targets, int64_t rows, int blocks, int V, float* loss, float* lse) {
+    layer_begin();
+    __shared__ float2 shared[8][32];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+    const bool real = row < rows;
+    float most = -INFINITY, sum = 0.f;
+    const auto add = [&](float2 p) {
+        const float next = fmaxf(most, p.x);  // finite: parts are, but for the first
+        sum = sum * power((most - next) * kLog2e) + p.y * power((p.x - next) * kLog2e);
+        most = next;
+    };
+    if (real)
+#pragma unroll 8
+        for (int k = warp; k < blocks; k += 8) add(parts[(int64_t)k * rows + row]);
+    shared[warp][lane] = make_float2(most, sum);
+    __syncthreads();
+    if (warp == 0 && real) {
+        for (int k = 1; k < 8; ++k)
+            if (k < blocks) add(shared[k][lane]);
+        const float l = most + logf(sum);
+        const int64_t t = targets[row];
+        lse[row] = l;
+        loss[row] = t < 0 ? 0.f : t >= V ? __uint_as_float(0x7fc00000u) : l - chosen[row];
+    }
+}
+
+// The gradient of a token's logits, without the factor that its worker's tokens
+// share: d = r (exp(l - lse) - onehot), rounded to bfloat16, or in three planes.
+template <int PLANES>
+struct LogitGradients {
+    const int64_t* targets;
+    const float *lse, *r;
+    __nv_bfloat16* d;  // [plane][W][M][pitch]
+    int64_t M, plane, pitch;
+    int V, first;      // the piece's first word
+    __device__ __forceinline__ void run(float (&v)[kHalf], int w, int, int a, int b) const {
+        if (a >= M) return;
+        const int64_t row = w * M + a, target = targets[row];
+        const bool ignored = target < 0;
+        const float l = target >= V ? __uint_as_float(0x7fc00000u) : lse[row], scale = ignored ? 0.f : r[row];
+        const int64_t hot = target - first - b;
+        __nv_bfloat16* to = d + row * pitch + b;
+#pragma unroll
+        for (int j = 0; j < kHalf; j += 8) {
+            float g[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p = power((v[j + e] - l) * kLog2e) - (j + e == hot ? 1.f : 0.f);
+                g[e] = ignored ? 0.f : p * scale;
+            }
+            if (b + j < pitch)
+#pragma unroll
+            for (int q = 0; q < PLANES; ++q) {
+                store_piece<8>(to + q * plane + j, g);
+                if (q + 1 < PLANES)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) g[e] -= __bfloat162float(__float2bfloat16_rn(g[e]));
+            }
+        }
+    }
+};
+
+// C written out, [b][a] with a contiguous: times the worker's factor, 0 in the rows of ignored tokens, or as a part
+// (float32, factor and targets NULL) that may be added to what is there.
+template <typename G>
+struct WriteOut {
+    G* out;
+    int64_t worker, split, row;
+    const float* factor;
+    const int64_t* targets;
+    int a_extent, b_extent, add;
+    __device__ __forceinline__ void run(const float (&v)[kHalf], int w, int s, int a, int b) const {
+        if (a >= a_extent) return;
+        G* to = out + w * worker + s * split + b * row + a;
+        const float f = factor != nullptr ? factor[w] : 1.f;
+        const int64_t* t = targets != nullptr ? targets + (int64_t)w * b_extent + b : nullptr;
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j) {
+            if (b + j < b_extent) {
+                float x = v[j];
+                if (factor != nullptr) x *= f;
+                if (t != nullptr && t[j] < 0) x = 0.f;
+                if constexpr (sizeof(G) == 4)
+                    if (add) x += to[j * row];
+                to[j * row] = from_float<G>(x);
+            }
+        }
+    }
+};
+
+// The sum of the splits' parts [split][W][rows][D], in their order, times the worker's factor; 0 in ignored tokens' rows.
+template <typename G>
+__global__ void __launch_bounds__(256)
+sum_parts_kernel(const float* parts, int splits, int64_t per_worker, int64_t all, int D, const float* factor, const int64_t* targets, G* out,
+                 int64_t worker) {
+    layer_begin();
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
+        float s = 0.f;
+        for (int k = 0; k < splits; ++k) s += load_once(parts + k * all + at);
+        const int64_t w = at / per_worker, in = at - w * per_worker;
+        s *= factor[w];
+        if (targets != nullptr && targets[at / D] < 0) s = 0.f;
+        out[w * worker + in] = from_float<G>(s);
+    }
+}
+
+// An operand as the tensor copies need it: bfloat16 rows at multiples of 16
+// bytes, [plane][W][rows][pitch], zeros in the rows of ignored tokens. Eight
+// elements per thread and turn.
+template <typename T, int PLANES>
+__global__ void __launch_bounds__(256)
+pack_kernel(const T* x, int64_t worker, int64_t stride, int64_t rows_each, int64_t rows, int D, int pitch, const int64_t* targets,
+            __nv_bfloat16* out) {
+    layer_begin();
+    const int lane = threadIdx.x % 32;
+    for (int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; row < rows; row += (int64_t)gridDim.x * 8) {
+        const int64_t w = row / rows_each;
+        const T* p = x + w * worker + (row - w * rows_each) * stride;
+        const bool there = targets == nullptr || targets[row] >= 0;
+        __nv_bfloat16* to = out + row * pitch;
+#pragma unroll 2
+        for (int k = lane * 8; k < pitch; k += 256) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                Piece<T, 1> one{};
+                one.load(p + k + e, there && k + e < D);
+                v[e] = one.get(0);
+            }
+#pragma unroll
+            for (int q = 0; q < PLANES; ++q) {
+                store_piece<8>(to + q * rows * pitch + k, v);
+                if (q + 1 < PLANES)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float rest = v[e] - __bfloat162float(__float2bfloat16_rn(v[e]));
+                        v[e] = isfinite(v[e]) ? rest : 0.f;
+                    }
+            }
+        }
+    }
+}
+
+// r = dloss / factor with factor the largest finite |dloss| of the worker's
+// tokens: where all have the same weight, r is 1 and d's rounding is that of
+// probabilities. One block per worker.
+__global__ void __launch_bounds__(1024)
+factor_kernel(const float* dloss, const int64_t* targets, int64_t M, float* r, float* factor) {
+    layer_begin();
+    __shared__ float parts[32];
+    const int64_t first = blockIdx.x * M;
+    float most = 0.f;
+#pragma unroll 4
+    for (int64_t m = threadIdx.x; m < M; m += 1024) {
+        const float g = fabsf(dloss[first + m]);
+        if (targets[first + m] >= 0 && isfinite(g)) most = fmaxf(most, g);
+    }
+    for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+    if (threadIdx.x % 32 == 0) parts[threadIdx.x / 32] = most;
+    __syncthreads();
+    most = parts[threadIdx.x % 32];
+    for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+    const float f = most > 0.f ? most : 1.f;
+    if (threadIdx.x == 0) factor[blockIdx.x] = f;
+#pragma unroll 4
+    for (int64_t m = threadIdx.x; m < M; m += 1024) r[first + m] = dloss[first + m] / f;
+}
+
+// -- the host's side -------------------------------------------------------------------------------------------------
+
+constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of d at a time
+
+int64_t padded(int64_t bytes) { return ceil_div(bytes, 256) * 256; }
+int64_t pitch_of(int64_t n) { return ceil_div(n, 8) * 8; }
+
+// How k is split among blocks: the number of parts that takes least time, by
+// the turns that the tiles take on the SMs. A step of a tile takes 0.3 us, its
+// start and end 3; parts cost their writing and reading at 4 TB/s and a launch.
+struct Splits {
+    int count, each;
+};
+Splits splits_of(int64_t tiles, int64_t steps, int64_t outputs) {
+    Splits best{1, static_cast<int>(steps)};
+    double least = 0;
+    const int64_t most = ceil_div(2 * kSMs, tiles);
+    for (int64_t count = 1; count <= most && (count == 1 || count * 4 <= steps); ++count) {
+        const int64_t each = std::max<int64_t>(ceil_div(steps, count), 1), parts = std::max<int64_t>(ceil_div(steps, each), 1);
+        double us = static_cast<double>(ceil_div(tiles * parts, kSMs)) * (each * 0.3 + 3.0);
+        if (parts > 1) us += 3.0 + 2e-6 * parts * outputs;
+        if (count == 1 || us < least) least = us, best = {static_cast<int>(parts), static_cast<int>(each)};
+    }
+    return best;
+}
+
+// What a call computes from its sizes.
+struct Plan {
+    int planes, segments;
+    int64_t x_copy, weight_copy;       // bytes of the copies that the tensor copies read; 0: in place
+    int64_t parts, chosen;             // forward
+    int words, pieces;                 // of a piece, and how many
+    int64_t pitch, d, rows;            // of d, its bytes; bytes of r and factor
+    Splits dx, dweight;
+    int64_t dx_parts, dweight_parts;   // bytes; 0: written in place
+    int64_t forward, backward;         // bytes in all
+};
+
+bool in_place(const void* p, int64_t worker, int64_t row, cpdp_dtype dtype, int W, int64_t rows, int64_t D) {
+    return dtype == CPDP_BF16 && aligned_to(p, 16) && (rows <= 1 || (row % 8 == 0 && row >= D && row < (int64_t(1) << 38))) &&
+           (W <= 1 || (worker % 8 == 0 && worker > 0 && worker < (int64_t(1) << 38)));
+}
+
+Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight, int64_t weight_worker, int64_t weight_row, cpdp_dtype dtype,
+             int W, int64_t M, int V, int D) {
+    Plan p{};
+    p.planes = dtype == CPDP_F32 ? kPlanes : 1;
+    p.segments = dtype == CPDP_F32 ? kPlaneProducts : 1;
+    const int64_t pitch = pitch_of(D), packed = padded(p.planes * W * M * pitch * 2);
+    p.x_copy = in_place(x, x_worker, x_row, dtype, W, M, D) ? 0 : packed;
+    p.weight_copy = in_place(weight, weight_worker, weight_row, dtype, W, V, D) ? 0 : padded(p.planes * W * (int64_t)V * pitch * 2);
+    const int64_t rows = W * M;
+    p.parts = padded(ceil_div(V, kTileB) * 2 * rows * 8);
+    p.chosen = padded(rows * 4);
+    p.forward = p.x_copy + p.weight_copy + p.parts + p.chosen;
+
+    const int64_t fit = std::max<int64_t>(kPieceBytes / (p.planes * 2 * std::max<int64_t>(rows, 1)), kTileB);
+    p.pieces = static_cast<int>(ceil_div(V, fit));
+    p.words = static_cast<int>(std::min<int64_t>(ceil_div(ceil_div(V, p.pieces), kTileB) * kTileB, ceil_div(V, kTileB) * kTileB));
+    p.pieces = static_cast<int>(ceil_div(V, p.words));
+    p.pitch = pitch_of(std::min(p.words, V));
+    p.d = padded(p.planes * rows * p.pitch * 2);
+    p.rows = padded(rows * 4) + padded(W * 4);
+    const int64_t tiles_d = ceil_div(D, kTileA);
+    p.dx = splits_of(W * tiles_d * ceil_div(M, kTileB), ceil_div(std::min(p.words, V), kStep) * p.segments, rows * D);
+    p.dweight = splits_of(W * tiles_d * ceil_div(std::min(p.words, V), kTileB), ceil_div(M, kStep) * p.segments, (int64_t)W * std::min(p.words, V) * D);
+    p.dx_parts = p.dx.count > 1 || p.pieces > 1 ? padded(p.dx.count * rows * D * 4) : 0;
+    p.dweight_parts = p.dweight.count > 1 ? padded((int64_t)p.dweight.count * W * std::min(p.words, V) * D * 4) : 0;
+    p.backward = packed + p.weight_copy + p.rows + p.d + p.dx_parts + p.dweight_parts;
+    return p;
+}
+
+// A matrix [plane][W][rows][columns] of bfloat16 and the box that a copy takes of it.
+cpdp_status encode(CUtensorMap* map, const void* p, int64_t columns, int64_t rows, int W, int planes, int64_t row, int64_t worker, int64_t plane,
+                   int box_rows) {
+    const EncodeTiled f = encode_tiled();
+    if (f == nullptr) return layer_error(CPDP_ECUDA, "the CUDA driver has no cuTensorMapEncodeTiled");
+    if (rows <= 1) row = pitch_of(columns);  // strides that no index uses
+    if (W <= 1) worker = row * rows;
+    if (planes <= 1) plane = worker * W;
+    const cuuint64_t dims[4] = {(cuuint64_t)columns, (cuuint64_t)rows, (cuuint64_t)W, (cuuint64_t)planes},
+                     strides[3] = {(cuuint64_t)row * 2, (cuuint64_t)worker * 2, (cuuint64_t)plane * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
+    const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return layer_error(CPDP_ECUDA, "cuTensorMapEncodeTiled: error %d", (int)r);
+    return CPDP_OK;
+}
+
+template <bool A_SLOW, bool B_SLOW, typename E>
+cpdp_status multiply_all(const CUtensorMap& a, const CUtensorMap& b, const Product& p, const E& epilogue, void* stream, const char* what) {
+    const int64_t tiles = (int64_t)p.W * p.splits * p.tiles_a * p.tiles_b;
+    cudaError_t e = allow_shared_memory<product_kernel<A_SLOW, B_SLOW, E>>(kSmemBytes);
+    if (e == cudaSuccess)
+        e = launch_layer(product_kernel<A_SLOW, B_SLOW, E>, static_cast<unsigned>(std::min<int64_t>(tiles, kSMs)), kThreads, kSmemBytes, stream, a, b, p,
+                         epilogue);
+    return layer_launched(e, what);
+}
+
+Product product(int W, int64_t a, int64_t b, int64_t k, int segments, Splits s = {1, 0}) {
+    Product p{};
+    p.W = W;
+    p.tiles_a = static_cast<int>(ceil_div(a, kTileA)), p.tiles_b = static_cast<int>(ceil_div(b, kTileB));
+    p.a_extent = static_cast<int>(a), p.b_extent = static_cast<int>(b);
+    p.steps = static_cast<int>(ceil_div(k, kStep)), p.segments = segments;
+    p.splits = s.count, p.each = s.each > 0 ? s.each : p.steps * segments;
+    return p;
+}
+
+cpdp_status pack(const void* x, int64_t worker, int64_t stride, cpdp_dtype dtype, int W, int64_t rows_each, int D, const int64_t* targets, void* out,
+                 void* stream, const char* what) {
+    const int64_t rows = W * rows_each;
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows, 8), kSMs * 8));
+    const int pitch = static_cast<int>(pitch_of(D));
+    auto* to = static_cast<__nv_bfloat16*>(out);
+    return layer_launched(dtype == CPDP_F32
+                              ? launch_layer(pack_kernel<float, kPlanes>, blocks, 256, 0, stream, static_cast<const float*>(x), worker, stride,
+                                             rows_each, rows, D, pitch, targets, to)
+                              : launch_layer(pack_kernel<__nv_bfloat16, 1>, blocks, 256, 0, stream, static_cast<const __nv_bfloat16*>(x), worker,
+                                             stride, rows_each, rows, D, pitch, targets, to),
+                          what);
+}
+
+cpdp_status check_loss(const void* x, int64_t x_worker, int64_t x_row, const void* weight, int64_t weight_worker, int64_t weight_row, cpdp_dtype dtype,
+                       int W, int64_t M, int V, int D, const int64_t* targets) {
+    CPDP_TRY(check_sizes(W, M, D));
+    CPDP_TRY(check_sizes(W, V, D));
+    CPDP_TRY(check_sizes(W, M, V));
+    if (!known_dtype(dtype)) return layer_error(CPDP_EINVAL, "unknown dtype %d", (int)dtype);
+    if (V < 1) return layer_error(CPDP_EINVAL, "V=%d must be at least 1", V);
+    CPDP_TRY(check_array("x", x, M > 0, dtype_size(dtype), x_worker, x_row));
+    CPDP_TRY(check_array("weight", weight, true, dtype_size(dtype), weight_worker, weight_row));
+    return check_array("targets", targets, M > 0, 8);
+}
+
+}  // namespace
+
+cudaError_t take_loss_timeouts(unsigned long long* count) {
+    unsigned long long zero = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(count, wait_timeouts, sizeof *count);
+    if (e == cudaSuccess) e = cudaMemcpyToSymbol(wait_timeouts, &zero, sizeof zero);
+    return e;
+}
+
+}  // namespace cpdp
+
+using namespace cpdp;
+
+static bool loss_sizes(int W, int64_t M, int V, int D) {
+    return check_sizes(W, M, D) == CPDP_OK && check_sizes(W, V, D) == CPDP_OK && check_sizes(W, M, V) == CPDP_OK && V >= 1;
+}
+
+size_t cpdp_linear_cross_entropy_workspace(const void* x, int64_t x_worker, int64_t x_row, const void* weight, int64_t weight_worker,
+                                           int64_t weight_row, cpdp_dtype dtype, int W, int64_t M, int V, int D) {
+    if (!loss_sizes(W, M, V, D) || M == 0) return 0;
+    return plan_of(x, x_worker, x_row, weight, weight_worker, weight_row, dtype, W, M, V, D).forward;
+}
+
+size_t cpdp_linear_cross_entropy_backward_workspace(const void* x, int64_t x_worker, int64_t x_row, const void* weight, int64_t weight_worker,
+                                                    int64_t weight_row, cpdp_dtype dtype, int W, int64_t M, int V, int D) {
+    if (!loss_sizes(W, M, V, D) || M == 0) return 0;
+    return plan_of(x, x_worker, x_row, weight, weight_worker, weight_row, dtype, W, M, V, D).backward;
+}
+
+namespace {
+struct Where {
+    const void* p;
+    int64_t worker, row, plane;
+};
+}  // namespace
+
+cpdp_status cpdp_linear_cross_entropy(const void* x, int64_t x_worker, int64_t x_row, const void* weight, int64_t weight_worker,
+                                      int64_t weight_row, const int64_t* targets, cpdp_dtype dtype, int W, int64_t M, int V, int D, float* loss,
+                                      float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    constexpr const char* what = "cpdp_linear_cross_entropy";
+    CPDP_TRY(check_loss(x, x_worker, x_row, weight, weight_worker, weight_row, dtype, W, M, V, D, targets));
+    CPDP_TRY(check_array("loss", loss, M > 0, 4));
+    CPDP_TRY(check_array("lse", lse, M > 0, 4));
+    if (M == 0) return CPDP_OK;
+    const Plan plan = plan_of(x, x_worker, x_row, weight, weight_worker, weight_row, dtype, W, M, V, D);
+    CPDP_TRY(check_workspace(workspace, workspace_bytes, plan.forward));
+    const int64_t pitch = pitch_of(D), rows = W * M;
+    char* at = static_cast<char*>(workspace);
+    Where xs{x, x_worker, x_row, 0}, ws{weight, weight_worker, weight_row, 0};
+    if (plan.x_copy) {
+        CPDP_TRY(pack(x, x_worker, x_row, dtype, W, M, D, nullptr, at, stream, what));
+        xs = {at, M * pitch, pitch, rows * pitch};
+        at += plan.x_copy;
+    }
+    if (plan.weight_copy) {
+        CPDP_TRY(pack(weight, weight_worker, weight_row, dtype, W, V, D, nullptr, at, stream, what));
+        ws = {at, V * pitch, pitch, (int64_t)W * V * pitch};
+        at += plan.weight_copy;
+    }
+    auto* parts = reinterpret_cast<float2*>(at);
+    auto* chosen = reinterpret_cast<float*>(at + plan.parts);
+    CUtensorMap a, b;
+    CPDP_TRY(encode(&a, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
+    CPDP_TRY(encode(&b, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileB));
+    CPDP_TRY((multiply_all<false, false>(a, b, product(W, M, V, D, plan.segments), RowSums{targets, parts, chosen, M, rows, V}, stream, what)));
+    return layer_launched(launch_layer(finish_rows_kernel, static_cast<unsigned>(ceil_div(rows, 32)), 256, 0, stream,
+                                       static_cast<const float2*>(parts), static_cast<const float*>(chosen), targets, rows,
+                                       static_cast<int>(ceil_div(V, kTileB) * 2), V, loss, lse),
+                          what);
+}
+
+template <typename G>
+static cpdp_status zero_rows(G* out, int64_t worker, int W, int64_t each, void* stream) {
+    for (int w = 0; w < W; ++w) {
+        const cudaError_t e = cudaMemsetAsync(out + w * worker, 0, each * sizeof(G), static_cast<cudaStream_t>(stream));
+        if (e != cudaSuccess) return layer_launched(e, "cpdp_linear_cross_entropy_backward");
+    }
+    return CPDP_OK;
+}
+
+cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x, int64_t x_worker, int64_t x_row, const void* weight,
+                                               int64_t weight_worker, int64_t weight_row, const int64_t* targets, const float* lse,
+                                               cpdp_dtype dtype, int W, int64_t M, int V, int D, void* dx, void* dweight, int64_t dweight_worker,
+                                               cpdp_dtype dweight_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    constexpr const char* what = "cpdp_linear_cross_entropy_backward";
+    CPDP_TRY(check_loss(x, x_worker, x_row, weight, weight_worker, weight_row, dtype, W, M, V, D, targets));
+    if (!known_dtype(dweight_dtype)) return layer_error(CPDP_EINVAL, "unknown dtype of dweight: %d", (int)dweight_dtype);
+    CPDP_TRY(check_array("dloss", dloss, M > 0, 4));
+    CPDP_TRY(check_array("lse", lse, M > 0, 4));
+    CPDP_TRY(check_array("dx", dx, M > 0, dtype_size(dtype)));
+    CPDP_TRY(check_array("dweight", dweight, true, dtype_size(dweight_dtype), dweight_worker));
+    CPDP_TRY(check_apart("dweight", W, dweight_worker, (int64_t)V * D));
+    if (M == 0)
+        return dweight_dtype == CPDP_F32 ? zero_rows(static_cast<float*>(dweight), dweight_worker, W, (int64_t)V * D, stream)
+                                         : zero_rows(static_cast<__nv_bfloat16*>(dweight), dweight_worker, W, (int64_t)V * D, stream);
+    const Plan plan = plan_of(x, x_worker, x_row, weight, weight_worker, weight_row, dtype, W, M, V, D);
+    CPDP_TRY(check_workspace(workspace, workspace_bytes, plan.backward));
+    const int64_t pitch = pitch_of(D), rows = W * M;
+    char* at = static_cast<char*>(workspace);
+    // x with zeros for ignored tokens: what lies there must not reach dweight
+    CPDP_TRY(pack(x, x_worker, x_row, dtype, W, M, D, targets, at, stream, what));
+    const Where xs{at, M * pitch, pitch, rows * pitch};
+    at += padded(plan.planes * rows * pitch * 2);
+    Where ws{weight, weight_worker, weight_row, 0};
+    if (plan.weight_copy) {
+        CPDP_TRY(pack(weight, weight_worker, weight_row, dtype, W, V, D, nullptr, at, stream, what));
+        ws = {at, V * pitch, pitch, (int64_t)W * V * pitch};
+        at += plan.weight_copy;
+    }
+    auto* r = reinterpret_cast<float*>(at);
+    auto* factor = reinterpret_cast<float*>(at + padded(rows * 4));
+    at += plan.rows;
+    auto* d = reinterpret_cast<__nv_bfloat16*>(at);
+    auto* dx_parts = reinterpret_cast<float*>(at + plan.d);
+    auto* dweight_parts = reinterpret_cast<float*>(at + plan.d + plan.dx_parts);
+    CPDP_TRY(layer_launched(launch_layer(factor_kernel, static_cast<unsigned>(W), 1024, 0, stream, dloss, targets, M, r, factor), what));
+
+    CUtensorMap x_rows, x_columns, w_rows, w_columns, d_rows, d_columns;
+    CPDP_TRY(encode(&x_rows, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
+    CPDP_TRY(encode(&x_columns, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kStep));
+    CPDP_TRY(encode(&w_rows, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileB));
+    CPDP_TRY(encode(&w_columns, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kStep));
+    const unsigned sum_blocks = kSMs * 8;
+    for (int piece = 0; piece < plan.pieces; ++piece) {
+        const int first = piece * plan.words, words = std::min(plan.words, V - first);
+        const int64_t plane = rows * plan.pitch;
+        CPDP_TRY(encode(&d_rows, d, words, M, W, plan.planes, plan.pitch, M * plan.pitch, plane, kTileB));
+        CPDP_TRY(encode(&d_columns, d, words, M, W, plan.planes, plan.pitch, M * plan.pitch, plane, kStep));
+        Product p = product(W, M, words, D, plan.segments);
+        p.b_at = first;
+        const auto gradients = [&](auto planes) {
+            constexpr int P = decltype(planes)::value;
+            return multiply_all<false, false>(x_rows, w_rows, p, LogitGradients<P>{targets, lse, r, d, M, plane, plan.pitch, V, first}, stream, what);
+        };
+        CPDP_TRY(plan.planes == 1 ? gradients(std::integral_constant<int, 1>{}) : gradients(std::integral_constant<int, kPlanes>{}));
+
+        p = product(W, D, M, words, plan.segments, plan.dx);
+        p.splits = static_cast<int>(ceil_div(p.steps * p.segments, p.each));  // a last piece may have fewer words
+        p.a_k = first;
+        if (plan.dx_parts) {
+            CPDP_TRY((multiply_all<true, false>(w_columns, d_rows, p,
+                                                WriteOut<float>{dx_parts, M * D, rows * D, D, nullptr, nullptr, D, (int)M, piece > 0}, stream, what)));
+        } else {
+            const auto write = [&](auto* out) {
+                using G = std::remove_pointer_t<decltype(out)>;
+                return multiply_all<true, false>(w_columns, d_rows, p, WriteOut<G>{out, M * D, 0, D, factor, targets, D, (int)M, 0}, stream, what);
+            };
+            CPDP_TRY(dtype == CPDP_F32 ? write(static_cast<float*>(dx)) : write(static_cast<__nv_bfloat16*>(dx)));
+        }
+
+        p = product(W, D, words, M, plan.segments, plan.dweight);
+        const int64_t part = (int64_t)words * D;
+        if (plan.dweight_parts) {
+            CPDP_TRY((multiply_all<true, true>(x_columns, d_columns, p,
+                                               WriteOut<float>{dweight_parts, part, W * part, D, nullptr, nullptr, D, words, 0}, stream, what)));
+            const auto sum = [&](auto* out) {
+                return launch_layer(sum_parts_kernel<std::remove_pointer_t<decltype(out)>>,
+                                    static_cast<unsigned>(std::min<int64_t>(ceil_div(W * part, 256), sum_blocks)), 256, 0, stream,
+                                    static_cast<const float*>(dweight_parts), p.splits, part, W * part, D, static_cast<const float*>(factor),
+                                    static_cast<const int64_t*>(nullptr), out + (int64_t)first * D, dweight_worker);
+            };
+            CPDP_TRY(layer_launched(dweight_dtype == CPDP_F32 ? sum(static_cast<float*>(dweight)) : sum(static_cast<__nv_bfloat16*>(dweight)), what));
+        } else {
+            const auto write = [&](auto* out) {
+                using G = std::remove_pointer_t<decltype(out)>;
+                return multiply_all<true, true>(x_columns, d_columns, p,
+                                                WriteOut<G>{out + (int64_t)first * D, dweight_worker, 0, D, factor, nullptr, D, words, 0}, stream, what);
+            };
+            CPDP_TRY(dweight_dtype == CPDP_F32 ? write(static_cast<float*>(dweight)) : write(static_cast<__nv_bfloat16*>(dweight)));
+        }
+    }
+    if (!plan.dx_parts) return CPDP_OK;
+    const auto sum = [&](auto* out) {
+        return launch_layer(sum_parts_kernel<std::remove_pointer_t<decltype(out)>>,
+                            static_cast<unsigned>(std::min<int64_t>(ceil_div(rows * D, 256), sum_blocks)), 256, 0, stream,
+                            static_cast<const float*>(dx_parts), plan.dx.count, M * D, rows * D, D, static_cast<const float*>(factor), targets, out,
+                            M * D);
+    };
+    return layer_launched(dtype == CPDP_F32 ? sum(static_cast<float*>(dx)) : sum(static_cast<__nv_bfloat16*>(dx)), what);
+}

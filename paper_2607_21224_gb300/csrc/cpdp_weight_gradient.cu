@@ -1,9 +1,6 @@
 // The weight gradient dW = dy^T x^ from activations held in 8 bits
 // (include/cpdp_layers.h).
-#include <atomic>
-#include <cuda.h>
-
-#include "cpdp_layers.cuh"
+#include "cpdp_tensor.cuh"
 
 namespace cpdp {
 namespace {
@@ -45,52 +42,10 @@ constexpr int kXBytes = kTileI / 64 * kBlockBytes, kDyBytes = kTileO / 64 * kBlo
 constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;  // and room to align the slots
 constexpr int kAhead = 2;                               // of its steps whose codes a group loads ahead
 #ifdef CPDP_CHECKED
-constexpr unsigned long long kWaitLimitNs = 200000000ull;
 // A step whose dy is never copied, so that waits run out; -1: none. Debug build only.
 __device__ int dropped_step = -1;
-#else
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 #endif
 static_assert(kStep * kTileI == kGroupWarps * 32 * kBlock8, "one block of features per converting thread and step");
-
-__device__ unsigned long long wait_timeouts;
-
-__device__ __forceinline__ uint32_t smem_at(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-__device__ __forceinline__ unsigned long long now_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-__device__ __forceinline__ void barrier_init(uint64_t* b, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void barrier_arrive(uint64_t* b) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_at(b)) : "memory");
-}
-// Whether the phase is done, after waiting in hardware for up to `ns`.
-__device__ __forceinline__ bool barrier_done(uint64_t* b, uint32_t parity, uint32_t ns) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(smem_at(b)), "r"(parity), "r"(ns)
-        : "memory");
-    return done != 0;
-}
-// False, counted and noted in the block's `failed`, where the phase does not end within the limit.
-__device__ __noinline__ bool barrier_wait_long(uint64_t* b, uint32_t parity, int* failed) {
-    const unsigned long long start = now_ns();
-    while (!barrier_done(b, parity, 100000u))
-        if (now_ns() - start > kWaitLimitNs) {
-            atomicAdd(&wait_timeouts, 1ull);
-            *static_cast<volatile int*>(failed) = 1;
-            return false;
-        }
-    return true;
-}
-__device__ __forceinline__ bool barrier_wait(uint64_t* b, uint32_t parity, int* failed) {
-    return barrier_done(b, parity, 100000u) || barrier_wait_long(b, parity, failed);
-}
 
 // A matrix in shared memory whose rows of 64 elements run along the summed
 // axis: blocks of columns kBlockBytes apart, groups of 8 rows 1,024 bytes
@@ -111,22 +66,6 @@ __device__ __forceinline__ void multiply(uint32_t sums, uint64_t a, uint64_t b, 
 }
 __device__ __forceinline__ void arrive_when_multiplied(uint64_t* b) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(b)) : "memory");
-}
-// 16 columns of the warp's 32 lanes; there once the wait is over.
-__device__ __forceinline__ void read_sums(uint32_t at, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(at)
-        : "memory");
-}
-// The loads' results are operands, so that nothing uses them before.
-__device__ __forceinline__ void wait_read(uint32_t (&r)[16]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
 __device__ __forceinline__ void store_sums(uint32_t at, const uint32_t (&r)[16]) {
     asm volatile(
@@ -474,22 +413,6 @@ Splits splits_of(int W, int64_t M, int O, int I) {
     return best;
 }
 
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-    static const EncodeTiled f = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
-            r != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return f;
-}
-
 }  // namespace
 }  // namespace cpdp
 
@@ -577,14 +500,7 @@ cpdp_status cpdp_weight_gradient(const void* dy, int64_t dy_worker, int64_t dy_r
     const dim3 grid(ceil_div(I, kTileI), ceil_div(O, kTileO), sp.count * W);
     const auto typed = [&](auto g) {
         using G = decltype(g);
-        static std::atomic<uint64_t> allowed{0};  // the devices on which this kernel has been allowed its shared memory
-        int device = 0;
-        cudaError_t e = cudaGetDevice(&device);
-        const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
-        if (e == cudaSuccess && (allowed.load() & bit) == 0) {
-            e = cudaFuncSetAttribute(weight_gradient_kernel<G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-            if (e == cudaSuccess) allowed |= bit;
-        }
+        const cudaError_t e = allow_shared_memory<weight_gradient_kernel<G>>(kSmemBytes);
         return e != cudaSuccess ? e : launch_layer(weight_gradient_kernel<G>, grid, kThreads, kSmemBytes, stream, map, p);
     };
     CPDP_TRY(layer_launched(parts || dW_dtype == CPDP_F32 ? typed(0.f) : typed(__nv_bfloat16{}), "cpdp_weight_gradient"));
@@ -606,10 +522,11 @@ extern "C" cpdp_status cpdp_layer_drop_step(int step) {
 
 cpdp_status cpdp_layer_timeouts(int64_t* count) {
     if (count == nullptr) return layer_error(CPDP_EINVAL, "count is NULL");
-    unsigned long long seen = 0, zero = 0;
+    unsigned long long seen = 0, loss = 0, zero = 0;
     cudaError_t e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&seen, wait_timeouts, sizeof seen);
     if (e == cudaSuccess) e = cudaMemcpyToSymbol(wait_timeouts, &zero, sizeof zero);
-    *count = static_cast<int64_t>(seen);
+    if (e == cudaSuccess) e = take_loss_timeouts(&loss);
+    *count = static_cast<int64_t>(seen + loss);
     return layer_launched(e, "cpdp_layer_timeouts");
 }

@@ -7,6 +7,8 @@ include/cpdp_layers.h, which make the gradients that ``CPDPState`` steps with.
   for the backward pass, and the weight gradient that reads them
 - ``gated_recurrence`` / ``gated_recurrence_backward`` /
   ``gated_recurrence_step``: h_t = a_t h_(t-1) + (1 - a_t) v_t, a = sigmoid(gate)
+- ``linear_cross_entropy`` / ``linear_cross_entropy_backward``: softmax cross
+  entropy over a vocabulary, from the activations and the head's weight
 
 Activations are (W, M, D): W workers, M tokens each, D features, contiguous
 along D, float32 or bfloat16. One model's (M, D) is taken too, with a weight
@@ -58,6 +60,10 @@ SIGNATURES = {
     "cpdp_gated_recurrence_backward": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _L, _I, _I, _L, _I, _P, _P, _P, _P, _P, _L, _L,
                                             _P, _P, _Z, _P]),
     "cpdp_gated_recurrence_step": (_I, [_P, _L, _P, _L, _I, _I, _I, _P, _P, _P]),
+    "cpdp_linear_cross_entropy_workspace": (_Z, [_P, _L, _L, _P, _L, _L, _I, _I, _L, _I, _I]),
+    "cpdp_linear_cross_entropy": (_I, [_P, _L, _L, _P, _L, _L, _P, _I, _I, _L, _I, _I, _P, _P, _P, _Z, _P]),
+    "cpdp_linear_cross_entropy_backward_workspace": (_Z, [_P, _L, _L, _P, _L, _L, _I, _I, _L, _I, _I]),
+    "cpdp_linear_cross_entropy_backward": (_I, [_P, _P, _L, _L, _P, _L, _L, _P, _P, _I, _I, _L, _I, _I, _P, _P, _L, _I, _P, _Z, _P]),
     "cpdp_layer_timeouts": (_I, [ctypes.POINTER(_L)]),
 }
 
@@ -473,10 +479,74 @@ def gated_recurrence_step(gate, value, state, *, stream=None):
     return h
 
 
+def _head(x, weight, targets) -> tuple:
+    """What the calls of the loss share: W, M, V, D and the arguments of x and weight."""
+    W, M, D = shape = _three(x, "x")
+    device, dtype, code = x.device, x.dtype, _dtype(x, "x")
+    xs = _input(x, "x", shape, dtype, device)
+    if weight.dim() != 3:
+        raise ValueError(f"weight must be (W, V, D), or (V, D) of one model; got {tuple(weight.shape)}")
+    V = _sized(weight, "weight")[1]
+    ws = _input(weight, "weight", (W, V, D), dtype, device)
+    targets_at = _whole(targets, "targets", (W, M), torch.int64, device)
+    return (W, M, V, D), (x.data_ptr(), xs[0], xs[1], weight.data_ptr(), ws[0], ws[1]), targets_at, code
+
+
+def linear_cross_entropy(x, weight, targets, *, stream=None):
+    """Cross entropy of each token's target under softmax(weight x): (loss, lse).
+
+    x (W, M, D) and weight (W, V, D) of one type, float32 or bfloat16; targets
+    int64 (W, M), negative where a token is ignored: its loss is 0. loss and
+    lse = log(sum(exp(logits))), which the backward pass takes, are float32
+    (W, M). A target of V or more has the loss NaN. The logits are not kept."""
+    if x.dim() == 2 and weight.dim() == 2:
+        loss, lse = linear_cross_entropy(x[None], weight[None], targets[None], stream=stream)
+        return loss[0], lse[0]
+    _no_autograd(x=x, weight=weight)
+    device = _cuda(x, "x")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return linear_cross_entropy(x, weight, targets)
+    (W, M, V, D), operands, targets_at, code = _head(x, weight, targets)
+    loss, lse = torch.empty((2, W, M), dtype=_F32, device=device).unbind(0)
+    needed = _entry("cpdp_linear_cross_entropy_workspace")(*operands, code, W, M, V, D)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_linear_cross_entropy")(*operands, targets_at, code, W, M, V, D, loss.data_ptr(), lse.data_ptr(), _ptr(work), needed,
+                                               _stream(device.index)))
+    return loss, lse
+
+
+def linear_cross_entropy_backward(dloss, x, weight, targets, lse, *, dweight=None, dtype=torch.float32, stream=None):
+    """Gradients of ``linear_cross_entropy``: (dx, dweight) from dloss float32
+    (W, M), the gradient of each token's loss (1 / M each for a mean). dx has x's
+    type and is 0 in ignored tokens' rows. dweight (W, V, D) is written into the
+    tensor given, float32 or bfloat16 (a view of the gradient rows, say), or into
+    a new one of ``dtype``."""
+    if x.dim() == 2 and weight.dim() == 2:
+        dx, dw = linear_cross_entropy_backward(dloss[None], x[None], weight[None], targets[None], lse[None],
+                                               dweight=None if dweight is None else dweight[None], dtype=dtype, stream=stream)
+        return dx[0], dw[0]
+    _no_autograd(dloss=dloss, x=x, weight=weight, lse=lse, dweight=dweight)
+    device = _cuda(x, "x")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return linear_cross_entropy_backward(dloss, x, weight, targets, lse, dweight=dweight, dtype=dtype)
+    (W, M, V, D), operands, targets_at, code = _head(x, weight, targets)
+    dloss_at, lse_at = _whole(dloss, "dloss", (W, M), _F32, device), _whole(lse, "lse", (W, M), _F32, device)
+    dweight = _gradient_out(dweight, "dweight", (W, V, D), dtype, device)
+    dx = torch.empty((W, M, D), dtype=x.dtype, device=device)
+    needed = _entry("cpdp_linear_cross_entropy_backward_workspace")(*operands, code, W, M, V, D)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_linear_cross_entropy_backward")(
+        dloss_at, *operands, targets_at, lse_at, code, W, M, V, D, dx.data_ptr(), dweight.data_ptr(), dweight.stride(0),
+        _CODES[dweight.dtype], _ptr(work), needed, _stream(device.index)))
+    return dx, dweight
+
+
 def wait_timeouts() -> int:
-    """Bounded waits of the weight gradient's kernel that ran out since the last
-    call (0 expected; the tiles of dW concerned are NaN). Waits for the current
-    device."""
+    """Bounded waits of the kernels of ``weight_gradient`` and of the loss that
+    ran out since the last call (0 expected; the tiles concerned are NaN). Waits
+    for the current device."""
     count = _L()
     _check(_entry("cpdp_layer_timeouts")(ctypes.byref(count)))
     return count.value
