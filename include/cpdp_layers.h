@@ -11,6 +11,10 @@
  *               backward pass, and its step for one token
  *   loss        softmax cross entropy over a vocabulary from the activations
  *               and the head's weight, without the logits; its backward pass
+ *   convolution y_t = silu(bias + sum_k weight_k x_(t-K+1+k)) over time, for each
+ *               channel; its backward pass, and its step for one token
+ *   clipping    the norm of each worker's gradient row, and the row scaled down
+ *               to a largest norm
  *
  * Layout. Arrays [W][M][D] hold worker w's M tokens (rows) of D features.
  * Features are contiguous; inputs have a worker stride and a row stride, in
@@ -236,6 +240,81 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float *dloss, const void *x
                                                cpdp_dtype dtype, int W, int64_t M, int V, int D, void *dx,
                                                void *dweight, int64_t dweight_worker, cpdp_dtype dweight_dtype,
                                                void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * cpdp_clip_gradients — norm = sqrt(sum(g^2)) of each worker's row of N
+ * gradients, and g * min(1, max_norm / norm).
+ *   grads     of dtype, worker w's N values at grads + w * grads_worker, at any
+ *             element alignment
+ *   max_norm  > 0; infinity: the rows stay as they are
+ *   norms     float32 [W]. The sum of squares is float32, in an order fixed by
+ *             the sizes and the rows' alignment, and neither overflows nor
+ *             vanishes where the norm itself is a float32 number.
+ *   out       of dtype, with a worker stride; or grads itself, with the same
+ *             stride: rows whose norm is not above max_norm are not written then
+ * A row with an infinite value has the norm infinity (0 for the finite values, NaN
+ * for the infinite ones), one with a NaN is NaN throughout. W * N is at most 2^40;
+ * with N = 0 the norms are 0.
+ */
+size_t cpdp_clip_gradients_workspace(int W, int64_t N);
+cpdp_status cpdp_clip_gradients(const void *grads, int64_t grads_worker, cpdp_dtype dtype, int W, int64_t N,
+                                float max_norm, float *norms, void *out, int64_t out_worker,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* Taps of the convolution: 2 to this many. */
+#define CPDP_CONV_MAX_TAPS 4
+
+/*
+ * cpdp_causal_conv — for B sequences of T <= 2^30 steps and D channels,
+ *   y_t = v_t * sigmoid(v_t),  v_t = bias + sum over k < K of weight[k] * x_(t-K+1+k)
+ * Worker w's weights are those of the sequences w * B / W to (w + 1) * B / W - 1
+ * (W divides B).
+ *   x        [B][T][D] of dtype, with a sequence and a step stride
+ *   weight   float32, worker w's [D][K] at weight + w * weight_worker
+ *   bias     float32, worker w's [D] at bias + w * bias_worker
+ *   state    [B][K - 1][D] of dtype, contiguous: the inputs before the first step
+ *            (NULL: 0)
+ *   lengths  int32 [B], each sequence's number of steps, clamped to 0..T (NULL: T
+ *            for all). Nothing is read beyond a length; y is 0 there.
+ *   y        [B][T][D] of dtype
+ *   last     [B][K - 1][D] of dtype: the last K - 1 inputs, of state and x
+ *            (NULL: not wanted)
+ */
+cpdp_status cpdp_causal_conv(const void *x, int64_t x_seq, int64_t x_step,
+                             const float *weight, int64_t weight_worker, const float *bias, int64_t bias_worker,
+                             const void *state, const int32_t *lengths,
+                             cpdp_dtype dtype, int W, int B, int64_t T, int D, int K,
+                             void *y, void *last, void *stream);
+
+/*
+ * cpdp_causal_conv_backward — with dv_t = dy_t * silu'(v_t), dx_t = sum over k of
+ * weight[k] * dv_(t+K-1-k), dweight[k] = sum over t of dv_t * x_(t-K+1+k) and
+ * dbias = sum over t of dv_t, over a worker's sequences.
+ *   dy       [B][T][D] of dtype, with strides; not read beyond a length
+ *   dlast    [B][K - 1][D] of dtype: the gradient of last (NULL: 0)
+ *   dx       [B][T][D] of dtype; 0 beyond a length
+ *   dstate   [B][K - 1][D] of dtype (NULL: not wanted)
+ *   dweight, dbias  dweight_dtype, worker w's [D][K] and [D] at + w * their
+ *            strides; sums are float32, in an order fixed by the sizes and by
+ *            whether every row is one of whole pieces of 4 elements
+ */
+size_t cpdp_causal_conv_backward_workspace(int W, int B, int64_t T, int D, int K);
+cpdp_status cpdp_causal_conv_backward(const void *dy, int64_t dy_seq, int64_t dy_step,
+                                      const void *x, int64_t x_seq, int64_t x_step,
+                                      const float *weight, int64_t weight_worker, const float *bias, int64_t bias_worker,
+                                      const void *state, const void *dlast, const int32_t *lengths,
+                                      cpdp_dtype dtype, int W, int B, int64_t T, int D, int K,
+                                      void *dx, void *dstate, void *dweight, int64_t dweight_worker,
+                                      void *dbias, int64_t dbias_worker, cpdp_dtype dweight_dtype,
+                                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * cpdp_causal_conv_step — one token for each of B sequences: x and y [B][D] of
+ * dtype (x with a sequence stride); state [B][K - 1][D] is moved on by x.
+ */
+cpdp_status cpdp_causal_conv_step(const void *x, int64_t x_seq, const float *weight, int64_t weight_worker,
+                                  const float *bias, int64_t bias_worker, cpdp_dtype dtype,
+                                  int W, int B, int D, int K, void *state, void *y, void *stream);
 
 /*
  * cpdp_layer_timeouts — the number of bounded waits that ran out since the last

@@ -1,0 +1,194 @@
+// Gradient norms over the workers' rows and their clipping
+// (include/cpdp_layers.h).
+#include <algorithm>
+#include <type_traits>
+
+#include "cpdp_layers.cuh"
+
+namespace cpdp {
+namespace {
+
+// norm = sqrt(sum(g^2)) of a row, out = g * min(1, max_norm / norm). Both passes
+// are bound by memory. The first leaves each block's part of the sum; in the
+// second every block adds up its row's parts, in their order, and walks the row
+// from its end, so that it begins with what is still in L2.
+constexpr int kThreads = 256, kVectors = 4;  // 16 bytes each, per thread and turn
+
+// Squares of float32 overflow from 1.8e19 on and vanish below 1e-23. Sums of
+// squares of values times 2^-96 and 2^96 stand in there.
+constexpr float kDown = 0x1p-96f, kUp = 0x1p96f;
+struct Squares {
+    float mid, down, up;
+    __device__ __forceinline__ void add(float g) {
+        mid = fmaf(g, g, mid);
+        down = fmaf(g * kDown, g * kDown, down);
+        up = fmaf(g * kUp, g * kUp, up);
+    }
+    __device__ __forceinline__ void add(const Squares& o) { mid += o.mid, down += o.down, up += o.up; }
+};
+__device__ __forceinline__ Squares over_warp(Squares s) {
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2)
+        s.add({__shfl_xor_sync(~0u, s.mid, d), __shfl_xor_sync(~0u, s.down, d), __shfl_xor_sync(~0u, s.up, d)});
+    return s;
+}
+__device__ __forceinline__ Squares over_block(Squares s) {
+    __shared__ Squares warps[kThreads / 32];
+    s = over_warp(s);
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = s;
+    __syncthreads();
+    s = warps[0];
+#pragma unroll
+    for (int i = 1; i < kThreads / 32; ++i) s.add(warps[i]);
+    return s;
+}
+// NaN where one is in the row, infinity where the norm is above the float32 range.
+__device__ __forceinline__ float norm_of(const Squares& s) {
+    if (s.mid >= 0x1p-90f && s.mid <= 0x1p100f) return sqrtf(s.mid);
+    if (s.mid < 0x1p-90f) return sqrtf(s.up) * kDown;
+    return sqrtf(s.down) * kUp;  // infinite and NaN sums too
+}
+
+// A row in 16-byte pieces: elements before the first whole piece, the pieces, and the elements after them.
+template <typename T>
+constexpr int kEach = 16 / sizeof(T);
+template <typename T>
+struct Row {
+    int64_t head, pieces;
+    __device__ __forceinline__ Row(const T* p, int64_t n) {
+        const int64_t before = ((16 - reinterpret_cast<uintptr_t>(p) % 16) % 16) / sizeof(T);
+        head = before < n ? before : n;
+        pieces = (n - head) / kEach<T>;
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+norms_kernel(const T* grads, int64_t worker, int64_t n, Squares* parts) {
+    layer_begin();
+    const T* g = grads + blockIdx.y * worker;
+    const Row<T> row(g, n);
+    Squares s{};
+    constexpr int64_t kTurn = kThreads * kVectors;
+    for (int64_t i = blockIdx.x * kTurn; i < row.pieces; i += gridDim.x * kTurn) {
+        Piece<T, kEach<T>> v[kVectors];
+#pragma unroll
+        for (int k = 0; k < kVectors; ++k) {
+            const int64_t at = i + k * kThreads + threadIdx.x;
+            if (at < row.pieces) v[k].v = *reinterpret_cast<const decltype(v[k].v)*>(g + row.head + at * kEach<T>);
+        }
+        Squares turn{};
+#pragma unroll
+        for (int k = 0; k < kVectors; ++k)
+            if (i + k * kThreads + threadIdx.x < row.pieces)
+#pragma unroll
+                for (int e = 0; e < kEach<T>; ++e) turn.add(v[k].get(e));
+        s.add(turn);
+    }
+    if (blockIdx.x == 0 && threadIdx.x < kEach<T>) {
+        const int64_t after = row.head + row.pieces * kEach<T> + threadIdx.x;
+        if (threadIdx.x < row.head) s.add(to_float(g[threadIdx.x]));
+        if (after < n) s.add(to_float(g[after]));
+    }
+    s = over_block(s);
+    if (threadIdx.x == 0) parts[blockIdx.y * gridDim.x + blockIdx.x] = s;
+}
+
+// ALIGNED: rows of out lie in 16 bytes as those of grads do.
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads)
+clip_kernel(const T* grads, int64_t worker, int64_t n, const Squares* parts, int count, float max_norm, float* norms, T* out, int64_t out_worker) {
+    layer_begin();
+    Squares s{};
+    for (int i = threadIdx.x; i < count; i += kThreads) s.add(parts[blockIdx.y * count + i]);
+    const float norm = norm_of(over_block(s));
+    if (blockIdx.x == 0 && threadIdx.x == 0) norms[blockIdx.y] = norm;
+    const float ratio = max_norm / norm, scale = ratio > 1.f ? 1.f : ratio;
+    const T* g = grads + blockIdx.y * worker;
+    T* to = out + blockIdx.y * out_worker;
+    if (g == to && scale == 1.f) return;
+    const Row<T> row(g, n);
+    constexpr int64_t kTurn = kThreads * kVectors;
+    if constexpr (ALIGNED) {
+        const int64_t turns = (row.pieces + kTurn - 1) / kTurn;
+        for (int64_t turn = turns - 1 - blockIdx.x; turn >= 0; turn -= gridDim.x) {
+            Piece<T, kEach<T>> v[kVectors];
+#pragma unroll
+            for (int k = 0; k < kVectors; ++k) {
+                const int64_t at = turn * kTurn + k * kThreads + threadIdx.x;
+                if (at < row.pieces) v[k].load(g + row.head + at * kEach<T>);
+            }
+#pragma unroll
+            for (int k = 0; k < kVectors; ++k) {
+                const int64_t at = turn * kTurn + k * kThreads + threadIdx.x;
+                float x[kEach<T>];
+#pragma unroll
+                for (int e = 0; e < kEach<T>; ++e) x[e] = v[k].get(e) * scale;
+                if (at < row.pieces) store_piece<kEach<T>>(to + row.head + at * kEach<T>, x);
+            }
+        }
+        if (blockIdx.x == 0 && threadIdx.x < kEach<T>) {
+            const int64_t after = row.head + row.pieces * kEach<T> + threadIdx.x;
+            if (threadIdx.x < row.head) to[threadIdx.x] = from_float<T>(to_float(g[threadIdx.x]) * scale);
+            if (after < n) to[after] = from_float<T>(to_float(g[after]) * scale);
+        }
+    } else {
+        const int64_t turns = (n + kThreads - 1) / kThreads;
+#pragma unroll 4
+        for (int64_t turn = turns - 1 - blockIdx.x; turn >= 0; turn -= gridDim.x) {
+            const int64_t at = turn * kThreads + threadIdx.x;
+            if (at < n) to[at] = from_float<T>(to_float(g[at]) * scale);
+        }
+    }
+}
+
+// Blocks of a row: one turn each where that is not more than run at once.
+int parts_of(int W, int64_t N) {
+    const int64_t turns = ceil_div(N * 4, kThreads * kVectors * 16), most = std::max<int64_t>(ceil_div(8 * kSMs, W), 1);
+    return static_cast<int>(std::max<int64_t>(std::min(turns, most), 1));
+}
+
+cpdp_status check_clip(int W, int64_t N) {
+    if (W < 1 || W > 4096) return layer_error(CPDP_EINVAL, "W=%d must be in [1, 4096]", W);
+    if (N < 0 || N > kLayerMaxElements / W) return layer_error(CPDP_EINVAL, "W=%d, N=%lld: W * N must be in [0, 2^40]", W, (long long)N);
+    return CPDP_OK;
+}
+
+}  // namespace
+}  // namespace cpdp
+
+using namespace cpdp;
+
+size_t cpdp_clip_gradients_workspace(int W, int64_t N) {
+    return check_clip(W, N) != CPDP_OK ? 0 : ceil_div(static_cast<int64_t>(W) * parts_of(W, N) * sizeof(Squares), 16) * 16;
+}
+
+cpdp_status cpdp_clip_gradients(const void* grads, int64_t grads_worker, cpdp_dtype dtype, int W, int64_t N, float max_norm, float* norms,
+                                void* out, int64_t out_worker, void* workspace, size_t workspace_bytes, void* stream) {
+    CPDP_TRY(check_clip(W, N));
+    if (!known_dtype(dtype)) return layer_error(CPDP_EINVAL, "unknown dtype %d", (int)dtype);
+    if (!(max_norm > 0.f)) return layer_error(CPDP_EINVAL, "max_norm=%g must be above 0", (double)max_norm);
+    const int64_t e = dtype_size(dtype);
+    CPDP_TRY(check_array("grads", grads, N > 0, e, grads_worker));
+    CPDP_TRY(check_array("norms", norms, true, 4));
+    CPDP_TRY(check_array("out", out, N > 0, e, out_worker));
+    CPDP_TRY(check_apart("out", W, out_worker, N));
+    if (out == grads && W > 1 && out_worker != grads_worker)
+        return layer_error(CPDP_EINVAL, "out is grads with another stride: %lld, not %lld", (long long)out_worker, (long long)grads_worker);
+    CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_clip_gradients_workspace(W, N)));
+    const int count = parts_of(W, N);
+    auto* parts = static_cast<Squares*>(workspace);
+    const dim3 grid(count, W);
+    const bool aligned = (reinterpret_cast<uintptr_t>(grads) - reinterpret_cast<uintptr_t>(out)) % 16 == 0 &&
+                         (W == 1 || (grads_worker - out_worker) * e % 16 == 0);
+    const auto go = [&](auto* to) {
+        using T = std::remove_pointer_t<decltype(to)>;
+        const auto* g = static_cast<const T*>(grads);
+        const cudaError_t first = launch_layer(norms_kernel<T>, grid, kThreads, 0, stream, g, grads_worker, N, parts);
+        if (first != cudaSuccess) return first;
+        return launch_layer(aligned ? clip_kernel<T, true> : clip_kernel<T, false>, grid, kThreads, 0, stream, g, grads_worker, N,
+                            static_cast<const Squares*>(parts), count, max_norm, norms, to, out_worker);
+    };
+    return layer_launched(dtype == CPDP_F32 ? go(static_cast<float*>(out)) : go(static_cast<__nv_bfloat16*>(out)), "cpdp_clip_gradients");
+}

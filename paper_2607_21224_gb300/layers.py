@@ -9,6 +9,10 @@ include/cpdp_layers.h, which make the gradients that ``CPDPState`` steps with.
   ``gated_recurrence_step``: h_t = a_t h_(t-1) + (1 - a_t) v_t, a = sigmoid(gate)
 - ``linear_cross_entropy`` / ``linear_cross_entropy_backward``: softmax cross
   entropy over a vocabulary, from the activations and the head's weight
+- ``causal_conv`` / ``causal_conv_backward`` / ``causal_conv_step``: a short
+  convolution over time for each channel, and its silu
+- ``clip_gradients``: the norms of the workers' gradient rows, and the rows
+  scaled down to a largest norm
 
 Activations are (W, M, D): W workers, M tokens each, D features, contiguous
 along D, float32 or bfloat16. One model's (M, D) is taken too, with a weight
@@ -42,6 +46,7 @@ from .state import _raw_stream
 BLOCK = 32  # features that share an exponent
 MAX_SIZE = 1 << 30  # of every axis
 CARRY_STEPS = 16  # CPDP_CARRY_STEPS
+CONV_MAX_TAPS = 4  # CPDP_CONV_MAX_TAPS
 NORM_MAX_FEATURES = 16384  # CPDP_NORM_MAX_FEATURES
 
 _P, _I, _L, _F, _Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -64,6 +69,13 @@ SIGNATURES = {
     "cpdp_linear_cross_entropy": (_I, [_P, _L, _L, _P, _L, _L, _P, _I, _I, _L, _I, _I, _P, _P, _P, _Z, _P]),
     "cpdp_linear_cross_entropy_backward_workspace": (_Z, [_P, _L, _L, _P, _L, _L, _I, _I, _L, _I, _I]),
     "cpdp_linear_cross_entropy_backward": (_I, [_P, _P, _L, _L, _P, _L, _L, _P, _P, _I, _I, _L, _I, _I, _P, _P, _L, _I, _P, _Z, _P]),
+    "cpdp_clip_gradients_workspace": (_Z, [_I, _L]),
+    "cpdp_clip_gradients": (_I, [_P, _L, _I, _I, _L, _F, _P, _P, _L, _P, _Z, _P]),
+    "cpdp_causal_conv": (_I, [_P, _L, _L, _P, _L, _P, _L, _P, _P, _I, _I, _I, _L, _I, _I, _P, _P, _P]),
+    "cpdp_causal_conv_backward_workspace": (_Z, [_I, _I, _L, _I, _I]),
+    "cpdp_causal_conv_backward": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _P, _L, _P, _P, _P, _I, _I, _I, _L, _I, _I, _P, _P, _P, _L, _P,
+                                       _L, _I, _P, _Z, _P]),
+    "cpdp_causal_conv_step": (_I, [_P, _L, _P, _L, _P, _L, _I, _I, _I, _I, _I, _P, _P, _P]),
     "cpdp_layer_timeouts": (_I, [ctypes.POINTER(_L)]),
 }
 
@@ -541,6 +553,171 @@ def linear_cross_entropy_backward(dloss, x, weight, targets, lse, *, dweight=Non
         dloss_at, *operands, targets_at, lse_at, code, W, M, V, D, dx.data_ptr(), dweight.data_ptr(), dweight.stride(0),
         _CODES[dweight.dtype], _ptr(work), needed, _stream(device.index)))
     return dx, dweight
+
+
+def _workers_part(t, name: str, tail: tuple, W: int, device) -> int:
+    """The worker stride of float32 weights (W, *tail) whose parts are contiguous each."""
+    shape = (W, *tail)
+    if t.shape != shape or t.dtype is not _F32 or t.device != device:
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+        if t.dtype != _F32:
+            raise TypeError(f"{name} must be float32, got {t.dtype}")
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if not t.is_contiguous() and not t[0].is_contiguous():
+        raise ValueError(f"each worker's part of {name} must be contiguous")
+    return t.stride(0)
+
+
+def _per_worker(B: int, weight, name: str, dims: int) -> int:
+    """The number of workers whose weights these are; their sequences are neighbours."""
+    if weight.dim() != dims:
+        raise ValueError(f"{name} must have {dims} axes, the workers' first; got {tuple(weight.shape)}")
+    W = weight.shape[0]
+    if W < 1 or B % W:
+        raise ValueError(f"{B} sequences are not as many for each of {W} workers")
+    return W
+
+
+def _sequence_shape(t, name: str) -> tuple:
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be (B, T, D), got {tuple(t.shape)}")
+    _dtype(t, name)
+    return _sized(t, name)
+
+
+def causal_conv(x, weight, bias, state=None, lengths=None, *, stream=None):
+    """y_t = silu(bias + sum_k weight[k] x_(t-K+1+k)), for B sequences: (y, last).
+
+    x (B, T, D) float32 or bfloat16; weight float32 (W, D, K) with K from 2 to
+    CONV_MAX_TAPS and bias (W, D): those of worker w are for the w-th of W equal
+    groups of sequences (one model's (D, K) and (D,) are taken too). state
+    (B, K - 1, D) of x's type holds the inputs before the first step (None:
+    zeros), last the ones before the next. lengths int32 (B,) or None: beyond its
+    length a sequence is not read and y is 0."""
+    if weight.dim() == 2 and bias.dim() == 1:
+        weight, bias = weight[None], bias[None]
+    _no_autograd(x=x, weight=weight, bias=bias, state=state)
+    device = _cuda(x, "x")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return causal_conv(x, weight, bias, state, lengths)
+    B, T, D = shape = _sequence_shape(x, "x")
+    dtype = x.dtype
+    W, K = _per_worker(B, weight, "weight", 3), weight.shape[2]
+    xs = _input(x, "x", shape, dtype, device)
+    ws, bs = _workers_part(weight, "weight", (D, K), W, device), _workers_part(bias, "bias", (D,), W, device)
+    state_at, n_at = _whole(state, "state", (B, K - 1, D), dtype, device), _whole(lengths, "lengths", (B,), torch.int32, device)
+    y = torch.empty(shape, dtype=dtype, device=device)
+    last = torch.empty((B, max(K - 1, 0), D), dtype=dtype, device=device)
+    _check(_entry("cpdp_causal_conv")(x.data_ptr(), xs[0], xs[1], weight.data_ptr(), ws, bias.data_ptr(), bs, state_at, n_at, _CODES[dtype],
+                                      W, B, T, D, K, y.data_ptr(), last.data_ptr(), _stream(device.index)))
+    return y, last
+
+
+def causal_conv_backward(dy, x, weight, bias, state=None, lengths=None, dlast=None, *, dweight=None, dbias=None, dstate=None,
+                         dtype=torch.float32, stream=None):
+    """Gradients of ``causal_conv``: (dx, dweight, dbias) from dy (B, T, D) and
+    dlast (B, K - 1, D) or None. dweight (W, D, K) and dbias (W, D) are written
+    into the tensors given, float32 or bfloat16 both (views of the gradient rows,
+    say), or into new ones of ``dtype``. Where dstate, (B, K - 1, D) of x's type,
+    is given, the gradient of state is written there."""
+    if weight.dim() == 2 and bias.dim() == 1:
+        dx, dw, db = causal_conv_backward(dy, x, weight[None], bias[None], state, lengths, dlast, dweight=None if dweight is None else dweight[None],
+                                          dbias=None if dbias is None else dbias[None], dstate=dstate, dtype=dtype, stream=stream)
+        return dx, dw[0], db[0]
+    _no_autograd(dy=dy, x=x, weight=weight, bias=bias, state=state, dlast=dlast, dweight=dweight, dbias=dbias, dstate=dstate)
+    device = _cuda(x, "x")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return causal_conv_backward(dy, x, weight, bias, state, lengths, dlast, dweight=dweight, dbias=dbias, dstate=dstate, dtype=dtype)
+    B, T, D = shape = _sequence_shape(x, "x")
+    kind = x.dtype
+    W, K = _per_worker(B, weight, "weight", 3), weight.shape[2]
+    xs, gs = _input(x, "x", shape, kind, device), _input(dy, "dy", shape, kind, device)
+    ws, bs = _workers_part(weight, "weight", (D, K), W, device), _workers_part(bias, "bias", (D,), W, device)
+    few = (B, K - 1, D)
+    state_at, n_at = _whole(state, "state", few, kind, device), _whole(lengths, "lengths", (B,), torch.int32, device)
+    dlast_at, dstate_at = _whole(dlast, "dlast", few, kind, device), _whole(dstate, "dstate", few, kind, device)
+    if dweight is not None:
+        dtype = dweight.dtype
+    elif dbias is not None:
+        dtype = dbias.dtype
+    dweight, dbias = _gradient_out(dweight, "dweight", (W, D, K), dtype, device), _gradient_out(dbias, "dbias", (W, D), dtype, device)
+    if dbias.dtype != dtype:
+        raise TypeError(f"dweight and dbias must have one type, got {dtype} and {dbias.dtype}")
+    dx = torch.empty(shape, dtype=kind, device=device)
+    needed = _entry("cpdp_causal_conv_backward_workspace")(W, B, T, D, K)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_causal_conv_backward")(
+        dy.data_ptr(), gs[0], gs[1], x.data_ptr(), xs[0], xs[1], weight.data_ptr(), ws, bias.data_ptr(), bs, state_at, dlast_at, n_at,
+        _CODES[kind], W, B, T, D, K, dx.data_ptr(), dstate_at, dweight.data_ptr(), dweight.stride(0), dbias.data_ptr(), dbias.stride(0),
+        _CODES[dtype], _ptr(work), needed, _stream(device.index)))
+    return dx, dweight, dbias
+
+
+def causal_conv_step(x, weight, bias, state, *, stream=None):
+    """One token for each of B sequences: x (B, D) gives y (B, D), and ``state``
+    (B, K - 1, D), the inputs before it, is moved on by x."""
+    if weight.dim() == 2 and bias.dim() == 1:
+        weight, bias = weight[None], bias[None]
+    shape, dtype, device, wshape = x.shape, x.dtype, x.device, weight.shape
+    xs, ws, bs, code = x.stride(), weight.stride(), bias.stride(), _CODES.get(dtype)
+    # one test where all is well: a decoding step costs what Python does around it
+    if not (stream is None and code is not None and x.is_cuda and device.index == _current_device() and len(shape) == 2 and len(wshape) == 3
+            and wshape[0] > 0 and shape[0] % wshape[0] == 0 and max(shape) <= MAX_SIZE and shape[1] == wshape[1] and xs[-1] == 1
+            and weight.dtype is _F32 is bias.dtype and ws[1:] == (wshape[2], 1) and bias.shape == wshape[:2] and bs[1] == 1
+            and state.dtype is dtype and state.shape == (shape[0], wshape[2] - 1, shape[1]) and state.is_contiguous()
+            and weight.device == device == bias.device == state.device
+            and not (x.requires_grad or weight.requires_grad or bias.requires_grad or state.requires_grad)):
+        _no_autograd(x=x, weight=weight, bias=bias, state=state)
+        if _elsewhere(_cuda(x, "x"), stream):
+            with _there(device, stream):
+                return causal_conv_step(x, weight, bias, state)
+        code = _dtype(x, "x")
+        if len(shape) != 2:
+            raise ValueError(f"x must be (B, D), got {tuple(shape)}")
+        B, D = _sized(x, "x")
+        W = _per_worker(B, weight, "weight", 3)
+        _input(x, "x", shape, dtype, device)
+        _workers_part(weight, "weight", (D, wshape[2]), W, device)
+        _workers_part(bias, "bias", (D,), W, device)
+        _whole(state, "state", (B, wshape[2] - 1, D), dtype, device)
+    B, D = shape
+    y = torch.empty(shape, dtype=dtype, device=device)
+    _check(_entry("cpdp_causal_conv_step")(x.data_ptr(), xs[0], weight.data_ptr(), ws[0], bias.data_ptr(), bs[0], code, wshape[0], B, D, wshape[2],
+                                           state.data_ptr(), y.data_ptr(), _stream(device.index)))
+    return y
+
+
+def clip_gradients(grads, max_norm: float, *, out=None, stream=None):
+    """The norm of each worker's row of grads (W, N), float32 (W,), and the rows
+    times min(1, max_norm / norm): written into ``out``, of grads' shape and type,
+    or over grads where none is given (rows that are within max_norm are left as
+    they are then). grads float32 or bfloat16; its rows may be slices of longer
+    ones. One model's (N,) is taken too."""
+    if grads.dim() == 1:
+        return clip_gradients(grads[None], max_norm, out=None if out is None else out[None], stream=stream)[0]
+    _no_autograd(grads=grads, out=out)
+    device = _cuda(grads, "grads")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return clip_gradients(grads, max_norm, out=out)
+    if grads.dim() != 2:
+        raise ValueError(f"grads must be (W, N), or (N,) of one model; got {tuple(grads.shape)}")
+    shape, dtype, code = grads.shape, grads.dtype, _dtype(grads, "grads")
+    if out is None:
+        out = grads
+    gs, os = _input(grads, "grads", shape, dtype, device), _input(out, "out", shape, dtype, device)
+    W, N = shape
+    norms = torch.empty((W,), dtype=_F32, device=device)
+    if W == 0:
+        return norms
+    needed = _entry("cpdp_clip_gradients_workspace")(W, N)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_clip_gradients")(grads.data_ptr(), gs[0], code, W, N, max_norm, norms.data_ptr(), out.data_ptr(), os[0], _ptr(work),
+                                         needed, _stream(device.index)))
+    return norms
 
 
 def wait_timeouts() -> int:
