@@ -13,6 +13,9 @@
  *               and the head's weight, without the logits; its backward pass
  *   convolution y_t = silu(bias + sum_k weight_k x_(t-K+1+k)) over time, for each
  *               channel; its backward pass, and its step for one token
+ *   scan        h_t = exp(-dt exp(a_log)) h_(t-1) + dt u_t b_t for some states per
+ *               channel, y_t = (sum_n c_t h_t + skip u_t) silu(z_t); its backward
+ *               pass, and its step for one token
  *   clipping    the norm of each worker's gradient row, and the row scaled down
  *               to a largest norm
  *
@@ -315,6 +318,91 @@ cpdp_status cpdp_causal_conv_backward(const void *dy, int64_t dy_seq, int64_t dy
 cpdp_status cpdp_causal_conv_step(const void *x, int64_t x_seq, const float *weight, int64_t weight_worker,
                                   const float *bias, int64_t bias_worker, cpdp_dtype dtype,
                                   int W, int B, int D, int K, void *state, void *y, void *stream);
+
+/* States per channel of the scan: 1 to this many. */
+#define CPDP_SCAN_MAX_STATES 32
+
+/*
+ * Inputs of the scan of B sequences of T <= 2^30 steps, D channels and N states
+ * per channel. Worker w's weights are those of the sequences w * B / W to
+ * (w + 1) * B / W - 1 (W divides B).
+ *   u, delta, z  [B][T][D] of dtype, each with a sequence and a step stride; z
+ *            NULL: no gate, silu(z) is 1
+ *   b, c     [B][T][N] of dtype, with strides
+ *   a_log, skip, bias  float32, worker w's [D][N], [D] and [D] at + w * their
+ *            strides
+ *   lengths  int32 [B], each sequence's number of steps, clamped to 0..T (NULL: T
+ *            for all)
+ */
+typedef struct cpdp_scan_inputs {
+    const void *u;
+    int64_t u_seq, u_step;
+    const void *delta;
+    int64_t delta_seq, delta_step;
+    const void *z;
+    int64_t z_seq, z_step;
+    const void *b;
+    int64_t b_seq, b_step;
+    const void *c;
+    int64_t c_seq, c_step;
+    const float *a_log;
+    int64_t a_log_worker;
+    const float *skip;
+    int64_t skip_worker;
+    const float *bias;
+    int64_t bias_worker;
+    const int32_t *lengths;
+} cpdp_scan_inputs;
+
+/*
+ * cpdp_selective_scan — with dt = log(1 + exp(delta + bias)),
+ *   h_t[n] = exp(-dt_t exp(a_log[n])) h_(t-1)[n] + dt_t u_t b_t[n]
+ *   y_t = (sum over n of c_t[n] h_t[n] + skip u_t) z_t sigmoid(z_t)
+ *   h0       float32 [B][D][N], the states before the first step (NULL: 0)
+ *   y        [B][T][D] of dtype; nothing is read beyond a length, y is 0 there
+ *            and the states stay
+ *   last     float32 [B][D][N], the states after the last step
+ *   carry    NULL, or float32 [B][ceil(T / CPDP_CARRY_STEPS)][D][N]: the states
+ *            before steps 0, CPDP_CARRY_STEPS, ..., for the backward pass
+ *            (defined up to each sequence's length)
+ * States and sums are float32. A decay x = exp(-p) is off by at most
+ * (2 + 2 p) 2^-23 of it. B * T * D is at most 2^34.
+ */
+size_t cpdp_selective_scan_workspace(int B, int64_t T, int D, int N);
+cpdp_status cpdp_selective_scan(const cpdp_scan_inputs *inputs, cpdp_dtype dtype, int W, int B, int64_t T, int D, int N,
+                                const float *h0, void *y, float *last, float *carry,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * cpdp_selective_scan_backward — the gradients of all inputs of the scan.
+ *   dy       [B][T][D] of dtype, with strides; not read beyond a length
+ *   carry    what the forward pass wrote; the states between are made again
+ *   dlast    float32 [B][D][N], the gradient of last (NULL: 0)
+ *   du, ddelta, dz  [B][T][D] of dtype; 0 beyond a length; dz may be NULL where
+ *            there is no z
+ *   db, dc   [B][T][N] of dtype; 0 beyond a length
+ *   dh0      float32 [B][D][N] (NULL: not wanted)
+ *   da_log, dskip, dbias  dweight_dtype, worker w's [D][N], [D] and [D] at + w *
+ *            their strides. Sums are float32, in an order fixed by the sizes.
+ */
+size_t cpdp_selective_scan_backward_workspace(int B, int64_t T, int D, int N);
+cpdp_status cpdp_selective_scan_backward(const void *dy, int64_t dy_seq, int64_t dy_step,
+                                         const cpdp_scan_inputs *inputs, cpdp_dtype dtype,
+                                         int W, int B, int64_t T, int D, int N,
+                                         const float *carry, const float *dlast,
+                                         void *du, void *ddelta, void *dz, void *db, void *dc, float *dh0,
+                                         void *da_log, int64_t da_log_worker, void *dskip, int64_t dskip_worker,
+                                         void *dbias, int64_t dbias_worker, cpdp_dtype dweight_dtype,
+                                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * cpdp_selective_scan_step — one token for each of B sequences: inputs of one
+ * step ([B][D] and [B][N], with the sequence strides; lengths and step strides
+ * are not looked at); state (float32 [B][D][N]) is replaced by the next one, and
+ * y ([B][D] of dtype) receives the output.
+ */
+cpdp_status cpdp_selective_scan_step(const cpdp_scan_inputs *inputs, cpdp_dtype dtype, int W, int B, int D, int N,
+                                     float *state, void *y, void *stream);
 
 /*
  * cpdp_layer_timeouts — the number of bounded waits that ran out since the last

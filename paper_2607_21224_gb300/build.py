@@ -16,7 +16,8 @@ INCLUDE = ROOT / "include"
 CSRC = PKG / "csrc"
 SOURCES = [CSRC / "cpdp.cu", CSRC / "cpdp_ragged.cu", CSRC / "cpdp_split.cu", CSRC / "cpdp_norm.cu",
            CSRC / "cpdp_checkpoint.cu", CSRC / "cpdp_weight_gradient.cu", CSRC / "cpdp_recurrence.cu",
-           CSRC / "cpdp_loss.cu", CSRC / "cpdp_clip.cu", CSRC / "cpdp_conv.cu"]
+           CSRC / "cpdp_loss.cu", CSRC / "cpdp_clip.cu", CSRC / "cpdp_conv.cu",
+           CSRC / "cpdp_scan.cu"]
 DEPENDS = SOURCES + [CSRC / "cpdp_kernels.cuh", CSRC / "cpdp_shapes.cuh", CSRC / "cpdp_tma.cuh",
                      CSRC / "cpdp_floor.cuh", CSRC / "cpdp_shuffle.cuh", CSRC / "cpdp_split.cuh",
                      CSRC / "cpdp_launch.cuh", CSRC / "cpdp_layers.cuh", CSRC / "cpdp_tensor.cuh", CSRC / "cpdp_gates.cuh",

@@ -2,6 +2,7 @@
 // argument checks, launches, and loads and stores of the two element types.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
@@ -89,6 +90,20 @@ cudaError_t launch_layer(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Lets a kernel have `bytes` of dynamic shared memory, once per device.
+template <auto KERNEL>
+cudaError_t allow_shared_memory(int bytes) {
+    static std::atomic<uint64_t> allowed{0};  // the devices on which this kernel has been allowed its shared memory
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+    if (e == cudaSuccess && (allowed.load() & bit) == 0) {
+        e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) allowed |= bit;
+    }
+    return e;
 }
 
 #ifdef __CUDACC__

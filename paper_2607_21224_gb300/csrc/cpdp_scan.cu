@@ -1,0 +1,1081 @@
+// The selective state space scan h_t = exp(-dt exp(a_log)) h_(t-1) + dt u_t b_t,
+// y_t = (sum_n c_t h_t + skip u_t) silu(z_t), dt = softplus(delta + bias), its
+// backward pass and its single step (include/cpdp_layers.h).
+#include <algorithm>
+#include <type_traits>
+
+#include "cpdp_gates.cuh"
+#include "cpdp_sums.cuh"
+
+namespace cpdp {
+namespace {
+
+// A warp takes kColumn neighbouring channels of a sequence (a column) with all
+// of their states, which are registers: S neighbouring lanes share the states of
+// C channels, each 4 of every channel's. So a sum over states passes through S
+// lanes, one over channels (the gradients of b and c) through 32 / S, after C
+// channels were added up in registers; S = C = 4 at 16 states takes the fewest
+// steps between lanes. Channels lie in pairs of registers, states apart.
+//
+// Chunks of R steps: their inputs are taken by lanes side by side along the
+// channels, two neighbours each, which make dt and dt u; these go through shared
+// memory to the walk and the walk's sums back. What the walk needs of b and c
+// lies there twice, for the pairs.
+template <int S_, int C_>
+struct Shape {
+    static constexpr int S = S_, C = C_, P = C / 2, kColumn = 32 / S * C, kStates = 4 * S;
+};
+constexpr int R = CPDP_CARRY_STEPS;
+constexpr int kBackwardWarps = 4;  // of a block of the backward pass, at most
+constexpr int kForwardBlocks = 12, kBackwardBlocks = 2;  // per SM
+constexpr float kLn2f = kLn2;
+
+struct Rows {
+    const void* p;
+    int64_t seq, step;
+};
+
+struct Scan {
+    Rows u, delta, z, b, c;  // z.p NULL: no gate
+    const float *a_log, *skip, *bias;
+    int64_t a_worker, skip_worker, bias_worker;
+    const int32_t* lengths;
+    int B, T, D, N, each;    // sequences of a worker
+    int groups;              // columns of a sequence
+    // Steps in `count` segments of `steps` (a multiple of R) where there are few columns: a first pass makes each
+    // segment's map of the state, exp(A sum(dt)) h + what the segment adds, a second one composes those before its own.
+    int count, steps;
+    Pair* maps;              // [column][segment][P * 5][32 lanes]
+};
+
+__device__ __forceinline__ float load_if(const float* p, bool there) {
+    float v = 0.f;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.f32 %0, [%1];\n\t}" : "+f"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t load_word_if(const void* p, bool there) {
+    uint32_t v = 0;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t load_half_if(const void* p, bool there) {
+    uint32_t v = 0;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u16 %0, [%1];\n\t}" : "+r"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
+    return v;
+}
+__device__ __forceinline__ Pair load_pair_if(const void* p, bool there) {
+    Pair v = 0;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.b64 %0, [%1];\n\t}" : "+l"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
+    return v;
+}
+
+// Two neighbouring elements as they lie in memory. WIDE: at a multiple of their size; the second is there where the first is.
+template <typename T, bool WIDE>
+struct Two;
+template <>
+struct Two<float, true> {
+    Pair v;
+    __device__ __forceinline__ void load(const float* p, bool first, bool) { v = load_pair_if(p, first); }
+    __device__ __forceinline__ Pair get() const { return v; }
+};
+template <>
+struct Two<float, false> {
+    float x, y;
+    __device__ __forceinline__ void load(const float* p, bool first, bool second) { x = load_if(p, first), y = load_if(p + 1, second); }
+    __device__ __forceinline__ Pair get() const { return pair(x, y); }
+};
+template <>
+struct Two<__nv_bfloat16, true> {
+    uint32_t v;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool first, bool) { v = load_word_if(p, first); }
+    __device__ __forceinline__ Pair get() const { return pair(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+};
+template <>
+struct Two<__nv_bfloat16, false> {
+    uint32_t x, y;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool first, bool second) {
+        x = load_half_if(p, first), y = load_half_if(p + 1, second);
+    }
+    __device__ __forceinline__ Pair get() const { return pair(__uint_as_float(x << 16), __uint_as_float(y << 16)); }
+};
+__device__ __forceinline__ uint32_t load_bits(const float* p, bool there) { return __float_as_uint(load_if(p, there)); }
+__device__ __forceinline__ uint32_t load_bits(const __nv_bfloat16* p, bool there) { return load_half_if(p, there) << 16; }
+
+template <bool WIDE>
+__device__ __forceinline__ void store_two(float* p, Pair both, bool second) {
+    const float2 v = floats(both);
+    if (WIDE) {
+        *reinterpret_cast<Pair*>(p) = both;
+    } else {
+        p[0] = v.x;
+        if (second) p[1] = v.y;
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void store_two(__nv_bfloat16* p, Pair both, bool second) {
+    const float2 v = floats(both);
+    if (WIDE) {
+        *reinterpret_cast<__nv_bfloat162*>(p) = __float22bfloat162_rn(v);
+    } else {
+        p[0] = __float2bfloat16_rn(v.x);
+        if (second) p[1] = __float2bfloat16_rn(v.y);
+    }
+}
+
+// softplus(x) = max(x, 0) + log(1 + t) with t = e^-|x|, and sigmoid(x). With s = t / (2 + t), at most 1/3,
+// log(1 + t) = 2 artanh(s) = 2 s (1 + s^2 / 3 + s^4 / 5 + ...), of which seven terms leave out 1.4e-8.
+template <typename T>
+__device__ __forceinline__ Pair softplus(Pair x) {
+    const float2 v = floats(x);
+    const Pair t = exp_of_minus<T>(v);
+    const float2 d = floats(add2(t, twice(2.f)));
+    const Pair s = mul2(t, pair(reciprocal(d.x), reciprocal(d.y))), q = mul2(s, s);
+    Pair sum = fma2(q, twice(1.f / 13.f), twice(1.f / 11.f));
+    sum = fma2(q, sum, twice(1.f / 9.f));
+    sum = fma2(q, sum, twice(1.f / 7.f));
+    sum = fma2(q, sum, twice(1.f / 5.f));
+    sum = fma2(q, sum, twice(1.f / 3.f));
+    sum = fma2(q, sum, kOnes);
+    return fma2(add2(s, s), sum, pair(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)));
+}
+
+// The decays 2^(dt A) of two channels, A = -exp(a_log) log2(e).
+__device__ __forceinline__ Pair decay_of(Pair dt, Pair A) {
+    const float2 x = floats(mul2(dt, A));
+    return pair(power_of_minus(-x.x), power_of_minus(-x.y));
+}
+__device__ __forceinline__ Pair shuffle(Pair v, int mask) { return __shfl_xor_sync(~0u, v, mask); }
+
+struct Task {
+    int64_t column;
+    int b, first_channel, order, group;
+};
+
+// The lane's place in the walk: states 4 q .. 4 q + 3 of C channels, pairs and states in an order of the lane's own, so
+// that what a sum between lanes keeps and what it sends lie in the same registers of every lane.
+template <typename X>
+struct Lane {
+    int lane, q, g, turn, channel;  // channel: of the column, the lane's first
+    __device__ __forceinline__ Lane()
+        : lane(threadIdx.x % 32), q(lane % X::S), g(lane / X::S), turn((g & 1) << 1 | (g >> 1 & 1)), channel(g * X::C) {}
+    __device__ __forceinline__ int pair_at(int p) const { return X::P == 2 ? channel + 2 * (p ^ (q & 1)) : channel; }
+    // Of sums of pairs over states, the channel's whose sum the lane gets.
+    __device__ __forceinline__ int summed_channel() const {
+        return X::P == 2 ? channel + 2 * (q & 1) + (q >> 1 & 1) : channel + (q & 1);
+    }
+};
+// Sums over the S lanes of a group.
+template <typename X>
+__device__ __forceinline__ float over_states(const Lane<X>& l, const Pair (&v)[X::P]) {
+    if constexpr (X::P == 2) {
+        const float2 r = floats(add2(v[0], shuffle(v[1], 1)));
+        const bool high = l.q & 2;
+        float s = (high ? r.y : r.x) + __shfl_xor_sync(~0u, high ? r.x : r.y, 2);
+        if constexpr (X::S == 8) s += __shfl_xor_sync(~0u, s, 4);
+        return s;
+    } else {
+        const float2 r = floats(v[0]);
+        const bool high = l.q & 1;
+        return (high ? r.y : r.x) + __shfl_xor_sync(~0u, high ? r.x : r.y, 1);
+    }
+}
+// Sums over the groups of lanes: of x and y for the lane's 4 states (in its order). The lane gets that of state
+// 4 q + turn; of x, of y where `second`, or of both (S = 8).
+template <typename X>
+__device__ __forceinline__ float2 over_channels(const Lane<X>& l, const float (&x)[4], const float (&y)[4]) {
+    const auto add = [](float keep, float send, int mask) { return keep + __shfl_xor_sync(~0u, send, mask); };
+    const float x0 = add(x[0], x[2], X::S), x1 = add(x[1], x[3], X::S), y0 = add(y[0], y[2], X::S), y1 = add(y[1], y[3], X::S);
+    const float xs = add(x0, x1, 2 * X::S), ys = add(y0, y1, 2 * X::S);
+    if constexpr (X::S == 8) {
+        return make_float2(xs, ys);
+    } else {
+        const bool second = l.g & 4;
+        float s = add(second ? ys : xs, second ? xs : ys, 4 * X::S);
+        if constexpr (X::S == 2) s += __shfl_xor_sync(~0u, s, 16);
+        return make_float2(s, s);
+    }
+}
+
+// 4 neighbouring values of two channels' rows [channel][N] of float32, in the lane's order, from and to memory.
+template <typename X>
+struct States {
+    int first, N, turn;
+    bool quads;  // N a multiple of 4 and rows at multiples of 16 bytes
+    __device__ __forceinline__ States(const Lane<X>& l, int n, bool aligned, bool turned)
+        : first(4 * l.q), N(n), turn(turned ? l.turn : 0), quads(aligned) {}
+    __device__ __forceinline__ void row(const float* p, bool there, float (&v)[4]) const {
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (quads) {
+            if (there && first < N) f = *reinterpret_cast<const float4*>(p + first);
+        } else if (there) {
+            if (first < N) f.x = p[first];
+            if (first + 1 < N) f.y = p[first + 1];
+            if (first + 2 < N) f.z = p[first + 2];
+            if (first + 3 < N) f.w = p[first + 3];
+        }
+        if (turn & 2) f = make_float4(f.z, f.w, f.x, f.y);
+        if (turn & 1) f = make_float4(f.y, f.x, f.w, f.z);
+        v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+    }
+    __device__ __forceinline__ void put_row(float* p, bool there, const float (&v)[4]) const {
+        if (!there) return;
+        float4 f = make_float4(v[0], v[1], v[2], v[3]);
+        if (turn & 1) f = make_float4(f.y, f.x, f.w, f.z);
+        if (turn & 2) f = make_float4(f.z, f.w, f.x, f.y);
+        if (quads) {
+            if (first < N) *reinterpret_cast<float4*>(p + first) = f;
+        } else {
+            if (first < N) p[first] = f.x;
+            if (first + 1 < N) p[first + 1] = f.y;
+            if (first + 2 < N) p[first + 2] = f.z;
+            if (first + 3 < N) p[first + 3] = f.w;
+        }
+    }
+    __device__ __forceinline__ void get(const float* p, bool first_there, bool second_there, Pair (&v)[4]) const {
+        float x[4], y[4];
+        row(p, first_there, x);
+        row(p + N, second_there, y);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = pair(x[j], y[j]);
+    }
+    __device__ __forceinline__ void put(float* p, bool first_there, bool second_there, const Pair (&v)[4]) const {
+        float x[4], y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = floats(v[j]).x, y[j] = floats(v[j]).y;
+        put_row(p, first_there, x);
+        put_row(p + N, second_there, y);
+    }
+};
+
+template <typename X>
+__device__ __forceinline__ void rates(const Scan& s, const Lane<X>& l, int b, int first_channel, bool turned, Pair (&A)[X::P][4]) {
+    const States<X> states(l, s.N, false, turned);
+    const float* rows = s.a_log + b / s.each * s.a_worker;
+#pragma unroll
+    for (int p = 0; p < X::P; ++p) {
+        const int d = first_channel + l.pair_at(p);
+        float x[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            states.row(rows + (int64_t)(d + i) * s.N, d + i < s.D, x[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = 4 * l.q + (turned ? j ^ l.turn : j);
+                x[i][j] = d + i < s.D && n < s.N ? -kLog2eHigh * expf(x[i][j]) : 0.f;  // 0: a state that stays 0
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) A[p][j] = pair(x[0][j], x[1][j]);
+    }
+}
+
+// h before the task's segment: the maps of those before it applied to h.
+template <typename X>
+__device__ __forceinline__ void state_before(const Scan& s, int64_t column, int order, const Pair (&A)[X::P][4], Pair (&h)[X::P][4]) {
+    const Pair* maps = s.maps + column * s.count * (X::P * 5 * 32) + threadIdx.x % 32;
+#pragma unroll 4
+    for (int i = 0; i < order; ++i, maps += X::P * 5 * 32)
+#pragma unroll
+        for (int p = 0; p < X::P; ++p) {
+            const Pair dt = maps[(p * 5 + 4) * 32];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h[p][j] = fma2(decay_of(dt, A[p][j]), h[p][j], maps[(p * 5 + j) * 32]);
+        }
+}
+template <typename X>
+__device__ __forceinline__ void put_map(const Scan& s, int64_t column, int order, const Pair (&h)[X::P][4], const Pair (&dt)[X::P]) {
+    Pair* maps = s.maps + (column * s.count + order) * (X::P * 5 * 32) + threadIdx.x % 32;
+#pragma unroll
+    for (int p = 0; p < X::P; ++p) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) maps[(p * 5 + j) * 32] = h[p][j];
+        maps[(p * 5 + 4) * 32] = dt[p];
+    }
+}
+
+// A chunk's inputs on their way: each lane has two neighbouring channels of kItems steps, and kFew values of b and c.
+template <typename X>
+struct Side {
+    static constexpr int kLanes = X::kColumn / 2, kDown = 32 / kLanes, kItems = R / kDown, kFew = R * X::kStates / 32;
+    int channel, row;
+    __device__ __forceinline__ Side() : channel(threadIdx.x % 32 % kLanes * 2), row(threadIdx.x % 32 / kLanes) {}
+};
+template <typename T, bool WIDE, typename X>
+struct Wide {
+    Two<T, WIDE> v[Side<X>::kItems];
+    // Rows of the chunk whose first is `p` (the column's first channel).
+    __device__ __forceinline__ void load(const Side<X>& side, const T* p, int64_t step, int rows, int channels) {
+#pragma unroll
+        for (int i = 0; i < Side<X>::kItems; ++i) {
+            const int r = side.row + i * Side<X>::kDown;
+            v[i].load(p + r * step + side.channel, r < rows && side.channel < channels, r < rows && side.channel + 1 < channels);
+        }
+    }
+};
+
+template <typename X>
+struct ForwardShared {
+    float dt[R][X::kColumn], x[R][X::kColumn], sum[R][X::kColumn];
+    float4 bc[R][X::kStates];
+};
+
+// MAPS: the first pass, which makes the segment's map.
+template <typename T, bool WIDE, bool MAPS, typename X>
+__global__ void __launch_bounds__(32, kForwardBlocks)
+scan_kernel(Scan s, const float* h0, T* y, float* last, float* carry, bool quads) {
+    layer_begin();
+    __shared__ ForwardShared<X> m;
+    const Lane<X> l;
+    const Side<X> side;
+    const int lane = l.lane;
+    const int64_t column = blockIdx.x / s.count;
+    const int order = static_cast<int>(blockIdx.x - column * s.count), b = static_cast<int>(column / s.groups);
+    if (MAPS && order == s.count - 1) return;  // nobody asks for the last one
+    const int d0 = static_cast<int>(column - (int64_t)b * s.groups) * X::kColumn, channels = s.D - d0, worker = b / s.each;
+    const int n = s.lengths == nullptr ? s.T : min(max(s.lengths[b], 0), s.T);
+    const int first = order * s.steps, end = min(first + s.steps, s.T), inside = min(max(n - first, 0), max(end - first, 0));
+    const T* u = static_cast<const T*>(s.u.p) + b * s.u.seq + first * s.u.step + d0;
+    const T* delta = static_cast<const T*>(s.delta.p) + b * s.delta.seq + first * s.delta.step + d0;
+    const T* z = s.z.p == nullptr ? nullptr : static_cast<const T*>(s.z.p) + b * s.z.seq + first * s.z.step + d0;
+    const T* bs = static_cast<const T*>(s.b.p) + b * s.b.seq + first * s.b.step;
+    const T* cs = static_cast<const T*>(s.c.p) + b * s.c.seq + first * s.c.step;
+
+    Wide<T, WIDE, X> next_u, next_delta, next_z;
+    uint32_t next_b[Side<X>::kFew], next_c[Side<X>::kFew];
+    const auto fetch = [&](int t) {
+        const int rows = inside - t;
+        next_u.load(side, u + t * s.u.step, s.u.step, rows, channels);
+        next_delta.load(side, delta + t * s.delta.step, s.delta.step, rows, channels);
+        if (!MAPS && z != nullptr) next_z.load(side, z + t * s.z.step, s.z.step, rows, channels);
+#pragma unroll
+        for (int i = 0; i < Side<X>::kFew; ++i) {
+            const int r = (i * 32 + lane) / X::kStates, k = (i * 32 + lane) % X::kStates;
+            next_b[i] = load_bits(bs + (t + r) * s.b.step + k, r < rows && k < s.N);
+            if (!MAPS) next_c[i] = load_bits(cs + (t + r) * s.c.step + k, r < rows && k < s.N);
+        }
+    };
+    fetch(0);
+
+    const States<X> states(l, s.N, quads, false);
+    Pair A[X::P][4], h[X::P][4], sum_dt[X::P];
+    rates<X>(s, l, b, d0, false, A);
+#pragma unroll
+    for (int p = 0; p < X::P; ++p) {
+        sum_dt[p] = kZeros;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[p][j] = kZeros;
+        const int d = l.pair_at(p);
+        if (h0 != nullptr && !MAPS) states.get(h0 + ((int64_t)b * s.D + d0 + d) * s.N, d < channels, d + 1 < channels, h[p]);
+    }
+    if (!MAPS && s.count > 1) state_before<X>(s, column, order, A, h);
+    const bool live = side.channel < channels, second = side.channel + 1 < channels;
+    const auto weight = [&](const float* p, int64_t stride) {
+        const float* at = p + worker * stride + d0 + side.channel;
+        return pair(live ? at[0] : 0.f, second ? at[1] : 0.f);
+    };
+    const Pair bias = weight(s.bias, s.bias_worker), skip = MAPS ? kZeros : weight(s.skip, s.skip_worker);
+    float* carries = carry == nullptr ? nullptr : carry + (((int64_t)b * ((s.T + R - 1) / R) + first / R) * s.D + d0) * s.N;
+    T* out = y + ((int64_t)b * s.T + first) * s.D + d0 + side.channel;
+
+    for (int t = 0; t < inside; t += R) {
+        const int rows = min(inside - t, R);
+        Pair held_u[Side<X>::kItems], held_z[Side<X>::kItems];
+#pragma unroll
+        for (int i = 0; i < Side<X>::kItems; ++i) {
+            const int r = side.row + i * Side<X>::kDown;
+            held_u[i] = next_u.v[i].get();
+            if (!MAPS && z != nullptr) held_z[i] = next_z.v[i].get();
+            const Pair dt = r < rows ? softplus<T>(add2(next_delta.v[i].get(), bias)) : kZeros;
+            *reinterpret_cast<Pair*>(&m.dt[r][side.channel]) = dt;
+            *reinterpret_cast<Pair*>(&m.x[r][side.channel]) = mul2(dt, held_u[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < Side<X>::kFew; ++i) {
+            const int r = (i * 32 + lane) / X::kStates, k = (i * 32 + lane) % X::kStates;
+            const float vb = __uint_as_float(next_b[i]), vc = MAPS ? 0.f : __uint_as_float(next_c[i]);
+            m.bc[r][k] = make_float4(vb, vb, vc, vc);
+        }
+        __syncwarp();
+        fetch(t + R);
+        if (!MAPS && carries != nullptr) {
+#pragma unroll
+            for (int p = 0; p < X::P; ++p) {
+                const int d = l.pair_at(p);
+                states.put(carries + (int64_t)d * s.N, d < channels, d + 1 < channels, h[p]);
+            }
+            carries += (int64_t)s.D * s.N;
+        }
+#pragma unroll 2
+        for (int r = 0; r < rows; ++r) {
+            Pair dt[X::P], x[X::P], sum[X::P];
+#pragma unroll
+            for (int p = 0; p < X::P; ++p) {
+                dt[p] = *reinterpret_cast<const Pair*>(&m.dt[r][l.pair_at(p)]);
+                x[p] = *reinterpret_cast<const Pair*>(&m.x[r][l.pair_at(p)]);
+                sum[p] = kZeros;
+                if (MAPS) sum_dt[p] = add2(sum_dt[p], dt[p]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const ulonglong2 bc = *reinterpret_cast<const ulonglong2*>(&m.bc[r][4 * l.q + j]);
+#pragma unroll
+                for (int p = 0; p < X::P; ++p) {
+                    h[p][j] = fma2(decay_of(dt[p], A[p][j]), h[p][j], mul2(x[p], bc.x));
+                    if (!MAPS) sum[p] = fma2(h[p][j], bc.y, sum[p]);
+                }
+            }
+            if constexpr (!MAPS) {
+                const float all = over_states<X>(l, sum);
+                if (X::S < 8 || l.q < 4) m.sum[r][l.summed_channel()] = all;
+            }
+        }
+        __syncwarp();
+        if constexpr (!MAPS) {
+#pragma unroll
+            for (int i = 0; i < Side<X>::kItems; ++i) {
+                const int r = side.row + i * Side<X>::kDown;
+                Pair v = fma2(skip, held_u[i], *reinterpret_cast<const Pair*>(&m.sum[r][side.channel]));
+                if (z != nullptr) {
+                    Pair a, rest;
+                    gate_of<T>(held_z[i], a, rest);
+                    v = mul2(v, mul2(held_z[i], a));
+                }
+                if (live && r < rows) store_two<WIDE>(out + (int64_t)(t + r) * s.D, v, second);
+            }
+            __syncwarp();
+        }
+    }
+    if constexpr (MAPS) {
+        put_map<X>(s, column, order, h, sum_dt);
+    } else {
+        if (live)
+            for (int t = inside + side.row; t < end - first; t += Side<X>::kDown) store_two<WIDE>(out + (int64_t)t * s.D, kZeros, second);
+        if (n > first ? n <= end : n == 0 && first == 0)
+#pragma unroll
+            for (int p = 0; p < X::P; ++p) {
+                const int d = l.pair_at(p);
+                states.put(last + ((int64_t)b * s.D + d0 + d) * s.N, d < channels, d + 1 < channels, h[p]);
+            }
+    }
+}
+
+struct ScanGradients {
+    Rows dy;
+    const float *carry, *dlast;
+    void *du, *ddelta, *dz;
+    float* dh0;
+    float* small;   // [B][segments][D N + D + D]: dA, dskip, dbias
+    float* few;     // [blocks of columns][B][T][2 kStates]: dc, db
+    int blocks;     // of columns per sequence
+};
+
+template <typename X>
+struct BackwardWarp {
+    ulonglong2 h[R / 2][X::P * 2][32];                                          // states before every second step
+    float dt[R][X::kColumn], x[R][X::kColumn], gy[R][X::kColumn];               // then what the walk sums up: below
+    float sums[R][2 * X::kStates];                                              // dc, db
+};
+template <typename X>
+struct BackwardShared {
+    float4 bc[R][X::kStates];
+    BackwardWarp<X> warps[kBackwardWarps];
+};
+
+// Backward pass, from the last step to the first. f_t, the gradient of h_t, is
+// g_t + c_t gy_t with g_t = a_(t+1) f_(t+1), gy = dy silu(z). A chunk's states
+// are made again from the carry and kept at every second step; the walk back
+// makes those between, two steps at a time.
+template <typename T, bool WIDE, typename X>
+__global__ void __launch_bounds__(kBackwardWarps * 32, kBackwardBlocks)
+scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
+    layer_begin();
+    extern __shared__ __align__(16) uint8_t raw[];
+    auto& shared = *reinterpret_cast<BackwardShared<X>*>(raw);
+    const int warps = blockDim.x / 32, warp = threadIdx.x / 32;
+    auto& m = shared.warps[warp];
+    const Lane<X> l;
+    const Side<X> side;
+    const int lane = l.lane;
+    const int64_t per = (int64_t)g.blocks * s.count, b64 = blockIdx.x / per;
+    const int b = static_cast<int>(b64), rest = static_cast<int>(blockIdx.x - b64 * per), order = rest % s.count, block = rest / s.count;
+    const int group = block * warps + warp, d0 = group * X::kColumn, channels = s.D - d0, worker = b / s.each;
+    const int64_t column = b64 * s.groups + group;
+    const bool works = group < s.groups;
+    const int n = s.lengths == nullptr ? s.T : min(max(s.lengths[b], 0), s.T);
+    const int segment = s.count - 1 - order;
+    const int first = segment * s.steps, end = min(first + s.steps, s.T), inside = min(max(n - first, 0), max(end - first, 0));
+    const auto rows_of = [&](const Rows& a) { return static_cast<const T*>(a.p) + b * a.seq + first * a.step; };
+    const T *u = rows_of(s.u) + d0, *delta = rows_of(s.delta) + d0, *z = s.z.p == nullptr ? nullptr : rows_of(s.z) + d0, *dy = rows_of(g.dy) + d0;
+    const T *bs = rows_of(s.b), *cs = rows_of(s.c);
+
+    const States<X> states(l, s.N, quads, true);
+    Pair A[X::P][4], flow[X::P][4], dA[X::P][4];
+#pragma unroll
+    for (int p = 0; p < X::P; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) A[p][j] = flow[p][j] = dA[p][j] = kZeros;
+    const bool live = works && side.channel < channels, second = works && side.channel + 1 < channels;
+    const auto weight = [&](const float* p, int64_t stride) {
+        const float* at = p + worker * stride + d0 + side.channel;
+        return pair(live ? at[0] : 0.f, second ? at[1] : 0.f);
+    };
+    const Pair bias = weight(s.bias, s.bias_worker), skip = weight(s.skip, s.skip_worker);
+    Pair dskip = kZeros, dbias = kZeros;
+    if (works) {
+        rates<X>(s, l, b, d0, true, A);
+#pragma unroll
+        for (int p = 0; p < X::P; ++p) {
+            const int d = l.pair_at(p);
+            if (g.dlast != nullptr) states.get(g.dlast + ((int64_t)b * s.D + d0 + d) * s.N, d < channels, d + 1 < channels, flow[p]);
+        }
+        if (s.count > 1) state_before<X>(s, column, order, A, flow);
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            for (int k = lane; k < 2 * X::kStates; k += 32) m.sums[r][k] = 0.f;
+    }
+    const int64_t out0 = ((int64_t)b * s.T + first) * s.D + d0 + side.channel;
+    if (live)
+        for (int t = inside + side.row; t < end - first; t += Side<X>::kDown) {
+            store_two<WIDE>(static_cast<T*>(g.du) + out0 + (int64_t)t * s.D, kZeros, second);
+            store_two<WIDE>(static_cast<T*>(g.ddelta) + out0 + (int64_t)t * s.D, kZeros, second);
+            if (z != nullptr) store_two<WIDE>(static_cast<T*>(g.dz) + out0 + (int64_t)t * s.D, kZeros, second);
+        }
+
+    for (int t = (inside - 1) / R * R; t >= 0 && inside > 0; t -= R) {
+        const int rows = min(inside - t, R), pairs = (rows + 1) / 2;
+        // b and c for the block, the rest for the warp
+        for (int i = threadIdx.x; i < R * X::kStates; i += blockDim.x) {
+            const int r = i / X::kStates, k = i % X::kStates;
+            const bool there = r < rows && k < s.N;
+            const float vb = __uint_as_float(load_bits(bs + (t + r) * s.b.step + k, there)), vc = __uint_as_float(load_bits(cs + (t + r) * s.c.step + k, there));
+            shared.bc[r][k] = make_float4(vb, vb, vc, vc);
+        }
+        Wide<T, WIDE, X> in_u, in_delta, in_z, in_dy;
+        Pair h[X::P][4], dts[Side<X>::kItems];
+        if (works) {
+            in_u.load(side, u + t * s.u.step, s.u.step, rows, channels);
+            in_delta.load(side, delta + t * s.delta.step, s.delta.step, rows, channels);
+            if (z != nullptr) in_z.load(side, z + t * s.z.step, s.z.step, rows, channels);
+            in_dy.load(side, dy + t * g.dy.step, g.dy.step, rows, channels);
+            const float* carries = g.carry + (((int64_t)b * ((s.T + R - 1) / R) + (first + t) / R) * s.D + d0) * s.N;
+#pragma unroll
+            for (int p = 0; p < X::P; ++p) {
+                const int d = l.pair_at(p);
+                states.get(carries + (int64_t)d * s.N, d < channels, d + 1 < channels, h[p]);
+            }
+#pragma unroll
+            for (int i = 0; i < Side<X>::kItems; ++i) {
+                const int r = side.row + i * Side<X>::kDown;
+                dts[i] = r < rows ? softplus<T>(add2(in_delta.v[i].get(), bias)) : kZeros;
+                Pair gy = in_dy.v[i].get();
+                if (z != nullptr) {
+                    Pair a, away;
+                    gate_of<T>(in_z.v[i].get(), a, away);
+                    gy = mul2(gy, mul2(in_z.v[i].get(), a));
+                }
+                *reinterpret_cast<Pair*>(&m.dt[r][side.channel]) = dts[i];
+                *reinterpret_cast<Pair*>(&m.x[r][side.channel]) = mul2(dts[i], in_u.v[i].get());
+                *reinterpret_cast<Pair*>(&m.gy[r][side.channel]) = gy;
+            }
+        }
+        __syncthreads();
+        if (works) {
+            for (int k = 0; k < pairs; ++k) {
+#pragma unroll
+                for (int p = 0; p < X::P; ++p)
+#pragma unroll
+                    for (int j = 0; j < 4; j += 2) m.h[k][p * 2 + j / 2][lane] = make_ulonglong2(h[p][j], h[p][j + 1]);
+                if (k + 1 == pairs) break;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = 2 * k + e;
+                    Pair dt[X::P], x[X::P];
+#pragma unroll
+                    for (int p = 0; p < X::P; ++p) {
+                        dt[p] = *reinterpret_cast<const Pair*>(&m.dt[r][l.pair_at(p)]);
+                        x[p] = *reinterpret_cast<const Pair*>(&m.x[r][l.pair_at(p)]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const Pair vb = *reinterpret_cast<const Pair*>(&shared.bc[r][4 * l.q + (j ^ l.turn)].x);
+#pragma unroll
+                        for (int p = 0; p < X::P; ++p) h[p][j] = fma2(decay_of(dt[p], A[p][j]), h[p][j], mul2(x[p], vb));
+                    }
+                }
+            }
+            for (int k = pairs - 1; k >= 0; --k) {
+                Pair dt[2][X::P], x[2][X::P], gy[2][X::P], through[2][X::P], reach[2][X::P], sum[2][X::P];
+                float dc[2][4], db[2][4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int p = 0; p < X::P; ++p) {
+                        dt[e][p] = *reinterpret_cast<const Pair*>(&m.dt[2 * k + e][l.pair_at(p)]);
+                        x[e][p] = *reinterpret_cast<const Pair*>(&m.x[2 * k + e][l.pair_at(p)]);
+                        gy[e][p] = *reinterpret_cast<const Pair*>(&m.gy[2 * k + e][l.pair_at(p)]);
+                        through[e][p] = reach[e][p] = sum[e][p] = kZeros;
+                    }
+                ulonglong2 kept[X::P * 2];
+#pragma unroll
+                for (int p = 0; p < X::P * 2; ++p) kept[p] = m.h[k][p][lane];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    ulonglong2 bc[2];
+                    Pair to_c[2] = {kZeros, kZeros}, to_b[2] = {kZeros, kZeros};
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) bc[e] = *reinterpret_cast<const ulonglong2*>(&shared.bc[2 * k + e][4 * l.q + (j ^ l.turn)]);
+#pragma unroll
+                    for (int p = 0; p < X::P; ++p) {
+                        Pair at[3], a[2];
+                        at[0] = j % 2 ? kept[p * 2 + j / 2].y : kept[p * 2 + j / 2].x;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            a[e] = decay_of(dt[e][p], A[p][j]);
+                            at[e + 1] = fma2(a[e], at[e], mul2(x[e][p], bc[e].x));
+                        }
+#pragma unroll
+                        for (int e = 1; e >= 0; --e) {
+                            const Pair f = fma2(gy[e][p], bc[e].y, flow[p][j]);
+                            to_c[e] = fma2(at[e + 1], gy[e][p], to_c[e]);
+                            to_b[e] = fma2(f, x[e][p], to_b[e]);
+                            through[e][p] = fma2(f, bc[e].x, through[e][p]);
+                            sum[e][p] = fma2(at[e + 1], bc[e].y, sum[e][p]);
+                            flow[p][j] = mul2(f, a[e]);
+                            const Pair r = mul2(flow[p][j], at[e]);
+                            reach[e][p] = fma2(r, A[p][j], reach[e][p]);
+                            dA[p][j] = fma2(r, dt[e][p], dA[p][j]);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        dc[e][j] = floats(to_c[e]).x + floats(to_c[e]).y;
+                        db[e][j] = floats(to_b[e]).x + floats(to_b[e]).y;
+                    }
+                }
+                __syncwarp();
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = 2 * k + e, d = l.summed_channel();
+                    const float all_through = over_states<X>(l, through[e]), all_reach = over_states<X>(l, reach[e]), all = over_states<X>(l, sum[e]);
+                    if (X::S < 8 || l.q < 4) m.dt[r][d] = all_through, m.x[r][d] = all_reach, m.gy[r][d] = all;
+                    const float2 few = over_channels<X>(l, dc[e], db[e]);
+                    const int state = 4 * l.q + l.turn;
+                    if constexpr (X::S == 8)
+                        m.sums[r][state] = few.x, m.sums[r][X::kStates + state] = few.y;
+                    else if (X::S == 4 || l.g < 8)
+                        m.sums[r][(l.g & 4 ? X::kStates : 0) + state] = few.x;
+                }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < Side<X>::kItems; ++i) {
+                const int r = side.row + i * Side<X>::kDown;
+                const Pair through = *reinterpret_cast<const Pair*>(&m.dt[r][side.channel]), reach = *reinterpret_cast<const Pair*>(&m.x[r][side.channel]);
+                const Pair sum = *reinterpret_cast<const Pair*>(&m.gy[r][side.channel]), vu = in_u.v[i].get(), vdy = in_dy.v[i].get();
+                Pair gy = vdy, gate, away;
+                const int64_t at = out0 + (int64_t)(t + r) * s.D;
+                const bool here = live && r < rows;
+                if (z != nullptr) {
+                    const Pair vz = in_z.v[i].get();
+                    gate_of<T>(vz, gate, away);
+                    gy = mul2(vdy, mul2(vz, gate));
+                    const Pair slope = mul2(gate, fma2(vz, away, kOnes));
+                    if (here) store_two<WIDE>(static_cast<T*>(g.dz) + at, mul2(mul2(vdy, slope), fma2(skip, vu, sum)), second);
+                }
+                gate_of<T>(add2(in_delta.v[i].get(), bias), gate, away);
+                const Pair dbase = mul2(fma2(through, vu, mul2(reach, twice(kLn2f))), gate);
+                if (here) {
+                    store_two<WIDE>(static_cast<T*>(g.du) + at, fma2(through, dts[i], mul2(skip, gy)), second);
+                    store_two<WIDE>(static_cast<T*>(g.ddelta) + at, dbase, second);
+                    dskip = fma2(gy, vu, dskip);
+                    dbias = add2(dbias, dbase);
+                }
+            }
+        }
+        __syncthreads();
+        float* few = g.few + (((int64_t)block * s.B + b) * s.T + first + t) * (2 * X::kStates);
+        for (int i = threadIdx.x; i < rows * 2 * X::kStates; i += blockDim.x) {
+            float v = (&shared.warps[0].sums[0][0])[i];
+            for (int w = 1; w < warps; ++w) v += (&shared.warps[w].sums[0][0])[i];
+            few[i] = v;
+        }
+    }
+    if (!works) return;
+    const int64_t each = (int64_t)s.D * (s.N + 2);
+    float* small = g.small + ((int64_t)b * s.count + segment) * each;
+    const States<X> unaligned(l, s.N, false, true);
+#pragma unroll
+    for (int p = 0; p < X::P; ++p) {
+        const int d = l.pair_at(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dA[p][j] = mul2(mul2(dA[p][j], A[p][j]), twice(kLn2f));
+        unaligned.put(small + (int64_t)(d0 + d) * s.N, d < channels, d + 1 < channels, dA[p]);
+        if (g.dh0 != nullptr && segment == 0) states.put(g.dh0 + ((int64_t)b * s.D + d0 + d) * s.N, d < channels, d + 1 < channels, flow[p]);
+    }
+#pragma unroll
+    for (int down = Side<X>::kLanes; down < 32; down *= 2) {
+        dskip = add2(dskip, shuffle(dskip, down));
+        dbias = add2(dbias, shuffle(dbias, down));
+    }
+    if (side.row == 0 && live) {
+        float* to = small + (int64_t)s.D * s.N + d0 + side.channel;
+        to[0] = floats(dskip).x, to[s.D] = floats(dbias).x;
+        if (second) to[1] = floats(dskip).y, to[s.D + 1] = floats(dbias).y;
+    }
+}
+
+// The segments' maps of what flows back.
+template <typename T, bool WIDE, typename X>
+__global__ void __launch_bounds__(32, kForwardBlocks)
+scan_backward_maps_kernel(Scan s, Rows grads) {
+    layer_begin();
+    __shared__ ForwardShared<X> m;
+    const Lane<X> l;
+    const Side<X> side;
+    const int lane = l.lane;
+    const int64_t column = blockIdx.x / s.count;
+    const int order = static_cast<int>(blockIdx.x - column * s.count), b = static_cast<int>(column / s.groups);
+    if (order == s.count - 1) return;
+    const int d0 = static_cast<int>(column - (int64_t)b * s.groups) * X::kColumn, channels = s.D - d0, worker = b / s.each;
+    const int n = s.lengths == nullptr ? s.T : min(max(s.lengths[b], 0), s.T);
+    const int first = (s.count - 1 - order) * s.steps, end = min(first + s.steps, s.T), inside = min(max(n - first, 0), max(end - first, 0));
+    const auto rows_of = [&](const Rows& a) { return static_cast<const T*>(a.p) + b * a.seq + first * a.step; };
+    const T *delta = rows_of(s.delta) + d0, *z = s.z.p == nullptr ? nullptr : rows_of(s.z) + d0, *dy = rows_of(grads) + d0, *cs = rows_of(s.c);
+    Pair A[X::P][4], flow[X::P][4], sum_dt[X::P];
+    rates<X>(s, l, b, d0, true, A);
+#pragma unroll
+    for (int p = 0; p < X::P; ++p) {
+        sum_dt[p] = kZeros;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) flow[p][j] = kZeros;
+    }
+    const float* at = s.bias + worker * s.bias_worker + d0 + side.channel;
+    const Pair bias = pair(side.channel < channels ? at[0] : 0.f, side.channel + 1 < channels ? at[1] : 0.f);
+    for (int t = (inside - 1) / R * R; t >= 0 && inside > 0; t -= R) {
+        const int rows = min(inside - t, R);
+        Wide<T, WIDE, X> in_delta, in_z, in_dy;
+        in_delta.load(side, delta + t * s.delta.step, s.delta.step, rows, channels);
+        if (z != nullptr) in_z.load(side, z + t * s.z.step, s.z.step, rows, channels);
+        in_dy.load(side, dy + t * grads.step, grads.step, rows, channels);
+#pragma unroll
+        for (int i = 0; i < Side<X>::kFew; ++i) {
+            const int r = (i * 32 + lane) / X::kStates, k = (i * 32 + lane) % X::kStates;
+            const float v = __uint_as_float(load_bits(cs + (t + r) * s.c.step + k, r < rows && k < s.N));
+            m.bc[r][k] = make_float4(v, v, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < Side<X>::kItems; ++i) {
+            const int r = side.row + i * Side<X>::kDown;
+            Pair gy = in_dy.v[i].get();
+            if (z != nullptr) {
+                Pair a, away;
+                gate_of<T>(in_z.v[i].get(), a, away);
+                gy = mul2(gy, mul2(in_z.v[i].get(), a));
+            }
+            *reinterpret_cast<Pair*>(&m.dt[r][side.channel]) = r < rows ? softplus<T>(add2(in_delta.v[i].get(), bias)) : kZeros;
+            *reinterpret_cast<Pair*>(&m.x[r][side.channel]) = gy;
+        }
+        __syncwarp();
+#pragma unroll 2
+        for (int r = rows - 1; r >= 0; --r) {
+            Pair dt[X::P], gy[X::P];
+#pragma unroll
+            for (int p = 0; p < X::P; ++p) {
+                dt[p] = *reinterpret_cast<const Pair*>(&m.dt[r][l.pair_at(p)]);
+                gy[p] = *reinterpret_cast<const Pair*>(&m.x[r][l.pair_at(p)]);
+                sum_dt[p] = add2(sum_dt[p], dt[p]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const Pair c = *reinterpret_cast<const Pair*>(&m.bc[r][4 * l.q + (j ^ l.turn)].x);
+#pragma unroll
+                for (int p = 0; p < X::P; ++p) flow[p][j] = mul2(decay_of(dt[p], A[p][j]), fma2(gy[p], c, flow[p][j]));
+            }
+        }
+        __syncwarp();
+    }
+    put_map<X>(s, column, order, flow, sum_dt);
+}
+
+// db and dc: the sum of the blocks' parts, 0 beyond a length.
+template <typename T>
+__global__ void __launch_bounds__(256)
+sum_few_kernel(const float* parts, int blocks, int B, int T_, int N, int states, const int32_t* lengths, T* db, T* dc) {
+    layer_begin();
+    const int64_t all = (int64_t)B * T_ * N, one = (int64_t)B * T_ * 2 * states;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / N, b = row / T_;
+        const int k = static_cast<int>(i - row * N), t = static_cast<int>(row - b * T_);
+        float vc = 0.f, vb = 0.f;
+        if (lengths == nullptr || t < lengths[b]) {
+            const float* p = parts + row * 2 * states + k;
+#pragma unroll 4
+            for (int g = 0; g < blocks; ++g) {
+                vc += p[g * one];
+                vb += p[g * one + states];
+            }
+        }
+        dc[i] = from_float<T>(vc);
+        db[i] = from_float<T>(vb);
+    }
+}
+
+// One step: 4 states of a channel per thread, S threads to a channel.
+template <typename T, int S>
+__global__ void __launch_bounds__(128)
+scan_step_kernel(Scan s, float* h, T* y) {
+    layer_begin();
+    const int64_t i = ((int64_t)blockIdx.x * 128 + threadIdx.x) / S, b = i / s.D;
+    const bool there = b < s.B;
+    const int d = static_cast<int>(i - b * s.D), q = threadIdx.x % S, worker = static_cast<int>(b / s.each);
+    float sum = 0.f, u = 0.f;
+    if (there) {
+        u = to_float(static_cast<const T*>(s.u.p)[b * s.u.seq + d]);
+        const float raw = to_float(static_cast<const T*>(s.delta.p)[b * s.delta.seq + d]) + s.bias[worker * s.bias_worker + d];
+        const float dt = floats(softplus<T>(pair(raw, 0.f))).x, x = dt * u;
+        const float* a = s.a_log + worker * s.a_worker + (int64_t)d * s.N;
+        float* state = h + i * s.N;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int n = 4 * q + j;
+            if (n < s.N) {
+                const float decay = power_of_minus(dt * (kLog2eHigh * expf(a[n])));
+                const float vb = to_float(static_cast<const T*>(s.b.p)[b * s.b.seq + n]), vc = to_float(static_cast<const T*>(s.c.p)[b * s.c.seq + n]);
+                const float next = fmaf(decay, state[n], x * vb);
+                state[n] = next;
+                sum = fmaf(next, vc, sum);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 1; k < S; k *= 2) sum += __shfl_xor_sync(~0u, sum, k);
+    if (!there || q > 0) return;
+    float v = fmaf(s.skip[worker * s.skip_worker + d], u, sum);
+    if (s.z.p != nullptr) {
+        const float z = to_float(static_cast<const T*>(s.z.p)[b * s.z.seq + d]);
+        Pair a, rest;
+        gate_of<T>(pair(z, 0.f), a, rest);
+        v *= z * floats(a).x;
+    }
+    y[i] = from_float<T>(v);
+}
+
+// -- the host's side -------------------------------------------------------------------------------------------------
+
+cpdp_status check_scan(int W, int B, int64_t T, int D, int N, cpdp_dtype dtype) {
+    if (B < 0) return layer_error(CPDP_EINVAL, "B=%d must be >= 0", B);
+    CPDP_TRY(check_sizes(1, T, D));
+    if (W < 1 || W > 4096 || B % W != 0) return layer_error(CPDP_EINVAL, "W=%d must be in [1, 4096] and divide B=%d", W, B);
+    if (N < 1 || N > CPDP_SCAN_MAX_STATES) return layer_error(CPDP_EINVAL, "N=%d must be in [1, %d]", N, CPDP_SCAN_MAX_STATES);
+    if (T > int64_t(1) << 30) return layer_error(CPDP_EINVAL, "T=%lld is at most 2^30", (long long)T);
+    if (B > 0) {
+        if (T > kLayerMaxRows / B || (T > 0 && D > kLayerMaxElements / 64 / (B * T)))
+            return layer_error(CPDP_EINVAL, "B=%d, T=%lld, D=%d: B * T is at most 2^31 - 1 and all elements at most 2^34", B, (long long)T, D);
+        if (ceil_div(D, 16) > (kLayerMaxRows >> 6) / B) return layer_error(CPDP_EINVAL, "B=%d, D=%d: more blocks than a launch takes", B, D);
+    }
+    if (!known_dtype(dtype)) return layer_error(CPDP_EINVAL, "unknown dtype %d", (int)dtype);
+    return CPDP_OK;
+}
+
+template <typename F>
+auto with_shape(int N, F&& f) {
+    return N <= 8 ? f(Shape<2, 2>{}) : N <= 16 ? f(Shape<4, 4>{}) : f(Shape<8, 4>{});
+}
+
+struct Plan {
+    int groups, column, states;   // columns of a sequence, channels of one, padded states
+    int count, steps;             // segments
+    int warps, blocks;            // of the backward pass: of a block, and blocks of columns per sequence
+    int64_t maps, few, small;     // bytes
+};
+// `warps`: as many as run at once on the GPU.
+Plan plan_of(int B, int64_t T, int D, int N, int64_t warps, bool backward) {
+    Plan p{};
+    with_shape(N, [&](auto x) { return p.column = decltype(x)::kColumn, p.states = decltype(x)::kStates, 0; });
+    p.groups = static_cast<int>(ceil_div(D, p.column));
+    const int64_t columns = (int64_t)B * p.groups;
+    int64_t count = columns * 3 <= warps ? warps / std::max<int64_t>(columns, 1) : 1;
+    count = std::max<int64_t>(std::min(count, T / (4 * R)), 1);
+    p.steps = static_cast<int>(ceil_div(ceil_div(std::max<int64_t>(T, 1), count), R) * R);
+    p.count = static_cast<int>(std::max<int64_t>(ceil_div(T, p.steps), 1));
+    const int pairs = N <= 8 ? 1 : 2;
+    p.maps = p.count > 1 ? columns * p.count * pairs * 5 * 32 * 8 : 0;
+    if (backward) {
+        p.warps = 1;
+        for (int w = 2; w <= kBackwardWarps; ++w)
+            if (ceil_div(p.groups, w) * w <= ceil_div(p.groups, p.warps) * p.warps + p.groups / 16) p.warps = w;
+        p.blocks = static_cast<int>(ceil_div(p.groups, p.warps));
+        p.few = ceil_div((int64_t)p.blocks * B * T * 2 * p.states * 4, 16) * 16;
+        p.small = ceil_div((int64_t)B * p.count * D * (N + 2) * 4, 16) * 16;
+    }
+    return p;
+}
+Plan forward_plan(int B, int64_t T, int D, int N) { return plan_of(B, T, D, N, kSMs * kForwardBlocks, false); }
+Plan backward_plan(int B, int64_t T, int D, int N) { return plan_of(B, T, D, N, kSMs * kBackwardBlocks * kBackwardWarps, true); }
+
+bool pairs_at(const Rows& r, int64_t e) { return aligned_to(r.p, 2 * e) && r.seq % 2 == 0 && r.step % 2 == 0; }
+
+cpdp_status check_inputs(const Scan& s, int64_t e, bool some, bool steps) {
+    CPDP_TRY(check_array("u", s.u.p, some, e, s.u.seq, s.u.step));
+    CPDP_TRY(check_array("delta", s.delta.p, some, e, s.delta.seq, s.delta.step));
+    CPDP_TRY(check_array("z", s.z.p, false, e, s.z.seq, s.z.step));
+    CPDP_TRY(check_array("b", s.b.p, some, e, s.b.seq, s.b.step));
+    CPDP_TRY(check_array("c", s.c.p, some, e, s.c.seq, s.c.step));
+    CPDP_TRY(check_array("a_log", s.a_log, true, 4, s.a_worker));
+    CPDP_TRY(check_array("skip", s.skip, true, 4, s.skip_worker));
+    CPDP_TRY(check_array("bias", s.bias, true, 4, s.bias_worker));
+    return check_array("lengths", s.lengths, false, 4);
+}
+
+Scan scan_of(const cpdp_scan_inputs& in, int W, int B, int64_t T, int D, int N) {
+    Scan s{};
+    s.u = {in.u, in.u_seq, in.u_step}, s.delta = {in.delta, in.delta_seq, in.delta_step}, s.z = {in.z, in.z_seq, in.z_step};
+    s.b = {in.b, in.b_seq, in.b_step}, s.c = {in.c, in.c_seq, in.c_step};
+    s.a_log = in.a_log, s.a_worker = in.a_log_worker, s.skip = in.skip, s.skip_worker = in.skip_worker, s.bias = in.bias, s.bias_worker = in.bias_worker;
+    s.lengths = in.lengths;
+    s.B = B, s.T = static_cast<int>(T), s.D = D, s.N = N, s.each = B / W;
+    return s;
+}
+
+}  // namespace
+}  // namespace cpdp
+
+using namespace cpdp;
+
+size_t cpdp_selective_scan_workspace(int B, int64_t T, int D, int N) {
+    return check_scan(1, B, T, D, N, CPDP_F32) != CPDP_OK || B == 0 ? 0 : forward_plan(B, T, D, N).maps;
+}
+
+size_t cpdp_selective_scan_backward_workspace(int B, int64_t T, int D, int N) {
+    if (check_scan(1, B, T, D, N, CPDP_F32) != CPDP_OK || B == 0) return 0;
+    const Plan p = backward_plan(B, T, D, N);
+    return p.maps + p.few + p.small;
+}
+
+cpdp_status cpdp_selective_scan(const cpdp_scan_inputs* inputs, cpdp_dtype dtype, int W, int B, int64_t T, int D, int N, const float* h0, void* y,
+                                float* last, float* carry, void* workspace, size_t workspace_bytes, void* stream) {
+    constexpr const char* what = "cpdp_selective_scan";
+    CPDP_TRY(check_scan(W, B, T, D, N, dtype));
+    if (inputs == nullptr) return layer_error(CPDP_EINVAL, "inputs is NULL");
+    Scan s = scan_of(*inputs, W, B, T, D, N);
+    const int64_t e = dtype_size(dtype);
+    const bool some = B > 0 && T > 0;
+    CPDP_TRY(check_inputs(s, e, some, true));
+    CPDP_TRY(check_array("h0", h0, false, 4));
+    CPDP_TRY(check_array("y", y, some, e));
+    CPDP_TRY(check_array("last", last, B > 0, 4));
+    CPDP_TRY(check_array("carry", carry, false, 4));
+    CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_selective_scan_workspace(B, T, D, N)));
+    if (B == 0) return CPDP_OK;
+    const Plan plan = forward_plan(B, T, D, N);
+    s.groups = plan.groups, s.count = plan.count, s.steps = plan.steps, s.maps = static_cast<Pair*>(workspace);
+    const bool quads = N % 4 == 0 && aligned_to(h0, 16) && aligned_to(last, 16) && aligned_to(carry, 16);
+    const bool wide = D % 2 == 0 && pairs_at(s.u, e) && pairs_at(s.delta, e) && pairs_at(s.z, e) && aligned_to(y, 2 * e);
+    const unsigned blocks = static_cast<unsigned>((int64_t)B * plan.groups * plan.count);
+    const auto go = [&](auto* out, auto two) {
+        using E = std::remove_pointer_t<decltype(out)>;
+        constexpr bool WIDE = decltype(two)::value;
+        return with_shape(N, [&](auto shape) {
+            using X = decltype(shape);
+            if (plan.count > 1) {
+                const cudaError_t first = launch_layer(scan_kernel<E, WIDE, true, X>, blocks, 32, 0, stream, s, h0, out, last, carry, quads);
+                if (first != cudaSuccess) return first;
+            }
+            return launch_layer(scan_kernel<E, WIDE, false, X>, blocks, 32, 0, stream, s, h0, out, last, carry, quads);
+        });
+    };
+    const auto typed = [&](auto* out) { return wide ? go(out, std::true_type{}) : go(out, std::false_type{}); };
+    return layer_launched(dtype == CPDP_F32 ? typed(static_cast<float*>(y)) : typed(static_cast<__nv_bfloat16*>(y)), what);
+}
+
+cpdp_status cpdp_selective_scan_backward(const void* dy, int64_t dy_seq, int64_t dy_step, const cpdp_scan_inputs* inputs, cpdp_dtype dtype, int W,
+                                         int B, int64_t T, int D, int N, const float* carry, const float* dlast, void* du, void* ddelta, void* dz,
+                                         void* db, void* dc, float* dh0, void* da_log, int64_t da_log_worker, void* dskip, int64_t dskip_worker,
+                                         void* dbias, int64_t dbias_worker, cpdp_dtype dweight_dtype, void* workspace, size_t workspace_bytes,
+                                         void* stream) {
+    constexpr const char* what = "cpdp_selective_scan_backward";
+    CPDP_TRY(check_scan(W, B, T, D, N, dtype));
+    if (inputs == nullptr) return layer_error(CPDP_EINVAL, "inputs is NULL");
+    if (!known_dtype(dweight_dtype)) return layer_error(CPDP_EINVAL, "unknown dtype of the weights' gradients: %d", (int)dweight_dtype);
+    Scan s = scan_of(*inputs, W, B, T, D, N);
+    const int64_t e = dtype_size(dtype), grad = dtype_size(dweight_dtype);
+    const bool some = B > 0 && T > 0;
+    CPDP_TRY(check_array("dy", dy, some, e, dy_seq, dy_step));
+    CPDP_TRY(check_inputs(s, e, some, true));
+    CPDP_TRY(check_array("carry", carry, some, 4));
+    CPDP_TRY(check_array("dlast", dlast, false, 4));
+    CPDP_TRY(check_array("du", du, some, e));
+    CPDP_TRY(check_array("ddelta", ddelta, some, e));
+    CPDP_TRY(check_array("dz", dz, some && s.z.p != nullptr, e));
+    CPDP_TRY(check_array("db", db, some, e));
+    CPDP_TRY(check_array("dc", dc, some, e));
+    CPDP_TRY(check_array("dh0", dh0, false, 4));
+    CPDP_TRY(check_array("da_log", da_log, true, grad, da_log_worker));
+    CPDP_TRY(check_array("dskip", dskip, true, grad, dskip_worker));
+    CPDP_TRY(check_array("dbias", dbias, true, grad, dbias_worker));
+    CPDP_TRY(check_apart("da_log", W, da_log_worker, (int64_t)D * N));
+    CPDP_TRY(check_apart("dskip", W, dskip_worker, D));
+    CPDP_TRY(check_apart("dbias", W, dbias_worker, D));
+    CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_selective_scan_backward_workspace(B, T, D, N)));
+    const SumsOut sums{{da_log, dskip, dbias}, {da_log_worker, dskip_worker, dbias_worker}, {(int64_t)D * N, D, D}};
+    if (B == 0) return layer_launched(sum_gradients(nullptr, 0, W, sums, dweight_dtype, stream), what);
+    const Plan plan = backward_plan(B, T, D, N);
+    s.groups = plan.groups, s.count = plan.count, s.steps = plan.steps, s.maps = static_cast<Pair*>(workspace);
+    ScanGradients g{};
+    g.dy = {dy, dy_seq, dy_step}, g.carry = carry, g.dlast = dlast, g.du = du, g.ddelta = ddelta, g.dz = dz, g.dh0 = dh0;
+    g.few = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.maps);
+    g.small = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.maps + plan.few);
+    g.blocks = plan.blocks;
+    const bool quads = N % 4 == 0 && aligned_to(carry, 16) && aligned_to(dlast, 16) && aligned_to(dh0, 16);
+    const bool wide = D % 2 == 0 && pairs_at(s.u, e) && pairs_at(s.delta, e) && pairs_at(s.z, e) && pairs_at(g.dy, e) && aligned_to(du, 2 * e) &&
+                      aligned_to(ddelta, 2 * e) && aligned_to(dz, 2 * e);
+    const auto go = [&](auto* out, auto two) {
+        using E = std::remove_pointer_t<decltype(out)>;
+        constexpr bool WIDE = decltype(two)::value;
+        return with_shape(N, [&](auto shape) {
+            using X = decltype(shape);
+            if (plan.count > 1) {
+                const cudaError_t first = launch_layer(scan_backward_maps_kernel<E, WIDE, X>, static_cast<unsigned>((int64_t)B * plan.groups * plan.count),
+                                                       32, 0, stream, s, g.dy);
+                if (first != cudaSuccess) return first;
+            }
+            const int smem = static_cast<int>(sizeof(BackwardShared<X>) - (kBackwardWarps - plan.warps) * sizeof(BackwardWarp<X>));
+            const cudaError_t allowed = allow_shared_memory<scan_backward_kernel<E, WIDE, X>>(sizeof(BackwardShared<X>));
+            if (allowed != cudaSuccess) return allowed;
+            return launch_layer(scan_backward_kernel<E, WIDE, X>, static_cast<unsigned>((int64_t)B * plan.blocks * plan.count), plan.warps * 32, smem,
+                                stream, s, g, quads);
+        });
+    };
+    const auto typed = [&](auto* out) { return wide ? go(out, std::true_type{}) : go(out, std::false_type{}); };
+    CPDP_TRY(layer_launched(dtype == CPDP_F32 ? typed(static_cast<float*>(du)) : typed(static_cast<__nv_bfloat16*>(du)), what));
+    if (T > 0) {
+        const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div((int64_t)B * T * N, 256), kSMs * 8));
+        const auto sum = [&](auto* out) {
+            using E = std::remove_pointer_t<decltype(out)>;
+            return launch_layer(sum_few_kernel<E>, blocks, 256, 0, stream, static_cast<const float*>(g.few), plan.blocks, B, static_cast<int>(T), N,
+                                plan.states, s.lengths, out, static_cast<E*>(dc));
+        };
+        CPDP_TRY(layer_launched(dtype == CPDP_F32 ? sum(static_cast<float*>(db)) : sum(static_cast<__nv_bfloat16*>(db)), what));
+    }
+    return layer_launched(sum_gradients(g.small, B / W * plan.count, W, sums, dweight_dtype, stream), what);
+}
+
+cpdp_status cpdp_selective_scan_step(const cpdp_scan_inputs* inputs, cpdp_dtype dtype, int W, int B, int D, int N, float* state, void* y, void* stream) {
+    CPDP_TRY(check_scan(W, B, 1, D, N, dtype));
+    if (inputs == nullptr) return layer_error(CPDP_EINVAL, "inputs is NULL");
+    const Scan s = scan_of(*inputs, W, B, 1, D, N);
+    const int64_t e = dtype_size(dtype);
+    CPDP_TRY(check_inputs(s, e, B > 0, false));
+    CPDP_TRY(check_array("state", state, B > 0, 4));
+    CPDP_TRY(check_array("y", y, B > 0, e));
+    if (B == 0) return CPDP_OK;
+    const auto go = [&](auto* out) {
+        using E = std::remove_pointer_t<decltype(out)>;
+        return with_shape(N, [&](auto shape) {
+            constexpr int S = decltype(shape)::S;
+            return launch_layer(scan_step_kernel<E, S>, static_cast<unsigned>(ceil_div((int64_t)B * D * S, 128)), 128, 0, stream, s, state, out);
+        });
+    };
+    return layer_launched(dtype == CPDP_F32 ? go(static_cast<float*>(y)) : go(static_cast<__nv_bfloat16*>(y)), "cpdp_selective_scan_step");
+}

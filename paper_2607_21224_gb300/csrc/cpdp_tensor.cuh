@@ -2,7 +2,6 @@
 // shared-memory matrices, tensor memory, tensor copies.
 #pragma once
 
-#include <atomic>
 #include <cuda.h>
 
 #include "cpdp_layers.cuh"
@@ -26,20 +25,6 @@ inline EncodeTiled encode_tiled() {
         return reinterpret_cast<EncodeTiled>(p);
     }();
     return f;
-}
-
-// Lets a kernel have `bytes` of dynamic shared memory, once per device.
-template <auto KERNEL>
-cudaError_t allow_shared_memory(int bytes) {
-    static std::atomic<uint64_t> allowed{0};  // the devices on which this kernel has been allowed its shared memory
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
-    if (e == cudaSuccess && (allowed.load() & bit) == 0) {
-        e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e == cudaSuccess) allowed |= bit;
-    }
-    return e;
 }
 
 #ifdef __CUDACC__

@@ -11,6 +11,9 @@ include/cpdp_layers.h, which make the gradients that ``CPDPState`` steps with.
   entropy over a vocabulary, from the activations and the head's weight
 - ``causal_conv`` / ``causal_conv_backward`` / ``causal_conv_step``: a short
   convolution over time for each channel, and its silu
+- ``selective_scan`` / ``selective_scan_backward`` / ``selective_scan_step``: a
+  state space with some states per channel, whose step size, input and output
+  weights depend on the token
 - ``clip_gradients``: the norms of the workers' gradient rows, and the rows
   scaled down to a largest norm
 
@@ -47,6 +50,7 @@ BLOCK = 32  # features that share an exponent
 MAX_SIZE = 1 << 30  # of every axis
 CARRY_STEPS = 16  # CPDP_CARRY_STEPS
 CONV_MAX_TAPS = 4  # CPDP_CONV_MAX_TAPS
+SCAN_MAX_STATES = 32  # CPDP_SCAN_MAX_STATES
 NORM_MAX_FEATURES = 16384  # CPDP_NORM_MAX_FEATURES
 
 _P, _I, _L, _F, _Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -76,6 +80,12 @@ SIGNATURES = {
     "cpdp_causal_conv_backward": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _P, _L, _P, _P, _P, _I, _I, _I, _L, _I, _I, _P, _P, _P, _L, _P,
                                        _L, _I, _P, _Z, _P]),
     "cpdp_causal_conv_step": (_I, [_P, _L, _P, _L, _P, _L, _I, _I, _I, _I, _I, _P, _P, _P]),
+    "cpdp_selective_scan_workspace": (_Z, [_I, _L, _I, _I]),
+    "cpdp_selective_scan": (_I, [_P, _I, _I, _I, _L, _I, _I, _P, _P, _P, _P, _P, _Z, _P]),
+    "cpdp_selective_scan_backward_workspace": (_Z, [_I, _L, _I, _I]),
+    "cpdp_selective_scan_backward": (_I, [_P, _L, _L, _P, _I, _I, _I, _L, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _L, _P, _L, _P,
+                                          _L, _I, _P, _Z, _P]),
+    "cpdp_selective_scan_step": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P]),
     "cpdp_layer_timeouts": (_I, [ctypes.POINTER(_L)]),
 }
 
@@ -687,6 +697,136 @@ def causal_conv_step(x, weight, bias, state, *, stream=None):
     y = torch.empty(shape, dtype=dtype, device=device)
     _check(_entry("cpdp_causal_conv_step")(x.data_ptr(), xs[0], weight.data_ptr(), ws[0], bias.data_ptr(), bs[0], code, wshape[0], B, D, wshape[2],
                                            state.data_ptr(), y.data_ptr(), _stream(device.index)))
+    return y
+
+
+class _ScanInputs(ctypes.Structure):
+    """cpdp_scan_inputs."""
+    _fields_ = [(n, t) for names, kinds in ((("u", "u_seq", "u_step"), (_P, _L, _L)), (("delta", "delta_seq", "delta_step"), (_P, _L, _L)),
+                                            (("z", "z_seq", "z_step"), (_P, _L, _L)), (("b", "b_seq", "b_step"), (_P, _L, _L)),
+                                            (("c", "c_seq", "c_step"), (_P, _L, _L)), (("a_log", "a_log_worker"), (_P, _L)),
+                                            (("skip", "skip_worker"), (_P, _L)), (("bias", "bias_worker"), (_P, _L)), (("lengths",), (_P,)))
+                for n, t in zip(names, kinds)]
+
+
+def _scan_inputs(u, delta, a_log, b, c, skip, bias, z, lengths, device) -> tuple:
+    """(W, the sizes, the inputs) of a scan; u is (B, T, D), or (B, D) of a single step."""
+    shape, dtype = u.shape, u.dtype
+    _dtype(u, "u")
+    _sized(u, "u")
+    B, D = shape[0], shape[-1]
+    W, N = _per_worker(B, a_log, "a_log", 3), a_log.shape[2]
+    few = (*shape[:-1], N)
+    step = len(shape) == 2
+
+    def at(t, name, shape):
+        s = _input(t, name, shape, dtype, device)
+        return t.data_ptr(), s[0], 0 if step else s[1]
+
+    inputs = _ScanInputs(*at(u, "u", shape), *at(delta, "delta", shape), *((None, 0, 0) if z is None else at(z, "z", shape)),
+                         *at(b, "b", few), *at(c, "c", few), a_log.data_ptr(), _workers_part(a_log, "a_log", (D, N), W, device),
+                         skip.data_ptr(), _workers_part(skip, "skip", (D,), W, device), bias.data_ptr(),
+                         _workers_part(bias, "bias", (D,), W, device), _whole(lengths, "lengths", (B,), torch.int32, device))
+    return W, N, inputs
+
+
+def _of_one_model(a_log, skip, bias) -> tuple:
+    """The weights with an axis of workers."""
+    return (a_log[None], skip[None], bias[None]) if a_log.dim() == 2 and skip.dim() == bias.dim() == 1 else (a_log, skip, bias)
+
+
+def selective_scan(u, delta, a_log, b, c, skip, bias, z=None, h0=None, lengths=None, *, carry: bool = True, stream=None):
+    """With dt = softplus(delta + bias), h_t = exp(-dt exp(a_log)) h_(t-1) + dt u_t b_t
+    for N states per channel and y_t = (sum_n c_t h_t + skip u_t) silu(z_t), for B
+    sequences: (y, last, carry).
+
+    u, delta, z (B, T, D) float32 or bfloat16 (z None: no gate); b, c (B, T, N) of
+    the same type; a_log float32 (W, D, N) with N up to SCAN_MAX_STATES, skip and
+    bias (W, D): those of worker w are for the w-th of W equal groups of
+    sequences (one model's, without the axis W, are taken too); h0 float32
+    (B, D, N) or None for zeros; lengths int32 (B,) or None: beyond its length a
+    sequence keeps its state and y is 0. last float32 (B, D, N); carry, the states
+    at every CARRY_STEPS steps, is what the backward pass starts from
+    (carry=False: None)."""
+    a_log, skip, bias = _of_one_model(a_log, skip, bias)
+    _no_autograd(u=u, delta=delta, a_log=a_log, b=b, c=c, skip=skip, bias=bias, z=z, h0=h0)
+    device = _cuda(u, "u")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return selective_scan(u, delta, a_log, b, c, skip, bias, z, h0, lengths, carry=carry)
+    B, T, D = shape = _sequence_shape(u, "u")
+    W, N, inputs = _scan_inputs(u, delta, a_log, b, c, skip, bias, z, lengths, device)
+    h0_at = _whole(h0, "h0", (B, D, N), _F32, device)
+    y, last = torch.empty(shape, dtype=u.dtype, device=device), torch.empty((B, D, N), dtype=_F32, device=device)
+    carries = torch.empty((B, -(-T // CARRY_STEPS), D, N), dtype=_F32, device=device) if carry else None
+    needed = _entry("cpdp_selective_scan_workspace")(B, T, D, N)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_selective_scan")(ctypes.byref(inputs), _CODES[u.dtype], W, B, T, D, N, h0_at, y.data_ptr(), last.data_ptr(), _ptr(carries),
+                                         _ptr(work), needed, _stream(device.index)))
+    return y, last, carries
+
+
+def selective_scan_backward(dy, u, delta, a_log, b, c, skip, bias, carry, z=None, dlast=None, lengths=None, *, da_log=None, dskip=None,
+                            dbias=None, dtype=torch.float32, stream=None):
+    """Gradients of ``selective_scan`` from dy (B, T, D) and dlast float32
+    (B, D, N) or None: (du, ddelta, da_log, db, dc, dskip, dbias, dz, dh0), dz None
+    where there is no z. The weights' are written into the tensors given, float32
+    or bfloat16 all (views of the gradient rows, say), or into new ones of
+    ``dtype``."""
+    if a_log.dim() == 2 and skip.dim() == bias.dim() == 1:
+        da_log, dskip, dbias = (None if t is None else t[None] for t in (da_log, dskip, dbias))
+        out = selective_scan_backward(dy, u, delta, a_log[None], b, c, skip[None], bias[None], carry, z, dlast, lengths, da_log=da_log,
+                                      dskip=dskip, dbias=dbias, dtype=dtype, stream=stream)
+        return tuple(t[0] if i in (2, 5, 6) else t for i, t in enumerate(out))
+    _no_autograd(dy=dy, u=u, delta=delta, a_log=a_log, b=b, c=c, skip=skip, bias=bias, carry=carry, z=z, dlast=dlast, da_log=da_log,
+                 dskip=dskip, dbias=dbias)
+    device = _cuda(u, "u")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return selective_scan_backward(dy, u, delta, a_log, b, c, skip, bias, carry, z, dlast, lengths, da_log=da_log, dskip=dskip,
+                                           dbias=dbias, dtype=dtype)
+    B, T, D = shape = _sequence_shape(u, "u")
+    kind = u.dtype
+    W, N, inputs = _scan_inputs(u, delta, a_log, b, c, skip, bias, z, lengths, device)
+    gs = _input(dy, "dy", shape, kind, device)
+    carry_at = _whole(carry, "carry", (B, -(-T // CARRY_STEPS), D, N), _F32, device)
+    dlast_at = _whole(dlast, "dlast", (B, D, N), _F32, device)
+    given = [t for t in (da_log, dskip, dbias) if t is not None]
+    dtype = given[0].dtype if given else dtype
+    da_log = _gradient_out(da_log, "da_log", (W, D, N), dtype, device)
+    dskip, dbias = _gradient_out(dskip, "dskip", (W, D), dtype, device), _gradient_out(dbias, "dbias", (W, D), dtype, device)
+    if not da_log.dtype == dskip.dtype == dbias.dtype:
+        raise TypeError(f"da_log, dskip and dbias must have one type, got {da_log.dtype}, {dskip.dtype} and {dbias.dtype}")
+    du, ddelta = torch.empty(shape, dtype=kind, device=device), torch.empty(shape, dtype=kind, device=device)
+    dz = None if z is None else torch.empty(shape, dtype=kind, device=device)
+    db, dc = (torch.empty((B, T, N), dtype=kind, device=device) for _ in range(2))
+    dh0 = torch.empty((B, D, N), dtype=_F32, device=device)
+    needed = _entry("cpdp_selective_scan_backward_workspace")(B, T, D, N)
+    work = _workspace(needed, device)
+    _check(_entry("cpdp_selective_scan_backward")(
+        dy.data_ptr(), gs[0], gs[1], ctypes.byref(inputs), _CODES[kind], W, B, T, D, N, carry_at, dlast_at, du.data_ptr(), ddelta.data_ptr(),
+        _ptr(dz), db.data_ptr(), dc.data_ptr(), dh0.data_ptr(), da_log.data_ptr(), da_log.stride(0), dskip.data_ptr(), dskip.stride(0),
+        dbias.data_ptr(), dbias.stride(0), _CODES[dtype], _ptr(work), needed, _stream(device.index)))
+    return du, ddelta, da_log, db, dc, dskip, dbias, dz, dh0
+
+
+def selective_scan_step(u, delta, a_log, b, c, skip, bias, state, z=None, *, stream=None):
+    """One token for each of B sequences: ``state`` (float32, (B, D, N)) is
+    replaced by the next state, and y (B, D) is returned. u, delta, z (B, D); b, c
+    (B, N); the weights as those of ``selective_scan``."""
+    a_log, skip, bias = _of_one_model(a_log, skip, bias)
+    _no_autograd(u=u, delta=delta, a_log=a_log, b=b, c=c, skip=skip, bias=bias, state=state, z=z)
+    device = _cuda(u, "u")
+    if _elsewhere(device, stream):
+        with _there(device, stream):
+            return selective_scan_step(u, delta, a_log, b, c, skip, bias, state, z)
+    if u.dim() != 2:
+        raise ValueError(f"u must be (B, D), got {tuple(u.shape)}")
+    W, N, inputs = _scan_inputs(u, delta, a_log, b, c, skip, bias, z, None, device)
+    B, D = shape = u.shape
+    state_at = _whole(state, "state", (B, D, N), _F32, device)
+    y = torch.empty(shape, dtype=u.dtype, device=device)
+    _check(_entry("cpdp_selective_scan_step")(ctypes.byref(inputs), _CODES[u.dtype], W, B, D, N, state_at, y.data_ptr(), _stream(device.index)))
     return y
 
 

@@ -137,3 +137,118 @@ def conv_backward(dy, x, weight, bias, state, lengths, dlast):
     edb = edv + (B * T + 8) * U32 * dv.abs()
     return {"dx": dext[:, K - 1:], "edx": edext[:, K - 1:], "dstate": dext[:, :K - 1], "edstate": edext[:, :K - 1],
             "dweight": workers(dw), "edweight": workers(edw), "dbias": workers(dv.sum(1)), "edbias": workers(edb.sum(1))}
+
+
+def scan(u, delta, a_log, b, c, skip, bias, z, h0, lengths):
+    """A dict of y, last, the states before each step, and what the backward pass needs, with bounds (an e in front; an s
+    in front of a magnitude that the formula adds up). u (B, T, D), b (B, T, N), a_log (W, D, N)."""
+    B, T, D = u.shape
+    N = a_log.shape[2]
+    n = torch.full((B,), T) if lengths is None else lengths.long().clamp(0, T)
+    on = (torch.arange(T)[None] < n[:, None])[..., None]
+    inside = lambda t: torch.where(on, t.double(), 0.0)  # noqa: E731
+    u, delta, b, c = inside(u), inside(delta), inside(b), inside(c)
+    rate = torch.exp(per_sequence(a_log, B))
+    skips, biases = per_sequence(skip, B)[:, None], per_sequence(bias, B)[:, None]
+    raw = delta + biases
+    # the addition's rounding reaches dt through a slope of sigmoid(raw); then the power, a division, seven terms
+    slip = (delta.abs() + biases.abs()) * U32
+    dt = torch.where(on, torch.logaddexp(raw, torch.zeros_like(raw)), 0.0)
+    edt = torch.where(on, dt * (24 + 4 * raw.abs()) * U32 + torch.sigmoid(raw) * slip, 0.0)
+    x, ex = dt * u, u.abs() * edt + 2 * U32 * (dt * u).abs()
+    f = {"u": u, "b": b, "c": c, "rate": rate, "skip": skips, "raw": raw, "slip": slip, "dt": dt, "edt": edt, "x": x, "ex": ex, "on": on, "n": n,
+         "z": None if z is None else inside(z), "delta": delta}
+    h = torch.zeros(B, D, N, dtype=torch.float64) if h0 is None else h0.double()
+    sh, eh = h.abs(), torch.zeros_like(h)
+    for k in ("before", "sbefore", "ebefore", "after", "safter", "eafter", "a", "ea"):
+        f[k] = torch.zeros(B, T, D, N, dtype=torch.float64)
+    sums, esums = torch.zeros_like(u), torch.zeros_like(u)
+    for t in range(T):
+        p = dt[:, t, :, None] * rate
+        a = torch.exp(-p)
+        # exponent: the rate (a power, a product), the product with dt; segments compose decays of sums of dt
+        ea = a * ((16 + 16 * p) * U32 + edt[:, t, :, None] * rate)
+        f["before"][:, t], f["sbefore"][:, t], f["ebefore"][:, t], f["a"][:, t], f["ea"][:, t] = h, sh, eh, a, ea
+        add = x[:, t, :, None] * b[:, t, None]
+        eh = a * eh + ea * sh + ex[:, t, :, None] * b[:, t, None].abs()
+        h, sh = a * h + add, a * sh + add.abs()
+        eh = eh + 3 * U32 * sh
+        off = ~on[:, t, :, None]
+        eh = torch.where(off, f["ebefore"][:, t], eh)
+        f["after"][:, t], f["safter"][:, t], f["eafter"][:, t] = h, sh, eh
+        sums[:, t] = (h * c[:, t, None]).sum(-1)
+        esums[:, t] = (c[:, t, None].abs() * (eh + (N + 4) * U32 * sh)).sum(-1)
+    v = sums + skips * u
+    ev = esums + 2 * U32 * ((f["safter"] * c[:, :, None].abs()).sum(-1) + (skips * u).abs())
+    f.update(v=v, ev=ev, last=h, elast=eh)
+    if z is None:
+        f.update(y=torch.where(on, v, 0.0), ey=torch.where(on, ev, 0.0))
+    else:
+        gate = f["z"] * torch.sigmoid(f["z"])
+        f.update(y=torch.where(on, v * gate, 0.0), ey=torch.where(on, gate.abs() * (ev + (v.abs() + ev) * gate_error(f["z"])), 0.0))
+    return f
+
+
+def scan_backward(dy, u, delta, a_log, b, c, skip, bias, z, h0, dlast, lengths):
+    """A dict of the gradients with bounds."""
+    f = scan(u, delta, a_log, b, c, skip, bias, z, h0, lengths)
+    B, T, D = u.shape
+    W, N = a_log.shape[0], a_log.shape[2]
+    on, u, b, c, dt, edt, x, ex, rate, v = (f[k] for k in ("on", "u", "b", "c", "dt", "edt", "x", "ex", "rate", "v"))
+    dy = torch.where(on, dy.double(), 0.0)
+    r = {}
+    if z is None:
+        gy, egy = dy, torch.zeros_like(dy)
+    else:
+        gate = f["z"] * torch.sigmoid(f["z"])
+        gy = dy * gate
+        egy = gy.abs() * (gate_error(f["z"]) + 3 * U32)
+        slope = silu_slope(f["z"])
+        r["dz"] = dy * v * slope
+        r["edz"] = dy.abs() * (f["ev"] * slope.abs() + (v.abs() + f["ev"]) * 2 * gate_error(f["z"]))
+    g = torch.zeros(B, D, N, dtype=torch.float64) if dlast is None else dlast.double()
+    sg, eg = g.abs(), torch.zeros_like(g)
+    for k in ("through", "ethrough", "sthrough", "reach", "ereach", "sreach"):
+        r[k] = torch.zeros_like(u)
+    for k in ("db", "edb", "dc", "edc"):
+        r[k] = torch.zeros_like(b)
+    da, eda = torch.zeros_like(rate), torch.zeros_like(rate)
+    depth, long = (D / 32 + 24) * U32, (B // W * T + 40) * U32
+    for t in range(T - 1, -1, -1):
+        off = ~on[:, t, :, None]
+        a, ea, cs, bs = f["a"][:, t], f["ea"][:, t], c[:, t, None], b[:, t, None]
+        gyt, egyt, xt, ext = gy[:, t, :, None], egy[:, t, :, None], x[:, t, :, None], ex[:, t, :, None]
+        h, sh, eh = f["after"][:, t], f["safter"][:, t], f["eafter"][:, t]
+        old, sold, eold = f["before"][:, t], f["sbefore"][:, t], f["ebefore"][:, t]
+        flow, sflow = g + gyt * cs, sg + (gyt * cs).abs()
+        eflow = eg + egyt * cs.abs() + 2 * U32 * sflow
+        r["dc"][:, t] = (gyt * h).sum(1)
+        r["edc"][:, t] = (egyt * sh + gyt.abs() * eh + depth * gyt.abs() * sh).sum(1)
+        r["db"][:, t] = (flow * xt).sum(1)
+        r["edb"][:, t] = (eflow * xt.abs() + (sflow + eflow) * ext + depth * sflow * xt.abs()).sum(1)
+        r["through"][:, t] = (flow * bs).sum(-1)
+        r["sthrough"][:, t] = (sflow * bs.abs()).sum(-1)
+        r["ethrough"][:, t] = (eflow * bs.abs()).sum(-1) + (N + 8) * U32 * r["sthrough"][:, t]
+        k, sk = a * flow * old, a * sflow * sold
+        ek = a * (eflow * sold + (sflow + eflow) * eold) + ea * (sflow + eflow) * (sold + eold) + 4 * U32 * sk
+        r["reach"][:, t] = (k * rate).sum(-1)
+        r["sreach"][:, t] = (sk * rate).sum(-1)
+        r["ereach"][:, t] = (ek * rate).sum(-1) + (N + 16) * U32 * r["sreach"][:, t]
+        da -= k * dt[:, t, :, None] * rate
+        eda += rate * (ek * dt[:, t, :, None] + sk * edt[:, t, :, None] + long * sk * dt[:, t, :, None])
+        new, enew = a * flow, a * eflow + ea * (sflow + eflow) + 2 * U32 * a * sflow
+        g, sg, eg = torch.where(off, g, new), torch.where(off, sg, a * sflow), torch.where(off, eg, enew)
+    sig = torch.sigmoid(f["raw"])
+    dsize = r["through"] * u - r["reach"]
+    ssize = r["sthrough"] * u.abs() + r["sreach"]
+    esize = r["ethrough"] * u.abs() + r["ereach"] + 6 * U32 * ssize
+    dbase = torch.where(on, dsize * sig, 0.0)
+    edbase = torch.where(on, sig * (esize + ssize * (gate_error(f["raw"]) + f["slip"])), 0.0)
+    workers = lambda t: t.unflatten(0, (W, B // W)).sum(1)  # noqa: E731
+    skips = f["skip"]
+    r["du"] = r["through"] * dt + skips * gy
+    r["edu"] = r["ethrough"] * dt + r["sthrough"] * edt + skips.abs() * egy + 4 * U32 * (r["sthrough"] * dt + (skips * gy).abs())
+    r.update(ddelta=dbase, eddelta=edbase, da_log=workers(da), eda_log=workers(eda), dskip=workers((gy * u).sum(1)),
+             edskip=workers((egy * u.abs() + long * (gy * u).abs()).sum(1)), dbias=workers(dbase.sum(1)),
+             edbias=workers((edbase + long * (dbase.abs() + edbase)).sum(1)), dh0=g, edh0=eg)
+    return r
