@@ -12,28 +12,56 @@ namespace {
 // A sequence's inputs with the K - 1 before it: e_0 .. e_(T+K-2), e_(K-1) = x_0,
 // and v_t = bias + sum_k weight_k e_(t+k). A thread walks a stretch of steps of V
 // neighbouring channels (16 or 8 bytes; 1 where rows are not whole pieces), with
-// the last K - 1 inputs in registers; kAhead rows are loaded at a time. Both
-// passes are bound by memory.
+// the last K - 1 inputs in registers, two channels to a pair; while kAhead rows
+// are worked on, the next are on their way. Both passes are bound by memory.
 constexpr int kThreads = 128, kAhead = 4;
 constexpr int kMostTaps = CPDP_CONV_MAX_TAPS;
 
+// V neighbouring elements as they lie in memory, loaded where they are there; else 0. Predicates, not branches: see load_once.
 template <typename T, int V>
-struct alignas(V * sizeof(T)) Few {
-    T e[V];
+struct Few {
+    static constexpr int kBytes = V * sizeof(T), kWords = (kBytes + 3) / 4, P = (V + 1) / 2;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p, bool there) {
+        const uint32_t on = there ? 1u : 0u;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0u;
+        if constexpr (kBytes == 16)
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                         : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])
+                         : "l"(p), "r"(on)
+                         : "memory");
+        else if constexpr (kBytes == 8)
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\t@p ld.global.v2.u32 {%0, %1}, [%2];\n\t}"
+                         : "+r"(w[0]), "+r"(w[1])
+                         : "l"(p), "r"(on)
+                         : "memory");
+        else if constexpr (kBytes == 4)
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(w[0]) : "l"(p), "r"(on) : "memory");
+        else
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u16 %0, [%1];\n\t}" : "+r"(w[0]) : "l"(p), "r"(on) : "memory");
+    }
+    __device__ __forceinline__ void get(Pair (&v)[P]) const {
+        if constexpr (V == 1) {
+            v[0] = pair(sizeof(T) == 4 ? __uint_as_float(w[0]) : __uint_as_float(w[0] << 16), 0.f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                v[i] = sizeof(T) == 4 ? pair(__uint_as_float(w[2 * i % kWords]), __uint_as_float(w[(2 * i + 1) % kWords]))
+                                      : pair(__uint_as_float(w[i % kWords] << 16), __uint_as_float(w[i % kWords] & 0xffff0000u));
+        }
+    }
 };
 template <typename T, int V>
-__device__ __forceinline__ void load_few(float (&v)[V], const T* p, bool there) {
-    Few<T, V> f{};
-    if (there) f = *reinterpret_cast<const Few<T, V>*>(p);
+__device__ __forceinline__ void store_few(T* p, const Pair (&v)[(V + 1) / 2]) {
+    if constexpr (V == 1) {
+        *p = from_float<T>(floats(v[0]).x);
+    } else {
+        float x[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = there ? to_float(f.e[i]) : 0.f;
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_few(T* p, const float (&v)[V]) {
-    Few<T, V> f;
-#pragma unroll
-    for (int i = 0; i < V; ++i) f.e[i] = from_float<T>(v[i]);
-    *reinterpret_cast<Few<T, V>*>(p) = f;
+        for (int i = 0; i < V; ++i) x[i] = i % 2 ? floats(v[i / 2]).y : floats(v[i / 2]).x;
+        store_piece<V>(p, x);
+    }
 }
 
 struct Conv {
@@ -49,15 +77,23 @@ struct Conv {
 
 template <typename T, int V, int K>
 struct Taps {
-    float w[K][V], bias[V];
+    static constexpr int P = (V + 1) / 2;
+    Pair w[K][P], bias[P];
     __device__ __forceinline__ Taps(const Conv& p, int worker, int d) {
-        const float* from = p.weight + worker * p.weight_worker + (int64_t)d * K;
+        const float *from = p.weight + worker * p.weight_worker + (int64_t)d * K, *b = p.bias + worker * p.bias_worker + d;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
+        for (int i = 0; i < P; ++i) {
+            constexpr int next = V > 1;
 #pragma unroll
-            for (int k = 0; k < K; ++k) w[k][i] = from[i * K + k];
-            bias[i] = p.bias[worker * p.bias_worker + d + i];
+            for (int k = 0; k < K; ++k) w[k][i] = pair(from[2 * i * K + k], next ? from[(2 * i + next) * K + k] : 0.f);
+            bias[i] = pair(b[2 * i], next ? b[2 * i + next] : 0.f);
         }
+    }
+    __device__ __forceinline__ Pair sum(const Pair (&e)[K][P], int i) const {
+        Pair v = bias[i];
+#pragma unroll
+        for (int k = 0; k < K; ++k) v = fma2(w[k][i], e[k][i], v);
+        return v;
     }
 };
 
@@ -70,65 +106,64 @@ struct Inputs {
     __device__ __forceinline__ Inputs(const Conv& p, int64_t b, int d)
         : x(static_cast<const T*>(p.x) + b * p.x_seq + d), state(p.state == nullptr ? nullptr : static_cast<const T*>(p.state) + b * (K - 1) * p.D + d),
           step(p.x_step), D(p.D), n(p.lengths == nullptr ? p.T : min(max(p.lengths[b], 0), p.T)) {}
-    __device__ __forceinline__ void get(float (&v)[V], int e) const {  // 0 behind the last
+    // e_k, 0 behind the last
+    __device__ __forceinline__ void get(Pair (&v)[(V + 1) / 2], int e) const {
+        Few<T, V> f;
         if (e < K - 1)
-            load_few<T, V>(v, state + (int64_t)e * D, state != nullptr);
+            f.load(state + (int64_t)e * D, state != nullptr);
         else
-            load_few<T, V>(v, x + (int64_t)(e - (K - 1)) * step, e - (K - 1) < n);
+            f.load(x + (int64_t)(e - (K - 1)) * step, e - (K - 1) < n);
+        f.get(v);
+    }
+    // kAhead rows of x from step t on
+    __device__ __forceinline__ void rows(Few<T, V> (&f)[kAhead], int t) const {
+        const T* p = x + t * step;
+#pragma unroll
+        for (int r = 0; r < kAhead; ++r) f[r].load(p + r * step, t + r < n);
     }
 };
-
-// silu(v) and, where asked for, its slope, for V channels.
-template <typename T, int V, bool SLOPE>
-__device__ __forceinline__ void silu(const float (&v)[V], float (&y)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; i += 2) {
-        const Pair x = pair(v[i], i + 1 < V ? v[i + 1] : 0.f);
-        Pair a, rest;
-        gate_of<T>(x, a, rest);
-        const float2 r = floats(SLOPE ? mul2(a, fma2(x, rest, kOnes)) : mul2(x, a));
-        y[i] = r.x;
-        if (i + 1 < V) y[i + 1] = r.y;
-    }
-}
 
 template <typename T, int V, int K>
 __global__ void __launch_bounds__(kThreads)
 conv_kernel(Conv p, T* y, T* last) {
     layer_begin();
+    constexpr int P = (V + 1) / 2;
     const int64_t columns = p.D / V, i = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = i / columns;
     const int64_t b = row / p.stretches;
     if (b >= p.B) return;
     const int d = static_cast<int>(i - row * columns) * V, stretch = static_cast<int>(row - b * p.stretches);
-    const Taps<T, V, K> taps(p, static_cast<int>(b / p.each), d);
     const Inputs<T, V, K> in(p, b, d);
     const int first = stretch * p.steps, end = min(first + p.steps, p.T), inside = min(end, in.n);
-    float e[K][V];
+    Few<T, V> next[kAhead];
+    in.rows(next, first);
+    Pair e[K][P];
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) in.get(e[k], first + k);
+    const Taps<T, V, K> taps(p, static_cast<int>(b / p.each), d);
     T* to = y + (b * p.T + first) * p.D + d;
     for (int t = first; t < inside; t += kAhead) {
-        float next[kAhead][V];
+        Few<T, V> now[kAhead];
 #pragma unroll
-        for (int r = 0; r < kAhead; ++r) in.get(next[r], t + r + K - 1);
+        for (int r = 0; r < kAhead; ++r) now[r] = next[r];
+        if (t + kAhead < inside) in.rows(next, t + kAhead);
 #pragma unroll
         for (int r = 0; r < kAhead; ++r) {
-            float v[V], out[V];
+            Pair out[P];
+            now[r].get(e[K - 1]);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                e[K - 1][i] = next[r][i];
-                v[i] = taps.bias[i];
-#pragma unroll
-                for (int k = 0; k < K; ++k) v[i] = fmaf(taps.w[k][i], e[k][i], v[i]);
+            for (int i = 0; i < P; ++i) {
+                const Pair v = taps.sum(e, i);
+                Pair a, rest;
+                gate_of<T>(v, a, rest);
+                out[i] = mul2(v, a);
 #pragma unroll
                 for (int k = 0; k + 1 < K; ++k) e[k][i] = e[k + 1][i];
             }
-            silu<T, V, false>(v, out);
             if (t + r < inside) store_few<T, V>(to, out);
             to += p.D;
         }
     }
-    const float none[V] = {};
+    const Pair none[P] = {};
     to = y + (b * p.T + max(first, inside)) * p.D + d;
     for (int t = max(first, inside); t < end; ++t, to += p.D) store_few<T, V>(to, none);
     if (stretch == 0 && last != nullptr)
@@ -158,78 +193,88 @@ __global__ void __launch_bounds__(kThreads)
 conv_backward_kernel(Conv p, ConvGradients g) {
     layer_begin();
     __shared__ float shared[kThreads][V * (K + 1) + 1];
+    constexpr int P = (V + 1) / 2;
     const int lane = threadIdx.x % g.lanes, team = threadIdx.x / g.lanes, teams = kThreads / g.lanes;
     const int group = blockIdx.x % g.groups, rest = blockIdx.x / g.groups, part = rest % g.part_count, worker = rest / g.part_count;
     const int d = (group * g.lanes + lane) * V;
     const bool live = d < p.D;
-    float dw[K][V] = {}, db[V] = {};
+    Pair dw[K][P] = {}, db[P] = {};
     if (live) {
         const Taps<T, V, K> taps(p, worker, d);
-        const int64_t items = (int64_t)p.each * p.stretches;
-        for (int64_t item = part * teams + team; item < items; item += (int64_t)g.part_count * teams) {
+        const int items = p.each * p.stretches;
+        for (int item = part * teams + team; item < items; item += g.part_count * teams) {
             const int64_t b = (int64_t)worker * p.each + item / p.stretches;
             const Inputs<T, V, K> in(p, b, d);
             const T* dy = static_cast<const T*>(g.dy) + b * g.dy_seq + d;
-            const int first = static_cast<int>(item % p.stretches) * p.steps, end = min(first + p.steps, p.T + K - 1);
+            const int first = item % p.stretches * p.steps, end = min(first + p.steps, p.T + K - 1);
             const int from = max(first - (K - 1), 0), inside = min(end, in.n);
-            float e[K][V], dv[K][V] = {};  // dv[k]: of step t - k
+            Few<T, V> next[kAhead], next_dy[kAhead];
+            const auto fetch = [&](int t) {
+                in.rows(next, t);
+                const T* q = dy + t * g.dy_step;
 #pragma unroll
-            for (int k = 0; k < K - 1; ++k) in.get(e[k], from + k);
+                for (int r = 0; r < kAhead; ++r) next_dy[r].load(q + r * g.dy_step, t + r < inside);
+            };
+            fetch(from);
+            Pair e[K][P] = {}, dv[K][P] = {};  // dv[k]: of step t - k
+            if (in.n > 0)
+#pragma unroll
+                for (int k = 0; k < K - 1; ++k) in.get(e[k], from + k);
             for (int t0 = from; t0 < end; t0 += kAhead) {
-                float next[kAhead][V], grad[kAhead][V];
+                Few<T, V> now[kAhead], now_dy[kAhead];
 #pragma unroll
-                for (int r = 0; r < kAhead; ++r) {
-                    in.get(next[r], t0 + r + K - 1);
-                    load_few<T, V>(grad[r], dy + (int64_t)(t0 + r) * g.dy_step, t0 + r < inside);
-                }
+                for (int r = 0; r < kAhead; ++r) now[r] = next[r], now_dy[r] = next_dy[r];
+                if (t0 + kAhead < end) fetch(t0 + kAhead);
 #pragma unroll
                 for (int r = 0; r < kAhead; ++r) {
                     const int t = t0 + r;
-                    float v[V], slope[V], out[V];
+                    Pair out[P], dy_r[P];
+                    now[r].get(e[K - 1]);
+                    now_dy[r].get(dy_r);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        e[K - 1][i] = next[r][i];
-                        v[i] = taps.bias[i];
-#pragma unroll
-                        for (int k = 0; k < K; ++k) v[i] = fmaf(taps.w[k][i], e[k][i], v[i]);
-                    }
-                    silu<T, V, true>(v, slope);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
+                    for (int i = 0; i < P; ++i) {
+                        const Pair v = taps.sum(e, i);
+                        Pair a, away;
+                        gate_of<T>(v, a, away);
 #pragma unroll
                         for (int k = K - 1; k > 0; --k) dv[k][i] = dv[k - 1][i];
-                        dv[0][i] = t < inside ? grad[r][i] * slope[i] : 0.f;
-                        const float own = t >= first && t < inside ? dv[0][i] : 0.f;
-                        db[i] += own;
-                        out[i] = 0.f;
+                        dv[0][i] = t < inside ? mul2(dy_r[i], mul2(a, fma2(v, away, kOnes))) : kZeros;
+                        const Pair own = t >= first ? dv[0][i] : kZeros;
+                        db[i] = add2(db[i], own);
+                        out[i] = mul2(taps.w[0][i], dv[0][i]);
+                        dw[0][i] = fma2(own, e[0][i], dw[0][i]);
 #pragma unroll
-                        for (int k = 0; k < K; ++k) {
-                            dw[k][i] = t < inside ? fmaf(own, e[k][i], dw[k][i]) : dw[k][i];
-                            out[i] = fmaf(taps.w[k][i], dv[k][i], out[i]);
+                        for (int k = 1; k < K; ++k) {
+                            dw[k][i] = fma2(own, e[k][i], dw[k][i]);
+                            out[i] = fma2(taps.w[k][i], dv[k][i], out[i]);
                         }
 #pragma unroll
                         for (int k = 0; k + 1 < K; ++k) e[k][i] = e[k + 1][i];
                     }
-                    if (t < first || t >= end) continue;
                     if (g.dlast != nullptr && t >= in.n && t < in.n + K - 1) {
-                        float more[V];
-                        load_few<T, V>(more, static_cast<const T*>(g.dlast) + (b * (K - 1) + t - in.n) * p.D + d, true);
+                        Few<T, V> f;
+                        Pair more[P];
+                        f.load(static_cast<const T*>(g.dlast) + (b * (K - 1) + t - in.n) * p.D + d, true);
+                        f.get(more);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) out[i] += more[i];
+                        for (int i = 0; i < P; ++i) out[i] = add2(out[i], more[i]);
                     }
-                    if (t >= K - 1)
-                        store_few<T, V>(static_cast<T*>(g.dx) + (b * p.T + t - (K - 1)) * p.D + d, out);
-                    else if (g.dstate != nullptr)
-                        store_few<T, V>(static_cast<T*>(g.dstate) + (b * (K - 1) + t) * p.D + d, out);
+                    if (t >= first && t < end) {
+                        if (t >= K - 1)
+                            store_few<T, V>(static_cast<T*>(g.dx) + (b * p.T + t - (K - 1)) * p.D + d, out);
+                        else if (g.dstate != nullptr)
+                            store_few<T, V>(static_cast<T*>(g.dstate) + (b * (K - 1) + t) * p.D + d, out);
+                    }
                 }
             }
         }
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
+        const auto half = [&](Pair v) { return i % 2 ? floats(v).y : floats(v).x; };
 #pragma unroll
-        for (int k = 0; k < K; ++k) shared[threadIdx.x][i * K + k] = dw[k][i];
-        shared[threadIdx.x][V * K + i] = db[i];
+        for (int k = 0; k < K; ++k) shared[threadIdx.x][i * K + k] = half(dw[k][i / 2]);
+        shared[threadIdx.x][V * K + i] = half(db[i / 2]);
     }
     __syncthreads();
     if (team > 0 || !live) return;
@@ -256,13 +301,15 @@ conv_step_kernel(Conv p, T* state, T* y) {
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) e[k] = s[(int64_t)k * p.D];
     e[K - 1] = static_cast<const T*>(p.x)[b * p.x_seq + d];
-    float v[1] = {taps.bias[0]}, out[1];
+    Pair held[K][1];
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[0] = fmaf(taps.w[k][0], to_float(e[k]), v[0]);
-    silu<T, 1, false>(v, out);
+    for (int k = 0; k < K; ++k) held[k][0] = pair(to_float(e[k]), 0.f);
+    const Pair v = taps.sum(held, 0);
+    Pair a, rest;
+    gate_of<T>(v, a, rest);
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) s[(int64_t)k * p.D] = e[k + 1];
-    y[i] = from_float<T>(out[0]);
+    y[i] = from_float<T>(floats(mul2(v, a)).x);
 }
 
 cpdp_status check_conv(int W, int B, int64_t T, int D, int K, cpdp_dtype dtype) {
@@ -279,7 +326,7 @@ cpdp_status check_conv(int W, int B, int64_t T, int D, int K, cpdp_dtype dtype) 
 
 // Steps of a stretch: enough threads for `threads` in all, within [least, 128].
 int stretch_of(int64_t rows, int64_t columns, int64_t least, int64_t threads) {
-    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(ceil_div(rows * columns, threads), least), 128));
+    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(ceil_div(rows * columns, threads), least), 128) / kAhead * kAhead);
 }
 
 // Whether rows of an array are whole pieces of `bytes`.
@@ -346,7 +393,7 @@ cpdp_status cpdp_causal_conv(const void* x, int64_t x_seq, int64_t x_step, const
         using E = std::remove_pointer_t<decltype(out)>;
         constexpr int V = decltype(many)::value;
         const int64_t columns = D / V;
-        p.steps = stretch_of((int64_t)B * T, columns, 8, kSMs * 1536);
+        p.steps = stretch_of((int64_t)B * T, columns, 8, kSMs * 768);
         p.stretches = static_cast<int>(std::max<int64_t>(ceil_div(T, p.steps), 1));
         const int64_t blocks = ceil_div((int64_t)B * p.stretches * columns, kThreads);
         if (blocks > kLayerMaxRows) return cudaErrorInvalidConfiguration;

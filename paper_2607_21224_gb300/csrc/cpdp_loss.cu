@@ -357,18 +357,27 @@ struct WriteOut {
     const int64_t* targets;
     int a_extent, b_extent, add;
     __device__ __forceinline__ void run(const float (&v)[kHalf], int w, int s, int a, int b) const {
+        // which of the columns' tokens are ignored: a load beside each store would wait for the store before it
+        uint32_t ignored[kHalf / 32] = {};
+        if (targets != nullptr)
+#pragma unroll
+            for (int j = 0; j < kHalf / 32; ++j) {
+                const int at = b + j * 32 + static_cast<int>(threadIdx.x % 32);
+                ignored[j] = __ballot_sync(~0u, at < b_extent && targets[(int64_t)w * b_extent + at] < 0);
+            }
+        const float f = factor != nullptr ? factor[w] : 1.f;
         if (a >= a_extent) return;
         G* to = out + w * worker + s * split + b * row + a;
-        const float f = factor != nullptr ? factor[w] : 1.f;
-        const int64_t* t = targets != nullptr ? targets + (int64_t)w * b_extent + b : nullptr;
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) {
             if (b + j < b_extent) {
-                float x = v[j];
-                if (factor != nullptr) x *= f;
-                if (t != nullptr && t[j] < 0) x = 0.f;
-                if constexpr (sizeof(G) == 4)
-                    if (add) x += to[j * row];
+                const float x = ignored[j / 32] >> j % 32 & 1 ? 0.f : v[j] * f;
+                if constexpr (sizeof(G) == 4) {
+                    if (add) {  // one addition to each element per launch: the order is that of the launches
+                        asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to + j * row), "f"(x) : "memory");
+                        continue;
+                    }
+                }
                 to[j * row] = from_float<G>(x);
             }
         }
@@ -376,18 +385,35 @@ struct WriteOut {
 };
 
 // The sum of the splits' parts [split][W][rows][D], in their order, times the worker's factor; 0 in ignored tokens' rows.
-template <typename G>
+// A warp per row; V neighbouring elements per lane.
+template <typename G, int V>
 __global__ void __launch_bounds__(256)
-sum_parts_kernel(const float* parts, int splits, int64_t per_worker, int64_t all, int D, const float* factor, const int64_t* targets, G* out,
+sum_parts_kernel(const float* parts, int splits, int64_t rows_each, int64_t rows, int D, const float* factor, const int64_t* targets, G* out,
                  int64_t worker) {
     layer_begin();
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
-        float s = 0.f;
-        for (int k = 0; k < splits; ++k) s += load_once(parts + k * all + at);
-        const int64_t w = at / per_worker, in = at - w * per_worker;
-        s *= factor[w];
-        if (targets != nullptr && targets[at / D] < 0) s = 0.f;
-        out[w * worker + in] = from_float<G>(s);
+    const int lane = threadIdx.x % 32;
+    const int64_t all = rows * D;
+    for (int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; r < rows; r += (int64_t)gridDim.x * 8) {
+        const int64_t w = r / rows_each;
+        const float f = targets != nullptr && targets[r] < 0 ? 0.f : factor[w];
+        const float* p = parts + r * D;
+        G* to = out + w * worker + (r - w * rows_each) * D;
+#pragma unroll 4
+        for (int k = lane * V; k < D; k += 32 * V) {
+            float s[V] = {};
+            for (int i = 0; i < splits; ++i) {
+                Piece<float, V> v{};
+                if constexpr (V == 1)
+                    v.load(p + i * all + k, true);
+                else
+                    v.load(p + i * all + k);
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[e] += v.get(e);
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[e] = f == 0.f ? 0.f : s[e] * f;
+            store_piece<V>(to + k, s);
+        }
     }
 }
 
@@ -455,7 +481,7 @@ factor_kernel(const float* dloss, const int64_t* targets, int64_t M, float* r, f
 
 // -- the host's side -------------------------------------------------------------------------------------------------
 
-constexpr int64_t kPieceBytes = int64_t(256) << 20;  // of d at a time
+constexpr int64_t kPieceBytes = int64_t(1) << 30;  // of d at a time
 
 int64_t padded(int64_t bytes) { return ceil_div(bytes, 256) * 256; }
 int64_t pitch_of(int64_t n) { return ceil_div(n, 8) * 8; }
@@ -660,6 +686,15 @@ cpdp_status cpdp_linear_cross_entropy(const void* x, int64_t x_worker, int64_t x
 }
 
 template <typename G>
+static cudaError_t sum_parts(const float* parts, int splits, int64_t rows_each, int W, int D, const float* factor, const int64_t* targets, G* out,
+                             int64_t worker, void* stream) {
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows_each * W, 8), kSMs * 8));
+    const bool fours = D % 4 == 0 && aligned_to(out, 4 * sizeof(G)) && (W == 1 || worker % 4 == 0);
+    return launch_layer(fours ? sum_parts_kernel<G, 4> : sum_parts_kernel<G, 1>, blocks, 256, 0, stream, parts, splits, rows_each, rows_each * W, D, factor,
+                        targets, out, worker);
+}
+
+template <typename G>
 static cpdp_status zero_rows(G* out, int64_t worker, int W, int64_t each, void* stream) {
     for (int w = 0; w < W; ++w) {
         const cudaError_t e = cudaMemsetAsync(out + w * worker, 0, each * sizeof(G), static_cast<cudaStream_t>(stream));
@@ -710,7 +745,6 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
     CPDP_TRY(encode(&x_columns, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kStep));
     CPDP_TRY(encode(&w_rows, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileB));
     CPDP_TRY(encode(&w_columns, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kStep));
-    const unsigned sum_blocks = kSMs * 8;
     for (int piece = 0; piece < plan.pieces; ++piece) {
         const int first = piece * plan.words, words = std::min(plan.words, V - first);
         const int64_t plane = rows * plan.pitch;
@@ -743,12 +777,7 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         if (plan.dweight_parts) {
             CPDP_TRY((multiply_all<true, true>(x_columns, d_columns, p,
                                                WriteOut<float>{dweight_parts, part, W * part, D, nullptr, nullptr, D, words, 0}, stream, what)));
-            const auto sum = [&](auto* out) {
-                return launch_layer(sum_parts_kernel<std::remove_pointer_t<decltype(out)>>,
-                                    static_cast<unsigned>(std::min<int64_t>(ceil_div(W * part, 256), sum_blocks)), 256, 0, stream,
-                                    static_cast<const float*>(dweight_parts), p.splits, part, W * part, D, static_cast<const float*>(factor),
-                                    static_cast<const int64_t*>(nullptr), out + (int64_t)first * D, dweight_worker);
-            };
+            const auto sum = [&](auto* out) { return sum_parts(dweight_parts, p.splits, words, W, D, factor, nullptr, out + (int64_t)first * D, dweight_worker, stream); };
             CPDP_TRY(layer_launched(dweight_dtype == CPDP_F32 ? sum(static_cast<float*>(dweight)) : sum(static_cast<__nv_bfloat16*>(dweight)), what));
         } else {
             const auto write = [&](auto* out) {
@@ -760,11 +789,6 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         }
     }
     if (!plan.dx_parts) return CPDP_OK;
-    const auto sum = [&](auto* out) {
-        return launch_layer(sum_parts_kernel<std::remove_pointer_t<decltype(out)>>,
-                            static_cast<unsigned>(std::min<int64_t>(ceil_div(rows * D, 256), sum_blocks)), 256, 0, stream,
-                            static_cast<const float*>(dx_parts), plan.dx.count, M * D, rows * D, D, static_cast<const float*>(factor), targets, out,
-                            M * D);
-    };
+    const auto sum = [&](auto* out) { return sum_parts(dx_parts, plan.dx.count, M, W, D, factor, targets, out, M * D, stream); };
     return layer_launched(dtype == CPDP_F32 ? sum(static_cast<float*>(dx)) : sum(static_cast<__nv_bfloat16*>(dx)), what);
 }
