@@ -328,7 +328,8 @@ cpdp_status cpdp_causal_conv_step(const void *x, int64_t x_seq, const float *wei
  * (w + 1) * B / W - 1 (W divides B).
  *   u, delta, z  [B][T][D] of dtype, each with a sequence and a step stride; z
  *            NULL: no gate, silu(z) is 1
- *   b, c     [B][T][N] of dtype, with strides
+ *   b, c     [B][T][N] of dtype, with strides. Step strides are below 2^28 where
+ *            T > 1.
  *   a_log, skip, bias  float32, worker w's [D][N], [D] and [D] at + w * their
  *            strides
  *   lengths  int32 [B], each sequence's number of steps, clamped to 0..T (NULL: T

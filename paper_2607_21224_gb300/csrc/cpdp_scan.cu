@@ -48,59 +48,84 @@ struct Scan {
     Pair* maps;              // [column][segment][P * 5][32 lanes]
 };
 
-__device__ __forceinline__ float load_if(const float* p, bool there) {
+// Where `there`, else 0; ALL: there. Predicates, not branches: see load_once.
+template <bool ALL>
+__device__ __forceinline__ float load_if(const void* p, bool there) {
     float v = 0.f;
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.f32 %0, [%1];\n\t}" : "+f"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
+    if constexpr (ALL)
+        asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.f32 %0, [%1];\n\t}" : "+f"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
     return v;
 }
+template <bool ALL>
 __device__ __forceinline__ uint32_t load_word_if(const void* p, bool there) {
     uint32_t v = 0;
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
+    if constexpr (ALL)
+        asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
     return v;
 }
+template <bool ALL>
 __device__ __forceinline__ uint32_t load_half_if(const void* p, bool there) {
     uint32_t v = 0;
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u16 %0, [%1];\n\t}" : "+r"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
+    if constexpr (ALL)
+        asm volatile("ld.global.u16 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.u16 %0, [%1];\n\t}" : "+r"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
     return v;
 }
+template <bool ALL>
 __device__ __forceinline__ Pair load_pair_if(const void* p, bool there) {
     Pair v = 0;
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.b64 %0, [%1];\n\t}" : "+l"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
+    if constexpr (ALL)
+        asm volatile("ld.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.b64 %0, [%1];\n\t}" : "+l"(v) : "l"(p), "r"(there ? 1u : 0u) : "memory");
     return v;
 }
 
-// Two neighbouring elements as they lie in memory. WIDE: at a multiple of their size; the second is there where the first is.
+// Two neighbouring elements as they lie in memory. WIDE: at a multiple of their size; the second is there where the first
+// is. ALL: both are.
 template <typename T, bool WIDE>
 struct Two;
 template <>
 struct Two<float, true> {
     Pair v;
-    __device__ __forceinline__ void load(const float* p, bool first, bool) { v = load_pair_if(p, first); }
+    template <bool ALL>
+    __device__ __forceinline__ void load(const float* p, bool first, bool) {
+        v = load_pair_if<ALL>(p, first);
+    }
     __device__ __forceinline__ Pair get() const { return v; }
 };
 template <>
 struct Two<float, false> {
     float x, y;
-    __device__ __forceinline__ void load(const float* p, bool first, bool second) { x = load_if(p, first), y = load_if(p + 1, second); }
+    template <bool ALL>
+    __device__ __forceinline__ void load(const float* p, bool first, bool second) {
+        x = load_if<ALL>(p, first), y = load_if<ALL>(p + 1, second);
+    }
     __device__ __forceinline__ Pair get() const { return pair(x, y); }
 };
 template <>
 struct Two<__nv_bfloat16, true> {
     uint32_t v;
-    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool first, bool) { v = load_word_if(p, first); }
+    template <bool ALL>
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool first, bool) {
+        v = load_word_if<ALL>(p, first);
+    }
     __device__ __forceinline__ Pair get() const { return pair(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
 };
 template <>
 struct Two<__nv_bfloat16, false> {
     uint32_t x, y;
+    template <bool ALL>
     __device__ __forceinline__ void load(const __nv_bfloat16* p, bool first, bool second) {
-        x = load_half_if(p, first), y = load_half_if(p + 1, second);
+        x = load_half_if<ALL>(p, first), y = load_half_if<ALL>(p + 1, second);
     }
     __device__ __forceinline__ Pair get() const { return pair(__uint_as_float(x << 16), __uint_as_float(y << 16)); }
 };
-__device__ __forceinline__ uint32_t load_bits(const float* p, bool there) { return __float_as_uint(load_if(p, there)); }
-__device__ __forceinline__ uint32_t load_bits(const __nv_bfloat16* p, bool there) { return load_half_if(p, there) << 16; }
-
 template <bool WIDE>
 __device__ __forceinline__ void store_two(float* p, Pair both, bool second) {
     const float2 v = floats(both);
@@ -157,8 +182,9 @@ template <typename X>
 struct Lane {
     int lane, q, g, turn, channel;  // channel: of the column, the lane's first
     __device__ __forceinline__ Lane()
-        : lane(threadIdx.x % 32), q(lane % X::S), g(lane / X::S), turn((g & 1) << 1 | (g >> 1 & 1)), channel(g * X::C) {}
+        : lane(threadIdx.x % 32), q(lane % X::S), g(lane / X::S), turn((g & 1) << 1), channel(g * X::C) {}
     __device__ __forceinline__ int pair_at(int p) const { return X::P == 2 ? channel + 2 * (p ^ (q & 1)) : channel; }
+    __device__ __forceinline__ int summed_state() const { return 4 * q + turn + (g >> 1 & 1); }
     // Of sums of pairs over states, the channel's whose sum the lane gets.
     __device__ __forceinline__ int summed_channel() const {
         return X::P == 2 ? channel + 2 * (q & 1) + (q >> 1 & 1) : channel + (q & 1);
@@ -180,12 +206,13 @@ __device__ __forceinline__ float over_states(const Lane<X>& l, const Pair (&v)[X
     }
 }
 // Sums over the groups of lanes: of x and y for the lane's 4 states (in its order). The lane gets that of state
-// 4 q + turn; of x, of y where `second`, or of both (S = 8).
+// summed_state(); of x, of y where `second`, or of both (S = 8).
 template <typename X>
 __device__ __forceinline__ float2 over_channels(const Lane<X>& l, const float (&x)[4], const float (&y)[4]) {
     const auto add = [](float keep, float send, int mask) { return keep + __shfl_xor_sync(~0u, send, mask); };
     const float x0 = add(x[0], x[2], X::S), x1 = add(x[1], x[3], X::S), y0 = add(y[0], y[2], X::S), y1 = add(y[1], y[3], X::S);
-    const float xs = add(x0, x1, 2 * X::S), ys = add(y0, y1, 2 * X::S);
+    const bool odd = l.g & 2;
+    const float xs = add(odd ? x1 : x0, odd ? x0 : x1, 2 * X::S), ys = add(odd ? y1 : y0, odd ? y0 : y1, 2 * X::S);
     if constexpr (X::S == 8) {
         return make_float2(xs, ys);
     } else {
@@ -213,15 +240,13 @@ struct States {
             if (first + 2 < N) f.z = p[first + 2];
             if (first + 3 < N) f.w = p[first + 3];
         }
-        if (turn & 2) f = make_float4(f.z, f.w, f.x, f.y);
-        if (turn & 1) f = make_float4(f.y, f.x, f.w, f.z);
+        if (turn) f = make_float4(f.z, f.w, f.x, f.y);
         v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
     }
     __device__ __forceinline__ void put_row(float* p, bool there, const float (&v)[4]) const {
         if (!there) return;
         float4 f = make_float4(v[0], v[1], v[2], v[3]);
-        if (turn & 1) f = make_float4(f.y, f.x, f.w, f.z);
-        if (turn & 2) f = make_float4(f.z, f.w, f.x, f.y);
+        if (turn) f = make_float4(f.z, f.w, f.x, f.y);
         if (quads) {
             if (first < N) *reinterpret_cast<float4*>(p + first) = f;
         } else {
@@ -293,30 +318,44 @@ __device__ __forceinline__ void put_map(const Scan& s, int64_t column, int order
     }
 }
 
-// A chunk's inputs on their way: each lane has two neighbouring channels of kItems steps, and kFew values of b and c.
-template <typename X>
+// Who takes which of a chunk's inputs: two neighbouring channels (or states) of every kDown-th step per lane.
+template <int COUNT>  // channels or states
 struct Side {
-    static constexpr int kLanes = X::kColumn / 2, kDown = 32 / kLanes, kItems = R / kDown, kFew = R * X::kStates / 32;
-    int channel, row;
-    __device__ __forceinline__ Side() : channel(threadIdx.x % 32 % kLanes * 2), row(threadIdx.x % 32 / kLanes) {}
+    static constexpr int kLanes = COUNT / 2 < 32 ? COUNT / 2 : 32, kDown = 32 / kLanes, kItems = R / kDown;
+    int at, row;
+    __device__ __forceinline__ Side() : at(threadIdx.x % 32 % kLanes * 2), row(threadIdx.x % 32 / kLanes) {}
 };
-template <typename T, bool WIDE, typename X>
+// An array's rows from the segment's first step on, and the lane's place in them. The rows' addresses are the same for
+// all lanes, and a lane's offset from them fits 32 bits.
+template <typename T>
+struct Place {
+    const T* rows;
+    int64_t step;
+    uint32_t offset;
+    template <int COUNT>
+    __device__ __forceinline__ Place(const Rows& r, int64_t b, int64_t first, int64_t column, const Side<COUNT>& side)
+        : rows(r.p == nullptr ? nullptr : static_cast<const T*>(r.p) + b * r.seq + first * r.step + column), step(r.step),
+          offset(static_cast<uint32_t>(side.row * r.step + side.at)) {}
+    __device__ __forceinline__ const T* at(int64_t t) const { return rows + t * step + offset; }
+};
+template <typename T, bool WIDE, int COUNT>
 struct Wide {
-    Two<T, WIDE> v[Side<X>::kItems];
-    // Rows of the chunk whose first is `p` (the column's first channel).
-    __device__ __forceinline__ void load(const Side<X>& side, const T* p, int64_t step, int rows, int channels) {
+    Two<T, WIDE> v[Side<COUNT>::kItems];
+    // From step t on; of `rows` steps and `there` channels. ALL: there are all.
+    template <bool ALL>
+    __device__ __forceinline__ void load(const Side<COUNT>& side, const Place<T>& p, int64_t t, int rows, int there) {
 #pragma unroll
-        for (int i = 0; i < Side<X>::kItems; ++i) {
-            const int r = side.row + i * Side<X>::kDown;
-            v[i].load(p + r * step + side.channel, r < rows && side.channel < channels, r < rows && side.channel + 1 < channels);
+        for (int i = 0; i < Side<COUNT>::kItems; ++i) {
+            const bool row = ALL || side.row + i * Side<COUNT>::kDown < rows;
+            v[i].template load<ALL>(p.at(t + i * Side<COUNT>::kDown), row && side.at < there, row && side.at + 1 < there);
         }
     }
 };
 
 template <typename X>
-struct ForwardShared {
+struct alignas(16) ForwardShared {
     float dt[R][X::kColumn], x[R][X::kColumn], sum[R][X::kColumn];
-    float4 bc[R][X::kStates];
+    float b[R][X::kStates], c[R][X::kStates];
 };
 
 // MAPS: the first pass, which makes the segment's map.
@@ -326,33 +365,34 @@ scan_kernel(Scan s, const float* h0, T* y, float* last, float* carry, bool quads
     layer_begin();
     __shared__ ForwardShared<X> m;
     const Lane<X> l;
-    const Side<X> side;
-    const int lane = l.lane;
+    const Side<X::kColumn> side;
+    const Side<X::kStates> few;
     const int64_t column = blockIdx.x / s.count;
     const int order = static_cast<int>(blockIdx.x - column * s.count), b = static_cast<int>(column / s.groups);
     if (MAPS && order == s.count - 1) return;  // nobody asks for the last one
     const int d0 = static_cast<int>(column - (int64_t)b * s.groups) * X::kColumn, channels = s.D - d0, worker = b / s.each;
     const int n = s.lengths == nullptr ? s.T : min(max(s.lengths[b], 0), s.T);
     const int first = order * s.steps, end = min(first + s.steps, s.T), inside = min(max(n - first, 0), max(end - first, 0));
-    const T* u = static_cast<const T*>(s.u.p) + b * s.u.seq + first * s.u.step + d0;
-    const T* delta = static_cast<const T*>(s.delta.p) + b * s.delta.seq + first * s.delta.step + d0;
-    const T* z = s.z.p == nullptr ? nullptr : static_cast<const T*>(s.z.p) + b * s.z.seq + first * s.z.step + d0;
-    const T* bs = static_cast<const T*>(s.b.p) + b * s.b.seq + first * s.b.step;
-    const T* cs = static_cast<const T*>(s.c.p) + b * s.c.seq + first * s.c.step;
+    const Place<T> u(s.u, b, first, d0, side), delta(s.delta, b, first, d0, side), z(s.z, b, first, d0, side);
+    const Place<T> bs(s.b, b, first, 0, few), cs(s.c, b, first, 0, few);
+    const bool gated = s.z.p != nullptr, whole = channels >= X::kColumn && s.N == X::kStates;
 
-    Wide<T, WIDE, X> next_u, next_delta, next_z;
-    uint32_t next_b[Side<X>::kFew], next_c[Side<X>::kFew];
+    Wide<T, WIDE, X::kColumn> next_u, next_delta, next_z;
+    Wide<T, WIDE, X::kStates> next_b, next_c;
     const auto fetch = [&](int t) {
         const int rows = inside - t;
-        next_u.load(side, u + t * s.u.step, s.u.step, rows, channels);
-        next_delta.load(side, delta + t * s.delta.step, s.delta.step, rows, channels);
-        if (!MAPS && z != nullptr) next_z.load(side, z + t * s.z.step, s.z.step, rows, channels);
-#pragma unroll
-        for (int i = 0; i < Side<X>::kFew; ++i) {
-            const int r = (i * 32 + lane) / X::kStates, k = (i * 32 + lane) % X::kStates;
-            next_b[i] = load_bits(bs + (t + r) * s.b.step + k, r < rows && k < s.N);
-            if (!MAPS) next_c[i] = load_bits(cs + (t + r) * s.c.step + k, r < rows && k < s.N);
-        }
+        const auto load = [&](auto known) {
+            constexpr bool ALL = decltype(known)::value;
+            next_u.template load<ALL>(side, u, t, rows, channels);
+            next_delta.template load<ALL>(side, delta, t, rows, channels);
+            if (!MAPS && gated) next_z.template load<ALL>(side, z, t, rows, channels);
+            next_b.template load<ALL>(few, bs, t, rows, s.N);
+            if (!MAPS) next_c.template load<ALL>(few, cs, t, rows, s.N);
+        };
+        if (whole && rows >= R)
+            load(std::true_type{});
+        else
+            load(std::false_type{});
     };
     fetch(0);
 
@@ -368,35 +408,34 @@ scan_kernel(Scan s, const float* h0, T* y, float* last, float* carry, bool quads
         if (h0 != nullptr && !MAPS) states.get(h0 + ((int64_t)b * s.D + d0 + d) * s.N, d < channels, d + 1 < channels, h[p]);
     }
     if (!MAPS && s.count > 1) state_before<X>(s, column, order, A, h);
-    const bool live = side.channel < channels, second = side.channel + 1 < channels;
+    const bool live = side.at < channels, second = side.at + 1 < channels;
     const auto weight = [&](const float* p, int64_t stride) {
-        const float* at = p + worker * stride + d0 + side.channel;
+        const float* at = p + worker * stride + d0 + side.at;
         return pair(live ? at[0] : 0.f, second ? at[1] : 0.f);
     };
     const Pair bias = weight(s.bias, s.bias_worker), skip = MAPS ? kZeros : weight(s.skip, s.skip_worker);
     float* carries = carry == nullptr ? nullptr : carry + (((int64_t)b * ((s.T + R - 1) / R) + first / R) * s.D + d0) * s.N;
-    T* out = y + ((int64_t)b * s.T + first) * s.D + d0 + side.channel;
+    const Rows out_rows{y, (int64_t)s.T * s.D, s.D};
+    const Place<T> out(out_rows, b, first, d0, side);
 
     for (int t = 0; t < inside; t += R) {
         const int rows = min(inside - t, R);
-        Pair held_u[Side<X>::kItems], held_z[Side<X>::kItems];
+        const Wide<T, WIDE, X::kColumn> now_u = next_u, now_z = next_z;
 #pragma unroll
-        for (int i = 0; i < Side<X>::kItems; ++i) {
-            const int r = side.row + i * Side<X>::kDown;
-            held_u[i] = next_u.v[i].get();
-            if (!MAPS && z != nullptr) held_z[i] = next_z.v[i].get();
-            const Pair dt = r < rows ? softplus<T>(add2(next_delta.v[i].get(), bias)) : kZeros;
-            *reinterpret_cast<Pair*>(&m.dt[r][side.channel]) = dt;
-            *reinterpret_cast<Pair*>(&m.x[r][side.channel]) = mul2(dt, held_u[i]);
+        for (int i = 0; i < side.kItems; ++i) {
+            const int r = side.row + i * side.kDown;
+            const Pair dt = softplus<T>(add2(next_delta.v[i].get(), bias));
+            *reinterpret_cast<Pair*>(&m.dt[r][side.at]) = dt;
+            *reinterpret_cast<Pair*>(&m.x[r][side.at]) = mul2(dt, now_u.v[i].get());
         }
 #pragma unroll
-        for (int i = 0; i < Side<X>::kFew; ++i) {
-            const int r = (i * 32 + lane) / X::kStates, k = (i * 32 + lane) % X::kStates;
-            const float vb = __uint_as_float(next_b[i]), vc = MAPS ? 0.f : __uint_as_float(next_c[i]);
-            m.bc[r][k] = make_float4(vb, vb, vc, vc);
+        for (int i = 0; i < few.kItems; ++i) {
+            const int r = few.row + i * few.kDown;
+            *reinterpret_cast<Pair*>(&m.b[r][few.at]) = next_b.v[i].get();
+            if (!MAPS) *reinterpret_cast<Pair*>(&m.c[r][few.at]) = next_c.v[i].get();
         }
         __syncwarp();
-        fetch(t + R);
+        if (t + R < inside) fetch(t + R);
         if (!MAPS && carries != nullptr) {
 #pragma unroll
             for (int p = 0; p < X::P; ++p) {
@@ -405,8 +444,7 @@ scan_kernel(Scan s, const float* h0, T* y, float* last, float* carry, bool quads
             }
             carries += (int64_t)s.D * s.N;
         }
-#pragma unroll 2
-        for (int r = 0; r < rows; ++r) {
+        const auto step = [&](int r) {
             Pair dt[X::P], x[X::P], sum[X::P];
 #pragma unroll
             for (int p = 0; p < X::P; ++p) {
@@ -415,32 +453,41 @@ scan_kernel(Scan s, const float* h0, T* y, float* last, float* carry, bool quads
                 sum[p] = kZeros;
                 if (MAPS) sum_dt[p] = add2(sum_dt[p], dt[p]);
             }
+            const float4 b4 = *reinterpret_cast<const float4*>(&m.b[r][4 * l.q]);
+            const float4 c4 = MAPS ? b4 : *reinterpret_cast<const float4*>(&m.c[r][4 * l.q]);
+            const float vb[4] = {b4.x, b4.y, b4.z, b4.w}, vc[4] = {c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const ulonglong2 bc = *reinterpret_cast<const ulonglong2*>(&m.bc[r][4 * l.q + j]);
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int p = 0; p < X::P; ++p) {
-                    h[p][j] = fma2(decay_of(dt[p], A[p][j]), h[p][j], mul2(x[p], bc.x));
-                    if (!MAPS) sum[p] = fma2(h[p][j], bc.y, sum[p]);
+                    h[p][j] = fma2(decay_of(dt[p], A[p][j]), h[p][j], mul2(x[p], twice(vb[j])));
+                    if (!MAPS) sum[p] = fma2(h[p][j], twice(vc[j]), sum[p]);
                 }
-            }
             if constexpr (!MAPS) {
                 const float all = over_states<X>(l, sum);
                 if (X::S < 8 || l.q < 4) m.sum[r][l.summed_channel()] = all;
             }
+        };
+        if (rows == R) {
+#pragma unroll 4
+            for (int r = 0; r < R; ++r) step(r);
+        } else {
+#pragma unroll 1
+            for (int r = 0; r < rows; ++r) step(r);
         }
         __syncwarp();
         if constexpr (!MAPS) {
 #pragma unroll
-            for (int i = 0; i < Side<X>::kItems; ++i) {
-                const int r = side.row + i * Side<X>::kDown;
-                Pair v = fma2(skip, held_u[i], *reinterpret_cast<const Pair*>(&m.sum[r][side.channel]));
-                if (z != nullptr) {
+            for (int i = 0; i < side.kItems; ++i) {
+                const int r = side.row + i * side.kDown;
+                Pair v = fma2(skip, now_u.v[i].get(), *reinterpret_cast<const Pair*>(&m.sum[r][side.at]));
+                if (gated) {
                     Pair a, rest;
-                    gate_of<T>(held_z[i], a, rest);
-                    v = mul2(v, mul2(held_z[i], a));
+                    const Pair vz = now_z.v[i].get();
+                    gate_of<T>(vz, a, rest);
+                    v = mul2(v, mul2(vz, a));
                 }
-                if (live && r < rows) store_two<WIDE>(out + (int64_t)(t + r) * s.D, v, second);
+                if (live && (rows == R || r < rows)) store_two<WIDE>(const_cast<T*>(out.at(t + i * side.kDown)), v, second);
             }
             __syncwarp();
         }
@@ -449,7 +496,7 @@ scan_kernel(Scan s, const float* h0, T* y, float* last, float* carry, bool quads
         put_map<X>(s, column, order, h, sum_dt);
     } else {
         if (live)
-            for (int t = inside + side.row; t < end - first; t += Side<X>::kDown) store_two<WIDE>(out + (int64_t)t * s.D, kZeros, second);
+            for (int t = inside; t + side.row < end - first; t += side.kDown) store_two<WIDE>(const_cast<T*>(out.at(t)), kZeros, second);
         if (n > first ? n <= end : n == 0 && first == 0)
 #pragma unroll
             for (int p = 0; p < X::P; ++p) {
@@ -471,13 +518,13 @@ struct ScanGradients {
 
 template <typename X>
 struct BackwardWarp {
-    ulonglong2 h[R / 2][X::P * 2][32];                                          // states before every second step
-    float dt[R][X::kColumn], x[R][X::kColumn], gy[R][X::kColumn];               // then what the walk sums up: below
-    float sums[R][2 * X::kStates];                                              // dc, db
+    ulonglong2 h[R / 2][X::P * 2][32];                             // states before every second step
+    float dt[R][X::kColumn], x[R][X::kColumn], gy[R][X::kColumn];  // then what the walk sums up
+    float sums[R][2 * X::kStates];                                 // dc, db
 };
 template <typename X>
 struct BackwardShared {
-    float4 bc[R][X::kStates];
+    float b[R][X::kStates], c[R][X::kStates];
     BackwardWarp<X> warps[kBackwardWarps];
 };
 
@@ -494,19 +541,19 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
     const int warps = blockDim.x / 32, warp = threadIdx.x / 32;
     auto& m = shared.warps[warp];
     const Lane<X> l;
-    const Side<X> side;
+    const Side<X::kColumn> side;
+    const Side<X::kStates> few;
     const int lane = l.lane;
     const int64_t per = (int64_t)g.blocks * s.count, b64 = blockIdx.x / per;
     const int b = static_cast<int>(b64), rest = static_cast<int>(blockIdx.x - b64 * per), order = rest % s.count, block = rest / s.count;
     const int group = block * warps + warp, d0 = group * X::kColumn, channels = s.D - d0, worker = b / s.each;
     const int64_t column = b64 * s.groups + group;
-    const bool works = group < s.groups;
+    const bool works = group < s.groups, gated = s.z.p != nullptr;
     const int n = s.lengths == nullptr ? s.T : min(max(s.lengths[b], 0), s.T);
     const int segment = s.count - 1 - order;
     const int first = segment * s.steps, end = min(first + s.steps, s.T), inside = min(max(n - first, 0), max(end - first, 0));
-    const auto rows_of = [&](const Rows& a) { return static_cast<const T*>(a.p) + b * a.seq + first * a.step; };
-    const T *u = rows_of(s.u) + d0, *delta = rows_of(s.delta) + d0, *z = s.z.p == nullptr ? nullptr : rows_of(s.z) + d0, *dy = rows_of(g.dy) + d0;
-    const T *bs = rows_of(s.b), *cs = rows_of(s.c);
+    const Place<T> u(s.u, b, first, d0, side), delta(s.delta, b, first, d0, side), z(s.z, b, first, d0, side), dy(g.dy, b, first, d0, side);
+    const Place<T> bs(s.b, b, first, 0, few), cs(s.c, b, first, 0, few);
 
     const States<X> states(l, s.N, quads, true);
     Pair A[X::P][4], flow[X::P][4], dA[X::P][4];
@@ -514,9 +561,9 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
     for (int p = 0; p < X::P; ++p)
 #pragma unroll
         for (int j = 0; j < 4; ++j) A[p][j] = flow[p][j] = dA[p][j] = kZeros;
-    const bool live = works && side.channel < channels, second = works && side.channel + 1 < channels;
+    const bool live = works && side.at < channels, second = works && side.at + 1 < channels;
     const auto weight = [&](const float* p, int64_t stride) {
-        const float* at = p + worker * stride + d0 + side.channel;
+        const float* at = p + worker * stride + d0 + side.at;
         return pair(live ? at[0] : 0.f, second ? at[1] : 0.f);
     };
     const Pair bias = weight(s.bias, s.bias_worker), skip = weight(s.skip, s.skip_worker);
@@ -534,30 +581,45 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
         for (int r = 0; r < R; ++r)
             for (int k = lane; k < 2 * X::kStates; k += 32) m.sums[r][k] = 0.f;
     }
-    const int64_t out0 = ((int64_t)b * s.T + first) * s.D + d0 + side.channel;
+    const Rows out_rows{nullptr, (int64_t)s.T * s.D, s.D};
+    const auto place = [&](void* p) { return Place<T>(Rows{p, out_rows.seq, out_rows.step}, b, first, d0, side); };
+    const Place<T> du = place(g.du), ddelta = place(g.ddelta), dz = place(g.dz);
+    const auto store = [&](const Place<T>& p, int t, Pair v) { store_two<WIDE>(const_cast<T*>(p.at(t)), v, second); };
     if (live)
-        for (int t = inside + side.row; t < end - first; t += Side<X>::kDown) {
-            store_two<WIDE>(static_cast<T*>(g.du) + out0 + (int64_t)t * s.D, kZeros, second);
-            store_two<WIDE>(static_cast<T*>(g.ddelta) + out0 + (int64_t)t * s.D, kZeros, second);
-            if (z != nullptr) store_two<WIDE>(static_cast<T*>(g.dz) + out0 + (int64_t)t * s.D, kZeros, second);
+        for (int t = inside; t + side.row < end - first; t += side.kDown) {
+            store(du, t, kZeros);
+            store(ddelta, t, kZeros);
+            if (gated) store(dz, t, kZeros);
         }
 
     for (int t = (inside - 1) / R * R; t >= 0 && inside > 0; t -= R) {
         const int rows = min(inside - t, R), pairs = (rows + 1) / 2;
+        Wide<T, WIDE, X::kColumn> in_u, in_delta, in_z, in_dy;
+        Pair h[X::P][4], dts[side.kItems];
         // b and c for the block, the rest for the warp
-        for (int i = threadIdx.x; i < R * X::kStates; i += blockDim.x) {
-            const int r = i / X::kStates, k = i % X::kStates;
-            const bool there = r < rows && k < s.N;
-            const float vb = __uint_as_float(load_bits(bs + (t + r) * s.b.step + k, there)), vc = __uint_as_float(load_bits(cs + (t + r) * s.c.step + k, there));
-            shared.bc[r][k] = make_float4(vb, vb, vc, vc);
+        if (warp == warps - 1) {
+            Wide<T, WIDE, X::kStates> in_b, in_c;
+            in_b.template load<false>(few, bs, t, rows, s.N);
+            in_c.template load<false>(few, cs, t, rows, s.N);
+#pragma unroll
+            for (int i = 0; i < few.kItems; ++i) {
+                const int r = few.row + i * few.kDown;
+                *reinterpret_cast<Pair*>(&shared.b[r][few.at]) = in_b.v[i].get();
+                *reinterpret_cast<Pair*>(&shared.c[r][few.at]) = in_c.v[i].get();
+            }
         }
-        Wide<T, WIDE, X> in_u, in_delta, in_z, in_dy;
-        Pair h[X::P][4], dts[Side<X>::kItems];
         if (works) {
-            in_u.load(side, u + t * s.u.step, s.u.step, rows, channels);
-            in_delta.load(side, delta + t * s.delta.step, s.delta.step, rows, channels);
-            if (z != nullptr) in_z.load(side, z + t * s.z.step, s.z.step, rows, channels);
-            in_dy.load(side, dy + t * g.dy.step, g.dy.step, rows, channels);
+            const auto load = [&](auto known) {
+                constexpr bool ALL = decltype(known)::value;
+                in_delta.template load<ALL>(side, delta, t, rows, channels);
+                in_dy.template load<ALL>(side, dy, t, rows, channels);
+                in_u.template load<ALL>(side, u, t, rows, channels);
+                if (gated) in_z.template load<ALL>(side, z, t, rows, channels);
+            };
+            if (rows == R && channels >= X::kColumn)
+                load(std::true_type{});
+            else
+                load(std::false_type{});
             const float* carries = g.carry + (((int64_t)b * ((s.T + R - 1) / R) + (first + t) / R) * s.D + d0) * s.N;
 #pragma unroll
             for (int p = 0; p < X::P; ++p) {
@@ -565,22 +627,27 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
                 states.get(carries + (int64_t)d * s.N, d < channels, d + 1 < channels, h[p]);
             }
 #pragma unroll
-            for (int i = 0; i < Side<X>::kItems; ++i) {
-                const int r = side.row + i * Side<X>::kDown;
-                dts[i] = r < rows ? softplus<T>(add2(in_delta.v[i].get(), bias)) : kZeros;
+            for (int i = 0; i < side.kItems; ++i) {
+                const int r = side.row + i * side.kDown;
+                dts[i] = softplus<T>(add2(in_delta.v[i].get(), bias));
+                if (rows < R && r >= rows) dts[i] = kZeros;
                 Pair gy = in_dy.v[i].get();
-                if (z != nullptr) {
+                if (gated) {
                     Pair a, away;
                     gate_of<T>(in_z.v[i].get(), a, away);
                     gy = mul2(gy, mul2(in_z.v[i].get(), a));
                 }
-                *reinterpret_cast<Pair*>(&m.dt[r][side.channel]) = dts[i];
-                *reinterpret_cast<Pair*>(&m.x[r][side.channel]) = mul2(dts[i], in_u.v[i].get());
-                *reinterpret_cast<Pair*>(&m.gy[r][side.channel]) = gy;
+                *reinterpret_cast<Pair*>(&m.dt[r][side.at]) = dts[i];
+                *reinterpret_cast<Pair*>(&m.x[r][side.at]) = mul2(dts[i], in_u.v[i].get());
+                *reinterpret_cast<Pair*>(&m.gy[r][side.at]) = gy;
             }
         }
         __syncthreads();
         if (works) {
+            // two of the lane's states, in its order
+            const auto two_of = [&](const float (&v)[R][X::kStates], int r, int half) {
+                return *reinterpret_cast<const float2*>(&v[r][4 * l.q + (2 * half ^ l.turn)]);
+            };
             for (int k = 0; k < pairs; ++k) {
 #pragma unroll
                 for (int p = 0; p < X::P; ++p)
@@ -597,10 +664,13 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
                         x[p] = *reinterpret_cast<const Pair*>(&m.x[r][l.pair_at(p)]);
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const Pair vb = *reinterpret_cast<const Pair*>(&shared.bc[r][4 * l.q + (j ^ l.turn)].x);
+                    for (int half = 0; half < 2; ++half) {
+                        const float2 vb = two_of(shared.b, r, half);
 #pragma unroll
-                        for (int p = 0; p < X::P; ++p) h[p][j] = fma2(decay_of(dt[p], A[p][j]), h[p][j], mul2(x[p], vb));
+                        for (int p = 0; p < X::P; ++p) {
+                            h[p][2 * half] = fma2(decay_of(dt[p], A[p][2 * half]), h[p][2 * half], mul2(x[p], twice(vb.x)));
+                            h[p][2 * half + 1] = fma2(decay_of(dt[p], A[p][2 * half + 1]), h[p][2 * half + 1], mul2(x[p], twice(vb.y)));
+                        }
                     }
                 }
             }
@@ -616,89 +686,93 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
                         gy[e][p] = *reinterpret_cast<const Pair*>(&m.gy[2 * k + e][l.pair_at(p)]);
                         through[e][p] = reach[e][p] = sum[e][p] = kZeros;
                     }
-                ulonglong2 kept[X::P * 2];
 #pragma unroll
-                for (int p = 0; p < X::P * 2; ++p) kept[p] = m.h[k][p][lane];
+                for (int half = 0; half < 2; ++half) {
+                    float2 vb[2], vc[2];
+                    ulonglong2 kept[X::P];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    ulonglong2 bc[2];
-                    Pair to_c[2] = {kZeros, kZeros}, to_b[2] = {kZeros, kZeros};
+                    for (int e = 0; e < 2; ++e) vb[e] = two_of(shared.b, 2 * k + e, half), vc[e] = two_of(shared.c, 2 * k + e, half);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) bc[e] = *reinterpret_cast<const ulonglong2*>(&shared.bc[2 * k + e][4 * l.q + (j ^ l.turn)]);
+                    for (int p = 0; p < X::P; ++p) kept[p] = m.h[k][p * 2 + half][lane];
 #pragma unroll
-                    for (int p = 0; p < X::P; ++p) {
-                        Pair at[3], a[2];
-                        at[0] = j % 2 ? kept[p * 2 + j / 2].y : kept[p * 2 + j / 2].x;
+                    for (int i = 0; i < 2; ++i) {
+                        const int j = 2 * half + i;
+                        Pair to_c[2] = {kZeros, kZeros}, to_b[2] = {kZeros, kZeros}, b2[2], c2[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) b2[e] = twice(i ? vb[e].y : vb[e].x), c2[e] = twice(i ? vc[e].y : vc[e].x);
+#pragma unroll
+                        for (int p = 0; p < X::P; ++p) {
+                            Pair at[3], a[2];
+                            at[0] = i ? kept[p].y : kept[p].x;
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                a[e] = decay_of(dt[e][p], A[p][j]);
+                                at[e + 1] = fma2(a[e], at[e], mul2(x[e][p], b2[e]));
+                            }
+#pragma unroll
+                            for (int e = 1; e >= 0; --e) {
+                                const Pair f = fma2(gy[e][p], c2[e], flow[p][j]);
+                                to_c[e] = fma2(at[e + 1], gy[e][p], to_c[e]);
+                                to_b[e] = fma2(f, x[e][p], to_b[e]);
+                                through[e][p] = fma2(f, b2[e], through[e][p]);
+                                sum[e][p] = fma2(at[e + 1], c2[e], sum[e][p]);
+                                flow[p][j] = mul2(f, a[e]);
+                                const Pair r = mul2(flow[p][j], at[e]);
+                                reach[e][p] = fma2(r, A[p][j], reach[e][p]);
+                                dA[p][j] = fma2(r, dt[e][p], dA[p][j]);
+                            }
+                        }
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            a[e] = decay_of(dt[e][p], A[p][j]);
-                            at[e + 1] = fma2(a[e], at[e], mul2(x[e][p], bc[e].x));
+                            dc[e][j] = floats(to_c[e]).x + floats(to_c[e]).y;
+                            db[e][j] = floats(to_b[e]).x + floats(to_b[e]).y;
                         }
-#pragma unroll
-                        for (int e = 1; e >= 0; --e) {
-                            const Pair f = fma2(gy[e][p], bc[e].y, flow[p][j]);
-                            to_c[e] = fma2(at[e + 1], gy[e][p], to_c[e]);
-                            to_b[e] = fma2(f, x[e][p], to_b[e]);
-                            through[e][p] = fma2(f, bc[e].x, through[e][p]);
-                            sum[e][p] = fma2(at[e + 1], bc[e].y, sum[e][p]);
-                            flow[p][j] = mul2(f, a[e]);
-                            const Pair r = mul2(flow[p][j], at[e]);
-                            reach[e][p] = fma2(r, A[p][j], reach[e][p]);
-                            dA[p][j] = fma2(r, dt[e][p], dA[p][j]);
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        dc[e][j] = floats(to_c[e]).x + floats(to_c[e]).y;
-                        db[e][j] = floats(to_b[e]).x + floats(to_b[e]).y;
                     }
                 }
                 __syncwarp();
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int r = 2 * k + e, d = l.summed_channel();
+                    const int r = 2 * k + e, d = l.summed_channel(), state = l.summed_state();
                     const float all_through = over_states<X>(l, through[e]), all_reach = over_states<X>(l, reach[e]), all = over_states<X>(l, sum[e]);
                     if (X::S < 8 || l.q < 4) m.dt[r][d] = all_through, m.x[r][d] = all_reach, m.gy[r][d] = all;
-                    const float2 few = over_channels<X>(l, dc[e], db[e]);
-                    const int state = 4 * l.q + l.turn;
+                    const float2 both = over_channels<X>(l, dc[e], db[e]);
                     if constexpr (X::S == 8)
-                        m.sums[r][state] = few.x, m.sums[r][X::kStates + state] = few.y;
+                        m.sums[r][state] = both.x, m.sums[r][X::kStates + state] = both.y;
                     else if (X::S == 4 || l.g < 8)
-                        m.sums[r][(l.g & 4 ? X::kStates : 0) + state] = few.x;
+                        m.sums[r][(l.g & 4 ? X::kStates : 0) + state] = both.x;
                 }
             }
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < Side<X>::kItems; ++i) {
-                const int r = side.row + i * Side<X>::kDown;
-                const Pair through = *reinterpret_cast<const Pair*>(&m.dt[r][side.channel]), reach = *reinterpret_cast<const Pair*>(&m.x[r][side.channel]);
-                const Pair sum = *reinterpret_cast<const Pair*>(&m.gy[r][side.channel]), vu = in_u.v[i].get(), vdy = in_dy.v[i].get();
+            for (int i = 0; i < side.kItems; ++i) {
+                const int r = side.row + i * side.kDown, at = t + i * side.kDown;
+                const Pair through = *reinterpret_cast<const Pair*>(&m.dt[r][side.at]), reach = *reinterpret_cast<const Pair*>(&m.x[r][side.at]);
+                const Pair sum = *reinterpret_cast<const Pair*>(&m.gy[r][side.at]), vu = in_u.v[i].get(), vdy = in_dy.v[i].get();
                 Pair gy = vdy, gate, away;
-                const int64_t at = out0 + (int64_t)(t + r) * s.D;
-                const bool here = live && r < rows;
-                if (z != nullptr) {
+                const bool here = live && (rows == R || r < rows);
+                if (gated) {
                     const Pair vz = in_z.v[i].get();
                     gate_of<T>(vz, gate, away);
                     gy = mul2(vdy, mul2(vz, gate));
                     const Pair slope = mul2(gate, fma2(vz, away, kOnes));
-                    if (here) store_two<WIDE>(static_cast<T*>(g.dz) + at, mul2(mul2(vdy, slope), fma2(skip, vu, sum)), second);
+                    if (here) store(dz, at, mul2(mul2(vdy, slope), fma2(skip, vu, sum)));
                 }
                 gate_of<T>(add2(in_delta.v[i].get(), bias), gate, away);
                 const Pair dbase = mul2(fma2(through, vu, mul2(reach, twice(kLn2f))), gate);
                 if (here) {
-                    store_two<WIDE>(static_cast<T*>(g.du) + at, fma2(through, dts[i], mul2(skip, gy)), second);
-                    store_two<WIDE>(static_cast<T*>(g.ddelta) + at, dbase, second);
+                    store(du, at, fma2(through, dts[i], mul2(skip, gy)));
+                    store(ddelta, at, dbase);
                     dskip = fma2(gy, vu, dskip);
                     dbias = add2(dbias, dbase);
                 }
             }
         }
         __syncthreads();
-        float* few = g.few + (((int64_t)block * s.B + b) * s.T + first + t) * (2 * X::kStates);
+        float* to = g.few + (((int64_t)block * s.B + b) * s.T + first + t) * (2 * X::kStates);
         for (int i = threadIdx.x; i < rows * 2 * X::kStates; i += blockDim.x) {
             float v = (&shared.warps[0].sums[0][0])[i];
             for (int w = 1; w < warps; ++w) v += (&shared.warps[w].sums[0][0])[i];
-            few[i] = v;
+            to[i] = v;
         }
     }
     if (!works) return;
@@ -714,12 +788,12 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
         if (g.dh0 != nullptr && segment == 0) states.put(g.dh0 + ((int64_t)b * s.D + d0 + d) * s.N, d < channels, d + 1 < channels, flow[p]);
     }
 #pragma unroll
-    for (int down = Side<X>::kLanes; down < 32; down *= 2) {
+    for (int down = side.kLanes; down < 32; down *= 2) {
         dskip = add2(dskip, shuffle(dskip, down));
         dbias = add2(dbias, shuffle(dbias, down));
     }
     if (side.row == 0 && live) {
-        float* to = small + (int64_t)s.D * s.N + d0 + side.channel;
+        float* to = small + (int64_t)s.D * s.N + d0 + side.at;
         to[0] = floats(dskip).x, to[s.D] = floats(dbias).x;
         if (second) to[1] = floats(dskip).y, to[s.D + 1] = floats(dbias).y;
     }
@@ -732,53 +806,62 @@ scan_backward_maps_kernel(Scan s, Rows grads) {
     layer_begin();
     __shared__ ForwardShared<X> m;
     const Lane<X> l;
-    const Side<X> side;
-    const int lane = l.lane;
+    const Side<X::kColumn> side;
+    const Side<X::kStates> few;
     const int64_t column = blockIdx.x / s.count;
     const int order = static_cast<int>(blockIdx.x - column * s.count), b = static_cast<int>(column / s.groups);
     if (order == s.count - 1) return;
     const int d0 = static_cast<int>(column - (int64_t)b * s.groups) * X::kColumn, channels = s.D - d0, worker = b / s.each;
     const int n = s.lengths == nullptr ? s.T : min(max(s.lengths[b], 0), s.T);
     const int first = (s.count - 1 - order) * s.steps, end = min(first + s.steps, s.T), inside = min(max(n - first, 0), max(end - first, 0));
-    const auto rows_of = [&](const Rows& a) { return static_cast<const T*>(a.p) + b * a.seq + first * a.step; };
-    const T *delta = rows_of(s.delta) + d0, *z = s.z.p == nullptr ? nullptr : rows_of(s.z) + d0, *dy = rows_of(grads) + d0, *cs = rows_of(s.c);
+    const Place<T> delta(s.delta, b, first, d0, side), z(s.z, b, first, d0, side), dy(grads, b, first, d0, side), cs(s.c, b, first, 0, few);
+    const bool gated = s.z.p != nullptr, whole = channels >= X::kColumn && s.N == X::kStates;
+    Wide<T, WIDE, X::kColumn> next_delta, next_z, next_dy;
+    Wide<T, WIDE, X::kStates> next_c;
+    const auto fetch = [&](int t) {
+        const int rows = inside - t;
+        const auto load = [&](auto known) {
+            constexpr bool ALL = decltype(known)::value;
+            next_delta.template load<ALL>(side, delta, t, rows, channels);
+            if (gated) next_z.template load<ALL>(side, z, t, rows, channels);
+            next_dy.template load<ALL>(side, dy, t, rows, channels);
+            next_c.template load<ALL>(few, cs, t, rows, s.N);
+        };
+        if (whole && rows >= R)
+            load(std::true_type{});
+        else
+            load(std::false_type{});
+    };
+    if (inside > 0) fetch((inside - 1) / R * R);
     Pair A[X::P][4], flow[X::P][4], sum_dt[X::P];
-    rates<X>(s, l, b, d0, true, A);
+    rates<X>(s, l, b, d0, false, A);
 #pragma unroll
     for (int p = 0; p < X::P; ++p) {
         sum_dt[p] = kZeros;
 #pragma unroll
         for (int j = 0; j < 4; ++j) flow[p][j] = kZeros;
     }
-    const float* at = s.bias + worker * s.bias_worker + d0 + side.channel;
-    const Pair bias = pair(side.channel < channels ? at[0] : 0.f, side.channel + 1 < channels ? at[1] : 0.f);
+    const float* at = s.bias + worker * s.bias_worker + d0 + side.at;
+    const Pair bias = pair(side.at < channels ? at[0] : 0.f, side.at + 1 < channels ? at[1] : 0.f);
     for (int t = (inside - 1) / R * R; t >= 0 && inside > 0; t -= R) {
         const int rows = min(inside - t, R);
-        Wide<T, WIDE, X> in_delta, in_z, in_dy;
-        in_delta.load(side, delta + t * s.delta.step, s.delta.step, rows, channels);
-        if (z != nullptr) in_z.load(side, z + t * s.z.step, s.z.step, rows, channels);
-        in_dy.load(side, dy + t * grads.step, grads.step, rows, channels);
 #pragma unroll
-        for (int i = 0; i < Side<X>::kFew; ++i) {
-            const int r = (i * 32 + lane) / X::kStates, k = (i * 32 + lane) % X::kStates;
-            const float v = __uint_as_float(load_bits(cs + (t + r) * s.c.step + k, r < rows && k < s.N));
-            m.bc[r][k] = make_float4(v, v, 0.f, 0.f);
-        }
+        for (int i = 0; i < few.kItems; ++i) *reinterpret_cast<Pair*>(&m.c[few.row + i * few.kDown][few.at]) = next_c.v[i].get();
 #pragma unroll
-        for (int i = 0; i < Side<X>::kItems; ++i) {
-            const int r = side.row + i * Side<X>::kDown;
-            Pair gy = in_dy.v[i].get();
-            if (z != nullptr) {
+        for (int i = 0; i < side.kItems; ++i) {
+            const int r = side.row + i * side.kDown;
+            Pair gy = next_dy.v[i].get();
+            if (gated) {
                 Pair a, away;
-                gate_of<T>(in_z.v[i].get(), a, away);
-                gy = mul2(gy, mul2(in_z.v[i].get(), a));
+                gate_of<T>(next_z.v[i].get(), a, away);
+                gy = mul2(gy, mul2(next_z.v[i].get(), a));
             }
-            *reinterpret_cast<Pair*>(&m.dt[r][side.channel]) = r < rows ? softplus<T>(add2(in_delta.v[i].get(), bias)) : kZeros;
-            *reinterpret_cast<Pair*>(&m.x[r][side.channel]) = gy;
+            *reinterpret_cast<Pair*>(&m.dt[r][side.at]) = softplus<T>(add2(next_delta.v[i].get(), bias));
+            *reinterpret_cast<Pair*>(&m.x[r][side.at]) = gy;
         }
         __syncwarp();
-#pragma unroll 2
-        for (int r = rows - 1; r >= 0; --r) {
+        if (t > 0) fetch(t - R);
+        const auto step = [&](int r) {
             Pair dt[X::P], gy[X::P];
 #pragma unroll
             for (int p = 0; p < X::P; ++p) {
@@ -786,15 +869,29 @@ scan_backward_maps_kernel(Scan s, Rows grads) {
                 gy[p] = *reinterpret_cast<const Pair*>(&m.x[r][l.pair_at(p)]);
                 sum_dt[p] = add2(sum_dt[p], dt[p]);
             }
+            const float4 c4 = *reinterpret_cast<const float4*>(&m.c[r][4 * l.q]);
+            const float vc[4] = {c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const Pair c = *reinterpret_cast<const Pair*>(&m.bc[r][4 * l.q + (j ^ l.turn)].x);
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int p = 0; p < X::P; ++p) flow[p][j] = mul2(decay_of(dt[p], A[p][j]), fma2(gy[p], c, flow[p][j]));
-            }
+                for (int p = 0; p < X::P; ++p) flow[p][j] = mul2(decay_of(dt[p], A[p][j]), fma2(gy[p], twice(vc[j]), flow[p][j]));
+        };
+        if (rows == R) {
+#pragma unroll 4
+            for (int r = R - 1; r >= 0; --r) step(r);
+        } else {
+#pragma unroll 1
+            for (int r = rows - 1; r >= 0; --r) step(r);
         }
         __syncwarp();
     }
+    // what reads it has two of the lane's states in another order
+#pragma unroll
+    for (int p = 0; p < X::P; ++p)
+        if (l.turn) {
+            const Pair a = flow[p][0], b = flow[p][1];
+            flow[p][0] = flow[p][2], flow[p][1] = flow[p][3], flow[p][2] = a, flow[p][3] = b;
+        }
     put_map<X>(s, column, order, flow, sum_dt);
 }
 
@@ -916,12 +1013,18 @@ Plan backward_plan(int B, int64_t T, int D, int N) { return plan_of(B, T, D, N, 
 
 bool pairs_at(const Rows& r, int64_t e) { return aligned_to(r.p, 2 * e) && r.seq % 2 == 0 && r.step % 2 == 0; }
 
-cpdp_status check_inputs(const Scan& s, int64_t e, bool some, bool steps) {
+cpdp_status check_step(const Rows& r, int64_t T) {  // a lane's offset from rows is held in 32 bits
+    if (T > 1 && r.step >= int64_t(1) << 28) return layer_error(CPDP_EINVAL, "step strides (%lld) must be below 2^28", (long long)r.step);
+    return CPDP_OK;
+}
+
+cpdp_status check_inputs(const Scan& s, int64_t e, bool some) {
     CPDP_TRY(check_array("u", s.u.p, some, e, s.u.seq, s.u.step));
     CPDP_TRY(check_array("delta", s.delta.p, some, e, s.delta.seq, s.delta.step));
     CPDP_TRY(check_array("z", s.z.p, false, e, s.z.seq, s.z.step));
     CPDP_TRY(check_array("b", s.b.p, some, e, s.b.seq, s.b.step));
     CPDP_TRY(check_array("c", s.c.p, some, e, s.c.seq, s.c.step));
+    for (const Rows* r : {&s.u, &s.delta, &s.z, &s.b, &s.c}) CPDP_TRY(check_step(*r, s.T));
     CPDP_TRY(check_array("a_log", s.a_log, true, 4, s.a_worker));
     CPDP_TRY(check_array("skip", s.skip, true, 4, s.skip_worker));
     CPDP_TRY(check_array("bias", s.bias, true, 4, s.bias_worker));
@@ -961,7 +1064,7 @@ cpdp_status cpdp_selective_scan(const cpdp_scan_inputs* inputs, cpdp_dtype dtype
     Scan s = scan_of(*inputs, W, B, T, D, N);
     const int64_t e = dtype_size(dtype);
     const bool some = B > 0 && T > 0;
-    CPDP_TRY(check_inputs(s, e, some, true));
+    CPDP_TRY(check_inputs(s, e, some));
     CPDP_TRY(check_array("h0", h0, false, 4));
     CPDP_TRY(check_array("y", y, some, e));
     CPDP_TRY(check_array("last", last, B > 0, 4));
@@ -971,7 +1074,8 @@ cpdp_status cpdp_selective_scan(const cpdp_scan_inputs* inputs, cpdp_dtype dtype
     const Plan plan = forward_plan(B, T, D, N);
     s.groups = plan.groups, s.count = plan.count, s.steps = plan.steps, s.maps = static_cast<Pair*>(workspace);
     const bool quads = N % 4 == 0 && aligned_to(h0, 16) && aligned_to(last, 16) && aligned_to(carry, 16);
-    const bool wide = D % 2 == 0 && pairs_at(s.u, e) && pairs_at(s.delta, e) && pairs_at(s.z, e) && aligned_to(y, 2 * e);
+    const bool wide = D % 2 == 0 && pairs_at(s.u, e) && pairs_at(s.delta, e) && pairs_at(s.z, e) && N % 2 == 0 && pairs_at(s.b, e) && pairs_at(s.c, e) &&
+                      aligned_to(y, 2 * e);
     const unsigned blocks = static_cast<unsigned>((int64_t)B * plan.groups * plan.count);
     const auto go = [&](auto* out, auto two) {
         using E = std::remove_pointer_t<decltype(out)>;
@@ -1002,7 +1106,8 @@ cpdp_status cpdp_selective_scan_backward(const void* dy, int64_t dy_seq, int64_t
     const int64_t e = dtype_size(dtype), grad = dtype_size(dweight_dtype);
     const bool some = B > 0 && T > 0;
     CPDP_TRY(check_array("dy", dy, some, e, dy_seq, dy_step));
-    CPDP_TRY(check_inputs(s, e, some, true));
+    CPDP_TRY(check_inputs(s, e, some));
+    CPDP_TRY(check_step({dy, dy_seq, dy_step}, T));
     CPDP_TRY(check_array("carry", carry, some, 4));
     CPDP_TRY(check_array("dlast", dlast, false, 4));
     CPDP_TRY(check_array("du", du, some, e));
@@ -1028,7 +1133,8 @@ cpdp_status cpdp_selective_scan_backward(const void* dy, int64_t dy_seq, int64_t
     g.small = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.maps + plan.few);
     g.blocks = plan.blocks;
     const bool quads = N % 4 == 0 && aligned_to(carry, 16) && aligned_to(dlast, 16) && aligned_to(dh0, 16);
-    const bool wide = D % 2 == 0 && pairs_at(s.u, e) && pairs_at(s.delta, e) && pairs_at(s.z, e) && pairs_at(g.dy, e) && aligned_to(du, 2 * e) &&
+    const bool wide = D % 2 == 0 && pairs_at(s.u, e) && pairs_at(s.delta, e) && pairs_at(s.z, e) && pairs_at(g.dy, e) && N % 2 == 0 &&
+                      pairs_at(s.b, e) && pairs_at(s.c, e) && aligned_to(du, 2 * e) &&
                       aligned_to(ddelta, 2 * e) && aligned_to(dz, 2 * e);
     const auto go = [&](auto* out, auto two) {
         using E = std::remove_pointer_t<decltype(out)>;
@@ -1066,7 +1172,7 @@ cpdp_status cpdp_selective_scan_step(const cpdp_scan_inputs* inputs, cpdp_dtype 
     if (inputs == nullptr) return layer_error(CPDP_EINVAL, "inputs is NULL");
     const Scan s = scan_of(*inputs, W, B, 1, D, N);
     const int64_t e = dtype_size(dtype);
-    CPDP_TRY(check_inputs(s, e, B > 0, false));
+    CPDP_TRY(check_inputs(s, e, B > 0));
     CPDP_TRY(check_array("state", state, B > 0, 4));
     CPDP_TRY(check_array("y", y, B > 0, e));
     if (B == 0) return CPDP_OK;
