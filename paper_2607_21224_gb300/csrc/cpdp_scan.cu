@@ -7,6 +7,18 @@
 #include "cpdp_gates.cuh"
 #include "cpdp_sums.cuh"
 
+#ifndef BB
+#define BB 3
+#endif
+#ifndef FC
+#define FC 4
+#endif
+#ifndef FB
+#define FB 12
+#endif
+#ifndef FU
+#define FU 4
+#endif
 namespace cpdp {
 namespace {
 
@@ -27,7 +39,8 @@ struct Shape {
 };
 constexpr int R = CPDP_CARRY_STEPS;
 constexpr int kBackwardWarps = 4;  // of a block of the backward pass, at most
-constexpr int kForwardBlocks = 12, kBackwardBlocks = 2;  // per SM
+constexpr int kAtOnce = FU;
+constexpr int kForwardBlocks = FB, kBackwardBlocks = BB;  // per SM
 constexpr float kLn2f = kLn2;
 
 struct Rows {
@@ -184,6 +197,7 @@ struct Lane {
     __device__ __forceinline__ Lane()
         : lane(threadIdx.x % 32), q(lane % X::S), g(lane / X::S), turn((g & 1) << 1), channel(g * X::C) {}
     __device__ __forceinline__ int pair_at(int p) const { return X::P == 2 ? channel + 2 * (p ^ (q & 1)) : channel; }
+    __device__ __forceinline__ bool sums_up() const { return q < 2 * X::P; }  // the others of the group have the same sums
     __device__ __forceinline__ int summed_state() const { return 4 * q + turn + (g >> 1 & 1); }
     // Of sums of pairs over states, the channel's whose sum the lane gets.
     __device__ __forceinline__ int summed_channel() const {
@@ -202,7 +216,10 @@ __device__ __forceinline__ float over_states(const Lane<X>& l, const Pair (&v)[X
     } else {
         const float2 r = floats(v[0]);
         const bool high = l.q & 1;
-        return (high ? r.y : r.x) + __shfl_xor_sync(~0u, high ? r.x : r.y, 1);
+        float s = (high ? r.y : r.x) + __shfl_xor_sync(~0u, high ? r.x : r.y, 1);
+#pragma unroll
+        for (int k = 2; k < X::S; k *= 2) s += __shfl_xor_sync(~0u, s, k);
+        return s;
     }
 }
 // Sums over the groups of lanes: of x and y for the lane's 4 states (in its order). The lane gets that of state
@@ -444,36 +461,47 @@ scan_kernel(Scan s, const float* h0, T* y, float* last, float* carry, bool quads
             }
             carries += (int64_t)s.D * s.N;
         }
-        const auto step = [&](int r) {
-            Pair dt[X::P], x[X::P], sum[X::P];
+        // `many` steps at a time, then their sums: what goes to shared memory in between would hold up the next step's loads
+        const auto walk = [&](int r0, auto many) {
+            constexpr int COUNT = decltype(many)::value;
+            Pair sum[COUNT][X::P];
 #pragma unroll
-            for (int p = 0; p < X::P; ++p) {
-                dt[p] = *reinterpret_cast<const Pair*>(&m.dt[r][l.pair_at(p)]);
-                x[p] = *reinterpret_cast<const Pair*>(&m.x[r][l.pair_at(p)]);
-                sum[p] = kZeros;
-                if (MAPS) sum_dt[p] = add2(sum_dt[p], dt[p]);
-            }
-            const float4 b4 = *reinterpret_cast<const float4*>(&m.b[r][4 * l.q]);
-            const float4 c4 = MAPS ? b4 : *reinterpret_cast<const float4*>(&m.c[r][4 * l.q]);
-            const float vb[4] = {b4.x, b4.y, b4.z, b4.w}, vc[4] = {c4.x, c4.y, c4.z, c4.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int e = 0; e < COUNT; ++e) {
+                const int r = r0 + e;
+                Pair dt[X::P], x[X::P];
 #pragma unroll
                 for (int p = 0; p < X::P; ++p) {
-                    h[p][j] = fma2(decay_of(dt[p], A[p][j]), h[p][j], mul2(x[p], twice(vb[j])));
-                    if (!MAPS) sum[p] = fma2(h[p][j], twice(vc[j]), sum[p]);
+                    dt[p] = *reinterpret_cast<const Pair*>(&m.dt[r][l.pair_at(p)]);
+                    x[p] = *reinterpret_cast<const Pair*>(&m.x[r][l.pair_at(p)]);
+                    sum[e][p] = kZeros;
+                    if (MAPS) sum_dt[p] = add2(sum_dt[p], dt[p]);
                 }
+                const float4 b4 = *reinterpret_cast<const float4*>(&m.b[r][4 * l.q]);
+                const float4 c4 = MAPS ? b4 : *reinterpret_cast<const float4*>(&m.c[r][4 * l.q]);
+                const float vb[4] = {b4.x, b4.y, b4.z, b4.w}, vc[4] = {c4.x, c4.y, c4.z, c4.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int p = 0; p < X::P; ++p) {
+                        h[p][j] = fma2(decay_of(dt[p], A[p][j]), h[p][j], mul2(x[p], twice(vb[j])));
+                        if (!MAPS) sum[e][p] = fma2(h[p][j], twice(vc[j]), sum[e][p]);
+                    }
+            }
             if constexpr (!MAPS) {
-                const float all = over_states<X>(l, sum);
-                if (X::S < 8 || l.q < 4) m.sum[r][l.summed_channel()] = all;
+                float all[COUNT];
+#pragma unroll
+                for (int e = 0; e < COUNT; ++e) all[e] = over_states<X>(l, sum[e]);
+                if (l.sums_up())
+#pragma unroll
+                    for (int e = 0; e < COUNT; ++e) m.sum[r0 + e][l.summed_channel()] = all[e];
             }
         };
         if (rows == R) {
-#pragma unroll 4
-            for (int r = 0; r < R; ++r) step(r);
+#pragma unroll 1
+            for (int r = 0; r < R; r += kAtOnce) walk(r, std::integral_constant<int, kAtOnce>{});
         } else {
 #pragma unroll 1
-            for (int r = 0; r < rows; ++r) step(r);
+            for (int r = 0; r < rows; ++r) walk(r, std::integral_constant<int, 1>{});
         }
         __syncwarp();
         if constexpr (!MAPS) {
@@ -734,7 +762,7 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
                 for (int e = 0; e < 2; ++e) {
                     const int r = 2 * k + e, d = l.summed_channel(), state = l.summed_state();
                     const float all_through = over_states<X>(l, through[e]), all_reach = over_states<X>(l, reach[e]), all = over_states<X>(l, sum[e]);
-                    if (X::S < 8 || l.q < 4) m.dt[r][d] = all_through, m.x[r][d] = all_reach, m.gy[r][d] = all;
+                    if (l.sums_up()) m.dt[r][d] = all_through, m.x[r][d] = all_reach, m.gy[r][d] = all;
                     const float2 both = over_channels<X>(l, dc[e], db[e]);
                     if constexpr (X::S == 8)
                         m.sums[r][state] = both.x, m.sums[r][X::kStates + state] = both.y;
@@ -969,15 +997,16 @@ cpdp_status check_scan(int W, int B, int64_t T, int D, int N, cpdp_dtype dtype) 
     if (B > 0) {
         if (T > kLayerMaxRows / B || (T > 0 && D > kLayerMaxElements / 64 / (B * T)))
             return layer_error(CPDP_EINVAL, "B=%d, T=%lld, D=%d: B * T is at most 2^31 - 1 and all elements at most 2^34", B, (long long)T, D);
-        if (ceil_div(D, 16) > (kLayerMaxRows >> 6) / B) return layer_error(CPDP_EINVAL, "B=%d, D=%d: more blocks than a launch takes", B, D);
+        if (ceil_div(D, 8) > (kLayerMaxRows >> 6) / B) return layer_error(CPDP_EINVAL, "B=%d, D=%d: more blocks than a launch takes", B, D);
     }
     if (!known_dtype(dtype)) return layer_error(CPDP_EINVAL, "unknown dtype %d", (int)dtype);
     return CPDP_OK;
 }
 
 template <typename F>
-auto with_shape(int N, F&& f) {
-    return N <= 8 ? f(Shape<2, 2>{}) : N <= 16 ? f(Shape<4, 4>{}) : f(Shape<8, 4>{});
+auto with_shape(bool backward, int N, F&& f) {
+    if (backward) return N <= 8 ? f(Shape<2, 2>{}) : N <= 16 ? f(Shape<4, 2>{}) : f(Shape<8, 2>{});
+    return N <= 8 ? f(Shape<2, 2>{}) : N <= 16 ? f(Shape<4, FC>{}) : f(Shape<8, FC>{});
 }
 
 struct Plan {
@@ -989,14 +1018,13 @@ struct Plan {
 // `warps`: as many as run at once on the GPU.
 Plan plan_of(int B, int64_t T, int D, int N, int64_t warps, bool backward) {
     Plan p{};
-    with_shape(N, [&](auto x) { return p.column = decltype(x)::kColumn, p.states = decltype(x)::kStates, 0; });
+    const int pairs = with_shape(backward, N, [&](auto x) { return p.column = decltype(x)::kColumn, p.states = decltype(x)::kStates, decltype(x)::P; });
     p.groups = static_cast<int>(ceil_div(D, p.column));
     const int64_t columns = (int64_t)B * p.groups;
     int64_t count = columns * 3 <= warps ? warps / std::max<int64_t>(columns, 1) : 1;
     count = std::max<int64_t>(std::min(count, T / (4 * R)), 1);
     p.steps = static_cast<int>(ceil_div(ceil_div(std::max<int64_t>(T, 1), count), R) * R);
     p.count = static_cast<int>(std::max<int64_t>(ceil_div(T, p.steps), 1));
-    const int pairs = N <= 8 ? 1 : 2;
     p.maps = p.count > 1 ? columns * p.count * pairs * 5 * 32 * 8 : 0;
     if (backward) {
         p.warps = 1;
@@ -1080,7 +1108,7 @@ cpdp_status cpdp_selective_scan(const cpdp_scan_inputs* inputs, cpdp_dtype dtype
     const auto go = [&](auto* out, auto two) {
         using E = std::remove_pointer_t<decltype(out)>;
         constexpr bool WIDE = decltype(two)::value;
-        return with_shape(N, [&](auto shape) {
+        return with_shape(false, N, [&](auto shape) {
             using X = decltype(shape);
             if (plan.count > 1) {
                 const cudaError_t first = launch_layer(scan_kernel<E, WIDE, true, X>, blocks, 32, 0, stream, s, h0, out, last, carry, quads);
@@ -1139,7 +1167,7 @@ cpdp_status cpdp_selective_scan_backward(const void* dy, int64_t dy_seq, int64_t
     const auto go = [&](auto* out, auto two) {
         using E = std::remove_pointer_t<decltype(out)>;
         constexpr bool WIDE = decltype(two)::value;
-        return with_shape(N, [&](auto shape) {
+        return with_shape(true, N, [&](auto shape) {
             using X = decltype(shape);
             if (plan.count > 1) {
                 const cudaError_t first = launch_layer(scan_backward_maps_kernel<E, WIDE, X>, static_cast<unsigned>((int64_t)B * plan.groups * plan.count),
@@ -1178,7 +1206,7 @@ cpdp_status cpdp_selective_scan_step(const cpdp_scan_inputs* inputs, cpdp_dtype 
     if (B == 0) return CPDP_OK;
     const auto go = [&](auto* out) {
         using E = std::remove_pointer_t<decltype(out)>;
-        return with_shape(N, [&](auto shape) {
+        return with_shape(false, N, [&](auto shape) {
             constexpr int S = decltype(shape)::S;
             return launch_layer(scan_step_kernel<E, S>, static_cast<unsigned>(ceil_div((int64_t)B * D * S, 128)), 128, 0, stream, s, state, out);
         });
