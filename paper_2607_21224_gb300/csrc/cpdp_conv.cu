@@ -12,9 +12,10 @@ namespace {
 // A sequence's inputs with the K - 1 before it: e_0 .. e_(T+K-2), e_(K-1) = x_0,
 // and v_t = bias + sum_k weight_k e_(t+k). A thread walks a stretch of steps of V
 // neighbouring channels (16 or 8 bytes; 1 where rows are not whole pieces), with
-// the last K - 1 inputs in registers, two channels to a pair; while kAhead rows
-// are worked on, the next are on their way. Both passes are bound by memory.
-constexpr int kThreads = 128, kAhead = 4;
+// the last K - 1 inputs in registers, two channels to a pair, and kAhead rows on
+// their way. Both passes are bound by memory.
+constexpr int kThreads = 128, kAhead = 8;
+constexpr int kForwardBlocks = 4, kBackwardBlocks = 3;  // per SM
 constexpr int kMostTaps = CPDP_CONV_MAX_TAPS;
 
 // V neighbouring elements as they lie in memory, loaded where they are there; else 0. Predicates, not branches: see load_once.
@@ -115,16 +116,12 @@ struct Inputs {
             f.load(x + (int64_t)(e - (K - 1)) * step, e - (K - 1) < n);
         f.get(v);
     }
-    // kAhead rows of x from step t on
-    __device__ __forceinline__ void rows(Few<T, V> (&f)[kAhead], int t) const {
-        const T* p = x + t * step;
-#pragma unroll
-        for (int r = 0; r < kAhead; ++r) f[r].load(p + r * step, t + r < n);
-    }
+    // x of step t
+    __device__ __forceinline__ void row(Few<T, V>& f, int t) const { f.load(x + t * step, t < n); }
 };
 
 template <typename T, int V, int K>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kForwardBlocks)
 conv_kernel(Conv p, T* y, T* last) {
     layer_begin();
     constexpr int P = (V + 1) / 2;
@@ -135,21 +132,19 @@ conv_kernel(Conv p, T* y, T* last) {
     const Inputs<T, V, K> in(p, b, d);
     const int first = stretch * p.steps, end = min(first + p.steps, p.T), inside = min(end, in.n);
     Few<T, V> next[kAhead];
-    in.rows(next, first);
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) in.row(next[r], first + r);
     Pair e[K][P];
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) in.get(e[k], first + k);
     const Taps<T, V, K> taps(p, static_cast<int>(b / p.each), d);
     T* to = y + (b * p.T + first) * p.D + d;
     for (int t = first; t < inside; t += kAhead) {
-        Few<T, V> now[kAhead];
-#pragma unroll
-        for (int r = 0; r < kAhead; ++r) now[r] = next[r];
-        if (t + kAhead < inside) in.rows(next, t + kAhead);
 #pragma unroll
         for (int r = 0; r < kAhead; ++r) {
             Pair out[P];
-            now[r].get(e[K - 1]);
+            next[r].get(e[K - 1]);
+            in.row(next[r], t + r + kAhead < inside ? t + r + kAhead : in.n);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 const Pair v = taps.sum(e, i);
@@ -189,7 +184,7 @@ struct ConvGradients {
 // stretches of a worker's sequences in turn; the block adds its teams' sums of
 // dweight and dbias up.
 template <typename T, int V, int K>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBackwardBlocks)
 conv_backward_kernel(Conv p, ConvGradients g) {
     layer_begin();
     __shared__ float shared[kThreads][V * (K + 1) + 1];
@@ -209,28 +204,24 @@ conv_backward_kernel(Conv p, ConvGradients g) {
             const int first = item % p.stretches * p.steps, end = min(first + p.steps, p.T + K - 1);
             const int from = max(first - (K - 1), 0), inside = min(end, in.n);
             Few<T, V> next[kAhead], next_dy[kAhead];
-            const auto fetch = [&](int t) {
-                in.rows(next, t);
-                const T* q = dy + t * g.dy_step;
-#pragma unroll
-                for (int r = 0; r < kAhead; ++r) next_dy[r].load(q + r * g.dy_step, t + r < inside);
+            const auto fetch = [&](int r, int t) {
+                in.row(next[r], t < end ? t : in.n);
+                next_dy[r].load(dy + t * g.dy_step, t < inside);
             };
-            fetch(from);
+#pragma unroll
+            for (int r = 0; r < kAhead; ++r) fetch(r, from + r);
             Pair e[K][P] = {}, dv[K][P] = {};  // dv[k]: of step t - k
             if (in.n > 0)
 #pragma unroll
                 for (int k = 0; k < K - 1; ++k) in.get(e[k], from + k);
             for (int t0 = from; t0 < end; t0 += kAhead) {
-                Few<T, V> now[kAhead], now_dy[kAhead];
-#pragma unroll
-                for (int r = 0; r < kAhead; ++r) now[r] = next[r], now_dy[r] = next_dy[r];
-                if (t0 + kAhead < end) fetch(t0 + kAhead);
 #pragma unroll
                 for (int r = 0; r < kAhead; ++r) {
                     const int t = t0 + r;
                     Pair out[P], dy_r[P];
-                    now[r].get(e[K - 1]);
-                    now_dy[r].get(dy_r);
+                    next[r].get(e[K - 1]);
+                    next_dy[r].get(dy_r);
+                    fetch(r, t + kAhead);
 #pragma unroll
                     for (int i = 0; i < P; ++i) {
                         const Pair v = taps.sum(e, i);
@@ -324,9 +315,10 @@ cpdp_status check_conv(int W, int B, int64_t T, int D, int K, cpdp_dtype dtype) 
     return CPDP_OK;
 }
 
-// Steps of a stretch: enough threads for `threads` in all, within [least, 128].
-int stretch_of(int64_t rows, int64_t columns, int64_t least, int64_t threads) {
-    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(ceil_div(rows * columns, threads), least), 128) / kAhead * kAhead);
+// Steps of a stretch of the forward pass: as many stretches as run at once.
+int stretch_of(int64_t T, int64_t rows) {
+    const int64_t count = std::max<int64_t>((int64_t)kSMs * kForwardBlocks * kThreads / std::max<int64_t>(rows, 1), 1);
+    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(ceil_div(T, count), 8), 128));
 }
 
 // Whether rows of an array are whole pieces of `bytes`.
@@ -337,16 +329,22 @@ bool in_pieces(const void* p, int64_t size, int64_t a, int64_t b, int64_t bytes)
 struct Spread {
     int steps, stretches, lanes, groups, parts;
 };
+// Of the backward pass: as many blocks as run at once, and stretches that make the teams' turns come out even; a stretch
+// costs some steps of its own.
 Spread spread_of(int W, int B, int64_t T, int D, int K, int V) {
     Spread s{};
-    const int64_t columns = ceil_div(D, V), rows = T + K - 1;
-    s.steps = stretch_of(B * rows, columns, 16, kSMs * 512);
-    s.stretches = static_cast<int>(ceil_div(rows, s.steps));
+    const int64_t columns = ceil_div(D, V), rows = T + K - 1, each = B / W;
     s.lanes = 1;
     while (s.lanes < 32 && s.lanes < columns) s.lanes *= 2;
     s.groups = static_cast<int>(ceil_div(columns, s.lanes));
-    const int64_t items = (int64_t)(B / W) * s.stretches, most = std::max<int64_t>(kSMs * 4 / ((int64_t)s.groups * W), 1);
-    s.parts = static_cast<int>(std::max<int64_t>(std::min(ceil_div(items, kThreads / s.lanes), most), 1));
+    const int64_t most = std::max<int64_t>(kSMs * kBackwardBlocks / ((int64_t)s.groups * W), 1), teams = most * (kThreads / s.lanes);
+    int64_t least = -1;
+    for (int64_t turns = 1; turns <= 16; ++turns) {
+        const int64_t steps = std::min<int64_t>(std::max<int64_t>(ceil_div(rows, std::max<int64_t>(turns * teams / each, 1)), 8), 256);
+        const int64_t stretches = ceil_div(rows, steps), cost = ceil_div(each * stretches, teams) * (steps + K + 5);
+        if (least < 0 || cost < least) least = cost, s.steps = static_cast<int>(steps), s.stretches = static_cast<int>(stretches);
+    }
+    s.parts = static_cast<int>(std::max<int64_t>(std::min(ceil_div(each * s.stretches, kThreads / s.lanes), most), 1));
     return s;
 }
 
@@ -393,7 +391,7 @@ cpdp_status cpdp_causal_conv(const void* x, int64_t x_seq, int64_t x_step, const
         using E = std::remove_pointer_t<decltype(out)>;
         constexpr int V = decltype(many)::value;
         const int64_t columns = D / V;
-        p.steps = stretch_of((int64_t)B * T, columns, 8, kSMs * 768);
+        p.steps = stretch_of(T, (int64_t)B * columns);
         p.stretches = static_cast<int>(std::max<int64_t>(ceil_div(T, p.steps), 1));
         const int64_t blocks = ceil_div((int64_t)B * p.stretches * columns, kThreads);
         if (blocks > kLayerMaxRows) return cudaErrorInvalidConfiguration;

@@ -11,7 +11,7 @@ namespace {
 //   logits   a: tokens, b: words, k: features; an epilogue leaves each row's
 //            maximum and sum of exponentials over 128 words
 //   again    the same in the backward pass; the epilogue leaves
-//            d = r (exp(l - lse) - onehot), for a piece of the vocabulary
+//            d = dloss (exp(l - lse) - onehot), for a piece of the vocabulary
 //   dx       a: features, b: tokens, k: words of the piece
 //   dweight  a: features, b: words of the piece, k: tokens
 // One block per SM walks tiles of 128 (a) x 256 (b). k passes in steps of 64
@@ -278,32 +278,40 @@ struct RowSums {
             for (int j = 0; j < kHalf; ++j) l = j == target ? v[j] : l;
             if (mine) chosen[row] = l;
         }
-        if (real) parts[(int64_t)(b / kHalf) * rows + row] = make_float2(isinf(most) ? 0.f : most, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+        if (real) parts[(int64_t)(b / kHalf) * rows + row] = make_float2(most == INFINITY ? 0.f : most, (sum[0] + sum[1]) + (sum[2] + sum[3]));
     }
 };
 
-// lse and loss of each token from its parts: 32 tokens per block, every eighth part to a warp.
+// lse and loss of each token from its parts: ROWS tokens per block, whose other threads share the parts.
+template <int ROWS>
 __global__ void __launch_bounds__(256)
 finish_rows_kernel(const float2* parts, const float* chosen, const int64_t* targets, int64_t rows, int blocks, int V, float* loss, float* lse) {
     layer_begin();
-    __shared__ float2 shared[8][32];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+    constexpr int kShares = 256 / ROWS;
+    __shared__ float2 shared[kShares][ROWS];
+    const int in = threadIdx.x % ROWS, share = threadIdx.x / ROWS;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + in;
     const bool real = row < rows;
     float most = -INFINITY, sum = 0.f;
     const auto add = [&](float2 p) {
-        const float next = fmaxf(most, p.x);  // finite: parts are, but for the first
+        if (p.y == 0.f) return;  // nothing there: words beyond the last, or logits of -infinity
+        const float next = fmaxf(most, p.x);
         sum = sum * power((most - next) * kLog2e) + p.y * power((p.x - next) * kLog2e);
         most = next;
     };
     if (real)
 #pragma unroll 8
-        for (int k = warp; k < blocks; k += 8) add(parts[(int64_t)k * rows + row]);
-    shared[warp][lane] = make_float2(most, sum);
-    __syncthreads();
-    if (warp == 0 && real) {
-        for (int k = 1; k < 8; ++k)
-            if (k < blocks) add(shared[k][lane]);
+        for (int k = share; k < blocks; k += kShares) add(parts[(int64_t)k * rows + row]);
+    shared[share][in] = make_float2(most, sum);
+#pragma unroll
+    for (int half = kShares / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (share < half) {
+            add(shared[share + half][in]);
+            shared[share][in] = make_float2(most, sum);
+        }
+    }
+    if (share == 0 && real) {
         const float l = most + logf(sum);
         const int64_t t = targets[row];
         lse[row] = l;
@@ -311,12 +319,12 @@ finish_rows_kernel(const float2* parts, const float* chosen, const int64_t* targ
     }
 }
 
-// The gradient of a token's logits, without the factor that its worker's tokens
-// share: d = r (exp(l - lse) - onehot), rounded to bfloat16, or in three planes.
+// The gradient of a token's logits, d = dloss (exp(l - lse) - onehot), rounded to
+// bfloat16 (the type of the products' operands), or in three planes.
 template <int PLANES>
 struct LogitGradients {
     const int64_t* targets;
-    const float *lse, *r;
+    const float *lse, *dloss;
     __nv_bfloat16* d;  // [plane][W][M][pitch]
     int64_t M, plane, pitch;
     int V, first;      // the piece's first word
@@ -324,7 +332,7 @@ struct LogitGradients {
         if (a >= M) return;
         const int64_t row = w * M + a, target = targets[row];
         const bool ignored = target < 0;
-        const float l = target >= V ? __uint_as_float(0x7fc00000u) : lse[row], scale = ignored ? 0.f : r[row];
+        const float l = target >= V ? __uint_as_float(0x7fc00000u) : lse[row], scale = ignored ? 0.f : dloss[row];
         const int64_t hot = target - first - b;
         __nv_bfloat16* to = d + row * pitch + b;
 #pragma unroll
@@ -347,13 +355,12 @@ struct LogitGradients {
     }
 };
 
-// C written out, [b][a] with a contiguous: times the worker's factor, 0 in the rows of ignored tokens, or as a part
-// (float32, factor and targets NULL) that may be added to what is there.
+// C written out, [b][a] with a contiguous; 0 in the rows of ignored tokens (targets not NULL). Or as a part of a sum
+// (float32, of a split), which may be added to what is there.
 template <typename G>
 struct WriteOut {
     G* out;
     int64_t worker, split, row;
-    const float* factor;
     const int64_t* targets;
     int a_extent, b_extent, add;
     __device__ __forceinline__ void run(const float (&v)[kHalf], int w, int s, int a, int b) const {
@@ -365,37 +372,31 @@ struct WriteOut {
                 const int at = b + j * 32 + static_cast<int>(threadIdx.x % 32);
                 ignored[j] = __ballot_sync(~0u, at < b_extent && targets[(int64_t)w * b_extent + at] < 0);
             }
-        const float f = factor != nullptr ? factor[w] : 1.f;
-        if (a >= a_extent) return;
+        const int there = a < a_extent ? b_extent - b : 0;
         G* to = out + w * worker + s * split + b * row + a;
+        if (sizeof(G) == 4 && add) {  // one addition to each element per launch: the order is that of the launches
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) {
-            if (b + j < b_extent) {
-                const float x = ignored[j / 32] >> j % 32 & 1 ? 0.f : v[j] * f;
-                if constexpr (sizeof(G) == 4) {
-                    if (add) {  // one addition to each element per launch: the order is that of the launches
-                        asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to + j * row), "f"(x) : "memory");
-                        continue;
-                    }
-                }
-                to[j * row] = from_float<G>(x);
-            }
+            for (int j = 0; j < kHalf; ++j, to += row)
+                if (j < there) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to), "f"(v[j]) : "memory");
+        } else {
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j, to += row)
+                if (j < there) *to = from_float<G>(ignored[j / 32] >> j % 32 & 1 ? 0.f : v[j]);
         }
     }
 };
 
-// The sum of the splits' parts [split][W][rows][D], in their order, times the worker's factor; 0 in ignored tokens' rows.
+// The sum of the splits' parts [split][W][rows][D], in their order; 0 in ignored tokens' rows.
 // A warp per row; V neighbouring elements per lane.
 template <typename G, int V>
 __global__ void __launch_bounds__(256)
-sum_parts_kernel(const float* parts, int splits, int64_t rows_each, int64_t rows, int D, const float* factor, const int64_t* targets, G* out,
-                 int64_t worker) {
+sum_parts_kernel(const float* parts, int splits, int64_t rows_each, int64_t rows, int D, const int64_t* targets, G* out, int64_t worker) {
     layer_begin();
     const int lane = threadIdx.x % 32;
     const int64_t all = rows * D;
     for (int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; r < rows; r += (int64_t)gridDim.x * 8) {
         const int64_t w = r / rows_each;
-        const float f = targets != nullptr && targets[r] < 0 ? 0.f : factor[w];
+        const bool ignored = targets != nullptr && targets[r] < 0;
         const float* p = parts + r * D;
         G* to = out + w * worker + (r - w * rows_each) * D;
 #pragma unroll 4
@@ -411,7 +412,7 @@ sum_parts_kernel(const float* parts, int splits, int64_t rows_each, int64_t rows
                 for (int e = 0; e < V; ++e) s[e] += v.get(e);
             }
 #pragma unroll
-            for (int e = 0; e < V; ++e) s[e] = f == 0.f ? 0.f : s[e] * f;
+            for (int e = 0; e < V; ++e) s[e] = ignored ? 0.f : s[e];
             store_piece<V>(to + k, s);
         }
     }
@@ -454,31 +455,6 @@ pack_kernel(const T* x, int64_t worker, int64_t stride, int64_t rows_each, int64
     }
 }
 
-// r = dloss / factor with factor the largest finite |dloss| of the worker's
-// tokens: where all have the same weight, r is 1 and d's rounding is that of
-// probabilities. One block per worker.
-__global__ void __launch_bounds__(1024)
-factor_kernel(const float* dloss, const int64_t* targets, int64_t M, float* r, float* factor) {
-    layer_begin();
-    __shared__ float parts[32];
-    const int64_t first = blockIdx.x * M;
-    float most = 0.f;
-#pragma unroll 4
-    for (int64_t m = threadIdx.x; m < M; m += 1024) {
-        const float g = fabsf(dloss[first + m]);
-        if (targets[first + m] >= 0 && isfinite(g)) most = fmaxf(most, g);
-    }
-    for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
-    if (threadIdx.x % 32 == 0) parts[threadIdx.x / 32] = most;
-    __syncthreads();
-    most = parts[threadIdx.x % 32];
-    for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
-    const float f = most > 0.f ? most : 1.f;
-    if (threadIdx.x == 0) factor[blockIdx.x] = f;
-#pragma unroll 4
-    for (int64_t m = threadIdx.x; m < M; m += 1024) r[first + m] = dloss[first + m] / f;
-}
-
 // -- the host's side -------------------------------------------------------------------------------------------------
 
 constexpr int64_t kPieceBytes = int64_t(1) << 30;  // of d at a time
@@ -511,7 +487,7 @@ struct Plan {
     int64_t x_copy, weight_copy;       // bytes of the copies that the tensor copies read; 0: in place
     int64_t parts, chosen;             // forward
     int words, pieces;                 // of a piece, and how many
-    int64_t pitch, d, rows;            // of d, its bytes; bytes of r and factor
+    int64_t pitch, d;                  // of d, and its bytes
     Splits dx, dweight;
     int64_t dx_parts, dweight_parts;   // bytes; 0: written in place
     int64_t forward, backward;         // bytes in all
@@ -541,13 +517,12 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
     p.pieces = static_cast<int>(ceil_div(V, p.words));
     p.pitch = pitch_of(std::min(p.words, V));
     p.d = padded(p.planes * rows * p.pitch * 2);
-    p.rows = padded(rows * 4) + padded(W * 4);
     const int64_t tiles_d = ceil_div(D, kTileA);
     p.dx = splits_of(W * tiles_d * ceil_div(M, kTileB), ceil_div(std::min(p.words, V), kStep) * p.segments, rows * D);
     p.dweight = splits_of(W * tiles_d * ceil_div(std::min(p.words, V), kTileB), ceil_div(M, kStep) * p.segments, (int64_t)W * std::min(p.words, V) * D);
     p.dx_parts = p.dx.count > 1 || p.pieces > 1 ? padded(p.dx.count * rows * D * 4) : 0;
     p.dweight_parts = p.dweight.count > 1 ? padded((int64_t)p.dweight.count * W * std::min(p.words, V) * D * 4) : 0;
-    p.backward = packed + p.weight_copy + p.rows + p.d + p.dx_parts + p.dweight_parts;
+    p.backward = packed + p.weight_copy + p.d + p.dx_parts + p.dweight_parts;
     return p;
 }
 
@@ -679,18 +654,20 @@ cpdp_status cpdp_linear_cross_entropy(const void* x, int64_t x_worker, int64_t x
     CPDP_TRY(encode(&a, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
     CPDP_TRY(encode(&b, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileB));
     CPDP_TRY((multiply_all<false, false>(a, b, product(W, M, V, D, plan.segments), RowSums{targets, parts, chosen, M, rows, V}, stream, what)));
-    return layer_launched(launch_layer(finish_rows_kernel, static_cast<unsigned>(ceil_div(rows, 32)), 256, 0, stream,
-                                       static_cast<const float2*>(parts), static_cast<const float*>(chosen), targets, rows,
-                                       static_cast<int>(ceil_div(V, kTileB) * 2), V, loss, lse),
-                          what);
+    const auto finish = [&](auto kernel, int each) {
+        return launch_layer(kernel, static_cast<unsigned>(ceil_div(rows, each)), 256, 0, stream, static_cast<const float2*>(parts),
+                            static_cast<const float*>(chosen), targets, rows, static_cast<int>(ceil_div(V, kTileB) * 2), V, loss, lse);
+    };
+    // few tokens: few blocks, and long sums for each of their threads
+    return layer_launched(rows < kSMs * 32 ? finish(finish_rows_kernel<4>, 4) : finish(finish_rows_kernel<32>, 32), what);
 }
 
 template <typename G>
-static cudaError_t sum_parts(const float* parts, int splits, int64_t rows_each, int W, int D, const float* factor, const int64_t* targets, G* out,
-                             int64_t worker, void* stream) {
+static cudaError_t sum_parts(const float* parts, int splits, int64_t rows_each, int W, int D, const int64_t* targets, G* out, int64_t worker,
+                             void* stream) {
     const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows_each * W, 8), kSMs * 8));
     const bool fours = D % 4 == 0 && aligned_to(out, 4 * sizeof(G)) && (W == 1 || worker % 4 == 0);
-    return launch_layer(fours ? sum_parts_kernel<G, 4> : sum_parts_kernel<G, 1>, blocks, 256, 0, stream, parts, splits, rows_each, rows_each * W, D, factor,
+    return launch_layer(fours ? sum_parts_kernel<G, 4> : sum_parts_kernel<G, 1>, blocks, 256, 0, stream, parts, splits, rows_each, rows_each * W, D,
                         targets, out, worker);
 }
 
@@ -732,13 +709,9 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         ws = {at, V * pitch, pitch, (int64_t)W * V * pitch};
         at += plan.weight_copy;
     }
-    auto* r = reinterpret_cast<float*>(at);
-    auto* factor = reinterpret_cast<float*>(at + padded(rows * 4));
-    at += plan.rows;
     auto* d = reinterpret_cast<__nv_bfloat16*>(at);
     auto* dx_parts = reinterpret_cast<float*>(at + plan.d);
     auto* dweight_parts = reinterpret_cast<float*>(at + plan.d + plan.dx_parts);
-    CPDP_TRY(layer_launched(launch_layer(factor_kernel, static_cast<unsigned>(W), 1024, 0, stream, dloss, targets, M, r, factor), what));
 
     CUtensorMap x_rows, x_columns, w_rows, w_columns, d_rows, d_columns;
     CPDP_TRY(encode(&x_rows, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
@@ -754,7 +727,7 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         p.b_at = first;
         const auto gradients = [&](auto planes) {
             constexpr int P = decltype(planes)::value;
-            return multiply_all<false, false>(x_rows, w_rows, p, LogitGradients<P>{targets, lse, r, d, M, plane, plan.pitch, V, first}, stream, what);
+            return multiply_all<false, false>(x_rows, w_rows, p, LogitGradients<P>{targets, lse, dloss, d, M, plane, plan.pitch, V, first}, stream, what);
         };
         CPDP_TRY(plan.planes == 1 ? gradients(std::integral_constant<int, 1>{}) : gradients(std::integral_constant<int, kPlanes>{}));
 
@@ -763,11 +736,11 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         p.a_k = first;
         if (plan.dx_parts) {
             CPDP_TRY((multiply_all<true, false>(w_columns, d_rows, p,
-                                                WriteOut<float>{dx_parts, M * D, rows * D, D, nullptr, nullptr, D, (int)M, piece > 0}, stream, what)));
+                                                WriteOut<float>{dx_parts, M * D, rows * D, D, nullptr, D, (int)M, piece > 0}, stream, what)));
         } else {
             const auto write = [&](auto* out) {
                 using G = std::remove_pointer_t<decltype(out)>;
-                return multiply_all<true, false>(w_columns, d_rows, p, WriteOut<G>{out, M * D, 0, D, factor, targets, D, (int)M, 0}, stream, what);
+                return multiply_all<true, false>(w_columns, d_rows, p, WriteOut<G>{out, M * D, 0, D, targets, D, (int)M, 0}, stream, what);
             };
             CPDP_TRY(dtype == CPDP_F32 ? write(static_cast<float*>(dx)) : write(static_cast<__nv_bfloat16*>(dx)));
         }
@@ -776,19 +749,19 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         const int64_t part = (int64_t)words * D;
         if (plan.dweight_parts) {
             CPDP_TRY((multiply_all<true, true>(x_columns, d_columns, p,
-                                               WriteOut<float>{dweight_parts, part, W * part, D, nullptr, nullptr, D, words, 0}, stream, what)));
-            const auto sum = [&](auto* out) { return sum_parts(dweight_parts, p.splits, words, W, D, factor, nullptr, out + (int64_t)first * D, dweight_worker, stream); };
+                                               WriteOut<float>{dweight_parts, part, W * part, D, nullptr, D, words, 0}, stream, what)));
+            const auto sum = [&](auto* out) { return sum_parts(dweight_parts, p.splits, words, W, D, nullptr, out + (int64_t)first * D, dweight_worker, stream); };
             CPDP_TRY(layer_launched(dweight_dtype == CPDP_F32 ? sum(static_cast<float*>(dweight)) : sum(static_cast<__nv_bfloat16*>(dweight)), what));
         } else {
             const auto write = [&](auto* out) {
                 using G = std::remove_pointer_t<decltype(out)>;
                 return multiply_all<true, true>(x_columns, d_columns, p,
-                                                WriteOut<G>{out + (int64_t)first * D, dweight_worker, 0, D, factor, nullptr, D, words, 0}, stream, what);
+                                                WriteOut<G>{out + (int64_t)first * D, dweight_worker, 0, D, nullptr, D, words, 0}, stream, what);
             };
             CPDP_TRY(dweight_dtype == CPDP_F32 ? write(static_cast<float*>(dweight)) : write(static_cast<__nv_bfloat16*>(dweight)));
         }
     }
     if (!plan.dx_parts) return CPDP_OK;
-    const auto sum = [&](auto* out) { return sum_parts(dx_parts, plan.dx.count, M, W, D, factor, targets, out, M * D, stream); };
+    const auto sum = [&](auto* out) { return sum_parts(dx_parts, plan.dx.count, M, W, D, targets, out, M * D, stream); };
     return layer_launched(dtype == CPDP_F32 ? sum(static_cast<float*>(dx)) : sum(static_cast<__nv_bfloat16*>(dx)), what);
 }

@@ -113,6 +113,19 @@ def test_large_and_equal_logits(dtype):
     near(lse, f["lse"], f["else"])
 
 
+@pytest.mark.parametrize("level", [-300.0, -90.0, 90.0, 300.0])
+@pytest.mark.parametrize("V", [3, 128, 129, 300, 4000])
+def test_all_logits_far_from_zero(V, level):
+    x, weight = torch.zeros(1, 5, 16), normal(rng(V), 1, V, 16)
+    x[..., 0], weight[..., 0] = 1.0, level
+    x[..., 1] = 1.0
+    targets = torch.arange(5)[None] % V
+    f = ref.loss(x, weight, targets)
+    loss, lse = layers.linear_cross_entropy(x.cuda(), weight.cuda(), targets.cuda())
+    near(loss, f["loss"], f["eloss"])
+    near(lse, f["lse"], f["else"])
+
+
 def test_several_pieces_of_the_vocabulary_and_splits():
     """More probabilities than are held at a time, a last piece of another size, and long sums split among blocks. The
     gradients of rows and words picked out are compared."""
