@@ -39,6 +39,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -503,15 +504,22 @@ def gated_recurrence_step(gate, value, state, *, stream=None):
 
 def _head(x, weight, targets) -> tuple:
     """What the calls of the loss share: W, M, V, D and the arguments of x and weight."""
-    W, M, D = shape = _three(x, "x")
-    device, dtype, code = x.device, x.dtype, _dtype(x, "x")
-    xs = _input(x, "x", shape, dtype, device)
-    if weight.dim() != 3:
-        raise ValueError(f"weight must be (W, V, D), or (V, D) of one model; got {tuple(weight.shape)}")
-    V = _sized(weight, "weight")[1]
-    ws = _input(weight, "weight", (W, V, D), dtype, device)
-    targets_at = _whole(targets, "targets", (W, M), torch.int64, device)
-    return (W, M, V, D), (x.data_ptr(), xs[0], xs[1], weight.data_ptr(), ws[0], ws[1]), targets_at, code
+    shape, dtype, device, ws, xs = x.shape, x.dtype, x.device, weight.shape, x.stride()
+    at, code = weight.stride(), _CODES.get(dtype)
+    # one test where all is well: few tokens cost what Python does around them
+    if not (code is not None and len(shape) == 3 and len(ws) == 3 and max(shape) <= MAX_SIZE and max(ws) <= MAX_SIZE
+            and ws[0] == shape[0] and ws[2] == shape[2] and weight.dtype is dtype and weight.device == device and xs[2] == 1 == at[2]
+            and targets.shape == shape[:2] and targets.dtype is torch.int64 and targets.device == device and targets.is_contiguous()):
+        W, M, D = _three(x, "x")
+        code = _dtype(x, "x")
+        xs = _input(x, "x", shape, dtype, device)
+        if weight.dim() != 3:
+            raise ValueError(f"weight must be (W, V, D), or (V, D) of one model; got {tuple(ws)}")
+        _sized(weight, "weight")
+        at = _input(weight, "weight", (W, ws[1], D), dtype, device)
+        _whole(targets, "targets", (W, M), torch.int64, device)
+    W, M, D = shape
+    return (W, M, ws[1], D), (x.data_ptr(), xs[0], xs[1], weight.data_ptr(), at[0], at[1]), targets.data_ptr(), code
 
 
 def linear_cross_entropy(x, weight, targets, *, stream=None):
@@ -524,13 +532,14 @@ def linear_cross_entropy(x, weight, targets, *, stream=None):
     if x.dim() == 2 and weight.dim() == 2:
         loss, lse = linear_cross_entropy(x[None], weight[None], targets[None], stream=stream)
         return loss[0], lse[0]
-    _no_autograd(x=x, weight=weight)
+    if x.requires_grad or weight.requires_grad:
+        _no_autograd(x=x, weight=weight)
     device = _cuda(x, "x")
     if _elsewhere(device, stream):
         with _there(device, stream):
             return linear_cross_entropy(x, weight, targets)
     (W, M, V, D), operands, targets_at, code = _head(x, weight, targets)
-    loss, lse = torch.empty((2, W, M), dtype=_F32, device=device).unbind(0)
+    loss, lse = torch.empty((W, M), dtype=_F32, device=device), torch.empty((W, M), dtype=_F32, device=device)
     needed = _entry("cpdp_linear_cross_entropy_workspace")(*operands, code, W, M, V, D)
     work = _workspace(needed, device)
     _check(_entry("cpdp_linear_cross_entropy")(*operands, targets_at, code, W, M, V, D, loss.data_ptr(), lse.data_ptr(), _ptr(work), needed,
@@ -700,13 +709,9 @@ def causal_conv_step(x, weight, bias, state, *, stream=None):
     return y
 
 
-class _ScanInputs(ctypes.Structure):
-    """cpdp_scan_inputs."""
-    _fields_ = [(n, t) for names, kinds in ((("u", "u_seq", "u_step"), (_P, _L, _L)), (("delta", "delta_seq", "delta_step"), (_P, _L, _L)),
-                                            (("z", "z_seq", "z_step"), (_P, _L, _L)), (("b", "b_seq", "b_step"), (_P, _L, _L)),
-                                            (("c", "c_seq", "c_step"), (_P, _L, _L)), (("a_log", "a_log_worker"), (_P, _L)),
-                                            (("skip", "skip_worker"), (_P, _L)), (("bias", "bias_worker"), (_P, _L)), (("lengths",), (_P,)))
-                for n, t in zip(names, kinds)]
+# cpdp_scan_inputs: a pointer and two strides each of u, delta, z, b and c; a pointer and a stride each of a_log, skip and
+# bias; lengths. All fields are of 8 bytes.
+_pack_scan = struct.Struct("=22q").pack
 
 
 def _scan_inputs(u, delta, a_log, b, c, skip, bias, z, lengths, device) -> tuple:
@@ -723,10 +728,10 @@ def _scan_inputs(u, delta, a_log, b, c, skip, bias, z, lengths, device) -> tuple
         s = _input(t, name, shape, dtype, device)
         return t.data_ptr(), s[0], 0 if step else s[1]
 
-    inputs = _ScanInputs(*at(u, "u", shape), *at(delta, "delta", shape), *((None, 0, 0) if z is None else at(z, "z", shape)),
-                         *at(b, "b", few), *at(c, "c", few), a_log.data_ptr(), _workers_part(a_log, "a_log", (D, N), W, device),
-                         skip.data_ptr(), _workers_part(skip, "skip", (D,), W, device), bias.data_ptr(),
-                         _workers_part(bias, "bias", (D,), W, device), _whole(lengths, "lengths", (B,), torch.int32, device))
+    inputs = _pack_scan(*at(u, "u", shape), *at(delta, "delta", shape), *((0, 0, 0) if z is None else at(z, "z", shape)),
+                        *at(b, "b", few), *at(c, "c", few), a_log.data_ptr(), _workers_part(a_log, "a_log", (D, N), W, device),
+                        skip.data_ptr(), _workers_part(skip, "skip", (D,), W, device), bias.data_ptr(),
+                        _workers_part(bias, "bias", (D,), W, device), _whole(lengths, "lengths", (B,), torch.int32, device) or 0)
     return W, N, inputs
 
 
@@ -761,7 +766,7 @@ def selective_scan(u, delta, a_log, b, c, skip, bias, z=None, h0=None, lengths=N
     carries = torch.empty((B, -(-T // CARRY_STEPS), D, N), dtype=_F32, device=device) if carry else None
     needed = _entry("cpdp_selective_scan_workspace")(B, T, D, N)
     work = _workspace(needed, device)
-    _check(_entry("cpdp_selective_scan")(ctypes.byref(inputs), _CODES[u.dtype], W, B, T, D, N, h0_at, y.data_ptr(), last.data_ptr(), _ptr(carries),
+    _check(_entry("cpdp_selective_scan")(inputs, _CODES[u.dtype], W, B, T, D, N, h0_at, y.data_ptr(), last.data_ptr(), _ptr(carries),
                                          _ptr(work), needed, _stream(device.index)))
     return y, last, carries
 
@@ -804,7 +809,7 @@ def selective_scan_backward(dy, u, delta, a_log, b, c, skip, bias, carry, z=None
     needed = _entry("cpdp_selective_scan_backward_workspace")(B, T, D, N)
     work = _workspace(needed, device)
     _check(_entry("cpdp_selective_scan_backward")(
-        dy.data_ptr(), gs[0], gs[1], ctypes.byref(inputs), _CODES[kind], W, B, T, D, N, carry_at, dlast_at, du.data_ptr(), ddelta.data_ptr(),
+        dy.data_ptr(), gs[0], gs[1], inputs, _CODES[kind], W, B, T, D, N, carry_at, dlast_at, du.data_ptr(), ddelta.data_ptr(),
         _ptr(dz), db.data_ptr(), dc.data_ptr(), dh0.data_ptr(), da_log.data_ptr(), da_log.stride(0), dskip.data_ptr(), dskip.stride(0),
         dbias.data_ptr(), dbias.stride(0), _CODES[dtype], _ptr(work), needed, _stream(device.index)))
     return du, ddelta, da_log, db, dc, dskip, dbias, dz, dh0
@@ -814,19 +819,36 @@ def selective_scan_step(u, delta, a_log, b, c, skip, bias, state, z=None, *, str
     """One token for each of B sequences: ``state`` (float32, (B, D, N)) is
     replaced by the next state, and y (B, D) is returned. u, delta, z (B, D); b, c
     (B, N); the weights as those of ``selective_scan``."""
-    a_log, skip, bias = _of_one_model(a_log, skip, bias)
-    _no_autograd(u=u, delta=delta, a_log=a_log, b=b, c=c, skip=skip, bias=bias, state=state, z=z)
-    device = _cuda(u, "u")
-    if _elsewhere(device, stream):
-        with _there(device, stream):
-            return selective_scan_step(u, delta, a_log, b, c, skip, bias, state, z)
-    if u.dim() != 2:
-        raise ValueError(f"u must be (B, D), got {tuple(u.shape)}")
-    W, N, inputs = _scan_inputs(u, delta, a_log, b, c, skip, bias, z, None, device)
-    B, D = shape = u.shape
-    state_at = _whole(state, "state", (B, D, N), _F32, device)
-    y = torch.empty(shape, dtype=u.dtype, device=device)
-    _check(_entry("cpdp_selective_scan_step")(ctypes.byref(inputs), _CODES[u.dtype], W, B, D, N, state_at, y.data_ptr(), _stream(device.index)))
+    if a_log.dim() == 2:
+        a_log, skip, bias = _of_one_model(a_log, skip, bias)
+    shape, dtype, device, few, weights = u.shape, u.dtype, u.device, b.shape, a_log.shape
+    us, ds, bs, cs, ws, ks, os = u.stride(), delta.stride(), b.stride(), c.stride(), a_log.stride(), skip.stride(), bias.stride()
+    zs, z_at = ((0, 1), 0) if z is None else (z.stride(), z.data_ptr())
+    # one test where all is well: a decoding step costs what Python does around it
+    if not (stream is None and dtype in _CODES and u.is_cuda and device.index == _current_device() and len(shape) == 2 and len(weights) == 3
+            and delta.shape == shape and (z is None or z.shape == shape and z.dtype is dtype and z.device == device and not z.requires_grad)
+            and weights[0] > 0 and shape[0] % weights[0] == 0 and max(shape) <= MAX_SIZE and shape[1] == weights[1]
+            and skip.shape == weights[:2] == bias.shape and few == (shape[0], weights[2]) == c.shape and state.shape == (*shape, weights[2])
+            and delta.dtype is dtype and b.dtype is dtype and c.dtype is dtype and state.dtype is _F32 and a_log.dtype is _F32
+            and skip.dtype is _F32 and bias.dtype is _F32 and ws[1:] == (weights[2], 1) and us[1] == ds[1] == zs[1] == bs[1] == cs[1] == ks[1] == os[1] == 1
+            and state.is_contiguous() and delta.device == device == b.device == c.device == state.device
+            and a_log.device == device == skip.device == bias.device
+            and not (u.requires_grad or delta.requires_grad or b.requires_grad or c.requires_grad or state.requires_grad
+                     or a_log.requires_grad or skip.requires_grad or bias.requires_grad)):
+        _no_autograd(u=u, delta=delta, a_log=a_log, b=b, c=c, skip=skip, bias=bias, state=state, z=z)
+        if _elsewhere(_cuda(u, "u"), stream):
+            with _there(device, stream):
+                return selective_scan_step(u, delta, a_log, b, c, skip, bias, state, z)
+        if len(shape) != 2:
+            raise ValueError(f"u must be (B, D), got {tuple(shape)}")
+        N = _scan_inputs(u, delta, a_log, b, c, skip, bias, z, None, device)[1]
+        _whole(state, "state", (*shape, N), _F32, device)
+    B, D = shape
+    inputs = _pack_scan(u.data_ptr(), us[0], 0, delta.data_ptr(), ds[0], 0, z_at, zs[0], 0, b.data_ptr(), bs[0], 0, c.data_ptr(), cs[0], 0,
+                        a_log.data_ptr(), ws[0], skip.data_ptr(), ks[0], bias.data_ptr(), os[0], 0)
+    y = torch.empty(shape, dtype=dtype, device=device)
+    _check(_entry("cpdp_selective_scan_step")(inputs, _CODES[dtype], weights[0], B, D, weights[2], state.data_ptr(), y.data_ptr(),
+                                              _stream(device.index)))
     return y
 
 
@@ -838,17 +860,22 @@ def clip_gradients(grads, max_norm: float, *, out=None, stream=None):
     ones. One model's (N,) is taken too."""
     if grads.dim() == 1:
         return clip_gradients(grads[None], max_norm, out=None if out is None else out[None], stream=stream)[0]
-    _no_autograd(grads=grads, out=out)
-    device = _cuda(grads, "grads")
-    if _elsewhere(device, stream):
-        with _there(device, stream):
-            return clip_gradients(grads, max_norm, out=out)
-    if grads.dim() != 2:
-        raise ValueError(f"grads must be (W, N), or (N,) of one model; got {tuple(grads.shape)}")
-    shape, dtype, code = grads.shape, grads.dtype, _dtype(grads, "grads")
     if out is None:
         out = grads
-    gs, os = _input(grads, "grads", shape, dtype, device), _input(out, "out", shape, dtype, device)
+    shape, dtype, device, gs, os = grads.shape, grads.dtype, grads.device, grads.stride(), out.stride()
+    code = _CODES.get(dtype)
+    # one test where all is well: a small model's rows cost what Python does around them
+    if not (stream is None and code is not None and grads.is_cuda and device.index == _current_device() and len(shape) == 2
+            and out.shape == shape and out.dtype is dtype and out.device == device and gs[1] == 1 == os[1]
+            and not (grads.requires_grad or out.requires_grad)):
+        _no_autograd(grads=grads, out=out)
+        if _elsewhere(_cuda(grads, "grads"), stream):
+            with _there(device, stream):
+                return clip_gradients(grads, max_norm, out=out)
+        if grads.dim() != 2:
+            raise ValueError(f"grads must be (W, N), or (N,) of one model; got {tuple(shape)}")
+        code = _dtype(grads, "grads")
+        gs, os = _input(grads, "grads", shape, dtype, device), _input(out, "out", shape, dtype, device)
     W, N = shape
     norms = torch.empty((W,), dtype=_F32, device=device)
     if W == 0:
