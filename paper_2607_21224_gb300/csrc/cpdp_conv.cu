@@ -12,10 +12,12 @@ namespace {
 // A sequence's inputs with the K - 1 before it: e_0 .. e_(T+K-2), e_(K-1) = x_0,
 // and v_t = bias + sum_k weight_k e_(t+k). A thread walks a stretch of steps of V
 // neighbouring channels (16 or 8 bytes; 1 where rows are not whole pieces), with
-// the last K - 1 inputs in registers, two channels to a pair, and kAhead rows on
-// their way. Both passes are bound by memory.
-constexpr int kThreads = 128, kAhead = 8;
-constexpr int kForwardBlocks = 4, kBackwardBlocks = 3;  // per SM
+// the last K - 1 inputs in registers, two channels to a pair, and some rows on
+// their way. Both passes are bound by memory: rows of 16 bytes per thread eight
+// ahead, in the backward pass four of x and dy of 8 bytes, at as many threads as
+// that leaves (eight ahead at three quarters of the threads: 3 us more of 36).
+constexpr int kThreads = 128, kForwardAhead = 8, kBackwardAhead = 4;
+constexpr int kForwardBlocks = 4, kBackwardBlocks = 4;  // per SM
 constexpr int kMostTaps = CPDP_CONV_MAX_TAPS;
 
 // V neighbouring elements as they lie in memory, loaded where they are there; else 0. Predicates, not branches: see load_once.
@@ -76,18 +78,44 @@ struct Conv {
     int steps, stretches;      // steps of a stretch
 };
 
+// The weights of a thread's channels. They lie together in memory, at any alignment; the warp's lanes read them side by
+// side and hand them over through shared memory (each reading its own took two thirds of a forward pass).
+template <int V, int K>
+struct TapsShared {
+    static constexpr int kEach = V * (K + 1);
+    float v[32][kEach | 1];
+};
 template <typename T, int V, int K>
 struct Taps {
     static constexpr int P = (V + 1) / 2;
     Pair w[K][P], bias[P];
-    __device__ __forceinline__ Taps(const Conv& p, int worker, int d) {
-        const float *from = p.weight + worker * p.weight_worker + (int64_t)d * K, *b = p.bias + worker * p.bias_worker + d;
+    // All lanes of the warp; `live`: the lane has channels.
+    __device__ __forceinline__ Taps(const Conv& p, int worker, int d, bool live, TapsShared<V, K>& s) {
+        const int lane = threadIdx.x % 32;
+        const int64_t weights = worker * p.weight_worker + (int64_t)d * K, biases = worker * p.bias_worker + d;
+        const unsigned there = __ballot_sync(~0u, live);
+        const auto fetch = [&](const float* from, int64_t at, auto many, int to) {
+            constexpr int COUNT = decltype(many)::value;
+            float v[COUNT];
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const int whose = (i * 32 + lane) / COUNT;
+                const int64_t start = __shfl_sync(~0u, at, whose);
+                v[i] = there >> whose & 1 ? from[start + (i * 32 + lane) % COUNT] : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) s.v[(i * 32 + lane) / COUNT][to + (i * 32 + lane) % COUNT] = v[i];
+        };
+        fetch(p.weight, weights, std::integral_constant<int, V * K>{}, 0);
+        fetch(p.bias, biases, std::integral_constant<int, V>{}, V * K);
+        __syncwarp();
+        const float* own = s.v[lane];
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             constexpr int next = V > 1;
 #pragma unroll
-            for (int k = 0; k < K; ++k) w[k][i] = pair(from[2 * i * K + k], next ? from[(2 * i + next) * K + k] : 0.f);
-            bias[i] = pair(b[2 * i], next ? b[2 * i + next] : 0.f);
+            for (int k = 0; k < K; ++k) w[k][i] = pair(own[2 * i * K + k], next ? own[(2 * i + next) * K + k] : 0.f);
+            bias[i] = pair(own[V * K + 2 * i], next ? own[V * K + 2 * i + next] : 0.f);
         }
     }
     __device__ __forceinline__ Pair sum(const Pair (&e)[K][P], int i) const {
@@ -125,32 +153,32 @@ __global__ void __launch_bounds__(kThreads, kForwardBlocks)
 conv_kernel(Conv p, T* y, T* last) {
     layer_begin();
     constexpr int P = (V + 1) / 2;
+    __shared__ TapsShared<V, K> shared[kThreads / 32];
     const int64_t columns = p.D / V, i = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = i / columns;
-    const int64_t b = row / p.stretches;
-    if (b >= p.B) return;
-    const int d = static_cast<int>(i - row * columns) * V, stretch = static_cast<int>(row - b * p.stretches);
+    const bool live = row / p.stretches < p.B;
+    const int64_t b = live ? row / p.stretches : 0;
+    const int d = static_cast<int>(i - row * columns) * V, stretch = live ? static_cast<int>(row - b * p.stretches) : 0;
     const Inputs<T, V, K> in(p, b, d);
-    const int first = stretch * p.steps, end = min(first + p.steps, p.T), inside = min(end, in.n);
-    Few<T, V> next[kAhead];
+    const int first = stretch * p.steps, end = live ? min(first + p.steps, p.T) : 0, inside = min(end, in.n);
+    Few<T, V> next[kForwardAhead];
 #pragma unroll
-    for (int r = 0; r < kAhead; ++r) in.row(next[r], first + r);
+    for (int r = 0; r < kForwardAhead; ++r) in.row(next[r], first + r < inside ? first + r : in.n);
     Pair e[K][P];
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) in.get(e[k], first + k);
-    const Taps<T, V, K> taps(p, static_cast<int>(b / p.each), d);
+    const Taps<T, V, K> taps(p, static_cast<int>(b / p.each), d, live, shared[threadIdx.x / 32]);
+    if (!live) return;
     T* to = y + (b * p.T + first) * p.D + d;
-    for (int t = first; t < inside; t += kAhead) {
+    for (int t = first; t < inside; t += kForwardAhead) {
 #pragma unroll
-        for (int r = 0; r < kAhead; ++r) {
+        for (int r = 0; r < kForwardAhead; ++r) {
             Pair out[P];
             next[r].get(e[K - 1]);
-            in.row(next[r], t + r + kAhead < inside ? t + r + kAhead : in.n);
+            in.row(next[r], t + r + kForwardAhead < inside ? t + r + kForwardAhead : in.n);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 const Pair v = taps.sum(e, i);
-                Pair a, rest;
-                gate_of<T>(v, a, rest);
-                out[i] = mul2(v, a);
+                out[i] = mul2(v, sigmoid(v));
 #pragma unroll
                 for (int k = 0; k + 1 < K; ++k) e[k][i] = e[k + 1][i];
             }
@@ -187,15 +215,20 @@ template <typename T, int V, int K>
 __global__ void __launch_bounds__(kThreads, kBackwardBlocks)
 conv_backward_kernel(Conv p, ConvGradients g) {
     layer_begin();
-    __shared__ float shared[kThreads][V * (K + 1) + 1];
+    __shared__ union {
+        float sums[kThreads][V * (K + 1) + 1];
+        TapsShared<V, K> taps[kThreads / 32];
+    } shared_memory;
+    auto& shared = shared_memory.sums;
     constexpr int P = (V + 1) / 2;
     const int lane = threadIdx.x % g.lanes, team = threadIdx.x / g.lanes, teams = kThreads / g.lanes;
     const int group = blockIdx.x % g.groups, rest = blockIdx.x / g.groups, part = rest % g.part_count, worker = rest / g.part_count;
     const int d = (group * g.lanes + lane) * V;
     const bool live = d < p.D;
     Pair dw[K][P] = {}, db[P] = {};
+    const Taps<T, V, K> taps(p, worker, d, live, shared_memory.taps[threadIdx.x / 32]);
+    __syncthreads();  // before the sums take the same memory
     if (live) {
-        const Taps<T, V, K> taps(p, worker, d);
         const int items = p.each * p.stretches;
         for (int item = part * teams + team; item < items; item += g.part_count * teams) {
             const int64_t b = (int64_t)worker * p.each + item / p.stretches;
@@ -203,34 +236,32 @@ conv_backward_kernel(Conv p, ConvGradients g) {
             const T* dy = static_cast<const T*>(g.dy) + b * g.dy_seq + d;
             const int first = item % p.stretches * p.steps, end = min(first + p.steps, p.T + K - 1);
             const int from = max(first - (K - 1), 0), inside = min(end, in.n);
-            Few<T, V> next[kAhead], next_dy[kAhead];
+            Few<T, V> next[kBackwardAhead], next_dy[kBackwardAhead];
             const auto fetch = [&](int r, int t) {
                 in.row(next[r], t < end ? t : in.n);
                 next_dy[r].load(dy + t * g.dy_step, t < inside);
             };
 #pragma unroll
-            for (int r = 0; r < kAhead; ++r) fetch(r, from + r);
+            for (int r = 0; r < kBackwardAhead; ++r) fetch(r, from + r);
             Pair e[K][P] = {}, dv[K][P] = {};  // dv[k]: of step t - k
             if (in.n > 0)
 #pragma unroll
                 for (int k = 0; k < K - 1; ++k) in.get(e[k], from + k);
-            for (int t0 = from; t0 < end; t0 += kAhead) {
+            for (int t0 = from; t0 < end; t0 += kBackwardAhead) {
 #pragma unroll
-                for (int r = 0; r < kAhead; ++r) {
+                for (int r = 0; r < kBackwardAhead; ++r) {
                     const int t = t0 + r;
                     Pair out[P], dy_r[P];
                     next[r].get(e[K - 1]);
                     next_dy[r].get(dy_r);
-                    fetch(r, t + kAhead);
+                    fetch(r, t + kBackwardAhead);
 #pragma unroll
                     for (int i = 0; i < P; ++i) {
                         const Pair v = taps.sum(e, i);
-                        Pair a, away;
-                        gate_of<T>(v, a, away);
 #pragma unroll
                         for (int k = K - 1; k > 0; --k) dv[k][i] = dv[k - 1][i];
-                        dv[0][i] = t < inside ? mul2(dy_r[i], mul2(a, fma2(v, away, kOnes))) : kZeros;
-                        const Pair own = t >= first ? dv[0][i] : kZeros;
+                        dv[0][i] = where(t < inside, mul2(dy_r[i], silu_slope(v, sigmoid(v))));
+                        const Pair own = where(t >= first, dv[0][i]);
                         db[i] = add2(db[i], own);
                         out[i] = mul2(taps.w[0][i], dv[0][i]);
                         dw[0][i] = fma2(own, e[0][i], dw[0][i]);
@@ -283,10 +314,12 @@ template <typename T, int K>
 __global__ void __launch_bounds__(kThreads)
 conv_step_kernel(Conv p, T* state, T* y) {
     layer_begin();
+    __shared__ TapsShared<1, K> shared[kThreads / 32];
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, b = i / p.D;
-    if (b >= p.B) return;
+    const bool live = b < p.B;
     const int d = static_cast<int>(i - b * p.D);
-    const Taps<T, 1, K> taps(p, static_cast<int>(b / p.each), d);
+    const Taps<T, 1, K> taps(p, static_cast<int>(b / p.each), d, live, shared[threadIdx.x / 32]);
+    if (!live) return;
     T* s = state + b * (K - 1) * p.D + d;
     T e[K];
 #pragma unroll
@@ -296,11 +329,9 @@ conv_step_kernel(Conv p, T* state, T* y) {
 #pragma unroll
     for (int k = 0; k < K; ++k) held[k][0] = pair(to_float(e[k]), 0.f);
     const Pair v = taps.sum(held, 0);
-    Pair a, rest;
-    gate_of<T>(v, a, rest);
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) s[(int64_t)k * p.D] = e[k + 1];
-    y[i] = from_float<T>(floats(mul2(v, a)).x);
+    y[i] = from_float<T>(floats(mul2(v, sigmoid(v))).x);
 }
 
 cpdp_status check_conv(int W, int B, int64_t T, int D, int K, cpdp_dtype dtype) {
@@ -318,7 +349,7 @@ cpdp_status check_conv(int W, int B, int64_t T, int D, int K, cpdp_dtype dtype) 
 // Steps of a stretch of the forward pass: as many stretches as run at once.
 int stretch_of(int64_t T, int64_t rows) {
     const int64_t count = std::max<int64_t>((int64_t)kSMs * kForwardBlocks * kThreads / std::max<int64_t>(rows, 1), 1);
-    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(ceil_div(T, count), 8), 128));
+    return static_cast<int>(std::min<int64_t>(std::max<int64_t>(ceil_div(ceil_div(T, count), kForwardAhead), 1) * kForwardAhead, 128));
 }
 
 // Whether rows of an array are whole pieces of `bytes`.
@@ -339,9 +370,8 @@ Spread spread_of(int W, int B, int64_t T, int D, int K, int V) {
     s.groups = static_cast<int>(ceil_div(columns, s.lanes));
     const int64_t most = std::max<int64_t>(kSMs * kBackwardBlocks / ((int64_t)s.groups * W), 1), teams = most * (kThreads / s.lanes);
     int64_t least = -1;
-    for (int64_t turns = 1; turns <= 16; ++turns) {
-        const int64_t steps = std::min<int64_t>(std::max<int64_t>(ceil_div(rows, std::max<int64_t>(turns * teams / each, 1)), 8), 256);
-        const int64_t stretches = ceil_div(rows, steps), cost = ceil_div(each * stretches, teams) * (steps + K + 5);
+    for (int64_t walked = 2 * kBackwardAhead; walked <= 32 * kBackwardAhead; walked += kBackwardAhead) {  // with the K - 1 steps before a stretch
+        const int64_t steps = walked - (K - 1), stretches = ceil_div(rows, steps), cost = ceil_div(each * stretches, teams) * (walked + kBackwardAhead);
         if (least < 0 || cost < least) least = cost, s.steps = static_cast<int>(steps), s.stretches = static_cast<int>(stretches);
     }
     s.parts = static_cast<int>(std::max<int64_t>(std::min(ceil_div(each * s.stretches, kThreads / s.lanes), most), 1));

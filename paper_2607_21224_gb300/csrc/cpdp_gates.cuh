@@ -82,6 +82,22 @@ __device__ __forceinline__ void gate_of(Pair gates, Pair& a, Pair& rest) {
     rest = pair(x.x >= 0.f ? q.x : r.x, x.y >= 0.f ? q.y : r.y);
 }
 
+// x or 0. Not a branch around what makes x, which ?: became where that is short (a backward pass of the convolution
+// took 62 us for 48).
+__device__ __forceinline__ Pair where(bool there, Pair x) {
+    Pair r;
+    asm("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\tselp.b64 %0, %1, 0, p;\n\t}" : "=l"(r) : "l"(x), "r"(there ? 1u : 0u));
+    return r;
+}
+// sigmoid(x) alone, as 1 / (1 + 2^(-x log2(e))): 6 instructions for both, where gate_of takes some 20. The power's
+// argument is rounded, which is |x| 2^-24 of the result; below -88 the power is infinite and the result 0.
+__device__ __forceinline__ Pair sigmoid(Pair x) {
+    const float2 p = floats(mul2(x, twice(kLog2eHigh))), s = floats(add2(pair(power_of_minus(p.x), power_of_minus(p.y)), kOnes));
+    return pair(reciprocal(s.x), reciprocal(s.y));
+}
+// The slope of x sigmoid(x), a = sigmoid(x): a (1 + x (1 - a)).
+__device__ __forceinline__ Pair silu_slope(Pair x, Pair a) { return mul2(a, fma2(x, fma2(a, kMinusOnes, kOnes), kOnes)); }
+
 }  // namespace
 }  // namespace cpdp
 #endif

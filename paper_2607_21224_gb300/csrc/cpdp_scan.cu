@@ -510,10 +510,8 @@ scan_kernel(Scan s, const float* h0, T* y, float* last, float* carry, bool quads
                 const int r = side.row + i * side.kDown;
                 Pair v = fma2(skip, now_u.v[i].get(), *reinterpret_cast<const Pair*>(&m.sum[r][side.at]));
                 if (gated) {
-                    Pair a, rest;
                     const Pair vz = now_z.v[i].get();
-                    gate_of<T>(vz, a, rest);
-                    v = mul2(v, mul2(vz, a));
+                    v = mul2(v, mul2(vz, sigmoid(vz)));
                 }
                 if (live && (rows == R || r < rows)) store_two<WIDE>(const_cast<T*>(out.at(t + i * side.kDown)), v, second);
             }
@@ -660,11 +658,7 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
                 dts[i] = softplus<T>(add2(in_delta.v[i].get(), bias));
                 if (rows < R && r >= rows) dts[i] = kZeros;
                 Pair gy = in_dy.v[i].get();
-                if (gated) {
-                    Pair a, away;
-                    gate_of<T>(in_z.v[i].get(), a, away);
-                    gy = mul2(gy, mul2(in_z.v[i].get(), a));
-                }
+                if (gated) gy = mul2(gy, mul2(in_z.v[i].get(), sigmoid(in_z.v[i].get())));
                 *reinterpret_cast<Pair*>(&m.dt[r][side.at]) = dts[i];
                 *reinterpret_cast<Pair*>(&m.x[r][side.at]) = mul2(dts[i], in_u.v[i].get());
                 *reinterpret_cast<Pair*>(&m.gy[r][side.at]) = gy;
@@ -776,17 +770,15 @@ scan_backward_kernel(Scan s, ScanGradients g, bool quads) {
                 const int r = side.row + i * side.kDown, at = t + i * side.kDown;
                 const Pair through = *reinterpret_cast<const Pair*>(&m.dt[r][side.at]), reach = *reinterpret_cast<const Pair*>(&m.x[r][side.at]);
                 const Pair sum = *reinterpret_cast<const Pair*>(&m.gy[r][side.at]), vu = in_u.v[i].get(), vdy = in_dy.v[i].get();
-                Pair gy = vdy, gate, away;
+                Pair gy = vdy;
                 const bool here = live && (rows == R || r < rows);
                 if (gated) {
                     const Pair vz = in_z.v[i].get();
-                    gate_of<T>(vz, gate, away);
+                    const Pair gate = sigmoid(vz);
                     gy = mul2(vdy, mul2(vz, gate));
-                    const Pair slope = mul2(gate, fma2(vz, away, kOnes));
-                    if (here) store(dz, at, mul2(mul2(vdy, slope), fma2(skip, vu, sum)));
+                    if (here) store(dz, at, mul2(mul2(vdy, silu_slope(vz, gate)), fma2(skip, vu, sum)));
                 }
-                gate_of<T>(add2(in_delta.v[i].get(), bias), gate, away);
-                const Pair dbase = mul2(fma2(through, vu, mul2(reach, twice(kLn2f))), gate);
+                const Pair dbase = mul2(fma2(through, vu, mul2(reach, twice(kLn2f))), sigmoid(add2(in_delta.v[i].get(), bias)));
                 if (here) {
                     store(du, at, fma2(through, dts[i], mul2(skip, gy)));
                     store(ddelta, at, dbase);
@@ -879,11 +871,7 @@ scan_backward_maps_kernel(Scan s, Rows grads) {
         for (int i = 0; i < side.kItems; ++i) {
             const int r = side.row + i * side.kDown;
             Pair gy = next_dy.v[i].get();
-            if (gated) {
-                Pair a, away;
-                gate_of<T>(next_z.v[i].get(), a, away);
-                gy = mul2(gy, mul2(next_z.v[i].get(), a));
-            }
+            if (gated) gy = mul2(gy, mul2(next_z.v[i].get(), sigmoid(next_z.v[i].get())));
             *reinterpret_cast<Pair*>(&m.dt[r][side.at]) = softplus<T>(add2(next_delta.v[i].get(), bias));
             *reinterpret_cast<Pair*>(&m.x[r][side.at]) = gy;
         }
@@ -979,9 +967,7 @@ scan_step_kernel(Scan s, float* h, T* y) {
     float v = fmaf(s.skip[worker * s.skip_worker + d], u, sum);
     if (s.z.p != nullptr) {
         const float z = to_float(static_cast<const T*>(s.z.p)[b * s.z.seq + d]);
-        Pair a, rest;
-        gate_of<T>(pair(z, 0.f), a, rest);
-        v *= z * floats(a).x;
+        v *= z * floats(sigmoid(pair(z, 0.f))).x;
     }
     y[i] = from_float<T>(v);
 }
