@@ -89,20 +89,20 @@ __device__ __forceinline__ void multiply(uint32_t sums, uint64_t a, uint64_t b, 
 __device__ __forceinline__ void arrive_when_multiplied(uint64_t* b) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(b)) : "memory");
 }
-__device__ __forceinline__ void copy_tile(uint32_t to, const CUtensorMap* map, int inner, int outer, int w, int plane, uint64_t* full) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
-        "l"(map), "r"(inner), "r"(outer), "r"(w), "r"(plane), "r"(smem_at(full))
-        : "memory");
-}
-template <bool SLOW, int EXTENT>
+// One copy per operand and step (boxes of 64 columns one by one took a sixth longer): an operand that has k as its slow
+// axis is a tensor of groups of 64 columns, each group's rows one after another in shared memory.
+template <bool SLOW>
 __device__ __forceinline__ void copy_operand(uint32_t to, const CUtensorMap* map, int at, int k, int w, int plane, uint64_t* full) {
-    if constexpr (SLOW) {
-#pragma unroll
-        for (int c = 0; c < EXTENT / 64; ++c) copy_tile(to + c * kBlockBytes, map, at + c * 64, k, w, plane, full);
-    } else {
-        copy_tile(to, map, k, at, w, plane, full);
-    }
+    if constexpr (SLOW)
+        asm volatile(
+            "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(to),
+            "l"(map), "r"(0), "r"(k), "r"(at / 64), "r"(w), "r"(plane), "r"(smem_at(full))
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
+            "l"(map), "r"(k), "r"(at), "r"(w), "r"(plane), "r"(smem_at(full))
+            : "memory");
 }
 
 // E: the epilogue. run(v, w, split, a, b) takes 128 sums of lane a, columns b to b + 127.
@@ -159,8 +159,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(&full[s])), "r"(kSlotBytes) : "memory");
                     const int segment = (first + k) / p.steps, at = (first + k - segment * p.steps) * kStep;
                     const uint32_t slot = slots + s * kSlotBytes;
-                    copy_operand<A_SLOW, kTileA>(slot, &map_a, p.a_at + t.a * kTileA, p.a_k + at, t.w, kPlanesA >> 4 * segment & 15, &full[s]);
-                    copy_operand<B_SLOW, kTileB>(slot + kABytes, &map_b, p.b_at + t.b * kTileB, p.b_k + at, t.w, kPlanesB >> 4 * segment & 15,
+                    copy_operand<A_SLOW>(slot, &map_a, p.a_at + t.a * kTileA, p.a_k + at, t.w, kPlanesA >> 4 * segment & 15, &full[s]);
+                    copy_operand<B_SLOW>(slot + kABytes, &map_b, p.b_at + t.b * kTileB, p.b_k + at, t.w, kPlanesB >> 4 * segment & 15,
                                                  &full[s]);
                 }
             }
@@ -336,20 +336,25 @@ struct LogitGradients {
         const int64_t hot = target - first - b;
         __nv_bfloat16* to = d + row * pitch + b;
 #pragma unroll
-        for (int j = 0; j < kHalf; j += 8) {
-            float g[8];
+        for (int j = 0; j < kHalf; j += 16) {  // 32 bytes, a whole sector of L2; the pitch is of whole ones
+            float g[16];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 16; ++e) {
                 const float p = power((v[j + e] - l) * kLog2e) - (j + e == hot ? 1.f : 0.f);
                 g[e] = ignored ? 0.f : p * scale;
             }
             if (b + j < pitch)
 #pragma unroll
             for (int q = 0; q < PLANES; ++q) {
-                store_piece<8>(to + q * plane + j, g);
+                uint32_t v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = cpdp::pack(g[2 * e], g[2 * e + 1]);
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + q * plane + j), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                             "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                             : "memory");
                 if (q + 1 < PLANES)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) g[e] -= __bfloat162float(__float2bfloat16_rn(g[e]));
+                    for (int e = 0; e < 16; ++e) g[e] -= __bfloat162float(__float2bfloat16_rn(g[e]));
             }
         }
     }
@@ -460,10 +465,10 @@ pack_kernel(const T* x, int64_t worker, int64_t stride, int64_t rows_each, int64
 constexpr int64_t kPieceBytes = int64_t(1) << 30;  // of d at a time
 
 int64_t padded(int64_t bytes) { return ceil_div(bytes, 256) * 256; }
-int64_t pitch_of(int64_t n) { return ceil_div(n, 8) * 8; }
+int64_t pitch_of(int64_t n) { return ceil_div(n, 64) * 64; }  // whole groups of columns
 
 // How k is split among blocks: the number of parts that takes least time, by
-// the turns that the tiles take on the SMs. A step of a tile takes 0.3 us, its
+// the turns that the tiles take on the SMs. A step of a tile takes 0.36 us, its
 // start and end 3; parts cost their writing and reading at 4 TB/s and a launch.
 struct Splits {
     int count, each;
@@ -471,10 +476,10 @@ struct Splits {
 Splits splits_of(int64_t tiles, int64_t steps, int64_t outputs) {
     Splits best{1, static_cast<int>(steps)};
     double least = 0;
-    const int64_t most = ceil_div(2 * kSMs, tiles);
+    const int64_t most = std::max<int64_t>(ceil_div(2 * kSMs, tiles), tiles < 8 * kSMs ? 4 : 1);
     for (int64_t count = 1; count <= most && (count == 1 || count * 4 <= steps); ++count) {
         const int64_t each = std::max<int64_t>(ceil_div(steps, count), 1), parts = std::max<int64_t>(ceil_div(steps, each), 1);
-        double us = static_cast<double>(ceil_div(tiles * parts, kSMs)) * (each * 0.3 + 3.0);
+        double us = static_cast<double>(ceil_div(tiles * parts, kSMs)) * (each * 0.36 + 3.0);
         if (parts > 1) us += 3.0 + 2e-6 * parts * outputs;
         if (count == 1 || us < least) least = us, best = {static_cast<int>(parts), static_cast<int>(each)};
     }
@@ -485,6 +490,7 @@ Splits splits_of(int64_t tiles, int64_t steps, int64_t outputs) {
 struct Plan {
     int planes, segments;
     int64_t x_copy, weight_copy;       // bytes of the copies that the tensor copies read; 0: in place
+    int64_t weight_columns;            // the same in the backward pass, which takes weight by whole groups of columns too
     int64_t parts, chosen;             // forward
     int words, pieces;                 // of a piece, and how many
     int64_t pitch, d;                  // of d, and its bytes
@@ -506,6 +512,7 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
     const int64_t pitch = pitch_of(D), packed = padded(p.planes * W * M * pitch * 2);
     p.x_copy = in_place(x, x_worker, x_row, dtype, W, M, D) ? 0 : packed;
     p.weight_copy = in_place(weight, weight_worker, weight_row, dtype, W, V, D) ? 0 : padded(p.planes * W * (int64_t)V * pitch * 2);
+    p.weight_columns = p.weight_copy || D % 64 == 0 ? p.weight_copy : padded(W * (int64_t)V * pitch * 2);
     const int64_t rows = W * M;
     p.parts = padded(ceil_div(V, kTileB) * 2 * rows * 8);
     p.chosen = padded(rows * 4);
@@ -516,13 +523,13 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
     p.words = static_cast<int>(std::min<int64_t>(ceil_div(ceil_div(V, p.pieces), kTileB) * kTileB, ceil_div(V, kTileB) * kTileB));
     p.pieces = static_cast<int>(ceil_div(V, p.words));
     p.pitch = pitch_of(std::min(p.words, V));
-    p.d = padded(p.planes * rows * p.pitch * 2);
+    p.d = padded(p.planes * rows * p.pitch * 2) + 16;  // room to begin at 32 bytes
     const int64_t tiles_d = ceil_div(D, kTileA);
     p.dx = splits_of(W * tiles_d * ceil_div(M, kTileB), ceil_div(std::min(p.words, V), kStep) * p.segments, rows * D);
     p.dweight = splits_of(W * tiles_d * ceil_div(std::min(p.words, V), kTileB), ceil_div(M, kStep) * p.segments, (int64_t)W * std::min(p.words, V) * D);
     p.dx_parts = p.dx.count > 1 || p.pieces > 1 ? padded(p.dx.count * rows * D * 4) : 0;
     p.dweight_parts = p.dweight.count > 1 ? padded((int64_t)p.dweight.count * W * std::min(p.words, V) * D * 4) : 0;
-    p.backward = packed + p.weight_copy + p.d + p.dx_parts + p.dweight_parts;
+    p.backward = packed + p.weight_columns + p.d + p.dx_parts + p.dweight_parts;
     return p;
 }
 
@@ -538,6 +545,24 @@ cpdp_status encode(CUtensorMap* map, const void* p, int64_t columns, int64_t row
                      strides[3] = {(cuuint64_t)row * 2, (cuuint64_t)worker * 2, (cuuint64_t)plane * 2};
     const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
     const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return layer_error(CPDP_ECUDA, "cuTensorMapEncodeTiled: error %d", (int)r);
+    return CPDP_OK;
+}
+
+// The same by groups of 64 columns, of which a box takes `box_columns` in kStep rows. What lies beside the columns of a
+// last, partial group is read, and must be there; no product that is kept uses it.
+cpdp_status encode_columns(CUtensorMap* map, const void* p, int64_t columns, int64_t rows, int W, int planes, int64_t row, int64_t worker,
+                           int64_t plane, int box_columns) {
+    const EncodeTiled f = encode_tiled();
+    if (f == nullptr) return layer_error(CPDP_ECUDA, "the CUDA driver has no cuTensorMapEncodeTiled");
+    if (rows <= 1) row = pitch_of(columns);
+    if (W <= 1) worker = row * rows;
+    if (planes <= 1) plane = worker * W;
+    const cuuint64_t dims[5] = {64, (cuuint64_t)rows, (cuuint64_t)ceil_div(columns, 64), (cuuint64_t)W, (cuuint64_t)planes},
+                     strides[4] = {(cuuint64_t)row * 2, 128, (cuuint64_t)worker * 2, (cuuint64_t)plane * 2};
+    const cuuint32_t box[5] = {64, kStep, (cuuint32_t)box_columns / 64, 1, 1}, one[5] = {1, 1, 1, 1, 1};
+    const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return layer_error(CPDP_ECUDA, "cuTensorMapEncodeTiled: error %d", (int)r);
     return CPDP_OK;
@@ -704,25 +729,25 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
     const Where xs{at, M * pitch, pitch, rows * pitch};
     at += padded(plan.planes * rows * pitch * 2);
     Where ws{weight, weight_worker, weight_row, 0};
-    if (plan.weight_copy) {
+    if (plan.weight_columns) {
         CPDP_TRY(pack(weight, weight_worker, weight_row, dtype, W, V, D, nullptr, at, stream, what));
         ws = {at, V * pitch, pitch, (int64_t)W * V * pitch};
-        at += plan.weight_copy;
+        at += plan.weight_columns;
     }
-    auto* d = reinterpret_cast<__nv_bfloat16*>(at);
+    auto* d = reinterpret_cast<__nv_bfloat16*>((reinterpret_cast<uintptr_t>(at) + 31) & ~uintptr_t(31));
     auto* dx_parts = reinterpret_cast<float*>(at + plan.d);
     auto* dweight_parts = reinterpret_cast<float*>(at + plan.d + plan.dx_parts);
 
     CUtensorMap x_rows, x_columns, w_rows, w_columns, d_rows, d_columns;
     CPDP_TRY(encode(&x_rows, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
-    CPDP_TRY(encode(&x_columns, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kStep));
+    CPDP_TRY(encode_columns(&x_columns, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
     CPDP_TRY(encode(&w_rows, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileB));
-    CPDP_TRY(encode(&w_columns, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kStep));
+    CPDP_TRY(encode_columns(&w_columns, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileA));
     for (int piece = 0; piece < plan.pieces; ++piece) {
         const int first = piece * plan.words, words = std::min(plan.words, V - first);
         const int64_t plane = rows * plan.pitch;
         CPDP_TRY(encode(&d_rows, d, words, M, W, plan.planes, plan.pitch, M * plan.pitch, plane, kTileB));
-        CPDP_TRY(encode(&d_columns, d, words, M, W, plan.planes, plan.pitch, M * plan.pitch, plane, kStep));
+        CPDP_TRY(encode_columns(&d_columns, d, words, M, W, plan.planes, plan.pitch, M * plan.pitch, plane, kTileB));
         Product p = product(W, M, words, D, plan.segments);
         p.b_at = first;
         const auto gradients = [&](auto planes) {
