@@ -7,18 +7,6 @@
 #include "cpdp_gates.cuh"
 #include "cpdp_sums.cuh"
 
-#ifndef BB
-#define BB 3
-#endif
-#ifndef FC
-#define FC 4
-#endif
-#ifndef FB
-#define FB 12
-#endif
-#ifndef FU
-#define FU 4
-#endif
 namespace cpdp {
 namespace {
 
@@ -39,8 +27,8 @@ struct Shape {
 };
 constexpr int R = CPDP_CARRY_STEPS;
 constexpr int kBackwardWarps = 4;  // of a block of the backward pass, at most
-constexpr int kAtOnce = FU;
-constexpr int kForwardBlocks = FB, kBackwardBlocks = BB;  // per SM
+constexpr int kAtOnce = 4;  // steps of the forward walk
+constexpr int kForwardBlocks = 12, kBackwardBlocks = 3;  // per SM
 constexpr float kLn2f = kLn2;
 
 struct Rows {
@@ -989,10 +977,12 @@ cpdp_status check_scan(int W, int B, int64_t T, int D, int N, cpdp_dtype dtype) 
     return CPDP_OK;
 }
 
-template <typename F>
-auto with_shape(bool backward, int N, F&& f) {
-    if (backward) return N <= 8 ? f(Shape<2, 2>{}) : N <= 16 ? f(Shape<4, 2>{}) : f(Shape<8, 2>{});
-    return N <= 8 ? f(Shape<2, 2>{}) : N <= 16 ? f(Shape<4, FC>{}) : f(Shape<8, FC>{});
+template <bool BACKWARD, typename F>
+auto with_shape(int N, F&& f) {
+    if constexpr (BACKWARD)
+        return N <= 8 ? f(Shape<2, 2>{}) : N <= 16 ? f(Shape<4, 2>{}) : f(Shape<8, 2>{});
+    else
+        return N <= 8 ? f(Shape<2, 2>{}) : N <= 16 ? f(Shape<4, 4>{}) : f(Shape<8, 4>{});
 }
 
 struct Plan {
@@ -1004,7 +994,8 @@ struct Plan {
 // `warps`: as many as run at once on the GPU.
 Plan plan_of(int B, int64_t T, int D, int N, int64_t warps, bool backward) {
     Plan p{};
-    const int pairs = with_shape(backward, N, [&](auto x) { return p.column = decltype(x)::kColumn, p.states = decltype(x)::kStates, decltype(x)::P; });
+    const auto shaped = [&](auto x) { return p.column = decltype(x)::kColumn, p.states = decltype(x)::kStates, decltype(x)::P; };
+    const int pairs = backward ? with_shape<true>(N, shaped) : with_shape<false>(N, shaped);
     p.groups = static_cast<int>(ceil_div(D, p.column));
     const int64_t columns = (int64_t)B * p.groups;
     int64_t count = columns * 3 <= warps ? warps / std::max<int64_t>(columns, 1) : 1;
@@ -1094,7 +1085,7 @@ cpdp_status cpdp_selective_scan(const cpdp_scan_inputs* inputs, cpdp_dtype dtype
     const auto go = [&](auto* out, auto two) {
         using E = std::remove_pointer_t<decltype(out)>;
         constexpr bool WIDE = decltype(two)::value;
-        return with_shape(false, N, [&](auto shape) {
+        return with_shape<false>(N, [&](auto shape) {
             using X = decltype(shape);
             if (plan.count > 1) {
                 const cudaError_t first = launch_layer(scan_kernel<E, WIDE, true, X>, blocks, 32, 0, stream, s, h0, out, last, carry, quads);
@@ -1153,7 +1144,7 @@ cpdp_status cpdp_selective_scan_backward(const void* dy, int64_t dy_seq, int64_t
     const auto go = [&](auto* out, auto two) {
         using E = std::remove_pointer_t<decltype(out)>;
         constexpr bool WIDE = decltype(two)::value;
-        return with_shape(true, N, [&](auto shape) {
+        return with_shape<true>(N, [&](auto shape) {
             using X = decltype(shape);
             if (plan.count > 1) {
                 const cudaError_t first = launch_layer(scan_backward_maps_kernel<E, WIDE, X>, static_cast<unsigned>((int64_t)B * plan.groups * plan.count),
@@ -1192,7 +1183,7 @@ cpdp_status cpdp_selective_scan_step(const cpdp_scan_inputs* inputs, cpdp_dtype 
     if (B == 0) return CPDP_OK;
     const auto go = [&](auto* out) {
         using E = std::remove_pointer_t<decltype(out)>;
-        return with_shape(false, N, [&](auto shape) {
+        return with_shape<false>(N, [&](auto shape) {
             constexpr int S = decltype(shape)::S;
             return launch_layer(scan_step_kernel<E, S>, static_cast<unsigned>(ceil_div((int64_t)B * D * S, 128)), 128, 0, stream, s, state, out);
         });
