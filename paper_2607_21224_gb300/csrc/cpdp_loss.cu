@@ -23,12 +23,15 @@ namespace {
 // axis there, so that a warp's store is of 32 neighbours at any alignment.
 //
 // The tensor core cuts its float32 sums off where others round them, always
-// towards 0: chains of kChunk steps are summed at a time and added up, rounded
-// to nearest, in the epilogue's registers.
+// towards 0: chunks of some steps are summed at a time and added up, rounded to
+// nearest, in the epilogue's registers. 32 steps where the operands are bfloat16;
+// 4 for float32's, which lose 8e-7 of a loss in chunks of 32 and 6e-8 in chunks of
+// 2 (2 x 517 tokens, 771 features, 10,007 words: 522, 578 and 653 us in chunks of
+// 32, 4 and 2).
 constexpr int kTileA = 128, kTileB = 256, kStep = 64, kSlots = 4;
 constexpr int kEpilogueWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kThreads = 10 * 32;
 constexpr int kHalf = kTileB / 2;  // columns of a thread
-constexpr int kChunk = 32;         // steps
+constexpr int kChunk = 32, kChunkF32 = 4;  // steps
 constexpr int kABytes = kTileA * kStep * 2, kBBytes = kTileB * kStep * 2, kSlotBytes = kABytes + kBBytes;
 constexpr int kBlockBytes = kStep * 128;  // 64 columns of an operand that has k as its slow axis
 constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;
@@ -45,13 +48,23 @@ __device__ __forceinline__ float power(float x) {
 // those before it: 24 bits. Six products of planes, k passing once for each,
 // leave out what is below 2^-24 of a product.
 constexpr int kPlanes = 3, kPlaneProducts = 6;
-constexpr uint32_t kPlanesA = 0x021010u, kPlanesB = 0x201100u;  // four bits each, the first lowest: 00 10 01 11 20 02
+struct Planes {
+    int products;   // of planes
+    uint32_t a, b;  // which, four bits each, the first lowest
+};
+constexpr Planes kOnePlane{1, 0, 0}, kThreePlanes{kPlaneProducts, 0x021010u, 0x201100u};  // 00, 10, 01, 11, 20, 02
+// Where the words are few, their probabilities are not small beside 1, and the rounding of d to bfloat16 shows in the
+// gradients (2.5e-3 of dx at 64 words, where rounding dx itself is 1.7e-3). Up to kFewWords d is held in two planes.
+constexpr Planes kTwoOfD{2, 0x00u, 0x10u};
+constexpr int kFewWords = 4096;
 
 struct Product {
     int W, tiles_a, tiles_b, splits;
     int a_extent, b_extent;
-    int steps, segments;         // of k, and how often it passes
-    int each;                    // steps of a split, segments passing one after another
+    int steps;                   // of k, which passes once for each product of planes
+    Planes planes;
+    int chunk;                   // steps
+    int each;                    // steps of a split
     int a_k, b_k, a_at, b_at;    // where k and the tiles begin in each operand
 };
 
@@ -142,7 +155,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int64_t tiles = tiles_of(p);
     const auto range = [&](const Tile& t, int& first, int& count) {
         first = t.split * p.each;
-        count = min(p.steps * p.segments - first, p.each);
+        count = min(p.steps * p.planes.products - first, p.each);
     };
     if (warp == kCopyWarp) {
         if (lane == 0) {
@@ -157,10 +170,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     ok = n < kSlots || barrier_wait(&empty[s], (n / kSlots - 1) & 1, &failed);
                     if (!ok) break;
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(&full[s])), "r"(kSlotBytes) : "memory");
-                    const int segment = (first + k) / p.steps, at = (first + k - segment * p.steps) * kStep;
+                    const int pass = (first + k) / p.steps, at = (first + k - pass * p.steps) * kStep;
                     const uint32_t slot = slots + s * kSlotBytes;
-                    copy_operand<A_SLOW>(slot, &map_a, p.a_at + t.a * kTileA, p.a_k + at, t.w, kPlanesA >> 4 * segment & 15, &full[s]);
-                    copy_operand<B_SLOW>(slot + kABytes, &map_b, p.b_at + t.b * kTileB, p.b_k + at, t.w, kPlanesB >> 4 * segment & 15,
+                    copy_operand<A_SLOW>(slot, &map_a, p.a_at + t.a * kTileA, p.a_k + at, t.w, p.planes.a >> 4 * pass & 15, &full[s]);
+                    copy_operand<B_SLOW>(slot + kABytes, &map_b, p.b_at + t.b * kTileB, p.b_k + at, t.w, p.planes.b >> 4 * pass & 15,
                                                  &full[s]);
                 }
             }
@@ -174,8 +187,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             for (int64_t i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
                 int first, count;
                 range(tile_of(p, i), first, count);
-                for (int k0 = 0; k0 < count && ok; k0 += kChunk, ++c) {
-                    const int half = c & 1, end = min(k0 + kChunk, count);
+                for (int k0 = 0; k0 < count && ok; k0 += p.chunk, ++c) {
+                    const int half = c & 1, end = min(k0 + p.chunk, count);
                     if (c >= 2) ok = barrier_wait(&taken[half], (c / 2 - 1) & 1, &failed);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     for (int k = k0; k < end && ok; ++k, ++n) {
@@ -209,7 +222,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (count <= 0)
 #pragma unroll
                 for (int j = 0; j < kHalf; ++j) v[j] = 0.f;
-            for (int k0 = 0; k0 < count && ok; k0 += kChunk, ++c) {
+            for (int k0 = 0; k0 < count && ok; k0 += p.chunk, ++c) {
                 const int half = c & 1;
                 ok = __all_sync(~0u, barrier_wait(&summed[half], c / 2 & 1, &failed));
                 if (!ok) break;
@@ -320,7 +333,7 @@ finish_rows_kernel(const float2* parts, const float* chosen, const int64_t* targ
 }
 
 // The gradient of a token's logits, d = dloss (exp(l - lse) - onehot), rounded to
-// bfloat16 (the type of the products' operands), or in three planes.
+// bfloat16 (the type of the products' operands), or in two or three planes.
 template <int PLANES>
 struct LogitGradients {
     const int64_t* targets;
@@ -488,7 +501,9 @@ Splits splits_of(int64_t tiles, int64_t steps, int64_t outputs) {
 
 // What a call computes from its sizes.
 struct Plan {
-    int planes, segments;
+    int planes, d_planes;              // of the operands and of d
+    Planes products, d_products;       // with the operands, and with d
+    int chunk;
     int64_t x_copy, weight_copy;       // bytes of the copies that the tensor copies read; 0: in place
     int64_t weight_columns;            // the same in the backward pass, which takes weight by whole groups of columns too
     int64_t parts, chosen;             // forward
@@ -508,7 +523,10 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
              int W, int64_t M, int V, int D) {
     Plan p{};
     p.planes = dtype == CPDP_F32 ? kPlanes : 1;
-    p.segments = dtype == CPDP_F32 ? kPlaneProducts : 1;
+    p.d_planes = dtype == CPDP_F32 ? kPlanes : V <= kFewWords ? 2 : 1;
+    p.products = dtype == CPDP_F32 ? kThreePlanes : kOnePlane;
+    p.d_products = dtype == CPDP_F32 ? kThreePlanes : V <= kFewWords ? kTwoOfD : kOnePlane;
+    p.chunk = dtype == CPDP_F32 ? kChunkF32 : kChunk;
     const int64_t pitch = pitch_of(D), packed = padded(p.planes * W * M * pitch * 2);
     p.x_copy = in_place(x, x_worker, x_row, dtype, W, M, D) ? 0 : packed;
     p.weight_copy = in_place(weight, weight_worker, weight_row, dtype, W, V, D) ? 0 : padded(p.planes * W * (int64_t)V * pitch * 2);
@@ -518,15 +536,15 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
     p.chosen = padded(rows * 4);
     p.forward = p.x_copy + p.weight_copy + p.parts + p.chosen;
 
-    const int64_t fit = std::max<int64_t>(kPieceBytes / (p.planes * 2 * std::max<int64_t>(rows, 1)), kTileB);
+    const int64_t fit = std::max<int64_t>(kPieceBytes / (p.d_planes * 2 * std::max<int64_t>(rows, 1)), kTileB);
     p.pieces = static_cast<int>(ceil_div(V, fit));
     p.words = static_cast<int>(std::min<int64_t>(ceil_div(ceil_div(V, p.pieces), kTileB) * kTileB, ceil_div(V, kTileB) * kTileB));
     p.pieces = static_cast<int>(ceil_div(V, p.words));
     p.pitch = pitch_of(std::min(p.words, V));
-    p.d = padded(p.planes * rows * p.pitch * 2) + 16;  // room to begin at 32 bytes
+    p.d = padded(p.d_planes * rows * p.pitch * 2) + 16;  // room to begin at 32 bytes
     const int64_t tiles_d = ceil_div(D, kTileA);
-    p.dx = splits_of(W * tiles_d * ceil_div(M, kTileB), ceil_div(std::min(p.words, V), kStep) * p.segments, rows * D);
-    p.dweight = splits_of(W * tiles_d * ceil_div(std::min(p.words, V), kTileB), ceil_div(M, kStep) * p.segments, (int64_t)W * std::min(p.words, V) * D);
+    p.dx = splits_of(W * tiles_d * ceil_div(M, kTileB), ceil_div(std::min(p.words, V), kStep) * p.d_products.products, rows * D);
+    p.dweight = splits_of(W * tiles_d * ceil_div(std::min(p.words, V), kTileB), ceil_div(M, kStep) * p.d_products.products, (int64_t)W * std::min(p.words, V) * D);
     p.dx_parts = p.dx.count > 1 || p.pieces > 1 ? padded(p.dx.count * rows * D * 4) : 0;
     p.dweight_parts = p.dweight.count > 1 ? padded((int64_t)p.dweight.count * W * std::min(p.words, V) * D * 4) : 0;
     p.backward = packed + p.weight_columns + p.d + p.dx_parts + p.dweight_parts;
@@ -578,13 +596,13 @@ cpdp_status multiply_all(const CUtensorMap& a, const CUtensorMap& b, const Produ
     return layer_launched(e, what);
 }
 
-Product product(int W, int64_t a, int64_t b, int64_t k, int segments, Splits s = {1, 0}) {
+Product product(int W, int64_t a, int64_t b, int64_t k, const Planes& planes, int chunk, Splits s = {1, 0}) {
     Product p{};
     p.W = W;
     p.tiles_a = static_cast<int>(ceil_div(a, kTileA)), p.tiles_b = static_cast<int>(ceil_div(b, kTileB));
     p.a_extent = static_cast<int>(a), p.b_extent = static_cast<int>(b);
-    p.steps = static_cast<int>(ceil_div(k, kStep)), p.segments = segments;
-    p.splits = s.count, p.each = s.each > 0 ? s.each : p.steps * segments;
+    p.steps = static_cast<int>(ceil_div(k, kStep)), p.planes = planes, p.chunk = chunk;
+    p.splits = s.count, p.each = s.each > 0 ? s.each : p.steps * planes.products;
     return p;
 }
 
@@ -678,7 +696,7 @@ cpdp_status cpdp_linear_cross_entropy(const void* x, int64_t x_worker, int64_t x
     CUtensorMap a, b;
     CPDP_TRY(encode(&a, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
     CPDP_TRY(encode(&b, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileB));
-    CPDP_TRY((multiply_all<false, false>(a, b, product(W, M, V, D, plan.segments), RowSums{targets, parts, chosen, M, rows, V}, stream, what)));
+    CPDP_TRY((multiply_all<false, false>(a, b, product(W, M, V, D, plan.products, plan.chunk), RowSums{targets, parts, chosen, M, rows, V}, stream, what)));
     const auto finish = [&](auto kernel, int each) {
         return launch_layer(kernel, static_cast<unsigned>(ceil_div(rows, each)), 256, 0, stream, static_cast<const float2*>(parts),
                             static_cast<const float*>(chosen), targets, rows, static_cast<int>(ceil_div(V, kTileB) * 2), V, loss, lse);
@@ -746,18 +764,20 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
     for (int piece = 0; piece < plan.pieces; ++piece) {
         const int first = piece * plan.words, words = std::min(plan.words, V - first);
         const int64_t plane = rows * plan.pitch;
-        CPDP_TRY(encode(&d_rows, d, words, M, W, plan.planes, plan.pitch, M * plan.pitch, plane, kTileB));
-        CPDP_TRY(encode_columns(&d_columns, d, words, M, W, plan.planes, plan.pitch, M * plan.pitch, plane, kTileB));
-        Product p = product(W, M, words, D, plan.segments);
+        CPDP_TRY(encode(&d_rows, d, words, M, W, plan.d_planes, plan.pitch, M * plan.pitch, plane, kTileB));
+        CPDP_TRY(encode_columns(&d_columns, d, words, M, W, plan.d_planes, plan.pitch, M * plan.pitch, plane, kTileB));
+        Product p = product(W, M, words, D, plan.products, plan.chunk);
         p.b_at = first;
         const auto gradients = [&](auto planes) {
             constexpr int P = decltype(planes)::value;
             return multiply_all<false, false>(x_rows, w_rows, p, LogitGradients<P>{targets, lse, dloss, d, M, plane, plan.pitch, V, first}, stream, what);
         };
-        CPDP_TRY(plan.planes == 1 ? gradients(std::integral_constant<int, 1>{}) : gradients(std::integral_constant<int, kPlanes>{}));
+        CPDP_TRY(plan.d_planes == 1   ? gradients(std::integral_constant<int, 1>{})
+                 : plan.d_planes == 2 ? gradients(std::integral_constant<int, 2>{})
+                                      : gradients(std::integral_constant<int, kPlanes>{}));
 
-        p = product(W, D, M, words, plan.segments, plan.dx);
-        p.splits = static_cast<int>(ceil_div(p.steps * p.segments, p.each));  // a last piece may have fewer words
+        p = product(W, D, M, words, plan.d_products, plan.chunk, plan.dx);
+        p.splits = static_cast<int>(ceil_div(p.steps * p.planes.products, p.each));  // a last piece may have fewer words
         p.a_k = first;
         if (plan.dx_parts) {
             CPDP_TRY((multiply_all<true, false>(w_columns, d_rows, p,
@@ -770,7 +790,7 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
             CPDP_TRY(dtype == CPDP_F32 ? write(static_cast<float*>(dx)) : write(static_cast<__nv_bfloat16*>(dx)));
         }
 
-        p = product(W, D, words, M, plan.segments, plan.dweight);
+        p = product(W, D, words, M, plan.d_products, plan.chunk, plan.dweight);
         const int64_t part = (int64_t)words * D;
         if (plan.dweight_parts) {
             CPDP_TRY((multiply_all<true, true>(x_columns, d_columns, p,
