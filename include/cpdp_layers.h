@@ -211,7 +211,8 @@ cpdp_status cpdp_gated_recurrence_step(const void *gate, int64_t gate_seq, const
  * The logits are float32 sums and stay on the chip. float32 operands are split
  * into three bfloat16 parts each, and products below 2^-24 of the largest part's
  * are left out; an infinite operand gives NaN there where the formula has an
- * infinity. W * V and the elements of [W][M][V] are bounded as those of an array.
+ * infinity. M and V are at most 2^30; W * V and the elements of [W][M][V] are
+ * bounded as those of an array.
  */
 size_t cpdp_linear_cross_entropy_workspace(const void *x, int64_t x_worker, int64_t x_row,
                                            const void *weight, int64_t weight_worker, int64_t weight_row,
@@ -367,7 +368,8 @@ typedef struct cpdp_scan_inputs {
  *            before steps 0, CPDP_CARRY_STEPS, ..., for the backward pass
  *            (defined up to each sequence's length)
  * States and sums are float32. A decay x = exp(-p) is off by at most
- * (2 + 2 p) 2^-23 of it. B * T * D is at most 2^34.
+ * (2 + 2 p) 2^-23 of it. Where dt, u, z, b or c is infinite, an output may be NaN
+ * that the formula has infinite. B * T * D is at most 2^34.
  */
 size_t cpdp_selective_scan_workspace(int B, int64_t T, int D, int N);
 cpdp_status cpdp_selective_scan(const cpdp_scan_inputs *inputs, cpdp_dtype dtype, int W, int B, int64_t T, int D, int N,
@@ -409,7 +411,8 @@ cpdp_status cpdp_selective_scan_step(const cpdp_scan_inputs *inputs, cpdp_dtype 
  * cpdp_layer_timeouts — the number of bounded waits that ran out since the last
  * call (0 expected): the warps of the weight gradient and of the loss wait for
  * the slots of a ring, for some seconds at most. A block in which one ran out
- * writes NaN for all of its tiles. Waits for the device.
+ * writes NaN: the weight gradient's for all of its tile of dW, the loss's for the
+ * tile at hand and those that it would have come to. Waits for the device.
  */
 cpdp_status cpdp_layer_timeouts(int64_t *count);
 

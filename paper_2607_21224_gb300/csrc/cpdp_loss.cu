@@ -58,6 +58,11 @@ constexpr Planes kOnePlane{1, 0, 0}, kThreePlanes{kPlaneProducts, 0x021010u, 0x2
 constexpr Planes kTwoOfD{2, 0x00u, 0x10u};
 constexpr int kFewWords = 4096;
 
+#ifdef CPDP_CHECKED
+// A block's step that is never copied, so that waits run out; -1: none. Debug build only.
+__device__ int dropped_step = -1;
+#endif
+
 struct Product {
     int W, tiles_a, tiles_b, splits;
     int a_extent, b_extent;
@@ -169,6 +174,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     const int s = static_cast<int>(n % kSlots);
                     ok = n < kSlots || barrier_wait(&empty[s], (n / kSlots - 1) & 1, &failed);
                     if (!ok) break;
+#ifdef CPDP_CHECKED
+                    if (n == *static_cast<volatile int*>(&dropped_step)) continue;
+#endif
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(&full[s])), "r"(kSlotBytes) : "memory");
                     const int pass = (first + k) / p.steps, at = (first + k - pass * p.steps) * kStep;
                     const uint32_t slot = slots + s * kSlotBytes;
@@ -626,13 +634,20 @@ cpdp_status check_loss(const void* x, int64_t x_worker, int64_t x_row, const voi
     CPDP_TRY(check_sizes(W, V, D));
     CPDP_TRY(check_sizes(W, M, V));
     if (!known_dtype(dtype)) return layer_error(CPDP_EINVAL, "unknown dtype %d", (int)dtype);
-    if (V < 1) return layer_error(CPDP_EINVAL, "V=%d must be at least 1", V);
+    if (V < 1 || V > kLayerMaxFeatures || M > kLayerMaxFeatures)
+        return layer_error(CPDP_EINVAL, "V=%d must be in [1, 2^30] and M=%lld at most 2^30", V, (long long)M);
     CPDP_TRY(check_array("x", x, M > 0, dtype_size(dtype), x_worker, x_row));
     CPDP_TRY(check_array("weight", weight, true, dtype_size(dtype), weight_worker, weight_row));
     return check_array("targets", targets, M > 0, 8);
 }
 
 }  // namespace
+
+#ifdef CPDP_CHECKED
+extern "C" cpdp_status cpdp_layer_drop_loss_step(int step) {
+    return layer_launched(cudaMemcpyToSymbol(dropped_step, &step, sizeof step), "cpdp_layer_drop_loss_step");
+}
+#endif
 
 cudaError_t take_loss_timeouts(unsigned long long* count) {
     unsigned long long zero = 0;
@@ -646,7 +661,8 @@ cudaError_t take_loss_timeouts(unsigned long long* count) {
 using namespace cpdp;
 
 static bool loss_sizes(int W, int64_t M, int V, int D) {
-    return check_sizes(W, M, D) == CPDP_OK && check_sizes(W, V, D) == CPDP_OK && check_sizes(W, M, V) == CPDP_OK && V >= 1;
+    return check_sizes(W, M, D) == CPDP_OK && check_sizes(W, V, D) == CPDP_OK && check_sizes(W, M, V) == CPDP_OK && V >= 1 &&
+           V <= kLayerMaxFeatures && M <= kLayerMaxFeatures;
 }
 
 size_t cpdp_linear_cross_entropy_workspace(const void* x, int64_t x_worker, int64_t x_row, const void* weight, int64_t weight_worker,
