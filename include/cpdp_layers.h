@@ -255,7 +255,8 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float *dloss, const void *x
  *             the sizes and the rows' alignment, and neither overflows nor
  *             vanishes where the norm itself is a float32 number.
  *   out       of dtype, with a worker stride; or grads itself, with the same
- *             stride: rows whose norm is not above max_norm are not written then
+ *             stride: rows whose norm is not above max_norm are not written then.
+ *             Other rows that overlap those of grads are refused.
  * A row with an infinite value has the norm infinity (0 for the finite values, NaN
  * for the infinite ones), one with a NaN is NaN throughout. W * N is at most 2^40;
  * with N = 0 the norms are 0.

@@ -174,6 +174,17 @@ cpdp_status check_clip(int W, int64_t N) {
     return CPDP_OK;
 }
 
+// Whether rows of `size` bytes at a and at b overlap, where they are not the same ones. Rows of one stride may lie between
+// each other.
+bool rows_meet(uintptr_t a, int64_t a_stride, uintptr_t b, int64_t b_stride, int W, int64_t size) {
+    if (size == 0 || a == b) return false;
+    const int64_t a_span = (W - 1) * a_stride + size, b_span = (W - 1) * b_stride + size;
+    if (a + a_span <= b || b + b_span <= a) return false;
+    if (W == 1 || a_stride != b_stride) return true;
+    const int64_t after = a < b ? (b - a) % a_stride : a_stride - (a - b) % a_stride;  // from a row of a to the next one of b
+    return after < size || after > a_stride - size;
+}
+
 }  // namespace
 }  // namespace cpdp
 
@@ -195,6 +206,8 @@ cpdp_status cpdp_clip_gradients(const void* grads, int64_t grads_worker, cpdp_dt
     CPDP_TRY(check_apart("out", W, out_worker, N));
     if (out == grads && W > 1 && out_worker != grads_worker)
         return layer_error(CPDP_EINVAL, "out is grads with another stride: %lld, not %lld", (long long)out_worker, (long long)grads_worker);
+    if (rows_meet(reinterpret_cast<uintptr_t>(grads), grads_worker * e, reinterpret_cast<uintptr_t>(out), out_worker * e, W, N * e))
+        return layer_error(CPDP_EINVAL, "rows of out (%p) overlap rows of grads (%p) and are not the same", out, grads);
     CPDP_TRY(check_workspace(workspace, workspace_bytes, cpdp_clip_gradients_workspace(W, N)));
     auto* parts = static_cast<Squares*>(workspace);
     const bool aligned = (reinterpret_cast<uintptr_t>(grads) - reinterpret_cast<uintptr_t>(out)) % 16 == 0 &&

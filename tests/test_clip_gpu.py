@@ -84,6 +84,21 @@ def test_large_rows_one_model_no_values_and_repeats():
     assert torch.equal(same, same[:1].expand(4))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("first,second", [(0, 1000), (1000, 0), (3, 1003)])
+def test_rows_between_those_of_the_gradients(first, second, dtype):
+    long = normal(rng(5), 3, 2003).to(dtype).cuda()
+    grads, out = long[:, first:first + 1000], long[:, second:second + 1000]
+    want = torch.empty(3, 1000, dtype=dtype, device="cuda")
+    norms = layers.clip_gradients(grads.clone(), 1.0, out=want)
+    before = grads.clone()
+    near(layers.clip_gradients(grads, 1.0, out=out), norms.double().cpu(), norms.double().cpu() * 1000 * 2.0 ** -24, F32)
+    assert torch.equal(grads, before)
+    near(out, want.double().cpu(), want.double().cpu().abs() * (1000 * 2.0 ** -24 + torch.finfo(dtype).eps / 2))
+    with pytest.raises(cpdp.CPDPError):
+        layers.clip_gradients(grads, 1.0, out=long[:, first + 1:first + 1001])
+
+
 def test_streams_and_graphs():
     g = torch.randn(2, 50000, device="cuda")
     out, other = torch.empty_like(g), torch.empty_like(g)

@@ -92,6 +92,22 @@ def test_an_output_that_is_the_input_with_another_stride_is_refused():
     assert layers._entry("cpdp_clip_gradients")(*arguments) == cpdp.CPDP_EINVAL
 
 
+@pytest.mark.parametrize("out,stride", [(P + 4 * k, 100) for k in (1, 99, 100, -1, -99, -100)] + [(P + 4 * 150, 160), (P - 4 * 150, 160)])
+def test_outputs_that_overlap_other_gradients_are_refused(out, stride):
+    arguments = list(GOOD["cpdp_clip_gradients"])
+    arguments[7:9] = out, stride
+    assert layers._entry("cpdp_clip_gradients")(*arguments) == cpdp.CPDP_EINVAL
+    assert "overlap" in cpdp.cpdp_last_error(None)
+
+
+@pytest.mark.parametrize("at,inner", [(50, 150), (150, 150), (-50, 150), (-150, 150), (50, 199), (-100, 199)])
+def test_outputs_that_cut_into_gradients_of_the_same_stride_are_refused(at, inner):
+    arguments = list(GOOD["cpdp_clip_gradients"])
+    arguments[1], arguments[7], arguments[8] = inner, P + 4 * at, inner
+    assert layers._entry("cpdp_clip_gradients")(*arguments) == cpdp.CPDP_EINVAL
+    assert "overlap" in cpdp.cpdp_last_error(None)
+
+
 def test_workspace_sizes():
     L = layers.lib()
     assert L.cpdp_linear_cross_entropy_workspace(P, 320, 32, P, 1600, 32, 0, 0, 10, 50, 32) == 0
