@@ -26,8 +26,8 @@ namespace {
 // towards 0: chunks of some steps are summed at a time and added up, rounded to
 // nearest, in the epilogue's registers. 32 steps where the operands are bfloat16;
 // 4 for float32's, which lose 8e-7 of a loss in chunks of 32 and 6e-8 in chunks of
-// 2 (2 x 517 tokens, 771 features, 10,007 words: 522, 578 and 653 us in chunks of
-// 32, 4 and 2).
+// 2 (2 x 517 tokens, 771 features, 10,007 words: 534 us in chunks of 4, 56 less in
+// chunks of 32 and 75 more in chunks of 2).
 constexpr int kTileA = 128, kTileB = 256, kStep = 64, kSlots = 4;
 constexpr int kEpilogueWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kThreads = 10 * 32;
 constexpr int kHalf = kTileB / 2;  // columns of a thread
@@ -412,34 +412,42 @@ struct WriteOut {
     }
 };
 
-// The sum of the splits' parts [split][W][rows][D], in their order; 0 in ignored tokens' rows.
-// A warp per row; V neighbouring elements per lane.
+// The sum of the splits' parts [split][W][rows][D], in their order; 0 in ignored tokens' rows. A warp per 128
+// neighbouring elements of a row, V of them together per lane: with a warp per row, 1,034 rows of 771 in 8 parts took
+// 51 us.
+constexpr int kSummed = 128;
 template <typename G, int V>
 __global__ void __launch_bounds__(256)
 sum_parts_kernel(const float* parts, int splits, int64_t rows_each, int64_t rows, int D, const int64_t* targets, G* out, int64_t worker) {
     layer_begin();
-    const int lane = threadIdx.x % 32;
-    const int64_t all = rows * D;
-    for (int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; r < rows; r += (int64_t)gridDim.x * 8) {
-        const int64_t w = r / rows_each;
+    constexpr int kPieces = kSummed / 32 / V;
+    const int lane = threadIdx.x % 32, chunks = (D + kSummed - 1) / kSummed;
+    const int64_t all = rows * D, tasks = rows * chunks;
+    for (int64_t task = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; task < tasks; task += (int64_t)gridDim.x * 8) {
+        const int64_t r = task / chunks, w = r / rows_each;
+        const int k0 = static_cast<int>(task - r * chunks) * kSummed + lane * V;
         const bool ignored = targets != nullptr && targets[r] < 0;
-        const float* p = parts + r * D;
-        G* to = out + w * worker + (r - w * rows_each) * D;
+        const float* p = parts + r * D + k0;
+        G* to = out + w * worker + (r - w * rows_each) * D + k0;
+        float s[kPieces][V] = {};
+        if (V == 1 || k0 < D)  // one piece per lane, or pieces that are loaded where they are there
 #pragma unroll 4
-        for (int k = lane * V; k < D; k += 32 * V) {
-            float s[V] = {};
-            for (int i = 0; i < splits; ++i) {
-                Piece<float, V> v{};
-                if constexpr (V == 1)
-                    v.load(p + i * all + k, true);
-                else
-                    v.load(p + i * all + k);
+            for (int i = 0; i < splits; ++i)
 #pragma unroll
-                for (int e = 0; e < V; ++e) s[e] += v.get(e);
-            }
+                for (int q = 0; q < kPieces; ++q) {
+                    Piece<float, V> v{};
+                    if constexpr (V == 1)
+                        v.load(p + i * all + q * 32, k0 + q * 32 < D);
+                    else
+                        v.load(p + i * all);
 #pragma unroll
-            for (int e = 0; e < V; ++e) s[e] = ignored ? 0.f : s[e];
-            store_piece<V>(to + k, s);
+                    for (int e = 0; e < V; ++e) s[q][e] += v.get(e);
+                }
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[q][e] = ignored ? 0.f : s[q][e];
+            if (k0 + q * 32 < D) store_piece<V>(to + q * 32, s[q]);
         }
     }
 }
@@ -724,7 +732,7 @@ cpdp_status cpdp_linear_cross_entropy(const void* x, int64_t x_worker, int64_t x
 template <typename G>
 static cudaError_t sum_parts(const float* parts, int splits, int64_t rows_each, int W, int D, const int64_t* targets, G* out, int64_t worker,
                              void* stream) {
-    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows_each * W, 8), kSMs * 8));
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(rows_each * W * ceil_div(D, kSummed), 8), kSMs * 8));
     const bool fours = D % 4 == 0 && aligned_to(out, 4 * sizeof(G)) && (W == 1 || worker % 4 == 0);
     return launch_layer(fours ? sum_parts_kernel<G, 4> : sum_parts_kernel<G, 1>, blocks, 256, 0, stream, parts, splits, rows_each, rows_each * W, D,
                         targets, out, worker);

@@ -19,8 +19,7 @@ namespace {
 //
 // Chunks of R steps: their inputs are taken by lanes side by side along the
 // channels, two neighbours each, which make dt and dt u; these go through shared
-// memory to the walk and the walk's sums back. What the walk needs of b and c
-// lies there twice, for the pairs.
+// memory to the walk and the walk's sums back.
 template <int S_, int C_>
 struct Shape {
     static constexpr int S = S_, C = C_, P = C / 2, kColumn = 32 / S * C, kStates = 4 * S;
