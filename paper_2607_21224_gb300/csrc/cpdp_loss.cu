@@ -340,12 +340,34 @@ finish_rows_kernel(const float2* parts, const float* chosen, const int64_t* targ
     }
 }
 
+// What a worker's dloss are measured in where d is one plane: the largest of them. 1 / M for each token, a mean's, would
+// be off by up to 2^-9 in bfloat16, all gradients by the same factor; in units of itself it is 1.
+__global__ void __launch_bounds__(1024)
+unit_kernel(const float* dloss, const int64_t* targets, int64_t M, float* unit) {
+    layer_begin();
+    __shared__ float warps[32];
+    float most = 0.f;
+    for (int64_t i = threadIdx.x; i < M; i += 1024) {
+        const float size = fabsf(dloss[blockIdx.x * M + i]);
+        if (targets[blockIdx.x * M + i] >= 0 && isfinite(size)) most = fmaxf(most, size);
+    }
+#pragma unroll
+    for (int k = 16; k > 0; k /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, k));
+    if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = most;
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    for (int k = 0; k < 32; ++k) most = fmaxf(most, warps[k]);
+    unit[blockIdx.x] = most > 0.f ? most : 1.f;
+}
+
 // The gradient of a token's logits, d = dloss (exp(l - lse) - onehot), rounded to
-// bfloat16 (the type of the products' operands), or in two or three planes.
+// bfloat16 (the type of the products' operands) in units of the worker's, or in
+// two or three planes.
 template <int PLANES>
 struct LogitGradients {
     const int64_t* targets;
     const float *lse, *dloss;
+    const float* unit;  // [W]; NULL: 1
     __nv_bfloat16* d;  // [plane][W][M][pitch]
     int64_t M, plane, pitch;
     int V, first;      // the piece's first word
@@ -353,7 +375,7 @@ struct LogitGradients {
         if (a >= M) return;
         const int64_t row = w * M + a, target = targets[row];
         const bool ignored = target < 0;
-        const float l = target >= V ? __uint_as_float(0x7fc00000u) : lse[row], scale = ignored ? 0.f : dloss[row];
+        const float l = target >= V ? __uint_as_float(0x7fc00000u) : lse[row], scale = ignored ? 0.f : unit == nullptr ? dloss[row] : dloss[row] / unit[w];
         const int64_t hot = target - first - b;
         __nv_bfloat16* to = d + row * pitch + b;
 #pragma unroll
@@ -381,13 +403,14 @@ struct LogitGradients {
     }
 };
 
-// C written out, [b][a] with a contiguous; 0 in the rows of ignored tokens (targets not NULL). Or as a part of a sum
+// C times its worker's unit written out, [b][a] with a contiguous; 0 in the rows of ignored tokens (targets not NULL). Or as a part of a sum
 // (float32, of a split), which may be added to what is there.
 template <typename G>
 struct WriteOut {
     G* out;
     int64_t worker, split, row;
     const int64_t* targets;
+    const float* unit;  // [W]; NULL: 1
     int a_extent, b_extent, add;
     __device__ __forceinline__ void run(const float (&v)[kHalf], int w, int s, int a, int b) const {
         // which of the columns' tokens are ignored: a load beside each store would wait for the store before it
@@ -399,15 +422,16 @@ struct WriteOut {
                 ignored[j] = __ballot_sync(~0u, at < b_extent && targets[(int64_t)w * b_extent + at] < 0);
             }
         const int there = a < a_extent ? b_extent - b : 0;
+        const float one = unit == nullptr ? 1.f : unit[w];
         G* to = out + w * worker + s * split + b * row + a;
         if (sizeof(G) == 4 && add) {  // one addition to each element per launch: the order is that of the launches
 #pragma unroll
             for (int j = 0; j < kHalf; ++j, to += row)
-                if (j < there) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to), "f"(v[j]) : "memory");
+                if (j < there) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to), "f"(v[j] * one) : "memory");
         } else {
 #pragma unroll
             for (int j = 0; j < kHalf; ++j, to += row)
-                if (j < there) *to = from_float<G>(ignored[j / 32] >> j % 32 & 1 ? 0.f : v[j]);
+                if (j < there) *to = from_float<G>(ignored[j / 32] >> j % 32 & 1 ? 0.f : v[j] * one);
         }
     }
 };
@@ -527,6 +551,7 @@ struct Plan {
     int64_t pitch, d;                  // of d, and its bytes
     Splits dx, dweight;
     int64_t dx_parts, dweight_parts;   // bytes; 0: written in place
+    int64_t units;                     // bytes; 0: d is not in units of the workers'
     int64_t forward, backward;         // bytes in all
 };
 
@@ -563,7 +588,8 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
     p.dweight = splits_of(W * tiles_d * ceil_div(std::min(p.words, V), kTileB), ceil_div(M, kStep) * p.d_products.products, (int64_t)W * std::min(p.words, V) * D);
     p.dx_parts = p.dx.count > 1 || p.pieces > 1 ? padded(p.dx.count * rows * D * 4) : 0;
     p.dweight_parts = p.dweight.count > 1 ? padded((int64_t)p.dweight.count * W * std::min(p.words, V) * D * 4) : 0;
-    p.backward = packed + p.weight_columns + p.d + p.dx_parts + p.dweight_parts;
+    p.units = p.d_planes == 1 ? padded(W * 4) : 0;
+    p.backward = packed + p.weight_columns + p.units + p.d + p.dx_parts + p.dweight_parts;
     return p;
 }
 
@@ -776,6 +802,12 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         ws = {at, V * pitch, pitch, (int64_t)W * V * pitch};
         at += plan.weight_columns;
     }
+    float* unit = nullptr;
+    if (plan.units) {
+        unit = reinterpret_cast<float*>(at);
+        at += plan.units;
+        CPDP_TRY(layer_launched(launch_layer(unit_kernel, W, 1024, 0, stream, dloss, targets, M, unit), what));
+    }
     auto* d = reinterpret_cast<__nv_bfloat16*>((reinterpret_cast<uintptr_t>(at) + 31) & ~uintptr_t(31));
     auto* dx_parts = reinterpret_cast<float*>(at + plan.d);
     auto* dweight_parts = reinterpret_cast<float*>(at + plan.d + plan.dx_parts);
@@ -794,7 +826,7 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         p.b_at = first;
         const auto gradients = [&](auto planes) {
             constexpr int P = decltype(planes)::value;
-            return multiply_all<false, false>(x_rows, w_rows, p, LogitGradients<P>{targets, lse, dloss, d, M, plane, plan.pitch, V, first}, stream, what);
+            return multiply_all<false, false>(x_rows, w_rows, p, LogitGradients<P>{targets, lse, dloss, unit, d, M, plane, plan.pitch, V, first}, stream, what);
         };
         CPDP_TRY(plan.d_planes == 1   ? gradients(std::integral_constant<int, 1>{})
                  : plan.d_planes == 2 ? gradients(std::integral_constant<int, 2>{})
@@ -805,11 +837,11 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         p.a_k = first;
         if (plan.dx_parts) {
             CPDP_TRY((multiply_all<true, false>(w_columns, d_rows, p,
-                                                WriteOut<float>{dx_parts, M * D, rows * D, D, nullptr, D, (int)M, piece > 0}, stream, what)));
+                                                WriteOut<float>{dx_parts, M * D, rows * D, D, nullptr, unit, D, (int)M, piece > 0}, stream, what)));
         } else {
             const auto write = [&](auto* out) {
                 using G = std::remove_pointer_t<decltype(out)>;
-                return multiply_all<true, false>(w_columns, d_rows, p, WriteOut<G>{out, M * D, 0, D, targets, D, (int)M, 0}, stream, what);
+                return multiply_all<true, false>(w_columns, d_rows, p, WriteOut<G>{out, M * D, 0, D, targets, unit, D, (int)M, 0}, stream, what);
             };
             CPDP_TRY(dtype == CPDP_F32 ? write(static_cast<float*>(dx)) : write(static_cast<__nv_bfloat16*>(dx)));
         }
@@ -818,14 +850,14 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         const int64_t part = (int64_t)words * D;
         if (plan.dweight_parts) {
             CPDP_TRY((multiply_all<true, true>(x_columns, d_columns, p,
-                                               WriteOut<float>{dweight_parts, part, W * part, D, nullptr, D, words, 0}, stream, what)));
+                                               WriteOut<float>{dweight_parts, part, W * part, D, nullptr, unit, D, words, 0}, stream, what)));
             const auto sum = [&](auto* out) { return sum_parts(dweight_parts, p.splits, words, W, D, nullptr, out + (int64_t)first * D, dweight_worker, stream); };
             CPDP_TRY(layer_launched(dweight_dtype == CPDP_F32 ? sum(static_cast<float*>(dweight)) : sum(static_cast<__nv_bfloat16*>(dweight)), what));
         } else {
             const auto write = [&](auto* out) {
                 using G = std::remove_pointer_t<decltype(out)>;
                 return multiply_all<true, true>(x_columns, d_columns, p,
-                                                WriteOut<G>{out + (int64_t)first * D, dweight_worker, 0, D, nullptr, D, words, 0}, stream, what);
+                                                WriteOut<G>{out + (int64_t)first * D, dweight_worker, 0, D, nullptr, unit, D, words, 0}, stream, what);
             };
             CPDP_TRY(dweight_dtype == CPDP_F32 ? write(static_cast<float*>(dweight)) : write(static_cast<__nv_bfloat16*>(dweight)));
         }

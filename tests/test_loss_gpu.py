@@ -151,6 +151,30 @@ def test_several_pieces_of_the_vocabulary_and_splits():
     near(dw[:, words.cuda()], want.cpu(), bound.cpu())
 
 
+@pytest.mark.parametrize("each", [1 / 7, 0.3, 1.0, 1e-20, 3e30])
+def test_a_weight_that_all_tokens_share_is_not_rounded(each):
+    """Logits near 0 over 5,000 words: d of a target is dloss (p - 1) with p at most 1.1 / 5,000, and bfloat16 holds 1 - p as
+    1. So a word that one token has for its target gets -dloss x within p; nothing adds up to more, since another token's
+    share of the word is p x at most."""
+    W, M, D, V = 2, 5, 64, 5000
+    gen = rng(3)
+    x, weight = normal(gen, W, M, D).bfloat16(), (normal(gen, W, V, D) * 1e-4).bfloat16()
+    targets = torch.arange(M).repeat(W, 1) * 900
+    dloss = torch.full((W, M), each)
+    dloss[1, 0] = 0.0
+    lse = layers.linear_cross_entropy(x.cuda(), weight.cuda(), targets.cuda())[1]
+    dx, dw = layers.linear_cross_entropy_backward(dloss.cuda(), x.cuda(), weight.cuda(), targets.cuda(), lse)
+    share = 1.1 / V
+    got = dw.cpu().double().gather(1, targets[..., None].expand(W, M, D))
+    size = x.double().abs().sum(1, keepdim=True)
+    assert ((got + dloss.double()[..., None] * x.double()).abs() <= 1.001 * each * share * size).all()
+    want = ref.loss_backward(dloss, x, weight, targets)[0]
+    # 1 - p held as 1, the other p rounded, and the sum of V products
+    most, every = weight.double().abs().amax(1, keepdim=True), weight.double().abs().sum(1, keepdim=True)
+    bound = each * share * (most + 2.0 ** -8 * every) + ref.product_bound(each * (most + share * every), V, BF16)
+    near(dx, want, bound.expand(W, M, D))
+
+
 def test_gradients_against_differences():
     W, M, D, V = 2, 37, 24, 90
     x, weight, targets, dloss = problem((W, M, D, V), F32, 9)
