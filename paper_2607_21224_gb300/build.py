@@ -57,8 +57,8 @@ def build_library(force: bool = False, verbose: bool = False, checked: bool = Fa
     report (registers, spills, shared memory per kernel) goes to _build/ptxas.txt.
     With `checked`, the debug build libcpdp_checked.so instead (-DCPDP_CHECKED:
     every index of the optimizer and reconcile kernels is checked against its
-    buffer's extent, and a weight gradient's copy can be left out; report in
-    _build/ptxas_checked.txt)."""
+    buffer's extent, and a copy of the weight gradient or of the loss can be left
+    out; report in _build/ptxas_checked.txt)."""
     out = CHECKED_LIBRARY if checked else LIBRARY
     if not force and not is_stale(out):
         return out
