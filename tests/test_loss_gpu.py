@@ -175,6 +175,27 @@ def test_a_weight_that_all_tokens_share_is_not_rounded(each):
     near(dx, want, bound.expand(W, M, D))
 
 
+@pytest.mark.parametrize("M", [8192, 8193, 30001])
+def test_weights_of_many_tokens(M):
+    """The largest weight of a worker may be any token's; a worker whose weights are all 0, and infinite and NaN ones of
+    ignored tokens."""
+    W, D, V = 3, 8, 4100
+    gen = rng(M)
+    x, weight = normal(gen, W, M, D, dtype=BF16), normal(gen, W, V, D, std=0.3, dtype=BF16)
+    targets = torch.randint(0, V, (W, M), generator=gen)
+    targets[:, 5:7] = -1
+    dloss = torch.rand((W, M), generator=gen) * 1e-3
+    dloss[0, M - 1], dloss[1] = 37.0, 0.0
+    dloss[:, 5], dloss[:, 6] = float("inf"), float("nan")
+    lse = layers.linear_cross_entropy(x.cuda(), weight.cuda(), targets.cuda())[1]
+    dx, dw = layers.linear_cross_entropy_backward(dloss.cuda(), x.cuda(), weight.cuda(), targets.cuda(), lse)
+    assert (dx[1] == 0).all() and (dw[1] == 0).all() and torch.isfinite(dw).all()
+    rows = torch.tensor([0, 5, 6, 100, 8191, M - 1])
+    dloss[:, 5:7] = 0.0
+    g = ref.loss_backward(dloss[:, rows], x[:, rows], weight, targets[:, rows])
+    near(dx[:, rows.cuda()], g[0], g[2])
+
+
 def test_gradients_against_differences():
     W, M, D, V = 2, 37, 24, 90
     x, weight, targets, dloss = problem((W, M, D, V), F32, 9)
