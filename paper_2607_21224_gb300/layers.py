@@ -592,7 +592,7 @@ def _per_worker(B: int, weight, name: str, dims: int) -> int:
     """The number of workers whose weights these are; their sequences are neighbours."""
     if weight.dim() != dims:
         raise ValueError(f"{name} must have {dims} axes, the workers' first; got {tuple(weight.shape)}")
-    W = weight.shape[0]
+    W = _sized(weight, name)[0]
     if W < 1 or B % W:
         raise ValueError(f"{B} sequences are not as many for each of {W} workers")
     return W
@@ -684,7 +684,7 @@ def causal_conv_step(x, weight, bias, state, *, stream=None):
     xs, ws, bs, code = x.stride(), weight.stride(), bias.stride(), _CODES.get(dtype)
     # one test where all is well: a decoding step costs what Python does around it
     if not (stream is None and code is not None and x.is_cuda and device.index == _current_device() and len(shape) == 2 and len(wshape) == 3
-            and wshape[0] > 0 and shape[0] % wshape[0] == 0 and max(shape) <= MAX_SIZE and shape[1] == wshape[1] and xs[-1] == 1
+            and wshape[0] > 0 and shape[0] % wshape[0] == 0 and max(shape) <= MAX_SIZE >= wshape[2] and shape[1] == wshape[1] and xs[-1] == 1
             and weight.dtype is _F32 is bias.dtype and ws[1:] == (wshape[2], 1) and bias.shape == wshape[:2] and bs[1] == 1
             and state.dtype is dtype and state.shape == (shape[0], wshape[2] - 1, shape[1]) and state.is_contiguous()
             and weight.device == device == bias.device == state.device
@@ -827,7 +827,7 @@ def selective_scan_step(u, delta, a_log, b, c, skip, bias, state, z=None, *, str
     # one test where all is well: a decoding step costs what Python does around it
     if not (stream is None and dtype in _CODES and u.is_cuda and device.index == _current_device() and len(shape) == 2 and len(weights) == 3
             and delta.shape == shape and (z is None or z.shape == shape and z.dtype is dtype and z.device == device and not z.requires_grad)
-            and weights[0] > 0 and shape[0] % weights[0] == 0 and max(shape) <= MAX_SIZE and shape[1] == weights[1]
+            and weights[0] > 0 and shape[0] % weights[0] == 0 and max(shape) <= MAX_SIZE >= weights[2] and shape[1] == weights[1]
             and skip.shape == weights[:2] == bias.shape and few == (shape[0], weights[2]) == c.shape and state.shape == (*shape, weights[2])
             and delta.dtype is dtype and b.dtype is dtype and c.dtype is dtype and state.dtype is _F32 and a_log.dtype is _F32
             and skip.dtype is _F32 and bias.dtype is _F32 and ws[1:] == (weights[2], 1) and us[1] == ds[1] == zs[1] == bs[1] == cs[1] == ks[1] == os[1] == 1
@@ -865,7 +865,7 @@ def clip_gradients(grads, max_norm: float, *, out=None, stream=None):
     shape, dtype, device, gs, os = grads.shape, grads.dtype, grads.device, grads.stride(), out.stride()
     code = _CODES.get(dtype)
     # one test where all is well: a small model's rows cost what Python does around them
-    if not (stream is None and code is not None and grads.is_cuda and device.index == _current_device() and len(shape) == 2
+    if not (stream is None and code is not None and grads.is_cuda and device.index == _current_device() and len(shape) == 2 and shape[0] <= MAX_SIZE
             and out.shape == shape and out.dtype is dtype and out.device == device and gs[1] == 1 == os[1]
             and not (grads.requires_grad or out.requires_grad)):
         _no_autograd(grads=grads, out=out)
@@ -874,6 +874,8 @@ def clip_gradients(grads, max_norm: float, *, out=None, stream=None):
                 return clip_gradients(grads, max_norm, out=out)
         if grads.dim() != 2:
             raise ValueError(f"grads must be (W, N), or (N,) of one model; got {tuple(shape)}")
+        if shape[0] > MAX_SIZE:
+            raise ValueError(f"grads has an axis of more than {MAX_SIZE} workers: {tuple(shape)}")
         code = _dtype(grads, "grads")
         gs, os = _input(grads, "grads", shape, dtype, device), _input(out, "out", shape, dtype, device)
     W, N = shape

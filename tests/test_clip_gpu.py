@@ -124,7 +124,7 @@ def test_refusals():
             bad()
     for bad in (lambda: layers.clip_gradients(g[None], 1.0), lambda: layers.clip_gradients(g[:, ::2], 1.0),
                 lambda: layers.clip_gradients(g, 1.0, out=g[:2]), lambda: layers.clip_gradients(g.clone().requires_grad_(), 1.0),
-                lambda: layers.clip_gradients(g.cpu(), 1.0)):
+                lambda: layers.clip_gradients(g.cpu(), 1.0), lambda: layers.clip_gradients(torch.empty(2 ** 32 + 1, 0, device="cuda"), 1.0)):
         with pytest.raises(ValueError):
             bad()
     for bad in (lambda: layers.clip_gradients(g, 0.0), lambda: layers.clip_gradients(g, float("nan")), lambda: layers.clip_gradients(g, -1.0),

@@ -145,6 +145,8 @@ def test_axes_beyond_the_arguments_are_refused():
     x, w, t = torch.zeros(1, 1, 1), torch.zeros(1).expand(1, 2 ** 32 + 5, 1), torch.zeros(1, 1, dtype=torch.int64)
     with pytest.raises(ValueError, match="axis"):
         layers._head(x, w, t)
+    with pytest.raises(ValueError, match="axis"):
+        layers._per_worker(1, torch.zeros(1).expand(1, 1, 2 ** 32 + 4), "weight", 3)
 
 
 def differences(f, tensors, gradients, gen, h=1e-6):
