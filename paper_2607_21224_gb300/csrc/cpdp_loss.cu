@@ -282,11 +282,11 @@ struct RowSums {
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) top[j % 4] = fmaxf(top[j % 4], j < there ? v[j] : -INFINITY);
         const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-        const float shift = isinf(most) ? 0.f : -most * kLog2e;  // an infinite one leaves infinity or 0, as the formula has it
+        const float base = isinf(most) ? 0.f : most;  // an infinite one leaves infinity or 0, as the formula has it
         float sum[4] = {};
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) {
-            const float e = power(fmaf(v[j], kLog2e, shift));
+            const float e = power((v[j] - base) * kLog2e);  // the difference first: 1 for the largest itself, however large
             sum[j % 4] += j < there ? e : 0.f;
         }
         const bool real = a < M;

@@ -126,6 +126,17 @@ def test_all_logits_far_from_zero(V, level):
     near(lse, f["lse"], f["else"])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_one_word(dtype):
+    """Its probability is 1 whatever the logit: the loss and both gradients are 0."""
+    gen = rng(2)
+    x, weight = normal(gen, 3, 50, 40, std=9.0, dtype=dtype).cuda(), normal(gen, 3, 1, 40, std=3.0, dtype=dtype).cuda()
+    targets = torch.zeros(3, 50, dtype=torch.int64, device="cuda")
+    loss, lse = layers.linear_cross_entropy(x, weight, targets)
+    dx, dw = layers.linear_cross_entropy_backward(torch.ones_like(loss), x, weight, targets, lse)
+    assert (loss == 0).all() and (lse != 0).all() and (dx == 0).all() and (dw == 0).all()
+
+
 def test_several_pieces_of_the_vocabulary_and_splits():
     """More probabilities than are held at a time, a last piece of another size, and long sums split among blocks. The
     gradients of rows and words picked out are compared."""
