@@ -208,10 +208,10 @@ cpdp_status cpdp_gated_recurrence_step(const void *gate, int64_t gate_seq, const
  *            ignored: its loss is 0 (lse is not). Where it is V or more its loss
  *            is NaN.
  *   loss, lse  float32 [W][M]
- * The logits are float32 sums and stay on the chip. float32 operands are split
- * into three bfloat16 parts each, and products below 2^-24 of the largest part's
- * are left out; an infinite operand gives NaN there where the formula has an
- * infinity. M and V are at most 2^30; W * V and the elements of [W][M][V] are
+ * The logits are float32 sums and stay on the chip. float32 operands of more than
+ * 24 tokens are split into three bfloat16 parts each, and products below 2^-24 of
+ * the largest part's are left out; an infinite operand gives NaN there where the
+ * formula has an infinity. M and V are at most 2^30; W * V and the elements of [W][M][V] are
  * bounded as those of an array.
  */
 size_t cpdp_linear_cross_entropy_workspace(const void *x, int64_t x_worker, int64_t x_row,
@@ -232,8 +232,10 @@ cpdp_status cpdp_linear_cross_entropy(const void *x, int64_t x_worker, int64_t x
  *            and lse reach nothing, infinite and NaN ones included
  *   dweight  dweight_dtype, worker w's [V][D] at dweight + w * dweight_worker
  * For bfloat16 operands d is rounded to bfloat16, in units of its worker's largest
- * finite |dloss| (up to 4,096 words to two of them, 16 bits); sums are float32, in an order fixed by the sizes, by whether
- * weight is read in place (16-byte pieces), and by the type.
+ * finite |dloss| (up to 4,096 words to two of them, 16 bits); float32 operands are
+ * split into three parts for any number of tokens. Sums are float32, in an order
+ * fixed by the sizes, by whether weight is read in place (16-byte pieces), and by
+ * the type.
  */
 size_t cpdp_linear_cross_entropy_backward_workspace(const void *x, int64_t x_worker, int64_t x_row,
                                                     const void *weight, int64_t weight_worker, int64_t weight_row,

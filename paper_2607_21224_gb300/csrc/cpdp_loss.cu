@@ -303,6 +303,88 @@ struct RowSums {
     }
 };
 
+// The same for float32 operands and few tokens, where making the planes of weight takes longer than all else: sums of
+// float32 products. A block takes 128 words and kTokens tokens; its warps 8 words at a time, lanes side by side along the
+// features, V of them together per lane. Up to 8 tokens it is bound by reading weight (seven workers' 4 tokens, 3,840 features,
+// 3,589 words: 97 us for 368 with planes), then by the multiplications and x's loads (six workers' 19 tokens, 2,176
+// features, 9,310 words: 251 for 448). At 32 tokens, 1,024 features and 32,768 words it takes 115 us for 126, at 771 features,
+// off 16 bytes, and 10,007 words of two workers 90 for 82: the limit lies below that.
+constexpr int kFewTokens = 24, kTokens = 8, kWordsAtOnce = 8;
+// A step of the sums over lanes: half of the 2 HALF sums that are left go to the lane HALF / 2 away. Where the rest begins.
+template <int HALF>
+__device__ __forceinline__ int hand_over(float (&sum)[kWordsAtOnce * kTokens], int lane) {
+    const bool high = lane & HALF / 2;
+#pragma unroll
+    for (int k = 0; k < HALF; ++k) {
+        const float send = high ? sum[k] : sum[k + HALF], keep = high ? sum[k + HALF] : sum[k];
+        sum[k] = keep + __shfl_xor_sync(~0u, send, HALF / 2);
+    }
+    return high ? HALF : 0;
+}
+template <int V>
+__global__ void __launch_bounds__(256, 2)
+few_tokens_kernel(const float* x, int64_t x_worker, int64_t x_row, const float* weight, int64_t weight_worker, int64_t weight_row,
+                  const int64_t* targets, int M, int words, int D, float2* parts, float* chosen, int64_t rows) {
+    layer_begin();
+    __shared__ float logits[kTokens][kHalf + 1];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, w = blockIdx.z, first = blockIdx.y * kTokens, b = blockIdx.x * kHalf;
+    const float* xs[kTokens];
+#pragma unroll
+    for (int j = 0; j < kTokens; ++j) xs[j] = x + w * x_worker + min(first + j, M - 1) * x_row;
+    for (int at = warp * 16; at < warp * 16 + 16 && b + at < words; at += kWordsAtOnce) {
+        const float* ws[kWordsAtOnce];
+#pragma unroll
+        for (int i = 0; i < kWordsAtOnce; ++i) ws[i] = weight + w * weight_worker + min(b + at + i, words - 1) * weight_row;
+        float sum[kWordsAtOnce * kTokens] = {};
+        for (int k = lane * V; k < D; k += 32 * V) {
+            Piece<float, V> v[kWordsAtOnce];
+#pragma unroll
+            for (int i = 0; i < kWordsAtOnce; ++i)
+                if constexpr (V == 1)
+                    v[i].v = 0.f, v[i].load(ws[i] + k, true);
+                else
+                    v[i].load(ws[i] + k);
+#pragma unroll
+            for (int j = 0; j < kTokens; ++j) {
+                float a[V];
+                if constexpr (V == 4) {
+                    const float4 four = *reinterpret_cast<const float4*>(xs[j] + k);
+                    a[0] = four.x, a[1] = four.y, a[2] = four.z, a[3] = four.w;
+                } else {
+                    a[0] = xs[j][k];
+                }
+#pragma unroll
+                for (int i = 0; i < kWordsAtOnce; ++i)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) sum[i * kTokens + j] = fmaf(v[i].get(e), a[e], sum[i * kTokens + j]);
+            }
+        }
+        int mine = hand_over<32>(sum, lane);  // one after another
+        mine += hand_over<16>(sum, lane);
+        mine += hand_over<8>(sum, lane);
+        mine += hand_over<4>(sum, lane);
+        mine += hand_over<2>(sum, lane);  // two are left to a lane
+#pragma unroll
+        for (int k = 0; k < 2; ++k) logits[(mine + k) % kTokens][at + (mine + k) / kTokens] = sum[k];
+    }
+    __syncthreads();
+    const int m = first + warp;  // a warp's token
+    if (m >= M) return;
+    const int64_t row = (int64_t)w * M + m, target = targets[row] - b;
+    const int there = min(words - b, kHalf);
+    float most = -INFINITY, all = 0.f;
+    for (int j = lane; j < there; j += 32) most = fmaxf(most, logits[warp][j]);
+#pragma unroll
+    for (int k = 16; k > 0; k /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, k));
+    const float base = isinf(most) ? 0.f : most;
+    for (int j = lane; j < there; j += 32) all += power((logits[warp][j] - base) * kLog2e);
+#pragma unroll
+    for (int k = 16; k > 0; k /= 2) all += __shfl_xor_sync(~0u, all, k);
+    if (lane > 0) return;
+    if (target >= 0 && target < there) chosen[row] = logits[warp][target];
+    parts[(int64_t)blockIdx.x * rows + row] = make_float2(most == INFINITY ? 0.f : most, all);
+}
+
 // lse and loss of each token from its parts: ROWS tokens per block, whose other threads share the parts.
 template <int ROWS>
 __global__ void __launch_bounds__(256)
@@ -556,6 +638,7 @@ struct Plan {
     int chunk;
     int64_t x_copy, weight_copy;       // bytes of the copies that the tensor copies read; 0: in place
     int64_t weight_columns;            // the same in the backward pass, which takes weight by whole groups of columns too
+    bool few;                          // forward: float32 products, without planes
     int64_t parts, chosen;             // forward
     int words, pieces;                 // of a piece, and how many
     int64_t pitch, d;                  // of d, and its bytes
@@ -585,6 +668,7 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
     const int64_t rows = W * M;
     p.parts = padded(ceil_div(V, kTileB) * 2 * rows * 8);
     p.chosen = padded(rows * 4);
+    if (dtype == CPDP_F32 && M <= kFewTokens) p.x_copy = p.weight_copy = 0, p.few = true;
     p.forward = p.x_copy + p.weight_copy + p.parts + p.chosen;
 
     const int64_t fit = std::max<int64_t>(kPieceBytes / (p.d_planes * 2 * std::max<int64_t>(rows, 1)), kTileB);
@@ -753,10 +837,21 @@ cpdp_status cpdp_linear_cross_entropy(const void* x, int64_t x_worker, int64_t x
     }
     auto* parts = reinterpret_cast<float2*>(at);
     auto* chosen = reinterpret_cast<float*>(at + plan.parts);
-    CUtensorMap a, b;
-    CPDP_TRY(encode(&a, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
-    CPDP_TRY(encode(&b, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileB));
-    CPDP_TRY((multiply_all<false, false>(a, b, product(W, M, V, D, plan.products, plan.chunk), RowSums{targets, parts, chosen, M, rows, V}, stream, what)));
+    if (plan.few) {
+        const auto fours = [&](const void* p, int64_t worker, int64_t row) { return aligned_to(p, 16) && worker % 4 == 0 && row % 4 == 0; };
+        const bool wide = D % 4 == 0 && fours(x, x_worker, x_row) && fours(weight, weight_worker, weight_row);
+        const dim3 grid(static_cast<unsigned>(ceil_div(V, kTileB) * 2), static_cast<unsigned>(ceil_div(M, kTokens)), W);
+        CPDP_TRY(layer_launched(launch_layer(wide ? few_tokens_kernel<4> : few_tokens_kernel<1>, grid, 256, 0, stream, static_cast<const float*>(x),
+                                             x_worker, x_row, static_cast<const float*>(weight), weight_worker, weight_row, targets,
+                                             static_cast<int>(M), V, D, parts, chosen, rows),
+                                what));
+    } else {
+        CUtensorMap a, b;
+        CPDP_TRY(encode(&a, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
+        CPDP_TRY(encode(&b, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileB));
+        CPDP_TRY((multiply_all<false, false>(a, b, product(W, M, V, D, plan.products, plan.chunk), RowSums{targets, parts, chosen, M, rows, V}, stream,
+                                             what)));
+    }
     const auto finish = [&](auto kernel, int each) {
         return launch_layer(kernel, static_cast<unsigned>(ceil_div(rows, each)), 256, 0, stream, static_cast<const float2*>(parts),
                             static_cast<const float*>(chosen), targets, rows, static_cast<int>(ceil_div(V, kTileB) * 2), V, loss, lse);

@@ -2,6 +2,8 @@
 (operators_reference.py): sizes around its tiles, odd widths and unaligned rows,
 ignored and impossible targets, infinities and NaN in ignored rows, pieces of the
 vocabulary, streams and graphs. Tolerances are the references' own bounds."""
+import math
+
 import pytest
 import torch
 
@@ -124,6 +126,38 @@ def test_all_logits_far_from_zero(V, level):
     loss, lse = layers.linear_cross_entropy(x.cuda(), weight.cuda(), targets.cuda())
     near(loss, f["loss"], f["eloss"])
     near(lse, f["lse"], f["else"])
+
+
+@pytest.mark.parametrize("M", [1, 7, 8, 9, 24, 25])
+@pytest.mark.parametrize("D,V", [(4, 1), (3, 127), (128, 128), (200, 129), (132, 391), (1028, 1000), (517, 2049)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_few_tokens(M, D, V, shift):
+    """Float32 products without planes, and the first size with them; rows at 16 bytes and off them."""
+    x, weight, targets, dloss = problem((2, M, D, V), F32, shift)
+    targets[0, 0], targets[1, M - 1] = V - 1, 0
+    each = (V * D + 7) // 4 * 4  # a worker's part, from a multiple of 16 bytes or one element on
+    ws = torch.full((2 * each + 1,), float("nan"), device="cuda").as_strided((2, V, D), (each, D, 1), shift)
+    ws.copy_(weight)
+    xs, ts = x.cuda(), targets.cuda()
+    f = ref.loss(x, weight, targets)
+    loss, lse = layers.linear_cross_entropy(xs, ws, ts)
+    near(loss, f["loss"], f["eloss"])
+    near(lse, f["lse"], f["else"])
+    again = layers.linear_cross_entropy(xs, ws, ts)
+    assert torch.equal(again[0], loss) and torch.equal(again[1], lse)
+    dx, dw, edx, edw = ref.loss_backward(dloss, x, weight, targets)
+    got, got_w = layers.linear_cross_entropy_backward(dloss.cuda(), xs, ws, ts, lse)
+    near(got, dx, edx)
+    near(got_w, dw, edw)
+
+
+def test_few_tokens_with_infinities():
+    """Float32 products keep an infinite word's logit infinite: all other words have the probability 0."""
+    x, weight = torch.ones(1, 3, 8), torch.zeros(1, 300, 8)
+    weight[0, 200, 3] = -float("inf")
+    targets = torch.tensor([[200, 5, -1]])
+    loss, lse = layers.linear_cross_entropy(x.cuda(), weight.cuda(), targets.cuda())
+    assert loss[0, 0] == float("inf") and loss[0, 2] == 0 and (lse - math.log(299)).abs().max() < 1e-5 and abs(float(loss[0, 1]) - math.log(299)) < 1e-5
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
