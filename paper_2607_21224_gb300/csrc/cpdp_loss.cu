@@ -24,14 +24,15 @@ namespace {
 //
 // The tensor core cuts its float32 sums off where others round them, always
 // towards 0: chunks of some steps are summed at a time and added up, rounded to
-// nearest, in the epilogue's registers. 32 steps where the operands are bfloat16;
-// 4 for float32's, which lose 8e-7 of a loss in chunks of 32 and 6e-8 in chunks of
-// 2 (2 x 517 tokens, 771 features, 10,007 words: 534 us in chunks of 4, 56 less in
-// chunks of 32 and 75 more in chunks of 2).
+// nearest, in the epilogue's registers. Chunks of 32 steps lose 3.6e-7 of lse at
+// 2,048 features and, float32 operands, 8e-7 of a loss at 771; chunks of 4 lose
+// 5e-8 and 7e-8, chunks of 2 4e-8 and 6e-8. Forwards (2 x 4,096 tokens, 2,048
+// features, 50,000 words, bfloat16): 1,082 us in chunks of 4, 989 in chunks of 8,
+// 969 in chunks of 32 and 1,397 in chunks of 2.
 constexpr int kTileA = 128, kTileB = 256, kStep = 64, kSlots = 4;
 constexpr int kEpilogueWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kThreads = 10 * 32;
 constexpr int kHalf = kTileB / 2;  // columns of a thread
-constexpr int kChunk = 32, kChunkF32 = 4;  // steps
+constexpr int kChunk = 4;  // steps
 constexpr int kABytes = kTileA * kStep * 2, kBBytes = kTileB * kStep * 2, kSlotBytes = kABytes + kBBytes;
 constexpr int kBlockBytes = kStep * 128;  // 64 columns of an operand that has k as its slow axis
 constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;
@@ -68,7 +69,6 @@ struct Product {
     int a_extent, b_extent;
     int steps;                   // of k, which passes once for each product of planes
     Planes planes;
-    int chunk;                   // steps
     int each;                    // steps of a split
     int a_k, b_k, a_at, b_at;    // where k and the tiles begin in each operand
 };
@@ -195,8 +195,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             for (int64_t i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
                 int first, count;
                 range(tile_of(p, i), first, count);
-                for (int k0 = 0; k0 < count && ok; k0 += p.chunk, ++c) {
-                    const int half = c & 1, end = min(k0 + p.chunk, count);
+                for (int k0 = 0; k0 < count && ok; k0 += kChunk, ++c) {
+                    const int half = c & 1, end = min(k0 + kChunk, count);
                     if (c >= 2) ok = barrier_wait(&taken[half], (c / 2 - 1) & 1, &failed);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     for (int k = k0; k < end && ok; ++k, ++n) {
@@ -230,7 +230,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (count <= 0)
 #pragma unroll
                 for (int j = 0; j < kHalf; ++j) v[j] = 0.f;
-            for (int k0 = 0; k0 < count && ok; k0 += p.chunk, ++c) {
+            for (int k0 = 0; k0 < count && ok; k0 += kChunk, ++c) {
                 const int half = c & 1;
                 ok = __all_sync(~0u, barrier_wait(&summed[half], c / 2 & 1, &failed));
                 if (!ok) break;
@@ -635,7 +635,6 @@ Splits splits_of(int64_t tiles, int64_t steps, int64_t outputs) {
 struct Plan {
     int planes, d_planes;              // of the operands and of d
     Planes products, d_products;       // with the operands, and with d
-    int chunk;
     int64_t x_copy, weight_copy;       // bytes of the copies that the tensor copies read; 0: in place
     int64_t weight_columns;            // the same in the backward pass, which takes weight by whole groups of columns too
     bool few;                          // forward: float32 products, without planes
@@ -660,7 +659,6 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
     p.d_planes = dtype == CPDP_F32 ? kPlanes : V <= kFewWords ? 2 : 1;
     p.products = dtype == CPDP_F32 ? kThreePlanes : kOnePlane;
     p.d_products = dtype == CPDP_F32 ? kThreePlanes : V <= kFewWords ? kTwoOfD : kOnePlane;
-    p.chunk = dtype == CPDP_F32 ? kChunkF32 : kChunk;
     const int64_t pitch = pitch_of(D), packed = padded(p.planes * W * M * pitch * 2);
     p.x_copy = in_place(x, x_worker, x_row, dtype, W, M, D) ? 0 : packed;
     p.weight_copy = in_place(weight, weight_worker, weight_row, dtype, W, V, D) ? 0 : padded(p.planes * W * (int64_t)V * pitch * 2);
@@ -732,12 +730,12 @@ cpdp_status multiply_all(const CUtensorMap& a, const CUtensorMap& b, const Produ
     return layer_launched(e, what);
 }
 
-Product product(int W, int64_t a, int64_t b, int64_t k, const Planes& planes, int chunk, Splits s = {1, 0}) {
+Product product(int W, int64_t a, int64_t b, int64_t k, const Planes& planes, Splits s = {1, 0}) {
     Product p{};
     p.W = W;
     p.tiles_a = static_cast<int>(ceil_div(a, kTileA)), p.tiles_b = static_cast<int>(ceil_div(b, kTileB));
     p.a_extent = static_cast<int>(a), p.b_extent = static_cast<int>(b);
-    p.steps = static_cast<int>(ceil_div(k, kStep)), p.planes = planes, p.chunk = chunk;
+    p.steps = static_cast<int>(ceil_div(k, kStep)), p.planes = planes;
     p.splits = s.count, p.each = s.each > 0 ? s.each : p.steps * planes.products;
     return p;
 }
@@ -849,7 +847,7 @@ cpdp_status cpdp_linear_cross_entropy(const void* x, int64_t x_worker, int64_t x
         CUtensorMap a, b;
         CPDP_TRY(encode(&a, xs.p, D, M, W, plan.planes, xs.row, xs.worker, xs.plane, kTileA));
         CPDP_TRY(encode(&b, ws.p, D, V, W, plan.planes, ws.row, ws.worker, ws.plane, kTileB));
-        CPDP_TRY((multiply_all<false, false>(a, b, product(W, M, V, D, plan.products, plan.chunk), RowSums{targets, parts, chosen, M, rows, V}, stream,
+        CPDP_TRY((multiply_all<false, false>(a, b, product(W, M, V, D, plan.products), RowSums{targets, parts, chosen, M, rows, V}, stream,
                                              what)));
     }
     const auto finish = [&](auto kernel, int each) {
@@ -929,7 +927,7 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         const int64_t plane = rows * plan.pitch;
         CPDP_TRY(encode(&d_rows, d, words, M, W, plan.d_planes, plan.pitch, M * plan.pitch, plane, kTileB));
         CPDP_TRY(encode_columns(&d_columns, d, words, M, W, plan.d_planes, plan.pitch, M * plan.pitch, plane, kTileB));
-        Product p = product(W, M, words, D, plan.products, plan.chunk);
+        Product p = product(W, M, words, D, plan.products);
         p.b_at = first;
         const auto gradients = [&](auto planes) {
             constexpr int P = decltype(planes)::value;
@@ -939,7 +937,7 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
                  : plan.d_planes == 2 ? gradients(std::integral_constant<int, 2>{})
                                       : gradients(std::integral_constant<int, kPlanes>{}));
 
-        p = product(W, D, M, words, plan.d_products, plan.chunk, plan.dx);
+        p = product(W, D, M, words, plan.d_products, plan.dx);
         p.splits = static_cast<int>(ceil_div(p.steps * p.planes.products, p.each));  // a last piece may have fewer words
         p.a_k = first;
         if (plan.dx_parts) {
@@ -953,7 +951,7 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
             CPDP_TRY(dtype == CPDP_F32 ? write(static_cast<float*>(dx)) : write(static_cast<__nv_bfloat16*>(dx)));
         }
 
-        p = product(W, D, words, M, plan.d_products, plan.chunk, plan.dweight);
+        p = product(W, D, words, M, plan.d_products, plan.dweight);
         const int64_t part = (int64_t)words * D;
         if (plan.dweight_parts) {
             CPDP_TRY((multiply_all<true, true>(x_columns, d_columns, p,
