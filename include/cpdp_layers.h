@@ -231,11 +231,10 @@ cpdp_status cpdp_linear_cross_entropy(const void *x, int64_t x_worker, int64_t x
  *   dx       [W][M][D] of dtype; 0 in the rows of ignored tokens, whose x, dloss
  *            and lse reach nothing, infinite and NaN ones included
  *   dweight  dweight_dtype, worker w's [V][D] at dweight + w * dweight_worker
- * For bfloat16 operands d is rounded to bfloat16, in units of its worker's largest
- * finite |dloss| (up to 4,096 words to two of them, 16 bits); float32 operands are
- * split into three parts for any number of tokens. Sums are float32, in an order
- * fixed by the sizes, by whether weight is read in place (16-byte pieces), and by
- * the type.
+ * d is float32, held in three bfloat16 parts that stay below 1 GiB at a time
+ * (or hold 256 words), and float32 operands are split into three parts for any
+ * number of tokens (an infinite dloss gives NaN there too). Sums are float32, in an order fixed by the sizes, by whether
+ * weight is read in place (16-byte pieces), and by the type.
  */
 size_t cpdp_linear_cross_entropy_backward_workspace(const void *x, int64_t x_worker, int64_t x_row,
                                                     const void *weight, int64_t weight_worker, int64_t weight_row,

@@ -54,10 +54,11 @@ struct Planes {
     uint32_t a, b;  // which, four bits each, the first lowest
 };
 constexpr Planes kOnePlane{1, 0, 0}, kThreePlanes{kPlaneProducts, 0x021010u, 0x201100u};  // 00, 10, 01, 11, 20, 02
-// Where the words are few, their probabilities are not small beside 1, and the rounding of d to bfloat16 shows in the
-// gradients (2.5e-3 of dx at 64 words, where rounding dx itself is 1.7e-3). Up to kFewWords d is held in two planes.
-constexpr Planes kTwoOfD{2, 0x00u, 0x10u};
-constexpr int kFewWords = 4096;
+// d, the gradient of the logits, is float32 whatever the operands' type: three planes of it with the one of a bfloat16
+// operand. In one plane, which takes a third of the products' time, it is the whole error of float32 gradients, 2.2e-4
+// of dweight's norm at 512 tokens, 128 features and 8,192 words, and in two 2.5e-6 at 64 words; in three 3.6e-7. (2 x 4,096
+// tokens, 2,048 features, 50,000 words, backwards: 8.7 ms, in one plane 3.4.)
+constexpr Planes kThreeOfD{kPlanes, 0x000u, 0x210u};
 
 #ifdef CPDP_CHECKED
 // A block's step that is never copied, so that waits run out; -1: none. Debug build only.
@@ -422,44 +423,11 @@ finish_rows_kernel(const float2* parts, const float* chosen, const int64_t* targ
     }
 }
 
-// What a worker's dloss are measured in where d is one plane: the largest of them. 1 / M for each token, a mean's, would
-// be off by up to 2^-9 in bfloat16, all gradients by the same factor; in units of itself it is 1. Blocks of 8,192 tokens;
-// where there are several, unit is 0 before. (One block for 2^20 tokens would take a tenth of the products' time at 64
-// features and 5,000 words.)
-constexpr int kUnitTokens = 8192;
-__global__ void __launch_bounds__(1024)
-unit_kernel(const float* dloss, const int64_t* targets, int64_t M, float* unit) {
-    layer_begin();
-    __shared__ float warps[32];
-    float most = 0.f;
-    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < M; i += (int64_t)gridDim.x * 1024) {
-        const float size = fabsf(dloss[blockIdx.y * M + i]);
-        if (targets[blockIdx.y * M + i] >= 0 && isfinite(size)) most = fmaxf(most, size);
-    }
-#pragma unroll
-    for (int k = 16; k > 0; k /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, k));
-    if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = most;
-    __syncthreads();
-    if (threadIdx.x > 0) return;
-    for (int k = 0; k < 32; ++k) most = fmaxf(most, warps[k]);
-    if (gridDim.x == 1)
-        unit[blockIdx.y] = most;
-    else  // numbers from 0 on are in the order of their bits
-        atomicMax(reinterpret_cast<int*>(unit + blockIdx.y), __float_as_int(most));
-}
-__device__ __forceinline__ float unit_of(const float* unit, int w) {
-    const float u = unit == nullptr ? 1.f : unit[w];
-    return u > 0.f ? u : 1.f;
-}
-
-// The gradient of a token's logits, d = dloss (exp(l - lse) - onehot), rounded to
-// bfloat16 (the type of the products' operands) in units of the worker's, or in
-// two or three planes.
-template <int PLANES>
+// The gradient of a token's logits, d = dloss (exp(l - lse) - onehot), in three
+// planes of bfloat16 (the type of the products' operands).
 struct LogitGradients {
     const int64_t* targets;
     const float *lse, *dloss;
-    const float* unit;  // [W]; NULL: 1
     __nv_bfloat16* d;  // [plane][W][M][pitch]
     int64_t M, plane, pitch;
     int V, first;      // the piece's first word
@@ -467,7 +435,7 @@ struct LogitGradients {
         if (a >= M) return;
         const int64_t row = w * M + a, target = targets[row];
         const bool ignored = target < 0;
-        const float l = target >= V ? __uint_as_float(0x7fc00000u) : lse[row], scale = ignored ? 0.f : dloss[row] / unit_of(unit, w);
+        const float l = target >= V ? __uint_as_float(0x7fc00000u) : lse[row], scale = ignored ? 0.f : dloss[row];
         const int64_t hot = target - first - b;
         __nv_bfloat16* to = d + row * pitch + b;
 #pragma unroll
@@ -480,29 +448,31 @@ struct LogitGradients {
             }
             if (b + j < pitch)
 #pragma unroll
-            for (int q = 0; q < PLANES; ++q) {
+            for (int q = 0; q < kPlanes; ++q) {
                 uint32_t v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = cpdp::pack(g[2 * e], g[2 * e + 1]);
                 asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + q * plane + j), "r"(v[0]), "r"(v[1]), "r"(v[2]),
                              "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                              : "memory");
-                if (q + 1 < PLANES)
+                if (q + 1 < kPlanes)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) g[e] -= __bfloat162float(__float2bfloat16_rn(g[e]));
+                    for (int e = 0; e < 16; ++e) {
+                        const float held = __bfloat162float(__float2bfloat16_rn(g[e]));
+                        g[e] = isfinite(held) ? g[e] - held : 0.f;
+                    }
             }
         }
     }
 };
 
-// C times its worker's unit written out, [b][a] with a contiguous; 0 in the rows of ignored tokens (targets not NULL). Or as a part of a sum
+// C written out, [b][a] with a contiguous; 0 in the rows of ignored tokens (targets not NULL). Or as a part of a sum
 // (float32, of a split), which may be added to what is there.
 template <typename G>
 struct WriteOut {
     G* out;
     int64_t worker, split, row;
     const int64_t* targets;
-    const float* unit;  // [W]; NULL: 1
     int a_extent, b_extent, add;
     __device__ __forceinline__ void run(const float (&v)[kHalf], int w, int s, int a, int b) const {
         // which of the columns' tokens are ignored: a load beside each store would wait for the store before it
@@ -514,16 +484,15 @@ struct WriteOut {
                 ignored[j] = __ballot_sync(~0u, at < b_extent && targets[(int64_t)w * b_extent + at] < 0);
             }
         const int there = a < a_extent ? b_extent - b : 0;
-        const float one = unit_of(unit, w);
         G* to = out + w * worker + s * split + b * row + a;
         if (sizeof(G) == 4 && add) {  // one addition to each element per launch: the order is that of the launches
 #pragma unroll
             for (int j = 0; j < kHalf; ++j, to += row)
-                if (j < there) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to), "f"(v[j] * one) : "memory");
+                if (j < there) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(to), "f"(v[j]) : "memory");
         } else {
 #pragma unroll
             for (int j = 0; j < kHalf; ++j, to += row)
-                if (j < there) *to = from_float<G>(ignored[j / 32] >> j % 32 & 1 ? 0.f : v[j] * one);
+                if (j < there) *to = from_float<G>(ignored[j / 32] >> j % 32 & 1 ? 0.f : v[j]);
         }
     }
 };
@@ -633,7 +602,7 @@ Splits splits_of(int64_t tiles, int64_t steps, int64_t outputs) {
 
 // What a call computes from its sizes.
 struct Plan {
-    int planes, d_planes;              // of the operands and of d
+    int planes;                        // of the operands
     Planes products, d_products;       // with the operands, and with d
     int64_t x_copy, weight_copy;       // bytes of the copies that the tensor copies read; 0: in place
     int64_t weight_columns;            // the same in the backward pass, which takes weight by whole groups of columns too
@@ -643,7 +612,6 @@ struct Plan {
     int64_t pitch, d;                  // of d, and its bytes
     Splits dx, dweight;
     int64_t dx_parts, dweight_parts;   // bytes; 0: written in place
-    int64_t units;                     // bytes; 0: d is not in units of the workers'
     int64_t forward, backward;         // bytes in all
 };
 
@@ -656,9 +624,8 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
              int W, int64_t M, int V, int D) {
     Plan p{};
     p.planes = dtype == CPDP_F32 ? kPlanes : 1;
-    p.d_planes = dtype == CPDP_F32 ? kPlanes : V <= kFewWords ? 2 : 1;
     p.products = dtype == CPDP_F32 ? kThreePlanes : kOnePlane;
-    p.d_products = dtype == CPDP_F32 ? kThreePlanes : V <= kFewWords ? kTwoOfD : kOnePlane;
+    p.d_products = dtype == CPDP_F32 ? kThreePlanes : kThreeOfD;
     const int64_t pitch = pitch_of(D), packed = padded(p.planes * W * M * pitch * 2);
     p.x_copy = in_place(x, x_worker, x_row, dtype, W, M, D) ? 0 : packed;
     p.weight_copy = in_place(weight, weight_worker, weight_row, dtype, W, V, D) ? 0 : padded(p.planes * W * (int64_t)V * pitch * 2);
@@ -669,19 +636,18 @@ Plan plan_of(const void* x, int64_t x_worker, int64_t x_row, const void* weight,
     if (dtype == CPDP_F32 && M <= kFewTokens) p.x_copy = p.weight_copy = 0, p.few = true;
     p.forward = p.x_copy + p.weight_copy + p.parts + p.chosen;
 
-    const int64_t fit = std::max<int64_t>(kPieceBytes / (p.d_planes * 2 * std::max<int64_t>(rows, 1)), kTileB);
+    const int64_t fit = std::max<int64_t>(kPieceBytes / (kPlanes * 2 * std::max<int64_t>(rows, 1)), kTileB);
     p.pieces = static_cast<int>(ceil_div(V, fit));
     p.words = static_cast<int>(std::min<int64_t>(ceil_div(ceil_div(V, p.pieces), kTileB) * kTileB, ceil_div(V, kTileB) * kTileB));
     p.pieces = static_cast<int>(ceil_div(V, p.words));
     p.pitch = pitch_of(std::min(p.words, V));
-    p.d = padded(p.d_planes * rows * p.pitch * 2) + 16;  // room to begin at 32 bytes
+    p.d = padded(kPlanes * rows * p.pitch * 2) + 16;  // room to begin at 32 bytes
     const int64_t tiles_d = ceil_div(D, kTileA);
     p.dx = splits_of(W * tiles_d * ceil_div(M, kTileB), ceil_div(std::min(p.words, V), kStep) * p.d_products.products, rows * D);
     p.dweight = splits_of(W * tiles_d * ceil_div(std::min(p.words, V), kTileB), ceil_div(M, kStep) * p.d_products.products, (int64_t)W * std::min(p.words, V) * D);
     p.dx_parts = p.dx.count > 1 || p.pieces > 1 ? padded(p.dx.count * rows * D * 4) : 0;
     p.dweight_parts = p.dweight.count > 1 ? padded((int64_t)p.dweight.count * W * std::min(p.words, V) * D * 4) : 0;
-    p.units = p.d_planes == 1 ? padded(W * 4) : 0;
-    p.backward = packed + p.weight_columns + p.units + p.d + p.dx_parts + p.dweight_parts;
+    p.backward = packed + p.weight_columns + p.d + p.dx_parts + p.dweight_parts;
     return p;
 }
 
@@ -905,14 +871,6 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         ws = {at, V * pitch, pitch, (int64_t)W * V * pitch};
         at += plan.weight_columns;
     }
-    float* unit = nullptr;
-    if (plan.units) {
-        unit = reinterpret_cast<float*>(at);
-        at += plan.units;
-        const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(M, kUnitTokens), kSMs));
-        if (blocks > 1) CPDP_TRY(layer_launched(cudaMemsetAsync(unit, 0, W * sizeof *unit, static_cast<cudaStream_t>(stream)), what));
-        CPDP_TRY(layer_launched(launch_layer(unit_kernel, dim3(blocks, W), 1024, 0, stream, dloss, targets, M, unit), what));
-    }
     auto* d = reinterpret_cast<__nv_bfloat16*>((reinterpret_cast<uintptr_t>(at) + 31) & ~uintptr_t(31));
     auto* dx_parts = reinterpret_cast<float*>(at + plan.d);
     auto* dweight_parts = reinterpret_cast<float*>(at + plan.d + plan.dx_parts);
@@ -925,28 +883,22 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
     for (int piece = 0; piece < plan.pieces; ++piece) {
         const int first = piece * plan.words, words = std::min(plan.words, V - first);
         const int64_t plane = rows * plan.pitch;
-        CPDP_TRY(encode(&d_rows, d, words, M, W, plan.d_planes, plan.pitch, M * plan.pitch, plane, kTileB));
-        CPDP_TRY(encode_columns(&d_columns, d, words, M, W, plan.d_planes, plan.pitch, M * plan.pitch, plane, kTileB));
+        CPDP_TRY(encode(&d_rows, d, words, M, W, kPlanes, plan.pitch, M * plan.pitch, plane, kTileB));
+        CPDP_TRY(encode_columns(&d_columns, d, words, M, W, kPlanes, plan.pitch, M * plan.pitch, plane, kTileB));
         Product p = product(W, M, words, D, plan.products);
         p.b_at = first;
-        const auto gradients = [&](auto planes) {
-            constexpr int P = decltype(planes)::value;
-            return multiply_all<false, false>(x_rows, w_rows, p, LogitGradients<P>{targets, lse, dloss, unit, d, M, plane, plan.pitch, V, first}, stream, what);
-        };
-        CPDP_TRY(plan.d_planes == 1   ? gradients(std::integral_constant<int, 1>{})
-                 : plan.d_planes == 2 ? gradients(std::integral_constant<int, 2>{})
-                                      : gradients(std::integral_constant<int, kPlanes>{}));
+        CPDP_TRY((multiply_all<false, false>(x_rows, w_rows, p, LogitGradients{targets, lse, dloss, d, M, plane, plan.pitch, V, first}, stream, what)));
 
         p = product(W, D, M, words, plan.d_products, plan.dx);
         p.splits = static_cast<int>(ceil_div(p.steps * p.planes.products, p.each));  // a last piece may have fewer words
         p.a_k = first;
         if (plan.dx_parts) {
             CPDP_TRY((multiply_all<true, false>(w_columns, d_rows, p,
-                                                WriteOut<float>{dx_parts, M * D, rows * D, D, nullptr, unit, D, (int)M, piece > 0}, stream, what)));
+                                                WriteOut<float>{dx_parts, M * D, rows * D, D, nullptr, D, (int)M, piece > 0}, stream, what)));
         } else {
             const auto write = [&](auto* out) {
                 using G = std::remove_pointer_t<decltype(out)>;
-                return multiply_all<true, false>(w_columns, d_rows, p, WriteOut<G>{out, M * D, 0, D, targets, unit, D, (int)M, 0}, stream, what);
+                return multiply_all<true, false>(w_columns, d_rows, p, WriteOut<G>{out, M * D, 0, D, targets, D, (int)M, 0}, stream, what);
             };
             CPDP_TRY(dtype == CPDP_F32 ? write(static_cast<float*>(dx)) : write(static_cast<__nv_bfloat16*>(dx)));
         }
@@ -955,14 +907,14 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float* dloss, const void* x
         const int64_t part = (int64_t)words * D;
         if (plan.dweight_parts) {
             CPDP_TRY((multiply_all<true, true>(x_columns, d_columns, p,
-                                               WriteOut<float>{dweight_parts, part, W * part, D, nullptr, unit, D, words, 0}, stream, what)));
+                                               WriteOut<float>{dweight_parts, part, W * part, D, nullptr, D, words, 0}, stream, what)));
             const auto sum = [&](auto* out) { return sum_parts(dweight_parts, p.splits, words, W, D, nullptr, out + (int64_t)first * D, dweight_worker, stream); };
             CPDP_TRY(layer_launched(dweight_dtype == CPDP_F32 ? sum(static_cast<float*>(dweight)) : sum(static_cast<__nv_bfloat16*>(dweight)), what));
         } else {
             const auto write = [&](auto* out) {
                 using G = std::remove_pointer_t<decltype(out)>;
                 return multiply_all<true, true>(x_columns, d_columns, p,
-                                                WriteOut<G>{out + (int64_t)first * D, dweight_worker, 0, D, nullptr, unit, D, words, 0}, stream, what);
+                                                WriteOut<G>{out + (int64_t)first * D, dweight_worker, 0, D, nullptr, D, words, 0}, stream, what);
             };
             CPDP_TRY(dweight_dtype == CPDP_F32 ? write(static_cast<float*>(dweight)) : write(static_cast<__nv_bfloat16*>(dweight)));
         }

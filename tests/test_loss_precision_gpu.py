@@ -52,3 +52,76 @@ def test_losses_of_bfloat16_operands(W, M, D, V):
     loss, lse = layers.linear_cross_entropy(x, weight, targets)
     want = formulas(x, weight, targets, dloss)
     assert off(loss, want[0]) < LOSS_OFF and off(lse, want[1]) < LOSS_OFF
+
+
+# The chunks' 4.6e-7, at a deviation of 0.3 of the logits; lse, which the backward pass takes as float32, is off by up to
+# half a spacing, 2.8e-7 on average between 8 and 16, which is a factor of the token's d; powers and planes by 1e-7 each.
+GRADIENTS_OFF = 1e-6
+# A bfloat16 output that is off by 1e-6 goes to another neighbour than the formula's value with a probability of at most
+# 1e-6 / 2^-8, and is a spacing away then, 2^-7.5 on average.
+BF16_OFF = (1e-6 * 2 ** 8) ** 0.5 * 2 ** -7.5
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("W,M,D,V", [(4, 200, 128, 64), (1, 300, 300, 4096), (1, 300, 300, 4097), (1, 512, 128, 8192), (2, 130, 1027, 20001),
+                                     (1, 2000, 96, 1000)])
+def test_gradients_of_bfloat16_operands(W, M, D, V):
+    x, weight, targets, dloss = operands(W, M, D, V, BF16)
+    lse = layers.linear_cross_entropy(x, weight, targets)[1]
+    dx, dweight = layers.linear_cross_entropy_backward(dloss, x, weight, targets, lse)
+    want = formulas(x, weight, targets, dloss)
+    assert dweight.dtype is F32 and off(dweight, want[3]) < GRADIENTS_OFF
+    narrow = layers.linear_cross_entropy_backward(dloss, x, weight, targets, lse, dtype=BF16)[1]
+    for got, exact in ((dx, want[2]), (narrow, want[3])):
+        assert got.dtype is BF16 and off(got, exact.to(BF16).double()) < BF16_OFF
+
+
+@pytest.mark.gpu
+def test_one_large_gradient_beside_small_ones():
+    """A token whose dloss is 2^40 times the others' takes nothing from their precision."""
+    x, weight, targets, dloss = operands(1, 200, 128, 5000, BF16)
+    dloss[0, 0] = 2.0 ** 40
+    lse = layers.linear_cross_entropy(x, weight, targets)[1]
+    dx = layers.linear_cross_entropy_backward(dloss, x, weight, targets, lse)[0]
+    want = formulas(x, weight, targets, dloss)[2]
+    assert off(dx[:, 1:], want[:, 1:].to(BF16).double()) < BF16_OFF
+
+
+@pytest.mark.gpu
+def test_an_infinite_gradient_follows_the_formula():
+    x, weight, targets, dloss = operands(1, 150, 128, 5000, BF16)
+    targets[0, 7], dloss[0, 7] = 3, float("inf")
+    lse = layers.linear_cross_entropy(x, weight, targets)[1]
+    dx, dweight = layers.linear_cross_entropy_backward(dloss, x, weight, targets, lse)
+    _, _, ex, ew = formulas(x, weight, targets, dloss)
+    assert torch.isnan(ex[0, 7]).all() and torch.isinf(ew).all()  # x has no zeros
+    for got, want in ((dx, ex), (dweight, ew)):
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got[torch.isinf(want)].double(), want[torch.isinf(want)])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("W,M,D,V", [(1, 25, 771, 5000), (2, 200, 300, 4001), (1, 130, 64, 70), (1, 300, 1024, 9000)])
+def test_float32_operands(W, M, D, V):
+    x, weight, targets, dloss = operands(W, M, D, V, F32)
+    loss, lse = layers.linear_cross_entropy(x, weight, targets)
+    got = loss, lse, *layers.linear_cross_entropy_backward(dloss, x, weight, targets, lse)
+    want = formulas(x, weight, targets, dloss)
+    for g, w, most in zip(got, want, (LOSS_OFF, LOSS_OFF, GRADIENTS_OFF, GRADIENTS_OFF)):
+        assert off(g, w) < most
+
+
+def test_a_lost_plane_is_seen():
+    """Three products of two planes each, on the CPU: what they leave out is above the limits."""
+    x, weight, targets, dloss = operands(1, 130, 300, 1000, F32, "cpu")
+
+    def planes(t, count):
+        held = torch.zeros_like(t)
+        for _ in range(count):
+            held = held + (t - held).to(BF16).float()
+        return held
+
+    want = formulas(x, weight, targets, dloss)
+    two = formulas(planes(x, 2), planes(weight, 2), targets, dloss)
+    assert all(off(t, w) > 2 * GRADIENTS_OFF for t, w in zip(two[2:], want[2:]))
+    three = formulas(planes(x, 3), planes(weight, 3), targets, dloss)
+    assert all(off(t, w) < 1e-7 for t, w in zip(three, want))
