@@ -251,15 +251,17 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float *dloss, const void *x
  * gradients, and g * min(1, max_norm / norm).
  *   grads     of dtype, worker w's N values at grads + w * grads_worker, at any
  *             element alignment
- *   max_norm  > 0; infinity: the rows stay as they are
+ *   max_norm  > 0; infinity: every row stays as it is, to the bit, whatever its
+ *             norm
  *   norms     float32 [W]. The sum of squares is float32, in an order fixed by
  *             the sizes and the rows' alignment, and neither overflows nor
  *             vanishes where the norm itself is a float32 number.
  *   out       of dtype, with a worker stride; or grads itself, with the same
  *             stride: rows whose norm is not above max_norm are not written then.
  *             Other rows that overlap those of grads are refused.
- * A row with an infinite value has the norm infinity (0 for the finite values, NaN
- * for the infinite ones), one with a NaN is NaN throughout. W * N is at most 2^40;
+ * A row whose norm is above the float32 range, or that has an infinite value, has
+ * the norm infinity; one with a NaN has the norm NaN. Under a finite max_norm the
+ * first becomes 0 (its infinite values NaN) and the second NaN throughout. W * N is at most 2^40;
  * with N = 0 the norms are 0.
  */
 size_t cpdp_clip_gradients_workspace(int W, int64_t N);

@@ -116,10 +116,13 @@ clip_kernel(const T* grads, int64_t worker, int64_t n, const Squares* parts, int
     for (int i = threadIdx.x; i < count; i += kThreads) s.add(parts[blockIdx.y * count + i]);
     const float norm = norm_of(over_block(s));
     if (blockIdx.x == 0 && threadIdx.x == 0) norms[blockIdx.y] = norm;
-    const float ratio = max_norm / norm, scale = ratio > 1.f ? 1.f : ratio;
+    // an infinite max_norm is above every norm, infinity and NaN too
+    const float ratio = max_norm / norm, scale = ratio > 1.f || isinf(max_norm) ? 1.f : ratio;
     const T* g = grads + blockIdx.y * worker;
     T* to = out + blockIdx.y * out_worker;
-    if (g == to && scale == 1.f) return;
+    const bool keep = scale == 1.f;  // as they lie in memory, whatever NaN's bits
+    if (g == to && keep) return;
+    const auto scaled = [&](T x) { return keep ? x : from_float<T>(to_float(x) * scale); };
     const Row<T> row(g, n);
     constexpr int64_t kTurn = kThreads * kVectors;
     if constexpr (ALIGNED) {
@@ -138,20 +141,25 @@ clip_kernel(const T* grads, int64_t worker, int64_t n, const Squares* parts, int
                 float x[kEach<T>];
 #pragma unroll
                 for (int e = 0; e < kEach<T>; ++e) x[e] = v[k].get(e) * scale;
-                if (at < row.pieces) store_streaming(to + row.head + at * kEach<T>, x);
+                if (at < row.pieces) {
+                    if (keep)
+                        __stcs(reinterpret_cast<decltype(v[k].v)*>(to + row.head + at * kEach<T>), v[k].v);
+                    else
+                        store_streaming(to + row.head + at * kEach<T>, x);
+                }
             }
         }
         if (blockIdx.x == 0 && threadIdx.x < kEach<T>) {
             const int64_t after = row.head + row.pieces * kEach<T> + threadIdx.x;
-            if (threadIdx.x < row.head) to[threadIdx.x] = from_float<T>(to_float(g[threadIdx.x]) * scale);
-            if (after < n) to[after] = from_float<T>(to_float(g[after]) * scale);
+            if (threadIdx.x < row.head) to[threadIdx.x] = scaled(g[threadIdx.x]);
+            if (after < n) to[after] = scaled(g[after]);
         }
     } else {
         const int64_t turns = (n + kThreads - 1) / kThreads;
 #pragma unroll 4
         for (int64_t turn = turns - 1 - blockIdx.x; turn >= 0; turn -= gridDim.x) {
             const int64_t at = turn * kThreads + threadIdx.x;
-            if (at < n) to[at] = from_float<T>(to_float(g[at]) * scale);
+            if (at < n) to[at] = scaled(g[at]);
         }
     }
 }

@@ -856,7 +856,7 @@ def clip_gradients(grads, max_norm: float, *, out=None, stream=None):
     """The norm of each worker's row of grads (W, N), float32 (W,), and the rows
     times min(1, max_norm / norm): written into ``out``, of grads' shape and type,
     or over grads where none is given (rows that are within max_norm are left as
-    they are then). grads float32 or bfloat16; its rows may be slices of longer
+    they are then). An infinite max_norm leaves every row as it is. grads float32 or bfloat16; its rows may be slices of longer
     ones. One model's (N,) is taken too."""
     if grads.dim() == 1:
         return clip_gradients(grads[None], max_norm, out=None if out is None else out[None], stream=stream)[0]
