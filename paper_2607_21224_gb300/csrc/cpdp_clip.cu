@@ -117,12 +117,16 @@ clip_kernel(const T* grads, int64_t worker, int64_t n, const Squares* parts, int
     const float norm = norm_of(over_block(s));
     if (blockIdx.x == 0 && threadIdx.x == 0) norms[blockIdx.y] = norm;
     // an infinite max_norm is above every norm, infinity and NaN too
-    const float ratio = max_norm / norm, scale = ratio > 1.f || isinf(max_norm) ? 1.f : ratio;
+    const float ratio = max_norm / norm;
+    // a ratio near the end of the float32 range would have few bits, or none: 2^112 of it, and the products times 2^-112
+    // (max_norm is below 2^8 then, and what is scaled below 2^120)
+    const bool tiny = ratio < 0x1p-120f && norm < INFINITY;
+    const float scale = ratio > 1.f || isinf(max_norm) ? 1.f : tiny ? max_norm * 0x1p112f / norm : ratio, after_scale = tiny ? 0x1p-112f : 1.f;
     const T* g = grads + blockIdx.y * worker;
     T* to = out + blockIdx.y * out_worker;
     const bool keep = scale == 1.f;  // as they lie in memory, whatever NaN's bits
     if (g == to && keep) return;
-    const auto scaled = [&](T x) { return keep ? x : from_float<T>(to_float(x) * scale); };
+    const auto scaled = [&](T x) { return keep ? x : from_float<T>(to_float(x) * scale * after_scale); };
     const Row<T> row(g, n);
     constexpr int64_t kTurn = kThreads * kVectors;
     if constexpr (ALIGNED) {
@@ -140,7 +144,7 @@ clip_kernel(const T* grads, int64_t worker, int64_t n, const Squares* parts, int
                 const int64_t at = turn * kTurn + k * kThreads + threadIdx.x;
                 float x[kEach<T>];
 #pragma unroll
-                for (int e = 0; e < kEach<T>; ++e) x[e] = v[k].get(e) * scale;
+                for (int e = 0; e < kEach<T>; ++e) x[e] = v[k].get(e) * scale * after_scale;
                 if (at < row.pieces) {
                     if (keep)
                         __stcs(reinterpret_cast<decltype(v[k].v)*>(to + row.head + at * kEach<T>), v[k].v);

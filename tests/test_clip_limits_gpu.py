@@ -3,7 +3,9 @@ from the norms'."""
 import pytest
 import torch
 
+import operators_reference as ref
 from paper_2607_21224_gb300 import layers
+from test_layers_gpu import near
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -33,3 +35,16 @@ def test_an_infinite_limit_leaves_every_row_as_it_is(N, shift, to, dtype):
     again = layers.clip_gradients(g, float("inf"))
     assert torch.equal(bits(again), bits(norms)) and torch.equal(bits(rows), bits(before))
     assert N == 1 or torch.isinf(norms[4])
+
+
+@pytest.mark.parametrize("most", [1.0, 1e-3, 1e-10, 1e-25])
+@pytest.mark.parametrize("size", [1e35, 1e36, 3e36])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,to", [(2001, 0), (2000, 1)])
+def test_limits_that_are_tiny_beside_the_norm(size, most, N, to, dtype):
+    """Ratios from 2e-37 down to 7e-64, where float32 has few bits (below 1.2e-38) or none (below 1.4e-45)."""
+    g = (torch.randn(2, N, generator=torch.Generator().manual_seed(5)) * size).to(dtype)
+    norms, out, enorms, eout = ref.clip(g, most)
+    got = torch.full((2, N + 8), 7.0, dtype=dtype, device="cuda")
+    near(layers.clip_gradients(g.cuda(), most, out=got[:, to:to + N]), norms, enorms, F32)
+    near(got[:, to:to + N], out, eout + 2.0 ** -133)
