@@ -174,6 +174,12 @@ __device__ __forceinline__ Pair decay_of(Pair dt, Pair A) {
     const float2 x = floats(fma2(dt, A, twice(kPowerBias)));
     return pair(power_of_minus(-x.x), power_of_minus(-x.y));
 }
+// A of a state's a_log, without the sign. Above 88.7 exp leaves float32; the largest number stands in there, which leaves
+// no state where dt is not 0, and 1 of it, not NaN, where dt is 0 (below 2^-126, or behind the last step).
+__device__ __forceinline__ float rate_of(float a_log) {
+    const float r = kLog2eHigh * expf(a_log);
+    return isinf(r) ? 3.40282347e38f : r;
+}
 __device__ __forceinline__ Pair shuffle(Pair v, int mask) { return __shfl_xor_sync(~0u, v, mask); }
 
 struct Task {
@@ -295,7 +301,7 @@ __device__ __forceinline__ void rates(const Scan& s, const Lane<X>& l, int b, in
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int n = 4 * l.q + (turned ? j ^ l.turn : j);
-                x[i][j] = d + i < s.D && n < s.N ? -kLog2eHigh * expf(x[i][j]) : 0.f;  // 0: a state that stays 0
+                x[i][j] = d + i < s.D && n < s.N ? -rate_of(x[i][j]) : 0.f;  // 0: a state that stays 0
             }
         }
 #pragma unroll
@@ -945,7 +951,7 @@ scan_step_kernel(Scan s, float* h, T* y) {
         for (int j = 0; j < 4; ++j) {
             const int n = 4 * q + j;
             if (n < s.N) {
-                const float decay = power_of_minus(dt * (kLog2eHigh * expf(a[n])));
+                const float decay = power_of_minus(dt * rate_of(a[n]));
                 const float vb = to_float(static_cast<const T*>(s.b.p)[b * s.b.seq + n]), vc = to_float(static_cast<const T*>(s.c.p)[b * s.c.seq + n]);
                 const float next = fmaf(decay, state[n], x * vb);
                 state[n] = next;
