@@ -63,3 +63,19 @@ def test_steps_of_no_size_leave_the_state(T):
     assert torch.equal(last.cpu(), h0) and torch.equal(carry[:, -1].cpu(), h0)
     dh0 = layers.selective_scan_backward(torch.zeros_like(y), *xs, carry, z.cuda(), dlast.cuda())[8]
     assert torch.equal(dh0.cpu(), dlast)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [3, 8, 16, 29])
+def test_steps_move_states_as_a_pass_does(N, dtype):
+    """To the bit: what single steps lose of slow states is what a pass loses."""
+    T = 100
+    tensors, (z, h0, _, _, _) = inputs((1, 3, T, 50, N), dtype, False, 7)
+    u, delta, a_log, b, c, skip, bias = on_gpu(tensors, "plain")
+    _, last, carry = layers.selective_scan(u, delta, a_log, b, c, skip, bias, h0=h0.cuda())
+    state = h0.cuda()
+    for t in range(T):
+        if t % layers.CARRY_STEPS == 0:
+            assert torch.equal(state, carry[:, t // layers.CARRY_STEPS])
+        layers.selective_scan_step(u[:, t], delta[:, t], a_log, b[:, t], c[:, t], skip, bias, state)
+    assert torch.equal(state, last)
