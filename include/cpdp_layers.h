@@ -372,7 +372,8 @@ typedef struct cpdp_scan_inputs {
  *            before steps 0, CPDP_CARRY_STEPS, ..., for the backward pass
  *            (defined up to each sequence's length)
  * States and sums are float32. A decay x = exp(-p) is off by at most
- * (2 + 2 p) 2^-23 of it. An exp(a_log) above the float32 range counts as its end:
+ * (2 + 2 p) 2^-23 of it; one across a segment of a split sequence, whose dt are
+ * summed first, by (2 + 10 p) 2^-23. An exp(a_log) above the float32 range counts as its end:
  * a step of no size (dt of 0) leaves the state, any other forgets it. Where dt, u, z, b or c is infinite, an output may be NaN
  * that the formula has infinite. B * T * D is at most 2^34.
  */

@@ -79,3 +79,26 @@ def test_steps_move_states_as_a_pass_does(N, dtype):
             assert torch.equal(state, carry[:, t // layers.CARRY_STEPS])
         layers.selective_scan_step(u[:, t], delta[:, t], a_log, b[:, t], c[:, t], skip, bias, state)
     assert torch.equal(state, last)
+
+
+def test_decays_across_long_segments():
+    """600 columns of 24,000 equal steps, in segments of 8,000: a segment's decay is that of its summed step sizes. The
+    half of the steps that the walk comes to last is of no size, so that the result is made of segments' decays alone."""
+    B, T, D = 600, 24000, 32
+    delta = torch.empty(D).uniform_(-6, 0, generator=torch.Generator().manual_seed(1))
+    dt = torch.log1p(torch.exp(delta.double()))
+    a_log = (2 / (dt * (T // 2))).log().float()  # exp(-2) of a state is left
+    want = torch.exp(-torch.exp(a_log.double()) * dt * (T // 2))
+    p = -want.log()
+    # of three segments' decays: dt's own error, sums of 16 steps rounded at most 15 times, each decay's
+    bound = want * (p * (24 + 4 * delta.double().abs()) * U32 + (3 * 2 + 10 * p) * 2 * U32)
+    early = torch.full((1, T, D), -300.0)
+    early[0, : T // 2] = delta
+    zero = torch.zeros(1, 1, D, device="cuda").expand(B, T, D)
+    weights = dict(a_log=a_log.cuda()[None, :, None], skip=torch.zeros(1, D, device="cuda"), bias=torch.zeros(1, D, device="cuda"))
+    few, one = zero[..., :1], torch.ones(B, D, 1, device="cuda")
+    last = layers.selective_scan(zero, early.cuda().expand(B, T, D), b=few, c=few, h0=one, carry=False, **weights)[1]
+    assert ((last[..., 0].double().cpu() - want).abs() <= bound).all()
+    carry = torch.zeros(B, T // layers.CARRY_STEPS, D, 1, device="cuda")
+    dh0 = layers.selective_scan_backward(zero, zero, early.flip(1).cuda().expand(B, T, D), b=few, c=few, carry=carry, dlast=one, **weights)[8]
+    assert ((dh0[..., 0].double().cpu() - want).abs() <= bound).all()
