@@ -48,3 +48,16 @@ def test_limits_that_are_tiny_beside_the_norm(size, most, N, to, dtype):
     got = torch.full((2, N + 8), 7.0, dtype=dtype, device="cuda")
     near(layers.clip_gradients(g.cuda(), most, out=got[:, to:to + N]), norms, enorms, F32)
     near(got[:, to:to + N], out, eout + 2.0 ** -133)
+
+
+@pytest.mark.parametrize("dtype,N", [(F32, 11000003), (BF16, 22000005)])
+@pytest.mark.parametrize("W", [3, 5])
+def test_a_last_group_of_fewer_rows(W, N, dtype):
+    """Rows of 44 MB pass two at a time."""
+    gen = torch.Generator(device="cuda").manual_seed(W)
+    g = torch.empty(W, N, device="cuda").normal_(0.0, 1.0, generator=gen)
+    g = (g * torch.tensor([0.5, 40.0, 1.0, 3.0, 7.0], device="cuda")[:W, None] / N ** 0.5).to(dtype)
+    norms, out, enorms, eout = ref.clip(g, 1.0)
+    for to in (torch.empty_like(g), g):
+        near(layers.clip_gradients(g, 1.0, out=to), norms.cpu(), enorms.cpu(), F32)
+        assert ((to.double() - out).abs() <= eout + ref.rounding(out, dtype)).all()

@@ -110,6 +110,22 @@ def test_float32_operands(W, M, D, V):
         assert off(g, w) < most
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("W,M,D,V,dtype", [(1, 900, 40, 220001, F32), (2, 450, 70, 200300, BF16)])
+def test_a_vocabulary_in_pieces(W, M, D, V, dtype):
+    """Three parts of d for 900 tokens stay below 1 GiB up to 198,841 words: two pieces, the second off every border."""
+    x, weight, targets, dloss = operands(W, M, D, V, dtype)
+    loss, lse = layers.linear_cross_entropy(x, weight, targets)
+    dx, dweight = layers.linear_cross_entropy_backward(dloss, x, weight, targets, lse)
+    want = formulas(x, weight, targets, dloss)
+    assert off(loss, want[0]) < LOSS_OFF and off(lse, want[1]) < LOSS_OFF
+    half = V // 2 + 1000
+    for part in (slice(0, half), slice(half, V), slice(V - 100, V)):
+        assert off(dweight[:, part], want[3][:, part]) < GRADIENTS_OFF
+    assert off(dx, want[2]) < GRADIENTS_OFF if dtype is F32 else off(dx, want[2].to(BF16).double()) < BF16_OFF
+    assert (dx[targets < 0] == 0).all()
+
+
 def test_a_lost_plane_is_seen():
     """Three products of two planes each, on the CPU: what they leave out is above the limits."""
     x, weight, targets, dloss = operands(1, 130, 300, 1000, F32, "cpu")

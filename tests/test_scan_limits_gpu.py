@@ -102,3 +102,13 @@ def test_decays_across_long_segments():
     carry = torch.zeros(B, T // layers.CARRY_STEPS, D, 1, device="cuda")
     dh0 = layers.selective_scan_backward(zero, zero, early.flip(1).cuda().expand(B, T, D), b=few, c=few, carry=carry, dlast=one, **weights)[8]
     assert ((dh0[..., 0].double().cpu() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(1, 7, 300, 21, 16), (2, 8, 200, 34, 5), (1, 6, 333, 16, 32)])
+def test_sequences_that_end_inside_a_segment(shape, dtype):
+    """Few columns, so that time is split from 128 steps on, with lengths at and around every kind of border."""
+    tensors, (z, h0, _, dy, dlast) = inputs(shape, dtype, False, 8)
+    W, B, T, D, N = shape
+    lengths = torch.tensor([T, 0, 1, 64, 65, 130, 191, T - 1])[:B].to(torch.int32)
+    check(tensors, z, h0, lengths, dy, dlast)
