@@ -562,11 +562,18 @@ pack_kernel(const T* x, int64_t worker, int64_t stride, int64_t rows_each, int64
             }
 #pragma unroll
             for (int q = 0; q < PLANES; ++q) {
-                store_piece<8>(to + q * rows * pitch + k, v);
+                float held[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    // the largest float32 numbers would round to infinity: bfloat16's largest stands in, the next plane holds the rest
+                    const float most = 3.38953139e38f, there = fminf(fmaxf(v[e], -most), most);
+                    held[e] = PLANES > 1 && isfinite(v[e]) ? there : v[e];
+                }
+                store_piece<8>(to + q * rows * pitch + k, held);
                 if (q + 1 < PLANES)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float rest = v[e] - __bfloat162float(__float2bfloat16_rn(v[e]));
+                        const float rest = v[e] - __bfloat162float(__float2bfloat16_rn(held[e]));
                         v[e] = isfinite(v[e]) ? rest : 0.f;
                     }
             }

@@ -111,6 +111,25 @@ def test_float32_operands(W, M, D, V):
 
 
 @pytest.mark.gpu
+def test_the_largest_float32_numbers():
+    """3.4e38 is nearer to 2^128 than to bfloat16's largest number."""
+    x, weight, targets, dloss = operands(1, 60, 100, 300, F32)
+    x[0, :, 0], x[0, 7, 0] = 0, torch.finfo(F32).max
+    weight[0, :, 0] = 0
+    loss, lse = layers.linear_cross_entropy(x, weight, targets)
+    dx, dweight = layers.linear_cross_entropy_backward(dloss * 1e-3, x, weight, targets, lse)
+    want = formulas(x, weight, targets, dloss * 1e-3)
+    assert off(loss, want[0]) < LOSS_OFF and off(lse, want[1]) < LOSS_OFF
+    assert off(dx, want[2]) < GRADIENTS_OFF and off(dweight[..., 0], want[3][..., 0]) < GRADIENTS_OFF
+    assert off(dweight[..., 1:], want[3][..., 1:]) < GRADIENTS_OFF
+    x, weight, targets, dloss = operands(1, 60, 100, 300, F32)  # and as weights
+    weight[0, 5, 0], weight[0, 6, 0] = torch.finfo(F32).max, -torch.finfo(F32).max
+    x[0, :, 0] = 0
+    loss, lse = layers.linear_cross_entropy(x, weight, targets)
+    assert off(loss, formulas(x, weight, targets, dloss)[0]) < LOSS_OFF
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("W,M,D,V,dtype", [(1, 900, 40, 220001, F32), (2, 450, 70, 200300, BF16)])
 def test_a_vocabulary_in_pieces(W, M, D, V, dtype):
     """Three parts of d for 900 tokens stay below 1 GiB up to 198,841 words: two pieces, the second off every border."""
