@@ -67,11 +67,10 @@ __device__ int dropped_step = -1;
 
 struct Product {
     int W, tiles_a, tiles_b, splits;
-    int a_extent, b_extent;
     int steps;                   // of k, which passes once for each product of planes
     Planes planes;
     int each;                    // steps of a split
-    int a_k, b_k, a_at, b_at;    // where k and the tiles begin in each operand
+    int a_k, b_at;               // where k begins in a, and the tiles in b
 };
 
 struct Tile {
@@ -181,8 +180,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(&full[s])), "r"(kSlotBytes) : "memory");
                     const int pass = (first + k) / p.steps, at = (first + k - pass * p.steps) * kStep;
                     const uint32_t slot = slots + s * kSlotBytes;
-                    copy_operand<A_SLOW>(slot, &map_a, p.a_at + t.a * kTileA, p.a_k + at, t.w, p.planes.a >> 4 * pass & 15, &full[s]);
-                    copy_operand<B_SLOW>(slot + kABytes, &map_b, p.b_at + t.b * kTileB, p.b_k + at, t.w, p.planes.b >> 4 * pass & 15,
+                    copy_operand<A_SLOW>(slot, &map_a, t.a * kTileA, p.a_k + at, t.w, p.planes.a >> 4 * pass & 15, &full[s]);
+                    copy_operand<B_SLOW>(slot + kABytes, &map_b, p.b_at + t.b * kTileB, at, t.w, p.planes.b >> 4 * pass & 15,
                                                  &full[s]);
                 }
             }
@@ -707,7 +706,6 @@ Product product(int W, int64_t a, int64_t b, int64_t k, const Planes& planes, Sp
     Product p{};
     p.W = W;
     p.tiles_a = static_cast<int>(ceil_div(a, kTileA)), p.tiles_b = static_cast<int>(ceil_div(b, kTileB));
-    p.a_extent = static_cast<int>(a), p.b_extent = static_cast<int>(b);
     p.steps = static_cast<int>(ceil_div(k, kStep)), p.planes = planes;
     p.splits = s.count, p.each = s.each > 0 ? s.each : p.steps * planes.products;
     return p;

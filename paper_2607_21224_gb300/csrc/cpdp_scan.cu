@@ -190,11 +190,6 @@ __device__ __forceinline__ void add_up(Pair& sum, Pair& lost, Pair x) {
 }
 __device__ __forceinline__ Pair shuffle(Pair v, int mask) { return __shfl_xor_sync(~0u, v, mask); }
 
-struct Task {
-    int64_t column;
-    int b, first_channel, order, group;
-};
-
 // The lane's place in the walk: states 4 q .. 4 q + 3 of C channels, pairs and states in an order of the lane's own, so
 // that what a sum between lanes keeps and what it sends lie in the same registers of every lane.
 template <typename X>
