@@ -4,8 +4,8 @@ one GPU, and the trained model generates tokens.
 Every worker's layers run in the same calls (paper_2607_21224_gb300.layers); the
 products between them are torch.bmm. Weights are views into ``CPDPState.params``
 and the backward pass writes its gradients straight into the [W][N] gradient
-buffer that ``CPDPState.step`` takes. What the backward pass needs of the
-activations is held in 8 bits.
+buffer that ``CPDPState.step`` takes. The inputs of the blocks' products are held
+in 8 bits for their weight gradients, the head's input and the rest in bfloat16.
 
 The model: an embedding, blocks of (norm, product, mixer, product) on a residual
 stream, a norm and a head, whose loss is taken without the logits. The mixer is a

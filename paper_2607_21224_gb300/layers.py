@@ -19,8 +19,10 @@ include/cpdp_layers.h, which make the gradients that ``CPDPState`` steps with.
 
 Activations are (W, M, D): W workers, M tokens each, D features, contiguous
 along D, float32 or bfloat16. One model's (M, D) is taken too, with a weight
-(D,). Weights are float32 and may be slices of ``CPDPState.params``, and weight
-gradients are written into slices of the [W][N] gradient buffer::
+(D,). Weights are float32 and may be slices of ``CPDPState.params`` (the head's,
+which the loss takes, has the activations' type instead: a bfloat16 model casts
+its slice), and weight gradients are written into slices of the [W][N] gradient
+buffer::
 
     weight = st.params[:, a:a + D]                          # (W, D)
     y, s, saved = layers.add_rmsnorm(x, weight, residual, checkpoint=True)
