@@ -231,10 +231,12 @@ cpdp_status cpdp_linear_cross_entropy(const void *x, int64_t x_worker, int64_t x
  *   dx       [W][M][D] of dtype; 0 in the rows of ignored tokens, whose x, dloss
  *            and lse reach nothing, infinite and NaN ones included
  *   dweight  dweight_dtype, worker w's [V][D] at dweight + w * dweight_worker
- * d is float32, held in three bfloat16 parts that stay below 1 GiB at a time
- * (or hold 256 words), and float32 operands are split into three parts for any
- * number of tokens (an infinite dloss gives NaN there too). Sums are float32, in an order fixed by the sizes, by whether
- * weight is read in place (16-byte pieces), and by the type.
+ * d is float32, held in three bfloat16 parts (what of it is below 2^-133 counts
+ * as 0) that stay below 1 GiB at a time or hold 256 words. float32 operands are
+ * split into three parts for any number of tokens, where an infinite dloss or
+ * operand gives NaN in the place of an infinity. Sums are float32, in an order
+ * fixed by the sizes, by whether weight is read in place (16-byte pieces), and by
+ * the type.
  */
 size_t cpdp_linear_cross_entropy_backward_workspace(const void *x, int64_t x_worker, int64_t x_row,
                                                     const void *weight, int64_t weight_worker, int64_t weight_row,
@@ -261,8 +263,8 @@ cpdp_status cpdp_linear_cross_entropy_backward(const float *dloss, const void *x
  *             Other rows that overlap those of grads are refused.
  * A row whose norm is above the float32 range, or that has an infinite value, has
  * the norm infinity; one with a NaN has the norm NaN. Under a finite max_norm the
- * first becomes 0 (its infinite values NaN) and the second NaN throughout. W * N is at most 2^40;
- * with N = 0 the norms are 0.
+ * first becomes 0 (its infinite values NaN) and the second NaN throughout. W * N is
+ * at most 2^40; with N = 0 the norms are 0.
  */
 size_t cpdp_clip_gradients_workspace(int W, int64_t N);
 cpdp_status cpdp_clip_gradients(const void *grads, int64_t grads_worker, cpdp_dtype dtype, int W, int64_t N,
